@@ -72,6 +72,7 @@ enum sfb_error {
 #define SFB_STATUS_LABEL_RANGE 0x1u
 #define SFB_STATUS_TIMEOUT     0x2u
 #define SFB_STATUS_SAMPLE_RANGE 0x4u   /* SDCA: a sample id outside [0, sdca_n) was skipped */
+#define SFB_STATUS_ADAPTER_RANGE 0x10u /* an adapter id outside [-1, adapters): the sample took none */
 #define SFB_STATUS_INDEX_RANGE 0x8u    /* sparse samples: a column index outside [0, cols), or row pointers that do not
                                           describe the stated number of entries; the entry or the sample was skipped */
 
@@ -327,6 +328,77 @@ int sfb_get_update_form(sfb_ctx* ctx, int32_t* form);
  *   parts    that a tile's contraction is cut into in the products 1, 2 and 5 (6: of an iteration; 2 where any is cut); 1 elsewhere
  *   merged   1: the softmax is merged, and the label rows are applied, in one launch (sfb_step of all K) */
 int sfb_get_plan(const sfb_config* cfg, int64_t samples, int32_t* product, int32_t* parts, int32_t* merged);
+
+/* ---- Low-rank adapters of many requests beside the shared W ---------------------------------------------------------
+ * An adapter is a set of `rank` sufficient-factor pairs that stays apart from W: the update of one client, one machine or one
+ * task that was not broadcast (Section 3: W + sum_t u_t v_t^T needs the pairs alone).  Samples of many requests, each with the
+ * adapter that its request names, are answered, and the adapters trained, beside one W that they all share:
+ *   forward    s_i = V[a_i] x_i,                 y_i  = W x_i + scale[a_i] U[a_i]^T s_i
+ *   backward   t_i = U[a_i] dy_i,                dx_i = W^T dy_i + scale[a_i] V[a_i]^T t_i
+ *              dU[a] = scale[a] sum_{i: a_i = a} s_i dy_i^T,   dV[a] = scale[a] sum_{i: a_i = a} t_i x_i^T
+ * a_i = ids_dev[i], -1: no adapter (y_i = W x_i).  An id outside [-1, adapters) sets SFB_STATUS_ADAPTER_RANGE and counts as -1.
+ *
+ *  - W_dev [rows x ldw], U_dev [adapters][rank][ldu], V_dev [adapters][rank][ldv] (pair-major, as the gathered factors are),
+ *    X_dev, dY_dev, Y_dev, dX_dev are bf16, sums fp32; scale_dev [adapters], S_dev [n x rank], dU_dev [adapters][rank][rows] and
+ *    dV_dev [adapters][rank][cols] fp32, the last three without gaps; ids_dev int32.  Every pitch of a bf16 operand is a multiple
+ *    of 8 entries (rows, cols, n and rank are any size), every such pointer 16-byte aligned; scale, S and ids 4-byte aligned.
+ *    The operand copy of W that sfb_get_operand_copy gives (SFB_MLR, bf16 mode) is such a W.
+ *  - What lies behind the last column of a row, or in rows of other samples and adapters, is neither read into a result nor
+ *    written: infinities and NaN in a sample or an adapter reach the results of that sample, or of that adapter's samples, alone.
+ *  - Outputs do not overlap the inputs or one another.
+ *  - The handle borrows W, U, V and scale (training may change their values between calls: nothing derived from them is kept)
+ *    and the workspace.  One handle per stream; calls on one handle are not re-entrant.  n = 0 .. max_samples. */
+typedef struct sfb_adapters sfb_adapters;
+#define SFB_ADAPTER_MAX_RANK 128
+typedef struct sfb_adapter_config {
+  int64_t rows, cols;         /* shape of W                                                            */
+  int64_t ldw, ldu, ldv;      /* row pitches in entries; 0: rows follow one another (cols, rows, cols) */
+  int32_t adapters;           /* 1 .. 65,536                                                           */
+  int32_t rank;               /* pairs per adapter, 1 .. SFB_ADAPTER_MAX_RANK (zeros fill up a smaller one) */
+  int64_t max_samples;        /* of a call                                                             */
+  void*   stream;             /* cudaStream_t                                                          */
+} sfb_adapter_config;
+
+/* Bytes of device workspace of a handle.  Host-only; no CUDA call. */
+int sfb_adapter_workspace_bytes(const sfb_adapter_config* cfg, size_t* out_bytes);
+/* workspace_dev: 1024-byte aligned.  Clears the status word (enqueued). */
+int sfb_adapter_init(const sfb_adapter_config* cfg, const void* W_dev, const void* U_dev, const void* V_dev,
+                     const float* scale_dev, void* workspace_dev, size_t workspace_bytes, sfb_adapters** out);
+/* Y_dev [n x ldy].  S_dev (may be null) receives s_i, which the backward pass takes; zeros for a sample without an adapter. */
+int sfb_adapter_forward(sfb_adapters* h, int64_t n, const void* X_dev, int64_t ldx, const int32_t* ids_dev, void* Y_dev,
+                        int64_t ldy, float* S_dev);
+/* S_dev: what the forward pass gave for these samples; may be null, and is computed again then.  Outputs that are not wanted are
+ * null: dX_dev [n x lddx], dU_dev, dV_dev.  dU and dV are written whole, zeros for adapters without a sample. */
+int sfb_adapter_backward(sfb_adapters* h, int64_t n, const void* dY_dev, int64_t lddy, const void* X_dev, int64_t ldx,
+                         const int32_t* ids_dev, const float* S_dev, void* dX_dev, int64_t lddx, float* dU_dev, float* dV_dev);
+/* As sfb_get_status, sfb_last_cuda_error and sfb_destroy. */
+int sfb_adapter_get_status(sfb_adapters* h, uint32_t* status_out);
+int sfb_adapter_last_cuda_error(sfb_adapters* h);
+int sfb_adapter_destroy(sfb_adapters* h);
+
+/* ---- Global norm of gradients, and clipping -----------------------------------------------------------------------------
+ * The column prox bounds the norm of a column of W; this bounds the norm of a whole step: with the tensors g_1 .. g_m taken as one
+ * vector,
+ *     norm = sqrt(sum_t sum_j g_tj^2),   coef = max_norm / norm where norm > max_norm, else 1,   out_t = coef * g_t.
+ * Squares are summed in fp64, in an order that does not depend on timing.  result_dev[0] = norm, result_dev[1] = coef (fp32).
+ * Where the norm is infinite or not a number, out_t = g_t unscaled and coef = 0 (a multiplier that drops the step).
+ *
+ *  - Tensor t has counts[t] >= 0 entries of dtypes[t] (0 fp32, 1 bf16, 2 fp16) without gaps at src[t], aligned to its entries; dst[t]
+ *    (of the same type) is src[t] itself, or does not overlap any tensor.  dst null: every tensor in place.
+ *  - The handle keeps these addresses (the table is copied to the workspace by sfb_clip_init, which waits for that copy),
+ *    never values.  One handle per stream; calls on one handle are not re-entrant.
+ *  - Gradients that lie on several GPUs: sfb_clip_sum writes this handle's sum of squares to sum_dev (fp64), the caller adds those
+ *    of all ranks, and sfb_clip_scale takes the total.  sfb_clip_gradients is both. */
+typedef struct sfb_clip sfb_clip;
+enum sfb_dtype { SFB_F32 = 0, SFB_BF16 = 1, SFB_F16 = 2 };
+int sfb_clip_workspace_bytes(int64_t tensors, const int64_t* counts, const int32_t* dtypes, size_t* out_bytes);
+int sfb_clip_init(int64_t tensors, const void* const* src, void* const* dst, const int64_t* counts, const int32_t* dtypes,
+                  void* workspace_dev, size_t workspace_bytes, void* stream, sfb_clip** out);
+int sfb_clip_sum(sfb_clip* h, double* sum_dev);
+int sfb_clip_scale(sfb_clip* h, float max_norm, const double* sum_dev, float* result_dev);
+int sfb_clip_gradients(sfb_clip* h, float max_norm, float* result_dev);
+int sfb_clip_last_cuda_error(sfb_clip* h);
+int sfb_clip_destroy(sfb_clip* h);
 
 /* Waits for the stream, then fills the counters. */
 int sfb_get_stats(sfb_ctx* ctx, sfb_stats* out);

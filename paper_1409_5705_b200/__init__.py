@@ -16,6 +16,8 @@ PREC_BF16, PREC_FP32, PREC_TF32X3, PREC_FP32_FFMA = 0, 1, 2, 3
 PROX_NONE, PROX_L1, PROX_L2SQ = 0, 1, 2
 CSR_UPDATE_AUTO, CSR_UPDATE_SPARSE, CSR_UPDATE_DENSE = 0, 1, 2
 STATUS_LABEL_RANGE, STATUS_TIMEOUT, STATUS_SAMPLE_RANGE, STATUS_INDEX_RANGE = 0x1, 0x2, 0x4, 0x8
+STATUS_ADAPTER_RANGE = 0x10
+F32, BF16, F16 = 0, 1, 2
 
 EXPORTS = ("sfb_workspace_bytes", "sfb_init", "sfb_compute_factors", "sfb_gather_factors", "sfb_apply_update",
            "sfb_step", "sfb_step_host", "sfb_dense_sync_step", "sfb_get_factors", "sfb_get_stats",
@@ -23,8 +25,13 @@ EXPORTS = ("sfb_workspace_bytes", "sfb_init", "sfb_compute_factors", "sfb_gather
            "sfb_selftest_wait_timeout", "sfb_set_row_shard", "sfb_forward_partials", "sfb_finish_factors",
            "sfb_replay_update", "sfb_refresh_operands", "sfb_sdca_set_dual", "sfb_sdca_compute_factors",
            "sfb_sdca_step", "sfb_set_factors", "sfb_set_eta", "sfb_get_operand_copy", "sfb_compute_factors_csr",
-           "sfb_step_csr", "sfb_export_factors", "sfb_forward_partials_pairs")
+           "sfb_step_csr", "sfb_export_factors", "sfb_forward_partials_pairs",
+           "sfb_adapter_workspace_bytes", "sfb_adapter_init", "sfb_adapter_forward", "sfb_adapter_backward",
+           "sfb_adapter_get_status", "sfb_adapter_last_cuda_error", "sfb_adapter_destroy",
+           "sfb_clip_workspace_bytes", "sfb_clip_init", "sfb_clip_sum", "sfb_clip_scale", "sfb_clip_gradients",
+           "sfb_clip_last_cuda_error", "sfb_clip_destroy")
 NOALLOC_MAX_COLS = 16384
+ADAPTER_MAX_RANK = 128
 
 
 class sfb_config(ctypes.Structure):
@@ -43,6 +50,12 @@ class sfb_stats(ctypes.Structure):
                 ("ms_gather", ctypes.c_float), ("ms_update", ctypes.c_float), ("last_loss", ctypes.c_float),
                 ("sc_lipschitz", ctypes.c_float), ("kernel_launches", ctypes.c_int64),
                 ("copy_pieces", ctypes.c_int64), ("copy_written", ctypes.c_int64), ("sparse_updates", ctypes.c_int64)]
+
+
+class sfb_adapter_config(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ldw", ctypes.c_int64), ("ldu", ctypes.c_int64),
+                ("ldv", ctypes.c_int64), ("adapters", ctypes.c_int32), ("rank", ctypes.c_int32),
+                ("max_samples", ctypes.c_int64), ("stream", ctypes.c_void_p)]
 
 
 class SfbError(RuntimeError):
@@ -99,6 +112,21 @@ def lib() -> ctypes.CDLL:
         L.sfb_get_operand_copy.argtypes = [vp, ctypes.POINTER(vp), ctypes.POINTER(i32), ctypes.POINTER(i64)]
         L.sfb_compute_factors_csr.argtypes = [vp, i32, vp, vp, vp, i64, vp]
         L.sfb_step_csr.argtypes = [vp, vp, vp, vp, i64, vp]
+        acfgp = ctypes.POINTER(sfb_adapter_config)
+        L.sfb_adapter_workspace_bytes.argtypes = [acfgp, ctypes.POINTER(ctypes.c_size_t)]
+        L.sfb_adapter_init.argtypes = [acfgp, vp, vp, vp, vp, vp, ctypes.c_size_t, ctypes.POINTER(vp)]
+        L.sfb_adapter_forward.argtypes = [vp, i64, vp, i64, vp, vp, i64, vp]
+        L.sfb_adapter_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp]
+        L.sfb_adapter_get_status.argtypes = [vp, ctypes.POINTER(ctypes.c_uint32)]
+        L.sfb_adapter_last_cuda_error.argtypes = [vp]
+        L.sfb_adapter_destroy.argtypes = [vp]
+        L.sfb_clip_workspace_bytes.argtypes = [i64, vp, vp, ctypes.POINTER(ctypes.c_size_t)]
+        L.sfb_clip_init.argtypes = [i64, vp, vp, vp, vp, vp, ctypes.c_size_t, vp, ctypes.POINTER(vp)]
+        L.sfb_clip_sum.argtypes = [vp, vp]
+        L.sfb_clip_scale.argtypes = [vp, ctypes.c_float, vp, vp]
+        L.sfb_clip_gradients.argtypes = [vp, ctypes.c_float, vp]
+        L.sfb_clip_last_cuda_error.argtypes = [vp]
+        L.sfb_clip_destroy.argtypes = [vp]
         for name in EXPORTS:
             if name != "sfb_strerror":
                 getattr(L, name).restype = ctypes.c_int
@@ -313,6 +341,214 @@ class Context:
     def close(self):
         if self._h:
             lib().sfb_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def sfb_adapter_workspace_bytes(cfg: sfb_adapter_config) -> int:
+    out = ctypes.c_size_t(0)
+    rc = lib().sfb_adapter_workspace_bytes(ctypes.byref(cfg), ctypes.byref(out))
+    if rc:
+        raise SfbError(rc, "sfb_adapter_workspace_bytes")
+    return out.value
+
+
+def _capture(stream, calls):
+    import torch
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=stream):
+        calls()
+    return g
+
+
+class Adapters:
+    """Owns one ``sfb_adapters``: low-rank adapters of many requests beside a shared ``W`` (include/sfb.h has the formulas).
+
+    ``W`` [rows, cols], ``U`` [adapters, rank, rows] and ``V`` [adapters, rank, cols] are bf16 CUDA tensors whose last
+    dimension has no gaps and whose rows start a multiple of 8 entries apart (``Context.operand_copy_as_tensor()[:, :cols]``
+    is such a W); ``scale`` [adapters] fp32.  They are borrowed: their values may change between calls, their memory stays.
+    All work is enqueued on ``stream`` (default: the current one at construction); tensors that other streams write or free
+    are ordered against it by the caller, as for ``Context``."""
+
+    def __init__(self, W, U, V, scale, max_samples, stream=None):
+        import torch
+        bf16, f32 = torch.bfloat16, torch.float32
+        if W.dim() != 2 or U.dim() != 3 or V.dim() != 3 or tuple(U.shape[:2]) != tuple(V.shape[:2]) or \
+                U.shape[2] != W.shape[0] or V.shape[2] != W.shape[1] or tuple(scale.shape) != (U.shape[0],):
+            raise ValueError("W [rows, cols], U [adapters, rank, rows], V [adapters, rank, cols], scale [adapters]")
+        self._device = W.device
+        for t, dt in ((W, bf16), (U, bf16), (V, bf16), (scale, f32)):
+            self._check(t, dt)
+        for t in (U, V):
+            if t.shape[0] > 1 and t.shape[1] > 1 and t.stride(0) != t.shape[1] * t.stride(1):
+                raise ValueError("the adapters of U and of V follow one another without gaps")
+        if not scale.is_contiguous():
+            raise ValueError("scale is contiguous")
+        self.W, self.U, self.V, self.scale = W, U, V, scale
+        self.adapters, self.rank, self.rows, self.cols = U.shape[0], U.shape[1], W.shape[0], W.shape[1]
+        self.stream = stream if stream is not None else torch.cuda.current_stream(W.device)
+        self.cfg = sfb_adapter_config(self.rows, self.cols, self._pitch(W), self._pitch(U), self._pitch(V), self.adapters,
+                                      self.rank, max_samples, self.stream.cuda_stream)
+        nbytes = sfb_adapter_workspace_bytes(self.cfg)
+        self._h = ctypes.c_void_p()
+        with torch.cuda.device(W.device):
+            self.workspace = torch.empty(nbytes + 1024, dtype=torch.uint8, device=W.device)
+            base = (self.workspace.data_ptr() + 1023) // 1024 * 1024
+            rc = lib().sfb_adapter_init(ctypes.byref(self.cfg), W.data_ptr(), U.data_ptr(), V.data_ptr(), scale.data_ptr(), base,
+                                        nbytes, ctypes.byref(self._h))
+        if rc:
+            raise SfbError(rc, "sfb_adapter_init")
+
+    def _check(self, t, dtype):
+        if t.dtype != dtype or t.device != self._device or not t.is_cuda:
+            raise ValueError(f"a {dtype} tensor on {self._device} is wanted, not {t.dtype} on {t.device}")
+        if t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError("the last dimension of a tensor has no gaps")
+
+    @staticmethod
+    def _pitch(t):
+        """Entries from a row to the next; of a single row, whose stride says nothing, any that would do."""
+        if t.shape[-2] > 1:
+            return t.stride(-2)
+        return t.stride(0) if t.dim() == 3 and t.shape[0] > 1 else (t.shape[-1] + 7) // 8 * 8
+
+    def _operand(self, t, n, width):
+        import torch
+        self._check(t, torch.bfloat16)
+        if t.dim() != 2 or t.shape[0] != n or t.shape[1] != width:
+            raise ValueError(f"a tensor [{n}, {width}] is wanted, not {list(t.shape)}")
+        return t.data_ptr(), self._pitch(t)
+
+    def _whole(self, t, dtype, shape):
+        if t is None:
+            return None
+        self._check(t, dtype)
+        if tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"a contiguous tensor {list(shape)} is wanted, not {list(t.shape)}")
+        return t.data_ptr()
+
+    def _ck(self, rc, what):
+        if rc:
+            raise SfbError(rc, what, lib().sfb_adapter_last_cuda_error(self._h))
+
+    def sfb_adapter_forward(self, X, ids, Y, S=None):
+        """Y [n, rows] (bf16) receives W x_i + scale[a_i] U[a_i]^T V[a_i] x_i for X [n, cols] (bf16) and ids [n] (int32; -1: no
+        adapter); S (fp32 [n, rank], may be None) V[a_i] x_i."""
+        import torch
+        n = X.shape[0]
+        x, ldx = self._operand(X, n, self.cols)
+        y, ldy = self._operand(Y, n, self.rows)
+        i, s = self._whole(ids, torch.int32, (n,)), self._whole(S, torch.float32, (n, self.rank))
+        self._ck(lib().sfb_adapter_forward(self._h, n, x, ldx, i, y, ldy, s), "sfb_adapter_forward")
+
+    def sfb_adapter_backward(self, dY, X, ids, S=None, dX=None, dU=None, dV=None):
+        """The gradients for dY [n, rows] (bf16): dX [n, cols] (bf16), dU [adapters, rank, rows] and dV [adapters, rank, cols]
+        (fp32, written whole); None: not wanted.  S: what the forward pass gave for these samples; None: computed again."""
+        import torch
+        n, a, r, f32 = X.shape[0], self.adapters, self.rank, torch.float32
+        x, ldx = self._operand(X, n, self.cols)
+        dy, lddy = self._operand(dY, n, self.rows)
+        dx, lddx = self._operand(dX, n, self.cols) if dX is not None else (None, 0)
+        i, s = self._whole(ids, torch.int32, (n,)), self._whole(S, f32, (n, r))
+        du, dv = self._whole(dU, f32, (a, r, self.rows)), self._whole(dV, f32, (a, r, self.cols))
+        self._ck(lib().sfb_adapter_backward(self._h, n, dy, lddy, x, ldx, i, s, dx, lddx, du, dv), "sfb_adapter_backward")
+
+    def sfb_adapter_get_status(self) -> int:
+        st = ctypes.c_uint32(0)
+        self._ck(lib().sfb_adapter_get_status(self._h, ctypes.byref(st)), "sfb_adapter_get_status")
+        return st.value
+
+    def capture(self, calls):
+        """As ``Context.capture``: the handle's stream is not the default one, and every kind of call has run once before."""
+        return _capture(self.stream, calls)
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib().sfb_adapter_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class GradientClip:
+    """Owns one ``sfb_clip``: the global norm of a list of gradient tensors, and the tensors rescaled where it is above a limit.
+
+    ``grads``: contiguous CUDA tensors of fp32, bf16 or fp16, any number, any mixture; ``outs``: where each goes rescaled (same
+    types and sizes), None: in place.  The handle keeps their addresses and the tensors alive.  All work is enqueued on
+    ``stream`` (default: the current one at construction)."""
+
+    def __init__(self, grads, outs=None, stream=None):
+        import torch
+        self.grads, self.outs = list(grads), list(outs) if outs is not None else None
+        types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+        if not self.grads:
+            raise ValueError("no tensors")
+        self._device = dev = self.grads[0].device
+        for g in self.grads + (self.outs or []):
+            if not g.is_cuda or g.device != dev or g.dtype not in types or not g.is_contiguous():
+                raise ValueError("contiguous fp32, bf16 or fp16 tensors on one CUDA device are wanted")
+        if self.outs is not None and (len(self.outs) != len(self.grads) or
+                                      any(o.dtype != g.dtype or o.numel() != g.numel() for o, g in zip(self.outs, self.grads))):
+            raise ValueError("outs have the types and sizes of grads")
+        self.stream = stream if stream is not None else torch.cuda.current_stream(dev)
+        m = len(self.grads)
+        counts = (ctypes.c_int64 * m)(*(g.numel() for g in self.grads))
+        dtypes = (ctypes.c_int32 * m)(*(types[g.dtype] for g in self.grads))
+        src = (ctypes.c_void_p * m)(*(g.data_ptr() for g in self.grads))
+        dst = (ctypes.c_void_p * m)(*(o.data_ptr() for o in self.outs)) if self.outs is not None else None
+        nbytes = ctypes.c_size_t(0)
+        rc = lib().sfb_clip_workspace_bytes(m, counts, dtypes, ctypes.byref(nbytes))
+        if rc:
+            raise SfbError(rc, "sfb_clip_workspace_bytes")
+        self._h = ctypes.c_void_p()
+        with torch.cuda.device(dev):
+            self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device=dev)
+            rc = lib().sfb_clip_init(m, src, dst, counts, dtypes, self.workspace.data_ptr(), nbytes.value, self.stream.cuda_stream,
+                                     ctypes.byref(self._h))
+        if rc:
+            raise SfbError(rc, "sfb_clip_init")
+
+    def _ck(self, rc, what):
+        if rc:
+            raise SfbError(rc, what, lib().sfb_clip_last_cuda_error(self._h))
+
+    def _out(self, t, dtype, n):
+        if t.dtype != dtype or t.device != self._device or t.numel() < n or not t.is_contiguous():
+            raise ValueError(f"{n} contiguous entries of {dtype} on {self._device} are wanted")
+        return t.data_ptr()
+
+    def sfb_clip_gradients(self, max_norm, result):
+        """result (fp32, 2 entries) receives the norm and the factor that the tensors were multiplied with."""
+        import torch
+        self._ck(lib().sfb_clip_gradients(self._h, max_norm, self._out(result, torch.float32, 2)), "sfb_clip_gradients")
+
+    def sfb_clip_sum(self, total):
+        """total (fp64, 1 entry) receives the sum of squares, for a sum over ranks."""
+        import torch
+        self._ck(lib().sfb_clip_sum(self._h, self._out(total, torch.float64, 1)), "sfb_clip_sum")
+
+    def sfb_clip_scale(self, max_norm, total, result):
+        """The rescaling, for a sum of squares (fp64, 1 entry) over all ranks."""
+        import torch
+        self._ck(lib().sfb_clip_scale(self._h, max_norm, self._out(total, torch.float64, 1), self._out(result, torch.float32, 2)),
+                 "sfb_clip_scale")
+
+    def capture(self, calls):
+        """As ``Context.capture``: the handle's stream is not the default one."""
+        return _capture(self.stream, calls)
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib().sfb_clip_destroy(self._h)
             self._h = ctypes.c_void_p()
 
     def __del__(self):
