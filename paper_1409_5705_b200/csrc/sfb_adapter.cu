@@ -1,9 +1,9 @@
 // Low-rank adapters of many requests beside the shared W (sfb_adapter_* in sfb.h): the logits of samples, each with the adapter
 // (a set of factor pairs) that its request names, and the gradients of the samples and of the adapters' factors.
 //
-// Launches of a forward pass:  adapter_rank_kernel (s = V x), adapter_product_kernel (y = W x, with scale U^T s at the end);
-// of a backward pass:  adapter_index_kernel, adapter_rank_kernel (t = U dy; s again where it is not given), adapter_product_kernel
-// (dx), adapter_gradient_kernel (dU, dV).
+// Launches of a forward pass:  adapter_rank_kernel (s = V x, in parts), then up to 64 samples adapter_few_kernel (y = W x + scale U^T s),
+// for more adapter_sum_kernel and adapter_pair_kernel;  of a backward pass:  adapter_index_kernel, adapter_rank_kernel (t = U dy; s again
+// where it is not given), the products as in a forward pass (dx), adapter_words_kernel and adapter_gradient_kernel (dU, dV).
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -23,10 +23,15 @@ constexpr int kMaxTile = 256;                       // samples of a tile, at mos
 constexpr int kTileBytesA = BM * BK * 2;
 constexpr int kMaxParts = 16;                       // of the contraction of adapter_rank_kernel
 constexpr int kMaxStages = 8;
-constexpr int kRing = 196608;                       // bytes of operand stages
+// The tensor cores cut off what an fp32 accumulator cannot hold, always towards zero: 1.4e-8 of the sum an instruction of 16 (measured:
+// -1.1e-6 after 78 of them, -8e-6 after 512).  Sums that leave in fp32 are taken out, and added up with rounding, every 12 k-blocks.
+constexpr int kDrain = 12;
+constexpr int kListPitch = kMaxTile + 8;            // entries of a tile's list: their number, then the adapters
+constexpr int kRing = 196608, kSmallRing = 98304;   // bytes of operand stages; of tiles of up to 64 samples, two blocks an SM
 
 __host__ __device__ constexpr int stage_bytes(int tn) { return kTileBytesA + tn * BK * 2; }
-int stages_of(int tn) { return std::min(kMaxStages, kRing / stage_bytes(tn)); }
+int ring_of(int tn) { return tn <= 64 ? kSmallRing : kRing; }
+int stages_of(int tn) { return std::min(kMaxStages, ring_of(tn) / stage_bytes(tn)); }
 
 // Samples of a tile: the fewest columns that hold n, up to 256.
 int tile_of(int64_t n) { return n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : n <= 128 ? 128 : kMaxTile; }
@@ -101,10 +106,12 @@ struct RankParams {
   int32_t rank, adapters;
   const int32_t* ids;
   float* out;                  // [parts][n][rank]
+  int32_t* lists;              // may be null: [tiles][kListPitch], and per sample its place in its tile's list
+  int32_t* place;
   uint32_t* status;
 };
 
-__global__ void __launch_bounds__(kRankThreads, 1)
+__global__ void __launch_bounds__(kRankThreads)
 adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ RankParams p) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ alignas(16) TileList L;
@@ -132,6 +139,14 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
   tc_fence_after();
   const uint32_t tmem_base = tmem_slot;
   const int per = (p.rank + kSlice - 1) / kSlice, slices = L.count * per, chunks = (slices + 7) / 8;
+  if (p.lists && part == 0 && blockIdx.z == 0) {
+    int32_t* to = p.lists + static_cast<int64_t>(blockIdx.y) * kListPitch;
+    if (threadIdx.x == 0) to[0] = L.count;
+    for (int t = threadIdx.x; t < p.tn; t += kRankThreads) {
+      if (t < L.count) to[1 + t] = L.list[t];
+      if (first + t < p.n) p.place[first + t] = L.place[t];
+    }
+  }
 
   if (warp == 0) {
     uint32_t s = 0, ph = 0;
@@ -156,17 +171,18 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
     const uint32_t idesc = umma_idesc_bf16(BM, p.tn);
     uint32_t s = 0, ph = 0, i = 0;
     bool ok = true;
-    for (int c = blockIdx.z; c < chunks && ok; c += gridDim.z, ++i) {
+    for (int c = blockIdx.z; c < chunks && ok; c += gridDim.z)
+    for (int k0 = kbeg; k0 < kend && ok; k0 += kDrain, ++i) {
       const uint32_t a = i & 1, aph = (i >> 1) & 1, d_tmem = tmem_base + a * cols;
       if (!mbar_wait_warp(&tempty[a], aph ^ 1, abort_flag)) { ok = false; break; }
       tc_fence_after();
-      for (int k = kbeg; k < kend; ++k) {
+      for (int k = k0; k < min(k0 + kDrain, kend); ++k) {
         if (!mbar_wait_warp(&full[s], ph, abort_flag)) { ok = false; break; }
         tc_fence_after();
         if (elect_one()) {
           const uint64_t da = umma_desc_k128(smem_u32(smem + s * stage)), db = umma_desc_k128(smem_u32(smem + s * stage + kTileBytesA));
 #pragma unroll
-          for (int j = 0; j < BK / 16; ++j) umma_bf16(d_tmem, da + 2 * j, db + 2 * j, idesc, (k - kbeg) | j ? 1u : 0u);
+          for (int j = 0; j < BK / 16; ++j) umma_bf16(d_tmem, da + 2 * j, db + 2 * j, idesc, (k - k0) | j ? 1u : 0u);
           umma_commit(&empty[s]);
         }
         if (++s == static_cast<uint32_t>(p.stages)) { s = 0; ph ^= 1; }
@@ -177,9 +193,11 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
     const int q = warp & 3;
     float* out = p.out + static_cast<int64_t>(part) * p.n * p.rank;
     uint32_t i = 0;
-    for (int c = blockIdx.z; c < chunks; c += gridDim.z, ++i) {
+    bool ok = true;
+    for (int c = blockIdx.z; c < chunks && ok; c += gridDim.z)
+    for (int k0 = kbeg; k0 < kend; k0 += kDrain, ++i) {
       const uint32_t a = i & 1, aph = (i >> 1) & 1;
-      if (!mbar_wait_warp(&tfull[a], aph, abort_flag)) break;
+      if (!mbar_wait_warp(&tfull[a], aph, abort_flag)) { ok = false; break; }
       tc_fence_after();
       const int g = c * 8 + q * 2 + (lane >> 4), at = g < slices ? g / per : -2, r = (g - at * per) * kSlice + (lane & 15);
 #pragma unroll 1
@@ -189,7 +207,10 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
         tmem_ld_wait();
 #pragma unroll
         for (int j = 0; j < 32; ++j)                 // (places behind a tile of 16 are -1)
-          if (L.place[t0 + j] == at && r < p.rank) out[static_cast<int64_t>(first + t0 + j) * p.rank + r] = __uint_as_float(acc[j]);
+          if (L.place[t0 + j] == at && r < p.rank) {
+            float* to = out + static_cast<int64_t>(first + t0 + j) * p.rank + r;
+            *to = __uint_as_float(acc[j]) + (k0 > kbeg ? *to : 0.f);
+          }
       }
       tc_fence_before();
       __syncwarp();
@@ -220,13 +241,16 @@ __device__ __forceinline__ float ranked(const Ranked& s, int64_t at) {
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// y_i = A z_i + scale F[a_i]^T p_i for a tile of 128 rows of A (rows of W; with MN, of its transpose: columns of W) and tn samples.  The
-// contraction is cut over the CTAs of a cluster; each of them finishes some of the samples, adding the parts in rank order and the
-// adapter's term in fp32.
+// y_i = A z_i + scale F[a_i]^T p_i for up to 64 samples: a tile of 128 rows of A (rows of W; with MN, of its transpose: columns of W) a
+// cluster, whose CTAs share the contraction.  Bound by the way of W to the SMs: two CTAs an SM, 190 KB of loads under way on it.  While
+// the products run the other warps form the adapters' terms in fp32 from p and F in global memory, a sample by one CTA of the cluster;
+// the parts are added in rank order, each CTA finishing some of the samples.
+// The loads of A and z do not wait for the launch before (adapter_rank_kernel lets this one start once those before it are done).
+// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..5 adapters' terms and epilogue.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kProdThreads = 192;
-struct ProductParams {
-  int32_t n, tn, tiles, m;     // samples; of a tile; tiles of samples; rows of A
+constexpr int kFewThreads = 192, kFewMost = 64, kMaxCluster = 8;
+struct FewParams {
+  int32_t n, m;                // samples; rows of A
   int32_t kseg, stages, parts; // k-blocks; operand stages; CTAs of a cluster
   int32_t rank, adapters;
   const int32_t* ids;
@@ -240,19 +264,20 @@ struct ProductParams {
   uint32_t* status;
 };
 
-template <bool MN>
-__global__ void __launch_bounds__(kProdThreads, 1)
-adapter_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ ProductParams p) {
+template <int TN, bool MN>
+__global__ void __launch_bounds__(kFewThreads)
+adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ FewParams p) {
+  constexpr int kStage = stage_bytes(TN), kCols = TN < 32 ? 32 : TN;
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kMaxStages], empty[kMaxStages], done;
   __shared__ uint32_t tmem_slot, abort_word;
+  __shared__ int32_t id_of[TN];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  float* ps = reinterpret_cast<float*>(smem + p.stages * kStage);           // [n][rank]: scale * p
   volatile uint32_t* abort_flag = &abort_word;
   const int warp = warp_index(), lane = threadIdx.x & 31;
-  const int mine = static_cast<int>(blockIdx.x) % p.parts, tile = static_cast<int>(blockIdx.x) / p.parts;
-  const int mt = tile / p.tiles, m0 = mt * BM, first = (tile - mt * p.tiles) * p.tn;
+  const int mine = static_cast<int>(blockIdx.x) % p.parts, m0 = static_cast<int>(blockIdx.x) / p.parts * BM;
   const int kbeg = mine * p.kseg / p.parts, nk = (mine + 1) * p.kseg / p.parts - kbeg;
-  const int cols = max(p.tn, 32), stage = stage_bytes(p.tn);
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
     for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
@@ -261,39 +286,39 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     fence_barrier_init();
     prefetch_tmap(&tmA); prefetch_tmap(&tmZ);
   }
-  if (warp == 1) { tmem_alloc(&tmem_slot, cols); tmem_relinquish(); }
+  if (warp == 1) { tmem_alloc(&tmem_slot, kCols); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = tmem_slot;
-  pdl_wait();
 
   if (warp == 0) {
+    const uint64_t pol_keep = policy_evict_last();      // every tile reads the samples
     bool ok = true;
     for (int k = 0; k < nk && ok; ++k) {
       const uint32_t s = k % p.stages, ph = (k / p.stages) & 1;
       ok = mbar_wait_warp(&empty[s], ph ^ 1, abort_flag);
       if (ok && elect_one()) {
-        uint8_t* st = smem + s * stage;
-        mbar_expect_tx(&full[s], stage);
+        uint8_t* st = smem + s * kStage;
+        mbar_expect_tx(&full[s], kStage);
         if (MN) {
           tma_load_2d(st, &tmA, m0, (kbeg + k) * BK, &full[s]);
           tma_load_2d(st + kTileBytesA / 2, &tmA, m0 + 64, (kbeg + k) * BK, &full[s]);
         } else {
           tma_load_2d(st, &tmA, (kbeg + k) * BK, m0, &full[s]);
         }
-        tma_load_2d(st + kTileBytesA, &tmZ, (kbeg + k) * BK, first, &full[s]);
+        tma_load_2d_hint(st + kTileBytesA, &tmZ, (kbeg + k) * BK, 0, &full[s], pol_keep);
       }
     }
   } else if (warp == 1) {
-    const uint32_t idesc = umma_idesc_bf16(BM, p.tn) | (MN ? 1u << 15 : 0u);
+    const uint32_t idesc = umma_idesc_bf16(BM, TN) | (MN ? 1u << 15 : 0u);
     bool ok = true;
     for (int k = 0; k < nk && ok; ++k) {
       const uint32_t s = k % p.stages, ph = (k / p.stages) & 1;
       ok = mbar_wait_warp(&full[s], ph, abort_flag);
       tc_fence_after();
       if (ok && elect_one()) {
-        const uint32_t a = smem_u32(smem + s * stage);
+        const uint32_t a = smem_u32(smem + s * kStage);
         const uint64_t da = MN ? umma_desc_mn128(a) : umma_desc_k128(a), db = umma_desc_k128(a + kTileBytesA);
 #pragma unroll
         for (int j = 0; j < BK / 16; ++j) umma_bf16(tmem_base, da + (MN ? 128 : 2) * j, db + 2 * j, idesc, k | j ? 1u : 0u);
@@ -302,19 +327,53 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     }
     if (ok && elect_one()) umma_commit(&done);
   } else {
-    // the accumulator to shared memory (the operand stages', which nothing uses any more): [sample][128 rows]
-    const int q = warp & 3;
+    const int q = warp & 3, tid = threadIdx.x - 64, m = m0 + q * 32 + lane;
+    pdl_wait();
+    for (int t = tid; t < TN; t += 128) {
+      const int id = t < p.n ? p.ids[t] : -1;
+      id_of[t] = id >= 0 && id < p.adapters ? id : -1;
+    }
+    asm volatile("bar.sync 1, 128;" ::: "memory");
+    for (int x = tid; x < p.n * p.rank; x += 128) {
+      const int id = id_of[x / p.rank];
+      const float v = id >= 0 ? ranked(p.p, x) : 0.f;
+      ps[x] = id >= 0 ? p.scale[id] * v : 0.f;
+      if (p.p_out && blockIdx.x == 0) p.p_out[x] = v;
+    }
+    asm volatile("bar.sync 1, 128;" ::: "memory");
+    float e[TN];
+#pragma unroll
+    for (int t = 0; t < TN; ++t) {
+      e[t] = 0.f;
+      if (t >= p.n || t % p.parts != mine || m >= p.m) continue;
+      const int id = id_of[t];
+      if (id < 0) continue;
+      const __nv_bfloat16* f = p.F + static_cast<int64_t>(id) * p.rank * p.ldf + m;
+      const float* w = ps + t * p.rank;
+      float v = 0.f;
+      int r = 0;
+      for (; r + 8 <= p.rank; r += 8) {
+        float x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[u] = __bfloat162float(f[(r + u) * p.ldf]);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v = fmaf(x[u], w[r + u], v);
+      }
+      for (; r < p.rank; ++r) v = fmaf(__bfloat162float(f[r * p.ldf]), w[r], v);
+      e[t] = v;
+    }
+    // the accumulator and the terms to shared memory (the operand stages', which nothing uses any more): [sample][128 rows]
     if (mbar_wait_warp(&done, 0, abort_flag)) {
       tc_fence_after();
       float* to = reinterpret_cast<float*>(smem) + q * 32 + lane;
-#pragma unroll 1
-      for (int t0 = 0; t0 < p.tn; t0 += 32) {
+#pragma unroll
+      for (int t0 = 0; t0 < TN; t0 += 32) {
         uint32_t acc[32];
         tmem_ld_32x32(tmem_base + (static_cast<uint32_t>(q * 32) << 16) + t0, acc);
         tmem_ld_wait();
 #pragma unroll
         for (int j = 0; j < 32; ++j)
-          if (t0 + j < p.tn) to[(t0 + j) * BM] = __uint_as_float(acc[j]);
+          if (t0 + j < TN) to[(t0 + j) * BM] = __uint_as_float(acc[j]) + e[t0 + j < TN ? t0 + j : 0];
       }
     }
   }
@@ -322,45 +381,20 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
   if (p.parts > 1) { cluster_arrive(); cluster_wait(); }
   else __syncthreads();
   if (!abort_word) {
-    const uint32_t base = smem_u32(smem);
-    const int t1 = (mine + 1) * p.tn / p.parts;
-    for (int t = mine * p.tn / p.parts + warp; t < t1; t += kProdThreads / 32) {
-      const int64_t i = first + t;
-      if (i >= p.n) break;
-      const int id = p.ids[i];
-      const bool has = id >= 0 && id < p.adapters;
-      const float sc = has ? p.scale[id] : 0.f;
-      float s[SFB_ADAPTER_MAX_RANK / 32];
-#pragma unroll
-      for (int u = 0; u < SFB_ADAPTER_MAX_RANK / 32; ++u) {
-        const int r = u * 32 + lane;
-        s[u] = has && r < p.rank ? ranked(p.p, i * p.rank + r) : 0.f;
-        if (p.p_out && mt == 0 && r < p.rank) p.p_out[i * p.rank + r] = s[u];
-        s[u] *= sc;
+    // a lane takes two rows of a sample, a warp half of its 128
+    const int t1 = min((mine + 1) * TN / p.parts, p.n);
+    for (int x = mine * TN / p.parts * 2 + warp; x < 2 * t1; x += kFewThreads / 32) {
+      const int t = x >> 1, row = (x & 1) * 64 + 2 * lane, m = m0 + row;
+      const uint32_t at = smem_u32(smem) + (t * BM + row) * 4;
+      float2 v = make_float2(0.f, 0.f);
+      for (int c = 0; c < p.parts; ++c) {
+        float2 w;
+        asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(w.x), "=f"(w.y) : "r"(mapa_u32(at, c)) : "memory");
+        v = c ? make_float2(v.x + w.x, v.y + w.y) : w;
       }
-#pragma unroll 1
-      for (int g = 0; g < BM / 32; ++g) {
-        const int m = m0 + g * 32 + lane;
-        float v = 0.f;
-        const uint32_t at = base + (t * BM + g * 32 + lane) * 4;
-        for (int c = 0; c < p.parts; ++c) {
-          float w;
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w) : "r"(mapa_u32(at, c)) : "memory");
-          v = c ? v + w : w;
-        }
-        if (has) {
-          const __nv_bfloat16* f = p.F + static_cast<int64_t>(id) * p.rank * p.ldf + m;
-#pragma unroll
-          for (int u = 0; u < SFB_ADAPTER_MAX_RANK / 32; ++u) {
-            const int left = min(32, p.rank - u * 32);
-            for (int r = 0; r < left; ++r) {
-              const float w = m < p.m ? __bfloat162float(f[(u * 32 + r) * p.ldf]) : 0.f;
-              v = fmaf(w, __shfl_sync(0xffffffffu, s[u], r), v);
-            }
-          }
-        }
-        if (m < p.m) p.Y[i * p.ldy + m] = __float2bfloat16_rn(v);
-      }
+      __nv_bfloat16* y = p.Y + t * p.ldy + m;
+      if (m + 1 < p.m) *reinterpret_cast<__nv_bfloat162*>(y) = __floats2bfloat162_rn(v.x, v.y);
+      else if (m < p.m) *y = __float2bfloat16_rn(v.x);
     }
   }
   __syncwarp();
@@ -372,7 +406,385 @@ adapter_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
     for (int i = 0; i < 64; ++i) __nanosleep(1000);
     __syncthreads();
   }
-  if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem_base, cols); }
+  if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem_base, kCols); }
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// The same for more samples, on pairs of CTAs (cta_group::2): a tile of 256 rows of A x tn samples (128 or 256), a CTA 128 of the rows in
+// its TMEM; it loads its own rows and its half of the samples, 32 KB a k-block.  Two accumulators: the end of a tile runs beside the next
+// one's products.  Whole rounds of tiles are taken whole, the k-blocks of the rest are shared out (Segments in sfb_tile.cuh).
+//
+// The adapters' term is more contraction: behind the k-blocks of A the pair that finishes a tile takes the factors of the adapters in
+// the tile's list, four slices of 16 ranks a k-block, against  scale p  of the samples in bf16 (one rounding, 2^-8 of the term; the
+// result is rounded by as much), with zeros where a sample has another adapter.  Zeros do not hide what is not finite: so the warps that
+// write these operands look through the factors too, replace what is not finite by zeros, and the end of the tile adds those entries
+// alone, in fp32, to the samples of their own adapter.
+//
+// Warps: 0 TMA producer, 1 MMA issuer (leader CTA) and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the columns), 10..13
+// the samples' operand of the adapters' term.
+// ---------------------------------------------------------------------------------------------------------
+constexpr int kPairThreads = 448, kEpi = 8, kBuild = 4, kGroup = 8;      // kGroup: tiles of samples that follow one another
+constexpr int kPairStages = 6, kPairStage = 2 * kTileBytesA;
+constexpr int kPairSmem = kPairStages * kPairStage + 1024;
+constexpr int kPartFloats = BM * kMaxTile;          // what a CTA leaves of a tile
+struct PairParams {
+  int32_t n, tn, tilesT, tilesM, m;
+  int32_t kseg, cut, whole;    // k-blocks; see Segments
+  int32_t rank, adapters;
+  const int32_t* ids;
+  const int32_t *lists, *place;
+  const float* scale;
+  const __nv_bfloat16* F;
+  int64_t ldf;
+  const float* p;              // [n][rank]
+  __nv_bfloat16* Y;
+  int64_t ldy;
+  float* partial;              // [pairs][2][kPartFloats]
+  uint32_t* ready;             // [pairs][2][kEpi]
+  uint32_t* status;
+};
+
+__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, volatile uint32_t* abort) {      // by a whole warp
+  const long long t0 = clock64();
+  bool got = false;
+  for (uint32_t i = 0; i < kMaxPolls; ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t"
+        ".reg .pred P;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 P, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, P;\n\t"
+        "}\n"
+        : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(kWaitHintNs) : "memory");
+    if (ok) { got = true; break; }
+    if (*abort) break;
+    if (clock64() - t0 > kMaxWaitCycles) { *abort = 1; break; }
+  }
+  return __all_sync(0xffffffffu, got);
+}
+
+// What is not finite of the adapter's term of sample i at row m.
+__device__ __noinline__ float not_finite_term(const PairParams& p, int i, int m) {
+  const int id = p.ids[i];
+  if (id < 0 || id >= p.adapters) return 0.f;
+  const __nv_bfloat16* f = p.F + static_cast<int64_t>(id) * p.rank * p.ldf + m;
+  const float* s = p.p + static_cast<int64_t>(i) * p.rank;
+  float v = 0.f;
+  for (int r = 0; r < p.rank; ++r) {
+    const float x = __bfloat162float(f[r * p.ldf]);
+    if (!isfinite(x)) v += p.scale[id] * s[r] * x;
+  }
+  return v;
+}
+
+template <bool MN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ CUtensorMap tmF,
+                    const __grid_constant__ PairParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t full[kPairStages], empty[kPairStages];       // full, built, tempty: the leader's are in use
+  __shared__ uint64_t landed[kPairStages], built[kPairStages];     // a k-block of factors has landed here; both CTAs have made it an operand
+  __shared__ uint64_t tfull[2], tempty[2], looked[2], taken[2];    // looked: what is not finite of a tile is known; taken: read
+  __shared__ uint32_t tmem_slot, abort_word, odd[2][kBuild];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  volatile uint32_t* abort_flag = &abort_word;
+  const int warp = warp_index(), lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1, half = p.tn / 2;
+  const Segments segs(p.kseg, p.cut != 0, p.whole, p.tilesT * p.tilesM, pair, gridDim.x >> 1);
+  const int per = (p.rank + kSlice - 1) / kSlice;
+  // Tiles that run at the same time: kGroup tiles of samples against as many rows of A as there are pairs for.
+  auto tile_coords = [&](int tile, int& m0, int& tt) {
+    const int in = kGroup * p.tilesM, g = tile / in, width = min(kGroup, p.tilesT - g * kGroup), at = tile - g * in;
+    m0 = at / width * (2 * BM) + static_cast<int>(rank) * BM;
+    tt = g * kGroup + at % width;
+  };
+  pdl_launch_dependents();
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kPairStages; ++i) {
+      mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&landed[i], 1); mbar_init(&built[i], 2 * kBuild);
+    }
+    for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 2 * kEpi); mbar_init(&looked[i], kBuild); mbar_init(&taken[i], kEpi); }
+    abort_word = 0;
+    fence_barrier_init();
+    prefetch_tmap(&tmA); prefetch_tmap(&tmZ); prefetch_tmap(&tmF);
+  }
+  if (warp == 1) { tmem_alloc_pair(&tmem_slot, 512); tmem_relinquish_pair(); }
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_slot;
+  pdl_wait();
+
+  if (warp == 0) {
+    // ---------------- TMA producer ----------------
+    const uint64_t pol = policy_evict_normal();
+    uint32_t s = 0, ph = 0;
+    bool ok = true;
+    for (int i = 0; i < segs.n && ok; ++i) {
+      const Segment sg = segs.get(i);
+      int m0, tt;
+      tile_coords(sg.tile, m0, tt);
+      const int z0 = tt * p.tn + static_cast<int>(rank) * half;
+      const int32_t* list = p.lists + static_cast<int64_t>(tt) * kListPitch;
+      const int slices = sg.k1 == p.kseg ? list[0] * per : 0, more = (slices + 3) / 4;
+      for (int k = sg.k0; k < sg.k1 + more; ++k) {
+        if (!mbar_wait_warp(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
+        uint8_t* st = smem + s * kPairStage;
+        if (k < sg.k1) {
+          if (elect_one()) {
+            if (rank == 0) mbar_expect_tx(&full[s], 2 * (kTileBytesA + half * BK * 2));
+            const uint32_t bar = mapa_u32(smem_u32(&full[s]), 0);
+            if (MN) {
+              tma_load_2d_pair(st, &tmA, m0, k * BK, bar, pol);
+              tma_load_2d_pair(st + kTileBytesA / 2, &tmA, m0 + 64, k * BK, bar, pol);
+            } else {
+              tma_load_2d_pair(st, &tmA, k * BK, m0, bar, pol);
+            }
+            tma_load_2d_pair(st + kTileBytesA, &tmZ, k * BK, z0, bar, pol);
+          }
+        } else {
+          const int g0 = (k - sg.k1) * 4, ns = min(4, slices - g0);
+          int a[4];
+          for (int j = 0; j < 4; ++j) a[j] = j < ns ? list[1 + (g0 + j) / per] : 0;
+          if (elect_one()) {
+            mbar_expect_tx(&landed[s], ns * 2 * kSlice * 128);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if (j >= ns) break;
+              const int y = (g0 + j) % per * kSlice;
+              tma_load_3d(st + j * (kSlice * 128), &tmF, m0, y, a[j], &landed[s]);
+              tma_load_3d(st + kTileBytesA / 2 + j * (kSlice * 128), &tmF, m0 + 64, y, a[j], &landed[s]);
+            }
+          }
+        }
+        if (++s == static_cast<uint32_t>(kPairStages)) { s = 0; ph ^= 1; }
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------- MMA issuer ----------------
+    if (rank == 0) {
+      const uint32_t idesc = umma_idesc_bf16(2 * BM, p.tn) | (MN ? 1u << 15 : 0u), idesc_f = umma_idesc_bf16(2 * BM, p.tn) | 1u << 15;
+      uint32_t s = 0, fph = 0, bph = 0;              // fph, bph: the phases of full and of built, a bit per stage
+      bool ok = true;
+      for (int i = 0; i < segs.n && ok; ++i) {
+        const Segment sg = segs.get(i);
+        int m0, tt;
+        tile_coords(sg.tile, m0, tt);
+        const int slices = sg.k1 == p.kseg ? p.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0, more = (slices + 3) / 4;
+        const uint32_t a = i & 1, aph = (i >> 1) & 1, d_tmem = tmem_base + a * kMaxTile;
+        if (!mbar_wait_warp(&tempty[a], aph ^ 1, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        for (int k = sg.k0; k < sg.k1 + more; ++k) {
+          const uint32_t st = smem_u32(smem + s * kPairStage);
+          if (k < sg.k1) {
+            if (!mbar_wait_warp(&full[s], (fph >> s) & 1, abort_flag)) { ok = false; break; }
+            fph ^= 1u << s;
+            tc_fence_after();
+            if (elect_one()) {
+              const uint64_t da = MN ? umma_desc_mn128(st) : umma_desc_k128(st), db = umma_desc_k128(st + kTileBytesA);
+#pragma unroll
+              for (int j = 0; j < BK / 16; ++j) umma_bf16_pair(d_tmem, da + (MN ? 128 : 2) * j, db + 2 * j, idesc, (k - sg.k0) | j ? 1u : 0u);
+              umma_commit_pair(&empty[s], 3);
+            }
+          } else {
+            if (!mbar_wait_cluster(&built[s], (bph >> s) & 1, abort_flag)) { ok = false; break; }
+            bph ^= 1u << s;
+            tc_fence_after();
+            const int ns = min(4, slices - (k - sg.k1) * 4);
+            if (elect_one()) {
+              const uint64_t da = umma_desc_mn128(st), db = umma_desc_k128(st + kTileBytesA);
+              for (int j = 0; j < ns; ++j) umma_bf16_pair(d_tmem, da + 128 * j, db + 2 * j, idesc_f, 1u);
+              umma_commit_pair(&empty[s], 3);
+            }
+          }
+          if (++s == static_cast<uint32_t>(kPairStages)) s = 0;
+        }
+        if (ok && elect_one()) umma_commit_pair(&tfull[a], 3);
+      }
+    }
+  } else if (warp < 2 + kEpi) {
+    // ---------------- epilogue ----------------
+    const int e = warp - 2, q = warp & 3, h = e >> 2, cols = half;     // columns of this warp: half of tn
+    const uint32_t tempty0 = mapa_u32(smem_u32(&tempty[0]), 0), tempty1 = mapa_u32(smem_u32(&tempty[1]), 0);
+    bool ok = true;
+    for (int i = 0; i < segs.n && ok; ++i) {
+      const Segment sg = segs.get(i);
+      int m0, tt;
+      tile_coords(sg.tile, m0, tt);
+      const uint32_t a = i & 1, aph = (i >> 1) & 1;
+      if (!mbar_wait_warp(&tfull[a], aph, abort_flag) || !mbar_wait_warp(&looked[a], aph, abort_flag)) { ok = false; break; }
+      tc_fence_after();
+      uint32_t any = 0;
+#pragma unroll
+      for (int w = 0; w < kBuild; ++w) any |= odd[a][w];
+      const uint32_t t_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + a * kMaxTile + h * cols;
+      const bool leave = sg.k1 < p.kseg;
+      const int from = leave ? pair : segs.first_part(sg);
+      const int slot = (static_cast<int>(rank) * kEpi + e);
+      if (!leave && from < pair) {
+        for (int j = from; j < pair && ok; ++j) ok = __all_sync(0xffffffffu, lane != 0 || flag_wait(p.ready + j * 2 * kEpi + slot, abort_flag));
+        if (!ok) break;
+        if (lane == 0)
+          for (int j = from; j < pair; ++j) p.ready[j * 2 * kEpi + slot] = 0;               // for the next launch
+        __syncwarp();
+      }
+      const int row = q * 32 + lane, m = m0 + row;
+      const int64_t mine = (static_cast<int64_t>(h) * cols) * BM + row;                     // of a CTA's part: [column][128 rows]
+#pragma unroll 1
+      for (int c = 0; c < cols; c += 32) {
+        uint32_t acc[32];
+        tmem_ld_32x32(t_addr + c, acc);
+        tmem_ld_wait();
+        if (c + 32 >= cols) {                        // the last read of the accumulator: hand it back
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(a ? tempty1 : tempty0);
+        }
+        if (leave) {
+          float* to = p.partial + (static_cast<int64_t>(pair) * 2 + rank) * kPartFloats + mine + static_cast<int64_t>(c) * BM;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) __stcg(to + j * BM, __uint_as_float(acc[j]));
+          continue;
+        }
+        for (int w = from; w < pair; ++w) {
+          const float* in = p.partial + (static_cast<int64_t>(w) * 2 + rank) * kPartFloats + mine + static_cast<int64_t>(c) * BM;
+          float x[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) x[j] = __ldcg(in + j * BM);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) acc[j] = __float_as_uint(__uint_as_float(acc[j]) + x[j]);
+        }
+        const int i0 = tt * p.tn + h * cols + c;
+        if (any && m < p.m) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (i0 + j < p.n) acc[j] = __float_as_uint(__uint_as_float(acc[j]) + not_finite_term(p, i0 + j, m));
+        }
+        // two samples at a time: even lanes store two rows of the first, odd lanes of the second
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+          const float x = __uint_as_float(acc[j]), y = __uint_as_float(acc[j + 1]);
+          const bool second = lane & 1;
+          const float got = __shfl_xor_sync(0xffffffffu, second ? x : y, 1);
+          const int i = i0 + j + (second ? 1 : 0), r = m & ~1;
+          if (i < p.n) {
+            __nv_bfloat16* to = p.Y + static_cast<int64_t>(i) * p.ldy + r;
+            const float lo = second ? got : x, hi = second ? y : got;
+            if (r + 1 < p.m) *reinterpret_cast<__nv_bfloat162*>(to) = __floats2bfloat162_rn(lo, hi);
+            else if (r < p.m) *to = __float2bfloat16_rn(lo);
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&taken[a]);
+        if (leave) {
+          __threadfence();
+          st_release(p.ready + pair * 2 * kEpi + slot, 1u);
+        }
+      }
+    }
+  } else {
+    // ---------------- the samples' operand of the adapters' term ----------------
+    const int w = warp - 2 - kEpi, t = w * 32 + lane;                  // this thread's sample of the CTA's half of the tile
+    uint32_t g = 0, lph = 0;                         // k-blocks so far; the phases of landed
+    bool ok = true;
+    for (int i = 0; i < segs.n && ok; ++i) {
+      const Segment sg = segs.get(i);
+      int m0, tt;
+      tile_coords(sg.tile, m0, tt);
+      const uint32_t a = i & 1, aph = (i >> 1) & 1;
+      if (!mbar_wait_warp(&taken[a], aph ^ 1, abort_flag)) { ok = false; break; }
+      g += sg.k1 - sg.k0;
+      const int slices = sg.k1 == p.kseg ? p.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0, more = (slices + 3) / 4;
+      const int smp = tt * p.tn + static_cast<int>(rank) * half + t;
+      const int at = t < half && smp < p.n ? p.place[smp] : -1;
+      const float sc = at >= 0 ? p.scale[p.ids[smp]] : 0.f;
+      const float* src = p.p + static_cast<int64_t>(smp) * p.rank;
+      uint32_t bad = 0;
+      for (int k = 0; k < more; ++k, ++g) {
+        const uint32_t s = g % kPairStages;
+        uint8_t* st = smem + s * kPairStage;
+        const int g0 = k * 4, ns = min(4, slices - g0);
+        // scale p before the factors have landed: the stage is this k-block's once they have
+        uint32_t words[4][8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bool own = j < ns && at >= 0 && (g0 + j) / per == at;
+          const int r0 = (g0 + j) % per * kSlice;
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            const float x = own && r0 + 2 * u < p.rank ? sc * src[r0 + 2 * u] : 0.f, y = own && r0 + 2 * u + 1 < p.rank ? sc * src[r0 + 2 * u + 1] : 0.f;
+            const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+            words[j][u] = *reinterpret_cast<const uint32_t*>(&v);
+          }
+        }
+        if (!mbar_wait_warp(&landed[s], (lph >> s) & 1, abort_flag)) { ok = false; break; }
+        lph ^= 1u << s;
+        if (t < half) {
+          const uint32_t to = smem_u32(st) + kTileBytesA + t * 128;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((2 * j + u) ^ (t & 7)) << 4)), "r"(words[j][4 * u]),
+                           "r"(words[j][4 * u + 1]), "r"(words[j][4 * u + 2]), "r"(words[j][4 * u + 3]) : "memory");
+        }
+        // the factors: ns slices of 2 KB in each of two panels
+        for (int x = t; x < ns * 256; x += 128) {
+          const int panel = x / (ns * 128), in = x - panel * ns * 128;
+          uint4* v = reinterpret_cast<uint4*>(st + panel * (kTileBytesA / 2)) + in;
+          uint4 f = *v;
+          uint32_t* fw = reinterpret_cast<uint32_t*>(&f);
+          uint32_t hit = 0;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {              // bit 15 / 31: the exponent of the low / high half is all ones
+            const uint32_t b = ((fw[u] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+            hit |= b;
+            fw[u] &= ~((b >> 15) * 0xffffu);
+          }
+          if (hit) { *v = f; bad = 1; }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(mapa_u32(smem_u32(&built[s]), 0));
+      }
+      bad = __any_sync(0xffffffffu, bad);
+      if (lane == 0) {
+        odd[a][w] = bad;
+        mbar_arrive(&looked[a]);
+      }
+    }
+  }
+
+  // ---------------- teardown ----------------
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (abort_word) {
+    if (threadIdx.x == 0) atomicOr(p.status, SFB_STATUS_TIMEOUT);
+    for (int i = 0; i < 64; ++i) __nanosleep(1000);
+    __syncthreads();
+  }
+  cluster_arrive();
+  cluster_wait();
+  if (warp == 1) { tc_fence_after(); tmem_dealloc_pair(tmem_base, 512); }
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// p from its parts, zeros for a sample without an adapter.
+// ---------------------------------------------------------------------------------------------------------
+__global__ void __launch_bounds__(256) adapter_sum_kernel(Ranked p, const int32_t* ids, int64_t n, int32_t rank, int32_t adapters, float* out) {
+  pdl_launch_dependents();
+  pdl_wait();
+  for (int64_t x = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; x < n * rank; x += static_cast<int64_t>(gridDim.x) * 256) {
+    const int id = ids[x / rank];
+    out[x] = id >= 0 && id < adapters ? ranked(p, x) : 0.f;
+  }
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -419,36 +831,126 @@ __global__ void __launch_bounds__(256) adapter_index_kernel(const int32_t* ids, 
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// dF[a] = scale sum_{i of a} p_i z_i^T for a tile of 128 columns of z: the columns are the accumulator's rows, the ranks its
-// columns, the samples the contraction, 64 of them at a time, gathered by the order that adapter_index_kernel wrote (so no sample of
-// another adapter is in the product).  p as a (hi, lo) pair of bf16, 2^-17 of it lost; z is bf16 as it is.
-// Warps: 0..3 loaders (z by asynchronous copies, p from fp32), 4 MMA issuer and TMEM owner, 5..8 epilogue.
+// scale p of the samples in the order of adapter_index_kernel, as three words of bf16 (24 bits): [position][word][rp], rp the rank rounded
+// up to 16 with zeros.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kGradThreads = 288, kGradStages = 4, kGradLag = 2;
+struct WordsParams {
+  Ranked p[2];                 // at null: not wanted
+  __nv_bfloat16* out[2];
+  const int32_t *ids, *order, *begin, *count;
+  const float* scale;
+  int32_t rank, adapters;
+};
+// v = w0 + w1 + w2.  (What overflows in the rounding to the first word is cut off instead; of what is not finite there is no rest.)
+__device__ __forceinline__ void three_words(float v, float (&w)[3]) {
+  w[0] = __bfloat162float(__float2bfloat16_rn(v));
+  if (isinf(w[0]) && !isinf(v)) w[0] = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+  const float rest = isfinite(v) ? v - w[0] : 0.f;
+  w[1] = __bfloat162float(__float2bfloat16_rn(rest));
+  w[2] = rest - w[1];
+}
+
+__global__ void __launch_bounds__(256) adapter_words_kernel(const __grid_constant__ WordsParams p) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int rp = (p.rank + 15) & ~15, pieces = rp / 8;
+  const int64_t total = static_cast<int64_t>(p.begin[p.adapters - 1] + p.count[p.adapters - 1]) * pieces;
+  const int side = blockIdx.y;
+  if (!p.out[side]) return;
+  for (int64_t x = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; x < total; x += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t at = x / pieces;
+    const int c = static_cast<int>(x - at * pieces), i = p.order[at];
+    const float sc = p.scale[p.ids[i]];
+    uint32_t w[3][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float u[3], v[3];
+      const int r = c * 8 + 2 * j;
+      three_words(r < p.rank ? sc * ranked(p.p[side], static_cast<int64_t>(i) * p.rank + r) : 0.f, u);
+      three_words(r + 1 < p.rank ? sc * ranked(p.p[side], static_cast<int64_t>(i) * p.rank + r + 1) : 0.f, v);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(u[k], v[k]);
+        w[k][j] = *reinterpret_cast<const uint32_t*>(&b);
+      }
+    }
+    __nv_bfloat16* to = p.out[side] + at * 3 * rp + c * 8;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(to + k * rp) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// dF[a] = sum_{i of a} (scale p_i) z_i^T for a tile of 128 columns of z: the columns are the accumulator's rows, the ranks of the three
+// words its columns (added at the end), the samples the contraction, 64 of them at a time, gathered in the order of adapter_index_kernel
+// (so no sample of another adapter is in the product).
+// Warps: 0..3 loaders (asynchronous copies of 16 bytes into both operands), 4 MMA issuer and TMEM owner, 5..8 epilogue.
+// ---------------------------------------------------------------------------------------------------------
+constexpr int kGradThreads = 288, kGradStages = 8, kGradRing = 196608;
 struct GradSide {
   const __nv_bfloat16* z;      // [n][ldz]
   int64_t ldz;
   int32_t width, tiles;        // columns; tiles of 128 of them (0: not wanted)
-  Ranked p;
+  const __nv_bfloat16* words;
   float* out;                  // [adapters][rank][width]
 };
 struct GradParams {
   GradSide side[2];
-  int32_t rank, adapters;
+  int32_t rank, adapters, stages;
   const int32_t *order, *begin, *count;
-  const float* scale;
   uint32_t* status;
 };
+__host__ __device__ inline int grad_panels(int rank) { return (3 * ((rank + 15) / 16 * 16) + 63) / 64; }
 
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-// v = hi + lo, as near as two bf16 come.  (What overflows in the rounding is cut off instead; an infinity has no rest.)
-__device__ __forceinline__ void two_words(float v, float& hi, float& lo) {
-  hi = __bfloat162float(__float2bfloat16_rn(v));
-  if (isinf(hi)) hi = isinf(v) ? v : __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-  lo = isinf(hi) ? 0.f : v - hi;
+template <int LAG>
+__device__ __forceinline__ void grad_load(const GradParams& p, uint8_t* smem, uint64_t* full, uint64_t* empty, volatile uint32_t* abort_flag, int64_t items0,
+                                          int64_t items) {
+  const int rp = (p.rank + 15) & ~15, pieces = 3 * rp / 8, stage = kTileBytesA + grad_panels(p.rank) * 8192, stages = p.stages;
+  const int tid = threadIdx.x, c16 = tid & 15, r0 = tid >> 4;
+  uint32_t g = 0, s = 0, ph = 0;                     // k-blocks so far; this one's stage and phase
+  uint32_t back = 0;                                 // the stage of the k-block LAG ago
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int side = it >= items0;
+    const int64_t in = side ? it - items0 : it;
+    const GradSide& sd = p.side[side];
+    const int a = static_cast<int>(in / sd.tiles), m0 = static_cast<int>(in - static_cast<int64_t>(a) * sd.tiles) * BM;
+    const int count = p.count[a], begin = p.begin[a], nk = (count + BK - 1) / BK;
+    const int col = m0 + c16 * 8, left = sd.width - col;
+    const uint32_t bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;
+    for (int k = 0; k < nk; ++k, ++g) {
+      int64_t row[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) { const int at = k * BK + r0 + j * 8; row[j] = at < count ? p.order[begin + at] : -1; }
+      if (!mbar_wait(&empty[s], ph ^ 1, abort_flag)) return;
+      const uint32_t st = smem_u32(smem + s * stage);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int kr = r0 + j * 8;
+        const uint32_t b = row[j] >= 0 ? bytes : 0;
+        cp_async_16(st + (c16 >> 3) * (kTileBytesA / 2) + kr * 128 + (((c16 & 7) ^ (kr & 7)) << 4), b ? sd.z + row[j] * sd.ldz + col : sd.z, b);
+      }
+      for (int x = tid; x < BK * pieces; x += 128) {
+        const int kr = x / pieces, ch = x - kr * pieces, at = k * BK + kr;
+        const uint32_t b = at < count ? 16 : 0;
+        cp_async_16(st + kTileBytesA + (ch >> 3) * 8192 + kr * 128 + (((ch & 7) ^ (kr & 7)) << 4),
+                    sd.words + (b ? (static_cast<int64_t>(begin) + at) * 3 * rp + ch * 8 : 0), b);
+      }
+      cp_async_commit();
+      if (g >= LAG) {
+        cp_async_wait<LAG>();
+        fence_proxy_async_smem();
+        mbar_arrive(&full[back]);
+        if (++back == static_cast<uint32_t>(stages)) back = 0;
+      }
+      if (++s == static_cast<uint32_t>(stages)) { s = 0; ph ^= 1; }
+    }
+  }
+  cp_async_wait<0>();
+  fence_proxy_async_smem();
+  for (uint32_t j = g > LAG ? g - LAG : 0; j < g; ++j) {
+    mbar_arrive(&full[back]);
+    if (++back == static_cast<uint32_t>(stages)) back = 0;
+  }
 }
 
 __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const __grid_constant__ GradParams p) {
@@ -458,150 +960,93 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   volatile uint32_t* abort_flag = &abort_word;
   const int warp = warp_index(), lane = threadIdx.x & 31;
-  const int rp = (p.rank + 15) & ~15, panels = (rp + 63) / 64, word = panels * 8192, stage = kTileBytesA + 2 * word;
+  const int rp = (p.rank + 15) & ~15, N = 3 * rp, stage = kTileBytesA + grad_panels(p.rank) * 8192;
+  const uint32_t buffers = N <= 256 ? 2 : 1;         // accumulators of 256 columns, or one of 512
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kGradStages; ++i) { mbar_init(&full[i], 128); mbar_init(&empty[i], 1); }
+    for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 128); mbar_init(&empty[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 4); }
     abort_word = 0;
     fence_barrier_init();
   }
-  if (warp == 4) { tmem_alloc(&tmem_slot, 256); tmem_relinquish(); }
+  if (warp == 4) { tmem_alloc(&tmem_slot, 512); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = tmem_slot;
   pdl_wait();
   const int64_t items0 = static_cast<int64_t>(p.side[0].tiles) * p.adapters, items = items0 + static_cast<int64_t>(p.side[1].tiles) * p.adapters;
-  auto locate = [&](int64_t it, int& side, int& a, int& m0) {
-    side = it >= items0;
-    if (side) it -= items0;
-    const int tiles = p.side[side].tiles;
-    a = static_cast<int>(it / tiles);
-    m0 = static_cast<int>(it - static_cast<int64_t>(a) * tiles) * BM;
-  };
 
   if (warp < 4) {
-    uint32_t g = 0;                                  // k-blocks so far
-    bool ok = true;
-    const int tid = threadIdx.x, c16 = tid & 15, r0 = tid >> 4, kb_row = tid >> 1, half = tid & 1;
-    for (int64_t it = blockIdx.x; it < items && ok; it += gridDim.x) {
-      int side, a, m0;
-      locate(it, side, a, m0);
-      const GradSide& sd = p.side[side];
-      const int count = p.count[a], nk = (count + BK - 1) / BK;
-      const int32_t* order = p.order + p.begin[a];
-      const float sc = p.scale[a];
-      const int col = m0 + c16 * 8, left = sd.width - col;
-      const uint32_t bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;
-      for (int k = 0; k < nk; ++k, ++g) {
-        const uint32_t s = g % kGradStages, ph = (g / kGradStages) & 1;
-        if (!mbar_wait(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
-        const uint32_t st = smem_u32(smem + s * stage);
-        int64_t row[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) { const int at = k * BK + r0 + j * 8; row[j] = at < count ? order[at] : -1; }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int kr = r0 + j * 8;
-          const uint32_t to = st + (c16 >> 3) * (kTileBytesA / 2) + kr * 128 + (((c16 & 7) ^ (kr & 7)) << 4);
-          const uint32_t b = row[j] >= 0 ? bytes : 0;
-          cp_async_16(to, b ? sd.z + row[j] * sd.ldz + col : sd.z, b);
-        }
-        cp_async_commit();
-        // p of sample kb_row: every other piece of eight ranks
-        const int at = k * BK + kb_row;
-        const int64_t i = at < count ? order[at] : -1;
-        for (int ch = half; ch < rp / 8; ch += 2) {
-          uint32_t hi[4], lo[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float h[2], l[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int r = ch * 8 + j * 2 + e;
-              two_words(i >= 0 && r < p.rank ? sc * ranked(sd.p, i * p.rank + r) : 0.f, h[e], l[e]);
-            }
-            hi[j] = pack2(h[0], h[1]);
-            lo[j] = pack2(l[0], l[1]);
-          }
-          const uint32_t to = st + kTileBytesA + (ch >> 3) * 8192 + kb_row * 128 + (((ch & 7) ^ (kb_row & 7)) << 4);
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + word), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
-        }
-        if (g >= kGradLag) {
-          cp_async_wait<kGradLag>();
-          fence_proxy_async_smem();
-          mbar_arrive(&full[(g - kGradLag) % kGradStages]);
-        }
-      }
-    }
-    cp_async_wait<0>();
-    fence_proxy_async_smem();
-    if (ok)
-      for (uint32_t j = g > kGradLag ? g - kGradLag : 0; j < g; ++j) mbar_arrive(&full[j % kGradStages]);
+    if (p.stages >= 6) grad_load<4>(p, smem, full, empty, abort_flag, items0, items);
+    else if (p.stages >= 4) grad_load<2>(p, smem, full, empty, abort_flag, items0, items);
+    else grad_load<1>(p, smem, full, empty, abort_flag, items0, items);
   } else if (warp == 4) {
-    const uint32_t idesc = umma_idesc_bf16(BM, rp) | kIdescMnMajor;
-    uint32_t g = 0, i = 0;
+    // more than 256 columns: 192 (three panels), then the rest
+    const uint32_t n1 = N <= 256 ? N : 192, n2 = N - n1;
+    const uint32_t idesc1 = umma_idesc_bf16(BM, n1) | kIdescMnMajor, idesc2 = umma_idesc_bf16(BM, n2 ? n2 : 16) | kIdescMnMajor;
+    uint32_t s = 0, ph = 0, i = 0;
     bool ok = true;
     for (int64_t it = blockIdx.x; it < items && ok; it += gridDim.x) {
-      int side, a, m0;
-      locate(it, side, a, m0);
-      const int nk = (p.count[a] + BK - 1) / BK;
-      if (nk == 0) continue;
-      const uint32_t b = i & 1, bph = (i >> 1) & 1, d_tmem = tmem_base + b * 128;
-      ++i;
-      if (!mbar_wait_warp(&tempty[b], bph ^ 1, abort_flag)) { ok = false; break; }
-      tc_fence_after();
-      for (int k = 0; k < nk; ++k, ++g) {
-        const uint32_t s = g % kGradStages, ph = (g / kGradStages) & 1;
-        if (!mbar_wait_warp(&full[s], ph, abort_flag)) { ok = false; break; }
+      const int64_t in = it >= items0 ? it - items0 : it;
+      const int nk = (p.count[in / p.side[it >= items0].tiles] + BK - 1) / BK;
+      for (int k0 = 0; k0 < nk && ok; k0 += kDrain, ++i) {
+        const uint32_t b = i % buffers, bph = (i / buffers) & 1, d_tmem = tmem_base + b * 256;
+        if (!mbar_wait_warp(&tempty[b], bph ^ 1, abort_flag)) { ok = false; break; }
         tc_fence_after();
-        if (elect_one()) {
-          const uint32_t st = smem_u32(smem + s * stage);
-          const uint64_t da = umma_desc_mn128(st), dh = umma_desc_mn128(st + kTileBytesA), dl = umma_desc_mn128(st + kTileBytesA + word);
+        for (int k = k0; k < min(k0 + kDrain, nk); ++k) {
+          if (!mbar_wait_warp(&full[s], ph, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          if (elect_one()) {
+            const uint32_t st = smem_u32(smem + s * stage);
+            const uint64_t da = umma_desc_mn128(st), db = umma_desc_mn128(st + kTileBytesA), db2 = umma_desc_mn128(st + kTileBytesA + 3 * 8192);
 #pragma unroll
-          for (int j = 0; j < BK / 16; ++j) {
-            umma_bf16(d_tmem, da + 128 * j, dh + 128 * j, idesc, k | j ? 1u : 0u);
-            umma_bf16(d_tmem, da + 128 * j, dl + 128 * j, idesc, 1u);
+            for (int j = 0; j < BK / 16; ++j) {
+              umma_bf16(d_tmem, da + 128 * j, db + 128 * j, idesc1, (k - k0) | j ? 1u : 0u);
+              if (n2) umma_bf16(d_tmem + 192, da + 128 * j, db2 + 128 * j, idesc2, (k - k0) | j ? 1u : 0u);
+            }
+            umma_commit(&empty[s]);
           }
-          umma_commit(&empty[s]);
+          if (++s == static_cast<uint32_t>(p.stages)) { s = 0; ph ^= 1; }
         }
+        if (ok && elect_one()) umma_commit(&tfull[b]);
       }
-      if (ok && elect_one()) umma_commit(&tfull[b]);
     }
   } else {
     const int q = warp & 3;
     uint32_t i = 0;
-    for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-      int side, a, m0;
-      locate(it, side, a, m0);
+    bool ok = true;
+    for (int64_t it = blockIdx.x; it < items && ok; it += gridDim.x) {
+      const int side = it >= items0;
+      const int64_t in = side ? it - items0 : it;
       const GradSide& sd = p.side[side];
-      const bool any = p.count[a] > 0;
-      const uint32_t b = i & 1, bph = (i >> 1) & 1;
-      const int m = m0 + q * 32 + lane;
+      const int a = static_cast<int>(in / sd.tiles), m = static_cast<int>(in - static_cast<int64_t>(a) * sd.tiles) * BM + q * 32 + lane;
+      const int nk = (p.count[a] + BK - 1) / BK;
       float* out = sd.out + static_cast<int64_t>(a) * p.rank * sd.width + m;
-      if (any) {
-        ++i;
-        if (!mbar_wait_warp(&tfull[b], bph, abort_flag)) break;
+      if (nk == 0 && m < sd.width)
+        for (int r = 0; r < p.rank; ++r) out[static_cast<int64_t>(r) * sd.width] = 0.f;
+      for (int k0 = 0; k0 < nk; k0 += kDrain, ++i) {
+        const uint32_t b = i % buffers, bph = (i / buffers) & 1;
+        if (!mbar_wait_warp(&tfull[b], bph, abort_flag)) { ok = false; break; }
         tc_fence_after();
-      }
+        const uint32_t t_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + b * 256;
 #pragma unroll 1
-      for (int r0 = 0; r0 < p.rank; r0 += 32) {
-        uint32_t acc[32];
-#pragma unroll
-        for (int j = 0; j < 32; ++j) acc[j] = 0u;
-        if (any) {
-          tmem_ld_32x32(tmem_base + (static_cast<uint32_t>(q * 32) << 16) + b * 128 + r0, acc);
+        for (int r0 = 0; r0 < p.rank; r0 += 16) {
+          uint32_t w0[16], w1[16], w2[16];
+          tmem_ld_32x16(t_addr + r0, w0);
+          tmem_ld_32x16(t_addr + rp + r0, w1);
+          tmem_ld_32x16(t_addr + 2 * rp + r0, w2);
           tmem_ld_wait();
-        }
-        if (m < sd.width) {
+          if (m < sd.width) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (r0 + j < p.rank) out[static_cast<int64_t>(r0 + j) * sd.width] = __uint_as_float(acc[j]);
+            for (int j = 0; j < 16; ++j)
+              if (r0 + j < p.rank) {
+                float* to = out + static_cast<int64_t>(r0 + j) * sd.width;
+                const float v = __uint_as_float(w0[j]) + (__uint_as_float(w1[j]) + __uint_as_float(w2[j]));
+                *to = k0 ? *to + v : v;
+              }
+          }
         }
-      }
-      if (any) {
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&tempty[b]);
@@ -616,7 +1061,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
     for (int i = 0; i < 64; ++i) __nanosleep(1000);
     __syncthreads();
   }
-  if (warp == 4) { tc_fence_after(); tmem_dealloc(tmem_base, 256); }
+  if (warp == 4) { tc_fence_after(); tmem_dealloc(tmem_base, 512); }
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -639,7 +1084,7 @@ int64_t rank_rows(int64_t n, int64_t d) {
 }
 
 struct AdapterLayout {
-  size_t status, s, t, order, begin, count, total;
+  size_t status, ready, s, t, ssum, tsum, swords, twords, order, begin, count, lists, place, partial, total;
 };
 
 int check(const sfb_adapter_config* c) {
@@ -658,10 +1103,19 @@ AdapterLayout layout_of(const sfb_adapter_config& c) {
   AdapterLayout L{};
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t at = off; off += (bytes + kAlign - 1) / kAlign * kAlign; return at; };
+  const size_t n = static_cast<size_t>(c.max_samples), rp = (static_cast<size_t>(c.rank) + 15) / 16 * 16;
   L.status = take(4);
+  L.ready = take(kModelSms * kEpi * 4);              // cleared with the status word
   L.s = take(static_cast<size_t>(rank_rows(c.max_samples, c.cols)) * c.rank * 4);
   L.t = take(static_cast<size_t>(rank_rows(c.max_samples, c.rows)) * c.rank * 4);
-  L.order = take(static_cast<size_t>(c.max_samples) * 4);
+  L.ssum = take(n * c.rank * 4);
+  L.tsum = take(n * c.rank * 4);
+  L.swords = take(n * 3 * rp * 2);
+  L.twords = take(n * 3 * rp * 2);
+  L.lists = take((n / kMaxTile + 1) * kListPitch * 4);
+  L.place = take(n * 4);
+  L.partial = take(n > kFewMost ? static_cast<size_t>(kModelSms) * kPartFloats * 4 : 0);
+  L.order = take(n * 4);
   L.begin = take(static_cast<size_t>(c.adapters) * 4);
   L.count = take(static_cast<size_t>(c.adapters) * 4);
   L.total = off;
@@ -680,7 +1134,7 @@ struct sfb_adapters {
   const float* scale;
   char* ws;
   cudaStream_t stream;
-  int device, last_cuda;
+  int device, last_cuda, max_pairs;
   CUtensorMap mapU, mapV;              // boxes of 64 entries x 16 ranks of an adapter
   sfb::TcState* tc;
 
@@ -720,6 +1174,7 @@ cudaError_t rank_products(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz
   RankParams p{};
   p.n = static_cast<int32_t>(n); p.tn = tn; p.kseg = static_cast<int32_t>((d + BK - 1) / BK); p.stages = stages_of(tn);
   p.rank = h->cfg.rank; p.adapters = h->cfg.adapters; p.ids = ids; p.out = out; p.status = h->at<uint32_t>(h->lay.status);
+  if (n > kFewMost) { p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place); }
   const int per = (h->cfg.rank + kSlice - 1) / kSlice, chunks = (std::min(tn, h->cfg.adapters) * per + 7) / 8;
   const int groups = std::max(1, std::min(chunks, kModelSms / (parts * tiles)));
   const int smem = p.stages * stage_bytes(tn) + 1024;
@@ -729,35 +1184,94 @@ cudaError_t rank_products(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz
   return launch_kernel(adapter_rank_kernel, dim3(parts, tiles, groups), dim3(kRankThreads), smem, h->stream, 1, mapF, mz, p);
 }
 
-// CTAs of a cluster: as many as leave every SM one and each four k-blocks.
-int product_parts(int64_t tiles, int64_t kseg) {
+// CTAs of a cluster of adapter_few_kernel: as many as leave all of them a place, two an SM, and each four k-blocks.
+int few_parts(int64_t tiles, int64_t kseg) {
   int best = 1;
-  for (int s = 2; s <= 8; s *= 2)
-    if (tiles * s <= kModelSms && kseg >= 4 * s) best = s;
+  for (int s = 2; s <= kMaxCluster; ++s)
+    if (tiles * s <= 2 * kModelSms && kseg >= 4 * s) best = s;
+  return best;
+}
+
+template <int TN, bool MN>
+cudaError_t few(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const int32_t* ids, const Ranked& s, float* p_out, void* Y, int64_t ldy) {
+  const sfb_adapter_config& c = h->cfg;
+  const int64_t m = MN ? c.cols : c.rows, d = MN ? c.rows : c.cols;
+  CUtensorMap ma, mz;
+  if (!make_map(h->tc, &ma, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, const_cast<void*>(h->W), c.cols, c.rows, c.ldw * 2, BK, MN ? BK : BM) ||
+      !make_map(h->tc, &mz, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, const_cast<void*>(Z), d, n, ldz * 2, BK, TN))
+    return cudaErrorInvalidValue;
+  FewParams p{};
+  p.n = static_cast<int32_t>(n); p.m = static_cast<int32_t>(m);
+  p.kseg = static_cast<int32_t>((d + BK - 1) / BK);
+  const int64_t tiles = (m + BM - 1) / BM;
+  p.parts = few_parts(tiles, p.kseg);
+  p.rank = c.rank; p.adapters = c.adapters; p.ids = ids; p.scale = h->scale;
+  p.F = static_cast<const __nv_bfloat16*>(MN ? h->V : h->U); p.ldf = MN ? c.ldv : c.ldu;
+  p.p = s; p.p_out = p_out; p.Y = static_cast<__nv_bfloat16*>(Y); p.ldy = ldy; p.status = h->at<uint32_t>(h->lay.status);
+  const int terms = static_cast<int>(n) * c.rank * 4;
+  p.stages = std::min(kMaxStages, (kSmallRing + 8192 - std::min(terms, 24576)) / stage_bytes(TN));
+  const int smem = p.stages * stage_bytes(TN) + terms + 1024;
+  cudaError_t e = allow_smem<adapter_few_kernel<TN, MN>>(kMaxStages * stage_bytes(TN) + TN * SFB_ADAPTER_MAX_RANK * 4 + 1024);
+  if (e != cudaSuccess) return e;
+  return launch_kernel(adapter_few_kernel<TN, MN>, dim3(static_cast<unsigned>(tiles * p.parts)), dim3(kFewThreads), smem, h->stream, p.parts, ma, mz, p);
+}
+
+// Cycles of a plan of adapter_pair_kernel: its k-blocks on a pair, 7,000 to start and to end, 9,000 and 2,000 a part to leave and to take
+// over parts of tiles.
+struct PairPlan { int cut, whole, pairs; };
+PairPlan plan_pairs(int64_t tiles, int64_t kseg, int tn, int64_t most) {
+  const double per_kb = std::max(2.1 * tn, (BM + tn / 2) * BK * 2 / 60.0), tile = std::max(static_cast<double>(kseg) * per_kb, 8000.0 * tn / kMaxTile);
+  const int64_t rounds = (tiles + most - 1) / most, full = tiles / most, whole = std::max<int64_t>(0, full - 1) * most, rest = tiles - whole;
+  PairPlan best{0, 0, static_cast<int>(std::min(tiles, most))};
+  double cost = static_cast<double>(rounds) * tile + 7000.0;
+  const int64_t cap = full > 0 ? most : std::max<int64_t>(1, std::min(most, rest * kseg / 4));
+  for (int64_t parts = 2; (full > 0 && parts == 2) || (parts - 1) * rest < cap; ++parts) {
+    const int64_t pairs = full > 0 ? most : std::min(cap, parts * rest), shared = (rest * kseg + pairs - 1) / pairs;
+    const double c = static_cast<double>(whole / most) * tile + static_cast<double>(shared) * per_kb + 16000.0 + 2000.0 * static_cast<double>(parts);
+    if (c < cost && rest % pairs != 0) { cost = c; best = PairPlan{1, static_cast<int>(whole), static_cast<int>(pairs)}; }
+  }
   return best;
 }
 
 template <bool MN>
-cudaError_t product(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const int32_t* ids, const Ranked& s, float* p_out, void* Y, int64_t ldy) {
+cudaError_t pairs(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const int32_t* ids, const float* s, void* Y, int64_t ldy) {
   const sfb_adapter_config& c = h->cfg;
   const int64_t m = MN ? c.cols : c.rows, d = MN ? c.rows : c.cols;
   const int tn = tile_of(n);
   CUtensorMap ma, mz;
   if (!make_map(h->tc, &ma, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, const_cast<void*>(h->W), c.cols, c.rows, c.ldw * 2, BK, MN ? BK : BM) ||
-      !make_map(h->tc, &mz, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, const_cast<void*>(Z), d, n, ldz * 2, BK, tn))
+      !make_map(h->tc, &mz, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, const_cast<void*>(Z), d, n, ldz * 2, BK, tn / 2))
     return cudaErrorInvalidValue;
-  ProductParams p{};
-  p.n = static_cast<int32_t>(n); p.tn = tn; p.tiles = static_cast<int32_t>((n + tn - 1) / tn); p.m = static_cast<int32_t>(m);
-  p.kseg = static_cast<int32_t>((d + BK - 1) / BK); p.stages = stages_of(tn);
-  const int64_t tiles = (m + BM - 1) / BM * p.tiles;
-  p.parts = product_parts(tiles, p.kseg);
-  p.rank = c.rank; p.adapters = c.adapters; p.ids = ids; p.scale = h->scale;
-  p.F = static_cast<const __nv_bfloat16*>(MN ? h->V : h->U); p.ldf = MN ? c.ldv : c.ldu;
-  p.p = s; p.p_out = p_out; p.Y = static_cast<__nv_bfloat16*>(Y); p.ldy = ldy; p.status = h->at<uint32_t>(h->lay.status);
-  const int smem = p.stages * stage_bytes(tn) + 1024;
-  cudaError_t e = allow_smem<adapter_product_kernel<MN>>(kRing + 1024);
+  PairParams p{};
+  p.n = static_cast<int32_t>(n); p.tn = tn; p.tilesT = static_cast<int32_t>((n + tn - 1) / tn);
+  p.tilesM = static_cast<int32_t>((m + 2 * BM - 1) / (2 * BM)); p.m = static_cast<int32_t>(m);
+  p.kseg = static_cast<int32_t>((d + BK - 1) / BK);
+  const PairPlan plan = plan_pairs(static_cast<int64_t>(p.tilesT) * p.tilesM, p.kseg, tn, h->max_pairs);
+  p.cut = plan.cut; p.whole = plan.whole;
+  p.rank = c.rank; p.adapters = c.adapters; p.ids = ids; p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place);
+  p.scale = h->scale; p.F = static_cast<const __nv_bfloat16*>(MN ? h->V : h->U); p.ldf = MN ? c.ldv : c.ldu;
+  p.p = s; p.Y = static_cast<__nv_bfloat16*>(Y); p.ldy = ldy;
+  p.partial = h->at<float>(h->lay.partial); p.ready = h->at<uint32_t>(h->lay.ready); p.status = h->at<uint32_t>(h->lay.status);
+  return launch_kernel_if(static_cast<int64_t>(p.tilesT) * p.tilesM <= plan.pairs, adapter_pair_kernel<MN>, dim3(2u * static_cast<unsigned>(plan.pairs)),
+                          dim3(kPairThreads), kPairSmem, h->stream, 1, ma, mz, MN ? h->mapV : h->mapU, p);
+}
+
+cudaError_t sum_parts(sfb_adapters* h, const Ranked& s, const int32_t* ids, int64_t n, float* out) {
+  return launch_kernel(adapter_sum_kernel, dim3(grid1d(n * h->cfg.rank, 256)), dim3(256), 0, h->stream, 1, s, ids, n, h->cfg.rank, h->cfg.adapters, out);
+}
+
+// y = A z + scale F^T p; p_out (may be null) receives p; *s: p where it is afterwards.
+template <bool MN>
+cudaError_t product(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const int32_t* ids, Ranked* s, float* p_out, float* room, void* Y, int64_t ldy) {
+  if (n <= 16) return few<16, MN>(h, n, Z, ldz, ids, *s, p_out, Y, ldy);
+  if (n <= 32) return few<32, MN>(h, n, Z, ldz, ids, *s, p_out, Y, ldy);
+  if (n <= kFewMost) return few<kFewMost, MN>(h, n, Z, ldz, ids, *s, p_out, Y, ldy);
+  if (s->parts == 1 && !p_out) return pairs<MN>(h, n, Z, ldz, ids, s->at, Y, ldy);
+  float* to = p_out ? p_out : room;
+  cudaError_t e = sum_parts(h, *s, ids, n, to);
   if (e != cudaSuccess) return e;
-  return launch_kernel(adapter_product_kernel<MN>, dim3(static_cast<unsigned>(tiles * p.parts)), dim3(kProdThreads), smem, h->stream, p.parts, ma, mz, p);
+  *s = Ranked{to, 1, 0};
+  return pairs<MN>(h, n, Z, ldz, ids, to, Y, ldy);
 }
 
 int fail(sfb_adapters* h, cudaError_t e) {
@@ -818,8 +1332,11 @@ extern "C" int sfb_adapter_init(const sfb_adapter_config* cfg, const void* W_dev
   h->stream = static_cast<cudaStream_t>(cfg->stream);
   h->device = dev;
   h->last_cuda = 0;
+  h->max_pairs = std::min(sm_count(), kModelSms) / 2;
   if (!factor_map(h, &h->mapU, U_dev, c.rows, c.ldu) || !factor_map(h, &h->mapV, V_dev, c.cols, c.ldv) ||
-      cudaMemsetAsync(h->ws + lay.status, 0, 4, h->stream) != cudaSuccess) {
+      prepare_pair_kernel(adapter_pair_kernel<false>, kPairThreads, kPairSmem, &h->max_pairs) != cudaSuccess ||
+      prepare_pair_kernel(adapter_pair_kernel<true>, kPairThreads, kPairSmem, &h->max_pairs) != cudaSuccess || h->max_pairs < 1 ||
+      cudaMemsetAsync(h->ws + lay.status, 0, lay.s - lay.status, h->stream) != cudaSuccess) {
     sfb_adapter_destroy(h);
     return SFB_ERR_CUDA;
   }
@@ -840,7 +1357,7 @@ extern "C" int sfb_adapter_forward(sfb_adapters* h, int64_t n, const void* X_dev
   ACK(on.err);
   Ranked s{};
   ACK(rank_products(h, n, X_dev, ldx, c.cols, h->mapV, ids_dev, h->at<float>(h->lay.s), &s));
-  ACK(product<false>(h, n, X_dev, ldx, ids_dev, s, S_dev, Y_dev, ldy));
+  ACK(product<false>(h, n, X_dev, ldx, ids_dev, &s, S_dev, h->at<float>(h->lay.ssum), Y_dev, ldy));
   return SFB_OK;
 }
 
@@ -870,17 +1387,25 @@ extern "C" int sfb_adapter_backward(sfb_adapters* h, int64_t n, const void* dY_d
   Ranked s{S_dev, 1, 0}, t{};
   if (dU_dev && !S_dev) ACK(rank_products(h, n, X_dev, ldx, c.cols, h->mapV, ids_dev, h->at<float>(h->lay.s), &s));
   if (dX_dev || dV_dev) ACK(rank_products(h, n, dY_dev, lddy, c.rows, h->mapU, ids_dev, h->at<float>(h->lay.t), &t));
-  if (dX_dev) ACK(product<true>(h, n, dY_dev, lddy, ids_dev, t, nullptr, dX_dev, lddx));
+  if (dX_dev) ACK(product<true>(h, n, dY_dev, lddy, ids_dev, &t, nullptr, h->at<float>(h->lay.tsum), dX_dev, lddx));
   if (dU_dev || dV_dev) {
+    __nv_bfloat16 *swords = h->at<__nv_bfloat16>(h->lay.swords), *twords = h->at<__nv_bfloat16>(h->lay.twords);
+    WordsParams w{};
+    if (dU_dev) { w.p[0] = s; w.out[0] = swords; }
+    if (dV_dev) { w.p[1] = t; w.out[1] = twords; }
+    w.ids = ids_dev; w.order = order; w.begin = begin; w.count = count; w.scale = h->scale; w.rank = c.rank; w.adapters = c.adapters;
+    ACK(launch_kernel(adapter_words_kernel, dim3(grid1d(n * ((c.rank + 15) / 16 * 2), 256), 2), dim3(256), 0, h->stream, 1, w));
     GradParams p{};
     if (dU_dev)
-      p.side[0] = GradSide{static_cast<const __nv_bfloat16*>(dY_dev), lddy, static_cast<int32_t>(c.rows), static_cast<int32_t>((c.rows + BM - 1) / BM), s, dU_dev};
+      p.side[0] = GradSide{static_cast<const __nv_bfloat16*>(dY_dev), lddy, static_cast<int32_t>(c.rows), static_cast<int32_t>((c.rows + BM - 1) / BM), swords, dU_dev};
     if (dV_dev)
-      p.side[1] = GradSide{static_cast<const __nv_bfloat16*>(X_dev), ldx, static_cast<int32_t>(c.cols), static_cast<int32_t>((c.cols + BM - 1) / BM), t, dV_dev};
-    p.rank = c.rank; p.adapters = c.adapters; p.order = order; p.begin = begin; p.count = count; p.scale = h->scale; p.status = status;
+      p.side[1] = GradSide{static_cast<const __nv_bfloat16*>(X_dev), ldx, static_cast<int32_t>(c.cols), static_cast<int32_t>((c.cols + BM - 1) / BM), twords, dV_dev};
+    p.rank = c.rank; p.adapters = c.adapters; p.order = order; p.begin = begin; p.count = count; p.status = status;
     const int64_t items = (static_cast<int64_t>(p.side[0].tiles) + p.side[1].tiles) * c.adapters;
-    const int panels = ((c.rank + 15) / 16 * 16 + 63) / 64, smem = kGradStages * (kTileBytesA + 2 * panels * 8192) + 1024;
-    ACK(allow_smem<adapter_gradient_kernel>(kGradStages * (kTileBytesA + 4 * 8192) + 1024));
+    const int stage = kTileBytesA + grad_panels(c.rank) * 8192;
+    p.stages = std::min(kGradStages, kGradRing / stage);
+    const int smem = p.stages * stage + 1024;
+    ACK(allow_smem<adapter_gradient_kernel>(kGradRing + 1024));
     ACK(launch_kernel(adapter_gradient_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(items, sm_count()))), dim3(kGradThreads), smem, h->stream, 1, p));
   }
   return SFB_OK;
@@ -893,6 +1418,7 @@ extern "C" int sfb_adapter_get_status(sfb_adapters* h, uint32_t* status_out) {
   ACK(cudaMemcpyAsync(status_out, h->ws + h->lay.status, 4, cudaMemcpyDeviceToHost, h->stream));
   ACK(cudaMemsetAsync(h->ws + h->lay.status, 0, 4, h->stream));
   ACK(cudaStreamSynchronize(h->stream));
+  if (*status_out & SFB_STATUS_TIMEOUT) ACK(cudaMemsetAsync(h->ws + h->lay.ready, 0, h->lay.s - h->lay.ready, h->stream));
   return SFB_OK;
 }
 

@@ -4,8 +4,8 @@ Bounds, derived before the first run.  bf16 products are exact in fp32.  A tenso
 most one unit of the last place, 2^-23 of what the accumulator then holds, which is at most the sum M of the products' magnitudes:
 d / 16 instructions leave d / 16 * 2^-23 * M, fp32 sums of parts and ranks less than (16 + rank) * 2^-23 * M more.  A result is rounded
 once to bf16 (2^-8 of it) or fp32 (2^-24).  Where the adapter's term goes over the tensor cores, scale * s is rounded to bf16 first:
-2^-8 of sum |scale s_t u_t|.  For dU and dV s and t go as two words of bf16, 2^-16 of sum |scale s_i| |dy_i| at most, and both words are
-contracted: 2 * n / 16 instructions.
+2^-8 of sum |scale s_t u_t|.  For dU and dV scale * s and scale * t go as three words of bf16, 2^-24 of them
+at most, beside one rounding of the product with scale; the contraction is over the adapter's samples.
 """
 import pytest
 import torch
@@ -13,7 +13,7 @@ import torch
 import paper_1409_5705_b200 as S
 
 pytestmark = pytest.mark.gpu
-U23, U16, U8 = 2.0 ** -23, 2.0 ** -16, 2.0 ** -8
+U24, U23, U8 = 2.0 ** -24, 2.0 ** -23, 2.0 ** -8
 
 
 def padded(shape, gen, std=1.0, fill=float("nan"), extra=0):
@@ -92,8 +92,8 @@ class Case:
                 i = torch.nonzero(ids == a).flatten()
                 if len(i):
                     g[a] = (sc[i] * p[i]).t() @ Z[i]
-                    b[a] = (sc[i].abs() * (p[i].abs() * (U16 + (len(i) / 8 + 16) * U23) + pe[i])).t() @ Z[i].abs()
-            got[name] = (g, b + 2.0 ** -24 * g.abs())
+                    b[a] = (sc[i].abs() * (p[i].abs() * (2 * U24 + (len(i) / 16 + 16) * U23) + pe[i])).t() @ Z[i].abs()
+            got[name] = (g, b + U24 * g.abs())
         return got
 
     def run(self, given=True, plan=None, want=("dX", "dU", "dV")):
