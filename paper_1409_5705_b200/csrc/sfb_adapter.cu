@@ -98,9 +98,9 @@ __device__ __forceinline__ void build_list(TileList& L, const int32_t* ids, int 
 // p_i = F[a_i] z_i:  the adapters' factors as the rows of the accumulator, 16 ranks (a slice) of one adapter after another, the
 // samples of a tile as its columns; each sample takes the rows of its own adapter, so what another adapter or sample holds does not
 // reach it.  Grid: parts of the contraction x tiles of samples x groups of the tile's slices, eight slices at a time.
-// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..5 epilogue.
+// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..9 epilogue (TMEM lane quarter q; 32 of every 64 samples).
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kRankThreads = 192;
+constexpr int kRankThreads = 320;
 struct RankParams {
   int32_t n, tn, kseg, stages;
   int32_t rank, adapters;
@@ -125,7 +125,7 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
   const int cols = max(p.tn, 32), stage = stage_bytes(p.tn);
   if (threadIdx.x == 0) {
     for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 4); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 8); }
     abort_word = 0;
     fence_barrier_init();
     prefetch_tmap(&tmF); prefetch_tmap(&tmZ);
@@ -190,7 +190,7 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
       if (ok && elect_one()) umma_commit(&tfull[a]);
     }
   } else {
-    const int q = warp & 3;
+    const int q = warp & 3, h = (warp - 2) >> 2;
     float* out = p.out + static_cast<int64_t>(part) * p.n * p.rank;
     uint32_t i = 0;
     bool ok = true;
@@ -201,16 +201,22 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
       tc_fence_after();
       const int g = c * 8 + q * 2 + (lane >> 4), at = g < slices ? g / per : -2, r = (g - at * per) * kSlice + (lane & 15);
 #pragma unroll 1
-      for (int t0 = 0; t0 < p.tn; t0 += 32) {
+      for (int t0 = h * 32; t0 < p.tn; t0 += 64) {
+        uint32_t own = 0;                            // of these samples: those of this lane's adapter (places behind a tile of 16 are -1)
+#pragma unroll
+        for (int j = 0; j < 32; ++j) own |= (L.place[t0 + j] == at ? 1u : 0u) << j;
+        if (r >= p.rank) own = 0;
+        if (!__any_sync(0xffffffffu, own)) continue;
+        float* to = out + static_cast<int64_t>(first + t0) * p.rank + r;
+        float old[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) old[j] = k0 > kbeg && (own >> j & 1) ? to[static_cast<int64_t>(j) * p.rank] : 0.f;
         uint32_t acc[32];
         tmem_ld_32x32(tmem_base + (static_cast<uint32_t>(q * 32) << 16) + a * cols + t0, acc);
         tmem_ld_wait();
 #pragma unroll
-        for (int j = 0; j < 32; ++j)                 // (places behind a tile of 16 are -1)
-          if (L.place[t0 + j] == at && r < p.rank) {
-            float* to = out + static_cast<int64_t>(first + t0 + j) * p.rank + r;
-            *to = __uint_as_float(acc[j]) + (k0 > kbeg ? *to : 0.f);
-          }
+        for (int j = 0; j < 32; ++j)
+          if (own >> j & 1) to[static_cast<int64_t>(j) * p.rank] = __uint_as_float(acc[j]) + old[j];
       }
       tc_fence_before();
       __syncwarp();
@@ -415,7 +421,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // one's products.  Whole rounds of tiles are taken whole, the k-blocks of the rest are shared out (Segments in sfb_tile.cuh).
 //
 // The adapters' term is more contraction: behind the k-blocks of A the pair that finishes a tile takes the factors of the adapters in
-// the tile's list, four slices of 16 ranks a k-block, against  scale p  of the samples in bf16 (one rounding, 2^-8 of the term; the
+// the tile's list, eight units of 8 ranks a k-block, against  scale p  of the samples in bf16 (one rounding, 2^-8 of the term; the
 // result is rounded by as much), with zeros where a sample has another adapter.  Zeros do not hide what is not finite: so the warps that
 // write these operands look through the factors too, replace what is not finite by zeros, and the end of the tile adds those entries
 // alone, in fp32, to the samples of their own adapter.
@@ -423,6 +429,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // Warps: 0 TMA producer, 1 MMA issuer (leader CTA) and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the columns), 10..13
 // the samples' operand of the adapters' term.
 // ---------------------------------------------------------------------------------------------------------
+constexpr int kUnit = 8, kUnits = BK / kUnit;
 constexpr int kPairThreads = 448, kEpi = 8, kBuild = 4, kGroup = 8;      // kGroup: tiles of samples that follow one another
 constexpr int kPairStages = 6, kPairStage = 2 * kTileBytesA;
 constexpr int kPairSmem = kPairStages * kPairStage + 1024;
@@ -437,6 +444,7 @@ struct PairParams {
   const __nv_bfloat16* F;
   int64_t ldf;
   const float* p;              // [n][rank]
+  const __nv_bfloat16* pb;     // [n][rank rounded up to 8]: scale p, zeros behind
   __nv_bfloat16* Y;
   int64_t ldy;
   float* partial;              // [pairs][2][kPartFloats]
@@ -492,7 +500,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x >> 1, half = p.tn / 2;
   const Segments segs(p.kseg, p.cut != 0, p.whole, p.tilesT * p.tilesM, pair, gridDim.x >> 1);
-  const int per = (p.rank + kSlice - 1) / kSlice;
+  const int per = (p.rank + kUnit - 1) / kUnit;      // units of an adapter
   // Tiles that run at the same time: kGroup tiles of samples against as many rows of A as there are pairs for.
   auto tile_coords = [&](int tile, int& m0, int& tt) {
     const int in = kGroup * p.tilesM, g = tile / in, width = min(kGroup, p.tilesT - g * kGroup), at = tile - g * in;
@@ -530,7 +538,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       tile_coords(sg.tile, m0, tt);
       const int z0 = tt * p.tn + static_cast<int>(rank) * half;
       const int32_t* list = p.lists + static_cast<int64_t>(tt) * kListPitch;
-      const int slices = sg.k1 == p.kseg ? list[0] * per : 0, more = (slices + 3) / 4;
+      const int units = sg.k1 == p.kseg ? list[0] * per : 0, more = (units + kUnits - 1) / kUnits;
       for (int k = sg.k0; k < sg.k1 + more; ++k) {
         if (!mbar_wait_warp(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
         uint8_t* st = smem + s * kPairStage;
@@ -547,17 +555,15 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             tma_load_2d_pair(st + kTileBytesA, &tmZ, k * BK, z0, bar, pol);
           }
         } else {
-          const int g0 = (k - sg.k1) * 4, ns = min(4, slices - g0);
-          int a[4];
-          for (int j = 0; j < 4; ++j) a[j] = j < ns ? list[1 + (g0 + j) / per] : 0;
-          if (elect_one()) {
-            mbar_expect_tx(&landed[s], ns * 2 * kSlice * 128);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if (j >= ns) break;
-              const int y = (g0 + j) % per * kSlice;
-              tma_load_3d(st + j * (kSlice * 128), &tmF, m0, y, a[j], &landed[s]);
-              tma_load_3d(st + kTileBytesA / 2 + j * (kSlice * 128), &tmF, m0 + 64, y, a[j], &landed[s]);
+          const int g0 = (k - sg.k1) * kUnits, nu = min(kUnits, units - g0);
+          const int mine = lane < nu ? list[1 + (g0 + lane) / per] : 0;              // the adapter of unit `lane`
+          if (elect_one()) mbar_expect_tx(&landed[s], nu * 2 * kUnit * 128);
+          __syncwarp();
+          for (int j = 0; j < nu; ++j) {
+            const int a = __shfl_sync(0xffffffffu, mine, j), y = (g0 + j) % per * kUnit;
+            if (elect_one()) {
+              tma_load_3d(st + j * (kUnit * 128), &tmF, m0, y, a, &landed[s]);
+              tma_load_3d(st + kTileBytesA / 2 + j * (kUnit * 128), &tmF, m0 + 64, y, a, &landed[s]);
             }
           }
         }
@@ -574,7 +580,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         const Segment sg = segs.get(i);
         int m0, tt;
         tile_coords(sg.tile, m0, tt);
-        const int slices = sg.k1 == p.kseg ? p.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0, more = (slices + 3) / 4;
+        const int units = sg.k1 == p.kseg ? p.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0, more = (units + kUnits - 1) / kUnits;
         const uint32_t a = i & 1, aph = (i >> 1) & 1, d_tmem = tmem_base + a * kMaxTile;
         if (!mbar_wait_warp(&tempty[a], aph ^ 1, abort_flag)) { ok = false; break; }
         tc_fence_after();
@@ -594,7 +600,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             if (!mbar_wait_cluster(&built[s], (bph >> s) & 1, abort_flag)) { ok = false; break; }
             bph ^= 1u << s;
             tc_fence_after();
-            const int ns = min(4, slices - (k - sg.k1) * 4);
+            const int ns = (min(kUnits, units - (k - sg.k1) * kUnits) + 1) / 2;      // instructions: two units each
             if (elect_one()) {
               const uint64_t da = umma_desc_mn128(st), db = umma_desc_k128(st + kTileBytesA);
               for (int j = 0; j < ns; ++j) umma_bf16_pair(d_tmem, da + 128 * j, db + 2 * j, idesc_f, 1u);
@@ -700,54 +706,49 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       const uint32_t a = i & 1, aph = (i >> 1) & 1;
       if (!mbar_wait_warp(&taken[a], aph ^ 1, abort_flag)) { ok = false; break; }
       g += sg.k1 - sg.k0;
-      const int slices = sg.k1 == p.kseg ? p.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0, more = (slices + 3) / 4;
+      const int units = sg.k1 == p.kseg ? p.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0, more = (units + kUnits - 1) / kUnits;
       const int smp = tt * p.tn + static_cast<int>(rank) * half + t;
-      const int at = t < half && smp < p.n ? p.place[smp] : -1;
-      const float sc = at >= 0 ? p.scale[p.ids[smp]] : 0.f;
-      const float* src = p.p + static_cast<int64_t>(smp) * p.rank;
+      const int at = t < half && smp < p.n ? p.place[smp] * per : -1;                // this sample's first unit
+      const uint4* src = reinterpret_cast<const uint4*>(p.pb) + static_cast<int64_t>(smp) * per;
       uint32_t bad = 0;
       for (int k = 0; k < more; ++k, ++g) {
         const uint32_t s = g % kPairStages;
         uint8_t* st = smem + s * kPairStage;
-        const int g0 = k * 4, ns = min(4, slices - g0);
-        // scale p before the factors have landed: the stage is this k-block's once they have
-        uint32_t words[4][8];
+        const int g0 = k * kUnits, nu = min(kUnits, units - g0);
+        uint4 words[kUnits];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bool own = j < ns && at >= 0 && (g0 + j) / per == at;
-          const int r0 = (g0 + j) % per * kSlice;
-#pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const float x = own && r0 + 2 * u < p.rank ? sc * src[r0 + 2 * u] : 0.f, y = own && r0 + 2 * u + 1 < p.rank ? sc * src[r0 + 2 * u + 1] : 0.f;
-            const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
-            words[j][u] = *reinterpret_cast<const uint32_t*>(&v);
-          }
+        for (int j = 0; j < kUnits; ++j) {
+          const int u = g0 + j - at;                 // (a sample without an adapter has none: its place is below zero)
+          words[j] = at >= 0 && j < nu && u >= 0 && u < per ? src[u] : make_uint4(0, 0, 0, 0);
         }
         if (!mbar_wait_warp(&landed[s], (lph >> s) & 1, abort_flag)) { ok = false; break; }
         lph ^= 1u << s;
         if (t < half) {
           const uint32_t to = smem_u32(st) + kTileBytesA + t * 128;
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((2 * j + u) ^ (t & 7)) << 4)), "r"(words[j][4 * u]),
-                           "r"(words[j][4 * u + 1]), "r"(words[j][4 * u + 2]), "r"(words[j][4 * u + 3]) : "memory");
+          for (int j = 0; j < kUnits; ++j)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((j ^ (t & 7)) << 4)), "r"(words[j].x), "r"(words[j].y),
+                         "r"(words[j].z), "r"(words[j].w) : "memory");
         }
-        // the factors: ns slices of 2 KB in each of two panels
-        for (int x = t; x < ns * 256; x += 128) {
-          const int panel = x / (ns * 128), in = x - panel * ns * 128;
-          uint4* v = reinterpret_cast<uint4*>(st + panel * (kTileBytesA / 2)) + in;
-          uint4 f = *v;
-          uint32_t* fw = reinterpret_cast<uint32_t*>(&f);
-          uint32_t hit = 0;
+        // the factors, 1 KB a unit in each of two panels: looked through; beside an odd last unit zeros
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {              // bit 15 / 31: the exponent of the low / high half is all ones
-            const uint32_t b = ((fw[u] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-            hit |= b;
-            fw[u] &= ~((b >> 15) * 0xffffu);
+        for (int x = 0; x < kUnits; ++x) {
+          const int panel = x / (kUnits / 2), unit = x % (kUnits / 2) * 2 + (t >> 6);
+          uint4* v = reinterpret_cast<uint4*>(st + panel * (kTileBytesA / 2) + unit * (kUnit * 128)) + (t & 63);
+          if (unit < nu) {
+            uint4 f = *v;
+            uint32_t* fw = reinterpret_cast<uint32_t*>(&f);
+            uint32_t hit = 0;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {            // bit 15 / 31: the exponent of the low / high half is all ones
+              const uint32_t b = ((fw[u] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+              hit |= b;
+              fw[u] &= ~((b >> 15) * 0xffffu);
+            }
+            if (hit) { *v = f; bad = 1; }
+          } else if (unit == nu && (nu & 1)) {
+            *v = make_uint4(0, 0, 0, 0);
           }
-          if (hit) { *v = f; bad = 1; }
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -776,35 +777,53 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// p from its parts, zeros for a sample without an adapter.
+// p from its parts, zeros for a sample without an adapter, and scale p in bf16 as adapter_pair_kernel takes it (pb).
 // ---------------------------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(256) adapter_sum_kernel(Ranked p, const int32_t* ids, int64_t n, int32_t rank, int32_t adapters, float* out) {
+__global__ void __launch_bounds__(256) adapter_sum_kernel(Ranked p, const int32_t* ids, const float* scale, int64_t n, int32_t rank, int32_t adapters,
+                                                          float* out, __nv_bfloat16* pb) {
   pdl_launch_dependents();
   pdl_wait();
-  for (int64_t x = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; x < n * rank; x += static_cast<int64_t>(gridDim.x) * 256) {
-    const int id = ids[x / rank];
-    out[x] = id >= 0 && id < adapters ? ranked(p, x) : 0.f;
+  const int per = (rank + kUnit - 1) / kUnit;
+  for (int64_t x = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; x < n * per; x += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t i = x / per;
+    const int r0 = static_cast<int>(x - i * per) * kUnit, id = ids[i];
+    const bool has = id >= 0 && id < adapters;
+    const float sc = has ? scale[id] : 0.f;
+    float v[kUnit];
+#pragma unroll
+    for (int j = 0; j < kUnit; ++j) {
+      v[j] = has && r0 + j < rank ? ranked(p, i * rank + r0 + j) : 0.f;
+      if (r0 + j < rank) out[i * rank + r0 + j] = v[j];
+    }
+    uint32_t w[kUnit / 2];
+#pragma unroll
+    for (int j = 0; j < kUnit / 2; ++j) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(has ? sc * v[2 * j] : 0.f, has ? sc * v[2 * j + 1] : 0.f);
+      w[j] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    reinterpret_cast<uint4*>(pb)[x] = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// The samples of each adapter, one adapter after another, in their order: a warp per adapter goes over all ids, counts the samples
-// of lower adapters and its own, then writes its own.  No sample without an adapter is among them.
+// The samples of each adapter, one adapter after another, in their order: a block per adapter, each of its warps over an eighth of the
+// ids, counts the samples of lower adapters and its own, then writes its own.  No sample without an adapter is among them.
 // ---------------------------------------------------------------------------------------------------------
 __global__ void __launch_bounds__(256) adapter_index_kernel(const int32_t* ids, int32_t n, int32_t adapters, int32_t* order, int32_t* begin, int32_t* count,
                                                             uint32_t* status) {
   pdl_launch_dependents();
   pdl_wait();
-  const int a = static_cast<int>(blockIdx.x) * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (a >= adapters) return;
+  __shared__ int below_of[8], own_of[8];
+  const int a = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t share = (static_cast<int64_t>(n) + 1023) / 1024 * 128, from = warp * share, to = min(static_cast<int64_t>(n), from + share);
   int below = 0, own = 0;
   bool bad = false;
-  for (int64_t b = 0; b < n; b += 128) {
-    int id[4];
+  for (int64_t b = from; b < to; b += 256) {
+    int id[8];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) id[u] = b + u * 32 + lane < n ? ids[b + u * 32 + lane] : -1;
+    for (int u = 0; u < 8; ++u) id[u] = b + u * 32 + lane < to ? ids[b + u * 32 + lane] : -1;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < 8; ++u) {
       bad |= id[u] < -1 || id[u] >= adapters;
       below += id[u] >= 0 && id[u] < a;
       own += id[u] == a;
@@ -813,19 +832,25 @@ __global__ void __launch_bounds__(256) adapter_index_kernel(const int32_t* ids, 
   below = __reduce_add_sync(0xffffffffu, below);
   own = __reduce_add_sync(0xffffffffu, own);
   if (a == 0 && bad) atomicOr(status, SFB_STATUS_ADAPTER_RANGE);
-  if (lane == 0) { begin[a] = below; count[a] = own; }
-  int64_t at = below;
-  if (own > 0) {
-    for (int64_t b = 0; b < n; b += 128) {
-      int id[4];
+  if (lane == 0) { below_of[warp] = below; own_of[warp] = own; }
+  __syncthreads();
+  int64_t at = 0;
+  int total = 0;
+  for (int w = 0; w < 8; ++w) {
+    at += below_of[w] + (w < warp ? own_of[w] : 0);
+    total += own_of[w];
+  }
+  if (threadIdx.x == 0) { begin[a] = static_cast<int32_t>(at); count[a] = total; }
+  if (own == 0) return;
+  for (int64_t b = from; b < to; b += 256) {
+    int id[8];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) id[u] = b + u * 32 + lane < n ? ids[b + u * 32 + lane] : -1;
+    for (int u = 0; u < 8; ++u) id[u] = b + u * 32 + lane < to ? ids[b + u * 32 + lane] : -1;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const uint32_t m = __ballot_sync(0xffffffffu, id[u] == a);
-        if (id[u] == a) order[at + __popc(m & ((1u << lane) - 1))] = static_cast<int32_t>(b + u * 32 + lane);
-        at += __popc(m);
-      }
+    for (int u = 0; u < 8; ++u) {
+      const uint32_t m = __ballot_sync(0xffffffffu, id[u] == a);
+      if (id[u] == a) order[at + __popc(m & ((1u << lane) - 1))] = static_cast<int32_t>(b + u * 32 + lane);
+      at += __popc(m);
     }
   }
 }
@@ -838,9 +863,12 @@ struct WordsParams {
   Ranked p[2];                 // at null: not wanted
   __nv_bfloat16* out[2];
   const int32_t *ids, *order, *begin, *count;
+  int64_t* work;               // [adapters + 1]: what a column tile takes of the adapters before each one (see adapter_work)
   const float* scale;
   int32_t rank, adapters;
 };
+// What a tile of dF[a] costs, in k-blocks: its contraction, and its end.
+__device__ __forceinline__ int adapter_work(int count) { return (count + BK - 1) / BK + 1; }
 // v = w0 + w1 + w2.  (What overflows in the rounding to the first word is cut off instead; of what is not finite there is no rest.)
 __device__ __forceinline__ void three_words(float v, float (&w)[3]) {
   w[0] = __bfloat162float(__float2bfloat16_rn(v));
@@ -856,6 +884,34 @@ __global__ void __launch_bounds__(256) adapter_words_kernel(const __grid_constan
   const int rp = (p.rank + 15) & ~15, pieces = rp / 8;
   const int64_t total = static_cast<int64_t>(p.begin[p.adapters - 1] + p.count[p.adapters - 1]) * pieces;
   const int side = blockIdx.y;
+  if (side == 2) {
+    if (blockIdx.x > 0) return;
+    __shared__ int64_t sums[256];
+    const int each = (p.adapters + 255) / 256, from = min(static_cast<int>(threadIdx.x) * each, p.adapters), to = min(from + each, p.adapters);
+    int64_t s = 0;
+    for (int a = from; a < to; ++a) s += adapter_work(p.count[a]);
+    sums[threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.x < 32) {                          // a lane the eight sums from 8 * lane on
+      int64_t v[8], all = 0;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) { v[u] = all; all += sums[threadIdx.x * 8 + u]; }
+      int64_t before = all;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t x = __shfl_up_sync(0xffffffffu, before, o);
+        if (static_cast<int>(threadIdx.x) >= o) before += x;
+      }
+      before -= all;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) sums[threadIdx.x * 8 + u] = before + v[u];
+    }
+    __syncthreads();
+    s = sums[threadIdx.x];
+    for (int a = from; a < to; ++a) { p.work[a] = s; s += adapter_work(p.count[a]); }
+    if (to == p.adapters && from < to) p.work[p.adapters] = s;
+    return;
+  }
   if (!p.out[side]) return;
   for (int64_t x = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; x < total; x += static_cast<int64_t>(gridDim.x) * 256) {
     const int64_t at = x / pieces;
@@ -898,42 +954,89 @@ struct GradParams {
   GradSide side[2];
   int32_t rank, adapters, stages;
   const int32_t *order, *begin, *count;
+  const int64_t* work;
   uint32_t* status;
 };
 __host__ __device__ inline int grad_panels(int rank) { return (3 * ((rank + 15) / 16 * 16) + 63) / 64; }
 
+// A block's tiles: those whose work begins in its share of all work, the columns of an adapter one after another, so that a block
+// keeps an adapter's samples at hand.
+struct GradWalk {
+  const GradParams& p;
+  int side, a, tile, count, begin;
+  int64_t at, end;             // where the tile's work begins; the end of the block's share
+  __device__ __forceinline__ GradWalk(const GradParams& p_) : p(p_) {
+    const int64_t each = p.work[p.adapters], first = each * p.side[0].tiles, all = first + each * p.side[1].tiles;
+    at = all * blockIdx.x / gridDim.x;
+    end = all * (blockIdx.x + 1) / gridDim.x;
+    side = at >= first;
+    const int64_t base = side ? first : 0, tiles = p.side[side].tiles;
+    int lo = 0, hi = p.adapters - 1;                 // the last adapter whose work begins at or before `at`
+    while (at < end && lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (base + p.work[mid] * tiles <= at) lo = mid; else hi = mid - 1;
+    }
+    a = lo;
+    if (at >= end) return;
+    load();
+    const int64_t from = base + p.work[a] * tiles, w = adapter_work(count);
+    tile = static_cast<int>((at - from + w - 1) / w);
+    at = from + tile * w;
+    settle();
+  }
+  __device__ __forceinline__ void load() { count = p.count[a]; begin = p.begin[a]; }
+  __device__ __forceinline__ void settle() {
+    while (at < end && tile >= p.side[side].tiles) {
+      tile = 0;
+      if (++a == p.adapters) { a = 0; ++side; }
+      if (side > 1) { at = end; return; }
+      load();
+    }
+  }
+  __device__ __forceinline__ bool valid() const { return at < end; }
+  __device__ __forceinline__ void next() {
+    at += adapter_work(count);
+    ++tile;
+    settle();
+  }
+};
+
 template <int LAG>
-__device__ __forceinline__ void grad_load(const GradParams& p, uint8_t* smem, uint64_t* full, uint64_t* empty, volatile uint32_t* abort_flag, int64_t items0,
-                                          int64_t items) {
+__device__ __forceinline__ void grad_load(const GradParams& p, uint8_t* smem, uint64_t* full, uint64_t* empty, volatile uint32_t* abort_flag) {
   const int rp = (p.rank + 15) & ~15, pieces = 3 * rp / 8, stage = kTileBytesA + grad_panels(p.rank) * 8192, stages = p.stages;
   const int tid = threadIdx.x, c16 = tid & 15, r0 = tid >> 4;
   uint32_t g = 0, s = 0, ph = 0;                     // k-blocks so far; this one's stage and phase
   uint32_t back = 0;                                 // the stage of the k-block LAG ago
-  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-    const int side = it >= items0;
-    const int64_t in = side ? it - items0 : it;
-    const GradSide& sd = p.side[side];
-    const int a = static_cast<int>(in / sd.tiles), m0 = static_cast<int>(in - static_cast<int64_t>(a) * sd.tiles) * BM;
-    const int count = p.count[a], begin = p.begin[a], nk = (count + BK - 1) / BK;
-    const int col = m0 + c16 * 8, left = sd.width - col;
+  int known = -1, known_k = -1;                      // the adapter and the k-block of the samples in row
+  int32_t row[8];
+  for (GradWalk it(p); it.valid(); it.next()) {
+    const GradSide& sd = p.side[it.side];
+    const int nk = (it.count + BK - 1) / BK;
+    const int col = it.tile * BM + c16 * 8, left = sd.width - col;
     const uint32_t bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;
     for (int k = 0; k < nk; ++k, ++g) {
-      int64_t row[8];
+      if (known != it.a || known_k != k) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) { const int at = k * BK + r0 + j * 8; row[j] = at < count ? p.order[begin + at] : -1; }
+        for (int j = 0; j < 8; ++j) { const int at = k * BK + r0 + j * 8; row[j] = at < it.count ? p.order[it.begin + at] : -1; }
+        known = it.a;
+        known_k = k;
+      }
+      const int rows = min(BK, (it.count - k * BK + 15) & ~15);       // whole instructions of 16
       if (!mbar_wait(&empty[s], ph ^ 1, abort_flag)) return;
       const uint32_t st = smem_u32(smem + s * stage);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int kr = r0 + j * 8;
+        if (kr >= rows) break;
         const uint32_t b = row[j] >= 0 ? bytes : 0;
-        cp_async_16(st + (c16 >> 3) * (kTileBytesA / 2) + kr * 128 + (((c16 & 7) ^ (kr & 7)) << 4), b ? sd.z + row[j] * sd.ldz + col : sd.z, b);
+        cp_async_16(st + (c16 >> 3) * (kTileBytesA / 2) + kr * 128 + (((c16 & 7) ^ (kr & 7)) << 4),
+                    b ? sd.z + static_cast<int64_t>(row[j]) * sd.ldz + col : sd.z, b);
       }
-      for (int x = tid; x < BK * pieces; x += 128) {
+      for (int x = tid; x < rows * pieces; x += 128) {
         const int kr = x / pieces, ch = x - kr * pieces, at = k * BK + kr;
-        const uint32_t b = at < count ? 16 : 0;
+        const uint32_t b = at < it.count ? 16 : 0;
         cp_async_16(st + kTileBytesA + (ch >> 3) * 8192 + kr * 128 + (((ch & 7) ^ (kr & 7)) << 4),
-                    sd.words + (b ? (static_cast<int64_t>(begin) + at) * 3 * rp + ch * 8 : 0), b);
+                    sd.words + (b ? (static_cast<int64_t>(it.begin) + at) * 3 * rp + ch * 8 : 0), b);
       }
       cp_async_commit();
       if (g >= LAG) {
@@ -975,21 +1078,19 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
   tc_fence_after();
   const uint32_t tmem_base = tmem_slot;
   pdl_wait();
-  const int64_t items0 = static_cast<int64_t>(p.side[0].tiles) * p.adapters, items = items0 + static_cast<int64_t>(p.side[1].tiles) * p.adapters;
 
   if (warp < 4) {
-    if (p.stages >= 6) grad_load<4>(p, smem, full, empty, abort_flag, items0, items);
-    else if (p.stages >= 4) grad_load<2>(p, smem, full, empty, abort_flag, items0, items);
-    else grad_load<1>(p, smem, full, empty, abort_flag, items0, items);
+    if (p.stages >= 6) grad_load<4>(p, smem, full, empty, abort_flag);
+    else if (p.stages >= 4) grad_load<2>(p, smem, full, empty, abort_flag);
+    else grad_load<1>(p, smem, full, empty, abort_flag);
   } else if (warp == 4) {
     // more than 256 columns: 192 (three panels), then the rest
     const uint32_t n1 = N <= 256 ? N : 192, n2 = N - n1;
     const uint32_t idesc1 = umma_idesc_bf16(BM, n1) | kIdescMnMajor, idesc2 = umma_idesc_bf16(BM, n2 ? n2 : 16) | kIdescMnMajor;
     uint32_t s = 0, ph = 0, i = 0;
     bool ok = true;
-    for (int64_t it = blockIdx.x; it < items && ok; it += gridDim.x) {
-      const int64_t in = it >= items0 ? it - items0 : it;
-      const int nk = (p.count[in / p.side[it >= items0].tiles] + BK - 1) / BK;
+    for (GradWalk it(p); it.valid() && ok; it.next()) {
+      const int nk = (it.count + BK - 1) / BK;
       for (int k0 = 0; k0 < nk && ok; k0 += kDrain, ++i) {
         const uint32_t b = i % buffers, bph = (i / buffers) & 1, d_tmem = tmem_base + b * 256;
         if (!mbar_wait_warp(&tempty[b], bph ^ 1, abort_flag)) { ok = false; break; }
@@ -997,11 +1098,11 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
         for (int k = k0; k < min(k0 + kDrain, nk); ++k) {
           if (!mbar_wait_warp(&full[s], ph, abort_flag)) { ok = false; break; }
           tc_fence_after();
+          const int steps = min(BK / 16, (it.count - k * BK + 15) / 16);
           if (elect_one()) {
             const uint32_t st = smem_u32(smem + s * stage);
             const uint64_t da = umma_desc_mn128(st), db = umma_desc_mn128(st + kTileBytesA), db2 = umma_desc_mn128(st + kTileBytesA + 3 * 8192);
-#pragma unroll
-            for (int j = 0; j < BK / 16; ++j) {
+            for (int j = 0; j < steps; ++j) {
               umma_bf16(d_tmem, da + 128 * j, db + 128 * j, idesc1, (k - k0) | j ? 1u : 0u);
               if (n2) umma_bf16(d_tmem + 192, da + 128 * j, db2 + 128 * j, idesc2, (k - k0) | j ? 1u : 0u);
             }
@@ -1016,13 +1117,10 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
     const int q = warp & 3;
     uint32_t i = 0;
     bool ok = true;
-    for (int64_t it = blockIdx.x; it < items && ok; it += gridDim.x) {
-      const int side = it >= items0;
-      const int64_t in = side ? it - items0 : it;
-      const GradSide& sd = p.side[side];
-      const int a = static_cast<int>(in / sd.tiles), m = static_cast<int>(in - static_cast<int64_t>(a) * sd.tiles) * BM + q * 32 + lane;
-      const int nk = (p.count[a] + BK - 1) / BK;
-      float* out = sd.out + static_cast<int64_t>(a) * p.rank * sd.width + m;
+    for (GradWalk it(p); it.valid() && ok; it.next()) {
+      const GradSide& sd = p.side[it.side];
+      const int m = it.tile * BM + q * 32 + lane, nk = (it.count + BK - 1) / BK;
+      float* out = sd.out + static_cast<int64_t>(it.a) * p.rank * sd.width + m;
       if (nk == 0 && m < sd.width)
         for (int r = 0; r < p.rank; ++r) out[static_cast<int64_t>(r) * sd.width] = 0.f;
       for (int k0 = 0; k0 < nk; k0 += kDrain, ++i) {
@@ -1033,6 +1131,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
 #pragma unroll 1
         for (int r0 = 0; r0 < p.rank; r0 += 16) {
           uint32_t w0[16], w1[16], w2[16];
+          float old[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) old[j] = k0 && m < sd.width && r0 + j < p.rank ? out[static_cast<int64_t>(r0 + j) * sd.width] : 0.f;
           tmem_ld_32x16(t_addr + r0, w0);
           tmem_ld_32x16(t_addr + rp + r0, w1);
           tmem_ld_32x16(t_addr + 2 * rp + r0, w2);
@@ -1040,11 +1141,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
           if (m < sd.width) {
 #pragma unroll
             for (int j = 0; j < 16; ++j)
-              if (r0 + j < p.rank) {
-                float* to = out + static_cast<int64_t>(r0 + j) * sd.width;
-                const float v = __uint_as_float(w0[j]) + (__uint_as_float(w1[j]) + __uint_as_float(w2[j]));
-                *to = k0 ? *to + v : v;
-              }
+              if (r0 + j < p.rank)
+                out[static_cast<int64_t>(r0 + j) * sd.width] = __uint_as_float(w0[j]) + (__uint_as_float(w1[j]) + __uint_as_float(w2[j])) + old[j];
           }
         }
         tc_fence_before();
@@ -1084,7 +1182,7 @@ int64_t rank_rows(int64_t n, int64_t d) {
 }
 
 struct AdapterLayout {
-  size_t status, ready, s, t, ssum, tsum, swords, twords, order, begin, count, lists, place, partial, total;
+  size_t status, ready, s, t, ssum, tsum, pb, swords, twords, order, begin, count, work, lists, place, partial, total;
 };
 
 int check(const sfb_adapter_config* c) {
@@ -1110,6 +1208,7 @@ AdapterLayout layout_of(const sfb_adapter_config& c) {
   L.t = take(static_cast<size_t>(rank_rows(c.max_samples, c.rows)) * c.rank * 4);
   L.ssum = take(n * c.rank * 4);
   L.tsum = take(n * c.rank * 4);
+  L.pb = take(n * ((static_cast<size_t>(c.rank) + kUnit - 1) / kUnit) * kUnit * 2);
   L.swords = take(n * 3 * rp * 2);
   L.twords = take(n * 3 * rp * 2);
   L.lists = take((n / kMaxTile + 1) * kListPitch * 4);
@@ -1117,6 +1216,7 @@ AdapterLayout layout_of(const sfb_adapter_config& c) {
   L.partial = take(n > kFewMost ? static_cast<size_t>(kModelSms) * kPartFloats * 4 : 0);
   L.order = take(n * 4);
   L.begin = take(static_cast<size_t>(c.adapters) * 4);
+  L.work = take((static_cast<size_t>(c.adapters) + 1) * 8);
   L.count = take(static_cast<size_t>(c.adapters) * 4);
   L.total = off;
   return L;
@@ -1136,6 +1236,7 @@ struct sfb_adapters {
   cudaStream_t stream;
   int device, last_cuda, max_pairs;
   CUtensorMap mapU, mapV;              // boxes of 64 entries x 16 ranks of an adapter
+  CUtensorMap unitU, unitV;            // x 8 ranks
   sfb::TcState* tc;
 
   template <typename T>
@@ -1157,10 +1258,10 @@ struct OnDevice {                      // the handle's device is current for the
   }
 };
 
-bool factor_map(sfb_adapters* h, CUtensorMap* m, const void* base, int64_t width, int64_t pitch) {
+bool factor_map(sfb_adapters* h, CUtensorMap* m, const void* base, int64_t width, int64_t pitch, int ranks) {
   cuuint64_t dims[3] = {static_cast<cuuint64_t>(width), static_cast<cuuint64_t>(h->cfg.rank), static_cast<cuuint64_t>(h->cfg.adapters)};
   cuuint64_t strides[2] = {static_cast<cuuint64_t>(pitch) * 2, static_cast<cuuint64_t>(pitch) * 2 * h->cfg.rank};
-  cuuint32_t box[3] = {BK, kSlice, 1}, estr[3] = {1, 1, 1};
+  cuuint32_t box[3] = {BK, static_cast<cuuint32_t>(ranks), 1}, estr[3] = {1, 1, 1};
   return h->tc->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -1250,14 +1351,10 @@ cudaError_t pairs(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const 
   p.cut = plan.cut; p.whole = plan.whole;
   p.rank = c.rank; p.adapters = c.adapters; p.ids = ids; p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place);
   p.scale = h->scale; p.F = static_cast<const __nv_bfloat16*>(MN ? h->V : h->U); p.ldf = MN ? c.ldv : c.ldu;
-  p.p = s; p.Y = static_cast<__nv_bfloat16*>(Y); p.ldy = ldy;
+  p.p = s; p.pb = h->at<__nv_bfloat16>(h->lay.pb); p.Y = static_cast<__nv_bfloat16*>(Y); p.ldy = ldy;
   p.partial = h->at<float>(h->lay.partial); p.ready = h->at<uint32_t>(h->lay.ready); p.status = h->at<uint32_t>(h->lay.status);
   return launch_kernel_if(static_cast<int64_t>(p.tilesT) * p.tilesM <= plan.pairs, adapter_pair_kernel<MN>, dim3(2u * static_cast<unsigned>(plan.pairs)),
-                          dim3(kPairThreads), kPairSmem, h->stream, 1, ma, mz, MN ? h->mapV : h->mapU, p);
-}
-
-cudaError_t sum_parts(sfb_adapters* h, const Ranked& s, const int32_t* ids, int64_t n, float* out) {
-  return launch_kernel(adapter_sum_kernel, dim3(grid1d(n * h->cfg.rank, 256)), dim3(256), 0, h->stream, 1, s, ids, n, h->cfg.rank, h->cfg.adapters, out);
+                          dim3(kPairThreads), kPairSmem, h->stream, 1, ma, mz, MN ? h->unitV : h->unitU, p);
 }
 
 // y = A z + scale F^T p; p_out (may be null) receives p; *s: p where it is afterwards.
@@ -1266,9 +1363,10 @@ cudaError_t product(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, cons
   if (n <= 16) return few<16, MN>(h, n, Z, ldz, ids, *s, p_out, Y, ldy);
   if (n <= 32) return few<32, MN>(h, n, Z, ldz, ids, *s, p_out, Y, ldy);
   if (n <= kFewMost) return few<kFewMost, MN>(h, n, Z, ldz, ids, *s, p_out, Y, ldy);
-  if (s->parts == 1 && !p_out) return pairs<MN>(h, n, Z, ldz, ids, s->at, Y, ldy);
   float* to = p_out ? p_out : room;
-  cudaError_t e = sum_parts(h, *s, ids, n, to);
+  const sfb_adapter_config& c = h->cfg;
+  const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(grid1d(n * ((c.rank + kUnit - 1) / kUnit), 256)), dim3(256), 0, h->stream, 1, *s, ids, h->scale,
+                                      n, c.rank, c.adapters, to, h->at<__nv_bfloat16>(h->lay.pb));
   if (e != cudaSuccess) return e;
   *s = Ranked{to, 1, 0};
   return pairs<MN>(h, n, Z, ldz, ids, to, Y, ldy);
@@ -1333,7 +1431,8 @@ extern "C" int sfb_adapter_init(const sfb_adapter_config* cfg, const void* W_dev
   h->device = dev;
   h->last_cuda = 0;
   h->max_pairs = std::min(sm_count(), kModelSms) / 2;
-  if (!factor_map(h, &h->mapU, U_dev, c.rows, c.ldu) || !factor_map(h, &h->mapV, V_dev, c.cols, c.ldv) ||
+  if (!factor_map(h, &h->mapU, U_dev, c.rows, c.ldu, kSlice) || !factor_map(h, &h->mapV, V_dev, c.cols, c.ldv, kSlice) ||
+      !factor_map(h, &h->unitU, U_dev, c.rows, c.ldu, kUnit) || !factor_map(h, &h->unitV, V_dev, c.cols, c.ldv, kUnit) ||
       prepare_pair_kernel(adapter_pair_kernel<false>, kPairThreads, kPairSmem, &h->max_pairs) != cudaSuccess ||
       prepare_pair_kernel(adapter_pair_kernel<true>, kPairThreads, kPairSmem, &h->max_pairs) != cudaSuccess || h->max_pairs < 1 ||
       cudaMemsetAsync(h->ws + lay.status, 0, lay.s - lay.status, h->stream) != cudaSuccess) {
@@ -1382,7 +1481,7 @@ extern "C" int sfb_adapter_backward(sfb_adapters* h, int64_t n, const void* dY_d
   uint32_t* status = h->at<uint32_t>(h->lay.status);
   int32_t *order = h->at<int32_t>(h->lay.order), *begin = h->at<int32_t>(h->lay.begin), *count = h->at<int32_t>(h->lay.count);
   if (dU_dev || dV_dev)
-    ACK(launch_kernel(adapter_index_kernel, dim3((c.adapters + 7) / 8), dim3(256), 0, h->stream, 1, ids_dev, static_cast<int32_t>(n), c.adapters, order,
+    ACK(launch_kernel(adapter_index_kernel, dim3(c.adapters), dim3(256), 0, h->stream, 1, ids_dev, static_cast<int32_t>(n), c.adapters, order,
                       begin, count, status));
   Ranked s{S_dev, 1, 0}, t{};
   if (dU_dev && !S_dev) ACK(rank_products(h, n, X_dev, ldx, c.cols, h->mapV, ids_dev, h->at<float>(h->lay.s), &s));
@@ -1393,14 +1492,14 @@ extern "C" int sfb_adapter_backward(sfb_adapters* h, int64_t n, const void* dY_d
     WordsParams w{};
     if (dU_dev) { w.p[0] = s; w.out[0] = swords; }
     if (dV_dev) { w.p[1] = t; w.out[1] = twords; }
-    w.ids = ids_dev; w.order = order; w.begin = begin; w.count = count; w.scale = h->scale; w.rank = c.rank; w.adapters = c.adapters;
-    ACK(launch_kernel(adapter_words_kernel, dim3(grid1d(n * ((c.rank + 15) / 16 * 2), 256), 2), dim3(256), 0, h->stream, 1, w));
+    w.ids = ids_dev; w.order = order; w.begin = begin; w.count = count; w.work = h->at<int64_t>(h->lay.work); w.scale = h->scale; w.rank = c.rank; w.adapters = c.adapters;
+    ACK(launch_kernel(adapter_words_kernel, dim3(grid1d(n * ((c.rank + 15) / 16 * 2), 256), 3), dim3(256), 0, h->stream, 1, w));
     GradParams p{};
     if (dU_dev)
       p.side[0] = GradSide{static_cast<const __nv_bfloat16*>(dY_dev), lddy, static_cast<int32_t>(c.rows), static_cast<int32_t>((c.rows + BM - 1) / BM), swords, dU_dev};
     if (dV_dev)
       p.side[1] = GradSide{static_cast<const __nv_bfloat16*>(X_dev), ldx, static_cast<int32_t>(c.cols), static_cast<int32_t>((c.cols + BM - 1) / BM), twords, dV_dev};
-    p.rank = c.rank; p.adapters = c.adapters; p.order = order; p.begin = begin; p.count = count; p.status = status;
+    p.rank = c.rank; p.adapters = c.adapters; p.order = order; p.begin = begin; p.count = count; p.work = w.work; p.status = status;
     const int64_t items = (static_cast<int64_t>(p.side[0].tiles) + p.side[1].tiles) * c.adapters;
     const int stage = kTileBytesA + grad_panels(c.rank) * 8192;
     p.stages = std::min(kGradStages, kGradRing / stage);
