@@ -106,8 +106,10 @@ struct RankParams {
   int32_t rank, adapters;
   const int32_t* ids;
   float* out;                  // [parts][n][rank]
-  int32_t* lists;              // may be null: [tiles][kListPitch], and per sample its place in its tile's list
+  int32_t* lists;              // may be null: [tiles][kListPitch], per sample its place in its tile's list,
   int32_t* place;
+  int32_t* mark;               // and for each adapter in a list, `call`
+  int32_t call;
   uint32_t* status;
 };
 
@@ -143,7 +145,7 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
     int32_t* to = p.lists + static_cast<int64_t>(blockIdx.y) * kListPitch;
     if (threadIdx.x == 0) to[0] = L.count;
     for (int t = threadIdx.x; t < p.tn; t += kRankThreads) {
-      if (t < L.count) to[1 + t] = L.list[t];
+      if (t < L.count) { to[1 + t] = L.list[t]; p.mark[L.list[t]] = p.call; }
       if (first + t < p.n) p.place[first + t] = L.place[t];
     }
   }
@@ -422,9 +424,9 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 //
 // The adapters' term is more contraction: behind the k-blocks of A the pair that finishes a tile takes the factors of the adapters in
 // the tile's list, eight units of 8 ranks a k-block, against  scale p  of the samples in bf16 (one rounding, 2^-8 of the term; the
-// result is rounded by as much), with zeros where a sample has another adapter.  Zeros do not hide what is not finite: so the warps that
-// write these operands look through the factors too, replace what is not finite by zeros, and the end of the tile adds those entries
-// alone, in fp32, to the samples of their own adapter.
+// result is rounded by as much), with zeros where a sample has another adapter.  Zeros do not hide what is not finite: adapter_sum_kernel
+// has looked through the factors, and one that holds such entries is not loaded (its units are out of the map's bounds, zeros); the end
+// of the tile forms the term of its own samples in fp32.
 //
 // Warps: 0 TMA producer, 1 MMA issuer (leader CTA) and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the columns), 10..13
 // the samples' operand of the adapters' term.
@@ -441,6 +443,7 @@ struct PairParams {
   const int32_t* ids;
   const int32_t *lists, *place;
   const float* scale;
+  const uint4* bad;            // [adapters]: not zero where the factors are not finite
   const __nv_bfloat16* F;
   int64_t ldf;
   const float* p;              // [n][rank]
@@ -471,17 +474,16 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity
   return __all_sync(0xffffffffu, got);
 }
 
-// What is not finite of the adapter's term of sample i at row m.
-__device__ __noinline__ float not_finite_term(const PairParams& p, int i, int m) {
+__device__ __forceinline__ bool is_bad(const uint4& b) { return (b.x | b.y | b.z | b.w) != 0; }
+// The adapter's term of sample i at row m, where its factors are not finite; else 0.
+__device__ __noinline__ float bad_term(const PairParams& p, int i, int m) {
   const int id = p.ids[i];
-  if (id < 0 || id >= p.adapters) return 0.f;
+  if (id < 0 || id >= p.adapters || !is_bad(p.bad[id])) return 0.f;
   const __nv_bfloat16* f = p.F + static_cast<int64_t>(id) * p.rank * p.ldf + m;
   const float* s = p.p + static_cast<int64_t>(i) * p.rank;
+  const float sc = p.scale[id];
   float v = 0.f;
-  for (int r = 0; r < p.rank; ++r) {
-    const float x = __bfloat162float(f[r * p.ldf]);
-    if (!isfinite(x)) v += p.scale[id] * s[r] * x;
-  }
+  for (int r = 0; r < p.rank; ++r) v = fmaf(__bfloat162float(f[r * p.ldf]), sc * s[r], v);
   return v;
 }
 
@@ -491,9 +493,10 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
                     const __grid_constant__ PairParams p) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kPairStages], empty[kPairStages];       // full, built, tempty: the leader's are in use
-  __shared__ uint64_t landed[kPairStages], built[kPairStages];     // a k-block of factors has landed here; both CTAs have made it an operand
-  __shared__ uint64_t tfull[2], tempty[2], looked[2], taken[2];    // looked: what is not finite of a tile is known; taken: read
-  __shared__ uint32_t tmem_slot, abort_word, odd[2][kBuild];
+  __shared__ uint64_t free_[kPairStages], built[kPairStages];      // of a k-block of factors: the stage is free for the samples' operand;
+                                                                   // both CTAs have written it
+  __shared__ uint64_t tfull[2], tempty[2];
+  __shared__ uint32_t tmem_slot, abort_word;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   volatile uint32_t* abort_flag = &abort_word;
   const int warp = warp_index(), lane = threadIdx.x & 31;
@@ -511,9 +514,9 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kPairStages; ++i) {
-      mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&landed[i], 1); mbar_init(&built[i], 2 * kBuild);
+      mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&built[i], 2 * kBuild);
     }
-    for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 2 * kEpi); mbar_init(&looked[i], kBuild); mbar_init(&taken[i], kEpi); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 2 * kEpi); }
     abort_word = 0;
     fence_barrier_init();
     prefetch_tmap(&tmA); prefetch_tmap(&tmZ); prefetch_tmap(&tmF);
@@ -539,6 +542,13 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       const int z0 = tt * p.tn + static_cast<int>(rank) * half;
       const int32_t* list = p.lists + static_cast<int64_t>(tt) * kListPitch;
       const int units = sg.k1 == p.kseg ? list[0] * per : 0, more = (units + kUnits - 1) / kUnits;
+      // the adapter of unit g (out of bounds where it is bad); of four k-blocks by the lanes
+      auto adapter_of = [&](int g) {
+        if (g >= units) return 0;
+        const int a = list[1 + g / per];
+        return is_bad(p.bad[a]) ? p.adapters : a;
+      };
+      int known = adapter_of(lane);
       for (int k = sg.k0; k < sg.k1 + more; ++k) {
         if (!mbar_wait_warp(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
         uint8_t* st = smem + s * kPairStage;
@@ -556,16 +566,19 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
           }
         } else {
           const int g0 = (k - sg.k1) * kUnits, nu = min(kUnits, units - g0);
-          const int mine = lane < nu ? list[1 + (g0 + lane) / per] : 0;              // the adapter of unit `lane`
-          if (elect_one()) mbar_expect_tx(&landed[s], nu * 2 * kUnit * 128);
-          __syncwarp();
+          if (elect_one()) {
+            mbar_arrive(&free_[s]);
+            if (rank == 0) mbar_expect_tx(&full[s], 2 * nu * 2 * kUnit * 128);
+          }
+          const uint32_t bar = mapa_u32(smem_u32(&full[s]), 0);
           for (int j = 0; j < nu; ++j) {
-            const int a = __shfl_sync(0xffffffffu, mine, j), y = (g0 + j) % per * kUnit;
+            const int a = __shfl_sync(0xffffffffu, known, (g0 + j) & 31), y = (g0 + j) % per * kUnit;
             if (elect_one()) {
-              tma_load_3d(st + j * (kUnit * 128), &tmF, m0, y, a, &landed[s]);
-              tma_load_3d(st + kTileBytesA / 2 + j * (kUnit * 128), &tmF, m0 + 64, y, a, &landed[s]);
+              tma_load_3d_pair(st + j * (kUnit * 128), &tmF, m0, y, a, bar);
+              tma_load_3d_pair(st + kTileBytesA / 2 + j * (kUnit * 128), &tmF, m0 + 64, y, a, bar);
             }
           }
+          if (((g0 + kUnits) & 31) == 0) known = adapter_of(g0 + kUnits + lane);
         }
         if (++s == static_cast<uint32_t>(kPairStages)) { s = 0; ph ^= 1; }
       }
@@ -574,7 +587,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     // ---------------- MMA issuer ----------------
     if (rank == 0) {
       const uint32_t idesc = umma_idesc_bf16(2 * BM, p.tn) | (MN ? 1u << 15 : 0u), idesc_f = umma_idesc_bf16(2 * BM, p.tn) | 1u << 15;
-      uint32_t s = 0, fph = 0, bph = 0;              // fph, bph: the phases of full and of built, a bit per stage
+      uint32_t s = 0, ph = 0, bph = 0;               // bph: the phases of built, a bit per stage
       bool ok = true;
       for (int i = 0; i < segs.n && ok; ++i) {
         const Segment sg = segs.get(i);
@@ -586,9 +599,8 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         tc_fence_after();
         for (int k = sg.k0; k < sg.k1 + more; ++k) {
           const uint32_t st = smem_u32(smem + s * kPairStage);
+          if (!mbar_wait_warp(&full[s], ph, abort_flag)) { ok = false; break; }
           if (k < sg.k1) {
-            if (!mbar_wait_warp(&full[s], (fph >> s) & 1, abort_flag)) { ok = false; break; }
-            fph ^= 1u << s;
             tc_fence_after();
             if (elect_one()) {
               const uint64_t da = MN ? umma_desc_mn128(st) : umma_desc_k128(st), db = umma_desc_k128(st + kTileBytesA);
@@ -607,7 +619,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
               umma_commit_pair(&empty[s], 3);
             }
           }
-          if (++s == static_cast<uint32_t>(kPairStages)) s = 0;
+          if (++s == static_cast<uint32_t>(kPairStages)) { s = 0; ph ^= 1; }
         }
         if (ok && elect_one()) umma_commit_pair(&tfull[a], 3);
       }
@@ -622,11 +634,13 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       int m0, tt;
       tile_coords(sg.tile, m0, tt);
       const uint32_t a = i & 1, aph = (i >> 1) & 1;
-      if (!mbar_wait_warp(&tfull[a], aph, abort_flag) || !mbar_wait_warp(&looked[a], aph, abort_flag)) { ok = false; break; }
+      const int32_t* list = p.lists + static_cast<int64_t>(tt) * kListPitch;
+      bool any = false;                              // some adapter of the tile is bad
+      if (sg.k1 == p.kseg)
+        for (int x = lane; x < list[0]; x += 32) any |= is_bad(p.bad[list[1 + x]]);
+      any = __any_sync(0xffffffffu, any);
+      if (!mbar_wait_warp(&tfull[a], aph, abort_flag)) { ok = false; break; }
       tc_fence_after();
-      uint32_t any = 0;
-#pragma unroll
-      for (int w = 0; w < kBuild; ++w) any |= odd[a][w];
       const uint32_t t_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + a * kMaxTile + h * cols;
       const bool leave = sg.k1 < p.kseg;
       const int from = leave ? pair : segs.first_part(sg);
@@ -668,7 +682,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         if (any && m < p.m) {
 #pragma unroll
           for (int j = 0; j < 32; ++j)
-            if (i0 + j < p.n) acc[j] = __float_as_uint(__uint_as_float(acc[j]) + not_finite_term(p, i0 + j, m));
+            if (i0 + j < p.n) acc[j] = __float_as_uint(__uint_as_float(acc[j]) + bad_term(p, i0 + j, m));
         }
         // two samples at a time: even lanes store two rows of the first, odd lanes of the second
 #pragma unroll
@@ -686,43 +700,37 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         }
       }
       __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(&taken[a]);
-        if (leave) {
-          __threadfence();
-          st_release(p.ready + pair * 2 * kEpi + slot, 1u);
-        }
+      if (leave && lane == 0) {
+        __threadfence();
+        st_release(p.ready + pair * 2 * kEpi + slot, 1u);
       }
     }
   } else {
     // ---------------- the samples' operand of the adapters' term ----------------
-    const int w = warp - 2 - kEpi, t = w * 32 + lane;                  // this thread's sample of the CTA's half of the tile
-    uint32_t g = 0, lph = 0;                         // k-blocks so far; the phases of landed
+    const int t = (warp - 2 - kEpi) * 32 + lane;                       // this thread's sample of the CTA's half of the tile
+    uint32_t g = 0, fph = 0;                         // k-blocks so far; the phases of free_, a bit per stage
     bool ok = true;
     for (int i = 0; i < segs.n && ok; ++i) {
       const Segment sg = segs.get(i);
       int m0, tt;
       tile_coords(sg.tile, m0, tt);
-      const uint32_t a = i & 1, aph = (i >> 1) & 1;
-      if (!mbar_wait_warp(&taken[a], aph ^ 1, abort_flag)) { ok = false; break; }
       g += sg.k1 - sg.k0;
       const int units = sg.k1 == p.kseg ? p.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0, more = (units + kUnits - 1) / kUnits;
       const int smp = tt * p.tn + static_cast<int>(rank) * half + t;
       const int at = t < half && smp < p.n ? p.place[smp] * per : -1;                // this sample's first unit
       const uint4* src = reinterpret_cast<const uint4*>(p.pb) + static_cast<int64_t>(smp) * per;
-      uint32_t bad = 0;
       for (int k = 0; k < more; ++k, ++g) {
         const uint32_t s = g % kPairStages;
-        uint8_t* st = smem + s * kPairStage;
         const int g0 = k * kUnits, nu = min(kUnits, units - g0);
+        uint8_t* st = smem + s * kPairStage;
         uint4 words[kUnits];
 #pragma unroll
         for (int j = 0; j < kUnits; ++j) {
           const int u = g0 + j - at;                 // (a sample without an adapter has none: its place is below zero)
           words[j] = at >= 0 && j < nu && u >= 0 && u < per ? src[u] : make_uint4(0, 0, 0, 0);
         }
-        if (!mbar_wait_warp(&landed[s], (lph >> s) & 1, abort_flag)) { ok = false; break; }
-        lph ^= 1u << s;
+        if (!mbar_wait_warp(&free_[s], (fph >> s) & 1, abort_flag)) { ok = false; break; }
+        fph ^= 1u << s;
         if (t < half) {
           const uint32_t to = smem_u32(st) + kTileBytesA + t * 128;
 #pragma unroll
@@ -730,34 +738,11 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((j ^ (t & 7)) << 4)), "r"(words[j].x), "r"(words[j].y),
                          "r"(words[j].z), "r"(words[j].w) : "memory");
         }
-        // the factors, 1 KB a unit in each of two panels: looked through; beside an odd last unit zeros
-#pragma unroll
-        for (int x = 0; x < kUnits; ++x) {
-          const int panel = x / (kUnits / 2), unit = x % (kUnits / 2) * 2 + (t >> 6);
-          uint4* v = reinterpret_cast<uint4*>(st + panel * (kTileBytesA / 2) + unit * (kUnit * 128)) + (t & 63);
-          if (unit < nu) {
-            uint4 f = *v;
-            uint32_t* fw = reinterpret_cast<uint32_t*>(&f);
-            uint32_t hit = 0;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {            // bit 15 / 31: the exponent of the low / high half is all ones
-              const uint32_t b = ((fw[u] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-              hit |= b;
-              fw[u] &= ~((b >> 15) * 0xffffu);
-            }
-            if (hit) { *v = f; bad = 1; }
-          } else if (unit == nu && (nu & 1)) {
-            *v = make_uint4(0, 0, 0, 0);
-          }
-        }
+        if (nu & 1)                                  // beside an odd last unit zeros
+          *reinterpret_cast<uint4*>(st + (t >> 6) * (kTileBytesA / 2) + nu * (kUnit * 128) + (t & 63) * 16) = make_uint4(0, 0, 0, 0);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(mapa_u32(smem_u32(&built[s]), 0));
-      }
-      bad = __any_sync(0xffffffffu, bad);
-      if (lane == 0) {
-        odd[a][w] = bad;
-        mbar_arrive(&looked[a]);
       }
     }
   }
@@ -777,23 +762,74 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// p from its parts, zeros for a sample without an adapter, and scale p in bf16 as adapter_pair_kernel takes it (pb).
+// Ahead of adapter_pair_kernel, in the first blocks: which of the adapters in the tiles' lists have factors that are not finite, a block a
+// sixteenth of an adapter's; in the others: p from its parts, zeros for a sample without an adapter, and scale p in bf16 (pb).
 // ---------------------------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(256) adapter_sum_kernel(Ranked p, const int32_t* ids, const float* scale, int64_t n, int32_t rank, int32_t adapters,
-                                                          float* out, __nv_bfloat16* pb) {
+constexpr int kLookMost = 512;                      // adapters that the grid looks at at once
+struct SumParams {
+  Ranked p;
+  const int32_t* ids;
+  const float* scale;
+  int64_t n;
+  int32_t rank, adapters;
+  float* out;
+  __nv_bfloat16* pb;
+  const __nv_bfloat16* F;      // [adapters][rank][ldf], `width` columns
+  int64_t ldf, width;
+  const int32_t* mark;
+  int32_t call, look;          // look: the first blocks, 16 per adapter of min(adapters, kLookMost)
+  uint8_t* bad;                // [adapters][16]
+};
+
+__global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant__ SumParams p) {
+  __shared__ int32_t list[256];
+  __shared__ int32_t count;
   pdl_launch_dependents();
   pdl_wait();
-  const int per = (rank + kUnit - 1) / kUnit;
-  for (int64_t x = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; x < n * per; x += static_cast<int64_t>(gridDim.x) * 256) {
+  if (static_cast<int>(blockIdx.x) < p.look) {
+    const int part = blockIdx.x & 15, first = blockIdx.x >> 4, step = p.look >> 4;
+    for (int base = first; base < p.adapters; base += 256 * step) {
+      if (threadIdx.x == 0) count = 0;
+      __syncthreads();
+      const int64_t mine = base + static_cast<int64_t>(threadIdx.x) * step;
+      if (mine < p.adapters && p.mark[mine] == p.call) list[atomicAdd(&count, 1)] = static_cast<int32_t>(mine);
+      __syncthreads();
+      for (int x = 0; x < count; ++x) {
+        const __nv_bfloat16* f = p.F + static_cast<int64_t>(list[x]) * p.rank * p.ldf;
+        bool hit = false;
+        // pieces of 8 columns of a row; of the last one what lies behind the row does not count
+        const int64_t pieces = (p.width + 7) / 8, all = pieces * p.rank, to = all * (part + 1) / 16;
+        for (int64_t i = all * part / 16 + threadIdx.x; i < to; i += 256) {
+          const int64_t r = i / pieces, c = i - r * pieces;
+          const uint4 v = *reinterpret_cast<const uint4*>(f + r * p.ldf + c * 8);
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+          const int64_t left = p.width - c * 8;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {              // bit 15 / 31: the exponent of the low / high half is all ones
+            const uint32_t b = ((w[u] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+            hit |= (b & 0x8000u) && 2 * u < left;
+            hit |= (b >> 31) && 2 * u + 1 < left;
+          }
+        }
+        hit = __syncthreads_or(hit);
+        if (threadIdx.x == 0) p.bad[static_cast<int64_t>(list[x]) * 16 + part] = hit;
+      }
+      __syncthreads();
+    }
+    return;
+  }
+  const int per = (p.rank + kUnit - 1) / kUnit;
+  const int64_t blocks = gridDim.x - p.look;
+  for (int64_t x = (static_cast<int64_t>(blockIdx.x) - p.look) * 256 + threadIdx.x; x < p.n * per; x += blocks * 256) {
     const int64_t i = x / per;
-    const int r0 = static_cast<int>(x - i * per) * kUnit, id = ids[i];
-    const bool has = id >= 0 && id < adapters;
-    const float sc = has ? scale[id] : 0.f;
+    const int r0 = static_cast<int>(x - i * per) * kUnit, id = p.ids[i];
+    const bool has = id >= 0 && id < p.adapters;
+    const float sc = has ? p.scale[id] : 0.f;
     float v[kUnit];
 #pragma unroll
     for (int j = 0; j < kUnit; ++j) {
-      v[j] = has && r0 + j < rank ? ranked(p, i * rank + r0 + j) : 0.f;
-      if (r0 + j < rank) out[i * rank + r0 + j] = v[j];
+      v[j] = has && r0 + j < p.rank ? ranked(p.p, i * p.rank + r0 + j) : 0.f;
+      if (r0 + j < p.rank) p.out[i * p.rank + r0 + j] = v[j];
     }
     uint32_t w[kUnit / 2];
 #pragma unroll
@@ -801,7 +837,7 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(Ranked p, const int32_
       const __nv_bfloat162 b = __floats2bfloat162_rn(has ? sc * v[2 * j] : 0.f, has ? sc * v[2 * j + 1] : 0.f);
       w[j] = *reinterpret_cast<const uint32_t*>(&b);
     }
-    reinterpret_cast<uint4*>(pb)[x] = make_uint4(w[0], w[1], w[2], w[3]);
+    reinterpret_cast<uint4*>(p.pb)[x] = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
@@ -1182,7 +1218,7 @@ int64_t rank_rows(int64_t n, int64_t d) {
 }
 
 struct AdapterLayout {
-  size_t status, ready, s, t, ssum, tsum, pb, swords, twords, order, begin, count, work, lists, place, partial, total;
+  size_t status, ready, s, t, ssum, tsum, pb, swords, twords, order, begin, count, work, mark, bad, lists, place, partial, total;
 };
 
 int check(const sfb_adapter_config* c) {
@@ -1203,7 +1239,9 @@ AdapterLayout layout_of(const sfb_adapter_config& c) {
   auto take = [&](size_t bytes) { const size_t at = off; off += (bytes + kAlign - 1) / kAlign * kAlign; return at; };
   const size_t n = static_cast<size_t>(c.max_samples), rp = (static_cast<size_t>(c.rank) + 15) / 16 * 16;
   L.status = take(4);
-  L.ready = take(kModelSms * kEpi * 4);              // cleared with the status word
+  L.ready = take(kModelSms * kEpi * 4);              // these are cleared with the status word
+  L.mark = take(static_cast<size_t>(c.adapters) * 4);
+  L.bad = take(static_cast<size_t>(c.adapters) * 16);
   L.s = take(static_cast<size_t>(rank_rows(c.max_samples, c.cols)) * c.rank * 4);
   L.t = take(static_cast<size_t>(rank_rows(c.max_samples, c.rows)) * c.rank * 4);
   L.ssum = take(n * c.rank * 4);
@@ -1235,9 +1273,11 @@ struct sfb_adapters {
   char* ws;
   cudaStream_t stream;
   int device, last_cuda, max_pairs;
+  uint32_t calls;                      // products on pairs so far: what such a call marks its adapters with (a replayed one with the same
+                                       // number each time, so that it may look at adapters of earlier replays too)
   CUtensorMap mapU, mapV;              // boxes of 64 entries x 16 ranks of an adapter
   CUtensorMap unitU, unitV;            // x 8 ranks
-  sfb::TcState* tc;
+  sfb::EncodeTiledFn encode;           // cuTensorMapEncodeTiled
 
   template <typename T>
   T* at(size_t off) const { return reinterpret_cast<T*>(ws + off); }
@@ -1258,11 +1298,20 @@ struct OnDevice {                      // the handle's device is current for the
   }
 };
 
+// A matrix [outer x inner] as make_map has it, but without asking for more than a box: with 256 bytes at a time the products take up to 1.3
+// times as long (8,192 samples, 10,000 x 5,000, whose rows are 16 bytes off a sector: 882 us, 755 without; 1,024, 10,000 x 20,000: 395, 302).
+bool operand_map(sfb_adapters* h, CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t pitch, int box_inner, int box_outer) {
+  cuuint64_t dims[2] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(outer)}, strides[1] = {static_cast<cuuint64_t>(pitch) * 2};
+  cuuint32_t box[2] = {static_cast<cuuint32_t>(box_inner), static_cast<cuuint32_t>(box_outer)}, estr[2] = {1, 1};
+  return h->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool factor_map(sfb_adapters* h, CUtensorMap* m, const void* base, int64_t width, int64_t pitch, int ranks) {
   cuuint64_t dims[3] = {static_cast<cuuint64_t>(width), static_cast<cuuint64_t>(h->cfg.rank), static_cast<cuuint64_t>(h->cfg.adapters)};
   cuuint64_t strides[2] = {static_cast<cuuint64_t>(pitch) * 2, static_cast<cuuint64_t>(pitch) * 2 * h->cfg.rank};
   cuuint32_t box[3] = {BK, static_cast<cuuint32_t>(ranks), 1}, estr[3] = {1, 1, 1};
-  return h->tc->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  return h->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -1271,11 +1320,14 @@ cudaError_t rank_products(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz
                           Ranked* got) {
   const int tn = tile_of(n), parts = rank_parts(n, d), tiles = static_cast<int>((n + tn - 1) / tn);
   CUtensorMap mz;
-  if (!make_map(h->tc, &mz, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, const_cast<void*>(Z), d, n, ldz * 2, BK, tn)) return cudaErrorInvalidValue;
+  if (!operand_map(h, &mz, Z, d, n, ldz, BK, tn)) return cudaErrorInvalidValue;
   RankParams p{};
   p.n = static_cast<int32_t>(n); p.tn = tn; p.kseg = static_cast<int32_t>((d + BK - 1) / BK); p.stages = stages_of(tn);
   p.rank = h->cfg.rank; p.adapters = h->cfg.adapters; p.ids = ids; p.out = out; p.status = h->at<uint32_t>(h->lay.status);
-  if (n > kFewMost) { p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place); }
+  if (n > kFewMost) {
+    p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place); p.mark = h->at<int32_t>(h->lay.mark);
+    p.call = static_cast<int32_t>(++h->calls);
+  }
   const int per = (h->cfg.rank + kSlice - 1) / kSlice, chunks = (std::min(tn, h->cfg.adapters) * per + 7) / 8;
   const int groups = std::max(1, std::min(chunks, kModelSms / (parts * tiles)));
   const int smem = p.stages * stage_bytes(tn) + 1024;
@@ -1298,8 +1350,8 @@ cudaError_t few(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const in
   const sfb_adapter_config& c = h->cfg;
   const int64_t m = MN ? c.cols : c.rows, d = MN ? c.rows : c.cols;
   CUtensorMap ma, mz;
-  if (!make_map(h->tc, &ma, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, const_cast<void*>(h->W), c.cols, c.rows, c.ldw * 2, BK, MN ? BK : BM) ||
-      !make_map(h->tc, &mz, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, const_cast<void*>(Z), d, n, ldz * 2, BK, TN))
+  if (!operand_map(h, &ma, h->W, c.cols, c.rows, c.ldw, BK, MN ? BK : BM) ||
+      !operand_map(h, &mz, Z, d, n, ldz, BK, TN))
     return cudaErrorInvalidValue;
   FewParams p{};
   p.n = static_cast<int32_t>(n); p.m = static_cast<int32_t>(m);
@@ -1340,8 +1392,8 @@ cudaError_t pairs(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const 
   const int64_t m = MN ? c.cols : c.rows, d = MN ? c.rows : c.cols;
   const int tn = tile_of(n);
   CUtensorMap ma, mz;
-  if (!make_map(h->tc, &ma, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, const_cast<void*>(h->W), c.cols, c.rows, c.ldw * 2, BK, MN ? BK : BM) ||
-      !make_map(h->tc, &mz, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, const_cast<void*>(Z), d, n, ldz * 2, BK, tn / 2))
+  if (!operand_map(h, &ma, h->W, c.cols, c.rows, c.ldw, BK, MN ? BK : BM) ||
+      !operand_map(h, &mz, Z, d, n, ldz, BK, tn / 2))
     return cudaErrorInvalidValue;
   PairParams p{};
   p.n = static_cast<int32_t>(n); p.tn = tn; p.tilesT = static_cast<int32_t>((n + tn - 1) / tn);
@@ -1350,7 +1402,7 @@ cudaError_t pairs(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const 
   const PairPlan plan = plan_pairs(static_cast<int64_t>(p.tilesT) * p.tilesM, p.kseg, tn, h->max_pairs);
   p.cut = plan.cut; p.whole = plan.whole;
   p.rank = c.rank; p.adapters = c.adapters; p.ids = ids; p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place);
-  p.scale = h->scale; p.F = static_cast<const __nv_bfloat16*>(MN ? h->V : h->U); p.ldf = MN ? c.ldv : c.ldu;
+  p.scale = h->scale; p.bad = h->at<uint4>(h->lay.bad); p.F = static_cast<const __nv_bfloat16*>(MN ? h->V : h->U); p.ldf = MN ? c.ldv : c.ldu;
   p.p = s; p.pb = h->at<__nv_bfloat16>(h->lay.pb); p.Y = static_cast<__nv_bfloat16*>(Y); p.ldy = ldy;
   p.partial = h->at<float>(h->lay.partial); p.ready = h->at<uint32_t>(h->lay.ready); p.status = h->at<uint32_t>(h->lay.status);
   return launch_kernel_if(static_cast<int64_t>(p.tilesT) * p.tilesM <= plan.pairs, adapter_pair_kernel<MN>, dim3(2u * static_cast<unsigned>(plan.pairs)),
@@ -1365,8 +1417,11 @@ cudaError_t product(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, cons
   if (n <= kFewMost) return few<kFewMost, MN>(h, n, Z, ldz, ids, *s, p_out, Y, ldy);
   float* to = p_out ? p_out : room;
   const sfb_adapter_config& c = h->cfg;
-  const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(grid1d(n * ((c.rank + kUnit - 1) / kUnit), 256)), dim3(256), 0, h->stream, 1, *s, ids, h->scale,
-                                      n, c.rank, c.adapters, to, h->at<__nv_bfloat16>(h->lay.pb));
+  SumParams p{};
+  p.p = *s; p.ids = ids; p.scale = h->scale; p.n = n; p.rank = c.rank; p.adapters = c.adapters; p.out = to; p.pb = h->at<__nv_bfloat16>(h->lay.pb);
+  p.F = static_cast<const __nv_bfloat16*>(MN ? h->V : h->U); p.ldf = MN ? c.ldv : c.ldu; p.width = MN ? c.cols : c.rows;
+  p.mark = h->at<int32_t>(h->lay.mark); p.call = static_cast<int32_t>(h->calls); p.look = std::min(c.adapters, kLookMost) * 16; p.bad = h->at<uint8_t>(h->lay.bad);
+  const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(p.look + grid1d(n * ((c.rank + kUnit - 1) / kUnit), 256)), dim3(256), 0, h->stream, 1, p);
   if (e != cudaSuccess) return e;
   *s = Ranked{to, 1, 0};
   return pairs<MN>(h, n, Z, ldz, ids, to, Y, ldy);
@@ -1415,10 +1470,8 @@ extern "C" int sfb_adapter_init(const sfb_adapter_config* cfg, const void* W_dev
   if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) != cudaSuccess) return SFB_ERR_CUDA;
   if (qres != cudaDriverEntryPointSuccess || !fn) return SFB_ERR_CUDA;
   sfb_adapters* h = new (std::nothrow) sfb_adapters();
-  TcState* st = new (std::nothrow) TcState();
-  if (!h || !st) { delete h; delete st; return SFB_ERR_ARG; }
-  h->tc = st;
-  st->encode = reinterpret_cast<EncodeTiledFn>(fn);
+  if (!h) return SFB_ERR_ARG;
+  h->encode = reinterpret_cast<EncodeTiledFn>(fn);
   h->cfg = *cfg;
   sfb_adapter_config& c = h->cfg;
   if (!c.ldw) c.ldw = c.cols;
@@ -1517,7 +1570,7 @@ extern "C" int sfb_adapter_get_status(sfb_adapters* h, uint32_t* status_out) {
   ACK(cudaMemcpyAsync(status_out, h->ws + h->lay.status, 4, cudaMemcpyDeviceToHost, h->stream));
   ACK(cudaMemsetAsync(h->ws + h->lay.status, 0, 4, h->stream));
   ACK(cudaStreamSynchronize(h->stream));
-  if (*status_out & SFB_STATUS_TIMEOUT) ACK(cudaMemsetAsync(h->ws + h->lay.ready, 0, h->lay.s - h->lay.ready, h->stream));
+  if (*status_out & SFB_STATUS_TIMEOUT) ACK(cudaMemsetAsync(h->ws + h->lay.ready, 0, h->lay.mark - h->lay.ready, h->stream));
   return SFB_OK;
 }
 
@@ -1525,7 +1578,6 @@ extern "C" int sfb_adapter_last_cuda_error(sfb_adapters* h) { return h ? h->last
 
 extern "C" int sfb_adapter_destroy(sfb_adapters* h) {
   if (!h) return SFB_ERR_ARG;
-  delete h->tc;
   delete h;
   return SFB_OK;
 }
