@@ -1,8 +1,8 @@
 // Low-rank adapters of many requests beside the shared W (sfb_adapter_* in sfb.h): the logits of samples, each with the adapter
 // (a set of factor pairs) that its request names, and the gradients of the samples and of the adapters' factors.
 //
-// Launches of a forward pass:  adapter_rank_kernel (s = V x, in parts), then up to 64 samples adapter_few_kernel (y = W x + scale U^T s),
-// for more adapter_sum_kernel and adapter_pair_kernel;  of a backward pass:  adapter_index_kernel, adapter_rank_kernel (t = U dy; s again
+// Launches of a forward pass:  adapter_rank_kernel (s = V x, in parts), adapter_sum_kernel, and for y = W x + scale U^T s up to 64 samples
+// adapter_few_kernel, for more adapter_pair_kernel;  of a backward pass:  adapter_index_kernel, adapter_rank_kernel (t = U dy; s again
 // where it is not given), the products as in a forward pass (dx), adapter_words_kernel and adapter_gradient_kernel (dU, dV).
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -21,17 +21,15 @@ using namespace ptx;
 constexpr int BM = 128, BK = 64, kSlice = 16;       // rows of the accumulator, k-block, ranks of a slice
 constexpr int kMaxTile = 256;                       // samples of a tile, at most
 constexpr int kTileBytesA = BM * BK * 2;
-constexpr int kMaxParts = 16;                       // of the contraction of adapter_rank_kernel
+constexpr int kMaxParts = 32;                       // of the contraction of adapter_rank_kernel
 constexpr int kMaxStages = 8;
 // The tensor cores cut off what an fp32 accumulator cannot hold, always towards zero: 1.4e-8 of the sum an instruction of 16 (measured:
 // -1.1e-6 after 78 of them, -8e-6 after 512).  Sums that leave in fp32 are taken out, and added up with rounding, every 12 k-blocks.
 constexpr int kDrain = 12;
 constexpr int kListPitch = kMaxTile + 8;            // entries of a tile's list: their number, then the adapters
-constexpr int kRing = 196608, kSmallRing = 98304;   // bytes of operand stages; of tiles of up to 64 samples, two blocks an SM
+constexpr int kSmallRing = 98304;                   // bytes of operand stages where two blocks share an SM
 
 __host__ __device__ constexpr int stage_bytes(int tn) { return kTileBytesA + tn * BK * 2; }
-int ring_of(int tn) { return tn <= 64 ? kSmallRing : kRing; }
-int stages_of(int tn) { return std::min(kMaxStages, ring_of(tn) / stage_bytes(tn)); }
 
 // Samples of a tile: the fewest columns that hold n, up to 256.
 int tile_of(int64_t n) { return n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : n <= 128 ? 128 : kMaxTile; }
@@ -40,16 +38,18 @@ int tile_of(int64_t n) { return n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : n <
 // Which adapters the samples of a tile take: list[0 .. count), in the order of their first samples, and each sample's place in it
 // (-1: none).  By all threads of a block.
 // ---------------------------------------------------------------------------------------------------------
+template <int MOST>
 struct TileList {
-  int32_t id[kMaxTile];
-  int32_t place[kMaxTile];
-  int32_t list[kMaxTile];
-  uint32_t firsts[kMaxTile / 32];
+  int32_t id[MOST];
+  int32_t place[MOST];
+  int32_t list[MOST];
+  uint32_t firsts[MOST / 32];
   int32_t count;
 };
 
-__device__ __forceinline__ void build_list(TileList& L, const int32_t* ids, int first, int n, int tn, int adapters, uint32_t* status) {
-  for (int t = threadIdx.x; t < kMaxTile; t += blockDim.x) {
+template <int MOST>
+__device__ __forceinline__ void build_list(TileList<MOST>& L, const int32_t* ids, int first, int n, int tn, int adapters, uint32_t* status) {
+  for (int t = threadIdx.x; t < MOST; t += blockDim.x) {
     int id = t < tn && first + t < n ? ids[first + t] : -1;
     if (id < -1 || id >= adapters) {
       atomicOr(status, SFB_STATUS_ADAPTER_RANGE);
@@ -59,27 +59,25 @@ __device__ __forceinline__ void build_list(TileList& L, const int32_t* ids, int 
   }
   __syncthreads();
   const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
-  for (int w = threadIdx.x >> 5; w < kMaxTile / 32; w += warps) {
+  for (int w = threadIdx.x >> 5; w < MOST / 32; w += warps) {
     const int t = w * 32 + lane, id = L.id[t];
     int f = t;
     if (w * 32 < tn) {
-      for (int u = (t & ~3) - 4; u >= 0; u -= 4) {                     // downwards: the last hit is the first sample
-        const int4 v = *reinterpret_cast<const int4*>(&L.id[u]);
-        if (v.w == id) f = u + 3;
-        if (v.z == id) f = u + 2;
-        if (v.y == id) f = u + 1;
-        if (v.x == id) f = u;
-      }
-      if (f == t)
-        for (int u = t - 1; u >= (t & ~3); --u)
-          if (L.id[u] == id) f = u;
+      const uint32_t same = __match_any_sync(0xffffffffu, id);
+      f = w * 32 + __ffs(same) - 1;
+      if (__any_sync(0xffffffffu, w > 0 && id >= 0))
+#pragma unroll 4
+        for (int u = w * 32 - 4; u >= 0; u -= 4) {                     // downwards: the last hit is the first sample
+          const int4 v = *reinterpret_cast<const int4*>(&L.id[u]);
+          f = v.x == id ? u : v.y == id ? u + 1 : v.z == id ? u + 2 : v.w == id ? u + 3 : f;
+        }
     }
     const uint32_t m = __ballot_sync(0xffffffffu, id >= 0 && f == t);
     if (lane == 0) L.firsts[w] = m;
     L.place[t] = f;                                                    // for now: the sample that has the place
   }
   __syncthreads();
-  for (int t = threadIdx.x; t < kMaxTile; t += blockDim.x) {
+  for (int t = threadIdx.x; t < MOST; t += blockDim.x) {
     const int f = L.place[t];
     int at = __popc(L.firsts[f >> 5] & ((1u << (f & 31)) - 1));
     for (int w = 0; w < (f >> 5); ++w) at += __popc(L.firsts[w]);
@@ -88,35 +86,35 @@ __device__ __forceinline__ void build_list(TileList& L, const int32_t* ids, int 
   }
   if (threadIdx.x == 0) {
     int c = 0;
-    for (int w = 0; w < kMaxTile / 32; ++w) c += __popc(L.firsts[w]);
+    for (int w = 0; w < MOST / 32; ++w) c += __popc(L.firsts[w]);
     L.count = c;
   }
   __syncthreads();
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// p_i = F[a_i] z_i:  the adapters' factors as the rows of the accumulator, 16 ranks (a slice) of one adapter after another, the
-// samples of a tile as its columns; each sample takes the rows of its own adapter, so what another adapter or sample holds does not
-// reach it.  Grid: parts of the contraction x tiles of samples x groups of the tile's slices, eight slices at a time.
-// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..9 epilogue (TMEM lane quarter q; 32 of every 64 samples).
+// p_i = F[a_i] z_i:  the adapters' factors as the rows of the accumulator, 16 ranks (a slice) of one adapter after another, up to 128
+// samples as its columns; each sample takes the rows of its own adapter, so what another adapter or sample holds does not reach it.
+// Grid: parts of the contraction x tiles of samples x groups of the tile's slices, eight slices at a time.  Bound by the way of z and F
+// to the SMs, and by latency at either end of a block: two blocks an SM.
+// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..9 epilogue (TMEM lane quarter q; 32 of every 64 samples), whose sums stay in
+// registers from drain to drain.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kRankThreads = 320;
+constexpr int kRankThreads = 320, kRankTile = 128;
 struct RankParams {
   int32_t n, tn, kseg, stages;
   int32_t rank, adapters;
   const int32_t* ids;
   float* out;                  // [parts][n][rank]
-  int32_t* lists;              // may be null: [tiles][kListPitch], per sample its place in its tile's list,
-  int32_t* place;
-  int32_t* mark;               // and for each adapter in a list, `call`
+  int32_t* mark;               // may be null: for each adapter in use, `call`
   int32_t call;
   uint32_t* status;
 };
 
-__global__ void __launch_bounds__(kRankThreads)
+__global__ void __launch_bounds__(kRankThreads, 2)
 adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ RankParams p) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ alignas(16) TileList L;
+  __shared__ alignas(16) TileList<kRankTile> L;
   __shared__ uint64_t full[kMaxStages], empty[kMaxStages], tfull[2], tempty[2];
   __shared__ uint32_t tmem_slot, abort_word;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -141,14 +139,8 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
   tc_fence_after();
   const uint32_t tmem_base = tmem_slot;
   const int per = (p.rank + kSlice - 1) / kSlice, slices = L.count * per, chunks = (slices + 7) / 8;
-  if (p.lists && part == 0 && blockIdx.z == 0) {
-    int32_t* to = p.lists + static_cast<int64_t>(blockIdx.y) * kListPitch;
-    if (threadIdx.x == 0) to[0] = L.count;
-    for (int t = threadIdx.x; t < p.tn; t += kRankThreads) {
-      if (t < L.count) { to[1 + t] = L.list[t]; p.mark[L.list[t]] = p.call; }
-      if (first + t < p.n) p.place[first + t] = L.place[t];
-    }
-  }
+  if (p.mark && part == 0 && blockIdx.z == 0)
+    for (int t = threadIdx.x; t < L.count; t += kRankThreads) p.mark[L.list[t]] = p.call;
 
   if (warp == 0) {
     uint32_t s = 0, ph = 0;
@@ -173,56 +165,74 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
     const uint32_t idesc = umma_idesc_bf16(BM, p.tn);
     uint32_t s = 0, ph = 0, i = 0;
     bool ok = true;
-    for (int c = blockIdx.z; c < chunks && ok; c += gridDim.z)
-    for (int k0 = kbeg; k0 < kend && ok; k0 += kDrain, ++i) {
-      const uint32_t a = i & 1, aph = (i >> 1) & 1, d_tmem = tmem_base + a * cols;
-      if (!mbar_wait_warp(&tempty[a], aph ^ 1, abort_flag)) { ok = false; break; }
-      tc_fence_after();
-      for (int k = k0; k < min(k0 + kDrain, kend); ++k) {
-        if (!mbar_wait_warp(&full[s], ph, abort_flag)) { ok = false; break; }
+    for (int c = blockIdx.z; c < chunks && ok; c += gridDim.z) {
+      for (int k0 = kbeg; k0 < kend && ok; k0 += kDrain, ++i) {
+        const uint32_t a = i & 1, aph = (i >> 1) & 1, d_tmem = tmem_base + a * cols;
+        if (!mbar_wait_warp(&tempty[a], aph ^ 1, abort_flag)) { ok = false; break; }
         tc_fence_after();
-        if (elect_one()) {
-          const uint64_t da = umma_desc_k128(smem_u32(smem + s * stage)), db = umma_desc_k128(smem_u32(smem + s * stage + kTileBytesA));
+        for (int k = k0; k < min(k0 + kDrain, kend); ++k) {
+          if (!mbar_wait_warp(&full[s], ph, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t da = umma_desc_k128(smem_u32(smem + s * stage)), db = umma_desc_k128(smem_u32(smem + s * stage + kTileBytesA));
 #pragma unroll
-          for (int j = 0; j < BK / 16; ++j) umma_bf16(d_tmem, da + 2 * j, db + 2 * j, idesc, (k - k0) | j ? 1u : 0u);
-          umma_commit(&empty[s]);
+            for (int j = 0; j < BK / 16; ++j) umma_bf16(d_tmem, da + 2 * j, db + 2 * j, idesc, (k - k0) | j ? 1u : 0u);
+            umma_commit(&empty[s]);
+          }
+          if (++s == static_cast<uint32_t>(p.stages)) { s = 0; ph ^= 1; }
         }
-        if (++s == static_cast<uint32_t>(p.stages)) { s = 0; ph ^= 1; }
+        if (ok && elect_one()) umma_commit(&tfull[a]);
       }
-      if (ok && elect_one()) umma_commit(&tfull[a]);
     }
   } else {
     const int q = warp & 3, h = (warp - 2) >> 2;
     float* out = p.out + static_cast<int64_t>(part) * p.n * p.rank;
     uint32_t i = 0;
     bool ok = true;
-    for (int c = blockIdx.z; c < chunks && ok; c += gridDim.z)
-    for (int k0 = kbeg; k0 < kend; k0 += kDrain, ++i) {
-      const uint32_t a = i & 1, aph = (i >> 1) & 1;
-      if (!mbar_wait_warp(&tfull[a], aph, abort_flag)) { ok = false; break; }
-      tc_fence_after();
+    for (int c = blockIdx.z; c < chunks && ok; c += gridDim.z) {
       const int g = c * 8 + q * 2 + (lane >> 4), at = g < slices ? g / per : -2, r = (g - at * per) * kSlice + (lane & 15);
-#pragma unroll 1
-      for (int t0 = h * 32; t0 < p.tn; t0 += 64) {
-        uint32_t own = 0;                            // of these samples: those of this lane's adapter (places behind a tile of 16 are -1)
+      uint32_t own[2];                               // of 32 samples: those of this lane's adapter (places behind a tile of 16 are -1)
+      float sum[2][32];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) own |= (L.place[t0 + j] == at ? 1u : 0u) << j;
-        if (r >= p.rank) own = 0;
-        if (!__any_sync(0xffffffffu, own)) continue;
-        float* to = out + static_cast<int64_t>(first + t0) * p.rank + r;
-        float old[32];
+      for (int x = 0; x < 2; ++x) {
+        const int t0 = h * 32 + x * 64;
+        own[x] = 0;
+        if (t0 < p.tn && r < p.rank) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) old[j] = k0 > kbeg && (own >> j & 1) ? to[static_cast<int64_t>(j) * p.rank] : 0.f;
-        uint32_t acc[32];
-        tmem_ld_32x32(tmem_base + (static_cast<uint32_t>(q * 32) << 16) + a * cols + t0, acc);
-        tmem_ld_wait();
+          for (int j = 0; j < 32; j += 4) {
+            const int4 v = *reinterpret_cast<const int4*>(&L.place[t0 + j]);
+            own[x] |= ((v.x == at ? 1u : 0u) | (v.y == at ? 2u : 0u) | (v.z == at ? 4u : 0u) | (v.w == at ? 8u : 0u)) << j;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 32; ++j) sum[x][j] = 0.f;
+      }
+      const bool any[2] = {__any_sync(0xffffffffu, own[0]) != 0, __any_sync(0xffffffffu, own[1]) != 0};
+      for (int k0 = kbeg; k0 < kend; k0 += kDrain, ++i) {
+        const uint32_t a = i & 1, aph = (i >> 1) & 1;
+        if (!mbar_wait_warp(&tfull[a], aph, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (!any[x]) continue;
+          uint32_t acc[32];
+          tmem_ld_32x32(tmem_base + (static_cast<uint32_t>(q * 32) << 16) + a * cols + h * 32 + x * 64, acc);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 32; ++j) sum[x][j] += __uint_as_float(acc[j]);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&tempty[a]);
+      }
+      if (!ok) break;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        float* to = out + static_cast<int64_t>(first + h * 32 + x * 64) * p.rank + r;
 #pragma unroll
         for (int j = 0; j < 32; ++j)
-          if (own >> j & 1) to[static_cast<int64_t>(j) * p.rank] = __uint_as_float(acc[j]) + old[j];
+          if (own[x] >> j & 1) to[static_cast<int64_t>(j) * p.rank] = sum[x][j];
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&tempty[a]);
     }
   }
   __syncwarp();
@@ -265,8 +275,7 @@ struct FewParams {
   const float* scale;
   const __nv_bfloat16* F;      // [adapters][rank][ldf]
   int64_t ldf;
-  Ranked p;
-  float* p_out;                // may be null: [n][rank]
+  const float* p;              // [n][rank]
   __nv_bfloat16* Y;
   int64_t ldy;
   uint32_t* status;
@@ -344,9 +353,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     asm volatile("bar.sync 1, 128;" ::: "memory");
     for (int x = tid; x < p.n * p.rank; x += 128) {
       const int id = id_of[x / p.rank];
-      const float v = id >= 0 ? ranked(p.p, x) : 0.f;
-      ps[x] = id >= 0 ? p.scale[id] * v : 0.f;
-      if (p.p_out && blockIdx.x == 0) p.p_out[x] = v;
+      ps[x] = id >= 0 ? p.scale[id] * p.p[x] : 0.f;
     }
     asm volatile("bar.sync 1, 128;" ::: "memory");
     float e[TN];
@@ -762,8 +769,8 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// Ahead of adapter_pair_kernel, in the first blocks: which of the adapters in the tiles' lists have factors that are not finite, a block a
-// sixteenth of an adapter's; in the others: p from its parts, zeros for a sample without an adapter, and scale p in bf16 (pb).
+// p from its parts, zeros for a sample without an adapter, and scale p in bf16 (pb).  Ahead of adapter_pair_kernel, in the first blocks:
+// which of the adapters in use have factors that are not finite, a block a sixteenth of an adapter's, and the lists of the tiles.
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kLookMost = 512;                      // adapters that the grid looks at at once
 struct SumParams {
@@ -777,16 +784,33 @@ struct SumParams {
   const __nv_bfloat16* F;      // [adapters][rank][ldf], `width` columns
   int64_t ldf, width;
   const int32_t* mark;
-  int32_t call, look;          // look: the first blocks, 16 per adapter of min(adapters, kLookMost)
+  int32_t call, look;          // look: the first blocks, 16 per adapter of min(adapters, kLookMost); then
+  int32_t tiles, tn;           // a block per tile of tn samples
   uint8_t* bad;                // [adapters][16]
+  int32_t* lists;              // [tiles][kListPitch]
+  int32_t* place;              // per sample its place in its tile's list
+  uint32_t* status;
 };
 
 __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant__ SumParams p) {
   __shared__ int32_t list[256];
   __shared__ int32_t count;
+  __shared__ alignas(16) TileList<kMaxTile> L;
   pdl_launch_dependents();
   pdl_wait();
-  if (static_cast<int>(blockIdx.x) < p.look) {
+  const int tile = static_cast<int>(blockIdx.x) - p.look;
+  if (tile >= 0 && tile < p.tiles) {
+    const int first = tile * p.tn;
+    build_list(L, p.ids, first, static_cast<int>(p.n), p.tn, p.adapters, p.status);
+    int32_t* to = p.lists + static_cast<int64_t>(tile) * kListPitch;
+    if (threadIdx.x == 0) to[0] = L.count;
+    for (int t = threadIdx.x; t < p.tn; t += 256) {
+      if (t < L.count) to[1 + t] = L.list[t];
+      if (first + t < p.n) p.place[first + t] = L.place[t];
+    }
+    return;
+  }
+  if (tile < 0) {
     const int part = blockIdx.x & 15, first = blockIdx.x >> 4, step = p.look >> 4;
     for (int base = first; base < p.adapters; base += 256 * step) {
       if (threadIdx.x == 0) count = 0;
@@ -819,8 +843,8 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
     return;
   }
   const int per = (p.rank + kUnit - 1) / kUnit;
-  const int64_t blocks = gridDim.x - p.look;
-  for (int64_t x = (static_cast<int64_t>(blockIdx.x) - p.look) * 256 + threadIdx.x; x < p.n * per; x += blocks * 256) {
+  const int64_t blocks = gridDim.x - p.look - p.tiles;
+  for (int64_t x = static_cast<int64_t>(tile - p.tiles) * 256 + threadIdx.x; x < p.n * per; x += blocks * 256) {
     const int64_t i = x / per;
     const int r0 = static_cast<int>(x - i * per) * kUnit, id = p.ids[i];
     const bool has = id >= 0 && id < p.adapters;
@@ -837,7 +861,7 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
       const __nv_bfloat162 b = __floats2bfloat162_rn(has ? sc * v[2 * j] : 0.f, has ? sc * v[2 * j + 1] : 0.f);
       w[j] = *reinterpret_cast<const uint32_t*>(&b);
     }
-    reinterpret_cast<uint4*>(p.pb)[x] = make_uint4(w[0], w[1], w[2], w[3]);
+    if (p.pb) reinterpret_cast<uint4*>(p.pb)[x] = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
@@ -976,7 +1000,8 @@ __global__ void __launch_bounds__(256) adapter_words_kernel(const __grid_constan
 // dF[a] = sum_{i of a} (scale p_i) z_i^T for a tile of 128 columns of z: the columns are the accumulator's rows, the ranks of the three
 // words its columns (added at the end), the samples the contraction, 64 of them at a time, gathered in the order of adapter_index_kernel
 // (so no sample of another adapter is in the product).
-// Warps: 0..3 loaders (asynchronous copies of 16 bytes into both operands), 4 MMA issuer and TMEM owner, 5..8 epilogue.
+// Warps: 0..3 loaders (asynchronous copies of 16 bytes into both operands, which arrive at the stage's barrier by themselves: a loader that
+// waited for its copies and fenced them had one k-block under way, 2 us each), 4 MMA issuer and TMEM owner, 5..8 epilogue.
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kGradThreads = 288, kGradStages = 8, kGradRing = 196608;
 struct GradSide {
@@ -1037,12 +1062,10 @@ struct GradWalk {
   }
 };
 
-template <int LAG>
 __device__ __forceinline__ void grad_load(const GradParams& p, uint8_t* smem, uint64_t* full, uint64_t* empty, volatile uint32_t* abort_flag) {
   const int rp = (p.rank + 15) & ~15, pieces = 3 * rp / 8, stage = kTileBytesA + grad_panels(p.rank) * 8192, stages = p.stages;
   const int tid = threadIdx.x, c16 = tid & 15, r0 = tid >> 4;
-  uint32_t g = 0, s = 0, ph = 0;                     // k-blocks so far; this one's stage and phase
-  uint32_t back = 0;                                 // the stage of the k-block LAG ago
+  uint32_t s = 0, ph = 0;
   int known = -1, known_k = -1;                      // the adapter and the k-block of the samples in row
   int32_t row[8];
   for (GradWalk it(p); it.valid(); it.next()) {
@@ -1050,7 +1073,7 @@ __device__ __forceinline__ void grad_load(const GradParams& p, uint8_t* smem, ui
     const int nk = (it.count + BK - 1) / BK;
     const int col = it.tile * BM + c16 * 8, left = sd.width - col;
     const uint32_t bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;
-    for (int k = 0; k < nk; ++k, ++g) {
+    for (int k = 0; k < nk; ++k) {
       if (known != it.a || known_k != k) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) { const int at = k * BK + r0 + j * 8; row[j] = at < it.count ? p.order[it.begin + at] : -1; }
@@ -1074,22 +1097,11 @@ __device__ __forceinline__ void grad_load(const GradParams& p, uint8_t* smem, ui
         cp_async_16(st + kTileBytesA + (ch >> 3) * 8192 + kr * 128 + (((ch & 7) ^ (kr & 7)) << 4),
                     sd.words + (b ? (static_cast<int64_t>(it.begin) + at) * 3 * rp + ch * 8 : 0), b);
       }
-      cp_async_commit();
-      if (g >= LAG) {
-        cp_async_wait<LAG>();
-        fence_proxy_async_smem();
-        mbar_arrive(&full[back]);
-        if (++back == static_cast<uint32_t>(stages)) back = 0;
-      }
+      cp_async_arrive(&full[s]);
       if (++s == static_cast<uint32_t>(stages)) { s = 0; ph ^= 1; }
     }
   }
-  cp_async_wait<0>();
-  fence_proxy_async_smem();
-  for (uint32_t j = g > LAG ? g - LAG : 0; j < g; ++j) {
-    mbar_arrive(&full[back]);
-    if (++back == static_cast<uint32_t>(stages)) back = 0;
-  }
+  cp_async_wait_all();
 }
 
 __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const __grid_constant__ GradParams p) {
@@ -1116,9 +1128,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
   pdl_wait();
 
   if (warp < 4) {
-    if (p.stages >= 6) grad_load<4>(p, smem, full, empty, abort_flag);
-    else if (p.stages >= 4) grad_load<2>(p, smem, full, empty, abort_flag);
-    else grad_load<1>(p, smem, full, empty, abort_flag);
+    grad_load(p, smem, full, empty, abort_flag);
   } else if (warp == 4) {
     // more than 256 columns: 192 (three panels), then the rest
     const uint32_t n1 = N <= 256 ? N : 192, n2 = N - n1;
@@ -1133,6 +1143,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
         tc_fence_after();
         for (int k = k0; k < min(k0 + kDrain, nk); ++k) {
           if (!mbar_wait_warp(&full[s], ph, abort_flag)) { ok = false; break; }
+          fence_proxy_async_smem();                  // the loaders' copies are generic writes: ahead of the tensor core's reads
           tc_fence_after();
           const int steps = min(BK / 16, (it.count - k * BK + 15) / 16);
           if (elect_one()) {
@@ -1201,16 +1212,17 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
 // ---------------------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------------------
-// Parts of the contraction of adapter_rank_kernel: as many as give every SM a block, of four k-blocks at least.
+// Samples of a tile of adapter_rank_kernel; parts of its contraction: as many as give every SM two blocks, of four k-blocks at least.
+int rank_tile(int64_t n) { return std::min(tile_of(n), kRankTile); }
 int rank_parts(int64_t n, int64_t d) {
-  const int64_t tiles = (n + tile_of(n) - 1) / tile_of(n), kseg = (d + BK - 1) / BK;
-  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({kMaxParts, kModelSms / tiles, kseg / 4})));
+  const int64_t tiles = (n + rank_tile(n) - 1) / rank_tile(n), kseg = (d + BK - 1) / BK;
+  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({kMaxParts, 2 * kModelSms / tiles, kseg / 4})));
 }
 // Most samples x parts of a call of up to n samples.
 int64_t rank_rows(int64_t n, int64_t d) {
   int64_t most = 0;
-  for (int64_t tiles = 1; tiles <= kModelSms; ++tiles) {
-    const int64_t m = std::min(n, tiles * kMaxTile);
+  for (int64_t tiles = 1; tiles <= 2 * kModelSms; ++tiles) {
+    const int64_t m = std::min(n, tiles * kRankTile);
     most = std::max(most, m * rank_parts(m, d));
     if (m == n) return most;
   }
@@ -1298,13 +1310,15 @@ struct OnDevice {                      // the handle's device is current for the
   }
 };
 
-// A matrix [outer x inner] as make_map has it, but without asking for more than a box: with 256 bytes at a time the products take up to 1.3
-// times as long (8,192 samples, 10,000 x 5,000, whose rows are 16 bytes off a sector: 882 us, 755 without; 1,024, 10,000 x 20,000: 395, 302).
-bool operand_map(sfb_adapters* h, CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t pitch, int box_inner, int box_outer) {
+// A matrix [outer x inner], boxes with the 128-byte swizzle.  Operands that are streamed once are asked for 256 bytes at a time (up to 64
+// samples, 10,000 x 20,000: 69 us, 75 with boxes alone; 325,000 x 10,000: 1,522 and 1,588), those that tiles share in L2 by boxes alone (8,192
+// samples, 10,000 x 5,000, whose rows are 16 bytes off a sector: 755 us, 882 with 256 bytes; 1,024, 10,000 x 20,000: 302 and 395).
+bool operand_map(sfb_adapters* h, CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t pitch, int box_inner, int box_outer,
+                 CUtensorMapL2promotion promotion) {
   cuuint64_t dims[2] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(outer)}, strides[1] = {static_cast<cuuint64_t>(pitch) * 2};
   cuuint32_t box[2] = {static_cast<cuuint32_t>(box_inner), static_cast<cuuint32_t>(box_outer)}, estr[2] = {1, 1};
   return h->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                   CU_TENSOR_MAP_SWIZZLE_128B, promotion, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 bool factor_map(sfb_adapters* h, CUtensorMap* m, const void* base, int64_t width, int64_t pitch, int ranks) {
@@ -1318,20 +1332,20 @@ bool factor_map(sfb_adapters* h, CUtensorMap* m, const void* base, int64_t width
 // p = F[a] z for n samples into `out`; *got: where and in how many parts.
 cudaError_t rank_products(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, int64_t d, const CUtensorMap& mapF, const int32_t* ids, float* out,
                           Ranked* got) {
-  const int tn = tile_of(n), parts = rank_parts(n, d), tiles = static_cast<int>((n + tn - 1) / tn);
+  const int tn = rank_tile(n), parts = rank_parts(n, d), tiles = static_cast<int>((n + tn - 1) / tn);
   CUtensorMap mz;
-  if (!operand_map(h, &mz, Z, d, n, ldz, BK, tn)) return cudaErrorInvalidValue;
+  if (!operand_map(h, &mz, Z, d, n, ldz, BK, tn, CU_TENSOR_MAP_L2_PROMOTION_L2_256B)) return cudaErrorInvalidValue;
   RankParams p{};
-  p.n = static_cast<int32_t>(n); p.tn = tn; p.kseg = static_cast<int32_t>((d + BK - 1) / BK); p.stages = stages_of(tn);
+  p.n = static_cast<int32_t>(n); p.tn = tn; p.kseg = static_cast<int32_t>((d + BK - 1) / BK); p.stages = std::min(kMaxStages, kSmallRing / stage_bytes(tn));
   p.rank = h->cfg.rank; p.adapters = h->cfg.adapters; p.ids = ids; p.out = out; p.status = h->at<uint32_t>(h->lay.status);
   if (n > kFewMost) {
-    p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place); p.mark = h->at<int32_t>(h->lay.mark);
+    p.mark = h->at<int32_t>(h->lay.mark);
     p.call = static_cast<int32_t>(++h->calls);
   }
   const int per = (h->cfg.rank + kSlice - 1) / kSlice, chunks = (std::min(tn, h->cfg.adapters) * per + 7) / 8;
-  const int groups = std::max(1, std::min(chunks, kModelSms / (parts * tiles)));
+  const int groups = std::max(1, std::min(chunks, 2 * kModelSms / (parts * tiles)));
   const int smem = p.stages * stage_bytes(tn) + 1024;
-  cudaError_t e = allow_smem<adapter_rank_kernel>(kRing + 1024);
+  cudaError_t e = allow_smem<adapter_rank_kernel>(kSmallRing + 1024);
   if (e != cudaSuccess) return e;
   *got = Ranked{out, parts, n * h->cfg.rank};
   return launch_kernel(adapter_rank_kernel, dim3(parts, tiles, groups), dim3(kRankThreads), smem, h->stream, 1, mapF, mz, p);
@@ -1346,12 +1360,12 @@ int few_parts(int64_t tiles, int64_t kseg) {
 }
 
 template <int TN, bool MN>
-cudaError_t few(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const int32_t* ids, const Ranked& s, float* p_out, void* Y, int64_t ldy) {
+cudaError_t few(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const int32_t* ids, const float* s, void* Y, int64_t ldy) {
   const sfb_adapter_config& c = h->cfg;
   const int64_t m = MN ? c.cols : c.rows, d = MN ? c.rows : c.cols;
   CUtensorMap ma, mz;
-  if (!operand_map(h, &ma, h->W, c.cols, c.rows, c.ldw, BK, MN ? BK : BM) ||
-      !operand_map(h, &mz, Z, d, n, ldz, BK, TN))
+  if (!operand_map(h, &ma, h->W, c.cols, c.rows, c.ldw, BK, MN ? BK : BM, CU_TENSOR_MAP_L2_PROMOTION_L2_256B) ||
+      !operand_map(h, &mz, Z, d, n, ldz, BK, TN, CU_TENSOR_MAP_L2_PROMOTION_L2_256B))
     return cudaErrorInvalidValue;
   FewParams p{};
   p.n = static_cast<int32_t>(n); p.m = static_cast<int32_t>(m);
@@ -1360,7 +1374,7 @@ cudaError_t few(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const in
   p.parts = few_parts(tiles, p.kseg);
   p.rank = c.rank; p.adapters = c.adapters; p.ids = ids; p.scale = h->scale;
   p.F = static_cast<const __nv_bfloat16*>(MN ? h->V : h->U); p.ldf = MN ? c.ldv : c.ldu;
-  p.p = s; p.p_out = p_out; p.Y = static_cast<__nv_bfloat16*>(Y); p.ldy = ldy; p.status = h->at<uint32_t>(h->lay.status);
+  p.p = s; p.Y = static_cast<__nv_bfloat16*>(Y); p.ldy = ldy; p.status = h->at<uint32_t>(h->lay.status);
   const int terms = static_cast<int>(n) * c.rank * 4;
   p.stages = std::min(kMaxStages, (kSmallRing + 8192 - std::min(terms, 24576)) / stage_bytes(TN));
   const int smem = p.stages * stage_bytes(TN) + terms + 1024;
@@ -1392,8 +1406,8 @@ cudaError_t pairs(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const 
   const int64_t m = MN ? c.cols : c.rows, d = MN ? c.rows : c.cols;
   const int tn = tile_of(n);
   CUtensorMap ma, mz;
-  if (!operand_map(h, &ma, h->W, c.cols, c.rows, c.ldw, BK, MN ? BK : BM) ||
-      !operand_map(h, &mz, Z, d, n, ldz, BK, tn / 2))
+  if (!operand_map(h, &ma, h->W, c.cols, c.rows, c.ldw, BK, MN ? BK : BM, CU_TENSOR_MAP_L2_PROMOTION_NONE) ||
+      !operand_map(h, &mz, Z, d, n, ldz, BK, tn / 2, CU_TENSOR_MAP_L2_PROMOTION_NONE))
     return cudaErrorInvalidValue;
   PairParams p{};
   p.n = static_cast<int32_t>(n); p.tn = tn; p.tilesT = static_cast<int32_t>((n + tn - 1) / tn);
@@ -1412,18 +1426,24 @@ cudaError_t pairs(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const 
 // y = A z + scale F^T p; p_out (may be null) receives p; *s: p where it is afterwards.
 template <bool MN>
 cudaError_t product(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const int32_t* ids, Ranked* s, float* p_out, float* room, void* Y, int64_t ldy) {
-  if (n <= 16) return few<16, MN>(h, n, Z, ldz, ids, *s, p_out, Y, ldy);
-  if (n <= 32) return few<32, MN>(h, n, Z, ldz, ids, *s, p_out, Y, ldy);
-  if (n <= kFewMost) return few<kFewMost, MN>(h, n, Z, ldz, ids, *s, p_out, Y, ldy);
   float* to = p_out ? p_out : room;
   const sfb_adapter_config& c = h->cfg;
   SumParams p{};
-  p.p = *s; p.ids = ids; p.scale = h->scale; p.n = n; p.rank = c.rank; p.adapters = c.adapters; p.out = to; p.pb = h->at<__nv_bfloat16>(h->lay.pb);
-  p.F = static_cast<const __nv_bfloat16*>(MN ? h->V : h->U); p.ldf = MN ? c.ldv : c.ldu; p.width = MN ? c.cols : c.rows;
-  p.mark = h->at<int32_t>(h->lay.mark); p.call = static_cast<int32_t>(h->calls); p.look = std::min(c.adapters, kLookMost) * 16; p.bad = h->at<uint8_t>(h->lay.bad);
-  const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(p.look + grid1d(n * ((c.rank + kUnit - 1) / kUnit), 256)), dim3(256), 0, h->stream, 1, p);
+  p.p = *s; p.ids = ids; p.scale = h->scale; p.n = n; p.rank = c.rank; p.adapters = c.adapters; p.out = to; p.status = h->at<uint32_t>(h->lay.status);
+  if (n > kFewMost) {
+    p.pb = h->at<__nv_bfloat16>(h->lay.pb);
+    p.F = static_cast<const __nv_bfloat16*>(MN ? h->V : h->U); p.ldf = MN ? c.ldv : c.ldu; p.width = MN ? c.cols : c.rows;
+    p.mark = h->at<int32_t>(h->lay.mark); p.call = static_cast<int32_t>(h->calls); p.look = std::min(c.adapters, kLookMost) * 16;
+    p.bad = h->at<uint8_t>(h->lay.bad);
+    p.tn = tile_of(n); p.tiles = static_cast<int32_t>((n + p.tn - 1) / p.tn); p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place);
+  }
+  const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(p.look + p.tiles + grid1d(n * ((c.rank + kUnit - 1) / kUnit), 256)), dim3(256), 0, h->stream,
+                                      1, p);
   if (e != cudaSuccess) return e;
   *s = Ranked{to, 1, 0};
+  if (n <= 16) return few<16, MN>(h, n, Z, ldz, ids, to, Y, ldy);
+  if (n <= 32) return few<32, MN>(h, n, Z, ldz, ids, to, Y, ldy);
+  if (n <= kFewMost) return few<kFewMost, MN>(h, n, Z, ldz, ids, to, Y, ldy);
   return pairs<MN>(h, n, Z, ldz, ids, to, Y, ldy);
 }
 
