@@ -2,7 +2,7 @@
 // (a set of factor pairs) that its request names, and the gradients of the samples and of the adapters' factors.
 //
 // Launches of a forward pass:  adapter_rank_kernel (s = V x, in parts), adapter_sum_kernel, and for y = W x + scale U^T s up to 64 samples
-// adapter_few_kernel, for more adapter_pair_kernel;  of a backward pass:  adapter_index_kernel, adapter_rank_kernel (t = U dy; s again
+// adapter_few_kernel or adapter_stream_kernel, for more adapter_pair_kernel;  of a backward pass:  adapter_index_kernel, adapter_rank_kernel (t = U dy; s again
 // where it is not given), the products as in a forward pass (dx), adapter_words_kernel and adapter_gradient_kernel (dU, dV).
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -27,7 +27,8 @@ constexpr int kMaxStages = 8;
 // -1.1e-6 after 78 of them, -8e-6 after 512).  Sums that leave in fp32 are taken out, and added up with rounding, every 12 k-blocks.
 constexpr int kDrain = 12;
 constexpr int kListPitch = kMaxTile + 8;            // entries of a tile's list: their number, then the adapters
-constexpr int kSmallRing = 98304;                   // bytes of operand stages where two blocks share an SM
+constexpr int kSmallRing = 98304;                   // bytes of operand stages where two blocks share an SM,
+constexpr int kFewRing = 73728;                     // and of a block of adapter_rank_kernel beside one of adapter_stream_kernel
 
 __host__ __device__ constexpr int stage_bytes(int tn) { return kTileBytesA + tn * BK * 2; }
 
@@ -106,7 +107,7 @@ struct RankParams {
   int32_t rank, adapters;
   const int32_t* ids;
   float* out;                  // [parts][n][rank]
-  int32_t* mark;               // may be null: for each adapter in use, `call`
+  int32_t* mark;               // for each adapter in use, `call`
   int32_t call;
   uint32_t* status;
 };
@@ -139,7 +140,7 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
   tc_fence_after();
   const uint32_t tmem_base = tmem_slot;
   const int per = (p.rank + kSlice - 1) / kSlice, slices = L.count * per, chunks = (slices + 7) / 8;
-  if (p.mark && part == 0 && blockIdx.z == 0)
+  if (part == 0 && blockIdx.z == 0)
     for (int t = threadIdx.x; t < L.count; t += kRankThreads) p.mark[L.list[t]] = p.call;
 
   if (warp == 0) {
@@ -253,149 +254,272 @@ struct Ranked {
   int64_t stride;              // entries from a part to the next
 };
 __device__ __forceinline__ float ranked(const Ranked& s, int64_t at) {
-  float v = s.at[at];
-  for (int c = 1; c < s.parts; ++c) v += s.at[c * s.stride + at];
+  float v = 0.f;
+  for (int c = 0; c < s.parts; c += 8) {             // eight on their way
+    float x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] = c + u < s.parts ? s.at[(c + u) * s.stride + at] : 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v += x[u];
+  }
   return v;
 }
 
+constexpr int kEpi = 8;                             // epilogue warps of the products
+// x, y: row m (this lane's) of samples i and i + 1.  Even lanes store two rows of the first sample, odd lanes of the second.  By a warp.
+__device__ __forceinline__ void store_two(__nv_bfloat16* Y, int64_t ldy, int i, int n, int m, int most, float x, float y, int lane) {
+  const bool second = lane & 1;
+  const float got = __shfl_xor_sync(0xffffffffu, second ? x : y, 1);
+  const int at = i + (second ? 1 : 0), r = m & ~1;
+  if (at < n) {
+    __nv_bfloat16* to = Y + static_cast<int64_t>(at) * ldy + r;
+    const float lo = second ? got : x, hi = second ? y : got;
+    if (r + 1 < most) *reinterpret_cast<__nv_bfloat162*>(to) = __floats2bfloat162_rn(lo, hi);
+    else if (r < most) *to = __float2bfloat16_rn(lo);
+  }
+}
+
 // ---------------------------------------------------------------------------------------------------------
-// y_i = A z_i + scale F[a_i]^T p_i for up to 64 samples: a tile of 128 rows of A (rows of W; with MN, of its transpose: columns of W) a
-// cluster, whose CTAs share the contraction.  Bound by the way of W to the SMs: two CTAs an SM, 190 KB of loads under way on it.  While
-// the products run the other warps form the adapters' terms in fp32 from p and F in global memory, a sample by one CTA of the cluster;
-// the parts are added in rank order, each CTA finishing some of the samples.
-// The loads of A and z do not wait for the launch before (adapter_rank_kernel lets this one start once those before it are done).
-// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..5 adapters' terms and epilogue.
+// The adapters' term, scale F[a_i]^T p_i, of the three products below is more contraction behind the k-blocks of A: the factors of the
+// adapters in the tile's list, eight units of 8 ranks a k-block, against  scale p  of the samples in bf16 (one rounding, 2^-8 of the term;
+// the result is rounded by as much), with zeros where a sample has another adapter.  Zeros do not hide what is not finite:
+// adapter_sum_kernel has looked through the factors, and one that holds such entries is not loaded (its units are out of the map's
+// bounds, zeros); the end of the tile forms the term of its own samples in fp32.
+// (In fp32 FMAs from global memory, as it was for up to 64 samples, a tile's term is a chain of loads: 64 samples of 8 ranks took 99 us a
+// tile of 325,000 x 10,000, whose rows of W stream by in 57.)
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kFewThreads = 192, kFewMost = 64, kMaxCluster = 8;
-struct FewParams {
-  int32_t n, m;                // samples; rows of A
-  int32_t kseg, stages, parts; // k-blocks; operand stages; CTAs of a cluster
+constexpr int kUnit = 8, kUnits = BK / kUnit;
+struct Term {
   int32_t rank, adapters;
-  const int32_t* ids;
+  const int32_t *ids, *lists, *place;
   const float* scale;
+  const uint4* bad;            // [adapters]: not zero where the factors are not finite
   const __nv_bfloat16* F;      // [adapters][rank][ldf]
   int64_t ldf;
   const float* p;              // [n][rank]
+  const uint4* pb;             // [n][units of an adapter]: scale p in bf16, zeros behind
+};
+__device__ __forceinline__ int units_of(const Term& t) { return (t.rank + kUnit - 1) / kUnit; }
+__device__ __forceinline__ bool is_bad(const uint4& b) { return (b.x | b.y | b.z | b.w) != 0; }
+// The term of sample i at row m, where its adapter's factors are not finite; else 0.
+__device__ __noinline__ float bad_term(const Term& p, int i, int m) {
+  const int id = p.ids[i];
+  if (id < 0 || id >= p.adapters || !is_bad(p.bad[id])) return 0.f;
+  const __nv_bfloat16* f = p.F + static_cast<int64_t>(id) * p.rank * p.ldf + m;
+  const float* s = p.p + static_cast<int64_t>(i) * p.rank;
+  const float sc = p.scale[id];
+  float v = 0.f;
+  for (int r = 0; r < p.rank; ++r) v = fmaf(__bfloat162float(f[r * p.ldf]), sc * s[r], v);
+  return v;
+}
+// Whether some adapter in a list is bad; by a warp.
+__device__ __forceinline__ bool any_bad(const Term& p, const int32_t* list, int lane) {
+  bool any = false;
+  for (int x = lane; x < list[0]; x += 32) any |= is_bad(p.bad[list[1 + x]]);
+  return __any_sync(0xffffffffu, any);
+}
+// The adapter of unit g of `units`, out of the map's bounds where it is bad.
+__device__ __forceinline__ int unit_adapter(const Term& p, const int32_t* list, int g, int units, int per) {
+  if (g >= units) return 0;
+  const int a = list[1 + g / per];
+  return is_bad(p.bad[a]) ? p.adapters : a;
+}
+// Row t of the samples' operand of k-block k: scale p of a sample whose first unit is `at` (below zero: no adapter), and, beside an odd last
+// unit, zeros in the factors' operand (by threads x of `threads`).
+template <int THREADS>
+__device__ __forceinline__ void write_units(const uint4 (&words)[kUnits], uint8_t* st, int t, bool row, int nu) {
+  if (row) {
+    const uint32_t to = smem_u32(st) + kTileBytesA + t * 128;
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j)
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((j ^ (t & 7)) << 4)), "r"(words[j].x), "r"(words[j].y),
+                   "r"(words[j].z), "r"(words[j].w) : "memory");
+  }
+  if (nu & 1)
+    for (int x = t; x < 128; x += THREADS)
+      *reinterpret_cast<uint4*>(st + (x >> 6) * (kTileBytesA / 2) + nu * (kUnit * 128) + (x & 63) * 16) = make_uint4(0, 0, 0, 0);
+}
+__device__ __forceinline__ void read_units(const uint4* src, int at, int g0, int nu, int per, uint4 (&words)[kUnits]) {
+#pragma unroll
+  for (int j = 0; j < kUnits; ++j) {
+    const int u = g0 + j - at;
+    words[j] = at >= 0 && j < nu && u >= 0 && u < per ? src[u] : make_uint4(0, 0, 0, 0);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// y_i = A z_i + scale F[a_i]^T p_i for up to 64 samples: the rows of A (rows of W; with MN, of its transpose: columns of W) are the rows
+// of the accumulator, 128 of them a tile.  Bound by the way of W to the SMs.  The loads of A and z do not wait for the launches before
+// (adapter_rank_kernel lets the next one start once those before it are done).
+//
+// adapter_few_kernel, for few tiles: a tile a cluster, whose CTAs share the contraction and the k-blocks of the term; the parts are added
+// in rank order, each CTA finishing some of the samples.  Two CTAs an SM.
+// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..5 epilogue, 6 and 7 the samples' operand of the term.
+// ---------------------------------------------------------------------------------------------------------
+constexpr int kFewThreads = 256, kFewMost = 64, kMaxCluster = 8;
+struct FewParams {
+  Term term;
+  int32_t n, m;                // samples; rows of A
+  int32_t kseg, stages, parts; // k-blocks; operand stages; CTAs of a cluster
   __nv_bfloat16* Y;
   int64_t ldy;
+  int32_t tiles, cut, whole;   // adapter_stream_kernel: tiles of 128 rows; see Segments
+  float* partial;              // [CTAs][64][128 rows]
+  uint32_t* ready;             // [CTAs][kEpi]
   uint32_t* status;
 };
 
+// One k-block of A and z, or of factors, into a stage; by the producer's warp.
 template <int TN, bool MN>
-__global__ void __launch_bounds__(kFewThreads)
-adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ FewParams p) {
+__device__ __forceinline__ void few_load(uint8_t* st, uint64_t* full, const CUtensorMap& tmA, const CUtensorMap& tmZ, int k, int m0, uint64_t keep) {
+  if (!elect_one()) return;
+  mbar_expect_tx(full, stage_bytes(TN));
+  if (MN) {
+    tma_load_2d(st, &tmA, m0, k * BK, full);
+    tma_load_2d(st + kTileBytesA / 2, &tmA, m0 + 64, k * BK, full);
+  } else {
+    tma_load_2d(st, &tmA, k * BK, m0, full);
+  }
+  tma_load_2d_hint(st + kTileBytesA, &tmZ, k * BK, 0, full, keep);     // (every tile reads the samples)
+}
+__device__ __forceinline__ void few_load_units(uint8_t* st, uint64_t* full, uint64_t* free_, const CUtensorMap& tmF, int known, int g0, int nu, int per, int m0) {
+  if (elect_one()) {
+    mbar_arrive(free_);
+    mbar_expect_tx(full, nu * 2 * kUnit * 128);
+  }
+  __syncwarp();
+  for (int j = 0; j < nu; ++j) {
+    const int a = __shfl_sync(0xffffffffu, known, (g0 + j) & 31), y = (g0 + j) % per * kUnit;
+    if (elect_one()) {
+      tma_load_3d(st + j * (kUnit * 128), &tmF, m0, y, a, full);
+      tma_load_3d(st + kTileBytesA / 2 + j * (kUnit * 128), &tmF, m0 + 64, y, a, full);
+    }
+  }
+}
+template <bool MN>
+__device__ __forceinline__ void few_mma(uint32_t st, uint32_t d_tmem, uint32_t idesc, bool first) {
+  const uint64_t da = MN ? umma_desc_mn128(st) : umma_desc_k128(st), db = umma_desc_k128(st + kTileBytesA);
+#pragma unroll
+  for (int j = 0; j < BK / 16; ++j) umma_bf16(d_tmem, da + (MN ? 128 : 2) * j, db + 2 * j, idesc, !first || j ? 1u : 0u);
+}
+__device__ __forceinline__ void few_mma_units(uint32_t st, uint32_t d_tmem, uint32_t idesc, int nu) {
+  const uint64_t da = umma_desc_mn128(st), db = umma_desc_k128(st + kTileBytesA);
+  for (int j = 0; j < (nu + 1) / 2; ++j) umma_bf16(d_tmem, da + 128 * j, db + 2 * j, idesc, 1u);
+}
+
+template <int TN, bool MN>
+__global__ void __launch_bounds__(kFewThreads, 2)
+adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ CUtensorMap tmF,
+                   const __grid_constant__ FewParams p) {
   constexpr int kStage = stage_bytes(TN), kCols = TN < 32 ? 32 : TN;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], done;
+  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], free_[kMaxStages], built[kMaxStages], done;
   __shared__ uint32_t tmem_slot, abort_word;
-  __shared__ int32_t id_of[TN];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  float* ps = reinterpret_cast<float*>(smem + p.stages * kStage);           // [n][rank]: scale * p
   volatile uint32_t* abort_flag = &abort_word;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const int mine = static_cast<int>(blockIdx.x) % p.parts, m0 = static_cast<int>(blockIdx.x) / p.parts * BM;
   const int kbeg = mine * p.kseg / p.parts, nk = (mine + 1) * p.kseg / p.parts - kbeg;
+  const int per = units_of(p.term);
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
-    for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+    for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&built[i], 2); }
     mbar_init(&done, 1);
     abort_word = 0;
     fence_barrier_init();
-    prefetch_tmap(&tmA); prefetch_tmap(&tmZ);
+    prefetch_tmap(&tmA); prefetch_tmap(&tmZ); prefetch_tmap(&tmF);
   }
   if (warp == 1) { tmem_alloc(&tmem_slot, kCols); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = tmem_slot;
+  bool any = false;                                  // some adapter is bad
 
   if (warp == 0) {
-    const uint64_t pol_keep = policy_evict_last();      // every tile reads the samples
+    const uint64_t keep = policy_evict_last();
+    uint32_t s = 0, ph = 0;
     bool ok = true;
-    for (int k = 0; k < nk && ok; ++k) {
-      const uint32_t s = k % p.stages, ph = (k / p.stages) & 1;
+    auto next = [&]() { if (++s == static_cast<uint32_t>(p.stages)) { s = 0; ph ^= 1; } };
+    for (int k = 0; k < nk && ok; ++k, next()) {
       ok = mbar_wait_warp(&empty[s], ph ^ 1, abort_flag);
-      if (ok && elect_one()) {
-        uint8_t* st = smem + s * kStage;
-        mbar_expect_tx(&full[s], kStage);
-        if (MN) {
-          tma_load_2d(st, &tmA, m0, (kbeg + k) * BK, &full[s]);
-          tma_load_2d(st + kTileBytesA / 2, &tmA, m0 + 64, (kbeg + k) * BK, &full[s]);
-        } else {
-          tma_load_2d(st, &tmA, (kbeg + k) * BK, m0, &full[s]);
-        }
-        tma_load_2d_hint(st + kTileBytesA, &tmZ, (kbeg + k) * BK, 0, &full[s], pol_keep);
-      }
+      if (ok) few_load<TN, MN>(smem + s * kStage, &full[s], tmA, tmZ, kbeg + k, m0, keep);
+    }
+    pdl_wait();
+    const int units = p.term.lists[0] * per;
+    for (int g0 = mine * kUnits; g0 < units && ok; g0 += p.parts * kUnits, next()) {
+      const int known = unit_adapter(p.term, p.term.lists, (g0 & ~31) + lane, units, per);
+      ok = mbar_wait_warp(&empty[s], ph ^ 1, abort_flag);
+      if (ok) few_load_units(smem + s * kStage, &full[s], &free_[s], tmF, known, g0, min(kUnits, units - g0), per, m0);
     }
   } else if (warp == 1) {
-    const uint32_t idesc = umma_idesc_bf16(BM, TN) | (MN ? 1u << 15 : 0u);
+    const uint32_t idesc_f = umma_idesc_bf16(BM, TN) | 1u << 15, idesc = MN ? idesc_f : umma_idesc_bf16(BM, TN);
+    uint32_t s = 0, ph = 0, bph = 0;
     bool ok = true;
-    for (int k = 0; k < nk && ok; ++k) {
-      const uint32_t s = k % p.stages, ph = (k / p.stages) & 1;
+    auto next = [&]() { if (++s == static_cast<uint32_t>(p.stages)) { s = 0; ph ^= 1; } };
+    for (int k = 0; k < nk && ok; ++k, next()) {
       ok = mbar_wait_warp(&full[s], ph, abort_flag);
       tc_fence_after();
       if (ok && elect_one()) {
-        const uint32_t a = smem_u32(smem + s * kStage);
-        const uint64_t da = MN ? umma_desc_mn128(a) : umma_desc_k128(a), db = umma_desc_k128(a + kTileBytesA);
-#pragma unroll
-        for (int j = 0; j < BK / 16; ++j) umma_bf16(tmem_base, da + (MN ? 128 : 2) * j, db + 2 * j, idesc, k | j ? 1u : 0u);
+        few_mma<MN>(smem_u32(smem + s * kStage), tmem_base, idesc, k == 0);
+        umma_commit(&empty[s]);
+      }
+    }
+    pdl_wait();
+    const int units = p.term.lists[0] * per;
+    for (int g0 = mine * kUnits; g0 < units && ok; g0 += p.parts * kUnits, next()) {
+      ok = mbar_wait_warp(&full[s], ph, abort_flag) && mbar_wait_warp(&built[s], (bph >> s) & 1, abort_flag);
+      bph ^= 1u << s;
+      tc_fence_after();
+      if (ok && elect_one()) {
+        few_mma_units(smem_u32(smem + s * kStage), tmem_base, idesc_f, min(kUnits, units - g0));
         umma_commit(&empty[s]);
       }
     }
     if (ok && elect_one()) umma_commit(&done);
-  } else {
-    const int q = warp & 3, tid = threadIdx.x - 64, m = m0 + q * 32 + lane;
+  } else if (warp < 6) {
     pdl_wait();
-    for (int t = tid; t < TN; t += 128) {
-      const int id = t < p.n ? p.ids[t] : -1;
-      id_of[t] = id >= 0 && id < p.adapters ? id : -1;
-    }
-    asm volatile("bar.sync 1, 128;" ::: "memory");
-    for (int x = tid; x < p.n * p.rank; x += 128) {
-      const int id = id_of[x / p.rank];
-      ps[x] = id >= 0 ? p.scale[id] * p.p[x] : 0.f;
-    }
-    asm volatile("bar.sync 1, 128;" ::: "memory");
-    float e[TN];
-#pragma unroll
-    for (int t = 0; t < TN; ++t) {
-      e[t] = 0.f;
-      if (t >= p.n || t % p.parts != mine || m >= p.m) continue;
-      const int id = id_of[t];
-      if (id < 0) continue;
-      const __nv_bfloat16* f = p.F + static_cast<int64_t>(id) * p.rank * p.ldf + m;
-      const float* w = ps + t * p.rank;
-      float v = 0.f;
-      int r = 0;
-      for (; r + 8 <= p.rank; r += 8) {
-        float x[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) x[u] = __bfloat162float(f[(r + u) * p.ldf]);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) v = fmaf(x[u], w[r + u], v);
-      }
-      for (; r < p.rank; ++r) v = fmaf(__bfloat162float(f[r * p.ldf]), w[r], v);
-      e[t] = v;
-    }
-    // the accumulator and the terms to shared memory (the operand stages', which nothing uses any more): [sample][128 rows]
+    // the accumulator to shared memory (the operand stages', which nothing uses any more): [sample][128 rows]
+    const int q = warp & 3;
     if (mbar_wait_warp(&done, 0, abort_flag)) {
       tc_fence_after();
       float* to = reinterpret_cast<float*>(smem) + q * 32 + lane;
-#pragma unroll
+#pragma unroll 1
       for (int t0 = 0; t0 < TN; t0 += 32) {
         uint32_t acc[32];
         tmem_ld_32x32(tmem_base + (static_cast<uint32_t>(q * 32) << 16) + t0, acc);
         tmem_ld_wait();
 #pragma unroll
         for (int j = 0; j < 32; ++j)
-          if (t0 + j < TN) to[(t0 + j) * BM] = __uint_as_float(acc[j]) + e[t0 + j < TN ? t0 + j : 0];
+          if (t0 + j < TN) to[(t0 + j) * BM] = __uint_as_float(acc[j]);
       }
+    }
+  } else {
+    pdl_wait();
+    const int t = (warp - 6) * 32 + lane;            // this thread's sample
+    const int units = p.term.lists[0] * per, at = t < p.n ? p.term.place[t] * per : -1;
+    const uint4* src = p.term.pb + t * per;
+    uint32_t s = static_cast<uint32_t>(nk) % p.stages, fph = 0;
+    bool ok = true;
+    for (int g0 = mine * kUnits; g0 < units && ok; g0 += p.parts * kUnits) {
+      const int nu = min(kUnits, units - g0);
+      uint4 words[kUnits];
+      read_units(src, at, g0, nu, per, words);
+      ok = mbar_wait_warp(&free_[s], (fph >> s) & 1, abort_flag);
+      if (!ok) break;
+      fph ^= 1u << s;
+      write_units<64>(words, smem + s * kStage, t, t < TN, nu);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&built[s]);
+      if (++s == static_cast<uint32_t>(p.stages)) s = 0;
     }
   }
   __syncwarp();
   if (p.parts > 1) { cluster_arrive(); cluster_wait(); }
   else __syncthreads();
   if (!abort_word) {
+    any = any_bad(p.term, p.term.lists, lane);
     // a lane takes two rows of a sample, a warp half of its 128
     const int t1 = min((mine + 1) * TN / p.parts, p.n);
     for (int x = mine * TN / p.parts * 2 + warp; x < 2 * t1; x += kFewThreads / 32) {
@@ -406,6 +530,10 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         float2 w;
         asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(w.x), "=f"(w.y) : "r"(mapa_u32(at, c)) : "memory");
         v = c ? make_float2(v.x + w.x, v.y + w.y) : w;
+      }
+      if (any) {
+        if (m < p.m) v.x += bad_term(p.term, t, m);
+        if (m + 1 < p.m) v.y += bad_term(p.term, t, m + 1);
       }
       __nv_bfloat16* y = p.Y + t * p.ldy + m;
       if (m + 1 < p.m) *reinterpret_cast<__nv_bfloat162*>(y) = __floats2bfloat162_rn(v.x, v.y);
@@ -425,36 +553,219 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 }
 
 // ---------------------------------------------------------------------------------------------------------
+// adapter_stream_kernel, for more tiles: a CTA an SM takes its even share of all k-blocks of A, whole tiles first (Segments in
+// sfb_tile.cuh), so that every SM streams as much of W as the others from the start to the end; the CTA that finishes a tile has its term.
+// Two accumulators: the end of a tile runs beside the next one's products.
+// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the samples), 10 and 11 the samples'
+// operand of the term.
+// ---------------------------------------------------------------------------------------------------------
+constexpr int kStreamThreads = 384, kStreamRing = 143360;
+template <int TN, bool MN>
+__global__ void __maxnreg__(88)                       // (a block of adapter_rank_kernel has registers beside it)
+adapter_stream_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ CUtensorMap tmF,
+                      const __grid_constant__ FewParams p) {
+  constexpr int kStage = stage_bytes(TN), kCols = TN < 32 ? 32 : TN, kMine = TN == 64 ? 32 : 16;      // columns of a warp
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], free_[kMaxStages], built[kMaxStages], tfull[2], tempty[2];
+  __shared__ uint32_t tmem_slot, abort_word;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  volatile uint32_t* abort_flag = &abort_word;
+  const int warp = warp_index(), lane = threadIdx.x & 31, cta = blockIdx.x, ctas = gridDim.x;
+  const Segments segs(p.kseg, p.cut != 0, p.whole, p.tiles, cta, ctas);
+  const int per = units_of(p.term);
+  pdl_launch_dependents();
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&built[i], 2); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], kEpi); }
+    abort_word = 0;
+    fence_barrier_init();
+    prefetch_tmap(&tmA); prefetch_tmap(&tmZ); prefetch_tmap(&tmF);
+  }
+  if (warp == 1) { tmem_alloc(&tmem_slot, 2 * kCols); tmem_relinquish(); }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_slot;
+
+  if (warp == 0) {
+    const uint64_t keep = policy_evict_last();
+    uint32_t s = 0, ph = 0;
+    bool ok = true;
+    auto next = [&]() { if (++s == static_cast<uint32_t>(p.stages)) { s = 0; ph ^= 1; } };
+    int units = -1, known0 = 0;                      // the first 32 units' adapters: the same for every tile
+    for (int i = 0; i < segs.n && ok; ++i) {
+      const Segment sg = segs.get(i);
+      const int m0 = sg.tile * BM;
+      for (int k = sg.k0; k < sg.k1 && ok; ++k, next()) {
+        ok = mbar_wait_warp(&empty[s], ph ^ 1, abort_flag);
+        if (ok) few_load<TN, MN>(smem + s * kStage, &full[s], tmA, tmZ, k, m0, keep);
+      }
+      if (sg.k1 < p.kseg) continue;
+      if (units < 0) {
+        pdl_wait();
+        units = p.term.lists[0] * per;
+        known0 = unit_adapter(p.term, p.term.lists, lane, units, per);
+      }
+      for (int g0 = 0, known = known0; g0 < units && ok; g0 += kUnits, next()) {
+        if (g0 && (g0 & 31) == 0) known = unit_adapter(p.term, p.term.lists, g0 + lane, units, per);
+        ok = mbar_wait_warp(&empty[s], ph ^ 1, abort_flag);
+        if (ok) few_load_units(smem + s * kStage, &full[s], &free_[s], tmF, known, g0, min(kUnits, units - g0), per, m0);
+      }
+    }
+  } else if (warp == 1) {
+    const uint32_t idesc_f = umma_idesc_bf16(BM, TN) | 1u << 15, idesc = MN ? idesc_f : umma_idesc_bf16(BM, TN);
+    uint32_t s = 0, ph = 0, bph = 0;
+    bool ok = true;
+    auto next = [&]() { if (++s == static_cast<uint32_t>(p.stages)) { s = 0; ph ^= 1; } };
+    int units = -1;
+    for (int i = 0; i < segs.n && ok; ++i) {
+      const Segment sg = segs.get(i);
+      const uint32_t a = i & 1, aph = (i >> 1) & 1, d_tmem = tmem_base + a * kCols;
+      if (!mbar_wait_warp(&tempty[a], aph ^ 1, abort_flag)) break;
+      tc_fence_after();
+      for (int k = sg.k0; k < sg.k1 && ok; ++k, next()) {
+        ok = mbar_wait_warp(&full[s], ph, abort_flag);
+        tc_fence_after();
+        if (ok && elect_one()) {
+          few_mma<MN>(smem_u32(smem + s * kStage), d_tmem, idesc, k == sg.k0);
+          umma_commit(&empty[s]);
+        }
+      }
+      if (sg.k1 == p.kseg) {
+        if (units < 0) {
+          pdl_wait();
+          units = p.term.lists[0] * per;
+        }
+        for (int g0 = 0; g0 < units && ok; g0 += kUnits, next()) {
+          ok = mbar_wait_warp(&full[s], ph, abort_flag) && mbar_wait_warp(&built[s], (bph >> s) & 1, abort_flag);
+          bph ^= 1u << s;
+          tc_fence_after();
+          if (ok && elect_one()) {
+            few_mma_units(smem_u32(smem + s * kStage), d_tmem, idesc_f, min(kUnits, units - g0));
+            umma_commit(&empty[s]);
+          }
+        }
+      }
+      if (ok && elect_one()) umma_commit(&tfull[a]);
+    }
+  } else if (warp < 2 + kEpi) {
+    const int w8 = warp - 2, q = warp & 3, h = w8 >> 2, t0 = h * kMine;
+    pdl_wait();
+    const bool any = any_bad(p.term, p.term.lists, lane);
+    for (int i = 0; i < segs.n; ++i) {
+      const Segment sg = segs.get(i);
+      const int m = sg.tile * BM + q * 32 + lane;
+      const uint32_t a = i & 1, aph = (i >> 1) & 1;
+      if (!mbar_wait_warp(&tfull[a], aph, abort_flag)) break;
+      tc_fence_after();
+      const bool mine = t0 < TN;
+      float v[kMine];
+      if (mine) {
+        uint32_t acc[kMine];
+        const uint32_t at = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + a * kCols + t0;
+        if constexpr (kMine == 32) tmem_ld_32x32(at, acc);
+        else tmem_ld_32x16(at, acc);
+        tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) v[j] = __uint_as_float(acc[j]);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&tempty[a]);
+      if (!mine) continue;
+      const int64_t to = static_cast<int64_t>(t0) * BM + q * 32 + lane;     // of a CTA's part: [sample][128 rows]
+      if (sg.k1 < p.kseg) {
+        float* part = p.partial + static_cast<int64_t>(cta) * kFewMost * BM + to;
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) __stcg(part + j * BM, v[j]);
+        __syncwarp();
+        if (lane == 0) {
+          __threadfence();
+          st_release(p.ready + cta * kEpi + w8, 1u);
+        }
+        continue;
+      }
+      const int from = segs.first_part(sg);
+      bool ok = true;
+      for (int c = from; c < cta && ok; ++c) ok = __all_sync(0xffffffffu, lane != 0 || flag_wait(p.ready + c * kEpi + w8, abort_flag));
+      if (!ok) break;
+      if (lane == 0)
+        for (int c = from; c < cta; ++c) p.ready[c * kEpi + w8] = 0;        // for the next launch
+      __syncwarp();
+      for (int c = from; c < cta; ++c) {
+        const float* part = p.partial + static_cast<int64_t>(c) * kFewMost * BM + to;
+#pragma unroll
+        for (int j0 = 0; j0 < kMine; j0 += 16) {
+          float x[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) x[j] = __ldcg(part + (j0 + j) * BM);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[j0 + j] += x[j];
+        }
+      }
+      if (any && m < p.m) {
+#pragma unroll
+        for (int j = 0; j < kMine; ++j)
+          if (t0 + j < p.n) v[j] += bad_term(p.term, t0 + j, m);
+      }
+#pragma unroll
+      for (int j = 0; j < kMine; j += 2) store_two(p.Y, p.ldy, t0 + j, p.n, m, p.m, v[j], v[j + 1], lane);
+    }
+  } else {
+    pdl_wait();
+    const int t = (warp - 2 - kEpi) * 32 + lane;     // this thread's sample
+    const int units = p.term.lists[0] * per, at = t < p.n ? p.term.place[t] * per : -1;
+    const uint4* src = p.term.pb + t * per;
+    uint32_t g = 0, fph = 0;                         // k-blocks so far; the phases of free_, a bit per stage
+    bool ok = true;
+    for (int i = 0; i < segs.n && ok; ++i) {
+      const Segment sg = segs.get(i);
+      g += sg.k1 - sg.k0;
+      if (sg.k1 < p.kseg) continue;
+      for (int g0 = 0; g0 < units; g0 += kUnits, ++g) {
+        const uint32_t s = g % p.stages;
+        const int nu = min(kUnits, units - g0);
+        uint4 words[kUnits];
+        read_units(src, at, g0, nu, per, words);
+        ok = mbar_wait_warp(&free_[s], (fph >> s) & 1, abort_flag);
+        if (!ok) break;
+        fph ^= 1u << s;
+        write_units<64>(words, smem + s * kStage, t, t < TN, nu);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&built[s]);
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (abort_word) {
+    if (threadIdx.x == 0) atomicOr(p.status, SFB_STATUS_TIMEOUT);
+    for (int i = 0; i < 64; ++i) __nanosleep(1000);
+    __syncthreads();
+  }
+  if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem_base, 2 * kCols); }
+}
+
+// ---------------------------------------------------------------------------------------------------------
 // The same for more samples, on pairs of CTAs (cta_group::2): a tile of 256 rows of A x tn samples (128 or 256), a CTA 128 of the rows in
 // its TMEM; it loads its own rows and its half of the samples, 32 KB a k-block.  Two accumulators: the end of a tile runs beside the next
 // one's products.  Whole rounds of tiles are taken whole, the k-blocks of the rest are shared out (Segments in sfb_tile.cuh).
 //
-// The adapters' term is more contraction: behind the k-blocks of A the pair that finishes a tile takes the factors of the adapters in
-// the tile's list, eight units of 8 ranks a k-block, against  scale p  of the samples in bf16 (one rounding, 2^-8 of the term; the
-// result is rounded by as much), with zeros where a sample has another adapter.  Zeros do not hide what is not finite: adapter_sum_kernel
-// has looked through the factors, and one that holds such entries is not loaded (its units are out of the map's bounds, zeros); the end
-// of the tile forms the term of its own samples in fp32.
+// The pair that finishes a tile has its term.
 //
 // Warps: 0 TMA producer, 1 MMA issuer (leader CTA) and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the columns), 10..13
 // the samples' operand of the adapters' term.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kUnit = 8, kUnits = BK / kUnit;
-constexpr int kPairThreads = 448, kEpi = 8, kBuild = 4, kGroup = 8;      // kGroup: tiles of samples that follow one another
+constexpr int kPairThreads = 448, kBuild = 4, kGroup = 8;      // kGroup: tiles of samples that follow one another
 constexpr int kPairStages = 6, kPairStage = 2 * kTileBytesA;
 constexpr int kPairSmem = kPairStages * kPairStage + 1024;
 constexpr int kPartFloats = BM * kMaxTile;          // what a CTA leaves of a tile
 struct PairParams {
+  Term term;
   int32_t n, tn, tilesT, tilesM, m;
   int32_t kseg, cut, whole;    // k-blocks; see Segments
-  int32_t rank, adapters;
-  const int32_t* ids;
-  const int32_t *lists, *place;
-  const float* scale;
-  const uint4* bad;            // [adapters]: not zero where the factors are not finite
-  const __nv_bfloat16* F;
-  int64_t ldf;
-  const float* p;              // [n][rank]
-  const __nv_bfloat16* pb;     // [n][rank rounded up to 8]: scale p, zeros behind
   __nv_bfloat16* Y;
   int64_t ldy;
   float* partial;              // [pairs][2][kPartFloats]
@@ -481,19 +792,6 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity
   return __all_sync(0xffffffffu, got);
 }
 
-__device__ __forceinline__ bool is_bad(const uint4& b) { return (b.x | b.y | b.z | b.w) != 0; }
-// The adapter's term of sample i at row m, where its factors are not finite; else 0.
-__device__ __noinline__ float bad_term(const PairParams& p, int i, int m) {
-  const int id = p.ids[i];
-  if (id < 0 || id >= p.adapters || !is_bad(p.bad[id])) return 0.f;
-  const __nv_bfloat16* f = p.F + static_cast<int64_t>(id) * p.rank * p.ldf + m;
-  const float* s = p.p + static_cast<int64_t>(i) * p.rank;
-  const float sc = p.scale[id];
-  float v = 0.f;
-  for (int r = 0; r < p.rank; ++r) v = fmaf(__bfloat162float(f[r * p.ldf]), sc * s[r], v);
-  return v;
-}
-
 template <bool MN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ CUtensorMap tmF,
@@ -510,7 +808,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x >> 1, half = p.tn / 2;
   const Segments segs(p.kseg, p.cut != 0, p.whole, p.tilesT * p.tilesM, pair, gridDim.x >> 1);
-  const int per = (p.rank + kUnit - 1) / kUnit;      // units of an adapter
+  const int per = units_of(p.term);
   // Tiles that run at the same time: kGroup tiles of samples against as many rows of A as there are pairs for.
   auto tile_coords = [&](int tile, int& m0, int& tt) {
     const int in = kGroup * p.tilesM, g = tile / in, width = min(kGroup, p.tilesT - g * kGroup), at = tile - g * in;
@@ -547,19 +845,16 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       int m0, tt;
       tile_coords(sg.tile, m0, tt);
       const int z0 = tt * p.tn + static_cast<int>(rank) * half;
-      const int32_t* list = p.lists + static_cast<int64_t>(tt) * kListPitch;
-      const int units = sg.k1 == p.kseg ? list[0] * per : 0, more = (units + kUnits - 1) / kUnits;
-      // the adapter of unit g (out of bounds where it is bad); of four k-blocks by the lanes
-      auto adapter_of = [&](int g) {
-        if (g >= units) return 0;
-        const int a = list[1 + g / per];
-        return is_bad(p.bad[a]) ? p.adapters : a;
-      };
-      int known = adapter_of(lane);
-      for (int k = sg.k0; k < sg.k1 + more; ++k) {
-        if (!mbar_wait_warp(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
-        uint8_t* st = smem + s * kPairStage;
-        if (k < sg.k1) {
+      // of four k-blocks of factors at a time the lanes hold the adapter of a unit, out of bounds where it is bad; what that needs is
+      // asked for ahead of the loads of A, one step before and one among them
+      const int32_t* list = p.term.lists + static_cast<int64_t>(tt) * kListPitch;
+      const int count = sg.k1 == p.kseg ? list[0] : 0;
+      int known = list[1 + lane / per];
+      auto settled = [&](int g, int a) { return g < count * per ? is_bad(p.term.bad[a]) ? p.term.adapters : a : 0; };
+      auto loads = [&](int k0, int k1) {
+        for (int k = k0; k < k1; ++k) {
+          if (!mbar_wait_warp(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
+          uint8_t* st = smem + s * kPairStage;
           if (elect_one()) {
             if (rank == 0) mbar_expect_tx(&full[s], 2 * (kTileBytesA + half * BK * 2));
             const uint32_t bar = mapa_u32(smem_u32(&full[s]), 0);
@@ -571,21 +866,33 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             }
             tma_load_2d_pair(st + kTileBytesA, &tmZ, k * BK, z0, bar, pol);
           }
-        } else {
-          const int g0 = (k - sg.k1) * kUnits, nu = min(kUnits, units - g0);
+          if (++s == static_cast<uint32_t>(kPairStages)) { s = 0; ph ^= 1; }
+        }
+      };
+      const int mid = min(sg.k0 + 4, sg.k1);
+      loads(sg.k0, mid);
+      known = settled(lane, known);
+      if (ok) loads(mid, sg.k1);
+      const int units = count * per, more = (units + kUnits - 1) / kUnits;
+      for (int k = 0; k < more && ok; ++k) {
+        if (!mbar_wait_warp(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
+        uint8_t* st = smem + s * kPairStage;
+        const int g0 = k * kUnits, nu = min(kUnits, units - g0);
+        if (elect_one()) {
+          mbar_arrive(&free_[s]);
+          if (rank == 0) mbar_expect_tx(&full[s], 2 * nu * 2 * kUnit * 128);
+        }
+        const uint32_t bar = mapa_u32(smem_u32(&full[s]), 0);
+        for (int j = 0; j < nu; ++j) {
+          const int a = __shfl_sync(0xffffffffu, known, (g0 + j) & 31), y = (g0 + j) % per * kUnit;
           if (elect_one()) {
-            mbar_arrive(&free_[s]);
-            if (rank == 0) mbar_expect_tx(&full[s], 2 * nu * 2 * kUnit * 128);
+            tma_load_3d_pair(st + j * (kUnit * 128), &tmF, m0, y, a, bar);
+            tma_load_3d_pair(st + kTileBytesA / 2 + j * (kUnit * 128), &tmF, m0 + 64, y, a, bar);
           }
-          const uint32_t bar = mapa_u32(smem_u32(&full[s]), 0);
-          for (int j = 0; j < nu; ++j) {
-            const int a = __shfl_sync(0xffffffffu, known, (g0 + j) & 31), y = (g0 + j) % per * kUnit;
-            if (elect_one()) {
-              tma_load_3d_pair(st + j * (kUnit * 128), &tmF, m0, y, a, bar);
-              tma_load_3d_pair(st + kTileBytesA / 2 + j * (kUnit * 128), &tmF, m0 + 64, y, a, bar);
-            }
-          }
-          if (((g0 + kUnits) & 31) == 0) known = adapter_of(g0 + kUnits + lane);
+        }
+        if (((g0 + kUnits) & 31) == 0 && g0 + kUnits < units) {
+          const int g = g0 + kUnits + lane;
+          known = settled(g, g < units ? list[1 + g / per] : 0);
         }
         if (++s == static_cast<uint32_t>(kPairStages)) { s = 0; ph ^= 1; }
       }
@@ -600,31 +907,32 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         const Segment sg = segs.get(i);
         int m0, tt;
         tile_coords(sg.tile, m0, tt);
-        const int units = sg.k1 == p.kseg ? p.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0, more = (units + kUnits - 1) / kUnits;
+        const int count = sg.k1 == p.kseg ? p.term.lists[static_cast<int64_t>(tt) * kListPitch] : 0;
         const uint32_t a = i & 1, aph = (i >> 1) & 1, d_tmem = tmem_base + a * kMaxTile;
         if (!mbar_wait_warp(&tempty[a], aph ^ 1, abort_flag)) { ok = false; break; }
         tc_fence_after();
-        for (int k = sg.k0; k < sg.k1 + more; ++k) {
-          const uint32_t st = smem_u32(smem + s * kPairStage);
+        for (int k = sg.k0; k < sg.k1; ++k) {
           if (!mbar_wait_warp(&full[s], ph, abort_flag)) { ok = false; break; }
-          if (k < sg.k1) {
-            tc_fence_after();
-            if (elect_one()) {
-              const uint64_t da = MN ? umma_desc_mn128(st) : umma_desc_k128(st), db = umma_desc_k128(st + kTileBytesA);
+          tc_fence_after();
+          if (elect_one()) {
+            const uint32_t st = smem_u32(smem + s * kPairStage);
+            const uint64_t da = MN ? umma_desc_mn128(st) : umma_desc_k128(st), db = umma_desc_k128(st + kTileBytesA);
 #pragma unroll
-              for (int j = 0; j < BK / 16; ++j) umma_bf16_pair(d_tmem, da + (MN ? 128 : 2) * j, db + 2 * j, idesc, (k - sg.k0) | j ? 1u : 0u);
-              umma_commit_pair(&empty[s], 3);
-            }
-          } else {
-            if (!mbar_wait_cluster(&built[s], (bph >> s) & 1, abort_flag)) { ok = false; break; }
-            bph ^= 1u << s;
-            tc_fence_after();
-            const int ns = (min(kUnits, units - (k - sg.k1) * kUnits) + 1) / 2;      // instructions: two units each
-            if (elect_one()) {
-              const uint64_t da = umma_desc_mn128(st), db = umma_desc_k128(st + kTileBytesA);
-              for (int j = 0; j < ns; ++j) umma_bf16_pair(d_tmem, da + 128 * j, db + 2 * j, idesc_f, 1u);
-              umma_commit_pair(&empty[s], 3);
-            }
+            for (int j = 0; j < BK / 16; ++j) umma_bf16_pair(d_tmem, da + (MN ? 128 : 2) * j, db + 2 * j, idesc, (k - sg.k0) | j ? 1u : 0u);
+            umma_commit_pair(&empty[s], 3);
+          }
+          if (++s == static_cast<uint32_t>(kPairStages)) { s = 0; ph ^= 1; }
+        }
+        for (int left = count * per; left > 0 && ok; left -= kUnits) {
+          if (!mbar_wait_warp(&full[s], ph, abort_flag) || !mbar_wait_cluster(&built[s], (bph >> s) & 1, abort_flag)) { ok = false; break; }
+          bph ^= 1u << s;
+          tc_fence_after();
+          const int ns = (min(kUnits, left) + 1) / 2;                  // instructions: two units each
+          if (elect_one()) {
+            const uint32_t st = smem_u32(smem + s * kPairStage);
+            const uint64_t da = umma_desc_mn128(st), db = umma_desc_k128(st + kTileBytesA);
+            for (int j = 0; j < ns; ++j) umma_bf16_pair(d_tmem, da + 128 * j, db + 2 * j, idesc_f, 1u);
+            umma_commit_pair(&empty[s], 3);
           }
           if (++s == static_cast<uint32_t>(kPairStages)) { s = 0; ph ^= 1; }
         }
@@ -641,11 +949,8 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       int m0, tt;
       tile_coords(sg.tile, m0, tt);
       const uint32_t a = i & 1, aph = (i >> 1) & 1;
-      const int32_t* list = p.lists + static_cast<int64_t>(tt) * kListPitch;
-      bool any = false;                              // some adapter of the tile is bad
-      if (sg.k1 == p.kseg)
-        for (int x = lane; x < list[0]; x += 32) any |= is_bad(p.bad[list[1 + x]]);
-      any = __any_sync(0xffffffffu, any);
+      const int32_t* list = p.term.lists + static_cast<int64_t>(tt) * kListPitch;
+      const bool any = sg.k1 == p.kseg && any_bad(p.term, list, lane);
       if (!mbar_wait_warp(&tfull[a], aph, abort_flag)) { ok = false; break; }
       tc_fence_after();
       const uint32_t t_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + a * kMaxTile + h * cols;
@@ -689,22 +994,11 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         if (any && m < p.m) {
 #pragma unroll
           for (int j = 0; j < 32; ++j)
-            if (i0 + j < p.n) acc[j] = __float_as_uint(__uint_as_float(acc[j]) + bad_term(p, i0 + j, m));
+            if (i0 + j < p.n) acc[j] = __float_as_uint(__uint_as_float(acc[j]) + bad_term(p.term, i0 + j, m));
         }
-        // two samples at a time: even lanes store two rows of the first, odd lanes of the second
 #pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-          const float x = __uint_as_float(acc[j]), y = __uint_as_float(acc[j + 1]);
-          const bool second = lane & 1;
-          const float got = __shfl_xor_sync(0xffffffffu, second ? x : y, 1);
-          const int i = i0 + j + (second ? 1 : 0), r = m & ~1;
-          if (i < p.n) {
-            __nv_bfloat16* to = p.Y + static_cast<int64_t>(i) * p.ldy + r;
-            const float lo = second ? got : x, hi = second ? y : got;
-            if (r + 1 < p.m) *reinterpret_cast<__nv_bfloat162*>(to) = __floats2bfloat162_rn(lo, hi);
-            else if (r < p.m) *to = __float2bfloat16_rn(lo);
-          }
-        }
+        for (int j = 0; j < 32; j += 2)
+          store_two(p.Y, p.ldy, i0 + j, p.n, m, p.m, __uint_as_float(acc[j]), __uint_as_float(acc[j + 1]), lane);
       }
       __syncwarp();
       if (leave && lane == 0) {
@@ -722,31 +1016,19 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       int m0, tt;
       tile_coords(sg.tile, m0, tt);
       g += sg.k1 - sg.k0;
-      const int units = sg.k1 == p.kseg ? p.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0, more = (units + kUnits - 1) / kUnits;
+      const int units = sg.k1 == p.kseg ? p.term.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0, more = (units + kUnits - 1) / kUnits;
       const int smp = tt * p.tn + static_cast<int>(rank) * half + t;
-      const int at = t < half && smp < p.n ? p.place[smp] * per : -1;                // this sample's first unit
-      const uint4* src = reinterpret_cast<const uint4*>(p.pb) + static_cast<int64_t>(smp) * per;
+      const int at = t < half && smp < p.n ? p.term.place[smp] * per : -1;                // this sample's first unit
+      const uint4* src = p.term.pb + static_cast<int64_t>(smp) * per;
       for (int k = 0; k < more; ++k, ++g) {
         const uint32_t s = g % kPairStages;
         const int g0 = k * kUnits, nu = min(kUnits, units - g0);
         uint8_t* st = smem + s * kPairStage;
         uint4 words[kUnits];
-#pragma unroll
-        for (int j = 0; j < kUnits; ++j) {
-          const int u = g0 + j - at;                 // (a sample without an adapter has none: its place is below zero)
-          words[j] = at >= 0 && j < nu && u >= 0 && u < per ? src[u] : make_uint4(0, 0, 0, 0);
-        }
+        read_units(src, at, g0, nu, per, words);
         if (!mbar_wait_warp(&free_[s], (fph >> s) & 1, abort_flag)) { ok = false; break; }
         fph ^= 1u << s;
-        if (t < half) {
-          const uint32_t to = smem_u32(st) + kTileBytesA + t * 128;
-#pragma unroll
-          for (int j = 0; j < kUnits; ++j)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((j ^ (t & 7)) << 4)), "r"(words[j].x), "r"(words[j].y),
-                         "r"(words[j].z), "r"(words[j].w) : "memory");
-        }
-        if (nu & 1)                                  // beside an odd last unit zeros
-          *reinterpret_cast<uint4*>(st + (t >> 6) * (kTileBytesA / 2) + nu * (kUnit * 128) + (t & 63) * 16) = make_uint4(0, 0, 0, 0);
+        write_units<128>(words, st, t, t < half, nu);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(mapa_u32(smem_u32(&built[s]), 0));
@@ -821,18 +1103,29 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
       for (int x = 0; x < count; ++x) {
         const __nv_bfloat16* f = p.F + static_cast<int64_t>(list[x]) * p.rank * p.ldf;
         bool hit = false;
-        // pieces of 8 columns of a row; of the last one what lies behind the row does not count
+        // pieces of 8 columns, row after row; of a row's last one what lies behind the row does not count
         const int64_t pieces = (p.width + 7) / 8, all = pieces * p.rank, to = all * (part + 1) / 16;
-        for (int64_t i = all * part / 16 + threadIdx.x; i < to; i += 256) {
-          const int64_t r = i / pieces, c = i - r * pieces;
-          const uint4 v = *reinterpret_cast<const uint4*>(f + r * p.ldf + c * 8);
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-          const int64_t left = p.width - c * 8;
+        int64_t i = all * part / 16 + threadIdx.x, r = i / pieces, c = i - r * pieces;
+        while (i < to) {
+          uint4 v[4];
+          int64_t left[4];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {              // bit 15 / 31: the exponent of the low / high half is all ones
-            const uint32_t b = ((w[u] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-            hit |= (b & 0x8000u) && 2 * u < left;
-            hit |= (b >> 31) && 2 * u + 1 < left;
+          for (int y = 0; y < 4; ++y) {
+            left[y] = i < to ? p.width - c * 8 : 0;
+            v[y] = i < to ? *reinterpret_cast<const uint4*>(f + r * p.ldf + c * 8) : make_uint4(0, 0, 0, 0);
+            i += 256;
+            c += 256;
+            while (c >= pieces) { c -= pieces; ++r; }
+          }
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const uint32_t w[4] = {v[y].x, v[y].y, v[y].z, v[y].w};
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {            // bit 15 / 31: the exponent of the low / high half is all ones
+              const uint32_t b = ((w[u] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+              hit |= (b & 0x8000u) && 2 * u < left[y];
+              hit |= (b >> 31) && 2 * u + 1 < left[y];
+            }
           }
         }
         hit = __syncthreads_or(hit);
@@ -844,16 +1137,47 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
   }
   const int per = (p.rank + kUnit - 1) / kUnit;
   const int64_t blocks = gridDim.x - p.look - p.tiles;
+  if (p.n <= kFewMost) {                             // entry by entry: few threads have all to do
+    for (int64_t x = static_cast<int64_t>(tile - p.tiles) * 256 + threadIdx.x; x < p.n * per * kUnit; x += blocks * 256) {
+      const int64_t i = x / (per * kUnit);
+      const int r = static_cast<int>(x - i * per * kUnit), id = p.ids[i];
+      const bool has = id >= 0 && id < p.adapters && r < p.rank;
+      const float v = has ? ranked(p.p, i * p.rank + r) : 0.f;
+      if (r < p.rank) p.out[i * p.rank + r] = v;
+      p.pb[x] = __float2bfloat16_rn(has ? p.scale[id] * v : 0.f);
+    }
+    return;
+  }
   for (int64_t x = static_cast<int64_t>(tile - p.tiles) * 256 + threadIdx.x; x < p.n * per; x += blocks * 256) {
     const int64_t i = x / per;
     const int r0 = static_cast<int>(x - i * per) * kUnit, id = p.ids[i];
     const bool has = id >= 0 && id < p.adapters;
     const float sc = has ? p.scale[id] : 0.f;
     float v[kUnit];
+    const int64_t from = i * p.rank + r0;
+    if (p.rank % kUnit == 0) {                       // (rows of p are whole pieces of 32 bytes then)
 #pragma unroll
-    for (int j = 0; j < kUnit; ++j) {
-      v[j] = has && r0 + j < p.rank ? ranked(p.p, i * p.rank + r0 + j) : 0.f;
-      if (r0 + j < p.rank) p.out[i * p.rank + r0 + j] = v[j];
+      for (int j = 0; j < kUnit; ++j) v[j] = 0.f;
+      if (has) {
+#pragma unroll 4
+        for (int c = 0; c < p.p.parts; ++c) {
+          const float4* in = reinterpret_cast<const float4*>(p.p.at + c * p.p.stride + from);
+          const float4 x = in[0], y = in[1];
+          v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j) v[j] = has && r0 + j < p.rank ? ranked(p.p, from + j) : 0.f;
+    }
+    if (p.rank % kUnit == 0 && (reinterpret_cast<uintptr_t>(p.out) & 15) == 0) {
+      float4* to = reinterpret_cast<float4*>(p.out + from);
+      to[0] = make_float4(v[0], v[1], v[2], v[3]);
+      to[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j)
+        if (r0 + j < p.rank) p.out[from + j] = v[j];
     }
     uint32_t w[kUnit / 2];
 #pragma unroll
@@ -861,7 +1185,7 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
       const __nv_bfloat162 b = __floats2bfloat162_rn(has ? sc * v[2 * j] : 0.f, has ? sc * v[2 * j + 1] : 0.f);
       w[j] = *reinterpret_cast<const uint32_t*>(&b);
     }
-    if (p.pb) reinterpret_cast<uint4*>(p.pb)[x] = make_uint4(w[0], w[1], w[2], w[3]);
+    reinterpret_cast<uint4*>(p.pb)[x] = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
@@ -1000,10 +1324,10 @@ __global__ void __launch_bounds__(256) adapter_words_kernel(const __grid_constan
 // dF[a] = sum_{i of a} (scale p_i) z_i^T for a tile of 128 columns of z: the columns are the accumulator's rows, the ranks of the three
 // words its columns (added at the end), the samples the contraction, 64 of them at a time, gathered in the order of adapter_index_kernel
 // (so no sample of another adapter is in the product).
-// Warps: 0..3 loaders (asynchronous copies of 16 bytes into both operands, which arrive at the stage's barrier by themselves: a loader that
-// waited for its copies and fenced them had one k-block under way, 2 us each), 4 MMA issuer and TMEM owner, 5..8 epilogue.
+// Warps: 0..7 loaders (asynchronous copies of 16 bytes into both operands, which arrive at the stage's barrier by themselves: a loader that
+// waited for its copies and fenced them had one k-block under way), 8 MMA issuer and TMEM owner, 9..12 epilogue.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kGradThreads = 288, kGradStages = 8, kGradRing = 196608;
+constexpr int kLoaders = 8, kGradThreads = 32 * (kLoaders + 5), kGradStages = 8, kGradRing = 196608;
 struct GradSide {
   const __nv_bfloat16* z;      // [n][ldz]
   int64_t ldz;
@@ -1063,42 +1387,44 @@ struct GradWalk {
 };
 
 __device__ __forceinline__ void grad_load(const GradParams& p, uint8_t* smem, uint64_t* full, uint64_t* empty, volatile uint32_t* abort_flag) {
-  const int rp = (p.rank + 15) & ~15, pieces = 3 * rp / 8, stage = kTileBytesA + grad_panels(p.rank) * 8192, stages = p.stages;
-  const int tid = threadIdx.x, c16 = tid & 15, r0 = tid >> 4;
+  const int rp = (p.rank + 15) & ~15, pieces = 3 * rp / 8, stage = kTileBytesA + grad_panels(p.rank) * 8192;
+  const int tid = threadIdx.x;
+  // of z: pieces of 16 bytes, c16 of the rows r0, r0 + 16, ..; of the words: pieces wc, wc + 4, .. of row wr
+  const int c16 = tid & 15, r0 = tid >> 4, wr = tid >> 2, wc = tid & 3;
+  const uint32_t base = smem_u32(smem);
+  const uint32_t to_z = (c16 >> 3) * (kTileBytesA / 2) + r0 * 128 + (((c16 & 7) ^ (r0 & 7)) << 4), to_w = kTileBytesA + wr * 128;
   uint32_t s = 0, ph = 0;
   int known = -1, known_k = -1;                      // the adapter and the k-block of the samples in row
-  int32_t row[8];
+  int32_t row[4];
   for (GradWalk it(p); it.valid(); it.next()) {
     const GradSide& sd = p.side[it.side];
     const int nk = (it.count + BK - 1) / BK;
     const int col = it.tile * BM + c16 * 8, left = sd.width - col;
     const uint32_t bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;
-    for (int k = 0; k < nk; ++k) {
+    const __nv_bfloat16* z = sd.z + (bytes ? col : 0);
+    const __nv_bfloat16* words = sd.words + (static_cast<int64_t>(it.begin) + wr) * 3 * rp + wc * 8;
+    for (int k = 0; k < nk; ++k, words += BK * 3 * rp) {
+      const int here = it.count - k * BK;            // samples from here on
       if (known != it.a || known_k != k) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) { const int at = k * BK + r0 + j * 8; row[j] = at < it.count ? p.order[it.begin + at] : -1; }
+        for (int j = 0; j < 4; ++j) row[j] = r0 + j * 16 < here ? p.order[it.begin + k * BK + r0 + j * 16] : -1;
         known = it.a;
         known_k = k;
       }
-      const int rows = min(BK, (it.count - k * BK + 15) & ~15);       // whole instructions of 16
+      const int rows = min(BK, (here + 15) & ~15);   // whole instructions of 16
       if (!mbar_wait(&empty[s], ph ^ 1, abort_flag)) return;
-      const uint32_t st = smem_u32(smem + s * stage);
+      const uint32_t st = base + s * stage;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int kr = r0 + j * 8;
-        if (kr >= rows) break;
-        const uint32_t b = row[j] >= 0 ? bytes : 0;
-        cp_async_16(st + (c16 >> 3) * (kTileBytesA / 2) + kr * 128 + (((c16 & 7) ^ (kr & 7)) << 4),
-                    b ? sd.z + static_cast<int64_t>(row[j]) * sd.ldz + col : sd.z, b);
-      }
-      for (int x = tid; x < rows * pieces; x += 128) {
-        const int kr = x / pieces, ch = x - kr * pieces, at = k * BK + kr;
-        const uint32_t b = at < it.count ? 16 : 0;
-        cp_async_16(st + kTileBytesA + (ch >> 3) * 8192 + kr * 128 + (((ch & 7) ^ (kr & 7)) << 4),
-                    sd.words + (b ? (static_cast<int64_t>(it.begin) + at) * 3 * rp + ch * 8 : 0), b);
+      for (int j = 0; j < 4; ++j)
+        if (j * 16 < rows) cp_async_16(st + to_z + j * 2048, row[j] >= 0 ? z + row[j] * sd.ldz : z, row[j] >= 0 ? bytes : 0);
+      if (wr < rows) {
+        const uint32_t b = wr < here ? 16 : 0;
+        const __nv_bfloat16* from = b ? words : sd.words;
+        for (int ch = wc; ch < pieces; ch += 4, from += b ? 32 : 0)
+          cp_async_16(st + to_w + (ch >> 3) * 8192 + (((ch & 7) ^ (wr & 7)) << 4), from, b);
       }
       cp_async_arrive(&full[s]);
-      if (++s == static_cast<uint32_t>(stages)) { s = 0; ph ^= 1; }
+      if (++s == static_cast<uint32_t>(p.stages)) { s = 0; ph ^= 1; }
     }
   }
   cp_async_wait_all();
@@ -1115,21 +1441,21 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
   const uint32_t buffers = N <= 256 ? 2 : 1;         // accumulators of 256 columns, or one of 512
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
-    for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 128); mbar_init(&empty[i], 1); }
+    for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 32 * kLoaders); mbar_init(&empty[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 4); }
     abort_word = 0;
     fence_barrier_init();
   }
-  if (warp == 4) { tmem_alloc(&tmem_slot, 512); tmem_relinquish(); }
+  if (warp == kLoaders) { tmem_alloc(&tmem_slot, 512); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = tmem_slot;
   pdl_wait();
 
-  if (warp < 4) {
+  if (warp < kLoaders) {
     grad_load(p, smem, full, empty, abort_flag);
-  } else if (warp == 4) {
+  } else if (warp == kLoaders) {
     // more than 256 columns: 192 (three panels), then the rest
     const uint32_t n1 = N <= 256 ? N : 192, n2 = N - n1;
     const uint32_t idesc1 = umma_idesc_bf16(BM, n1) | kIdescMnMajor, idesc2 = umma_idesc_bf16(BM, n2 ? n2 : 16) | kIdescMnMajor;
@@ -1206,7 +1532,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
     for (int i = 0; i < 64; ++i) __nanosleep(1000);
     __syncthreads();
   }
-  if (warp == 4) { tc_fence_after(); tmem_dealloc(tmem_base, 512); }
+  if (warp == kLoaders) { tc_fence_after(); tmem_dealloc(tmem_base, 512); }
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -1263,7 +1589,7 @@ AdapterLayout layout_of(const sfb_adapter_config& c) {
   L.twords = take(n * 3 * rp * 2);
   L.lists = take((n / kMaxTile + 1) * kListPitch * 4);
   L.place = take(n * 4);
-  L.partial = take(n > kFewMost ? static_cast<size_t>(kModelSms) * kPartFloats * 4 : 0);
+  L.partial = take(static_cast<size_t>(kModelSms) * (n > kFewMost ? kPartFloats : kFewMost * BM) * 4);
   L.order = take(n * 4);
   L.begin = take(static_cast<size_t>(c.adapters) * 4);
   L.work = take((static_cast<size_t>(c.adapters) + 1) * 8);
@@ -1285,7 +1611,7 @@ struct sfb_adapters {
   char* ws;
   cudaStream_t stream;
   int device, last_cuda, max_pairs;
-  uint32_t calls;                      // products on pairs so far: what such a call marks its adapters with (a replayed one with the same
+  uint32_t calls;                      // products with factors so far: what such a call marks its adapters with (a replayed one with the same
                                        // number each time, so that it may look at adapters of earlier replays too)
   CUtensorMap mapU, mapV;              // boxes of 64 entries x 16 ranks of an adapter
   CUtensorMap unitU, unitV;            // x 8 ranks
@@ -1336,14 +1662,12 @@ cudaError_t rank_products(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz
   CUtensorMap mz;
   if (!operand_map(h, &mz, Z, d, n, ldz, BK, tn, CU_TENSOR_MAP_L2_PROMOTION_L2_256B)) return cudaErrorInvalidValue;
   RankParams p{};
-  p.n = static_cast<int32_t>(n); p.tn = tn; p.kseg = static_cast<int32_t>((d + BK - 1) / BK); p.stages = std::min(kMaxStages, kSmallRing / stage_bytes(tn));
+  p.n = static_cast<int32_t>(n); p.tn = tn; p.kseg = static_cast<int32_t>((d + BK - 1) / BK); p.stages = std::min(kMaxStages, (n <= kFewMost ? kFewRing : kSmallRing) / stage_bytes(tn));
   p.rank = h->cfg.rank; p.adapters = h->cfg.adapters; p.ids = ids; p.out = out; p.status = h->at<uint32_t>(h->lay.status);
-  if (n > kFewMost) {
-    p.mark = h->at<int32_t>(h->lay.mark);
-    p.call = static_cast<int32_t>(++h->calls);
-  }
+  p.mark = h->at<int32_t>(h->lay.mark);
+  p.call = static_cast<int32_t>(++h->calls);
   const int per = (h->cfg.rank + kSlice - 1) / kSlice, chunks = (std::min(tn, h->cfg.adapters) * per + 7) / 8;
-  const int groups = std::max(1, std::min(chunks, 2 * kModelSms / (parts * tiles)));
+  const int groups = std::max(1, std::min(chunks, (n <= kFewMost ? 1 : 2) * kModelSms / (parts * tiles)));
   const int smem = p.stages * stage_bytes(tn) + 1024;
   cudaError_t e = allow_smem<adapter_rank_kernel>(kSmallRing + 1024);
   if (e != cudaSuccess) return e;
@@ -1351,6 +1675,7 @@ cudaError_t rank_products(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz
   return launch_kernel(adapter_rank_kernel, dim3(parts, tiles, groups), dim3(kRankThreads), smem, h->stream, 1, mapF, mz, p);
 }
 
+constexpr int64_t kClusterTiles = 2 * kModelSms / kMaxCluster;      // tiles up to which eight CTAs share each
 // CTAs of a cluster of adapter_few_kernel: as many as leave all of them a place, two an SM, and each four k-blocks.
 int few_parts(int64_t tiles, int64_t kseg) {
   int best = 1;
@@ -1359,28 +1684,48 @@ int few_parts(int64_t tiles, int64_t kseg) {
   return best;
 }
 
+// What adapter_sum_kernel leaves for the products.
+template <bool MN>
+Term term_of(const sfb_adapters* h, const int32_t* ids, const float* p) {
+  const sfb_adapter_config& c = h->cfg;
+  return Term{c.rank, c.adapters, ids, h->at<int32_t>(h->lay.lists), h->at<int32_t>(h->lay.place), h->scale, h->at<uint4>(h->lay.bad),
+              static_cast<const __nv_bfloat16*>(MN ? h->V : h->U), MN ? c.ldv : c.ldu, p, h->at<uint4>(h->lay.pb)};
+}
+
 template <int TN, bool MN>
-cudaError_t few(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const int32_t* ids, const float* s, void* Y, int64_t ldy) {
+cudaError_t few(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const Term& term, void* Y, int64_t ldy) {
   const sfb_adapter_config& c = h->cfg;
   const int64_t m = MN ? c.cols : c.rows, d = MN ? c.rows : c.cols;
   CUtensorMap ma, mz;
   if (!operand_map(h, &ma, h->W, c.cols, c.rows, c.ldw, BK, MN ? BK : BM, CU_TENSOR_MAP_L2_PROMOTION_L2_256B) ||
       !operand_map(h, &mz, Z, d, n, ldz, BK, TN, CU_TENSOR_MAP_L2_PROMOTION_L2_256B))
     return cudaErrorInvalidValue;
+  const CUtensorMap& mf = MN ? h->unitV : h->unitU;
   FewParams p{};
+  p.term = term;
   p.n = static_cast<int32_t>(n); p.m = static_cast<int32_t>(m);
   p.kseg = static_cast<int32_t>((d + BK - 1) / BK);
+  p.Y = static_cast<__nv_bfloat16*>(Y); p.ldy = ldy; p.status = h->at<uint32_t>(h->lay.status);
   const int64_t tiles = (m + BM - 1) / BM;
-  p.parts = few_parts(tiles, p.kseg);
-  p.rank = c.rank; p.adapters = c.adapters; p.ids = ids; p.scale = h->scale;
-  p.F = static_cast<const __nv_bfloat16*>(MN ? h->V : h->U); p.ldf = MN ? c.ldv : c.ldu;
-  p.p = s; p.Y = static_cast<__nv_bfloat16*>(Y); p.ldy = ldy; p.status = h->at<uint32_t>(h->lay.status);
-  const int terms = static_cast<int>(n) * c.rank * 4;
-  p.stages = std::min(kMaxStages, (kSmallRing + 8192 - std::min(terms, 24576)) / stage_bytes(TN));
-  const int smem = p.stages * stage_bytes(TN) + terms + 1024;
-  cudaError_t e = allow_smem<adapter_few_kernel<TN, MN>>(kMaxStages * stage_bytes(TN) + TN * SFB_ADAPTER_MAX_RANK * 4 + 1024);
+  if (tiles <= kClusterTiles) {
+    p.parts = few_parts(tiles, p.kseg);
+    p.stages = std::min(kMaxStages, kSmallRing / stage_bytes(TN));
+    const cudaError_t e = allow_smem<adapter_few_kernel<TN, MN>>(kSmallRing + 1024);
+    if (e != cudaSuccess) return e;
+    return launch_kernel(adapter_few_kernel<TN, MN>, dim3(static_cast<unsigned>(tiles * p.parts)), dim3(kFewThreads), p.stages * stage_bytes(TN) + 1024,
+                         h->stream, p.parts, ma, mz, mf, p);
+  }
+  // every CTA has k-blocks of the tiles that are shared out: at least a tile's worth, or four where there are fewer tiles than SMs
+  const int64_t sms = std::min(sm_count(), kModelSms), ctas = tiles >= sms ? sms : std::max<int64_t>(1, std::min(sms, tiles * p.kseg / 4));
+  p.tiles = static_cast<int32_t>(tiles);
+  p.cut = tiles % ctas != 0;
+  p.whole = p.cut ? static_cast<int32_t>(std::max<int64_t>(0, tiles / ctas - 1) * ctas) : 0;
+  p.stages = std::min(kMaxStages, kStreamRing / stage_bytes(TN));
+  p.partial = h->at<float>(h->lay.partial); p.ready = h->at<uint32_t>(h->lay.ready);
+  const cudaError_t e = allow_smem<adapter_stream_kernel<TN, MN>>(kStreamRing + 1024);
   if (e != cudaSuccess) return e;
-  return launch_kernel(adapter_few_kernel<TN, MN>, dim3(static_cast<unsigned>(tiles * p.parts)), dim3(kFewThreads), smem, h->stream, p.parts, ma, mz, p);
+  return launch_kernel(adapter_stream_kernel<TN, MN>, dim3(static_cast<unsigned>(ctas)), dim3(kStreamThreads), p.stages * stage_bytes(TN) + 1024, h->stream, 1,
+                       ma, mz, mf, p);
 }
 
 // Cycles of a plan of adapter_pair_kernel: its k-blocks on a pair, 7,000 to start and to end, 9,000 and 2,000 a part to leave and to take
@@ -1401,7 +1746,7 @@ PairPlan plan_pairs(int64_t tiles, int64_t kseg, int tn, int64_t most) {
 }
 
 template <bool MN>
-cudaError_t pairs(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const int32_t* ids, const float* s, void* Y, int64_t ldy) {
+cudaError_t pairs(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const Term& term, void* Y, int64_t ldy) {
   const sfb_adapter_config& c = h->cfg;
   const int64_t m = MN ? c.cols : c.rows, d = MN ? c.rows : c.cols;
   const int tn = tile_of(n);
@@ -1415,9 +1760,7 @@ cudaError_t pairs(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const 
   p.kseg = static_cast<int32_t>((d + BK - 1) / BK);
   const PairPlan plan = plan_pairs(static_cast<int64_t>(p.tilesT) * p.tilesM, p.kseg, tn, h->max_pairs);
   p.cut = plan.cut; p.whole = plan.whole;
-  p.rank = c.rank; p.adapters = c.adapters; p.ids = ids; p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place);
-  p.scale = h->scale; p.bad = h->at<uint4>(h->lay.bad); p.F = static_cast<const __nv_bfloat16*>(MN ? h->V : h->U); p.ldf = MN ? c.ldv : c.ldu;
-  p.p = s; p.pb = h->at<__nv_bfloat16>(h->lay.pb); p.Y = static_cast<__nv_bfloat16*>(Y); p.ldy = ldy;
+  p.term = term; p.Y = static_cast<__nv_bfloat16*>(Y); p.ldy = ldy;
   p.partial = h->at<float>(h->lay.partial); p.ready = h->at<uint32_t>(h->lay.ready); p.status = h->at<uint32_t>(h->lay.status);
   return launch_kernel_if(static_cast<int64_t>(p.tilesT) * p.tilesM <= plan.pairs, adapter_pair_kernel<MN>, dim3(2u * static_cast<unsigned>(plan.pairs)),
                           dim3(kPairThreads), kPairSmem, h->stream, 1, ma, mz, MN ? h->unitV : h->unitU, p);
@@ -1430,21 +1773,20 @@ cudaError_t product(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, cons
   const sfb_adapter_config& c = h->cfg;
   SumParams p{};
   p.p = *s; p.ids = ids; p.scale = h->scale; p.n = n; p.rank = c.rank; p.adapters = c.adapters; p.out = to; p.status = h->at<uint32_t>(h->lay.status);
-  if (n > kFewMost) {
-    p.pb = h->at<__nv_bfloat16>(h->lay.pb);
-    p.F = static_cast<const __nv_bfloat16*>(MN ? h->V : h->U); p.ldf = MN ? c.ldv : c.ldu; p.width = MN ? c.cols : c.rows;
-    p.mark = h->at<int32_t>(h->lay.mark); p.call = static_cast<int32_t>(h->calls); p.look = std::min(c.adapters, kLookMost) * 16;
-    p.bad = h->at<uint8_t>(h->lay.bad);
-    p.tn = tile_of(n); p.tiles = static_cast<int32_t>((n + p.tn - 1) / p.tn); p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place);
-  }
-  const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(p.look + p.tiles + grid1d(n * ((c.rank + kUnit - 1) / kUnit), 256)), dim3(256), 0, h->stream,
+  p.pb = h->at<__nv_bfloat16>(h->lay.pb);
+  p.F = static_cast<const __nv_bfloat16*>(MN ? h->V : h->U); p.ldf = MN ? c.ldv : c.ldu; p.width = MN ? c.cols : c.rows;
+  p.mark = h->at<int32_t>(h->lay.mark); p.call = static_cast<int32_t>(h->calls); p.look = std::min(c.adapters, kLookMost) * 16;
+  p.bad = h->at<uint8_t>(h->lay.bad);
+  p.tn = tile_of(n); p.tiles = static_cast<int32_t>((n + p.tn - 1) / p.tn); p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place);
+  const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(p.look + p.tiles + grid1d(n * ((c.rank + kUnit - 1) / kUnit) * (n <= kFewMost ? kUnit : 1), 256)), dim3(256), 0, h->stream,
                                       1, p);
   if (e != cudaSuccess) return e;
   *s = Ranked{to, 1, 0};
-  if (n <= 16) return few<16, MN>(h, n, Z, ldz, ids, to, Y, ldy);
-  if (n <= 32) return few<32, MN>(h, n, Z, ldz, ids, to, Y, ldy);
-  if (n <= kFewMost) return few<kFewMost, MN>(h, n, Z, ldz, ids, to, Y, ldy);
-  return pairs<MN>(h, n, Z, ldz, ids, to, Y, ldy);
+  const Term term = term_of<MN>(h, ids, to);
+  if (n <= 16) return few<16, MN>(h, n, Z, ldz, term, Y, ldy);
+  if (n <= 32) return few<32, MN>(h, n, Z, ldz, term, Y, ldy);
+  if (n <= kFewMost) return few<kFewMost, MN>(h, n, Z, ldz, term, Y, ldy);
+  return pairs<MN>(h, n, Z, ldz, term, Y, ldy);
 }
 
 int fail(sfb_adapters* h, cudaError_t e) {

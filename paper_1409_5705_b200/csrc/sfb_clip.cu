@@ -1,6 +1,6 @@
 // Global norm of a list of gradient tensors, and their copies rescaled where it is above a limit (sfb_clip_* in sfb.h).
 //
-// The table, made once: pieces of at most 32 KB of a tensor, each with its addresses, entries and type, so that tensors of any
+// The table, made once: pieces of at most 16 KB of a tensor, each with its addresses, entries and type, so that tensors of any
 // number and length are one even list.  Two launches:
 //   clip_sum_kernel    blocks take pieces in turn; a thread's squares go into fp64 sums, a block's sum to its place
 //   clip_scale_kernel  every block adds the blocks' sums in the same order, and takes its pieces from the list's end backwards: what
@@ -24,8 +24,8 @@ using sfb::pdl_launch_dependents;
 using sfb::pdl_wait;
 
 constexpr int kThreads = 256;
-constexpr int64_t kPieceBytes = 32768;
-constexpr int kBlocksPerSm = 4;
+constexpr int64_t kPieceBytes = 16384;               // four 16-byte loads a thread
+constexpr int kBlocksPerSm = 5;
 
 struct Piece {
   const char* src;
@@ -132,12 +132,14 @@ __device__ __forceinline__ double block_sum(double v) {
   return s;
 }
 
-__global__ void __launch_bounds__(kThreads) clip_sum_kernel(const Piece* pieces, int64_t n, double* part) {
+__global__ void __launch_bounds__(kThreads, 5) clip_sum_kernel(const Piece* pieces, int64_t n, double* part) {
   pdl_launch_dependents();
   pdl_wait();
   double sum = 0.0;
+  Piece next = blockIdx.x < n ? pieces[blockIdx.x] : Piece{};
   for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
-    const Piece c = pieces[i];
+    const Piece c = next;
+    if (i + gridDim.x < n) next = pieces[i + gridDim.x];
     if (c.dtype == SFB_F32) sum_piece(reinterpret_cast<const float*>(c.src), c.count, sum);
     else if (c.dtype == SFB_BF16) sum_piece(reinterpret_cast<const __nv_bfloat16*>(c.src), c.count, sum);
     else sum_piece(reinterpret_cast<const __half*>(c.src), c.count, sum);
@@ -171,8 +173,10 @@ __global__ void __launch_bounds__(kThreads) clip_scale_kernel(const Piece* piece
     result[0] = static_cast<float>(norm);
     result[1] = finite ? coef : 0.f;
   }
+  Piece next = n > blockIdx.x ? pieces[n - 1 - blockIdx.x] : Piece{};
   for (int64_t i = n - 1 - blockIdx.x; i >= 0; i -= gridDim.x) {
-    const Piece c = pieces[i];
+    const Piece c = next;
+    if (i >= gridDim.x) next = pieces[i - gridDim.x];
     if (coef == 1.f && c.src == c.dst) continue;
     if (c.dtype == SFB_F32) scale_piece(reinterpret_cast<const float*>(c.src), reinterpret_cast<float*>(c.dst), c.count, coef);
     else if (c.dtype == SFB_BF16)

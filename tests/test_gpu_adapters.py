@@ -147,6 +147,13 @@ SIZES = [
     (2500, 700, 600, 4, 48, "runs"),
     (300, 200, 200, 5, 16, "none"),
     (513, 100, 3001, 300, 16, "every"),
+    # up to 64 samples with more rows than 37 tiles of 128: fewer tiles than SMs, more, whole rounds, a k-block each
+    (1, 5001, 300, 2, 16, "one"),
+    (16, 4900, 70, 5, 5, "mixed"),
+    (33, 6000, 999, 8, 24, "mixed"),
+    (64, 20001, 130, 9, 128, "mixed"),
+    (29, 18944, 264, 29, 8, "every"),
+    (40, 300, 9001, 4, 20, "mixed"),
 ]
 
 
