@@ -1,8 +1,8 @@
 // Low-rank adapters of many requests beside the shared W (sfb_adapter_* in sfb.h): the logits of samples, each with the adapter
 // (a set of factor pairs) that its request names, and the gradients of the samples and of the adapters' factors.
 //
-// Launches of a forward pass:  adapter_rank_kernel (s = V x, in parts), adapter_sum_kernel, and for y = W x + scale U^T s up to 64 samples
-// adapter_few_kernel or adapter_stream_kernel, for more adapter_pair_kernel;  of a backward pass:  adapter_index_kernel, adapter_rank_kernel (t = U dy; s again
+// Launches of a forward pass:  adapter_rank_kernel (s = V x), then for y = W x + scale U^T s up to 64 samples adapter_few_kernel or
+// adapter_stream_kernel, for more adapter_sum_kernel and adapter_pair_kernel;  of a backward pass:  adapter_index_kernel, adapter_rank_kernel (t = U dy; s again
 // where it is not given), the products as in a forward pass (dx), adapter_words_kernel and adapter_gradient_kernel (dU, dV).
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -93,36 +93,65 @@ __device__ __forceinline__ void build_list(TileList<MOST>& L, const int32_t* ids
   __syncthreads();
 }
 
+// The products p_i as adapter_rank_kernel leaves them, or as the caller has them (one part).
+struct Ranked {
+  const float* at;
+  int32_t parts;
+  int64_t stride;              // entries from a part to the next
+};
+__device__ __forceinline__ float ranked(const Ranked& s, int64_t at) {
+  float v = 0.f;
+  for (int c = 0; c < s.parts; c += 8) {             // eight on their way
+    float x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] = c + u < s.parts ? __ldcg(s.at + (c + u) * s.stride + at) : 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v += x[u];
+  }
+  return v;
+}
+
+constexpr int kUnit = 8, kUnits = BK / kUnit;       // ranks of a unit of the adapters' term (see Term), units of a k-block
+
 // ---------------------------------------------------------------------------------------------------------
 // p_i = F[a_i] z_i:  the adapters' factors as the rows of the accumulator, 16 ranks (a slice) of one adapter after another, up to 128
 // samples as its columns; each sample takes the rows of its own adapter, so what another adapter or sample holds does not reach it.
-// Grid: parts of the contraction x tiles of samples x groups of the tile's slices, eight slices at a time.  Bound by the way of z and F
-// to the SMs, and by latency at either end of a block: two blocks an SM.
+// Eight slices (a chunk) at a time; the contraction in parts.  Bound by the way of z and F to the SMs, and by latency at either end of a
+// block.  Grid: parts x tiles of samples x groups of chunks, two blocks an SM.
+// FEW, up to 64 samples: one tile, a block an SM, chunks and parts shared out once the chunks are known; the block that finishes the last
+// part of a chunk adds them (in their order) and writes p and pb, the first one the list, so that the product is the next launch.
 // Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..9 epilogue (TMEM lane quarter q; 32 of every 64 samples), whose sums stay in
 // registers from drain to drain.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kRankThreads = 320, kRankTile = 128;
+constexpr int kRankThreads = 320, kRankTile = 128, kFewChunks = 64;
 struct RankParams {
   int32_t n, tn, kseg, stages;
   int32_t rank, adapters;
   const int32_t* ids;
   float* out;                  // [parts][n][rank]
-  int32_t* mark;               // for each adapter in use, `call`
+  int32_t* mark;               // for each adapter in use, `call` (not FEW)
   int32_t call;
   uint32_t* status;
+  // FEW
+  const float* scale;
+  float* p;                    // [n][rank]
+  __nv_bfloat16* pb;           // [n][rank rounded up to 8]
+  int32_t *lists, *place;
+  uint32_t* arrived;           // [kFewChunks]
 };
 
+template <bool FEW>
 __global__ void __launch_bounds__(kRankThreads, 2)
 adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ RankParams p) {
+  constexpr int kHeld = FEW ? 1 : 2;                 // times 32 samples of an epilogue warp
   extern __shared__ uint8_t smem_raw[];
   __shared__ alignas(16) TileList<kRankTile> L;
   __shared__ uint64_t full[kMaxStages], empty[kMaxStages], tfull[2], tempty[2];
-  __shared__ uint32_t tmem_slot, abort_word;
+  __shared__ uint32_t tmem_slot, abort_word, last;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   volatile uint32_t* abort_flag = &abort_word;
   const int warp = warp_index(), lane = threadIdx.x & 31;
-  const int part = blockIdx.x, parts = gridDim.x, first = blockIdx.y * p.tn;
-  const int kbeg = static_cast<int>(static_cast<int64_t>(part) * p.kseg / parts), kend = static_cast<int>(static_cast<int64_t>(part + 1) * p.kseg / parts);
+  const int first = FEW ? 0 : blockIdx.y * p.tn;
   const int cols = max(p.tn, 32), stage = stage_bytes(p.tn);
   if (threadIdx.x == 0) {
     for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
@@ -140,13 +169,38 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
   tc_fence_after();
   const uint32_t tmem_base = tmem_slot;
   const int per = (p.rank + kSlice - 1) / kSlice, slices = L.count * per, chunks = (slices + 7) / 8;
-  if (part == 0 && blockIdx.z == 0)
+  // this block's chunks [c0, c0 + step, ..) and its part of their contraction
+  int c0 = blockIdx.z, step = gridDim.z, part = blockIdx.x, parts = gridDim.x;
+  if (FEW) {
+    parts = chunks ? max(1, min(min(kMaxParts, static_cast<int>(gridDim.x) / chunks), p.kseg / 4)) : 1;
+    step = parts > 1 ? chunks : gridDim.x;
+    c0 = parts > 1 ? blockIdx.x % chunks : blockIdx.x;
+    part = parts > 1 ? blockIdx.x / chunks : 0;
+    if (part >= parts) c0 = chunks;                  // nothing
+  }
+  const int kbeg = static_cast<int>(static_cast<int64_t>(part) * p.kseg / parts), kend = static_cast<int>(static_cast<int64_t>(part + 1) * p.kseg / parts);
+  if (FEW) {
+    if (blockIdx.x == 0) {
+      if (threadIdx.x == 0) p.lists[0] = L.count;
+      const int per8 = (p.rank + kUnit - 1) / kUnit * kUnit;
+      for (int t = threadIdx.x; t < p.tn; t += kRankThreads) {
+        if (t < L.count) p.lists[1 + t] = L.list[t];
+        if (t < p.n) p.place[t] = L.place[t];
+      }
+      for (int x = threadIdx.x; x < p.n * per8; x += kRankThreads) {       // samples without an adapter, and what lies behind the ranks
+        const int t = x / per8, r = x - t * per8;
+        if (r >= p.rank || L.place[t] < 0) p.pb[x] = __float2bfloat16_rn(0.f);
+        if (r < p.rank && L.place[t] < 0) p.p[t * p.rank + r] = 0.f;
+      }
+    }
+  } else if (blockIdx.x == 0 && blockIdx.z == 0) {
     for (int t = threadIdx.x; t < L.count; t += kRankThreads) p.mark[L.list[t]] = p.call;
+  }
 
   if (warp == 0) {
     uint32_t s = 0, ph = 0;
     bool ok = true;
-    for (int c = blockIdx.z; c < chunks && ok; c += gridDim.z) {
+    for (int c = c0; c < chunks && ok; c += step) {
       const int ns = min(8, slices - c * 8);
       for (int k = kbeg; k < kend; ++k) {
         if (!mbar_wait_warp(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
@@ -166,7 +220,7 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
     const uint32_t idesc = umma_idesc_bf16(BM, p.tn);
     uint32_t s = 0, ph = 0, i = 0;
     bool ok = true;
-    for (int c = blockIdx.z; c < chunks && ok; c += gridDim.z) {
+    for (int c = c0; c < chunks && ok; c += step) {
       for (int k0 = kbeg; k0 < kend && ok; k0 += kDrain, ++i) {
         const uint32_t a = i & 1, aph = (i >> 1) & 1, d_tmem = tmem_base + a * cols;
         if (!mbar_wait_warp(&tempty[a], aph ^ 1, abort_flag)) { ok = false; break; }
@@ -190,12 +244,13 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
     float* out = p.out + static_cast<int64_t>(part) * p.n * p.rank;
     uint32_t i = 0;
     bool ok = true;
-    for (int c = blockIdx.z; c < chunks && ok; c += gridDim.z) {
+    for (int c = c0; c < chunks && ok; c += step) {
       const int g = c * 8 + q * 2 + (lane >> 4), at = g < slices ? g / per : -2, r = (g - at * per) * kSlice + (lane & 15);
-      uint32_t own[2];                               // of 32 samples: those of this lane's adapter (places behind a tile of 16 are -1)
-      float sum[2][32];
+      uint32_t own[kHeld];                           // of 32 samples: those of this lane's adapter (places behind a tile of 16 are -1)
+      bool any[kHeld];
+      float sum[kHeld][32];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
+      for (int x = 0; x < kHeld; ++x) {
         const int t0 = h * 32 + x * 64;
         own[x] = 0;
         if (t0 < p.tn && r < p.rank) {
@@ -205,22 +260,25 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
             own[x] |= ((v.x == at ? 1u : 0u) | (v.y == at ? 2u : 0u) | (v.z == at ? 4u : 0u) | (v.w == at ? 8u : 0u)) << j;
           }
         }
+        any[x] = __any_sync(0xffffffffu, own[x]) != 0;
 #pragma unroll
         for (int j = 0; j < 32; ++j) sum[x][j] = 0.f;
       }
-      const bool any[2] = {__any_sync(0xffffffffu, own[0]) != 0, __any_sync(0xffffffffu, own[1]) != 0};
       for (int k0 = kbeg; k0 < kend; k0 += kDrain, ++i) {
         const uint32_t a = i & 1, aph = (i >> 1) & 1;
         if (!mbar_wait_warp(&tfull[a], aph, abort_flag)) { ok = false; break; }
         tc_fence_after();
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < kHeld; ++x) {
           if (!any[x]) continue;
-          uint32_t acc[32];
-          tmem_ld_32x32(tmem_base + (static_cast<uint32_t>(q * 32) << 16) + a * cols + h * 32 + x * 64, acc);
-          tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 32; ++j) sum[x][j] += __uint_as_float(acc[j]);
+          for (int j0 = 0; j0 < 32; j0 += 16) {
+            uint32_t acc[16];
+            tmem_ld_32x16(tmem_base + (static_cast<uint32_t>(q * 32) << 16) + a * cols + h * 32 + x * 64 + j0, acc);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sum[x][j0 + j] += __uint_as_float(acc[j]);
+          }
         }
         tc_fence_before();
         __syncwarp();
@@ -228,7 +286,7 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
       }
       if (!ok) break;
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
+      for (int x = 0; x < kHeld; ++x) {
         float* to = out + static_cast<int64_t>(first + h * 32 + x * 64) * p.rank + r;
 #pragma unroll
         for (int j = 0; j < 32; ++j)
@@ -239,30 +297,34 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
   __syncwarp();
   tc_fence_before();
   __syncthreads();
+  if (FEW && !abort_word) {
+    for (int c = c0; c < chunks; c += step) {
+      if (threadIdx.x == 0) {
+        __threadfence();
+        last = atomicAdd(&p.arrived[c], 1u) == static_cast<uint32_t>(parts) - 1;
+        if (last) p.arrived[c] = 0;                  // for the next launch
+        __threadfence();
+      }
+      __syncthreads();
+      if (last) {
+        const int per8 = (p.rank + kUnit - 1) / kUnit * kUnit;
+        for (int x = threadIdx.x; x < p.n * p.rank; x += kRankThreads) {
+          const int t = x / p.rank, r = x - t * p.rank, at = L.place[t];
+          if (at < 0 || (at * per + r / kSlice) / 8 != c) continue;
+          const float v = ranked(Ranked{p.out, parts, static_cast<int64_t>(p.n) * p.rank}, x);
+          p.p[x] = v;
+          p.pb[t * per8 + r] = __float2bfloat16_rn(p.scale[L.list[at]] * v);
+        }
+      }
+      __syncthreads();
+    }
+  }
   if (abort_word) {
     if (threadIdx.x == 0) atomicOr(p.status, SFB_STATUS_TIMEOUT);
     for (int i = 0; i < 64; ++i) __nanosleep(1000);
     __syncthreads();
   }
   if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem_base, 2 * cols); }
-}
-
-// The products p_i as adapter_rank_kernel leaves them, or as the caller has them (one part).
-struct Ranked {
-  const float* at;
-  int32_t parts;
-  int64_t stride;              // entries from a part to the next
-};
-__device__ __forceinline__ float ranked(const Ranked& s, int64_t at) {
-  float v = 0.f;
-  for (int c = 0; c < s.parts; c += 8) {             // eight on their way
-    float x[8];
-#pragma unroll
-    for (int u = 0; u < 8; ++u) x[u] = c + u < s.parts ? s.at[(c + u) * s.stride + at] : 0.f;
-#pragma unroll
-    for (int u = 0; u < 8; ++u) v += x[u];
-  }
-  return v;
 }
 
 constexpr int kEpi = 8;                             // epilogue warps of the products
@@ -282,18 +344,19 @@ __device__ __forceinline__ void store_two(__nv_bfloat16* Y, int64_t ldy, int i, 
 // ---------------------------------------------------------------------------------------------------------
 // The adapters' term, scale F[a_i]^T p_i, of the three products below is more contraction behind the k-blocks of A: the factors of the
 // adapters in the tile's list, eight units of 8 ranks a k-block, against  scale p  of the samples in bf16 (one rounding, 2^-8 of the term;
-// the result is rounded by as much), with zeros where a sample has another adapter.  Zeros do not hide what is not finite:
-// adapter_sum_kernel has looked through the factors, and one that holds such entries is not loaded (its units are out of the map's
-// bounds, zeros); the end of the tile forms the term of its own samples in fp32.
+// the result is rounded by as much), with zeros where a sample has another adapter.  Zeros do not hide what is not finite.  Up to 64
+// samples, where a factor is read once, the warps that write the samples' operand look through the factors in shared memory, replace what
+// is not finite by zeros, and the end of the tile adds those entries alone to their own samples, in fp32.  For more samples
+// adapter_sum_kernel has looked through the factors, and an adapter that holds such entries is not loaded (its units are out of the map's
+// bounds, zeros): the end of the tile forms the whole term of its samples in fp32.
 // (In fp32 FMAs from global memory, as it was for up to 64 samples, a tile's term is a chain of loads: 64 samples of 8 ranks took 99 us a
 // tile of 325,000 x 10,000, whose rows of W stream by in 57.)
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kUnit = 8, kUnits = BK / kUnit;
 struct Term {
   int32_t rank, adapters;
   const int32_t *ids, *lists, *place;
   const float* scale;
-  const uint4* bad;            // [adapters]: not zero where the factors are not finite
+  const uint4* bad;            // [adapters]: not zero where the factors are not finite (null up to 64 samples)
   const __nv_bfloat16* F;      // [adapters][rank][ldf]
   int64_t ldf;
   const float* p;              // [n][rank]
@@ -301,15 +364,18 @@ struct Term {
 };
 __device__ __forceinline__ int units_of(const Term& t) { return (t.rank + kUnit - 1) / kUnit; }
 __device__ __forceinline__ bool is_bad(const uint4& b) { return (b.x | b.y | b.z | b.w) != 0; }
-// The term of sample i at row m, where its adapter's factors are not finite; else 0.
+// What the tensor cores have left out of the term of sample i at row m.
 __device__ __noinline__ float bad_term(const Term& p, int i, int m) {
   const int id = p.ids[i];
-  if (id < 0 || id >= p.adapters || !is_bad(p.bad[id])) return 0.f;
+  if (id < 0 || id >= p.adapters || (p.bad && !is_bad(p.bad[id]))) return 0.f;
   const __nv_bfloat16* f = p.F + static_cast<int64_t>(id) * p.rank * p.ldf + m;
   const float* s = p.p + static_cast<int64_t>(i) * p.rank;
   const float sc = p.scale[id];
   float v = 0.f;
-  for (int r = 0; r < p.rank; ++r) v = fmaf(__bfloat162float(f[r * p.ldf]), sc * s[r], v);
+  for (int r = 0; r < p.rank; ++r) {
+    const float x = __bfloat162float(f[r * p.ldf]);
+    if (p.bad || !isfinite(x)) v = fmaf(x, sc * s[r], v);
+  }
   return v;
 }
 // Whether some adapter in a list is bad; by a warp.
@@ -318,11 +384,31 @@ __device__ __forceinline__ bool any_bad(const Term& p, const int32_t* list, int 
   for (int x = lane; x < list[0]; x += 32) any |= is_bad(p.bad[list[1 + x]]);
   return __any_sync(0xffffffffu, any);
 }
-// The adapter of unit g of `units`, out of the map's bounds where it is bad.
-__device__ __forceinline__ int unit_adapter(const Term& p, const int32_t* list, int g, int units, int per) {
-  if (g >= units) return 0;
-  const int a = list[1 + g / per];
-  return is_bad(p.bad[a]) ? p.adapters : a;
+// The adapter of unit g of `units`.
+__device__ __forceinline__ int unit_adapter(const int32_t* list, int g, int units, int per) {
+  return g < units ? list[1 + g / per] : 0;
+}
+// Replaces what is not finite of the factors of `nu` units in a stage by zeros; whether there was anything.  By THREADS threads, t of them.
+template <int THREADS>
+__device__ __forceinline__ uint32_t clean_units(uint8_t* st, int t, int nu) {
+  uint32_t bad = 0;
+#pragma unroll
+  for (int x = 0; x < 2 * kUnits * 64 / THREADS; ++x) {
+    const int i = x * THREADS + t, panel = i / (kUnits * 64), in = i % (kUnits * 64);
+    if (in >= nu * 64) continue;
+    uint4* v = reinterpret_cast<uint4*>(st + panel * (kTileBytesA / 2)) + in;
+    uint4 f = *v;
+    uint32_t* fw = reinterpret_cast<uint32_t*>(&f);
+    uint32_t hit = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {                    // bit 15 / 31: the exponent of the low / high half is all ones
+      const uint32_t b = ((fw[u] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+      hit |= b;
+      fw[u] &= ~((b >> 15) * 0xffffu);
+    }
+    if (hit) { *v = f; bad = 1; }
+  }
+  return bad;
 }
 // Row t of the samples' operand of k-block k: scale p of a sample whose first unit is `at` (below zero: no adapter), and, beside an odd last
 // unit, zeros in the factors' operand (by threads x of `threads`).
@@ -354,9 +440,10 @@ __device__ __forceinline__ void read_units(const uint4* src, int at, int g0, int
 //
 // adapter_few_kernel, for few tiles: a tile a cluster, whose CTAs share the contraction and the k-blocks of the term; the parts are added
 // in rank order, each CTA finishing some of the samples.  Two CTAs an SM.
-// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..5 epilogue, 6 and 7 the samples' operand of the term.
+// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..5 epilogue, 6..9 the samples' operand of the term.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kFewThreads = 256, kFewMost = 64, kMaxCluster = 8;
+constexpr int kBuild = 4;                           // warps that write the samples' operand of the term
+constexpr int kFewThreads = 32 * (6 + kBuild), kFewMost = 64, kMaxCluster = 8;
 struct FewParams {
   Term term;
   int32_t n, m;                // samples; rows of A
@@ -382,17 +469,14 @@ __device__ __forceinline__ void few_load(uint8_t* st, uint64_t* full, const CUte
   }
   tma_load_2d_hint(st + kTileBytesA, &tmZ, k * BK, 0, full, keep);     // (every tile reads the samples)
 }
-__device__ __forceinline__ void few_load_units(uint8_t* st, uint64_t* full, uint64_t* free_, const CUtensorMap& tmF, int known, int g0, int nu, int per, int m0) {
-  if (elect_one()) {
-    mbar_arrive(free_);
-    mbar_expect_tx(full, nu * 2 * kUnit * 128);
-  }
+__device__ __forceinline__ void few_load_units(uint8_t* st, uint64_t* landed, const CUtensorMap& tmF, int known, int g0, int nu, int per, int m0) {
+  if (elect_one()) mbar_expect_tx(landed, nu * 2 * kUnit * 128);
   __syncwarp();
   for (int j = 0; j < nu; ++j) {
     const int a = __shfl_sync(0xffffffffu, known, (g0 + j) & 31), y = (g0 + j) % per * kUnit;
     if (elect_one()) {
-      tma_load_3d(st + j * (kUnit * 128), &tmF, m0, y, a, full);
-      tma_load_3d(st + kTileBytesA / 2 + j * (kUnit * 128), &tmF, m0 + 64, y, a, full);
+      tma_load_3d(st + j * (kUnit * 128), &tmF, m0, y, a, landed);
+      tma_load_3d(st + kTileBytesA / 2 + j * (kUnit * 128), &tmF, m0 + 64, y, a, landed);
     }
   }
 }
@@ -413,8 +497,8 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                    const __grid_constant__ FewParams p) {
   constexpr int kStage = stage_bytes(TN), kCols = TN < 32 ? 32 : TN;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], free_[kMaxStages], built[kMaxStages], done;
-  __shared__ uint32_t tmem_slot, abort_word;
+  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], landed[kMaxStages], built[kMaxStages], done;
+  __shared__ uint32_t tmem_slot, abort_word, odd;    // odd: some factor here was not finite
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   volatile uint32_t* abort_flag = &abort_word;
   const int warp = warp_index(), lane = threadIdx.x & 31;
@@ -423,9 +507,9 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   const int per = units_of(p.term);
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
-    for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&built[i], 2); }
+    for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&landed[i], 1); mbar_init(&built[i], kBuild); }
     mbar_init(&done, 1);
-    abort_word = 0;
+    abort_word = odd = 0;
     fence_barrier_init();
     prefetch_tmap(&tmA); prefetch_tmap(&tmZ); prefetch_tmap(&tmF);
   }
@@ -434,7 +518,6 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = tmem_slot;
-  bool any = false;                                  // some adapter is bad
 
   if (warp == 0) {
     const uint64_t keep = policy_evict_last();
@@ -448,17 +531,18 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     pdl_wait();
     const int units = p.term.lists[0] * per;
     for (int g0 = mine * kUnits; g0 < units && ok; g0 += p.parts * kUnits, next()) {
-      const int known = unit_adapter(p.term, p.term.lists, (g0 & ~31) + lane, units, per);
+      const int known = unit_adapter(p.term.lists, (g0 & ~31) + lane, units, per);
       ok = mbar_wait_warp(&empty[s], ph ^ 1, abort_flag);
-      if (ok) few_load_units(smem + s * kStage, &full[s], &free_[s], tmF, known, g0, min(kUnits, units - g0), per, m0);
+      if (ok) few_load_units(smem + s * kStage, &landed[s], tmF, known, g0, min(kUnits, units - g0), per, m0);
     }
   } else if (warp == 1) {
     const uint32_t idesc_f = umma_idesc_bf16(BM, TN) | 1u << 15, idesc = MN ? idesc_f : umma_idesc_bf16(BM, TN);
-    uint32_t s = 0, ph = 0, bph = 0;
+    uint32_t s = 0, fph = 0, bph = 0;                // the phases of full and of built, a bit per stage
     bool ok = true;
-    auto next = [&]() { if (++s == static_cast<uint32_t>(p.stages)) { s = 0; ph ^= 1; } };
+    auto next = [&]() { if (++s == static_cast<uint32_t>(p.stages)) s = 0; };
     for (int k = 0; k < nk && ok; ++k, next()) {
-      ok = mbar_wait_warp(&full[s], ph, abort_flag);
+      ok = mbar_wait_warp(&full[s], (fph >> s) & 1, abort_flag);
+      fph ^= 1u << s;
       tc_fence_after();
       if (ok && elect_one()) {
         few_mma<MN>(smem_u32(smem + s * kStage), tmem_base, idesc, k == 0);
@@ -468,7 +552,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     pdl_wait();
     const int units = p.term.lists[0] * per;
     for (int g0 = mine * kUnits; g0 < units && ok; g0 += p.parts * kUnits, next()) {
-      ok = mbar_wait_warp(&full[s], ph, abort_flag) && mbar_wait_warp(&built[s], (bph >> s) & 1, abort_flag);
+      ok = mbar_wait_warp(&built[s], (bph >> s) & 1, abort_flag);
       bph ^= 1u << s;
       tc_fence_after();
       if (ok && elect_one()) {
@@ -496,30 +580,37 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     }
   } else {
     pdl_wait();
-    const int t = (warp - 6) * 32 + lane;            // this thread's sample
+    const int t = (warp - 6) * 32 + lane;            // this thread's sample, and share of the factors
     const int units = p.term.lists[0] * per, at = t < p.n ? p.term.place[t] * per : -1;
     const uint4* src = p.term.pb + t * per;
-    uint32_t s = static_cast<uint32_t>(nk) % p.stages, fph = 0;
+    uint32_t s = static_cast<uint32_t>(nk) % p.stages, lph = 0, bad = 0;
     bool ok = true;
     for (int g0 = mine * kUnits; g0 < units && ok; g0 += p.parts * kUnits) {
       const int nu = min(kUnits, units - g0);
       uint4 words[kUnits];
       read_units(src, at, g0, nu, per, words);
-      ok = mbar_wait_warp(&free_[s], (fph >> s) & 1, abort_flag);
+      ok = mbar_wait_warp(&landed[s], (lph >> s) & 1, abort_flag);
       if (!ok) break;
-      fph ^= 1u << s;
-      write_units<64>(words, smem + s * kStage, t, t < TN, nu);
+      lph ^= 1u << s;
+      write_units<32 * kBuild>(words, smem + s * kStage, t, t < TN, nu);
+      bad |= clean_units<32 * kBuild>(smem + s * kStage, t, nu);
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&built[s]);
       if (++s == static_cast<uint32_t>(p.stages)) s = 0;
     }
+    if (bad) odd = 1;
   }
   __syncwarp();
   if (p.parts > 1) { cluster_arrive(); cluster_wait(); }
   else __syncthreads();
   if (!abort_word) {
-    any = any_bad(p.term, p.term.lists, lane);
+    bool any = false;
+    for (int c = 0; c < p.parts; ++c) {
+      uint32_t w;
+      asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(w) : "r"(mapa_u32(smem_u32(&odd), c)) : "memory");
+      any |= w != 0;
+    }
     // a lane takes two rows of a sample, a warp half of its 128
     const int t1 = min((mine + 1) * TN / p.parts, p.n);
     for (int x = mine * TN / p.parts * 2 + warp; x < 2 * t1; x += kFewThreads / 32) {
@@ -554,20 +645,23 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 
 // ---------------------------------------------------------------------------------------------------------
 // adapter_stream_kernel, for more tiles: a CTA an SM takes its even share of all k-blocks of A, whole tiles first (Segments in
-// sfb_tile.cuh), so that every SM streams as much of W as the others from the start to the end; the CTA that finishes a tile has its term.
-// Two accumulators: the end of a tile runs beside the next one's products.
-// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the samples), 10 and 11 the samples'
+// sfb_tile.cuh), so that every SM streams as much of W as the others from the start to the end; the CTA that finishes a tile has its term,
+// in the middle of its k-blocks, where nothing waits for it.  Two accumulators: the end of a tile runs beside the next one's products.
+// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the samples), 10..13 the samples'
 // operand of the term.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kStreamThreads = 384, kStreamRing = 143360;
+constexpr int kStreamThreads = 32 * (2 + kEpi + kBuild), kStreamRing = 143360;
+// The k-block ahead of which a segment has its tile's term (behind the first one, which clears the accumulator); its end where it has none.
+__device__ __forceinline__ int term_at(const Segment& sg, int kseg) { return sg.k1 == kseg ? sg.k0 + max(1, (sg.k1 - sg.k0) / 2) : sg.k1; }
 template <int TN, bool MN>
-__global__ void __maxnreg__(88)                       // (a block of adapter_rank_kernel has registers beside it)
+__global__ void __maxnreg__(80)                       // (a block of adapter_rank_kernel has registers beside it)
 adapter_stream_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ CUtensorMap tmF,
                       const __grid_constant__ FewParams p) {
   constexpr int kStage = stage_bytes(TN), kCols = TN < 32 ? 32 : TN, kMine = TN == 64 ? 32 : 16;      // columns of a warp
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], free_[kMaxStages], built[kMaxStages], tfull[2], tempty[2];
-  __shared__ uint32_t tmem_slot, abort_word;
+  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], landed[kMaxStages], built[kMaxStages], tfull[2], tempty[2];
+  __shared__ uint64_t looked[2], taken[2];           // whether factors of a tile were not finite is known; read
+  __shared__ uint32_t tmem_slot, abort_word, odd[2][kBuild];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   volatile uint32_t* abort_flag = &abort_word;
   const int warp = warp_index(), lane = threadIdx.x & 31, cta = blockIdx.x, ctas = gridDim.x;
@@ -575,8 +669,8 @@ adapter_stream_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
   const int per = units_of(p.term);
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
-    for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&built[i], 2); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], kEpi); }
+    for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&landed[i], 1); mbar_init(&built[i], kBuild); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], kEpi); mbar_init(&looked[i], kBuild); mbar_init(&taken[i], kEpi); }
     abort_word = 0;
     fence_barrier_init();
     prefetch_tmap(&tmA); prefetch_tmap(&tmZ); prefetch_tmap(&tmF);
@@ -596,48 +690,58 @@ adapter_stream_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
     for (int i = 0; i < segs.n && ok; ++i) {
       const Segment sg = segs.get(i);
       const int m0 = sg.tile * BM;
-      for (int k = sg.k0; k < sg.k1 && ok; ++k, next()) {
-        ok = mbar_wait_warp(&empty[s], ph ^ 1, abort_flag);
-        if (ok) few_load<TN, MN>(smem + s * kStage, &full[s], tmA, tmZ, k, m0, keep);
-      }
+      auto load = [&](int k0, int k1) {
+        for (int k = k0; k < k1 && ok; ++k, next()) {
+          ok = mbar_wait_warp(&empty[s], ph ^ 1, abort_flag);
+          if (ok) few_load<TN, MN>(smem + s * kStage, &full[s], tmA, tmZ, k, m0, keep);
+        }
+      };
+      const int mid = term_at(sg, p.kseg);
+      load(sg.k0, mid);
       if (sg.k1 < p.kseg) continue;
       if (units < 0) {
         pdl_wait();
         units = p.term.lists[0] * per;
-        known0 = unit_adapter(p.term, p.term.lists, lane, units, per);
+        known0 = unit_adapter(p.term.lists, lane, units, per);
       }
       for (int g0 = 0, known = known0; g0 < units && ok; g0 += kUnits, next()) {
-        if (g0 && (g0 & 31) == 0) known = unit_adapter(p.term, p.term.lists, g0 + lane, units, per);
+        if (g0 && (g0 & 31) == 0) known = unit_adapter(p.term.lists, g0 + lane, units, per);
         ok = mbar_wait_warp(&empty[s], ph ^ 1, abort_flag);
-        if (ok) few_load_units(smem + s * kStage, &full[s], &free_[s], tmF, known, g0, min(kUnits, units - g0), per, m0);
+        if (ok) few_load_units(smem + s * kStage, &landed[s], tmF, known, g0, min(kUnits, units - g0), per, m0);
       }
+      load(mid, sg.k1);
     }
   } else if (warp == 1) {
     const uint32_t idesc_f = umma_idesc_bf16(BM, TN) | 1u << 15, idesc = MN ? idesc_f : umma_idesc_bf16(BM, TN);
-    uint32_t s = 0, ph = 0, bph = 0;
+    uint32_t s = 0, fph = 0, bph = 0;                // the phases of full and of built, a bit per stage
     bool ok = true;
-    auto next = [&]() { if (++s == static_cast<uint32_t>(p.stages)) { s = 0; ph ^= 1; } };
+    auto next = [&]() { if (++s == static_cast<uint32_t>(p.stages)) s = 0; };
     int units = -1;
     for (int i = 0; i < segs.n && ok; ++i) {
       const Segment sg = segs.get(i);
       const uint32_t a = i & 1, aph = (i >> 1) & 1, d_tmem = tmem_base + a * kCols;
       if (!mbar_wait_warp(&tempty[a], aph ^ 1, abort_flag)) break;
       tc_fence_after();
-      for (int k = sg.k0; k < sg.k1 && ok; ++k, next()) {
-        ok = mbar_wait_warp(&full[s], ph, abort_flag);
-        tc_fence_after();
-        if (ok && elect_one()) {
-          few_mma<MN>(smem_u32(smem + s * kStage), d_tmem, idesc, k == sg.k0);
-          umma_commit(&empty[s]);
+      auto mma = [&](int k0, int k1) {
+        for (int k = k0; k < k1 && ok; ++k, next()) {
+          ok = mbar_wait_warp(&full[s], (fph >> s) & 1, abort_flag);
+          fph ^= 1u << s;
+          tc_fence_after();
+          if (ok && elect_one()) {
+            few_mma<MN>(smem_u32(smem + s * kStage), d_tmem, idesc, k == sg.k0);
+            umma_commit(&empty[s]);
+          }
         }
-      }
+      };
+      const int mid = term_at(sg, p.kseg);
+      mma(sg.k0, mid);
       if (sg.k1 == p.kseg) {
         if (units < 0) {
           pdl_wait();
           units = p.term.lists[0] * per;
         }
         for (int g0 = 0; g0 < units && ok; g0 += kUnits, next()) {
-          ok = mbar_wait_warp(&full[s], ph, abort_flag) && mbar_wait_warp(&built[s], (bph >> s) & 1, abort_flag);
+          ok = mbar_wait_warp(&built[s], (bph >> s) & 1, abort_flag);
           bph ^= 1u << s;
           tc_fence_after();
           if (ok && elect_one()) {
@@ -645,19 +749,22 @@ adapter_stream_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
             umma_commit(&empty[s]);
           }
         }
+        mma(mid, sg.k1);
       }
       if (ok && elect_one()) umma_commit(&tfull[a]);
     }
   } else if (warp < 2 + kEpi) {
     const int w8 = warp - 2, q = warp & 3, h = w8 >> 2, t0 = h * kMine;
     pdl_wait();
-    const bool any = any_bad(p.term, p.term.lists, lane);
     for (int i = 0; i < segs.n; ++i) {
       const Segment sg = segs.get(i);
       const int m = sg.tile * BM + q * 32 + lane;
       const uint32_t a = i & 1, aph = (i >> 1) & 1;
-      if (!mbar_wait_warp(&tfull[a], aph, abort_flag)) break;
+      if (!mbar_wait_warp(&tfull[a], aph, abort_flag) || !mbar_wait_warp(&looked[a], aph, abort_flag)) break;
       tc_fence_after();
+      uint32_t any = 0;
+#pragma unroll
+      for (int w = 0; w < kBuild; ++w) any |= odd[a][w];
       const bool mine = t0 < TN;
       float v[kMine];
       if (mine) {
@@ -671,7 +778,7 @@ adapter_stream_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&tempty[a]);
+      if (lane == 0) { mbar_arrive(&tempty[a]); mbar_arrive(&taken[a]); }
       if (!mine) continue;
       const int64_t to = static_cast<int64_t>(t0) * BM + q * 32 + lane;     // of a CTA's part: [sample][128 rows]
       if (sg.k1 < p.kseg) {
@@ -713,27 +820,37 @@ adapter_stream_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
     }
   } else {
     pdl_wait();
-    const int t = (warp - 2 - kEpi) * 32 + lane;     // this thread's sample
+    const int w = warp - 2 - kEpi, t = w * 32 + lane;                  // this thread's sample, and share of the factors
     const int units = p.term.lists[0] * per, at = t < p.n ? p.term.place[t] * per : -1;
     const uint4* src = p.term.pb + t * per;
-    uint32_t g = 0, fph = 0;                         // k-blocks so far; the phases of free_, a bit per stage
+    uint32_t g = 0, lph = 0;                         // k-blocks so far; the phases of landed, a bit per stage
     bool ok = true;
     for (int i = 0; i < segs.n && ok; ++i) {
       const Segment sg = segs.get(i);
-      g += sg.k1 - sg.k0;
-      if (sg.k1 < p.kseg) continue;
-      for (int g0 = 0; g0 < units; g0 += kUnits, ++g) {
+      const int mid = term_at(sg, p.kseg);
+      const uint32_t a = i & 1, aph = (i >> 1) & 1;
+      if (!mbar_wait_warp(&taken[a], aph ^ 1, abort_flag)) break;
+      uint32_t bad = 0;
+      g += mid - sg.k0;
+      for (int g0 = 0; g0 < units && sg.k1 == p.kseg; g0 += kUnits, ++g) {
         const uint32_t s = g % p.stages;
         const int nu = min(kUnits, units - g0);
         uint4 words[kUnits];
         read_units(src, at, g0, nu, per, words);
-        ok = mbar_wait_warp(&free_[s], (fph >> s) & 1, abort_flag);
+        ok = mbar_wait_warp(&landed[s], (lph >> s) & 1, abort_flag);
         if (!ok) break;
-        fph ^= 1u << s;
-        write_units<64>(words, smem + s * kStage, t, t < TN, nu);
+        lph ^= 1u << s;
+        write_units<32 * kBuild>(words, smem + s * kStage, t, t < TN, nu);
+        bad |= clean_units<32 * kBuild>(smem + s * kStage, t, nu);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&built[s]);
+      }
+      g += sg.k1 - mid;
+      bad = __any_sync(0xffffffffu, bad);
+      if (lane == 0) {
+        odd[a][w] = bad;
+        mbar_arrive(&looked[a]);
       }
     }
   }
@@ -758,7 +875,7 @@ adapter_stream_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
 // Warps: 0 TMA producer, 1 MMA issuer (leader CTA) and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the columns), 10..13
 // the samples' operand of the adapters' term.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kPairThreads = 448, kBuild = 4, kGroup = 8;      // kGroup: tiles of samples that follow one another
+constexpr int kPairThreads = 448, kGroup = 8;      // kGroup: tiles of samples that follow one another
 constexpr int kPairStages = 6, kPairStage = 2 * kTileBytesA;
 constexpr int kPairSmem = kPairStages * kPairStage + 1024;
 constexpr int kPartFloats = BM * kMaxTile;          // what a CTA leaves of a tile
@@ -1051,9 +1168,40 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// p from its parts, zeros for a sample without an adapter, and scale p in bf16 (pb).  Ahead of adapter_pair_kernel, in the first blocks:
+// More than 64 samples: p from its parts, zeros for a sample without an adapter, and scale p in bf16 (pb).  In the first blocks:
 // which of the adapters in use have factors that are not finite, a block a sixteenth of an adapter's, and the lists of the tiles.
 // ---------------------------------------------------------------------------------------------------------
+// Whether columns [0, width) of part `part` of 16 of an adapter's factors f [rank][ldf] hold an infinity or a NaN; by a block.
+__device__ __forceinline__ bool holds_not_finite(const __nv_bfloat16* f, int rank, int64_t ldf, int64_t width, int part) {
+  bool hit = false;
+  // pieces of 8 columns, row after row; of a row's last one what lies behind the row does not count
+  const int64_t pieces = (width + 7) / 8, all = pieces * rank, to = all * (part + 1) / 16;
+  int64_t i = all * part / 16 + threadIdx.x, r = i / pieces, c = i - r * pieces;
+  while (i < to) {
+    uint4 v[4];
+    int64_t left[4];
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      left[y] = i < to ? width - c * 8 : 0;
+      v[y] = i < to ? *reinterpret_cast<const uint4*>(f + r * ldf + c * 8) : make_uint4(0, 0, 0, 0);
+      i += blockDim.x;
+      c += blockDim.x;
+      while (c >= pieces) { c -= pieces; ++r; }
+    }
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const uint32_t w[4] = {v[y].x, v[y].y, v[y].z, v[y].w};
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {                  // bit 15 / 31: the exponent of the low / high half is all ones
+        const uint32_t b = ((w[u] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+        hit |= (b & 0x8000u) && 2 * u < left[y];
+        hit |= (b >> 31) && 2 * u + 1 < left[y];
+      }
+    }
+  }
+  return __syncthreads_or(hit);
+}
+
 constexpr int kLookMost = 512;                      // adapters that the grid looks at at once
 struct SumParams {
   Ranked p;
@@ -1101,34 +1249,7 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
       if (mine < p.adapters && p.mark[mine] == p.call) list[atomicAdd(&count, 1)] = static_cast<int32_t>(mine);
       __syncthreads();
       for (int x = 0; x < count; ++x) {
-        const __nv_bfloat16* f = p.F + static_cast<int64_t>(list[x]) * p.rank * p.ldf;
-        bool hit = false;
-        // pieces of 8 columns, row after row; of a row's last one what lies behind the row does not count
-        const int64_t pieces = (p.width + 7) / 8, all = pieces * p.rank, to = all * (part + 1) / 16;
-        int64_t i = all * part / 16 + threadIdx.x, r = i / pieces, c = i - r * pieces;
-        while (i < to) {
-          uint4 v[4];
-          int64_t left[4];
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            left[y] = i < to ? p.width - c * 8 : 0;
-            v[y] = i < to ? *reinterpret_cast<const uint4*>(f + r * p.ldf + c * 8) : make_uint4(0, 0, 0, 0);
-            i += 256;
-            c += 256;
-            while (c >= pieces) { c -= pieces; ++r; }
-          }
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const uint32_t w[4] = {v[y].x, v[y].y, v[y].z, v[y].w};
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {            // bit 15 / 31: the exponent of the low / high half is all ones
-              const uint32_t b = ((w[u] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-              hit |= (b & 0x8000u) && 2 * u < left[y];
-              hit |= (b >> 31) && 2 * u + 1 < left[y];
-            }
-          }
-        }
-        hit = __syncthreads_or(hit);
+        const bool hit = holds_not_finite(p.F + static_cast<int64_t>(list[x]) * p.rank * p.ldf, p.rank, p.ldf, p.width, part);
         if (threadIdx.x == 0) p.bad[static_cast<int64_t>(list[x]) * 16 + part] = hit;
       }
       __syncthreads();
@@ -1137,17 +1258,6 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
   }
   const int per = (p.rank + kUnit - 1) / kUnit;
   const int64_t blocks = gridDim.x - p.look - p.tiles;
-  if (p.n <= kFewMost) {                             // entry by entry: few threads have all to do
-    for (int64_t x = static_cast<int64_t>(tile - p.tiles) * 256 + threadIdx.x; x < p.n * per * kUnit; x += blocks * 256) {
-      const int64_t i = x / (per * kUnit);
-      const int r = static_cast<int>(x - i * per * kUnit), id = p.ids[i];
-      const bool has = id >= 0 && id < p.adapters && r < p.rank;
-      const float v = has ? ranked(p.p, i * p.rank + r) : 0.f;
-      if (r < p.rank) p.out[i * p.rank + r] = v;
-      p.pb[x] = __float2bfloat16_rn(has ? p.scale[id] * v : 0.f);
-    }
-    return;
-  }
   for (int64_t x = static_cast<int64_t>(tile - p.tiles) * 256 + threadIdx.x; x < p.n * per; x += blocks * 256) {
     const int64_t i = x / per;
     const int r0 = static_cast<int>(x - i * per) * kUnit, id = p.ids[i];
@@ -1556,7 +1666,7 @@ int64_t rank_rows(int64_t n, int64_t d) {
 }
 
 struct AdapterLayout {
-  size_t status, ready, s, t, ssum, tsum, pb, swords, twords, order, begin, count, work, mark, bad, lists, place, partial, total;
+  size_t status, ready, arrived, s, t, ssum, tsum, pb, swords, twords, order, begin, count, work, mark, bad, lists, place, partial, total;
 };
 
 int check(const sfb_adapter_config* c) {
@@ -1578,6 +1688,7 @@ AdapterLayout layout_of(const sfb_adapter_config& c) {
   const size_t n = static_cast<size_t>(c.max_samples), rp = (static_cast<size_t>(c.rank) + 15) / 16 * 16;
   L.status = take(4);
   L.ready = take(kModelSms * kEpi * 4);              // these are cleared with the status word
+  L.arrived = take(kFewChunks * 4);
   L.mark = take(static_cast<size_t>(c.adapters) * 4);
   L.bad = take(static_cast<size_t>(c.adapters) * 16);
   L.s = take(static_cast<size_t>(rank_rows(c.max_samples, c.cols)) * c.rank * 4);
@@ -1655,24 +1766,54 @@ bool factor_map(sfb_adapters* h, CUtensorMap* m, const void* base, int64_t width
                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// p = F[a] z for n samples into `out`; *got: where and in how many parts.
-cudaError_t rank_products(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, int64_t d, const CUtensorMap& mapF, const int32_t* ids, float* out,
-                          Ranked* got) {
+// allow_smem for a kernel that runs beside another one: the SM's memory as shared memory from the start (as much as the first of the two
+// asks for by itself would keep the second one out until it is done).
+template <auto Kernel>
+cudaError_t allow_beside(int bytes) {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(Kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  if (e == cudaSuccess) e = allow_smem<Kernel>(bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+  return e;
+}
+
+// p = F[a] z for n samples.  *got: where, and in how many parts.  Up to 64 samples it is in `sum` in one part, with all that a product
+// with the other factors (MN: with V) takes; for more adapter_sum_kernel has to follow.
+template <bool MN>
+cudaError_t rank_products(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const int32_t* ids, float* out, float* sum, Ranked* got) {
+  const sfb_adapter_config& c = h->cfg;
+  const int64_t d = MN ? c.rows : c.cols;
   const int tn = rank_tile(n), parts = rank_parts(n, d), tiles = static_cast<int>((n + tn - 1) / tn);
+  const CUtensorMap& mf = MN ? h->mapU : h->mapV;
   CUtensorMap mz;
   if (!operand_map(h, &mz, Z, d, n, ldz, BK, tn, CU_TENSOR_MAP_L2_PROMOTION_L2_256B)) return cudaErrorInvalidValue;
   RankParams p{};
-  p.n = static_cast<int32_t>(n); p.tn = tn; p.kseg = static_cast<int32_t>((d + BK - 1) / BK); p.stages = std::min(kMaxStages, (n <= kFewMost ? kFewRing : kSmallRing) / stage_bytes(tn));
-  p.rank = h->cfg.rank; p.adapters = h->cfg.adapters; p.ids = ids; p.out = out; p.status = h->at<uint32_t>(h->lay.status);
+  p.n = static_cast<int32_t>(n); p.tn = tn; p.kseg = static_cast<int32_t>((d + BK - 1) / BK);
+  p.stages = std::min(kMaxStages, (n <= kFewMost ? kFewRing : kSmallRing) / stage_bytes(tn));
+  p.rank = c.rank; p.adapters = c.adapters; p.ids = ids; p.out = out; p.status = h->at<uint32_t>(h->lay.status);
+  const int per = (c.rank + kSlice - 1) / kSlice, chunks = (std::min(tn, c.adapters) * per + 7) / 8;
+  const int smem = p.stages * stage_bytes(tn) + 1024;
+  if (n <= kFewMost) {
+    p.scale = h->scale; p.p = sum; p.pb = h->at<__nv_bfloat16>(h->lay.pb);
+    p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place); p.arrived = h->at<uint32_t>(h->lay.arrived);
+    const cudaError_t e = allow_beside<adapter_rank_kernel<true>>(kFewRing + 1024);
+    if (e != cudaSuccess) return e;
+    *got = Ranked{sum, 1, 0};
+    // a block an SM, and no more than there can be parts of chunks
+    return launch_kernel(adapter_rank_kernel<true>, dim3(std::max(1, std::min(kModelSms, chunks * parts))), dim3(kRankThreads), smem, h->stream, 1, mf, mz, p);
+  }
   p.mark = h->at<int32_t>(h->lay.mark);
   p.call = static_cast<int32_t>(++h->calls);
-  const int per = (h->cfg.rank + kSlice - 1) / kSlice, chunks = (std::min(tn, h->cfg.adapters) * per + 7) / 8;
-  const int groups = std::max(1, std::min(chunks, (n <= kFewMost ? 1 : 2) * kModelSms / (parts * tiles)));
-  const int smem = p.stages * stage_bytes(tn) + 1024;
-  cudaError_t e = allow_smem<adapter_rank_kernel>(kSmallRing + 1024);
+  const int groups = std::max(1, std::min(chunks, 2 * kModelSms / (parts * tiles)));
+  const cudaError_t e = allow_smem<adapter_rank_kernel<false>>(kSmallRing + 1024);
   if (e != cudaSuccess) return e;
-  *got = Ranked{out, parts, n * h->cfg.rank};
-  return launch_kernel(adapter_rank_kernel, dim3(parts, tiles, groups), dim3(kRankThreads), smem, h->stream, 1, mapF, mz, p);
+  *got = Ranked{out, parts, n * c.rank};
+  return launch_kernel(adapter_rank_kernel<false>, dim3(parts, tiles, groups), dim3(kRankThreads), smem, h->stream, 1, mf, mz, p);
 }
 
 constexpr int64_t kClusterTiles = 2 * kModelSms / kMaxCluster;      // tiles up to which eight CTAs share each
@@ -1684,11 +1825,11 @@ int few_parts(int64_t tiles, int64_t kseg) {
   return best;
 }
 
-// What adapter_sum_kernel leaves for the products.
+// What adapter_rank_kernel or adapter_sum_kernel leaves for the products.
 template <bool MN>
-Term term_of(const sfb_adapters* h, const int32_t* ids, const float* p) {
+Term term_of(const sfb_adapters* h, const int32_t* ids, const float* p, bool bad) {
   const sfb_adapter_config& c = h->cfg;
-  return Term{c.rank, c.adapters, ids, h->at<int32_t>(h->lay.lists), h->at<int32_t>(h->lay.place), h->scale, h->at<uint4>(h->lay.bad),
+  return Term{c.rank, c.adapters, ids, h->at<int32_t>(h->lay.lists), h->at<int32_t>(h->lay.place), h->scale, bad ? h->at<uint4>(h->lay.bad) : nullptr,
               static_cast<const __nv_bfloat16*>(MN ? h->V : h->U), MN ? c.ldv : c.ldu, p, h->at<uint4>(h->lay.pb)};
 }
 
@@ -1710,7 +1851,7 @@ cudaError_t few(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const Te
   if (tiles <= kClusterTiles) {
     p.parts = few_parts(tiles, p.kseg);
     p.stages = std::min(kMaxStages, kSmallRing / stage_bytes(TN));
-    const cudaError_t e = allow_smem<adapter_few_kernel<TN, MN>>(kSmallRing + 1024);
+    const cudaError_t e = allow_beside<adapter_few_kernel<TN, MN>>(kSmallRing + 1024);
     if (e != cudaSuccess) return e;
     return launch_kernel(adapter_few_kernel<TN, MN>, dim3(static_cast<unsigned>(tiles * p.parts)), dim3(kFewThreads), p.stages * stage_bytes(TN) + 1024,
                          h->stream, p.parts, ma, mz, mf, p);
@@ -1722,7 +1863,7 @@ cudaError_t few(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const Te
   p.whole = p.cut ? static_cast<int32_t>(std::max<int64_t>(0, tiles / ctas - 1) * ctas) : 0;
   p.stages = std::min(kMaxStages, kStreamRing / stage_bytes(TN));
   p.partial = h->at<float>(h->lay.partial); p.ready = h->at<uint32_t>(h->lay.ready);
-  const cudaError_t e = allow_smem<adapter_stream_kernel<TN, MN>>(kStreamRing + 1024);
+  const cudaError_t e = allow_beside<adapter_stream_kernel<TN, MN>>(kStreamRing + 1024);
   if (e != cudaSuccess) return e;
   return launch_kernel(adapter_stream_kernel<TN, MN>, dim3(static_cast<unsigned>(ctas)), dim3(kStreamThreads), p.stages * stage_bytes(TN) + 1024, h->stream, 1,
                        ma, mz, mf, p);
@@ -1766,11 +1907,14 @@ cudaError_t pairs(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const 
                           dim3(kPairThreads), kPairSmem, h->stream, 1, ma, mz, MN ? h->unitV : h->unitU, p);
 }
 
-// y = A z + scale F^T p; p_out (may be null) receives p; *s: p where it is afterwards.
+// y = A z + scale F^T p.  p in parts goes to `to` first; *s: p where it is afterwards.
 template <bool MN>
-cudaError_t product(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const int32_t* ids, Ranked* s, float* p_out, float* room, void* Y, int64_t ldy) {
-  float* to = p_out ? p_out : room;
+cudaError_t product(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const int32_t* ids, Ranked* s, float* to, void* Y, int64_t ldy) {
   const sfb_adapter_config& c = h->cfg;
+  if (n <= kFewMost) {
+    const Term term = term_of<MN>(h, ids, s->at, false);
+    return n <= 16 ? few<16, MN>(h, n, Z, ldz, term, Y, ldy) : n <= 32 ? few<32, MN>(h, n, Z, ldz, term, Y, ldy) : few<kFewMost, MN>(h, n, Z, ldz, term, Y, ldy);
+  }
   SumParams p{};
   p.p = *s; p.ids = ids; p.scale = h->scale; p.n = n; p.rank = c.rank; p.adapters = c.adapters; p.out = to; p.status = h->at<uint32_t>(h->lay.status);
   p.pb = h->at<__nv_bfloat16>(h->lay.pb);
@@ -1778,15 +1922,11 @@ cudaError_t product(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, cons
   p.mark = h->at<int32_t>(h->lay.mark); p.call = static_cast<int32_t>(h->calls); p.look = std::min(c.adapters, kLookMost) * 16;
   p.bad = h->at<uint8_t>(h->lay.bad);
   p.tn = tile_of(n); p.tiles = static_cast<int32_t>((n + p.tn - 1) / p.tn); p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place);
-  const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(p.look + p.tiles + grid1d(n * ((c.rank + kUnit - 1) / kUnit) * (n <= kFewMost ? kUnit : 1), 256)), dim3(256), 0, h->stream,
+  const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(p.look + p.tiles + grid1d(n * ((c.rank + kUnit - 1) / kUnit), 256)), dim3(256), 0, h->stream,
                                       1, p);
   if (e != cudaSuccess) return e;
   *s = Ranked{to, 1, 0};
-  const Term term = term_of<MN>(h, ids, to);
-  if (n <= 16) return few<16, MN>(h, n, Z, ldz, term, Y, ldy);
-  if (n <= 32) return few<32, MN>(h, n, Z, ldz, term, Y, ldy);
-  if (n <= kFewMost) return few<kFewMost, MN>(h, n, Z, ldz, term, Y, ldy);
-  return pairs<MN>(h, n, Z, ldz, term, Y, ldy);
+  return pairs<MN>(h, n, Z, ldz, term_of<MN>(h, ids, to, true), Y, ldy);
 }
 
 int fail(sfb_adapters* h, cudaError_t e) {
@@ -1870,8 +2010,9 @@ extern "C" int sfb_adapter_forward(sfb_adapters* h, int64_t n, const void* X_dev
   const OnDevice on(h->device);
   ACK(on.err);
   Ranked s{};
-  ACK(rank_products(h, n, X_dev, ldx, c.cols, h->mapV, ids_dev, h->at<float>(h->lay.s), &s));
-  ACK(product<false>(h, n, X_dev, ldx, ids_dev, &s, S_dev, h->at<float>(h->lay.ssum), Y_dev, ldy));
+  float* sum = S_dev ? S_dev : h->at<float>(h->lay.ssum);
+  ACK(rank_products<false>(h, n, X_dev, ldx, ids_dev, h->at<float>(h->lay.s), sum, &s));
+  ACK(product<false>(h, n, X_dev, ldx, ids_dev, &s, sum, Y_dev, ldy));
   return SFB_OK;
 }
 
@@ -1899,9 +2040,9 @@ extern "C" int sfb_adapter_backward(sfb_adapters* h, int64_t n, const void* dY_d
     ACK(launch_kernel(adapter_index_kernel, dim3(c.adapters), dim3(256), 0, h->stream, 1, ids_dev, static_cast<int32_t>(n), c.adapters, order,
                       begin, count, status));
   Ranked s{S_dev, 1, 0}, t{};
-  if (dU_dev && !S_dev) ACK(rank_products(h, n, X_dev, ldx, c.cols, h->mapV, ids_dev, h->at<float>(h->lay.s), &s));
-  if (dX_dev || dV_dev) ACK(rank_products(h, n, dY_dev, lddy, c.rows, h->mapU, ids_dev, h->at<float>(h->lay.t), &t));
-  if (dX_dev) ACK(product<true>(h, n, dY_dev, lddy, ids_dev, &t, nullptr, h->at<float>(h->lay.tsum), dX_dev, lddx));
+  if (dU_dev && !S_dev) ACK(rank_products<false>(h, n, X_dev, ldx, ids_dev, h->at<float>(h->lay.s), h->at<float>(h->lay.ssum), &s));
+  if (dX_dev || dV_dev) ACK(rank_products<true>(h, n, dY_dev, lddy, ids_dev, h->at<float>(h->lay.t), h->at<float>(h->lay.tsum), &t));
+  if (dX_dev) ACK(product<true>(h, n, dY_dev, lddy, ids_dev, &t, h->at<float>(h->lay.tsum), dX_dev, lddx));
   if (dU_dev || dV_dev) {
     __nv_bfloat16 *swords = h->at<__nv_bfloat16>(h->lay.swords), *twords = h->at<__nv_bfloat16>(h->lay.twords);
     WordsParams w{};
