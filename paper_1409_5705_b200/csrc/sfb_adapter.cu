@@ -354,6 +354,7 @@ __device__ __forceinline__ void store_two(__nv_bfloat16* Y, int64_t ldy, int i, 
 // ---------------------------------------------------------------------------------------------------------
 struct Term {
   int32_t rank, adapters;
+  int32_t boxed;               // units that one copy of factors brings: a power of two that divides those of an adapter
   const int32_t *ids, *lists, *place;
   const float* scale;
   const uint4* bad;            // [adapters]: not zero where the factors are not finite (null up to 64 samples)
@@ -388,25 +389,46 @@ __device__ __forceinline__ bool any_bad(const Term& p, const int32_t* list, int 
 __device__ __forceinline__ int unit_adapter(const int32_t* list, int g, int units, int per) {
   return g < units ? list[1 + g / per] : 0;
 }
+__device__ __forceinline__ uint4 lds_v4(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
 // Replaces what is not finite of the factors of `nu` units in a stage by zeros; whether there was anything.  By THREADS threads, t of them.
 template <int THREADS>
 __device__ __forceinline__ uint32_t clean_units(uint8_t* st, int t, int nu) {
+  // bit 15 / 31: the exponent of the low / high half is all ones
+  auto found = [](uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; };
+  constexpr int kBatch = 4, kPieces = 2 * kUnits * 64 / THREADS;       // of a thread, in both panels
   uint32_t bad = 0;
-#pragma unroll
-  for (int x = 0; x < 2 * kUnits * 64 / THREADS; ++x) {
-    const int i = x * THREADS + t, panel = i / (kUnits * 64), in = i % (kUnits * 64);
-    if (in >= nu * 64) continue;
-    uint4* v = reinterpret_cast<uint4*>(st + panel * (kTileBytesA / 2)) + in;
-    uint4 f = *v;
-    uint32_t* fw = reinterpret_cast<uint32_t*>(&f);
+#pragma unroll 1
+  for (int b = 0; b < kPieces; b += kBatch) {        // (loads first: with a branch behind each of them a block took 1.3 us)
     uint32_t hit = 0;
+    uint4 v[kBatch];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {                    // bit 15 / 31: the exponent of the low / high half is all ones
-      const uint32_t b = ((fw[u] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-      hit |= b;
-      fw[u] &= ~((b >> 15) * 0xffffu);
+    for (int u = 0; u < kBatch; ++u) {
+      const int i = (b + u) * THREADS + t, panel = i / (kUnits * 64), in = i % (kUnits * 64);
+      v[u] = lds_v4(smem_u32(st) + panel * (kTileBytesA / 2) + in * 16);
     }
-    if (hit) { *v = f; bad = 1; }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int in = ((b + u) * THREADS + t) % (kUnits * 64);
+      const uint32_t f = found(v[u].x) | found(v[u].y) | found(v[u].z) | found(v[u].w);
+      hit |= in < nu * 64 ? f : 0u;
+    }
+    if (hit) {
+      bad = 1;
+#pragma unroll 1
+      for (int u = 0; u < kBatch; ++u) {
+        const int i = (b + u) * THREADS + t, panel = i / (kUnits * 64), in = i % (kUnits * 64);
+        if (in >= nu * 64) continue;
+        const uint32_t at = smem_u32(st) + panel * (kTileBytesA / 2) + in * 16;
+        uint4 w = lds_v4(at);
+        w.x &= ~((found(w.x) >> 15) * 0xffffu); w.y &= ~((found(w.y) >> 15) * 0xffffu);
+        w.z &= ~((found(w.z) >> 15) * 0xffffu); w.w &= ~((found(w.w) >> 15) * 0xffffu);
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+      }
+    }
   }
   return bad;
 }
@@ -440,9 +462,11 @@ __device__ __forceinline__ void read_units(const uint4* src, int at, int g0, int
 //
 // adapter_few_kernel, for few tiles: a tile a cluster, whose CTAs share the contraction and the k-blocks of the term; the parts are added
 // in rank order, each CTA finishing some of the samples.  Two CTAs an SM.
-// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..5 epilogue, 6..9 the samples' operand of the term.
+// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..5 epilogue, 6 and 7 the samples' operand of the term, 8 and 9
+// its factors.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kBuild = 4;                           // warps that write the samples' operand of the term
+constexpr int kWrite = 2, kClean = 2, kBuild = kWrite + kClean;      // warps that write the samples' operand of the term, that look
+                                                                     // through the factors
 constexpr int kFewThreads = 32 * (6 + kBuild), kFewMost = 64, kMaxCluster = 8;
 struct FewParams {
   Term term;
@@ -469,10 +493,14 @@ __device__ __forceinline__ void few_load(uint8_t* st, uint64_t* full, const CUte
   }
   tma_load_2d_hint(st + kTileBytesA, &tmZ, k * BK, 0, full, keep);     // (every tile reads the samples)
 }
-__device__ __forceinline__ void few_load_units(uint8_t* st, uint64_t* landed, const CUtensorMap& tmF, int known, int g0, int nu, int per, int m0) {
-  if (elect_one()) mbar_expect_tx(landed, nu * 2 * kUnit * 128);
+__device__ __forceinline__ void few_load_units(uint8_t* st, uint64_t* landed, uint64_t* free_, const CUtensorMap& tmF, int known, int g0, int nu, int per,
+                                               int boxed, int m0) {
+  if (elect_one()) {
+    mbar_arrive(free_);
+    mbar_expect_tx(landed, nu * 2 * kUnit * 128);
+  }
   __syncwarp();
-  for (int j = 0; j < nu; ++j) {
+  for (int j = 0; j < nu; j += boxed) {
     const int a = __shfl_sync(0xffffffffu, known, (g0 + j) & 31), y = (g0 + j) % per * kUnit;
     if (elect_one()) {
       tma_load_3d(st + j * (kUnit * 128), &tmF, m0, y, a, landed);
@@ -497,7 +525,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                    const __grid_constant__ FewParams p) {
   constexpr int kStage = stage_bytes(TN), kCols = TN < 32 ? 32 : TN;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], landed[kMaxStages], built[kMaxStages], done;
+  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], free_[kMaxStages], landed[kMaxStages], built[kMaxStages], done;
   __shared__ uint32_t tmem_slot, abort_word, odd;    // odd: some factor here was not finite
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   volatile uint32_t* abort_flag = &abort_word;
@@ -507,7 +535,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   const int per = units_of(p.term);
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
-    for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&landed[i], 1); mbar_init(&built[i], kBuild); }
+    for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&landed[i], 1); mbar_init(&built[i], kBuild); }
     mbar_init(&done, 1);
     abort_word = odd = 0;
     fence_barrier_init();
@@ -533,7 +561,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     for (int g0 = mine * kUnits; g0 < units && ok; g0 += p.parts * kUnits, next()) {
       const int known = unit_adapter(p.term.lists, (g0 & ~31) + lane, units, per);
       ok = mbar_wait_warp(&empty[s], ph ^ 1, abort_flag);
-      if (ok) few_load_units(smem + s * kStage, &landed[s], tmF, known, g0, min(kUnits, units - g0), per, m0);
+      if (ok) few_load_units(smem + s * kStage, &landed[s], &free_[s], tmF, known, g0, min(kUnits, units - g0), per, p.term.boxed, m0);
     }
   } else if (warp == 1) {
     const uint32_t idesc_f = umma_idesc_bf16(BM, TN) | 1u << 15, idesc = MN ? idesc_f : umma_idesc_bf16(BM, TN);
@@ -580,23 +608,24 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     }
   } else {
     pdl_wait();
-    const int t = (warp - 6) * 32 + lane;            // this thread's sample, and share of the factors
-    const int units = p.term.lists[0] * per, at = t < p.n ? p.term.place[t] * per : -1;
+    const bool writes = warp < 6 + kWrite;
+    const int t = (writes ? warp - 6 : warp - 6 - kWrite) * 32 + lane;     // this thread's sample, or share of the factors
+    const int units = p.term.lists[0] * per, at = writes && t < p.n ? p.term.place[t] * per : -1;
     const uint4* src = p.term.pb + t * per;
-    uint32_t s = static_cast<uint32_t>(nk) % p.stages, lph = 0, bad = 0;
-    bool ok = true;
-    for (int g0 = mine * kUnits; g0 < units && ok; g0 += p.parts * kUnits) {
+    uint32_t s = static_cast<uint32_t>(nk) % p.stages, ph = 0, bad = 0;    // ph: the phases of free_, or of landed, a bit per stage
+    uint4 words[kUnits];
+    if (writes) read_units(src, at, mine * kUnits, min(kUnits, units - mine * kUnits), per, words);
+    for (int g0 = mine * kUnits; g0 < units; g0 += p.parts * kUnits) {
       const int nu = min(kUnits, units - g0);
-      uint4 words[kUnits];
-      read_units(src, at, g0, nu, per, words);
-      ok = mbar_wait_warp(&landed[s], (lph >> s) & 1, abort_flag);
-      if (!ok) break;
-      lph ^= 1u << s;
-      write_units<32 * kBuild>(words, smem + s * kStage, t, t < TN, nu);
-      bad |= clean_units<32 * kBuild>(smem + s * kStage, t, nu);
-      fence_proxy_async_smem();
+      if (!mbar_wait_warp(writes ? &free_[s] : &landed[s], (ph >> s) & 1, abort_flag)) break;
+      ph ^= 1u << s;
+      uint32_t wrote = 1;
+      if (writes) write_units<32 * kWrite>(words, smem + s * kStage, t, t < TN, nu);
+      else bad |= wrote = clean_units<32 * kClean>(smem + s * kStage, t, nu);
+      if (wrote) fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&built[s]);
+      if (writes) read_units(src, at, g0 + p.parts * kUnits, min(kUnits, units - g0 - p.parts * kUnits), per, words);
       if (++s == static_cast<uint32_t>(p.stages)) s = 0;
     }
     if (bad) odd = 1;
@@ -646,22 +675,22 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // ---------------------------------------------------------------------------------------------------------
 // adapter_stream_kernel, for more tiles: a CTA an SM takes its even share of all k-blocks of A, whole tiles first (Segments in
 // sfb_tile.cuh), so that every SM streams as much of W as the others from the start to the end; the CTA that finishes a tile has its term,
-// in the middle of its k-blocks, where nothing waits for it.  Two accumulators: the end of a tile runs beside the next one's products.
-// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the samples), 10..13 the samples'
-// operand of the term.
+// behind three quarters of its k-blocks, where p should be there and nothing waits for it.  Two accumulators: the end of a tile runs beside the next one's products.
+// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the samples), 10 and 11 the samples'
+// operand of the term, 12 and 13 its factors.
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kStreamThreads = 32 * (2 + kEpi + kBuild), kStreamRing = 143360;
 // The k-block ahead of which a segment has its tile's term (behind the first one, which clears the accumulator); its end where it has none.
-__device__ __forceinline__ int term_at(const Segment& sg, int kseg) { return sg.k1 == kseg ? sg.k0 + max(1, (sg.k1 - sg.k0) / 2) : sg.k1; }
+__device__ __forceinline__ int term_at(const Segment& sg, int kseg) { return sg.k1 == kseg ? sg.k0 + max(1, (sg.k1 - sg.k0) * 3 / 4) : sg.k1; }
 template <int TN, bool MN>
 __global__ void __maxnreg__(80)                       // (a block of adapter_rank_kernel has registers beside it)
 adapter_stream_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ CUtensorMap tmF,
                       const __grid_constant__ FewParams p) {
   constexpr int kStage = stage_bytes(TN), kCols = TN < 32 ? 32 : TN, kMine = TN == 64 ? 32 : 16;      // columns of a warp
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], landed[kMaxStages], built[kMaxStages], tfull[2], tempty[2];
+  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], free_[kMaxStages], landed[kMaxStages], built[kMaxStages], tfull[2], tempty[2];
   __shared__ uint64_t looked[2], taken[2];           // whether factors of a tile were not finite is known; read
-  __shared__ uint32_t tmem_slot, abort_word, odd[2][kBuild];
+  __shared__ uint32_t tmem_slot, abort_word, odd[2][kClean];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   volatile uint32_t* abort_flag = &abort_word;
   const int warp = warp_index(), lane = threadIdx.x & 31, cta = blockIdx.x, ctas = gridDim.x;
@@ -669,8 +698,8 @@ adapter_stream_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
   const int per = units_of(p.term);
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
-    for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&landed[i], 1); mbar_init(&built[i], kBuild); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], kEpi); mbar_init(&looked[i], kBuild); mbar_init(&taken[i], kEpi); }
+    for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&landed[i], 1); mbar_init(&built[i], kBuild); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], kEpi); mbar_init(&looked[i], kClean); mbar_init(&taken[i], kEpi); }
     abort_word = 0;
     fence_barrier_init();
     prefetch_tmap(&tmA); prefetch_tmap(&tmZ); prefetch_tmap(&tmF);
@@ -707,7 +736,7 @@ adapter_stream_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
       for (int g0 = 0, known = known0; g0 < units && ok; g0 += kUnits, next()) {
         if (g0 && (g0 & 31) == 0) known = unit_adapter(p.term.lists, g0 + lane, units, per);
         ok = mbar_wait_warp(&empty[s], ph ^ 1, abort_flag);
-        if (ok) few_load_units(smem + s * kStage, &landed[s], tmF, known, g0, min(kUnits, units - g0), per, m0);
+        if (ok) few_load_units(smem + s * kStage, &landed[s], &free_[s], tmF, known, g0, min(kUnits, units - g0), per, p.term.boxed, m0);
       }
       load(mid, sg.k1);
     }
@@ -764,7 +793,7 @@ adapter_stream_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
       tc_fence_after();
       uint32_t any = 0;
 #pragma unroll
-      for (int w = 0; w < kBuild; ++w) any |= odd[a][w];
+      for (int w = 0; w < kClean; ++w) any |= odd[a][w];
       const bool mine = t0 < TN;
       float v[kMine];
       if (mine) {
@@ -820,35 +849,39 @@ adapter_stream_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_cons
     }
   } else {
     pdl_wait();
-    const int w = warp - 2 - kEpi, t = w * 32 + lane;                  // this thread's sample, and share of the factors
-    const int units = p.term.lists[0] * per, at = t < p.n ? p.term.place[t] * per : -1;
+    const bool writes = warp < 2 + kEpi + kWrite;
+    const int w = warp - 2 - kEpi - (writes ? 0 : kWrite), t = w * 32 + lane;        // this thread's sample, or share of the factors
+    const int units = p.term.lists[0] * per, at = writes && t < p.n ? p.term.place[t] * per : -1;
     const uint4* src = p.term.pb + t * per;
-    uint32_t g = 0, lph = 0;                         // k-blocks so far; the phases of landed, a bit per stage
+    uint32_t g = 0, ph = 0;                          // k-blocks so far; the phases of free_, or of landed, a bit per stage
+    uint4 words[kUnits];
+    if (writes) read_units(src, at, 0, min(kUnits, units), per, words);
     bool ok = true;
     for (int i = 0; i < segs.n && ok; ++i) {
       const Segment sg = segs.get(i);
       const int mid = term_at(sg, p.kseg);
       const uint32_t a = i & 1, aph = (i >> 1) & 1;
-      if (!mbar_wait_warp(&taken[a], aph ^ 1, abort_flag)) break;
+      if (!writes && !mbar_wait_warp(&taken[a], aph ^ 1, abort_flag)) break;
       uint32_t bad = 0;
       g += mid - sg.k0;
       for (int g0 = 0; g0 < units && sg.k1 == p.kseg; g0 += kUnits, ++g) {
         const uint32_t s = g % p.stages;
         const int nu = min(kUnits, units - g0);
-        uint4 words[kUnits];
-        read_units(src, at, g0, nu, per, words);
-        ok = mbar_wait_warp(&landed[s], (lph >> s) & 1, abort_flag);
+        ok = mbar_wait_warp(writes ? &free_[s] : &landed[s], (ph >> s) & 1, abort_flag);
         if (!ok) break;
-        lph ^= 1u << s;
-        write_units<32 * kBuild>(words, smem + s * kStage, t, t < TN, nu);
-        bad |= clean_units<32 * kBuild>(smem + s * kStage, t, nu);
-        fence_proxy_async_smem();
+        ph ^= 1u << s;
+        uint32_t wrote = 1;
+        if (writes) write_units<32 * kWrite>(words, smem + s * kStage, t, t < TN, nu);
+        else bad |= wrote = clean_units<32 * kClean>(smem + s * kStage, t, nu);
+        if (wrote) fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&built[s]);
+        const int next = g0 + kUnits < units ? g0 + kUnits : 0;        // (the next tile begins again)
+        if (writes) read_units(src, at, next, min(kUnits, units - next), per, words);
       }
       g += sg.k1 - mid;
       bad = __any_sync(0xffffffffu, bad);
-      if (lane == 0) {
+      if (!writes && lane == 0) {
         odd[a][w] = bad;
         mbar_arrive(&looked[a]);
       }
@@ -1000,7 +1033,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
           if (rank == 0) mbar_expect_tx(&full[s], 2 * nu * 2 * kUnit * 128);
         }
         const uint32_t bar = mapa_u32(smem_u32(&full[s]), 0);
-        for (int j = 0; j < nu; ++j) {
+        for (int j = 0; j < nu; j += p.term.boxed) {
           const int a = __shfl_sync(0xffffffffu, known, (g0 + j) & 31), y = (g0 + j) % per * kUnit;
           if (elect_one()) {
             tma_load_3d_pair(st + j * (kUnit * 128), &tmF, m0, y, a, bar);
@@ -1725,7 +1758,8 @@ struct sfb_adapters {
   uint32_t calls;                      // products with factors so far: what such a call marks its adapters with (a replayed one with the same
                                        // number each time, so that it may look at adapters of earlier replays too)
   CUtensorMap mapU, mapV;              // boxes of 64 entries x 16 ranks of an adapter
-  CUtensorMap unitU, unitV;            // x 8 ranks
+  CUtensorMap unitU, unitV;            // x `boxed` units of 8 ranks
+  int32_t boxed;
   sfb::EncodeTiledFn encode;           // cuTensorMapEncodeTiled
 
   template <typename T>
@@ -1829,7 +1863,7 @@ int few_parts(int64_t tiles, int64_t kseg) {
 template <bool MN>
 Term term_of(const sfb_adapters* h, const int32_t* ids, const float* p, bool bad) {
   const sfb_adapter_config& c = h->cfg;
-  return Term{c.rank, c.adapters, ids, h->at<int32_t>(h->lay.lists), h->at<int32_t>(h->lay.place), h->scale, bad ? h->at<uint4>(h->lay.bad) : nullptr,
+  return Term{c.rank, c.adapters, h->boxed, ids, h->at<int32_t>(h->lay.lists), h->at<int32_t>(h->lay.place), h->scale, bad ? h->at<uint4>(h->lay.bad) : nullptr,
               static_cast<const __nv_bfloat16*>(MN ? h->V : h->U), MN ? c.ldv : c.ldu, p, h->at<uint4>(h->lay.pb)};
 }
 
@@ -1986,8 +2020,10 @@ extern "C" int sfb_adapter_init(const sfb_adapter_config* cfg, const void* W_dev
   h->device = dev;
   h->last_cuda = 0;
   h->max_pairs = std::min(sm_count(), kModelSms) / 2;
+  h->boxed = 1;
+  while (h->boxed < kUnits && (c.rank + kUnit - 1) / kUnit % (2 * h->boxed) == 0) h->boxed *= 2;
   if (!factor_map(h, &h->mapU, U_dev, c.rows, c.ldu, kSlice) || !factor_map(h, &h->mapV, V_dev, c.cols, c.ldv, kSlice) ||
-      !factor_map(h, &h->unitU, U_dev, c.rows, c.ldu, kUnit) || !factor_map(h, &h->unitV, V_dev, c.cols, c.ldv, kUnit) ||
+      !factor_map(h, &h->unitU, U_dev, c.rows, c.ldu, kUnit * h->boxed) || !factor_map(h, &h->unitV, V_dev, c.cols, c.ldv, kUnit * h->boxed) ||
       prepare_pair_kernel(adapter_pair_kernel<false>, kPairThreads, kPairSmem, &h->max_pairs) != cudaSuccess ||
       prepare_pair_kernel(adapter_pair_kernel<true>, kPairThreads, kPairSmem, &h->max_pairs) != cudaSuccess || h->max_pairs < 1 ||
       cudaMemsetAsync(h->ws + lay.status, 0, lay.s - lay.status, h->stream) != cudaSuccess) {
