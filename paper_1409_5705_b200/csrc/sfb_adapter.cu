@@ -1,8 +1,8 @@
 // Low-rank adapters of many requests beside the shared W (sfb_adapter_* in sfb.h): the logits of samples, each with the adapter
 // (a set of factor pairs) that its request names, and the gradients of the samples and of the adapters' factors.
 //
-// Launches of a forward pass:  adapter_rank_kernel (s = V x), then for y = W x + scale U^T s up to 64 samples adapter_few_kernel or
-// adapter_stream_kernel, for more adapter_sum_kernel and adapter_pair_kernel;  of a backward pass:  adapter_index_kernel, adapter_rank_kernel (t = U dy; s again
+// Launches of a forward pass:  adapter_rank_kernel (s = V x), then for y = W x + scale U^T s up to 64 samples adapter_few_kernel, for
+// more adapter_sum_kernel and adapter_pair_kernel;  of a backward pass:  adapter_index_kernel, adapter_rank_kernel (t = U dy; s again
 // where it is not given), the products as in a forward pass (dx), adapter_words_kernel and adapter_gradient_kernel (dU, dV).
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -28,7 +28,7 @@ constexpr int kMaxStages = 8;
 constexpr int kDrain = 12;
 constexpr int kListPitch = kMaxTile + 8;            // entries of a tile's list: their number, then the adapters
 constexpr int kSmallRing = 98304;                   // bytes of operand stages where two blocks share an SM,
-constexpr int kFewRing = 73728;                     // and of a block of adapter_rank_kernel beside one of adapter_stream_kernel
+constexpr int kFewRing = 73728;                     // of adapter_rank_kernel beside one of adapter_few_kernel
 
 __host__ __device__ constexpr int stage_bytes(int tn) { return kTileBytesA + tn * BK * 2; }
 
@@ -457,11 +457,11 @@ __device__ __forceinline__ void read_units(const uint4* src, int at, int g0, int
 
 // ---------------------------------------------------------------------------------------------------------
 // y_i = A z_i + scale F[a_i]^T p_i for up to 64 samples: the rows of A (rows of W; with MN, of its transpose: columns of W) are the rows
-// of the accumulator, 128 of them a tile.  Bound by the way of W to the SMs.  The loads of A and z do not wait for the launches before
-// (adapter_rank_kernel lets the next one start once those before it are done).
-//
-// adapter_few_kernel, for few tiles: a tile a cluster, whose CTAs share the contraction and the k-blocks of the term; the parts are added
-// in rank order, each CTA finishing some of the samples.  Two CTAs an SM.
+// of the accumulator, 128 of them a tile.  Bound by the way of W to the SMs: two CTAs an SM, up to 192 KB of loads under way on it.  A tile
+// a cluster, whose CTAs share the contraction and the k-blocks of the term; the parts are added in rank order, each CTA finishing some of
+// the samples.  The loads of A and z do not wait for the launch before (adapter_rank_kernel lets this one start once those before it are
+// done).  325,000 x 10,000 with 64 samples: 961 us, 6.9 TB/s.  (A CTA an SM that takes its even share of all tiles, with parts through
+// global memory: 1,030; 10,000 x 20,000 with 37 samples of 64 adapters 84, here 77.)
 // Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..5 epilogue, 6 and 7 the samples' operand of the term, 8 and 9
 // its factors.
 // ---------------------------------------------------------------------------------------------------------
@@ -474,9 +474,6 @@ struct FewParams {
   int32_t kseg, stages, parts; // k-blocks; operand stages; CTAs of a cluster
   __nv_bfloat16* Y;
   int64_t ldy;
-  int32_t tiles, cut, whole;   // adapter_stream_kernel: tiles of 128 rows; see Segments
-  float* partial;              // [CTAs][64][128 rows]
-  uint32_t* ready;             // [CTAs][kEpi]
   uint32_t* status;
 };
 
@@ -670,232 +667,6 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     __syncthreads();
   }
   if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem_base, kCols); }
-}
-
-// ---------------------------------------------------------------------------------------------------------
-// adapter_stream_kernel, for more tiles: a CTA an SM takes its even share of all k-blocks of A, whole tiles first (Segments in
-// sfb_tile.cuh), so that every SM streams as much of W as the others from the start to the end; the CTA that finishes a tile has its term,
-// behind three quarters of its k-blocks, where p should be there and nothing waits for it.  Two accumulators: the end of a tile runs beside the next one's products.
-// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the samples), 10 and 11 the samples'
-// operand of the term, 12 and 13 its factors.
-// ---------------------------------------------------------------------------------------------------------
-constexpr int kStreamThreads = 32 * (2 + kEpi + kBuild), kStreamRing = 143360;
-// The k-block ahead of which a segment has its tile's term (behind the first one, which clears the accumulator); its end where it has none.
-__device__ __forceinline__ int term_at(const Segment& sg, int kseg) { return sg.k1 == kseg ? sg.k0 + max(1, (sg.k1 - sg.k0) * 3 / 4) : sg.k1; }
-template <int TN, bool MN>
-__global__ void __maxnreg__(80)                       // (a block of adapter_rank_kernel has registers beside it)
-adapter_stream_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ CUtensorMap tmF,
-                      const __grid_constant__ FewParams p) {
-  constexpr int kStage = stage_bytes(TN), kCols = TN < 32 ? 32 : TN, kMine = TN == 64 ? 32 : 16;      // columns of a warp
-  extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], free_[kMaxStages], landed[kMaxStages], built[kMaxStages], tfull[2], tempty[2];
-  __shared__ uint64_t looked[2], taken[2];           // whether factors of a tile were not finite is known; read
-  __shared__ uint32_t tmem_slot, abort_word, odd[2][kClean];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  volatile uint32_t* abort_flag = &abort_word;
-  const int warp = warp_index(), lane = threadIdx.x & 31, cta = blockIdx.x, ctas = gridDim.x;
-  const Segments segs(p.kseg, p.cut != 0, p.whole, p.tiles, cta, ctas);
-  const int per = units_of(p.term);
-  pdl_launch_dependents();
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&landed[i], 1); mbar_init(&built[i], kBuild); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], kEpi); mbar_init(&looked[i], kClean); mbar_init(&taken[i], kEpi); }
-    abort_word = 0;
-    fence_barrier_init();
-    prefetch_tmap(&tmA); prefetch_tmap(&tmZ); prefetch_tmap(&tmF);
-  }
-  if (warp == 1) { tmem_alloc(&tmem_slot, 2 * kCols); tmem_relinquish(); }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem_base = tmem_slot;
-
-  if (warp == 0) {
-    const uint64_t keep = policy_evict_last();
-    uint32_t s = 0, ph = 0;
-    bool ok = true;
-    auto next = [&]() { if (++s == static_cast<uint32_t>(p.stages)) { s = 0; ph ^= 1; } };
-    int units = -1, known0 = 0;                      // the first 32 units' adapters: the same for every tile
-    for (int i = 0; i < segs.n && ok; ++i) {
-      const Segment sg = segs.get(i);
-      const int m0 = sg.tile * BM;
-      auto load = [&](int k0, int k1) {
-        for (int k = k0; k < k1 && ok; ++k, next()) {
-          ok = mbar_wait_warp(&empty[s], ph ^ 1, abort_flag);
-          if (ok) few_load<TN, MN>(smem + s * kStage, &full[s], tmA, tmZ, k, m0, keep);
-        }
-      };
-      const int mid = term_at(sg, p.kseg);
-      load(sg.k0, mid);
-      if (sg.k1 < p.kseg) continue;
-      if (units < 0) {
-        pdl_wait();
-        units = p.term.lists[0] * per;
-        known0 = unit_adapter(p.term.lists, lane, units, per);
-      }
-      for (int g0 = 0, known = known0; g0 < units && ok; g0 += kUnits, next()) {
-        if (g0 && (g0 & 31) == 0) known = unit_adapter(p.term.lists, g0 + lane, units, per);
-        ok = mbar_wait_warp(&empty[s], ph ^ 1, abort_flag);
-        if (ok) few_load_units(smem + s * kStage, &landed[s], &free_[s], tmF, known, g0, min(kUnits, units - g0), per, p.term.boxed, m0);
-      }
-      load(mid, sg.k1);
-    }
-  } else if (warp == 1) {
-    const uint32_t idesc_f = umma_idesc_bf16(BM, TN) | 1u << 15, idesc = MN ? idesc_f : umma_idesc_bf16(BM, TN);
-    uint32_t s = 0, fph = 0, bph = 0;                // the phases of full and of built, a bit per stage
-    bool ok = true;
-    auto next = [&]() { if (++s == static_cast<uint32_t>(p.stages)) s = 0; };
-    int units = -1;
-    for (int i = 0; i < segs.n && ok; ++i) {
-      const Segment sg = segs.get(i);
-      const uint32_t a = i & 1, aph = (i >> 1) & 1, d_tmem = tmem_base + a * kCols;
-      if (!mbar_wait_warp(&tempty[a], aph ^ 1, abort_flag)) break;
-      tc_fence_after();
-      auto mma = [&](int k0, int k1) {
-        for (int k = k0; k < k1 && ok; ++k, next()) {
-          ok = mbar_wait_warp(&full[s], (fph >> s) & 1, abort_flag);
-          fph ^= 1u << s;
-          tc_fence_after();
-          if (ok && elect_one()) {
-            few_mma<MN>(smem_u32(smem + s * kStage), d_tmem, idesc, k == sg.k0);
-            umma_commit(&empty[s]);
-          }
-        }
-      };
-      const int mid = term_at(sg, p.kseg);
-      mma(sg.k0, mid);
-      if (sg.k1 == p.kseg) {
-        if (units < 0) {
-          pdl_wait();
-          units = p.term.lists[0] * per;
-        }
-        for (int g0 = 0; g0 < units && ok; g0 += kUnits, next()) {
-          ok = mbar_wait_warp(&built[s], (bph >> s) & 1, abort_flag);
-          bph ^= 1u << s;
-          tc_fence_after();
-          if (ok && elect_one()) {
-            few_mma_units(smem_u32(smem + s * kStage), d_tmem, idesc_f, min(kUnits, units - g0));
-            umma_commit(&empty[s]);
-          }
-        }
-        mma(mid, sg.k1);
-      }
-      if (ok && elect_one()) umma_commit(&tfull[a]);
-    }
-  } else if (warp < 2 + kEpi) {
-    const int w8 = warp - 2, q = warp & 3, h = w8 >> 2, t0 = h * kMine;
-    pdl_wait();
-    for (int i = 0; i < segs.n; ++i) {
-      const Segment sg = segs.get(i);
-      const int m = sg.tile * BM + q * 32 + lane;
-      const uint32_t a = i & 1, aph = (i >> 1) & 1;
-      if (!mbar_wait_warp(&tfull[a], aph, abort_flag) || !mbar_wait_warp(&looked[a], aph, abort_flag)) break;
-      tc_fence_after();
-      uint32_t any = 0;
-#pragma unroll
-      for (int w = 0; w < kClean; ++w) any |= odd[a][w];
-      const bool mine = t0 < TN;
-      float v[kMine];
-      if (mine) {
-        uint32_t acc[kMine];
-        const uint32_t at = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + a * kCols + t0;
-        if constexpr (kMine == 32) tmem_ld_32x32(at, acc);
-        else tmem_ld_32x16(at, acc);
-        tmem_ld_wait();
-#pragma unroll
-        for (int j = 0; j < kMine; ++j) v[j] = __uint_as_float(acc[j]);
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) { mbar_arrive(&tempty[a]); mbar_arrive(&taken[a]); }
-      if (!mine) continue;
-      const int64_t to = static_cast<int64_t>(t0) * BM + q * 32 + lane;     // of a CTA's part: [sample][128 rows]
-      if (sg.k1 < p.kseg) {
-        float* part = p.partial + static_cast<int64_t>(cta) * kFewMost * BM + to;
-#pragma unroll
-        for (int j = 0; j < kMine; ++j) __stcg(part + j * BM, v[j]);
-        __syncwarp();
-        if (lane == 0) {
-          __threadfence();
-          st_release(p.ready + cta * kEpi + w8, 1u);
-        }
-        continue;
-      }
-      const int from = segs.first_part(sg);
-      bool ok = true;
-      for (int c = from; c < cta && ok; ++c) ok = __all_sync(0xffffffffu, lane != 0 || flag_wait(p.ready + c * kEpi + w8, abort_flag));
-      if (!ok) break;
-      if (lane == 0)
-        for (int c = from; c < cta; ++c) p.ready[c * kEpi + w8] = 0;        // for the next launch
-      __syncwarp();
-      for (int c = from; c < cta; ++c) {
-        const float* part = p.partial + static_cast<int64_t>(c) * kFewMost * BM + to;
-#pragma unroll
-        for (int j0 = 0; j0 < kMine; j0 += 16) {
-          float x[16];
-#pragma unroll
-          for (int j = 0; j < 16; ++j) x[j] = __ldcg(part + (j0 + j) * BM);
-#pragma unroll
-          for (int j = 0; j < 16; ++j) v[j0 + j] += x[j];
-        }
-      }
-      if (any && m < p.m) {
-#pragma unroll
-        for (int j = 0; j < kMine; ++j)
-          if (t0 + j < p.n) v[j] += bad_term(p.term, t0 + j, m);
-      }
-#pragma unroll
-      for (int j = 0; j < kMine; j += 2) store_two(p.Y, p.ldy, t0 + j, p.n, m, p.m, v[j], v[j + 1], lane);
-    }
-  } else {
-    pdl_wait();
-    const bool writes = warp < 2 + kEpi + kWrite;
-    const int w = warp - 2 - kEpi - (writes ? 0 : kWrite), t = w * 32 + lane;        // this thread's sample, or share of the factors
-    const int units = p.term.lists[0] * per, at = writes && t < p.n ? p.term.place[t] * per : -1;
-    const uint4* src = p.term.pb + t * per;
-    uint32_t g = 0, ph = 0;                          // k-blocks so far; the phases of free_, or of landed, a bit per stage
-    uint4 words[kUnits];
-    if (writes) read_units(src, at, 0, min(kUnits, units), per, words);
-    bool ok = true;
-    for (int i = 0; i < segs.n && ok; ++i) {
-      const Segment sg = segs.get(i);
-      const int mid = term_at(sg, p.kseg);
-      const uint32_t a = i & 1, aph = (i >> 1) & 1;
-      if (!writes && !mbar_wait_warp(&taken[a], aph ^ 1, abort_flag)) break;
-      uint32_t bad = 0;
-      g += mid - sg.k0;
-      for (int g0 = 0; g0 < units && sg.k1 == p.kseg; g0 += kUnits, ++g) {
-        const uint32_t s = g % p.stages;
-        const int nu = min(kUnits, units - g0);
-        ok = mbar_wait_warp(writes ? &free_[s] : &landed[s], (ph >> s) & 1, abort_flag);
-        if (!ok) break;
-        ph ^= 1u << s;
-        uint32_t wrote = 1;
-        if (writes) write_units<32 * kWrite>(words, smem + s * kStage, t, t < TN, nu);
-        else bad |= wrote = clean_units<32 * kClean>(smem + s * kStage, t, nu);
-        if (wrote) fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&built[s]);
-        const int next = g0 + kUnits < units ? g0 + kUnits : 0;        // (the next tile begins again)
-        if (writes) read_units(src, at, next, min(kUnits, units - next), per, words);
-      }
-      g += sg.k1 - mid;
-      bad = __any_sync(0xffffffffu, bad);
-      if (!writes && lane == 0) {
-        odd[a][w] = bad;
-        mbar_arrive(&looked[a]);
-      }
-    }
-  }
-  __syncwarp();
-  tc_fence_before();
-  __syncthreads();
-  if (abort_word) {
-    if (threadIdx.x == 0) atomicOr(p.status, SFB_STATUS_TIMEOUT);
-    for (int i = 0; i < 64; ++i) __nanosleep(1000);
-    __syncthreads();
-  }
-  if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem_base, 2 * kCols); }
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -1733,7 +1504,7 @@ AdapterLayout layout_of(const sfb_adapter_config& c) {
   L.twords = take(n * 3 * rp * 2);
   L.lists = take((n / kMaxTile + 1) * kListPitch * 4);
   L.place = take(n * 4);
-  L.partial = take(static_cast<size_t>(kModelSms) * (n > kFewMost ? kPartFloats : kFewMost * BM) * 4);
+  L.partial = take(n > kFewMost ? static_cast<size_t>(kModelSms) * kPartFloats * 4 : 0);
   L.order = take(n * 4);
   L.begin = take(static_cast<size_t>(c.adapters) * 4);
   L.work = take((static_cast<size_t>(c.adapters) + 1) * 8);
@@ -1850,12 +1621,13 @@ cudaError_t rank_products(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz
   return launch_kernel(adapter_rank_kernel<false>, dim3(parts, tiles, groups), dim3(kRankThreads), smem, h->stream, 1, mf, mz, p);
 }
 
-constexpr int64_t kClusterTiles = 2 * kModelSms / kMaxCluster;      // tiles up to which eight CTAs share each
-// CTAs of a cluster of adapter_few_kernel: as many as leave all of them a place, two an SM, and each four k-blocks.
+// CTAs of a cluster of adapter_few_kernel, each with four k-blocks at least: up to four as long as nine tenths of the places, two an SM,
+// hold them all, more only where every CTA has an SM of its own.  (us with one sample: 10,000 x 20,000, 79 tiles, 1 CTA 75, 3 CTAs 64; 5,000 x
+// 10,000, 40 tiles, 3 CTAs 22.6, 6 CTAs 25.5; 18,944 x 10,000, 148 tiles, 1 CTA 61, 2 CTAs 65.)
 int few_parts(int64_t tiles, int64_t kseg) {
   int best = 1;
   for (int s = 2; s <= kMaxCluster; ++s)
-    if (tiles * s <= 2 * kModelSms && kseg >= 4 * s) best = s;
+    if (tiles * s <= (s <= 4 ? 2 * kModelSms * 9 / 10 : kModelSms) && kseg >= 4 * s) best = s;
   return best;
 }
 
@@ -1882,25 +1654,12 @@ cudaError_t few(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const Te
   p.kseg = static_cast<int32_t>((d + BK - 1) / BK);
   p.Y = static_cast<__nv_bfloat16*>(Y); p.ldy = ldy; p.status = h->at<uint32_t>(h->lay.status);
   const int64_t tiles = (m + BM - 1) / BM;
-  if (tiles <= kClusterTiles) {
-    p.parts = few_parts(tiles, p.kseg);
-    p.stages = std::min(kMaxStages, kSmallRing / stage_bytes(TN));
-    const cudaError_t e = allow_beside<adapter_few_kernel<TN, MN>>(kSmallRing + 1024);
-    if (e != cudaSuccess) return e;
-    return launch_kernel(adapter_few_kernel<TN, MN>, dim3(static_cast<unsigned>(tiles * p.parts)), dim3(kFewThreads), p.stages * stage_bytes(TN) + 1024,
-                         h->stream, p.parts, ma, mz, mf, p);
-  }
-  // every CTA has k-blocks of the tiles that are shared out: at least a tile's worth, or four where there are fewer tiles than SMs
-  const int64_t sms = std::min(sm_count(), kModelSms), ctas = tiles >= sms ? sms : std::max<int64_t>(1, std::min(sms, tiles * p.kseg / 4));
-  p.tiles = static_cast<int32_t>(tiles);
-  p.cut = tiles % ctas != 0;
-  p.whole = p.cut ? static_cast<int32_t>(std::max<int64_t>(0, tiles / ctas - 1) * ctas) : 0;
-  p.stages = std::min(kMaxStages, kStreamRing / stage_bytes(TN));
-  p.partial = h->at<float>(h->lay.partial); p.ready = h->at<uint32_t>(h->lay.ready);
-  const cudaError_t e = allow_beside<adapter_stream_kernel<TN, MN>>(kStreamRing + 1024);
+  p.parts = few_parts(tiles, p.kseg);
+  p.stages = std::min(kMaxStages, kSmallRing / stage_bytes(TN));
+  const cudaError_t e = allow_beside<adapter_few_kernel<TN, MN>>(kSmallRing + 1024);
   if (e != cudaSuccess) return e;
-  return launch_kernel(adapter_stream_kernel<TN, MN>, dim3(static_cast<unsigned>(ctas)), dim3(kStreamThreads), p.stages * stage_bytes(TN) + 1024, h->stream, 1,
-                       ma, mz, mf, p);
+  return launch_kernel(adapter_few_kernel<TN, MN>, dim3(static_cast<unsigned>(tiles * p.parts)), dim3(kFewThreads), p.stages * stage_bytes(TN) + 1024,
+                       h->stream, p.parts, ma, mz, mf, p);
 }
 
 // Cycles of a plan of adapter_pair_kernel: its k-blocks on a pair, 7,000 to start and to end, 9,000 and 2,000 a part to leave and to take
