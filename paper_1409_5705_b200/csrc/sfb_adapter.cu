@@ -129,8 +129,6 @@ struct RankParams {
   int32_t rank, adapters;
   const int32_t* ids;
   float* out;                  // [parts][n][rank]
-  int32_t* mark;               // for each adapter in use, `call` (not FEW)
-  int32_t call;
   uint32_t* status;
   // FEW
   const float* scale;
@@ -193,8 +191,6 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
         if (r < p.rank && L.place[t] < 0) p.p[t * p.rank + r] = 0.f;
       }
     }
-  } else if (blockIdx.x == 0 && blockIdx.z == 0) {
-    for (int t = threadIdx.x; t < L.count; t += kRankThreads) p.mark[L.list[t]] = p.call;
   }
 
   if (warp == 0) {
@@ -328,27 +324,40 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
 }
 
 constexpr int kEpi = 8;                             // epilogue warps of the products
-// x, y: row m (this lane's) of samples i and i + 1.  Even lanes store two rows of the first sample, odd lanes of the second.  By a warp.
-__device__ __forceinline__ void store_two(__nv_bfloat16* Y, int64_t ldy, int i, int n, int m, int most, float x, float y, int lane) {
+// acc: row m (this lane's) of the samples i .. i + 31.  Even lanes store two rows of every other sample, odd lanes of the ones between; by a
+// warp, whose rows begin at m - lane.  (First all exchanges, then all stores, without a branch where the chunk is whole: with one behind each
+// exchange a tile's end took 6.5 us.)
+__device__ __forceinline__ void store_chunk(__nv_bfloat16* Y, int64_t ldy, int i, int n, int m, int most, const uint32_t (&acc)[32], int lane) {
   const bool second = lane & 1;
-  const float got = __shfl_xor_sync(0xffffffffu, second ? x : y, 1);
+  uint32_t two[16];
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    const float x = __uint_as_float(acc[2 * j]), y = __uint_as_float(acc[2 * j + 1]);
+    const float got = __shfl_xor_sync(0xffffffffu, second ? x : y, 1);
+    const __nv_bfloat162 v = __floats2bfloat162_rn(second ? got : x, second ? y : got);
+    two[j] = *reinterpret_cast<const uint32_t*>(&v);
+  }
   const int at = i + (second ? 1 : 0), r = m & ~1;
-  if (at < n) {
-    __nv_bfloat16* to = Y + static_cast<int64_t>(at) * ldy + r;
-    const float lo = second ? got : x, hi = second ? y : got;
-    if (r + 1 < most) *reinterpret_cast<__nv_bfloat162*>(to) = __floats2bfloat162_rn(lo, hi);
-    else if (r < most) *to = __float2bfloat16_rn(lo);
+  __nv_bfloat16* to = Y + static_cast<int64_t>(at) * ldy + r;
+  if (i + 32 <= n && m - lane + 32 <= most) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) *reinterpret_cast<uint32_t*>(to + 2 * j * ldy) = two[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      if (at + 2 * j >= n || r >= most) continue;
+      if (r + 1 < most) *reinterpret_cast<uint32_t*>(to + 2 * j * ldy) = two[j];
+      else *reinterpret_cast<uint16_t*>(to + 2 * j * ldy) = static_cast<uint16_t>(two[j] & 0xffffu);
+    }
   }
 }
 
 // ---------------------------------------------------------------------------------------------------------
 // The adapters' term, scale F[a_i]^T p_i, of the three products below is more contraction behind the k-blocks of A: the factors of the
 // adapters in the tile's list, eight units of 8 ranks a k-block, against  scale p  of the samples in bf16 (one rounding, 2^-8 of the term;
-// the result is rounded by as much), with zeros where a sample has another adapter.  Zeros do not hide what is not finite.  Up to 64
-// samples, where a factor is read once, the warps that write the samples' operand look through the factors in shared memory, replace what
-// is not finite by zeros, and the end of the tile adds those entries alone to their own samples, in fp32.  For more samples
-// adapter_sum_kernel has looked through the factors, and an adapter that holds such entries is not loaded (its units are out of the map's
-// bounds, zeros): the end of the tile forms the whole term of its samples in fp32.
+// the result is rounded by as much), with zeros where a sample has another adapter.  Zeros do not hide what is not finite: some warps look
+// through the factors in shared memory and replace what is not finite by zeros, and the end of the tile adds those entries alone to their
+// own samples, in fp32.
 // (In fp32 FMAs from global memory, as it was for up to 64 samples, a tile's term is a chain of loads: 64 samples of 8 ranks took 99 us a
 // tile of 325,000 x 10,000, whose rows of W stream by in 57.)
 // ---------------------------------------------------------------------------------------------------------
@@ -357,33 +366,25 @@ struct Term {
   int32_t boxed;               // units that one copy of factors brings: a power of two that divides those of an adapter
   const int32_t *ids, *lists, *place;
   const float* scale;
-  const uint4* bad;            // [adapters]: not zero where the factors are not finite (null up to 64 samples)
   const __nv_bfloat16* F;      // [adapters][rank][ldf]
   int64_t ldf;
   const float* p;              // [n][rank]
   const uint4* pb;             // [n][units of an adapter]: scale p in bf16, zeros behind
 };
 __device__ __forceinline__ int units_of(const Term& t) { return (t.rank + kUnit - 1) / kUnit; }
-__device__ __forceinline__ bool is_bad(const uint4& b) { return (b.x | b.y | b.z | b.w) != 0; }
-// What the tensor cores have left out of the term of sample i at row m.
-__device__ __noinline__ float bad_term(const Term& p, int i, int m) {
+// What the tensor cores have left out of the term of sample i at row m: the factors that are not finite.
+__device__ __noinline__ float odd_term(const Term& p, int i, int m) {
   const int id = p.ids[i];
-  if (id < 0 || id >= p.adapters || (p.bad && !is_bad(p.bad[id]))) return 0.f;
+  if (id < 0 || id >= p.adapters) return 0.f;
   const __nv_bfloat16* f = p.F + static_cast<int64_t>(id) * p.rank * p.ldf + m;
   const float* s = p.p + static_cast<int64_t>(i) * p.rank;
   const float sc = p.scale[id];
   float v = 0.f;
   for (int r = 0; r < p.rank; ++r) {
     const float x = __bfloat162float(f[r * p.ldf]);
-    if (p.bad || !isfinite(x)) v = fmaf(x, sc * s[r], v);
+    if (!isfinite(x)) v = fmaf(x, sc * s[r], v);
   }
   return v;
-}
-// Whether some adapter in a list is bad; by a warp.
-__device__ __forceinline__ bool any_bad(const Term& p, const int32_t* list, int lane) {
-  bool any = false;
-  for (int x = lane; x < list[0]; x += 32) any |= is_bad(p.bad[list[1 + x]]);
-  return __any_sync(0xffffffffu, any);
 }
 // The adapter of unit g of `units`.
 __device__ __forceinline__ int unit_adapter(const int32_t* list, int g, int units, int per) {
@@ -649,8 +650,8 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         v = c ? make_float2(v.x + w.x, v.y + w.y) : w;
       }
       if (any) {
-        if (m < p.m) v.x += bad_term(p.term, t, m);
-        if (m + 1 < p.m) v.y += bad_term(p.term, t, m + 1);
+        if (m < p.m) v.x += odd_term(p.term, t, m);
+        if (m + 1 < p.m) v.y += odd_term(p.term, t, m + 1);
       }
       __nv_bfloat16* y = p.Y + t * p.ldy + m;
       if (m + 1 < p.m) *reinterpret_cast<__nv_bfloat162*>(y) = __floats2bfloat162_rn(v.x, v.y);
@@ -677,9 +678,9 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // The pair that finishes a tile has its term.
 //
 // Warps: 0 TMA producer, 1 MMA issuer (leader CTA) and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the columns), 10..13
-// the samples' operand of the adapters' term.
+// the samples' operand of the term, 14..17 its factors.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kPairThreads = 448, kGroup = 8;      // kGroup: tiles of samples that follow one another
+constexpr int kPairBuild = 4, kPairThreads = 32 * (2 + kEpi + 2 * kPairBuild), kGroup = 8;      // kGroup: tiles of samples that follow one another
 constexpr int kPairStages = 6, kPairStage = 2 * kTileBytesA;
 constexpr int kPairSmem = kPairStages * kPairStage + 1024;
 constexpr int kPartFloats = BM * kMaxTile;          // what a CTA leaves of a tile
@@ -721,8 +722,9 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   __shared__ uint64_t full[kPairStages], empty[kPairStages];       // full, built, tempty: the leader's are in use
   __shared__ uint64_t free_[kPairStages], built[kPairStages];      // of a k-block of factors: the stage is free for the samples' operand;
                                                                    // both CTAs have written it
-  __shared__ uint64_t tfull[2], tempty[2];
-  __shared__ uint32_t tmem_slot, abort_word;
+  __shared__ uint64_t landed[kPairStages];                         // its factors are here
+  __shared__ uint64_t tfull[2], tempty[2], looked[2], taken[2];    // looked: whether factors of a tile were not finite is known; taken: read
+  __shared__ uint32_t tmem_slot, abort_word, odd[2][kPairBuild];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   volatile uint32_t* abort_flag = &abort_word;
   const int warp = warp_index(), lane = threadIdx.x & 31;
@@ -740,9 +742,9 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kPairStages; ++i) {
-      mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&built[i], 2 * kBuild);
+      mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&landed[i], 1); mbar_init(&built[i], 4 * kPairBuild);
     }
-    for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 2 * kEpi); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 2 * kEpi); mbar_init(&looked[i], kPairBuild); mbar_init(&taken[i], kEpi); }
     abort_word = 0;
     fence_barrier_init();
     prefetch_tmap(&tmA); prefetch_tmap(&tmZ); prefetch_tmap(&tmF);
@@ -766,12 +768,10 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       int m0, tt;
       tile_coords(sg.tile, m0, tt);
       const int z0 = tt * p.tn + static_cast<int>(rank) * half;
-      // of four k-blocks of factors at a time the lanes hold the adapter of a unit, out of bounds where it is bad; what that needs is
-      // asked for ahead of the loads of A, one step before and one among them
+      // of four k-blocks of factors at a time the lanes hold the adapter of a unit, asked for ahead of the loads of A
       const int32_t* list = p.term.lists + static_cast<int64_t>(tt) * kListPitch;
       const int count = sg.k1 == p.kseg ? list[0] : 0;
       int known = list[1 + lane / per];
-      auto settled = [&](int g, int a) { return g < count * per ? is_bad(p.term.bad[a]) ? p.term.adapters : a : 0; };
       auto loads = [&](int k0, int k1) {
         for (int k = k0; k < k1; ++k) {
           if (!mbar_wait_warp(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
@@ -790,10 +790,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
           if (++s == static_cast<uint32_t>(kPairStages)) { s = 0; ph ^= 1; }
         }
       };
-      const int mid = min(sg.k0 + 4, sg.k1);
-      loads(sg.k0, mid);
-      known = settled(lane, known);
-      if (ok) loads(mid, sg.k1);
+      loads(sg.k0, sg.k1);
       const int units = count * per, more = (units + kUnits - 1) / kUnits;
       for (int k = 0; k < more && ok; ++k) {
         if (!mbar_wait_warp(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
@@ -801,20 +798,17 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         const int g0 = k * kUnits, nu = min(kUnits, units - g0);
         if (elect_one()) {
           mbar_arrive(&free_[s]);
-          if (rank == 0) mbar_expect_tx(&full[s], 2 * nu * 2 * kUnit * 128);
+          mbar_expect_tx(&landed[s], nu * 2 * kUnit * 128);
         }
-        const uint32_t bar = mapa_u32(smem_u32(&full[s]), 0);
+        __syncwarp();
         for (int j = 0; j < nu; j += p.term.boxed) {
           const int a = __shfl_sync(0xffffffffu, known, (g0 + j) & 31), y = (g0 + j) % per * kUnit;
           if (elect_one()) {
-            tma_load_3d_pair(st + j * (kUnit * 128), &tmF, m0, y, a, bar);
-            tma_load_3d_pair(st + kTileBytesA / 2 + j * (kUnit * 128), &tmF, m0 + 64, y, a, bar);
+            tma_load_3d(st + j * (kUnit * 128), &tmF, m0, y, a, &landed[s]);
+            tma_load_3d(st + kTileBytesA / 2 + j * (kUnit * 128), &tmF, m0 + 64, y, a, &landed[s]);
           }
         }
-        if (((g0 + kUnits) & 31) == 0 && g0 + kUnits < units) {
-          const int g = g0 + kUnits + lane;
-          known = settled(g, g < units ? list[1 + g / per] : 0);
-        }
+        if (((g0 + kUnits) & 31) == 0 && g0 + kUnits < units) known = unit_adapter(list, g0 + kUnits + lane, units, per);
         if (++s == static_cast<uint32_t>(kPairStages)) { s = 0; ph ^= 1; }
       }
     }
@@ -822,7 +816,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     // ---------------- MMA issuer ----------------
     if (rank == 0) {
       const uint32_t idesc = umma_idesc_bf16(2 * BM, p.tn) | (MN ? 1u << 15 : 0u), idesc_f = umma_idesc_bf16(2 * BM, p.tn) | 1u << 15;
-      uint32_t s = 0, ph = 0, bph = 0;               // bph: the phases of built, a bit per stage
+      uint32_t s = 0, fph = 0, bph = 0;              // the phases of full and of built, a bit per stage
       bool ok = true;
       for (int i = 0; i < segs.n && ok; ++i) {
         const Segment sg = segs.get(i);
@@ -833,7 +827,8 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         if (!mbar_wait_warp(&tempty[a], aph ^ 1, abort_flag)) { ok = false; break; }
         tc_fence_after();
         for (int k = sg.k0; k < sg.k1; ++k) {
-          if (!mbar_wait_warp(&full[s], ph, abort_flag)) { ok = false; break; }
+          if (!mbar_wait_warp(&full[s], (fph >> s) & 1, abort_flag)) { ok = false; break; }
+          fph ^= 1u << s;
           tc_fence_after();
           if (elect_one()) {
             const uint32_t st = smem_u32(smem + s * kPairStage);
@@ -842,10 +837,10 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             for (int j = 0; j < BK / 16; ++j) umma_bf16_pair(d_tmem, da + (MN ? 128 : 2) * j, db + 2 * j, idesc, (k - sg.k0) | j ? 1u : 0u);
             umma_commit_pair(&empty[s], 3);
           }
-          if (++s == static_cast<uint32_t>(kPairStages)) { s = 0; ph ^= 1; }
+          if (++s == static_cast<uint32_t>(kPairStages)) s = 0;
         }
         for (int left = count * per; left > 0 && ok; left -= kUnits) {
-          if (!mbar_wait_warp(&full[s], ph, abort_flag) || !mbar_wait_cluster(&built[s], (bph >> s) & 1, abort_flag)) { ok = false; break; }
+          if (!mbar_wait_cluster(&built[s], (bph >> s) & 1, abort_flag)) { ok = false; break; }
           bph ^= 1u << s;
           tc_fence_after();
           const int ns = (min(kUnits, left) + 1) / 2;                  // instructions: two units each
@@ -855,7 +850,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             for (int j = 0; j < ns; ++j) umma_bf16_pair(d_tmem, da + 128 * j, db + 2 * j, idesc_f, 1u);
             umma_commit_pair(&empty[s], 3);
           }
-          if (++s == static_cast<uint32_t>(kPairStages)) { s = 0; ph ^= 1; }
+          if (++s == static_cast<uint32_t>(kPairStages)) s = 0;
         }
         if (ok && elect_one()) umma_commit_pair(&tfull[a], 3);
       }
@@ -870,10 +865,13 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       int m0, tt;
       tile_coords(sg.tile, m0, tt);
       const uint32_t a = i & 1, aph = (i >> 1) & 1;
-      const int32_t* list = p.term.lists + static_cast<int64_t>(tt) * kListPitch;
-      const bool any = sg.k1 == p.kseg && any_bad(p.term, list, lane);
-      if (!mbar_wait_warp(&tfull[a], aph, abort_flag)) { ok = false; break; }
+      if (!mbar_wait_warp(&tfull[a], aph, abort_flag) || !mbar_wait_warp(&looked[a], aph, abort_flag)) { ok = false; break; }
       tc_fence_after();
+      uint32_t any = 0;
+#pragma unroll
+      for (int w = 0; w < kPairBuild; ++w) any |= odd[a][w];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&taken[a]);
       const uint32_t t_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + a * kMaxTile + h * cols;
       const bool leave = sg.k1 < p.kseg;
       const int from = leave ? pair : segs.first_part(sg);
@@ -915,11 +913,9 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         if (any && m < p.m) {
 #pragma unroll
           for (int j = 0; j < 32; ++j)
-            if (i0 + j < p.n) acc[j] = __float_as_uint(__uint_as_float(acc[j]) + bad_term(p.term, i0 + j, m));
+            if (i0 + j < p.n) acc[j] = __float_as_uint(__uint_as_float(acc[j]) + odd_term(p.term, i0 + j, m));
         }
-#pragma unroll
-        for (int j = 0; j < 32; j += 2)
-          store_two(p.Y, p.ldy, i0 + j, p.n, m, p.m, __uint_as_float(acc[j]), __uint_as_float(acc[j + 1]), lane);
+        store_chunk(p.Y, p.ldy, i0, p.n, m, p.m, acc, lane);
       }
       __syncwarp();
       if (leave && lane == 0) {
@@ -929,30 +925,42 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     }
   } else {
     // ---------------- the samples' operand of the adapters' term ----------------
-    const int t = (warp - 2 - kEpi) * 32 + lane;                       // this thread's sample of the CTA's half of the tile
-    uint32_t g = 0, fph = 0;                         // k-blocks so far; the phases of free_, a bit per stage
+    const bool writes = warp < 2 + kEpi + kPairBuild;
+    const int w = warp - 2 - kEpi - (writes ? 0 : kPairBuild), t = w * 32 + lane;    // this thread's sample of the CTA's half of the tile, or
+    uint32_t s = 0, ph = 0;                          // share of the factors; ph: the phases of free_, or of landed, a bit per stage
     bool ok = true;
     for (int i = 0; i < segs.n && ok; ++i) {
       const Segment sg = segs.get(i);
       int m0, tt;
       tile_coords(sg.tile, m0, tt);
-      g += sg.k1 - sg.k0;
-      const int units = sg.k1 == p.kseg ? p.term.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0, more = (units + kUnits - 1) / kUnits;
+      s = (s + sg.k1 - sg.k0) % kPairStages;
+      const int units = sg.k1 == p.kseg ? p.term.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0;
       const int smp = tt * p.tn + static_cast<int>(rank) * half + t;
-      const int at = t < half && smp < p.n ? p.term.place[smp] * per : -1;                // this sample's first unit
+      const int at = writes && t < half && smp < p.n ? p.term.place[smp] * per : -1;   // this sample's first unit
       const uint4* src = p.term.pb + static_cast<int64_t>(smp) * per;
-      for (int k = 0; k < more; ++k, ++g) {
-        const uint32_t s = g % kPairStages;
-        const int g0 = k * kUnits, nu = min(kUnits, units - g0);
+      const uint32_t a = i & 1, aph = (i >> 1) & 1;
+      uint4 words[kUnits];
+      if (writes) read_units(src, at, 0, min(kUnits, units), per, words);
+      else if (!mbar_wait_warp(&taken[a], aph ^ 1, abort_flag)) break;
+      uint32_t bad = 0;
+      for (int g0 = 0; g0 < units; g0 += kUnits) {
+        const int nu = min(kUnits, units - g0);
         uint8_t* st = smem + s * kPairStage;
-        uint4 words[kUnits];
-        read_units(src, at, g0, nu, per, words);
-        if (!mbar_wait_warp(&free_[s], (fph >> s) & 1, abort_flag)) { ok = false; break; }
-        fph ^= 1u << s;
-        write_units<128>(words, st, t, t < half, nu);
-        fence_proxy_async_smem();
+        if (!mbar_wait_warp(writes ? &free_[s] : &landed[s], (ph >> s) & 1, abort_flag)) { ok = false; break; }
+        ph ^= 1u << s;
+        uint32_t wrote = 1;
+        if (writes) write_units<32 * kPairBuild>(words, st, t, t < half, nu);
+        else bad |= wrote = clean_units<32 * kPairBuild>(st, t, nu);
+        if (wrote) fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(mapa_u32(smem_u32(&built[s]), 0));
+        if (writes && g0 + kUnits < units) read_units(src, at, g0 + kUnits, min(kUnits, units - g0 - kUnits), per, words);
+        if (++s == static_cast<uint32_t>(kPairStages)) s = 0;
+      }
+      bad = __any_sync(0xffffffffu, bad);
+      if (!writes && lane == 0) {
+        odd[a][w] = bad;
+        mbar_arrive(&looked[a]);
       }
     }
   }
@@ -972,41 +980,9 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// More than 64 samples: p from its parts, zeros for a sample without an adapter, and scale p in bf16 (pb).  In the first blocks:
-// which of the adapters in use have factors that are not finite, a block a sixteenth of an adapter's, and the lists of the tiles.
+// More than 64 samples: p from its parts, zeros for a sample without an adapter, and scale p in bf16 (pb).  In the first blocks the lists of
+// the tiles of the product.
 // ---------------------------------------------------------------------------------------------------------
-// Whether columns [0, width) of part `part` of 16 of an adapter's factors f [rank][ldf] hold an infinity or a NaN; by a block.
-__device__ __forceinline__ bool holds_not_finite(const __nv_bfloat16* f, int rank, int64_t ldf, int64_t width, int part) {
-  bool hit = false;
-  // pieces of 8 columns, row after row; of a row's last one what lies behind the row does not count
-  const int64_t pieces = (width + 7) / 8, all = pieces * rank, to = all * (part + 1) / 16;
-  int64_t i = all * part / 16 + threadIdx.x, r = i / pieces, c = i - r * pieces;
-  while (i < to) {
-    uint4 v[4];
-    int64_t left[4];
-#pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      left[y] = i < to ? width - c * 8 : 0;
-      v[y] = i < to ? *reinterpret_cast<const uint4*>(f + r * ldf + c * 8) : make_uint4(0, 0, 0, 0);
-      i += blockDim.x;
-      c += blockDim.x;
-      while (c >= pieces) { c -= pieces; ++r; }
-    }
-#pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      const uint32_t w[4] = {v[y].x, v[y].y, v[y].z, v[y].w};
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {                  // bit 15 / 31: the exponent of the low / high half is all ones
-        const uint32_t b = ((w[u] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-        hit |= (b & 0x8000u) && 2 * u < left[y];
-        hit |= (b >> 31) && 2 * u + 1 < left[y];
-      }
-    }
-  }
-  return __syncthreads_or(hit);
-}
-
-constexpr int kLookMost = 512;                      // adapters that the grid looks at at once
 struct SumParams {
   Ranked p;
   const int32_t* ids;
@@ -1015,25 +991,18 @@ struct SumParams {
   int32_t rank, adapters;
   float* out;
   __nv_bfloat16* pb;
-  const __nv_bfloat16* F;      // [adapters][rank][ldf], `width` columns
-  int64_t ldf, width;
-  const int32_t* mark;
-  int32_t call, look;          // look: the first blocks, 16 per adapter of min(adapters, kLookMost); then
   int32_t tiles, tn;           // a block per tile of tn samples
-  uint8_t* bad;                // [adapters][16]
   int32_t* lists;              // [tiles][kListPitch]
   int32_t* place;              // per sample its place in its tile's list
   uint32_t* status;
 };
 
 __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant__ SumParams p) {
-  __shared__ int32_t list[256];
-  __shared__ int32_t count;
   __shared__ alignas(16) TileList<kMaxTile> L;
   pdl_launch_dependents();
   pdl_wait();
-  const int tile = static_cast<int>(blockIdx.x) - p.look;
-  if (tile >= 0 && tile < p.tiles) {
+  const int tile = blockIdx.x;
+  if (tile < p.tiles) {
     const int first = tile * p.tn;
     build_list(L, p.ids, first, static_cast<int>(p.n), p.tn, p.adapters, p.status);
     int32_t* to = p.lists + static_cast<int64_t>(tile) * kListPitch;
@@ -1044,24 +1013,8 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
     }
     return;
   }
-  if (tile < 0) {
-    const int part = blockIdx.x & 15, first = blockIdx.x >> 4, step = p.look >> 4;
-    for (int base = first; base < p.adapters; base += 256 * step) {
-      if (threadIdx.x == 0) count = 0;
-      __syncthreads();
-      const int64_t mine = base + static_cast<int64_t>(threadIdx.x) * step;
-      if (mine < p.adapters && p.mark[mine] == p.call) list[atomicAdd(&count, 1)] = static_cast<int32_t>(mine);
-      __syncthreads();
-      for (int x = 0; x < count; ++x) {
-        const bool hit = holds_not_finite(p.F + static_cast<int64_t>(list[x]) * p.rank * p.ldf, p.rank, p.ldf, p.width, part);
-        if (threadIdx.x == 0) p.bad[static_cast<int64_t>(list[x]) * 16 + part] = hit;
-      }
-      __syncthreads();
-    }
-    return;
-  }
   const int per = (p.rank + kUnit - 1) / kUnit;
-  const int64_t blocks = gridDim.x - p.look - p.tiles;
+  const int64_t blocks = gridDim.x - p.tiles;
   for (int64_t x = static_cast<int64_t>(tile - p.tiles) * 256 + threadIdx.x; x < p.n * per; x += blocks * 256) {
     const int64_t i = x / per;
     const int r0 = static_cast<int>(x - i * per) * kUnit, id = p.ids[i];
@@ -1239,9 +1192,10 @@ __global__ void __launch_bounds__(256) adapter_words_kernel(const __grid_constan
 // words its columns (added at the end), the samples the contraction, 64 of them at a time, gathered in the order of adapter_index_kernel
 // (so no sample of another adapter is in the product).
 // Warps: 0..7 loaders (asynchronous copies of 16 bytes into both operands, which arrive at the stage's barrier by themselves: a loader that
-// waited for its copies and fenced them had one k-block under way), 8 MMA issuer and TMEM owner, 9..12 epilogue.
+// waited for its copies and fenced them had one k-block under way), 8 MMA issuer and TMEM owner, 9..16 epilogue, four of them a
+// tile in turn.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kLoaders = 8, kGradThreads = 32 * (kLoaders + 5), kGradStages = 8, kGradRing = 196608;
+constexpr int kLoaders = 8, kGradThreads = 32 * (kLoaders + 9), kGradBuffers = 8, kGradStages = 8, kGradRing = 196608;
 struct GradSide {
   const __nv_bfloat16* z;      // [n][ldz]
   int64_t ldz;
@@ -1346,17 +1300,19 @@ __device__ __forceinline__ void grad_load(const GradParams& p, uint8_t* smem, ui
 
 __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const __grid_constant__ GradParams p) {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t full[kGradStages], empty[kGradStages], tfull[2], tempty[2];
+  __shared__ uint64_t full[kGradStages], empty[kGradStages], tfull[kGradBuffers], tempty[kGradBuffers];
   __shared__ uint32_t tmem_slot, abort_word;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   volatile uint32_t* abort_flag = &abort_word;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const int rp = (p.rank + 15) & ~15, N = 3 * rp, stage = kTileBytesA + grad_panels(p.rank) * 8192;
-  const uint32_t buffers = N <= 256 ? 2 : 1;         // accumulators of 256 columns, or one of 512
+  // Accumulators of `pitch` columns, each epilogue group's own ones (so that it sees all phases of their barriers); one group where there
+  // is one accumulator.
+  const uint32_t pitch = (N + 31) & ~31, all = min(static_cast<uint32_t>(kGradBuffers), 512 / pitch), groups = all > 1 ? 2 : 1, each = all / groups;
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
     for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 32 * kLoaders); mbar_init(&empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 4); }
+    for (int i = 0; i < kGradBuffers; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 4); }
     abort_word = 0;
     fence_barrier_init();
   }
@@ -1373,12 +1329,14 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
     // more than 256 columns: 192 (three panels), then the rest
     const uint32_t n1 = N <= 256 ? N : 192, n2 = N - n1;
     const uint32_t idesc1 = umma_idesc_bf16(BM, n1) | kIdescMnMajor, idesc2 = umma_idesc_bf16(BM, n2 ? n2 : 16) | kIdescMnMajor;
-    uint32_t s = 0, ph = 0, i = 0;
+    uint32_t s = 0, ph = 0, used[2] = {0, 0}, g = groups - 1;  // used: accumulators of a group so far; g: whose tile this is
     bool ok = true;
     for (GradWalk it(p); it.valid() && ok; it.next()) {
+      g = groups - 1 - g;
+      uint32_t i = g ? used[1] : used[0];
       const int nk = (it.count + BK - 1) / BK;
       for (int k0 = 0; k0 < nk && ok; k0 += kDrain, ++i) {
-        const uint32_t b = i % buffers, bph = (i / buffers) & 1, d_tmem = tmem_base + b * 256;
+        const uint32_t b = g * each + i % each, bph = (i / each) & 1, d_tmem = tmem_base + b * pitch;
         if (!mbar_wait_warp(&tempty[b], bph ^ 1, abort_flag)) { ok = false; break; }
         tc_fence_after();
         for (int k = k0; k < min(k0 + kDrain, nk); ++k) {
@@ -1399,22 +1357,26 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
         }
         if (ok && elect_one()) umma_commit(&tfull[b]);
       }
+      (g ? used[1] : used[0]) = i;
     }
   } else {
     const int q = warp & 3;
-    uint32_t i = 0;
-    bool ok = true;
+    const uint32_t mine = (warp - kLoaders - 1) >> 2;
+    uint32_t i = 0, g = groups - 1;
+    bool ok = mine < groups;
     for (GradWalk it(p); it.valid() && ok; it.next()) {
+      g = groups - 1 - g;
+      if (g != mine) continue;
       const GradSide& sd = p.side[it.side];
       const int m = it.tile * BM + q * 32 + lane, nk = (it.count + BK - 1) / BK;
       float* out = sd.out + static_cast<int64_t>(it.a) * p.rank * sd.width + m;
       if (nk == 0 && m < sd.width)
         for (int r = 0; r < p.rank; ++r) out[static_cast<int64_t>(r) * sd.width] = 0.f;
       for (int k0 = 0; k0 < nk; k0 += kDrain, ++i) {
-        const uint32_t b = i % buffers, bph = (i / buffers) & 1;
+        const uint32_t b = mine * each + i % each, bph = (i / each) & 1;
         if (!mbar_wait_warp(&tfull[b], bph, abort_flag)) { ok = false; break; }
         tc_fence_after();
-        const uint32_t t_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + b * 256;
+        const uint32_t t_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + b * pitch;
 #pragma unroll 1
         for (int r0 = 0; r0 < p.rank; r0 += 16) {
           uint32_t w0[16], w1[16], w2[16];
@@ -1470,7 +1432,7 @@ int64_t rank_rows(int64_t n, int64_t d) {
 }
 
 struct AdapterLayout {
-  size_t status, ready, arrived, s, t, ssum, tsum, pb, swords, twords, order, begin, count, work, mark, bad, lists, place, partial, total;
+  size_t status, ready, arrived, s, t, ssum, tsum, pb, swords, twords, order, begin, count, work, lists, place, partial, total;
 };
 
 int check(const sfb_adapter_config* c) {
@@ -1493,8 +1455,6 @@ AdapterLayout layout_of(const sfb_adapter_config& c) {
   L.status = take(4);
   L.ready = take(kModelSms * kEpi * 4);              // these are cleared with the status word
   L.arrived = take(kFewChunks * 4);
-  L.mark = take(static_cast<size_t>(c.adapters) * 4);
-  L.bad = take(static_cast<size_t>(c.adapters) * 16);
   L.s = take(static_cast<size_t>(rank_rows(c.max_samples, c.cols)) * c.rank * 4);
   L.t = take(static_cast<size_t>(rank_rows(c.max_samples, c.rows)) * c.rank * 4);
   L.ssum = take(n * c.rank * 4);
@@ -1526,8 +1486,6 @@ struct sfb_adapters {
   char* ws;
   cudaStream_t stream;
   int device, last_cuda, max_pairs;
-  uint32_t calls;                      // products with factors so far: what such a call marks its adapters with (a replayed one with the same
-                                       // number each time, so that it may look at adapters of earlier replays too)
   CUtensorMap mapU, mapV;              // boxes of 64 entries x 16 ranks of an adapter
   CUtensorMap unitU, unitV;            // x `boxed` units of 8 ranks
   int32_t boxed;
@@ -1612,8 +1570,6 @@ cudaError_t rank_products(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz
     // a block an SM, and no more than there can be parts of chunks
     return launch_kernel(adapter_rank_kernel<true>, dim3(std::max(1, std::min(kModelSms, chunks * parts))), dim3(kRankThreads), smem, h->stream, 1, mf, mz, p);
   }
-  p.mark = h->at<int32_t>(h->lay.mark);
-  p.call = static_cast<int32_t>(++h->calls);
   const int groups = std::max(1, std::min(chunks, 2 * kModelSms / (parts * tiles)));
   const cudaError_t e = allow_smem<adapter_rank_kernel<false>>(kSmallRing + 1024);
   if (e != cudaSuccess) return e;
@@ -1633,9 +1589,9 @@ int few_parts(int64_t tiles, int64_t kseg) {
 
 // What adapter_rank_kernel or adapter_sum_kernel leaves for the products.
 template <bool MN>
-Term term_of(const sfb_adapters* h, const int32_t* ids, const float* p, bool bad) {
+Term term_of(const sfb_adapters* h, const int32_t* ids, const float* p) {
   const sfb_adapter_config& c = h->cfg;
-  return Term{c.rank, c.adapters, h->boxed, ids, h->at<int32_t>(h->lay.lists), h->at<int32_t>(h->lay.place), h->scale, bad ? h->at<uint4>(h->lay.bad) : nullptr,
+  return Term{c.rank, c.adapters, h->boxed, ids, h->at<int32_t>(h->lay.lists), h->at<int32_t>(h->lay.place), h->scale,
               static_cast<const __nv_bfloat16*>(MN ? h->V : h->U), MN ? c.ldv : c.ldu, p, h->at<uint4>(h->lay.pb)};
 }
 
@@ -1705,21 +1661,18 @@ template <bool MN>
 cudaError_t product(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const int32_t* ids, Ranked* s, float* to, void* Y, int64_t ldy) {
   const sfb_adapter_config& c = h->cfg;
   if (n <= kFewMost) {
-    const Term term = term_of<MN>(h, ids, s->at, false);
+    const Term term = term_of<MN>(h, ids, s->at);
     return n <= 16 ? few<16, MN>(h, n, Z, ldz, term, Y, ldy) : n <= 32 ? few<32, MN>(h, n, Z, ldz, term, Y, ldy) : few<kFewMost, MN>(h, n, Z, ldz, term, Y, ldy);
   }
   SumParams p{};
   p.p = *s; p.ids = ids; p.scale = h->scale; p.n = n; p.rank = c.rank; p.adapters = c.adapters; p.out = to; p.status = h->at<uint32_t>(h->lay.status);
   p.pb = h->at<__nv_bfloat16>(h->lay.pb);
-  p.F = static_cast<const __nv_bfloat16*>(MN ? h->V : h->U); p.ldf = MN ? c.ldv : c.ldu; p.width = MN ? c.cols : c.rows;
-  p.mark = h->at<int32_t>(h->lay.mark); p.call = static_cast<int32_t>(h->calls); p.look = std::min(c.adapters, kLookMost) * 16;
-  p.bad = h->at<uint8_t>(h->lay.bad);
   p.tn = tile_of(n); p.tiles = static_cast<int32_t>((n + p.tn - 1) / p.tn); p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place);
-  const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(p.look + p.tiles + grid1d(n * ((c.rank + kUnit - 1) / kUnit), 256)), dim3(256), 0, h->stream,
+  const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(p.tiles + grid1d(n * ((c.rank + kUnit - 1) / kUnit), 256)), dim3(256), 0, h->stream,
                                       1, p);
   if (e != cudaSuccess) return e;
   *s = Ranked{to, 1, 0};
-  return pairs<MN>(h, n, Z, ldz, term_of<MN>(h, ids, to, true), Y, ldy);
+  return pairs<MN>(h, n, Z, ldz, term_of<MN>(h, ids, to), Y, ldy);
 }
 
 int fail(sfb_adapters* h, cudaError_t e) {
@@ -1868,7 +1821,7 @@ extern "C" int sfb_adapter_get_status(sfb_adapters* h, uint32_t* status_out) {
   ACK(cudaMemcpyAsync(status_out, h->ws + h->lay.status, 4, cudaMemcpyDeviceToHost, h->stream));
   ACK(cudaMemsetAsync(h->ws + h->lay.status, 0, 4, h->stream));
   ACK(cudaStreamSynchronize(h->stream));
-  if (*status_out & SFB_STATUS_TIMEOUT) ACK(cudaMemsetAsync(h->ws + h->lay.ready, 0, h->lay.mark - h->lay.ready, h->stream));
+  if (*status_out & SFB_STATUS_TIMEOUT) ACK(cudaMemsetAsync(h->ws + h->lay.ready, 0, h->lay.s - h->lay.ready, h->stream));
   return SFB_OK;
 }
 

@@ -25,7 +25,7 @@ using sfb::pdl_wait;
 
 constexpr int kThreads = 256;
 constexpr int64_t kPieceBytes = 16384;               // four 16-byte loads a thread
-constexpr int kBlocksPerSm = 5;
+constexpr int kSumBlocks = 4, kScaleBlocks = 4;      // an SM
 
 struct Piece {
   const char* src;
@@ -42,12 +42,54 @@ template <> __device__ __forceinline__ float from_f<float>(float v) { return v; 
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
 
+// The entries of 16 bytes.
+__device__ __forceinline__ void widen(const uint4& w, float (&v)[4], const float*) {
+  v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
+}
+__device__ __forceinline__ void widen(const uint4& w, float (&v)[8], const __nv_bfloat16*) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[2 * j] = __uint_as_float(u[j] << 16);
+    v[2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void widen(const uint4& w, float (&v)[8], const __half*) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[j]));
+    v[2 * j] = f.x;
+    v[2 * j + 1] = f.y;
+  }
+}
+__device__ __forceinline__ uint4 narrow(const float (&v)[4], const float*) {
+  return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+}
+__device__ __forceinline__ uint32_t two(__nv_bfloat162 v) { return *reinterpret_cast<const uint32_t*>(&v); }
+__device__ __forceinline__ uint32_t two(__half2 v) { return *reinterpret_cast<const uint32_t*>(&v); }
+__device__ __forceinline__ uint4 narrow(const float (&v)[8], const __nv_bfloat16*) {
+  return make_uint4(two(__floats2bfloat162_rn(v[0], v[1])), two(__floats2bfloat162_rn(v[2], v[3])), two(__floats2bfloat162_rn(v[4], v[5])),
+                    two(__floats2bfloat162_rn(v[6], v[7])));
+}
+__device__ __forceinline__ uint4 narrow(const float (&v)[8], const __half*) {
+  return make_uint4(two(__floats2half2_rn(v[0], v[1])), two(__floats2half2_rn(v[2], v[3])), two(__floats2half2_rn(v[4], v[5])),
+                    two(__floats2half2_rn(v[6], v[7])));
+}
+
+template <int N>
+__device__ __forceinline__ bool all_zero(const float (&v)[N]) {
+  bool z = true;
+#pragma unroll
+  for (int j = 0; j < N; ++j) z &= v[j] == 0.f;
+  return z;
+}
 template <int N>
 __device__ __forceinline__ void add_squares(const float (&v)[N], double& sum) {
   float q = 0.f;
 #pragma unroll
   for (int j = 0; j < N; ++j) q = fmaf(v[j], v[j], q);
-  if (q >= 1e-30f && q <= 1e37f) {
+  if ((q >= 1e-30f && q <= 1e37f) || (q == 0.f && all_zero(v))) {
     sum += static_cast<double>(q);
   } else {
 #pragma unroll
@@ -58,30 +100,29 @@ __device__ __forceinline__ void add_squares(const float (&v)[N], double& sum) {
 // Entries [0, n) of a piece: up to the first 16-byte boundary and behind the last one singly, the rest 16 bytes at a time, four of
 // them under way.
 template <typename T>
-__device__ __forceinline__ void sum_piece(const T* __restrict__ p, int n, double& sum) {
+__device__ __forceinline__ double sum_piece(const T* p, int n, double sum) {
   constexpr int kV = 16 / sizeof(T);
   const int lead = min(n, static_cast<int>(((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / sizeof(T)));
   const int vecs = (n - lead) / kV;
   for (int i = threadIdx.x; i < lead; i += kThreads) { const float v[1] = {to_f(p[i])}; add_squares(v, sum); }
   for (int i = lead + vecs * kV + threadIdx.x; i < n; i += kThreads) { const float v[1] = {to_f(p[i])}; add_squares(v, sum); }
-  const uint4* __restrict__ q = reinterpret_cast<const uint4*>(p + lead);
+  const uint4* q = reinterpret_cast<const uint4*>(p + lead);
   for (int i = threadIdx.x; i < vecs; i += 4 * kThreads) {
     uint4 w[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) w[u] = i + u * kThreads < vecs ? q[i + u * kThreads] : make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (i + u * kThreads >= vecs) break;
-      const T* e = reinterpret_cast<const T*>(&w[u]);
+    for (int u = 0; u < 4; ++u) {                    // (what lies behind the last one is zero)
       float v[kV];
-#pragma unroll
-      for (int j = 0; j < kV; ++j) v[j] = to_f(e[j]);
+      widen(w[u], v, static_cast<const T*>(nullptr));
       add_squares(v, sum);
     }
   }
+  return sum;
 }
 
-// dst = coef * src, or src bit for bit where coef is 1; the two may be the same addresses.  The vectors follow dst's boundary; a src that lies otherwise is read singly.
+// dst = coef * src, or src bit for bit where coef is 1; the two may be the same addresses.  Where they lie differently to a 16-byte boundary,
+// entry by entry.
 template <typename T>
 __device__ __forceinline__ void scale_piece(const T* src, T* dst, int n, float coef) {
   constexpr int kV = 16 / sizeof(T);
@@ -93,28 +134,27 @@ __device__ __forceinline__ void scale_piece(const T* src, T* dst, int n, float c
   for (int i = threadIdx.x; i < lead; i += kThreads) dst[i] = scaled(src[i]);
   for (int i = lead + vecs * kV + threadIdx.x; i < n; i += kThreads) dst[i] = scaled(src[i]);
   uint4* d = reinterpret_cast<uint4*>(dst + lead);
+  if (!same) {
+    for (int i = threadIdx.x; i < vecs * kV; i += kThreads) dst[lead + i] = scaled(src[lead + i]);
+    return;
+  }
+  const uint4* q = reinterpret_cast<const uint4*>(src + lead);
   for (int i = threadIdx.x; i < vecs; i += 4 * kThreads) {
     uint4 w[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int k = i + u * kThreads;
-      if (k >= vecs) continue;
-      if (same) {
-        w[u] = reinterpret_cast<const uint4*>(src + lead)[k];
-      } else {
-        T* e = reinterpret_cast<T*>(&w[u]);
+    for (int u = 0; u < 4; ++u)
+      if (i + u * kThreads < vecs) w[u] = __ldcs(q + i + u * kThreads);          // (not read again, nor what is written)
 #pragma unroll
-        for (int j = 0; j < kV; ++j) e[j] = src[lead + k * kV + j];
+    for (int u = 0; u < 4; ++u) {
+      if (i + u * kThreads >= vecs) break;
+      if (!copy) {
+        float v[kV];
+        widen(w[u], v, static_cast<const T*>(nullptr));
+#pragma unroll
+        for (int j = 0; j < kV; ++j) v[j] *= coef;
+        w[u] = narrow(v, static_cast<const T*>(nullptr));
       }
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int k = i + u * kThreads;
-      if (k >= vecs) break;
-      T* e = reinterpret_cast<T*>(&w[u]);
-#pragma unroll
-      for (int j = 0; j < kV; ++j) e[j] = scaled(e[j]);
-      d[k] = w[u];
+      __stcs(d + i + u * kThreads, w[u]);
     }
   }
 }
@@ -132,7 +172,7 @@ __device__ __forceinline__ double block_sum(double v) {
   return s;
 }
 
-__global__ void __launch_bounds__(kThreads, 5) clip_sum_kernel(const Piece* pieces, int64_t n, double* part) {
+__global__ void __launch_bounds__(kThreads, kSumBlocks) clip_sum_kernel(const Piece* pieces, int64_t n, double* part) {
   pdl_launch_dependents();
   pdl_wait();
   double sum = 0.0;
@@ -140,9 +180,9 @@ __global__ void __launch_bounds__(kThreads, 5) clip_sum_kernel(const Piece* piec
   for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
     const Piece c = next;
     if (i + gridDim.x < n) next = pieces[i + gridDim.x];
-    if (c.dtype == SFB_F32) sum_piece(reinterpret_cast<const float*>(c.src), c.count, sum);
-    else if (c.dtype == SFB_BF16) sum_piece(reinterpret_cast<const __nv_bfloat16*>(c.src), c.count, sum);
-    else sum_piece(reinterpret_cast<const __half*>(c.src), c.count, sum);
+    if (c.dtype == SFB_F32) sum = sum_piece(reinterpret_cast<const float*>(c.src), c.count, sum);
+    else if (c.dtype == SFB_BF16) sum = sum_piece(reinterpret_cast<const __nv_bfloat16*>(c.src), c.count, sum);
+    else sum = sum_piece(reinterpret_cast<const __half*>(c.src), c.count, sum);
   }
   sum = block_sum(sum);
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
@@ -162,7 +202,7 @@ __global__ void __launch_bounds__(kThreads) clip_total_kernel(const double* part
   if (threadIdx.x == 0) *sum = s;
 }
 
-__global__ void __launch_bounds__(kThreads) clip_scale_kernel(const Piece* pieces, int64_t n, const double* part, int parts, float max_norm,
+__global__ void __launch_bounds__(kThreads, kScaleBlocks) clip_scale_kernel(const Piece* pieces, int64_t n, const double* part, int parts, float max_norm,
                                                               float* result) {
   pdl_launch_dependents();
   pdl_wait();
@@ -266,7 +306,8 @@ int launch_sum(sfb_clip* h) {
 }
 
 int launch_scale(sfb_clip* h, float max_norm, const double* part, int parts, float* result) {
-  const cudaError_t e = sfb::launch_kernel(clip_scale_kernel, dim3(h->blocks), dim3(kThreads), 0, h->stream, 1,
+  const unsigned blocks = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(h->pieces, sfb::sm_count() * kScaleBlocks)));
+  const cudaError_t e = sfb::launch_kernel(clip_scale_kernel, dim3(blocks), dim3(kThreads), 0, h->stream, 1,
                                            reinterpret_cast<const Piece*>(h->ws + kPartBytes), h->pieces, part, parts, max_norm, result);
   return e == cudaSuccess ? SFB_OK : fail(h, e);
 }
@@ -319,7 +360,7 @@ extern "C" int sfb_clip_init(int64_t tensors, const void* const* src, void* cons
     h = new sfb_clip();
     h->ws = static_cast<char*>(workspace_dev);
     h->pieces = static_cast<int64_t>(table.size());
-    h->blocks = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(h->pieces, std::min(sfb::sm_count() * kBlocksPerSm, kMaxParts))));
+    h->blocks = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(h->pieces, std::min(sfb::sm_count() * kSumBlocks, kMaxParts))));
     h->stream = static_cast<cudaStream_t>(stream);
     h->device = dev;
     h->last_cuda = 0;
