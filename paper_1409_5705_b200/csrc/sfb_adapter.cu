@@ -386,9 +386,27 @@ __device__ __noinline__ float odd_term(const Term& p, int i, int m) {
   }
   return v;
 }
-// The adapter of unit g of `units`.
-__device__ __forceinline__ int unit_adapter(const int32_t* list, int g, int units, int per) {
-  return g < units ? list[1 + g / per] : 0;
+// The factors of units [g0, g0 + nu) into a stage, by `warps` warps, w of them, each some of the copies (one warp, the producer's, took 90 ns a
+// copy, 1.4 us a k-block of 16).  held: of the 32 units that unit g0 is among, the adapter and the first rank of each, by the lanes.
+struct Held { int a, y; };
+__device__ __forceinline__ Held hold_units(const int32_t* list, int g, int units, int per) {
+  Held h{0, 0};
+  if (g < units) {
+    const int at = g / per;
+    h.a = list[1 + at];
+    h.y = (g - at * per) * kUnit;
+  }
+  return h;
+}
+template <int WARPS>
+__device__ __forceinline__ void load_units(uint8_t* st, uint64_t* landed, const CUtensorMap& tmF, const Held& held, int g0, int nu, int boxed, int m0, int w) {
+  for (int j = w * boxed; j < nu; j += WARPS * boxed) {
+    const int a = __shfl_sync(0xffffffffu, held.a, (g0 + j) & 31), y = __shfl_sync(0xffffffffu, held.y, (g0 + j) & 31);
+    if (elect_one()) {
+      tma_load_3d(st + j * (kUnit * 128), &tmF, m0, y, a, landed);
+      tma_load_3d(st + kTileBytesA / 2 + j * (kUnit * 128), &tmF, m0 + 64, y, a, landed);
+    }
+  }
 }
 __device__ __forceinline__ uint4 lds_v4(uint32_t at) {
   uint4 v;
@@ -463,8 +481,8 @@ __device__ __forceinline__ void read_units(const uint4* src, int at, int g0, int
 // the samples.  The loads of A and z do not wait for the launch before (adapter_rank_kernel lets this one start once those before it are
 // done).  325,000 x 10,000 with 64 samples: 961 us, 6.9 TB/s.  (A CTA an SM that takes its even share of all tiles, with parts through
 // global memory: 1,030; 10,000 x 20,000 with 37 samples of 64 adapters 84, here 77.)
-// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..5 epilogue, 6 and 7 the samples' operand of the term, 8 and 9
-// its factors.
+// Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..5 epilogue, 6 and 7 the samples' operand of the term and the
+// loads of its factors, 8 and 9 the look at them.
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kWrite = 2, kClean = 2, kBuild = kWrite + kClean;      // warps that write the samples' operand of the term, that look
                                                                      // through the factors
@@ -490,21 +508,6 @@ __device__ __forceinline__ void few_load(uint8_t* st, uint64_t* full, const CUte
     tma_load_2d(st, &tmA, k * BK, m0, full);
   }
   tma_load_2d_hint(st + kTileBytesA, &tmZ, k * BK, 0, full, keep);     // (every tile reads the samples)
-}
-__device__ __forceinline__ void few_load_units(uint8_t* st, uint64_t* landed, uint64_t* free_, const CUtensorMap& tmF, int known, int g0, int nu, int per,
-                                               int boxed, int m0) {
-  if (elect_one()) {
-    mbar_arrive(free_);
-    mbar_expect_tx(landed, nu * 2 * kUnit * 128);
-  }
-  __syncwarp();
-  for (int j = 0; j < nu; j += boxed) {
-    const int a = __shfl_sync(0xffffffffu, known, (g0 + j) & 31), y = (g0 + j) % per * kUnit;
-    if (elect_one()) {
-      tma_load_3d(st + j * (kUnit * 128), &tmF, m0, y, a, landed);
-      tma_load_3d(st + kTileBytesA / 2 + j * (kUnit * 128), &tmF, m0 + 64, y, a, landed);
-    }
-  }
 }
 template <bool MN>
 __device__ __forceinline__ void few_mma(uint32_t st, uint32_t d_tmem, uint32_t idesc, bool first) {
@@ -557,9 +560,11 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     pdl_wait();
     const int units = p.term.lists[0] * per;
     for (int g0 = mine * kUnits; g0 < units && ok; g0 += p.parts * kUnits, next()) {
-      const int known = unit_adapter(p.term.lists, (g0 & ~31) + lane, units, per);
       ok = mbar_wait_warp(&empty[s], ph ^ 1, abort_flag);
-      if (ok) few_load_units(smem + s * kStage, &landed[s], &free_[s], tmF, known, g0, min(kUnits, units - g0), per, p.term.boxed, m0);
+      if (ok && elect_one()) {
+        mbar_expect_tx(&landed[s], min(kUnits, units - g0) * 2 * kUnit * 128);
+        mbar_arrive(&free_[s]);
+      }
     }
   } else if (warp == 1) {
     const uint32_t idesc_f = umma_idesc_bf16(BM, TN) | 1u << 15, idesc = MN ? idesc_f : umma_idesc_bf16(BM, TN);
@@ -618,8 +623,10 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
       if (!mbar_wait_warp(writes ? &free_[s] : &landed[s], (ph >> s) & 1, abort_flag)) break;
       ph ^= 1u << s;
       uint32_t wrote = 1;
-      if (writes) write_units<32 * kWrite>(words, smem + s * kStage, t, t < TN, nu);
-      else bad |= wrote = clean_units<32 * kClean>(smem + s * kStage, t, nu);
+      if (writes) {
+        load_units<kWrite>(smem + s * kStage, &landed[s], tmF, hold_units(p.term.lists, (g0 & ~31) + lane, units, per), g0, nu, p.term.boxed, m0, warp - 6);
+        write_units<32 * kWrite>(words, smem + s * kStage, t, t < TN, nu);
+      } else bad |= wrote = clean_units<32 * kClean>(smem + s * kStage, t, nu);
       if (wrote) fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&built[s]);
@@ -678,7 +685,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // The pair that finishes a tile has its term.
 //
 // Warps: 0 TMA producer, 1 MMA issuer (leader CTA) and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the columns), 10..13
-// the samples' operand of the term, 14..17 its factors.
+// the samples' operand of the term and the loads of its factors, 14..17 the look at them.
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kPairBuild = 4, kPairThreads = 32 * (2 + kEpi + 2 * kPairBuild), kGroup = 8;      // kGroup: tiles of samples that follow one another
 constexpr int kPairStages = 6, kPairStage = 2 * kTileBytesA;
@@ -768,10 +775,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       int m0, tt;
       tile_coords(sg.tile, m0, tt);
       const int z0 = tt * p.tn + static_cast<int>(rank) * half;
-      // of four k-blocks of factors at a time the lanes hold the adapter of a unit, asked for ahead of the loads of A
-      const int32_t* list = p.term.lists + static_cast<int64_t>(tt) * kListPitch;
-      const int count = sg.k1 == p.kseg ? list[0] : 0;
-      int known = list[1 + lane / per];
+      const int count = sg.k1 == p.kseg ? p.term.lists[static_cast<int64_t>(tt) * kListPitch] : 0;
       auto loads = [&](int k0, int k1) {
         for (int k = k0; k < k1; ++k) {
           if (!mbar_wait_warp(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
@@ -794,21 +798,11 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       const int units = count * per, more = (units + kUnits - 1) / kUnits;
       for (int k = 0; k < more && ok; ++k) {
         if (!mbar_wait_warp(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
-        uint8_t* st = smem + s * kPairStage;
-        const int g0 = k * kUnits, nu = min(kUnits, units - g0);
+        const int nu = min(kUnits, units - k * kUnits);
         if (elect_one()) {
-          mbar_arrive(&free_[s]);
           mbar_expect_tx(&landed[s], nu * 2 * kUnit * 128);
+          mbar_arrive(&free_[s]);
         }
-        __syncwarp();
-        for (int j = 0; j < nu; j += p.term.boxed) {
-          const int a = __shfl_sync(0xffffffffu, known, (g0 + j) & 31), y = (g0 + j) % per * kUnit;
-          if (elect_one()) {
-            tma_load_3d(st + j * (kUnit * 128), &tmF, m0, y, a, &landed[s]);
-            tma_load_3d(st + kTileBytesA / 2 + j * (kUnit * 128), &tmF, m0 + 64, y, a, &landed[s]);
-          }
-        }
-        if (((g0 + kUnits) & 31) == 0 && g0 + kUnits < units) known = unit_adapter(list, g0 + kUnits + lane, units, per);
         if (++s == static_cast<uint32_t>(kPairStages)) { s = 0; ph ^= 1; }
       }
     }
@@ -939,6 +933,8 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       const int at = writes && t < half && smp < p.n ? p.term.place[smp] * per : -1;   // this sample's first unit
       const uint4* src = p.term.pb + static_cast<int64_t>(smp) * per;
       const uint32_t a = i & 1, aph = (i >> 1) & 1;
+      const int32_t* list = p.term.lists + static_cast<int64_t>(tt) * kListPitch;
+      Held held = hold_units(list, lane, writes ? units : 0, per);
       uint4 words[kUnits];
       if (writes) read_units(src, at, 0, min(kUnits, units), per, words);
       else if (!mbar_wait_warp(&taken[a], aph ^ 1, abort_flag)) break;
@@ -949,8 +945,11 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         if (!mbar_wait_warp(writes ? &free_[s] : &landed[s], (ph >> s) & 1, abort_flag)) { ok = false; break; }
         ph ^= 1u << s;
         uint32_t wrote = 1;
-        if (writes) write_units<32 * kPairBuild>(words, st, t, t < half, nu);
-        else bad |= wrote = clean_units<32 * kPairBuild>(st, t, nu);
+        if (writes) {
+          load_units<kPairBuild>(st, &landed[s], tmF, held, g0, nu, p.term.boxed, m0, w);
+          write_units<32 * kPairBuild>(words, st, t, t < half, nu);
+          if (((g0 + kUnits) & 31) == 0) held = hold_units(list, g0 + kUnits + lane, units, per);
+        } else bad |= wrote = clean_units<32 * kPairBuild>(st, t, nu);
         if (wrote) fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(mapa_u32(smem_u32(&built[s]), 0));
@@ -1015,8 +1014,10 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
   }
   const int per = (p.rank + kUnit - 1) / kUnit;
   const int64_t blocks = gridDim.x - p.tiles;
-  for (int64_t x = static_cast<int64_t>(tile - p.tiles) * 256 + threadIdx.x; x < p.n * per; x += blocks * 256) {
-    const int64_t i = x / per;
+  // four lanes a unit, each some of the parts (by whole warps: a unit behind the last one is formed, not written)
+  const int turn = threadIdx.x & 3;
+  for (int64_t base = static_cast<int64_t>(tile - p.tiles) * 64; base < p.n * per; base += blocks * 64) {
+    const int64_t at = base + (threadIdx.x >> 2), x = min(at, p.n * per - 1), i = x / per;
     const int r0 = static_cast<int>(x - i * per) * kUnit, id = p.ids[i];
     const bool has = id >= 0 && id < p.adapters;
     const float sc = has ? p.scale[id] : 0.f;
@@ -1027,13 +1028,20 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
       for (int j = 0; j < kUnit; ++j) v[j] = 0.f;
       if (has) {
 #pragma unroll 4
-        for (int c = 0; c < p.p.parts; ++c) {
+        for (int c = turn; c < p.p.parts; c += 4) {
           const float4* in = reinterpret_cast<const float4*>(p.p.at + c * p.p.stride + from);
-          const float4 x = in[0], y = in[1];
-          v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+          const float4 a = in[0], b = in[1];
+          v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
         }
       }
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j) {
+        v[j] += __shfl_xor_sync(0xffffffffu, v[j], 1);
+        v[j] += __shfl_xor_sync(0xffffffffu, v[j], 2);
+      }
+      if (turn || at >= p.n * per) continue;
     } else {
+      if (turn || at >= p.n * per) continue;
 #pragma unroll
       for (int j = 0; j < kUnit; ++j) v[j] = has && r0 + j < p.rank ? ranked(p.p, from + j) : 0.f;
     }
@@ -1668,7 +1676,7 @@ cudaError_t product(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, cons
   p.p = *s; p.ids = ids; p.scale = h->scale; p.n = n; p.rank = c.rank; p.adapters = c.adapters; p.out = to; p.status = h->at<uint32_t>(h->lay.status);
   p.pb = h->at<__nv_bfloat16>(h->lay.pb);
   p.tn = tile_of(n); p.tiles = static_cast<int32_t>((n + p.tn - 1) / p.tn); p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place);
-  const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(p.tiles + grid1d(n * ((c.rank + kUnit - 1) / kUnit), 256)), dim3(256), 0, h->stream,
+  const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(p.tiles + grid1d(n * ((c.rank + kUnit - 1) / kUnit), 64)), dim3(256), 0, h->stream,
                                       1, p);
   if (e != cudaSuccess) return e;
   *s = Ranked{to, 1, 0};
