@@ -400,12 +400,21 @@ __device__ __forceinline__ Held hold_units(const int32_t* list, int g, int units
 }
 template <int WARPS>
 __device__ __forceinline__ void load_units(uint8_t* st, uint64_t* landed, const CUtensorMap& tmF, const Held& held, int g0, int nu, int boxed, int m0, int w) {
-  for (int j = w * boxed; j < nu; j += WARPS * boxed) {
-    const int a = __shfl_sync(0xffffffffu, held.a, (g0 + j) & 31), y = __shfl_sync(0xffffffffu, held.y, (g0 + j) & 31);
-    if (elect_one()) {
-      tma_load_3d(st + j * (kUnit * 128), &tmF, m0, y, a, landed);
-      tma_load_3d(st + kTileBytesA / 2 + j * (kUnit * 128), &tmF, m0 + 64, y, a, landed);
-    }
+  constexpr int kMost = kUnits / WARPS;              // copies of a warp, for each of the two panels
+  int a[kMost], y[kMost];
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    const int j = (w + i * WARPS) * boxed;
+    a[i] = __shfl_sync(0xffffffffu, held.a, (g0 + j) & 31);
+    y[i] = __shfl_sync(0xffffffffu, held.y, (g0 + j) & 31);
+  }
+  if (!elect_one()) return;
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) {
+    const int j = (w + i * WARPS) * boxed;
+    if (j >= nu) break;
+    tma_load_3d(st + j * (kUnit * 128), &tmF, m0, y[i], a[i], landed);
+    tma_load_3d(st + kTileBytesA / 2 + j * (kUnit * 128), &tmF, m0 + 64, y[i], a[i], landed);
   }
 }
 __device__ __forceinline__ uint4 lds_v4(uint32_t at) {
@@ -685,11 +694,11 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // The pair that finishes a tile has its term.
 //
 // Warps: 0 TMA producer, 1 MMA issuer (leader CTA) and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the columns), 10..13
-// the samples' operand of the term and the loads of its factors, 14..17 the look at them.
+// the samples' operand of the term and the loads of its factors, 14..17 the look at them, 18..20 hand the other CTA's on to the leader.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kPairBuild = 4, kPairThreads = 32 * (2 + kEpi + 2 * kPairBuild), kGroup = 8;      // kGroup: tiles of samples that follow one another
+constexpr int kPairBuild = 4, kHand = 3, kPairThreads = 32 * (2 + kEpi + 2 * kPairBuild + kHand), kGroup = 8;      // kGroup: tiles of samples that follow one another
 constexpr int kPairStages = 6, kPairStage = 2 * kTileBytesA;
-constexpr int kPairSmem = kPairStages * kPairStage + 1024;
+constexpr int kPairSmem = kPairStages * kPairStage + 128 * SFB_ADAPTER_MAX_RANK * 2 + 1024;      // (behind the stages: a row of pb per writing thread)
 constexpr int kPartFloats = BM * kMaxTile;          // what a CTA leaves of a tile
 struct PairParams {
   Term term;
@@ -728,8 +737,8 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kPairStages], empty[kPairStages];       // full, built, tempty: the leader's are in use
   __shared__ uint64_t free_[kPairStages], built[kPairStages];      // of a k-block of factors: the stage is free for the samples' operand;
-                                                                   // both CTAs have written it
-  __shared__ uint64_t landed[kPairStages];                         // its factors are here
+                                                                   // this CTA has its operands
+  __shared__ uint64_t landed[kPairStages], joined[kPairStages];    // its factors are here; the leader's: the other CTA has built its operands
   __shared__ uint64_t tfull[2], tempty[2], looked[2], taken[2];    // looked: whether factors of a tile were not finite is known; taken: read
   __shared__ uint32_t tmem_slot, abort_word, odd[2][kPairBuild];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -749,7 +758,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kPairStages; ++i) {
-      mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&landed[i], 1); mbar_init(&built[i], 4 * kPairBuild);
+      mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&landed[i], 1); mbar_init(&built[i], 2 * kPairBuild); mbar_init(&joined[i], 1);
     }
     for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 2 * kEpi); mbar_init(&looked[i], kPairBuild); mbar_init(&taken[i], kEpi); }
     abort_word = 0;
@@ -834,7 +843,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
           if (++s == static_cast<uint32_t>(kPairStages)) s = 0;
         }
         for (int left = count * per; left > 0 && ok; left -= kUnits) {
-          if (!mbar_wait_cluster(&built[s], (bph >> s) & 1, abort_flag)) { ok = false; break; }
+          if (!mbar_wait_warp(&built[s], (bph >> s) & 1, abort_flag) || !mbar_wait_cluster(&joined[s], (bph >> s) & 1, abort_flag)) { ok = false; break; }
           bph ^= 1u << s;
           tc_fence_after();
           const int ns = (min(kUnits, left) + 1) / 2;                  // instructions: two units each
@@ -917,11 +926,35 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         st_release(p.ready + pair * 2 * kEpi + slot, 1u);
       }
     }
+  } else if (warp >= 2 + kEpi + 2 * kPairBuild) {
+    // ---------------- hand on the other CTA's operands ----------------
+    // (A release to the cluster by each of the eight warps that make them took 1 us a k-block, and one warp, with no accesses of its own,
+    // that hands all of them on is not much faster: these take them in turn.  Gradients of 1,024 samples of 64 adapters, 1,000 x 20,000: 98,
+    // 89 and 78 us.)
+    uint32_t s = 0, bph = 0, turn = warp - 2 - kEpi - 2 * kPairBuild;
+    bool ok = true;
+    for (int i = 0; i < segs.n && ok && rank == 1; ++i) {
+      const Segment sg = segs.get(i);
+      int m0, tt;
+      tile_coords(sg.tile, m0, tt);
+      s = (s + sg.k1 - sg.k0) % kPairStages;
+      for (int left = sg.k1 == p.kseg ? p.term.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0; left > 0 && ok; left -= kUnits) {
+        ok = mbar_wait_warp(&built[s], (bph >> s) & 1, abort_flag);
+        bph ^= 1u << s;
+        if (turn == 0) {
+          if (ok && lane == 0) mbar_arrive_cluster(mapa_u32(smem_u32(&joined[s]), 0));
+          turn = kHand;
+        }
+        --turn;
+        if (++s == static_cast<uint32_t>(kPairStages)) s = 0;
+      }
+    }
   } else {
-    // ---------------- the samples' operand of the adapters' term ----------------
+    // ---------------- the samples' operand of the term, and its factors ----------------
     const bool writes = warp < 2 + kEpi + kPairBuild;
     const int w = warp - 2 - kEpi - (writes ? 0 : kPairBuild), t = w * 32 + lane;    // this thread's sample of the CTA's half of the tile, or
     uint32_t s = 0, ph = 0;                          // share of the factors; ph: the phases of free_, or of landed, a bit per stage
+    const uint32_t mine = smem_u32(smem + kPairStages * kPairStage) + t * (SFB_ADAPTER_MAX_RANK * 2);
     bool ok = true;
     for (int i = 0; i < segs.n && ok; ++i) {
       const Segment sg = segs.get(i);
@@ -935,9 +968,11 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       const uint32_t a = i & 1, aph = (i >> 1) & 1;
       const int32_t* list = p.term.lists + static_cast<int64_t>(tt) * kListPitch;
       Held held = hold_units(list, lane, writes ? units : 0, per);
-      uint4 words[kUnits];
-      if (writes) read_units(src, at, 0, min(kUnits, units), per, words);
-      else if (!mbar_wait_warp(&taken[a], aph ^ 1, abort_flag)) break;
+      // a thread's own row of pb comes to shared memory while the k-blocks of A are under way
+      if (writes) {
+        if (units > 0 && at >= 0)
+          for (int u = 0; u < per; ++u) cp_async_16(mine + u * 16, src + u, 16);
+      } else if (!mbar_wait_warp(&taken[a], aph ^ 1, abort_flag)) break;
       uint32_t bad = 0;
       for (int g0 = 0; g0 < units; g0 += kUnits) {
         const int nu = min(kUnits, units - g0);
@@ -947,13 +982,19 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         uint32_t wrote = 1;
         if (writes) {
           load_units<kPairBuild>(st, &landed[s], tmF, held, g0, nu, p.term.boxed, m0, w);
+          if (g0 == 0) cp_async_wait_all();
+          uint4 words[kUnits];
+#pragma unroll
+          for (int j = 0; j < kUnits; ++j) {
+            const int u = g0 + j - at;
+            words[j] = at >= 0 && j < nu && u >= 0 && u < per ? lds_v4(mine + u * 16) : make_uint4(0, 0, 0, 0);
+          }
           write_units<32 * kPairBuild>(words, st, t, t < half, nu);
           if (((g0 + kUnits) & 31) == 0) held = hold_units(list, g0 + kUnits + lane, units, per);
         } else bad |= wrote = clean_units<32 * kPairBuild>(st, t, nu);
         if (wrote) fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(mapa_u32(smem_u32(&built[s]), 0));
-        if (writes && g0 + kUnits < units) read_units(src, at, g0 + kUnits, min(kUnits, units - g0 - kUnits), per, words);
+        if (lane == 0) mbar_arrive(&built[s]);
         if (++s == static_cast<uint32_t>(kPairStages)) s = 0;
       }
       bad = __any_sync(0xffffffffu, bad);
