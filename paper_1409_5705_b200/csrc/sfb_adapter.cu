@@ -694,9 +694,9 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // The pair that finishes a tile has its term.
 //
 // Warps: 0 TMA producer, 1 MMA issuer (leader CTA) and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the columns), 10..13
-// the samples' operand of the term and the loads of its factors, 14..17 the look at them, 18..20 hand the other CTA's on to the leader.
+// the samples' operand of the term and the loads of its factors, 14..17 the look at them, 18 and 19 hand the other CTA's on to the leader.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kPairBuild = 4, kHand = 3, kPairThreads = 32 * (2 + kEpi + 2 * kPairBuild + kHand), kGroup = 8;      // kGroup: tiles of samples that follow one another
+constexpr int kPairBuild = 4, kHand = 2, kPairThreads = 32 * (2 + kEpi + 2 * kPairBuild + kHand), kGroup = 8;      // kGroup: tiles of samples that follow one another
 constexpr int kPairStages = 6, kPairStage = 2 * kTileBytesA;
 constexpr int kPairSmem = kPairStages * kPairStage + 128 * SFB_ADAPTER_MAX_RANK * 2 + 1024;      // (behind the stages: a row of pb per writing thread)
 constexpr int kPartFloats = BM * kMaxTile;          // what a CTA leaves of a tile
@@ -930,7 +930,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     // ---------------- hand on the other CTA's operands ----------------
     // (A release to the cluster by each of the eight warps that make them took 1 us a k-block, and one warp, with no accesses of its own,
     // that hands all of them on is not much faster: these take them in turn.  Gradients of 1,024 samples of 64 adapters, 1,000 x 20,000: 98,
-    // 89 and 78 us.)
+    // 89 and 76 us.)
     uint32_t s = 0, bph = 0, turn = warp - 2 - kEpi - 2 * kPairBuild;
     bool ok = true;
     for (int i = 0; i < segs.n && ok && rank == 1; ++i) {
@@ -1237,18 +1237,20 @@ __global__ void __launch_bounds__(256) adapter_words_kernel(const __grid_constan
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// dF[a] = sum_{i of a} (scale p_i) z_i^T for a tile of 128 columns of z: the columns are the accumulator's rows, the ranks of the three
-// words its columns (added at the end), the samples the contraction, 64 of them at a time, gathered in the order of adapter_index_kernel
-// (so no sample of another adapter is in the product).
+// dF[a] = sum_{i of a} (scale p_i) z_i^T for a tile of 256 columns of z (128 where the ranks fill the accumulators): the columns are the
+// rows of two accumulators, the ranks of the three words their columns (added at the end), the samples the contraction, 64 of them at a
+// time, gathered in the order of adapter_index_kernel (so no sample of another adapter is in the product).
 // Warps: 0..7 loaders (asynchronous copies of 16 bytes into both operands, which arrive at the stage's barrier by themselves: a loader that
-// waited for its copies and fenced them had one k-block under way), 8 MMA issuer and TMEM owner, 9..16 epilogue, four of them a
-// tile in turn.
+// waited for its copies and fenced them had one k-block under way), 8 MMA issuer and TMEM owner, 9..16 epilogue, four of them a half of
+// the columns.
+// Bound by the instructions around a k-block, of which an adapter with few samples has one a tile: 1,024 samples of 64 adapters, 21,000
+// columns, 8 ranks: 63 us with tiles of 128 columns, 40 with 256.
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kLoaders = 8, kGradThreads = 32 * (kLoaders + 9), kGradBuffers = 8, kGradStages = 8, kGradRing = 196608;
 struct GradSide {
   const __nv_bfloat16* z;      // [n][ldz]
   int64_t ldz;
-  int32_t width, tiles;        // columns; tiles of 128 of them (0: not wanted)
+  int32_t width, tiles;        // columns; tiles of them (0: not wanted)
   const __nv_bfloat16* words;
   float* out;                  // [adapters][rank][width]
 };
@@ -1259,7 +1261,11 @@ struct GradParams {
   const int64_t* work;
   uint32_t* status;
 };
+// Columns of an accumulator for the three words of all ranks; halves of a tile; panels of 64 ranks; bytes of a stage.
+__host__ __device__ inline int grad_pitch(int rank) { return (3 * ((rank + 15) / 16 * 16) + 31) / 32 * 32; }
+__host__ __device__ inline int grad_halves(int rank) { return grad_pitch(rank) <= 256 ? 2 : 1; }
 __host__ __device__ inline int grad_panels(int rank) { return (3 * ((rank + 15) / 16 * 16) + 63) / 64; }
+__host__ __device__ inline int grad_stage(int rank) { return grad_halves(rank) * kTileBytesA + grad_panels(rank) * 8192; }
 
 // A block's tiles: those whose work begins in its share of all work, the columns of an adapter one after another, so that a block
 // keeps an adapter's samples at hand.
@@ -1304,19 +1310,19 @@ struct GradWalk {
 };
 
 __device__ __forceinline__ void grad_load(const GradParams& p, uint8_t* smem, uint64_t* full, uint64_t* empty, volatile uint32_t* abort_flag) {
-  const int rp = (p.rank + 15) & ~15, pieces = 3 * rp / 8, stage = kTileBytesA + grad_panels(p.rank) * 8192;
+  const int rp = (p.rank + 15) & ~15, pieces = 3 * rp / 8, stage = grad_stage(p.rank), halves = grad_halves(p.rank), shift = halves + 3;
   const int tid = threadIdx.x;
-  // of z: pieces of 16 bytes, c16 of the rows r0, r0 + 16, ..; of the words: pieces wc, wc + 4, .. of row wr
-  const int c16 = tid & 15, r0 = tid >> 4, wr = tid >> 2, wc = tid & 3;
+  // of z: pieces of 16 bytes, c of the rows r0, r0 + step, ..; of the words: pieces wc, wc + 4, .. of row wr
+  const int c = tid & ((1 << shift) - 1), r0 = tid >> shift, step = (32 * kLoaders) >> shift, wr = tid >> 2, wc = tid & 3;
   const uint32_t base = smem_u32(smem);
-  const uint32_t to_z = (c16 >> 3) * (kTileBytesA / 2) + r0 * 128 + (((c16 & 7) ^ (r0 & 7)) << 4), to_w = kTileBytesA + wr * 128;
+  const uint32_t to_z = (c >> 3) * (kTileBytesA / 2) + r0 * 128 + (((c & 7) ^ (r0 & 7)) << 4), to_w = halves * kTileBytesA + wr * 128;
   uint32_t s = 0, ph = 0;
   int known = -1, known_k = -1;                      // the adapter and the k-block of the samples in row
-  int32_t row[4];
+  int32_t row[8];
   for (GradWalk it(p); it.valid(); it.next()) {
     const GradSide& sd = p.side[it.side];
     const int nk = (it.count + BK - 1) / BK;
-    const int col = it.tile * BM + c16 * 8, left = sd.width - col;
+    const int col = it.tile * (halves * BM) + c * 8, left = sd.width - col;
     const uint32_t bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;
     const __nv_bfloat16* z = sd.z + (bytes ? col : 0);
     const __nv_bfloat16* words = sd.words + (static_cast<int64_t>(it.begin) + wr) * 3 * rp + wc * 8;
@@ -1324,7 +1330,7 @@ __device__ __forceinline__ void grad_load(const GradParams& p, uint8_t* smem, ui
       const int here = it.count - k * BK;            // samples from here on
       if (known != it.a || known_k != k) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) row[j] = r0 + j * 16 < here ? p.order[it.begin + k * BK + r0 + j * 16] : -1;
+        for (int j = 0; j < 8; ++j) row[j] = r0 + j * step < min(here, BK) ? p.order[it.begin + k * BK + r0 + j * step] : -1;
         known = it.a;
         known_k = k;
       }
@@ -1332,8 +1338,10 @@ __device__ __forceinline__ void grad_load(const GradParams& p, uint8_t* smem, ui
       if (!mbar_wait(&empty[s], ph ^ 1, abort_flag)) return;
       const uint32_t st = base + s * stage;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (j * 16 < rows) cp_async_16(st + to_z + j * 2048, row[j] >= 0 ? z + row[j] * sd.ldz : z, row[j] >= 0 ? bytes : 0);
+      for (int j = 0; j < 8; ++j) {
+        if (j * step >= rows) break;
+        cp_async_16(st + to_z + j * step * 128, row[j] >= 0 ? z + row[j] * sd.ldz : z, row[j] >= 0 ? bytes : 0);
+      }
       if (wr < rows) {
         const uint32_t b = wr < here ? 16 : 0;
         const __nv_bfloat16* from = b ? words : sd.words;
@@ -1354,10 +1362,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   volatile uint32_t* abort_flag = &abort_word;
   const int warp = warp_index(), lane = threadIdx.x & 31;
-  const int rp = (p.rank + 15) & ~15, N = 3 * rp, stage = kTileBytesA + grad_panels(p.rank) * 8192;
-  // Accumulators of `pitch` columns, each epilogue group's own ones (so that it sees all phases of their barriers); one group where there
-  // is one accumulator.
-  const uint32_t pitch = (N + 31) & ~31, all = min(static_cast<uint32_t>(kGradBuffers), 512 / pitch), groups = all > 1 ? 2 : 1, each = all / groups;
+  const int rp = (p.rank + 15) & ~15, N = 3 * rp, stage = grad_stage(p.rank);
+  const uint32_t pitch = grad_pitch(p.rank), halves = grad_halves(p.rank), each = min(static_cast<uint32_t>(kGradBuffers), 512 / pitch) / halves;
   pdl_launch_dependents();
   if (threadIdx.x == 0) {
     for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 32 * kLoaders); mbar_init(&empty[i], 1); }
@@ -1378,15 +1384,13 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
     // more than 256 columns: 192 (three panels), then the rest
     const uint32_t n1 = N <= 256 ? N : 192, n2 = N - n1;
     const uint32_t idesc1 = umma_idesc_bf16(BM, n1) | kIdescMnMajor, idesc2 = umma_idesc_bf16(BM, n2 ? n2 : 16) | kIdescMnMajor;
-    uint32_t s = 0, ph = 0, used[2] = {0, 0}, g = groups - 1;  // used: accumulators of a group so far; g: whose tile this is
+    uint32_t s = 0, ph = 0, b = 0, bph = 0;          // stage and phase; accumulator (of each half) and phase
     bool ok = true;
     for (GradWalk it(p); it.valid() && ok; it.next()) {
-      g = groups - 1 - g;
-      uint32_t i = g ? used[1] : used[0];
       const int nk = (it.count + BK - 1) / BK;
-      for (int k0 = 0; k0 < nk && ok; k0 += kDrain, ++i) {
-        const uint32_t b = g * each + i % each, bph = (i / each) & 1, d_tmem = tmem_base + b * pitch;
-        if (!mbar_wait_warp(&tempty[b], bph ^ 1, abort_flag)) { ok = false; break; }
+      for (int k0 = 0; k0 < nk && ok; k0 += kDrain) {
+        for (uint32_t h = 0; h < halves && ok; ++h) ok = mbar_wait_warp(&tempty[h * each + b], bph ^ 1, abort_flag);
+        if (!ok) break;
         tc_fence_after();
         for (int k = k0; k < min(k0 + kDrain, nk); ++k) {
           if (!mbar_wait_warp(&full[s], ph, abort_flag)) { ok = false; break; }
@@ -1394,58 +1398,71 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
           tc_fence_after();
           const int steps = min(BK / 16, (it.count - k * BK + 15) / 16);
           if (elect_one()) {
-            const uint32_t st = smem_u32(smem + s * stage);
-            const uint64_t da = umma_desc_mn128(st), db = umma_desc_mn128(st + kTileBytesA), db2 = umma_desc_mn128(st + kTileBytesA + 3 * 8192);
-            for (int j = 0; j < steps; ++j) {
-              umma_bf16(d_tmem, da + 128 * j, db + 128 * j, idesc1, (k - k0) | j ? 1u : 0u);
-              if (n2) umma_bf16(d_tmem + 192, da + 128 * j, db2 + 128 * j, idesc2, (k - k0) | j ? 1u : 0u);
+            const uint32_t st = smem_u32(smem + s * stage), bt = st + halves * kTileBytesA;
+            const uint64_t db = umma_desc_mn128(bt), db2 = umma_desc_mn128(bt + 3 * 8192);
+            for (uint32_t h = 0; h < halves; ++h) {
+              const uint64_t da = umma_desc_mn128(st + h * kTileBytesA);
+              const uint32_t d_tmem = tmem_base + (h * each + b) * pitch;
+              for (int j = 0; j < steps; ++j) {
+                umma_bf16(d_tmem, da + 128 * j, db + 128 * j, idesc1, (k - k0) | j ? 1u : 0u);
+                if (n2) umma_bf16(d_tmem + 192, da + 128 * j, db2 + 128 * j, idesc2, (k - k0) | j ? 1u : 0u);
+              }
             }
             umma_commit(&empty[s]);
           }
           if (++s == static_cast<uint32_t>(p.stages)) { s = 0; ph ^= 1; }
         }
-        if (ok && elect_one()) umma_commit(&tfull[b]);
+        if (ok && elect_one())
+          for (uint32_t h = 0; h < halves; ++h) umma_commit(&tfull[h * each + b]);
+        if (++b == each) { b = 0; bph ^= 1; }
       }
-      (g ? used[1] : used[0]) = i;
     }
   } else {
     const int q = warp & 3;
-    const uint32_t mine = (warp - kLoaders - 1) >> 2;
-    uint32_t i = 0, g = groups - 1;
-    bool ok = mine < groups;
+    const uint32_t h = (warp - kLoaders - 1) >> 2;
+    uint32_t b = 0, bph = 0;
+    bool ok = h < halves;
     for (GradWalk it(p); it.valid() && ok; it.next()) {
-      g = groups - 1 - g;
-      if (g != mine) continue;
       const GradSide& sd = p.side[it.side];
-      const int m = it.tile * BM + q * 32 + lane, nk = (it.count + BK - 1) / BK;
-      float* out = sd.out + static_cast<int64_t>(it.a) * p.rank * sd.width + m;
-      if (nk == 0 && m < sd.width)
-        for (int r = 0; r < p.rank; ++r) out[static_cast<int64_t>(r) * sd.width] = 0.f;
-      for (int k0 = 0; k0 < nk; k0 += kDrain, ++i) {
-        const uint32_t b = mine * each + i % each, bph = (i / each) & 1;
-        if (!mbar_wait_warp(&tfull[b], bph, abort_flag)) { ok = false; break; }
+      const int m = (it.tile * static_cast<int>(halves) + static_cast<int>(h)) * BM + q * 32 + lane, nk = (it.count + BK - 1) / BK;
+      const bool in = m < sd.width;
+      const int64_t width = sd.width;
+      float* const out = sd.out + static_cast<int64_t>(it.a) * p.rank * width + m;
+      if (nk == 0 && in) {
+        float* to = out;
+        for (int r = 0; r < p.rank; ++r, to += width) *to = 0.f;
+      }
+      for (int k0 = 0; k0 < nk; k0 += kDrain) {
+        if (!mbar_wait_warp(&tfull[h * each + b], bph, abort_flag)) { ok = false; break; }
         tc_fence_after();
-        const uint32_t t_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + b * pitch;
+        const uint32_t t_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + (h * each + b) * pitch;
+        float* to = out;
 #pragma unroll 1
-        for (int r0 = 0; r0 < p.rank; r0 += 16) {
-          uint32_t w0[16], w1[16], w2[16];
-          float old[16];
-#pragma unroll
-          for (int j = 0; j < 16; ++j) old[j] = k0 && m < sd.width && r0 + j < p.rank ? out[static_cast<int64_t>(r0 + j) * sd.width] : 0.f;
-          tmem_ld_32x16(t_addr + r0, w0);
-          tmem_ld_32x16(t_addr + rp + r0, w1);
-          tmem_ld_32x16(t_addr + 2 * rp + r0, w2);
+        for (int r0 = 0; r0 < p.rank; r0 += 8, to += 8 * width) {
+          uint32_t w0[8], w1[8], w2[8];
+          tmem_ld_32x8(t_addr + r0, w0);
+          tmem_ld_32x8(t_addr + rp + r0, w1);
+          tmem_ld_32x8(t_addr + 2 * rp + r0, w2);
           tmem_ld_wait();
-          if (m < sd.width) {
+          float v[8];
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-              if (r0 + j < p.rank)
-                out[static_cast<int64_t>(r0 + j) * sd.width] = __uint_as_float(w0[j]) + (__uint_as_float(w1[j]) + __uint_as_float(w2[j])) + old[j];
+          for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w0[j]) + (__uint_as_float(w1[j]) + __uint_as_float(w2[j]));
+          const int live = in ? p.rank - r0 : 0;
+          if (k0) {
+            float old[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) old[j] = j < live ? to[j * width] : 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += old[j];
           }
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j < live) to[j * width] = v[j];
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&tempty[b]);
+        if (lane == 0) mbar_arrive(&tempty[h * each + b]);
+        if (++b == each) { b = 0; bph ^= 1; }
       }
     }
   }
@@ -1848,13 +1865,14 @@ extern "C" int sfb_adapter_backward(sfb_adapters* h, int64_t n, const void* dY_d
     w.ids = ids_dev; w.order = order; w.begin = begin; w.count = count; w.work = h->at<int64_t>(h->lay.work); w.scale = h->scale; w.rank = c.rank; w.adapters = c.adapters;
     ACK(launch_kernel(adapter_words_kernel, dim3(grid1d(n * ((c.rank + 15) / 16 * 2), 256), 3), dim3(256), 0, h->stream, 1, w));
     GradParams p{};
+    const int tile = grad_halves(c.rank) * BM;
     if (dU_dev)
-      p.side[0] = GradSide{static_cast<const __nv_bfloat16*>(dY_dev), lddy, static_cast<int32_t>(c.rows), static_cast<int32_t>((c.rows + BM - 1) / BM), swords, dU_dev};
+      p.side[0] = GradSide{static_cast<const __nv_bfloat16*>(dY_dev), lddy, static_cast<int32_t>(c.rows), static_cast<int32_t>((c.rows + tile - 1) / tile), swords, dU_dev};
     if (dV_dev)
-      p.side[1] = GradSide{static_cast<const __nv_bfloat16*>(X_dev), ldx, static_cast<int32_t>(c.cols), static_cast<int32_t>((c.cols + BM - 1) / BM), twords, dV_dev};
+      p.side[1] = GradSide{static_cast<const __nv_bfloat16*>(X_dev), ldx, static_cast<int32_t>(c.cols), static_cast<int32_t>((c.cols + tile - 1) / tile), twords, dV_dev};
     p.rank = c.rank; p.adapters = c.adapters; p.order = order; p.begin = begin; p.count = count; p.work = w.work; p.status = status;
     const int64_t items = (static_cast<int64_t>(p.side[0].tiles) + p.side[1].tiles) * c.adapters;
-    const int stage = kTileBytesA + grad_panels(c.rank) * 8192;
+    const int stage = grad_stage(c.rank);
     p.stages = std::min(kGradStages, kGradRing / stage);
     const int smem = p.stages * stage + 1024;
     ACK(allow_smem<adapter_gradient_kernel>(kGradRing + 1024));
