@@ -1106,6 +1106,36 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
 }
 
 // ---------------------------------------------------------------------------------------------------------
+// [rows][pitch_in] to [rows][pitch_out], `pieces` of 16 bytes a row.  A row of a box is 128 bytes, four sectors of L2; where the rows of an
+// operand are an odd multiple of 16 bytes apart, half of them are five, and the products of many samples, which move their operands
+// through L2 at its rate, take up to 1.4 times as long (8,192 samples, 10,000 x 5,000 in a loop: pitches of 5,000 entries 997 us, 5,008 774,
+// 5,056 720).  Such operands are copied where the copy, 4 bytes an entry at HBM's rate, costs less than that: from 2,100 uses of a row on.
+// ---------------------------------------------------------------------------------------------------------
+constexpr int64_t kCopyUses = 4096;
+__global__ void __launch_bounds__(256) adapter_copy_kernel(const uint4* in, int64_t pitch_in, uint4* out, int64_t pitch_out, int64_t rows, int64_t pieces) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int64_t step = static_cast<int64_t>(gridDim.x) * 256, step_r = step / pieces, step_c = step - step_r * pieces;
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  int64_t r = first / pieces, c = first - r * pieces;
+  while (r < rows) {
+    uint4 v[4];
+    int64_t to[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      to[u] = r < rows ? r * pitch_out + c : -1;
+      if (r < rows) v[u] = __ldcs(in + r * pitch_in + c);
+      r += step_r;
+      c += step_c;
+      if (c >= pieces) { c -= pieces; ++r; }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (to[u] >= 0) out[to[u]] = v[u];
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------
 // The samples of each adapter, one adapter after another, in their order: a block per adapter, each of its warps over an eighth of the
 // ids, counts the samples of lower adapters and its own, then writes its own.  No sample without an adapter is among them.
 // ---------------------------------------------------------------------------------------------------------
@@ -1497,8 +1527,10 @@ int64_t rank_rows(int64_t n, int64_t d) {
   return std::max(most, n);
 }
 
+bool pitch_odd(int64_t pitch) { return pitch % 16 != 0; }      // of bf16 entries: not a multiple of 32 bytes
+
 struct AdapterLayout {
-  size_t status, ready, arrived, s, t, ssum, tsum, pb, swords, twords, order, begin, count, work, lists, place, partial, total;
+  size_t status, ready, arrived, s, t, ssum, tsum, pb, swords, twords, order, begin, count, work, lists, place, partial, wcopy, zcopy, total;
 };
 
 int check(const sfb_adapter_config* c) {
@@ -1531,6 +1563,11 @@ AdapterLayout layout_of(const sfb_adapter_config& c) {
   L.lists = take((n / kMaxTile + 1) * kListPitch * 4);
   L.place = take(n * 4);
   L.partial = take(n > kFewMost ? static_cast<size_t>(kModelSms) * kPartFloats * 4 : 0);
+  // copies of operands whose rows, without gaps between them, are an odd multiple of 16 bytes apart (see adapter_copy_kernel)
+  const bool odd_w = pitch_odd(c.ldw ? c.ldw : c.cols) && c.max_samples >= kCopyUses;
+  const bool odd_x = pitch_odd(round_up(c.cols, 8)) && c.rows >= kCopyUses, odd_y = pitch_odd(round_up(c.rows, 8)) && c.cols >= kCopyUses;
+  L.wcopy = take(odd_w ? static_cast<size_t>(c.rows) * round_up(c.cols, BK) * 2 : 0);
+  L.zcopy = take(n <= kFewMost ? 0 : std::max(odd_x ? n * round_up(c.cols, BK) * 2 : 0, odd_y ? n * round_up(c.rows, BK) * 2 : 0));
   L.order = take(n * 4);
   L.begin = take(static_cast<size_t>(c.adapters) * 4);
   L.work = take((static_cast<size_t>(c.adapters) + 1) * 8);
@@ -1653,6 +1690,18 @@ int few_parts(int64_t tiles, int64_t kseg) {
   return best;
 }
 
+// A bf16 operand [outer x inner] where the products take it: itself, or a copy in `room`, with *pitch entries from row to row.
+cudaError_t placed(sfb_adapters* h, const void** at, int64_t* pitch, int64_t outer, int64_t inner, int64_t uses, size_t room, size_t bytes) {
+  const int64_t to = round_up(inner, BK);
+  if (!pitch_odd(*pitch) || uses < kCopyUses || bytes < static_cast<size_t>(outer) * to * 2) return cudaSuccess;
+  uint4* copy = h->at<uint4>(room);
+  const cudaError_t e = launch_kernel(adapter_copy_kernel, dim3(grid1d(outer * ((inner + 7) / 8), 1024)), dim3(256), 0, h->stream, 1,
+                                      static_cast<const uint4*>(*at), *pitch / 8, copy, to / 8, outer, (inner + 7) / 8);
+  *at = copy;
+  *pitch = to;
+  return e;
+}
+
 // What adapter_rank_kernel or adapter_sum_kernel leaves for the products.
 template <bool MN>
 Term term_of(const sfb_adapters* h, const int32_t* ids, const float* p) {
@@ -1706,8 +1755,12 @@ cudaError_t pairs(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const 
   const sfb_adapter_config& c = h->cfg;
   const int64_t m = MN ? c.cols : c.rows, d = MN ? c.rows : c.cols;
   const int tn = tile_of(n);
+  const void* W = h->W;
+  int64_t ldw = c.ldw;
+  cudaError_t e = placed(h, &W, &ldw, c.rows, c.cols, n, h->lay.wcopy, h->lay.zcopy - h->lay.wcopy);
+  if (e != cudaSuccess) return e;
   CUtensorMap ma, mz;
-  if (!operand_map(h, &ma, h->W, c.cols, c.rows, c.ldw, BK, MN ? BK : BM, CU_TENSOR_MAP_L2_PROMOTION_NONE) ||
+  if (!operand_map(h, &ma, W, c.cols, c.rows, ldw, BK, MN ? BK : BM, CU_TENSOR_MAP_L2_PROMOTION_NONE) ||
       !operand_map(h, &mz, Z, d, n, ldz, BK, tn / 2, CU_TENSOR_MAP_L2_PROMOTION_NONE))
     return cudaErrorInvalidValue;
   PairParams p{};
@@ -1825,6 +1878,7 @@ extern "C" int sfb_adapter_forward(sfb_adapters* h, int64_t n, const void* X_dev
   ACK(on.err);
   Ranked s{};
   float* sum = S_dev ? S_dev : h->at<float>(h->lay.ssum);
+  if (n > kFewMost) ACK(placed(h, &X_dev, &ldx, n, c.cols, c.rows, h->lay.zcopy, h->lay.order - h->lay.zcopy));
   ACK(rank_products<false>(h, n, X_dev, ldx, ids_dev, h->at<float>(h->lay.s), sum, &s));
   ACK(product<false>(h, n, X_dev, ldx, ids_dev, &s, sum, Y_dev, ldy));
   return SFB_OK;
@@ -1855,8 +1909,11 @@ extern "C" int sfb_adapter_backward(sfb_adapters* h, int64_t n, const void* dY_d
                       begin, count, status));
   Ranked s{S_dev, 1, 0}, t{};
   if (dU_dev && !S_dev) ACK(rank_products<false>(h, n, X_dev, ldx, ids_dev, h->at<float>(h->lay.s), h->at<float>(h->lay.ssum), &s));
-  if (dX_dev || dV_dev) ACK(rank_products<true>(h, n, dY_dev, lddy, ids_dev, h->at<float>(h->lay.t), h->at<float>(h->lay.tsum), &t));
-  if (dX_dev) ACK(product<true>(h, n, dY_dev, lddy, ids_dev, &t, h->at<float>(h->lay.tsum), dX_dev, lddx));
+  const void* Z = dY_dev;
+  int64_t ldz = lddy;
+  if (dX_dev && n > kFewMost) ACK(placed(h, &Z, &ldz, n, c.rows, c.cols, h->lay.zcopy, h->lay.order - h->lay.zcopy));
+  if (dX_dev || dV_dev) ACK(rank_products<true>(h, n, Z, ldz, ids_dev, h->at<float>(h->lay.t), h->at<float>(h->lay.tsum), &t));
+  if (dX_dev) ACK(product<true>(h, n, Z, ldz, ids_dev, &t, h->at<float>(h->lay.tsum), dX_dev, lddx));
   if (dU_dev || dV_dev) {
     __nv_bfloat16 *swords = h->at<__nv_bfloat16>(h->lay.swords), *twords = h->at<__nv_bfloat16>(h->lay.twords);
     WordsParams w{};

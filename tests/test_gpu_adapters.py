@@ -154,6 +154,12 @@ SIZES = [
     (64, 20001, 130, 9, 128, "mixed"),
     (29, 18944, 264, 29, 8, "every"),
     (40, 300, 9001, 4, 20, "mixed"),
+    # operands that are copied first: rows an odd multiple of 16 bytes apart (X and dY; W)
+    (70, 5000, 4104, 3, 16, "mixed"),
+    (4100, 72, 136, 3, 24, "runs"),
+    # as many samples of one adapter as are taken out of the accumulators in several turns; the widest adapters
+    (3000, 300, 200, 1, 20, "one"),
+    (900, 136, 264, 2, 128, "mixed"),
 ]
 
 
