@@ -127,6 +127,7 @@ constexpr int kRankThreads = 320, kRankTile = 128, kFewChunks = 64;
 struct RankParams {
   int32_t n, tn, kseg, stages;
   int32_t rank, adapters;
+  int32_t boxed;               // slices that one copy of factors brings
   const int32_t* ids;
   float* out;                  // [parts][n][rank]
   uint32_t* status;
@@ -204,7 +205,7 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
           mbar_expect_tx(&full[s], ns * (kSlice * BK * 2) + p.tn * BK * 2);
           uint8_t* st = smem + s * stage;
           tma_load_2d(st + kTileBytesA, &tmZ, k * BK, first, &full[s]);
-          for (int j = 0; j < ns; ++j) {
+          for (int j = 0; j < ns; j += p.boxed) {
             const int g = c * 8 + j, at = g / per;
             tma_load_3d(st + j * (kSlice * BK * 2), &tmF, k * BK, (g - at * per) * kSlice, L.list[at], &full[s]);
           }
@@ -1589,9 +1590,9 @@ struct sfb_adapters {
   char* ws;
   cudaStream_t stream;
   int device, last_cuda, max_pairs;
-  CUtensorMap mapU, mapV;              // boxes of 64 entries x 16 ranks of an adapter
+  CUtensorMap mapU, mapV;              // boxes of 64 entries x `boxed_slices` times 16 ranks of an adapter
   CUtensorMap unitU, unitV;            // x `boxed` units of 8 ranks
-  int32_t boxed;
+  int32_t boxed, boxed_slices;
   sfb::EncodeTiledFn encode;           // cuTensorMapEncodeTiled
 
   template <typename T>
@@ -1661,7 +1662,7 @@ cudaError_t rank_products(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz
   RankParams p{};
   p.n = static_cast<int32_t>(n); p.tn = tn; p.kseg = static_cast<int32_t>((d + BK - 1) / BK);
   p.stages = std::min(kMaxStages, (n <= kFewMost ? kFewRing : kSmallRing) / stage_bytes(tn));
-  p.rank = c.rank; p.adapters = c.adapters; p.ids = ids; p.out = out; p.status = h->at<uint32_t>(h->lay.status);
+  p.rank = c.rank; p.adapters = c.adapters; p.boxed = h->boxed_slices; p.ids = ids; p.out = out; p.status = h->at<uint32_t>(h->lay.status);
   const int per = (c.rank + kSlice - 1) / kSlice, chunks = (std::min(tn, c.adapters) * per + 7) / 8;
   const int smem = p.stages * stage_bytes(tn) + 1024;
   if (n <= kFewMost) {
@@ -1851,9 +1852,10 @@ extern "C" int sfb_adapter_init(const sfb_adapter_config* cfg, const void* W_dev
   h->device = dev;
   h->last_cuda = 0;
   h->max_pairs = std::min(sm_count(), kModelSms) / 2;
-  h->boxed = 1;
+  h->boxed = h->boxed_slices = 1;
+  while (h->boxed_slices < 8 && (c.rank + kSlice - 1) / kSlice % (2 * h->boxed_slices) == 0) h->boxed_slices *= 2;
   while (h->boxed < kUnits && (c.rank + kUnit - 1) / kUnit % (2 * h->boxed) == 0) h->boxed *= 2;
-  if (!factor_map(h, &h->mapU, U_dev, c.rows, c.ldu, kSlice) || !factor_map(h, &h->mapV, V_dev, c.cols, c.ldv, kSlice) ||
+  if (!factor_map(h, &h->mapU, U_dev, c.rows, c.ldu, kSlice * h->boxed_slices) || !factor_map(h, &h->mapV, V_dev, c.cols, c.ldv, kSlice * h->boxed_slices) ||
       !factor_map(h, &h->unitU, U_dev, c.rows, c.ldu, kUnit * h->boxed) || !factor_map(h, &h->unitV, V_dev, c.cols, c.ldv, kUnit * h->boxed) ||
       prepare_pair_kernel(adapter_pair_kernel<false>, kPairThreads, kPairSmem, &h->max_pairs) != cudaSuccess ||
       prepare_pair_kernel(adapter_pair_kernel<true>, kPairThreads, kPairSmem, &h->max_pairs) != cudaSuccess || h->max_pairs < 1 ||
