@@ -13,7 +13,7 @@
 
 #include <algorithm>
 #include <cmath>
-#include <new>
+#include <exception>
 #include <vector>
 
 #include "sfb_internal.h"
@@ -339,7 +339,7 @@ extern "C" int sfb_clip_init(int64_t tensors, const void* const* src, void* cons
   if (workspace_bytes < need) return SFB_ERR_WORKSPACE;
   try {
     if (overlapping(tensors, src, dst, counts, dtypes)) return SFB_ERR_ARG;
-  } catch (const std::bad_alloc&) {
+  } catch (const std::exception&) {
     return SFB_ERR_ARG;
   }
   int dev = 0, major = 0;
@@ -369,7 +369,7 @@ extern "C" int sfb_clip_init(int64_t tensors, const void* const* src, void* cons
       if (e == cudaSuccess) e = cudaStreamSynchronize(h->stream);
       if (e != cudaSuccess) { delete h; return SFB_ERR_CUDA; }
     }
-  } catch (const std::bad_alloc&) {
+  } catch (const std::exception&) {
     delete h;
     return SFB_ERR_ARG;
   }
