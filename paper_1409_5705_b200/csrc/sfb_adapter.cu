@@ -2,7 +2,7 @@
 // (a set of factor pairs) that its request names, and the gradients of the samples and of the adapters' factors.
 //
 // Launches of a forward pass:  adapter_rank_kernel (s = V x), then for y = W x + scale U^T s up to 64 samples adapter_few_kernel, for
-// more adapter_sum_kernel and adapter_pair_kernel;  of a backward pass:  adapter_index_kernel, adapter_rank_kernel (t = U dy; s again
+// more adapter_sum_kernel and adapter_pair_kernel (many samples: adapter_copy_kernel first, where rows lie badly);  of a backward pass:  adapter_index_kernel, adapter_rank_kernel (t = U dy; s again
 // where it is not given), the products as in a forward pass (dx), adapter_words_kernel and adapter_gradient_kernel (dU, dV).
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -461,8 +461,8 @@ __device__ __forceinline__ uint32_t clean_units(uint8_t* st, int t, int nu) {
   }
   return bad;
 }
-// Row t of the samples' operand of k-block k: scale p of a sample whose first unit is `at` (below zero: no adapter), and, beside an odd last
-// unit, zeros in the factors' operand (by threads x of `threads`).
+// Row t of the samples' operand of a k-block of `nu` units (row: this thread has one), and, beside an odd last unit, zeros in the factors'
+// operand.  By THREADS threads, t of them.
 template <int THREADS>
 __device__ __forceinline__ void write_units(const uint4 (&words)[kUnits], uint8_t* st, int t, bool row, int nu) {
   if (row) {
@@ -476,6 +476,7 @@ __device__ __forceinline__ void write_units(const uint4 (&words)[kUnits], uint8_
     for (int x = t; x < 128; x += THREADS)
       *reinterpret_cast<uint4*>(st + (x >> 6) * (kTileBytesA / 2) + nu * (kUnit * 128) + (x & 63) * 16) = make_uint4(0, 0, 0, 0);
 }
+// The words of the units [g0, g0 + nu) of a sample whose first unit is `at` (below zero: no adapter): zeros for those that are not its own.
 __device__ __forceinline__ void read_units(const uint4* src, int at, int g0, int nu, int per, uint4 (&words)[kUnits]) {
 #pragma unroll
   for (int j = 0; j < kUnits; ++j) {
@@ -506,7 +507,7 @@ struct FewParams {
   uint32_t* status;
 };
 
-// One k-block of A and z, or of factors, into a stage; by the producer's warp.
+// One k-block of A and z into a stage; by the producer's warp.
 template <int TN, bool MN>
 __device__ __forceinline__ void few_load(uint8_t* st, uint64_t* full, const CUtensorMap& tmA, const CUtensorMap& tmZ, int k, int m0, uint64_t keep) {
   if (!elect_one()) return;
@@ -1477,7 +1478,10 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
           tmem_ld_wait();
           float v[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w0[j]) + (__uint_as_float(w1[j]) + __uint_as_float(w2[j]));
+          for (int j = 0; j < 8; ++j) {               // (an infinite entry of z times a second word may be NaN, or the other infinity)
+            const float first = __uint_as_float(w0[j]), rest = __uint_as_float(w1[j]) + __uint_as_float(w2[j]);
+            v[j] = isfinite(first) ? first + rest : first;
+          }
           const int live = in ? p.rank - r0 : 0;
           if (k0) {
             float old[8];

@@ -219,6 +219,26 @@ def test_infinite_products_are_infinite():
     assert (got["dU"][1] == float("inf")).all()
 
 
+@pytest.mark.parametrize("rank", [4, 96])
+def test_gradients_of_infinite_entries_are_infinite(rank):
+    """An infinite entry of dy or x reaches dU or dV with the sign of the product, whatever the finite factor's lower bits are."""
+    n, d = 40, 64
+    c = Case(n, d, d, 2, rank, "one", seed=1)
+    c.scale.fill_(1.0)
+    c.V[1] = c.V[1].abs() + 0.25
+    c.U[1] = -c.U[1].abs() - 0.25
+    c.X.copy_(c.X.abs())
+    c.dY.copy_(c.dY.abs())
+    assert c.ids[3] == 1
+    c.dY[3, 7] = float("inf")
+    got = c.run()                                        # s > 0
+    keep = torch.arange(d, device="cuda") != 7
+    assert (got["dU"][1][:, 7] == float("inf")).all() and torch.isfinite(got["dU"][1][:, keep]).all()
+    c.dY[3, 7], c.X[3, 7] = 1.0, float("inf")
+    got = c.run()                                        # t < 0
+    assert (got["dV"][1][:, 7] == float("-inf")).all() and torch.isfinite(got["dV"][1][:, keep]).all()
+
+
 def test_ids_out_of_range_take_no_adapter_and_are_reported():
     c = Case(50, 100, 200, 4, 8, "mixed", seed=2)
     c.ids[7], c.ids[20], c.ids[49] = 4, -2, 2 ** 31 - 1
