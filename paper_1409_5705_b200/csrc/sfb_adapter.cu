@@ -159,8 +159,8 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
     fence_barrier_init();
     prefetch_tmap(&tmF); prefetch_tmap(&tmZ);
   }
-  if (warp == 1) { tmem_alloc(&tmem_slot, 2 * cols); tmem_relinquish(); }
   pdl_wait();
+  if (warp == 1) { tmem_alloc(&tmem_slot, 2 * cols); tmem_relinquish(); }
   pdl_launch_dependents();
   build_list(L, p.ids, first, p.n, p.tn, p.adapters, p.status);
   tc_fence_before();
@@ -545,7 +545,6 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   const int mine = static_cast<int>(blockIdx.x) % p.parts, m0 = static_cast<int>(blockIdx.x) / p.parts * BM;
   const int kbeg = mine * p.kseg / p.parts, nk = (mine + 1) * p.kseg / p.parts - kbeg;
   const int per = units_of(p.term);
-  pdl_launch_dependents();
   if (threadIdx.x == 0) {
     for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&landed[i], 1); mbar_init(&built[i], kBuild); }
     mbar_init(&done, 1);
@@ -557,6 +556,7 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_launch_dependents();                           // (not before this block has its columns of TMEM: the next launch takes some before it waits)
   const uint32_t tmem_base = tmem_slot;
 
   if (warp == 0) {
@@ -756,7 +756,6 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     m0 = at / width * (2 * BM) + static_cast<int>(rank) * BM;
     tt = g * kGroup + at % width;
   };
-  pdl_launch_dependents();
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kPairStages; ++i) {
@@ -773,6 +772,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   cluster_arrive();
   cluster_wait();
   tc_fence_after();
+  pdl_launch_dependents();
   const uint32_t tmem_base = tmem_slot;
   pdl_wait();
 
@@ -1276,7 +1276,8 @@ __global__ void __launch_bounds__(256) adapter_words_kernel(const __grid_constan
 // waited for its copies and fenced them had one k-block under way), 8 MMA issuer and TMEM owner, 9..16 epilogue, four of them a half of
 // the columns.
 // Bound by the instructions around a k-block, of which an adapter with few samples has one a tile: 1,024 samples of 64 adapters, 21,000
-// columns, 8 ranks: 63 us with tiles of 128 columns, 40 with 256.
+// columns, 8 ranks: 63 us with tiles of 128 columns, 40 with 256, 31 with two blocks an SM, which share its TMEM (up to 16 ranks: with more
+// a block has no second accumulator then, and 24 to 32 ranks take 1.2 times as long).
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kLoaders = 8, kGradThreads = 32 * (kLoaders + 9), kGradBuffers = 8, kGradStages = 8, kGradRing = 196608;
 struct GradSide {
@@ -1296,6 +1297,7 @@ struct GradParams {
 // Columns of an accumulator for the three words of all ranks; halves of a tile; panels of 64 ranks; bytes of a stage.
 __host__ __device__ inline int grad_pitch(int rank) { return (3 * ((rank + 15) / 16 * 16) + 31) / 32 * 32; }
 __host__ __device__ inline int grad_halves(int rank) { return grad_pitch(rank) <= 256 ? 2 : 1; }
+__host__ __device__ inline int grad_blocks(int rank) { return grad_pitch(rank) <= 64 ? 2 : 1; }           // that share an SM
 __host__ __device__ inline int grad_panels(int rank) { return (3 * ((rank + 15) / 16 * 16) + 63) / 64; }
 __host__ __device__ inline int grad_stage(int rank) { return grad_halves(rank) * kTileBytesA + grad_panels(rank) * 8192; }
 
@@ -1303,6 +1305,7 @@ __host__ __device__ inline int grad_stage(int rank) { return grad_halves(rank) *
 // keeps an adapter's samples at hand.
 struct GradWalk {
   const GradParams& p;
+  GradSide sd;
   int side, a, tile, count, begin;
   int64_t at, end;             // where the tile's work begins; the end of the block's share
   __device__ __forceinline__ GradWalk(const GradParams& p_) : p(p_) {
@@ -1310,11 +1313,15 @@ struct GradWalk {
     at = all * blockIdx.x / gridDim.x;
     end = all * (blockIdx.x + 1) / gridDim.x;
     side = at >= first;
-    const int64_t base = side ? first : 0, tiles = p.side[side].tiles;
-    int lo = 0, hi = p.adapters - 1;                 // the last adapter whose work begins at or before `at`
-    while (at < end && lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (base + p.work[mid] * tiles <= at) lo = mid; else hi = mid - 1;
+    sd = side ? p.side[1] : p.side[0];
+    const int64_t base = side ? first : 0, tiles = sd.tiles;
+    int lo = 0, len = at < end ? p.adapters : 1;     // the last adapter whose work begins at or before `at`
+    const int lane = threadIdx.x & 31;
+    while (len > 1) {
+      const int step = (len + 31) / 32, x = lane * step;
+      const int j = 31 - __clz(__ballot_sync(0xffffffffu, x < len && (x == 0 || base + p.work[lo + x] * tiles <= at)));
+      lo += j * step;
+      len = min(step, len - j * step);
     }
     a = lo;
     if (at >= end) return;
@@ -1326,10 +1333,13 @@ struct GradWalk {
   }
   __device__ __forceinline__ void load() { count = p.count[a]; begin = p.begin[a]; }
   __device__ __forceinline__ void settle() {
-    while (at < end && tile >= p.side[side].tiles) {
+    while (at < end && tile >= sd.tiles) {
       tile = 0;
-      if (++a == p.adapters) { a = 0; ++side; }
-      if (side > 1) { at = end; return; }
+      if (++a == p.adapters) {
+        a = 0;
+        if (++side > 1) { at = end; return; }
+        sd = p.side[1];
+      }
       load();
     }
   }
@@ -1352,7 +1362,7 @@ __device__ __forceinline__ void grad_load(const GradParams& p, uint8_t* smem, ui
   int known = -1, known_k = -1;                      // the adapter and the k-block of the samples in row
   int32_t row[8];
   for (GradWalk it(p); it.valid(); it.next()) {
-    const GradSide& sd = p.side[it.side];
+    const GradSide& sd = it.sd;
     const int nk = (it.count + BK - 1) / BK;
     const int col = it.tile * (halves * BM) + c * 8, left = sd.width - col;
     const uint32_t bytes = left >= 8 ? 16 : left > 0 ? left * 2 : 0;
@@ -1387,7 +1397,8 @@ __device__ __forceinline__ void grad_load(const GradParams& p, uint8_t* smem, ui
   cp_async_wait_all();
 }
 
-__global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const __grid_constant__ GradParams p) {
+template <int BLOCKS>
+__global__ void __launch_bounds__(kGradThreads, BLOCKS) adapter_gradient_kernel(const __grid_constant__ GradParams p) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kGradStages], empty[kGradStages], tfull[kGradBuffers], tempty[kGradBuffers];
   __shared__ uint32_t tmem_slot, abort_word;
@@ -1395,18 +1406,19 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
   volatile uint32_t* abort_flag = &abort_word;
   const int warp = warp_index(), lane = threadIdx.x & 31;
   const int rp = (p.rank + 15) & ~15, N = 3 * rp, stage = grad_stage(p.rank);
-  const uint32_t pitch = grad_pitch(p.rank), halves = grad_halves(p.rank), each = min(static_cast<uint32_t>(kGradBuffers), 512 / pitch) / halves;
-  pdl_launch_dependents();
+  constexpr uint32_t kColumns = 512 / BLOCKS;
+  const uint32_t pitch = grad_pitch(p.rank), halves = grad_halves(p.rank), each = min(static_cast<uint32_t>(kGradBuffers), kColumns / pitch) / halves;
   if (threadIdx.x == 0) {
     for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 32 * kLoaders); mbar_init(&empty[i], 1); }
     for (int i = 0; i < kGradBuffers; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 4); }
     abort_word = 0;
     fence_barrier_init();
   }
-  if (warp == kLoaders) { tmem_alloc(&tmem_slot, 512); tmem_relinquish(); }
+  if (warp == kLoaders) { tmem_alloc(&tmem_slot, kColumns); tmem_relinquish(); }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_launch_dependents();
   const uint32_t tmem_base = tmem_slot;
   pdl_wait();
 
@@ -1455,7 +1467,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
     uint32_t b = 0, bph = 0;
     bool ok = h < halves;
     for (GradWalk it(p); it.valid() && ok; it.next()) {
-      const GradSide& sd = p.side[it.side];
+      const GradSide& sd = it.sd;
       const int m = (it.tile * static_cast<int>(halves) + static_cast<int>(h)) * BM + q * 32 + lane, nk = (it.count + BK - 1) / BK;
       const bool in = m < sd.width;
       const int64_t width = sd.width;
@@ -1509,7 +1521,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) adapter_gradient_kernel(const
     for (int i = 0; i < 64; ++i) __nanosleep(1000);
     __syncthreads();
   }
-  if (warp == kLoaders) { tc_fence_after(); tmem_dealloc(tmem_base, 512); }
+  if (warp == kLoaders) { tc_fence_after(); tmem_dealloc(tmem_base, kColumns); }
 }
 
 // ---------------------------------------------------------------------------------------------------------
@@ -1936,10 +1948,17 @@ extern "C" int sfb_adapter_backward(sfb_adapters* h, int64_t n, const void* dY_d
     p.rank = c.rank; p.adapters = c.adapters; p.order = order; p.begin = begin; p.count = count; p.work = w.work; p.status = status;
     const int64_t items = (static_cast<int64_t>(p.side[0].tiles) + p.side[1].tiles) * c.adapters;
     const int stage = grad_stage(c.rank);
-    p.stages = std::min(kGradStages, kGradRing / stage);
+    const int blocks = grad_blocks(c.rank);
+    p.stages = std::min(kGradStages, kGradRing / blocks / stage);
     const int smem = p.stages * stage + 1024;
-    ACK(allow_smem<adapter_gradient_kernel>(kGradRing + 1024));
-    ACK(launch_kernel(adapter_gradient_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(items, sm_count()))), dim3(kGradThreads), smem, h->stream, 1, p));
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(items, blocks * sm_count())));
+    if (blocks == 2) {
+      ACK(allow_beside<adapter_gradient_kernel<2>>(kGradRing / 2 + 1024));
+      ACK(launch_kernel(adapter_gradient_kernel<2>, grid, dim3(kGradThreads), smem, h->stream, 1, p));
+    } else {
+      ACK(allow_smem<adapter_gradient_kernel<1>>(kGradRing + 1024));
+      ACK(launch_kernel(adapter_gradient_kernel<1>, grid, dim3(kGradThreads), smem, h->stream, 1, p));
+    }
   }
   return SFB_OK;
 }
