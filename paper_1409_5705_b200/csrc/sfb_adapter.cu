@@ -1,9 +1,11 @@
 // Low-rank adapters of many requests beside the shared W (sfb_adapter_* in sfb.h): the logits of samples, each with the adapter
 // (a set of factor pairs) that its request names, and the gradients of the samples and of the adapters' factors.
 //
-// Launches of a forward pass:  adapter_rank_kernel (s = V x), then for y = W x + scale U^T s up to 64 samples adapter_few_kernel, for
-// more adapter_sum_kernel and adapter_pair_kernel (many samples: adapter_copy_kernel first, where rows lie badly);  of a backward pass:  adapter_index_kernel, adapter_rank_kernel (t = U dy; s again
-// where it is not given), the products as in a forward pass (dx), adapter_words_kernel and adapter_gradient_kernel (dU, dV).
+// Launches of a forward pass of up to 64 samples:  adapter_rank_kernel (s = V x), adapter_few_kernel (y = W x + scale U^T s).  Of more:
+// adapter_index_kernel and adapter_copy_kernel (where the samples had better be taken in the order of their adapters, or copied because of the
+// way their rows lie), adapter_rank_kernel, adapter_sum_kernel (what follows s), adapter_pair_kernel (y).
+// Of a backward pass:  adapter_index_kernel (the samples of each adapter), the products as in a forward pass (t = U dy, dx), adapter_words_kernel
+// where adapter_sum_kernel has not done its work, adapter_gradient_kernel (dU, dV).
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -111,6 +113,14 @@ __device__ __forceinline__ float ranked(const Ranked& s, int64_t at) {
   return v;
 }
 
+// Where adapter_index_kernel has found that it pays, more than 64 samples are taken in the order of their adapters: position i is sample
+// order[i] then.  (sorted null: never.)
+struct Sorting {
+  const uint32_t* sorted;
+  const int32_t *order, *ids;  // of the positions
+  __device__ __forceinline__ bool on() const { return sorted && *sorted; }
+};
+
 constexpr int kUnit = 8, kUnits = BK / kUnit;       // ranks of a unit of the adapters' term (see Term), units of a k-block
 
 // ---------------------------------------------------------------------------------------------------------
@@ -129,8 +139,9 @@ struct RankParams {
   int32_t rank, adapters;
   int32_t boxed;               // slices that one copy of factors brings
   const int32_t* ids;
-  float* out;                  // [parts][n][rank]
+  float* out;                  // [parts][n][rank], by positions
   uint32_t* status;
+  Sorting sort;                // not FEW
   // FEW
   const float* scale;
   float* p;                    // [n][rank]
@@ -141,7 +152,8 @@ struct RankParams {
 
 template <bool FEW>
 __global__ void __launch_bounds__(kRankThreads, 2)
-adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ RankParams p) {
+adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ CUtensorMap tmSorted,
+                    const __grid_constant__ RankParams p) {
   constexpr int kHeld = FEW ? 1 : 2;                 // times 32 samples of an epilogue warp
   extern __shared__ uint8_t smem_raw[];
   __shared__ alignas(16) TileList<kRankTile> L;
@@ -162,7 +174,8 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
   pdl_wait();
   if (warp == 1) { tmem_alloc(&tmem_slot, 2 * cols); tmem_relinquish(); }
   pdl_launch_dependents();
-  build_list(L, p.ids, first, p.n, p.tn, p.adapters, p.status);
+  const bool sorted = !FEW && p.sort.on();
+  build_list(L, sorted ? p.sort.ids : p.ids, first, p.n, p.tn, p.adapters, p.status);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -204,7 +217,7 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
         if (elect_one()) {
           mbar_expect_tx(&full[s], ns * (kSlice * BK * 2) + p.tn * BK * 2);
           uint8_t* st = smem + s * stage;
-          tma_load_2d(st + kTileBytesA, &tmZ, k * BK, first, &full[s]);
+          tma_load_2d(st + kTileBytesA, sorted ? &tmSorted : &tmZ, k * BK, first, &full[s]);
           for (int j = 0; j < ns; j += p.boxed) {
             const int g = c * 8 + j, at = g / per;
             tma_load_3d(st + j * (kSlice * BK * 2), &tmF, k * BK, (g - at * per) * kSlice, L.list[at], &full[s]);
@@ -325,11 +338,12 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
 }
 
 constexpr int kEpi = 8;                             // epilogue warps of the products
-// acc: row m (this lane's) of the samples i .. i + 31.  Even lanes store two rows of every other sample, odd lanes of the ones between; by a
-// warp, whose rows begin at m - lane.  (First all exchanges, then all stores, without a branch where the chunk is whole: with one behind each
-// exchange a tile's end took 6.5 us.)
-__device__ __forceinline__ void store_chunk(__nv_bfloat16* Y, int64_t ldy, int i, int n, int m, int most, const uint32_t (&acc)[32], int lane) {
-  const bool second = lane & 1;
+// acc: row m (this lane's) of the positions i .. i + 31; sample: of position i + lane.  Even lanes store two rows of every other sample, odd
+// lanes of the ones between; by a warp, whose rows begin at m - lane.  sorted: the samples do not follow one another.  (First all exchanges, then all stores, without a branch where the chunk
+// is whole: with one behind each exchange a tile's end took 6.5 us.)
+__device__ __forceinline__ void store_chunk(__nv_bfloat16* Y, int64_t ldy, int i, int n, bool sorted, int sample, int m, int most, const uint32_t (&acc)[32],
+                                            int lane) {
+  const int second = lane & 1;
   uint32_t two[16];
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
@@ -338,17 +352,22 @@ __device__ __forceinline__ void store_chunk(__nv_bfloat16* Y, int64_t ldy, int i
     const __nv_bfloat162 v = __floats2bfloat162_rn(second ? got : x, second ? y : got);
     two[j] = *reinterpret_cast<const uint32_t*>(&v);
   }
-  const int at = i + (second ? 1 : 0), r = m & ~1;
-  __nv_bfloat16* to = Y + static_cast<int64_t>(at) * ldy + r;
-  if (i + 32 <= n && m - lane + 32 <= most) {
+  const int r = m & ~1;
+  __nv_bfloat16* to = Y + r;
+  if (i + 32 <= n && m - lane + 32 <= most && !sorted) {
+    to += static_cast<int64_t>(i + second) * ldy;
 #pragma unroll
     for (int j = 0; j < 16; ++j) *reinterpret_cast<uint32_t*>(to + 2 * j * ldy) = two[j];
+  } else if (i + 32 <= n && m - lane + 32 <= most) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) *reinterpret_cast<uint32_t*>(to + __shfl_sync(0xffffffffu, sample, 2 * j + second) * ldy) = two[j];
   } else {
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
-      if (at + 2 * j >= n || r >= most) continue;
-      if (r + 1 < most) *reinterpret_cast<uint32_t*>(to + 2 * j * ldy) = two[j];
-      else *reinterpret_cast<uint16_t*>(to + 2 * j * ldy) = static_cast<uint16_t>(two[j] & 0xffffu);
+      const int64_t at = __shfl_sync(0xffffffffu, sample, 2 * j + second) * ldy;
+      if (i + second + 2 * j >= n || r >= most) continue;
+      if (r + 1 < most) *reinterpret_cast<uint32_t*>(to + at) = two[j];
+      else *reinterpret_cast<uint16_t*>(to + at) = static_cast<uint16_t>(two[j] & 0xffffu);
     }
   }
 }
@@ -704,6 +723,7 @@ constexpr int kPairSmem = kPairStages * kPairStage + 128 * SFB_ADAPTER_MAX_RANK 
 constexpr int kPartFloats = BM * kMaxTile;          // what a CTA leaves of a tile
 struct PairParams {
   Term term;
+  Sorting sort;
   int32_t n, tn, tilesT, tilesM, m;
   int32_t kseg, cut, whole;    // k-blocks; see Segments
   __nv_bfloat16* Y;
@@ -734,8 +754,8 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity
 
 template <bool MN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
-adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ CUtensorMap tmF,
-                    const __grid_constant__ PairParams p) {
+adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmZ, const __grid_constant__ CUtensorMap tmSorted,
+                    const __grid_constant__ CUtensorMap tmF, const __grid_constant__ PairParams p) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ uint64_t full[kPairStages], empty[kPairStages];       // full, built, tempty: the leader's are in use
   __shared__ uint64_t free_[kPairStages], built[kPairStages];      // of a k-block of factors: the stage is free for the samples' operand;
@@ -779,6 +799,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   if (warp == 0) {
     // ---------------- TMA producer ----------------
     const uint64_t pol = policy_evict_normal();
+    const CUtensorMap* tz = p.sort.on() ? &tmSorted : &tmZ;
     uint32_t s = 0, ph = 0;
     bool ok = true;
     for (int i = 0; i < segs.n && ok; ++i) {
@@ -800,7 +821,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
             } else {
               tma_load_2d_pair(st, &tmA, k * BK, m0, bar, pol);
             }
-            tma_load_2d_pair(st + kTileBytesA, &tmZ, k * BK, z0, bar, pol);
+            tma_load_2d_pair(st + kTileBytesA, tz, k * BK, z0, bar, pol);
           }
           if (++s == static_cast<uint32_t>(kPairStages)) { s = 0; ph ^= 1; }
         }
@@ -863,6 +884,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   } else if (warp < 2 + kEpi) {
     // ---------------- epilogue ----------------
     const int e = warp - 2, q = warp & 3, h = e >> 2, cols = half;     // columns of this warp: half of tn
+    const int32_t* order = p.sort.on() ? p.sort.order : nullptr;
     const uint32_t tempty0 = mapa_u32(smem_u32(&tempty[0]), 0), tempty1 = mapa_u32(smem_u32(&tempty[1]), 0);
     bool ok = true;
     for (int i = 0; i < segs.n && ok; ++i) {
@@ -914,13 +936,15 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
 #pragma unroll
           for (int j = 0; j < 32; ++j) acc[j] = __float_as_uint(__uint_as_float(acc[j]) + x[j]);
         }
-        const int i0 = tt * p.tn + h * cols + c;
-        if (any && m < p.m) {
+        const int i0 = tt * p.tn + h * cols + c, sample = order && i0 + lane < p.n ? order[i0 + lane] : i0 + lane;
+        if (any) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (i0 + j < p.n) acc[j] = __float_as_uint(__uint_as_float(acc[j]) + odd_term(p.term, i0 + j, m));
+          for (int j = 0; j < 32; ++j) {
+            const int i = __shfl_sync(0xffffffffu, sample, j);
+            if (i0 + j < p.n && m < p.m) acc[j] = __float_as_uint(__uint_as_float(acc[j]) + odd_term(p.term, i, m));
+          }
         }
-        store_chunk(p.Y, p.ldy, i0, p.n, m, p.m, acc, lane);
+        store_chunk(p.Y, p.ldy, i0, p.n, order != nullptr, sample, m, p.m, acc, lane);
       }
       __syncwarp();
       if (leave && lane == 0) {
@@ -1022,31 +1046,130 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
 }
 
 // ---------------------------------------------------------------------------------------------------------
+// scale p of the samples in the order of adapter_index_kernel, as three words of bf16 (24 bits): [position][word][rp], rp the rank rounded
+// up to 16 with zeros: what adapter_gradient_kernel takes.  adapter_sum_kernel writes them where it forms p anyway (a launch less: 5 us a
+// call), adapter_words_kernel elsewhere.
+// ---------------------------------------------------------------------------------------------------------
+struct WordsParams {
+  Ranked p[2];                 // at null: not wanted
+  __nv_bfloat16* out[2];       // both null: none
+  const int32_t *ids, *order, *begin, *count;
+  const int32_t* position;     // of a sample in `order`
+  int64_t* work;               // [adapters + 1]: what a column tile takes of the adapters before each one (see adapter_work)
+  const float* scale;
+  int32_t rank, adapters;
+};
+// What a tile of dF[a] costs, in k-blocks: its contraction, and its end.
+__device__ __forceinline__ int adapter_work(int count) { return (count + BK - 1) / BK + 1; }
+// v = w0 + w1 + w2.  (What overflows in the rounding to the first word is cut off instead; of what is not finite there is no rest.)
+__device__ __forceinline__ void three_words(float v, float (&w)[3]) {
+  w[0] = __bfloat162float(__float2bfloat16_rn(v));
+  if (isinf(w[0]) && !isinf(v)) w[0] = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+  const float rest = isfinite(v) ? v - w[0] : 0.f;
+  w[1] = __bfloat162float(__float2bfloat16_rn(rest));
+  w[2] = rest - w[1];
+}
+// The words of eight values (scaled) to `to`, `to` + rp and `to` + 2 rp.
+__device__ __forceinline__ void put_words(__nv_bfloat16* to, int rp, const float (&x)[8]) {
+  uint32_t w[3][4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float u[3], v[3];
+    three_words(x[2 * j], u);
+    three_words(x[2 * j + 1], v);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(u[k], v[k]);
+      w[k][j] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(to + k * rp) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+}
+// work, by a block of 256 threads.
+__device__ __forceinline__ void sum_work(const WordsParams& p, int64_t (&sums)[256]) {
+  const int each = (p.adapters + 255) / 256, from = min(static_cast<int>(threadIdx.x) * each, p.adapters), to = min(from + each, p.adapters);
+  int64_t s = 0;
+  for (int a = from; a < to; ++a) s += adapter_work(p.count[a]);
+  sums[threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.x < 32) {                            // a lane the eight sums from 8 * lane on
+    int64_t v[8], all = 0;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) { v[u] = all; all += sums[threadIdx.x * 8 + u]; }
+    int64_t before = all;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t x = __shfl_up_sync(0xffffffffu, before, o);
+      if (static_cast<int>(threadIdx.x) >= o) before += x;
+    }
+    before -= all;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) sums[threadIdx.x * 8 + u] = before + v[u];
+  }
+  __syncthreads();
+  s = sums[threadIdx.x];
+  for (int a = from; a < to; ++a) { p.work[a] = s; s += adapter_work(p.count[a]); }
+  if (to == p.adapters && from < to) p.work[p.adapters] = s;
+}
+
+__global__ void __launch_bounds__(256) adapter_words_kernel(const __grid_constant__ WordsParams p) {
+  __shared__ int64_t sums[256];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int rp = (p.rank + 15) & ~15, pieces = rp / 8;
+  const int64_t total = static_cast<int64_t>(p.begin[p.adapters - 1] + p.count[p.adapters - 1]) * pieces;
+  const int side = blockIdx.y;
+  if (side == 2) {
+    if (blockIdx.x == 0) sum_work(p, sums);
+    return;
+  }
+  if (!p.out[side]) return;
+  for (int64_t x = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; x < total; x += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t at = x / pieces;
+    const int c = static_cast<int>(x - at * pieces), i = p.order[at];
+    const float sc = p.scale[p.ids[i]];
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int r = c * 8 + j;
+      v[j] = r < p.rank ? sc * ranked(p.p[side], static_cast<int64_t>(i) * p.rank + r) : 0.f;
+    }
+    put_words(p.out[side] + at * 3 * rp + c * 8, rp, v);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------
 // More than 64 samples: p from its parts, zeros for a sample without an adapter, and scale p in bf16 (pb).  In the first blocks the lists of
 // the tiles of the product.
 // ---------------------------------------------------------------------------------------------------------
 struct SumParams {
   Ranked p;
   const int32_t* ids;
+  Sorting sort;
   const float* scale;
   int64_t n;
   int32_t rank, adapters;
-  float* out;
+  float* out;                  // by samples; all else by positions
   __nv_bfloat16* pb;
   int32_t tiles, tn;           // a block per tile of tn samples
   int32_t* lists;              // [tiles][kListPitch]
   int32_t* place;              // per sample its place in its tile's list
   uint32_t* status;
+  WordsParams words;           // of p (p[1], from here) and of the other side's products
 };
 
 __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant__ SumParams p) {
   __shared__ alignas(16) TileList<kMaxTile> L;
+  __shared__ int64_t sums[256];
   pdl_launch_dependents();
   pdl_wait();
   const int tile = blockIdx.x;
+  const bool sorted = p.sort.on();
+  const int32_t* ids = sorted ? p.sort.ids : p.ids;
   if (tile < p.tiles) {
     const int first = tile * p.tn;
-    build_list(L, p.ids, first, static_cast<int>(p.n), p.tn, p.adapters, p.status);
+    build_list(L, ids, first, static_cast<int>(p.n), p.tn, p.adapters, p.status);
     int32_t* to = p.lists + static_cast<int64_t>(tile) * kListPitch;
     if (threadIdx.x == 0) to[0] = L.count;
     for (int t = threadIdx.x; t < p.tn; t += 256) {
@@ -1055,17 +1178,23 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
     }
     return;
   }
-  const int per = (p.rank + kUnit - 1) / kUnit;
-  const int64_t blocks = gridDim.x - p.tiles;
+  const bool wanted = p.words.out[0] || p.words.out[1];
+  const int more = p.tiles + (wanted ? 1 : 0);
+  if (tile < more) {
+    sum_work(p.words, sums);
+    return;
+  }
+  const int per = (p.rank + kUnit - 1) / kUnit, rp = (p.rank + 15) & ~15;
+  const int64_t blocks = gridDim.x - more;
   // four lanes a unit, each some of the parts (by whole warps: a unit behind the last one is formed, not written)
   const int turn = threadIdx.x & 3;
-  for (int64_t base = static_cast<int64_t>(tile - p.tiles) * 64; base < p.n * per; base += blocks * 64) {
+  for (int64_t base = static_cast<int64_t>(tile - more) * 64; base < p.n * per; base += blocks * 64) {
     const int64_t at = base + (threadIdx.x >> 2), x = min(at, p.n * per - 1), i = x / per;
-    const int r0 = static_cast<int>(x - i * per) * kUnit, id = p.ids[i];
+    const int r0 = static_cast<int>(x - i * per) * kUnit, id = ids[i];
     const bool has = id >= 0 && id < p.adapters;
     const float sc = has ? p.scale[id] : 0.f;
     float v[kUnit];
-    const int64_t from = i * p.rank + r0;
+    const int64_t sample = sorted ? p.sort.order[i] : i, from = i * p.rank + r0, into = sample * p.rank + r0;
     if (p.rank % kUnit == 0) {                       // (rows of p are whole pieces of 32 bytes then)
 #pragma unroll
       for (int j = 0; j < kUnit; ++j) v[j] = 0.f;
@@ -1089,13 +1218,13 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
       for (int j = 0; j < kUnit; ++j) v[j] = has && r0 + j < p.rank ? ranked(p.p, from + j) : 0.f;
     }
     if (p.rank % kUnit == 0 && (reinterpret_cast<uintptr_t>(p.out) & 15) == 0) {
-      float4* to = reinterpret_cast<float4*>(p.out + from);
+      float4* to = reinterpret_cast<float4*>(p.out + into);
       to[0] = make_float4(v[0], v[1], v[2], v[3]);
       to[1] = make_float4(v[4], v[5], v[6], v[7]);
     } else {
 #pragma unroll
       for (int j = 0; j < kUnit; ++j)
-        if (r0 + j < p.rank) p.out[from + j] = v[j];
+        if (r0 + j < p.rank) p.out[into + j] = v[j];
     }
     uint32_t w[kUnit / 2];
 #pragma unroll
@@ -1104,6 +1233,19 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
       w[j] = *reinterpret_cast<const uint32_t*>(&b);
     }
     reinterpret_cast<uint4*>(p.pb)[x] = make_uint4(w[0], w[1], w[2], w[3]);
+    if (!wanted || !has) continue;
+    const int64_t row = (static_cast<int64_t>(p.words.position[sample]) * 3) * rp + r0;
+    const bool behind = r0 + 2 * kUnit == rp && r0 + kUnit >= p.rank;        // a piece of zeros follows
+    const float zeros[kUnit] = {};
+    for (int side = 0; side < 2; ++side) {
+      __nv_bfloat16* to = p.words.out[side];
+      if (!to) continue;
+      float u[kUnit];
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j) u[j] = r0 + j < p.rank ? sc * (side ? v[j] : ranked(p.words.p[0], into + j)) : 0.f;
+      put_words(to + row, rp, u);
+      if (behind) put_words(to + row + kUnit, rp, zeros);
+    }
   }
 }
 
@@ -1113,10 +1255,14 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
 // through L2 at its rate, take up to 1.4 times as long (8,192 samples, 10,000 x 5,000 in a loop: pitches of 5,000 entries 997 us, 5,008 774,
 // 5,056 720).  Such operands are copied where the copy, 4 bytes an entry at HBM's rate, costs less than that: from 2,100 uses of a row on.
 // ---------------------------------------------------------------------------------------------------------
+// Samples that are taken in the order of their adapters come here too (if_sorted: only then is there anything to do).
 constexpr int64_t kCopyUses = 4096;
-__global__ void __launch_bounds__(256) adapter_copy_kernel(const uint4* in, int64_t pitch_in, uint4* out, int64_t pitch_out, int64_t rows, int64_t pieces) {
+__global__ void __launch_bounds__(256) adapter_copy_kernel(const uint4* in, int64_t pitch_in, uint4* out, int64_t pitch_out, int64_t rows, int64_t pieces,
+                                                           const __grid_constant__ Sorting sort, bool if_sorted) {
   pdl_launch_dependents();
   pdl_wait();
+  const bool sorted = sort.on();
+  if (if_sorted && !sorted) return;
   const int64_t step = static_cast<int64_t>(gridDim.x) * 256, step_r = step / pieces, step_c = step - step_r * pieces;
   const int64_t first = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   int64_t r = first / pieces, c = first - r * pieces;
@@ -1126,7 +1272,7 @@ __global__ void __launch_bounds__(256) adapter_copy_kernel(const uint4* in, int6
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       to[u] = r < rows ? r * pitch_out + c : -1;
-      if (r < rows) v[u] = __ldcs(in + r * pitch_in + c);
+      if (r < rows) v[u] = __ldcs(in + (sorted ? sort.order[r] : r) * pitch_in + c);
       r += step_r;
       c += step_c;
       if (c >= pieces) { c -= pieces; ++r; }
@@ -1138,133 +1284,101 @@ __global__ void __launch_bounds__(256) adapter_copy_kernel(const uint4* in, int6
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// The samples of each adapter, one adapter after another, in their order: a block per adapter, each of its warps over an eighth of the
-// ids, counts the samples of lower adapters and its own, then writes its own.  No sample without an adapter is among them.
+// The samples of each adapter, one adapter after another, in their order, and those without one behind them: a block per adapter, each of its
+// warps (8, beyond 2,048 samples 32) over a share of the ids, counts the samples of lower adapters and its own, then writes its own.
+//
+// Whether the products had better take the samples in that order: a tile of samples reads the factors of each adapter among them, and its
+// share of the term grows by as much, while samples in order have to be copied.  More blocks (tiles of them) count the adapters of each 128
+// samples as they come, and the last block of all compares what a column costs: 2 bytes a rank of each pair of a tile and an adapter that
+// there are fewer of, against 4 a sample.  (Gradients, us as the samples come and in order: 1,024 samples of 64 adapters of 8 ranks at random,
+// 1,000 x 20,000: 143 and 132; 2,000 of 100 adapters of 32 ranks, 5,000 x 5,000: 330 and 206; 4,096 of 8 adapters of 128, 4,000 x 20,000: 855
+// and 695.  Finding out that it does not pay, a forward pass of 8,192 samples one request after another, 10,000 x 5,000: 670 and 679.)
 // ---------------------------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(256) adapter_index_kernel(const int32_t* ids, int32_t n, int32_t adapters, int32_t* order, int32_t* begin, int32_t* count,
-                                                            uint32_t* status) {
-  pdl_launch_dependents();
-  pdl_wait();
-  __shared__ int below_of[8], own_of[8];
-  const int a = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t share = (static_cast<int64_t>(n) + 1023) / 1024 * 128, from = warp * share, to = min(static_cast<int64_t>(n), from + share);
-  int below = 0, own = 0;
+struct IndexParams {
+  const int32_t* ids;
+  int32_t n, adapters, rank16;
+  int32_t *order, *begin, *count, *position;
+  int32_t* sorted_ids;
+  int32_t tiles;               // 0: the samples stay as they are
+  uint32_t *tally, *sorted;    // [3]: pairs, adapters with samples, blocks done
+  uint32_t* status;
+};
+
+constexpr int kIndexWarps = 32;                      // at most
+__device__ __forceinline__ void index_adapter(const IndexParams& p, int a, int (&below_of)[kIndexWarps], int (&own_of)[kIndexWarps]) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const int64_t share = (static_cast<int64_t>(p.n) + 256 * warps - 1) / (256 * warps) * 256, from = warp * share, to = min(static_cast<int64_t>(p.n), from + share);
   bool bad = false;
+  auto key = [&](int64_t i) {                        // samples without an adapter come last
+    const int id = i < to ? p.ids[i] : -1;
+    bad |= id < -1 || id >= p.adapters;
+    return i < to ? (id >= 0 && id < p.adapters ? id : p.adapters) : p.adapters + 1;
+  };
+  int below = 0, own = 0;
   for (int64_t b = from; b < to; b += 256) {
     int id[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) id[u] = b + u * 32 + lane < to ? ids[b + u * 32 + lane] : -1;
+    for (int u = 0; u < 8; ++u) id[u] = key(b + u * 32 + lane);
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      bad |= id[u] < -1 || id[u] >= adapters;
-      below += id[u] >= 0 && id[u] < a;
+      below += id[u] < a;
       own += id[u] == a;
     }
   }
+  if (a == 0 && bad) atomicOr(p.status, SFB_STATUS_ADAPTER_RANGE);
   below = __reduce_add_sync(0xffffffffu, below);
   own = __reduce_add_sync(0xffffffffu, own);
-  if (a == 0 && bad) atomicOr(status, SFB_STATUS_ADAPTER_RANGE);
   if (lane == 0) { below_of[warp] = below; own_of[warp] = own; }
   __syncthreads();
   int64_t at = 0;
   int total = 0;
-  for (int w = 0; w < 8; ++w) {
+  for (int w = 0; w < warps; ++w) {
     at += below_of[w] + (w < warp ? own_of[w] : 0);
     total += own_of[w];
   }
-  if (threadIdx.x == 0) { begin[a] = static_cast<int32_t>(at); count[a] = total; }
+  if (threadIdx.x == 0) {
+    if (a < p.adapters) { p.begin[a] = static_cast<int32_t>(at); p.count[a] = total; }
+    if (p.tiles && a < p.adapters && total) atomicAdd(p.tally + 1, 1u);
+  }
   if (own == 0) return;
   for (int64_t b = from; b < to; b += 256) {
     int id[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) id[u] = b + u * 32 + lane < to ? ids[b + u * 32 + lane] : -1;
+    for (int u = 0; u < 8; ++u) id[u] = key(b + u * 32 + lane);
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const uint32_t m = __ballot_sync(0xffffffffu, id[u] == a);
-      if (id[u] == a) order[at + __popc(m & ((1u << lane) - 1))] = static_cast<int32_t>(b + u * 32 + lane);
+      if (id[u] == a) {
+        const int64_t to_at = at + __popc(m & ((1u << lane) - 1));
+        p.order[to_at] = static_cast<int32_t>(b + u * 32 + lane);
+        p.position[b + u * 32 + lane] = static_cast<int32_t>(to_at);
+        if (p.tiles) p.sorted_ids[to_at] = a < p.adapters ? a : -1;
+      }
       at += __popc(m);
     }
   }
 }
 
-// ---------------------------------------------------------------------------------------------------------
-// scale p of the samples in the order of adapter_index_kernel, as three words of bf16 (24 bits): [position][word][rp], rp the rank rounded
-// up to 16 with zeros.
-// ---------------------------------------------------------------------------------------------------------
-struct WordsParams {
-  Ranked p[2];                 // at null: not wanted
-  __nv_bfloat16* out[2];
-  const int32_t *ids, *order, *begin, *count;
-  int64_t* work;               // [adapters + 1]: what a column tile takes of the adapters before each one (see adapter_work)
-  const float* scale;
-  int32_t rank, adapters;
-};
-// What a tile of dF[a] costs, in k-blocks: its contraction, and its end.
-__device__ __forceinline__ int adapter_work(int count) { return (count + BK - 1) / BK + 1; }
-// v = w0 + w1 + w2.  (What overflows in the rounding to the first word is cut off instead; of what is not finite there is no rest.)
-__device__ __forceinline__ void three_words(float v, float (&w)[3]) {
-  w[0] = __bfloat162float(__float2bfloat16_rn(v));
-  if (isinf(w[0]) && !isinf(v)) w[0] = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-  const float rest = isfinite(v) ? v - w[0] : 0.f;
-  w[1] = __bfloat162float(__float2bfloat16_rn(rest));
-  w[2] = rest - w[1];
-}
-
-__global__ void __launch_bounds__(256) adapter_words_kernel(const __grid_constant__ WordsParams p) {
+__global__ void __launch_bounds__(32 * kIndexWarps) adapter_index_kernel(const __grid_constant__ IndexParams p) {
+  __shared__ alignas(16) TileList<kRankTile> L;
+  __shared__ int below_of[kIndexWarps], own_of[kIndexWarps];
   pdl_launch_dependents();
   pdl_wait();
-  const int rp = (p.rank + 15) & ~15, pieces = rp / 8;
-  const int64_t total = static_cast<int64_t>(p.begin[p.adapters - 1] + p.count[p.adapters - 1]) * pieces;
-  const int side = blockIdx.y;
-  if (side == 2) {
-    if (blockIdx.x > 0) return;
-    __shared__ int64_t sums[256];
-    const int each = (p.adapters + 255) / 256, from = min(static_cast<int>(threadIdx.x) * each, p.adapters), to = min(from + each, p.adapters);
-    int64_t s = 0;
-    for (int a = from; a < to; ++a) s += adapter_work(p.count[a]);
-    sums[threadIdx.x] = s;
-    __syncthreads();
-    if (threadIdx.x < 32) {                          // a lane the eight sums from 8 * lane on
-      int64_t v[8], all = 0;
-#pragma unroll
-      for (int u = 0; u < 8; ++u) { v[u] = all; all += sums[threadIdx.x * 8 + u]; }
-      int64_t before = all;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int64_t x = __shfl_up_sync(0xffffffffu, before, o);
-        if (static_cast<int>(threadIdx.x) >= o) before += x;
-      }
-      before -= all;
-#pragma unroll
-      for (int u = 0; u < 8; ++u) sums[threadIdx.x * 8 + u] = before + v[u];
-    }
-    __syncthreads();
-    s = sums[threadIdx.x];
-    for (int a = from; a < to; ++a) { p.work[a] = s; s += adapter_work(p.count[a]); }
-    if (to == p.adapters && from < to) p.work[p.adapters] = s;
-    return;
+  const int tile = static_cast<int>(blockIdx.x) - p.adapters - 1;
+  if (tile < 0) {
+    index_adapter(p, blockIdx.x, below_of, own_of);
+  } else {
+    build_list(L, p.ids, tile * kRankTile, p.n, kRankTile, p.adapters, p.status);
+    if (threadIdx.x == 0) atomicAdd(p.tally, static_cast<uint32_t>(L.count));
   }
-  if (!p.out[side]) return;
-  for (int64_t x = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; x < total; x += static_cast<int64_t>(gridDim.x) * 256) {
-    const int64_t at = x / pieces;
-    const int c = static_cast<int>(x - at * pieces), i = p.order[at];
-    const float sc = p.scale[p.ids[i]];
-    uint32_t w[3][4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float u[3], v[3];
-      const int r = c * 8 + 2 * j;
-      three_words(r < p.rank ? sc * ranked(p.p[side], static_cast<int64_t>(i) * p.rank + r) : 0.f, u);
-      three_words(r + 1 < p.rank ? sc * ranked(p.p[side], static_cast<int64_t>(i) * p.rank + r + 1) : 0.f, v);
-#pragma unroll
-      for (int k = 0; k < 3; ++k) {
-        const __nv_bfloat162 b = __floats2bfloat162_rn(u[k], v[k]);
-        w[k][j] = *reinterpret_cast<const uint32_t*>(&b);
-      }
+  if (p.tiles && threadIdx.x == 0) {
+    __threadfence();
+    if (atomicAdd(p.tally + 2, 1u) == gridDim.x - 1) {
+      __threadfence();
+      const int64_t fewer = static_cast<int64_t>(__ldcg(p.tally)) - p.tiles - __ldcg(p.tally + 1);
+      *p.sorted = fewer * p.rank16 > 2ll * p.n;
+      p.tally[0] = p.tally[1] = p.tally[2] = 0;      // for the next launch
     }
-    __nv_bfloat16* to = p.out[side] + at * 3 * rp + c * 8;
-#pragma unroll
-    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(to + k * rp) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
   }
 }
 
@@ -1544,10 +1658,19 @@ int64_t rank_rows(int64_t n, int64_t d) {
   return std::max(most, n);
 }
 
+// Whether n samples, each with an adapter at random, had better be taken in the order of their adapters (see adapter_index_kernel), and would
+// read 32 MB less of factors, 5 us, which is what finding out takes.
+bool sort_may_pay(const sfb_adapter_config& c, int64_t n) {
+  const int64_t tiles = (n + kRankTile - 1) / kRankTile, rank16 = (c.rank + kSlice - 1) / kSlice * kSlice;
+  const int64_t fewer = tiles * std::min<int64_t>(c.adapters, kRankTile) - tiles - c.adapters;
+  return n > kFewMost && fewer * rank16 > 2 * n && fewer * rank16 * (c.rows + c.cols) > 16 << 20;
+}
+
 bool pitch_odd(int64_t pitch) { return pitch % 16 != 0; }      // of bf16 entries: not a multiple of 32 bytes
 
 struct AdapterLayout {
-  size_t status, ready, arrived, s, t, ssum, tsum, pb, swords, twords, order, begin, count, work, lists, place, partial, wcopy, zcopy, total;
+  size_t status, ready, arrived, tally, sorted, s, t, ssum, tsum, pb, swords, twords, order, sorted_ids, begin, count, position, work, lists, place, partial, wcopy,
+      zcopy, total;
 };
 
 int check(const sfb_adapter_config* c) {
@@ -1570,6 +1693,8 @@ AdapterLayout layout_of(const sfb_adapter_config& c) {
   L.status = take(4);
   L.ready = take(kModelSms * kEpi * 4);              // these are cleared with the status word
   L.arrived = take(kFewChunks * 4);
+  L.tally = take(3 * 4);
+  L.sorted = take(4);
   L.s = take(static_cast<size_t>(rank_rows(c.max_samples, c.cols)) * c.rank * 4);
   L.t = take(static_cast<size_t>(rank_rows(c.max_samples, c.rows)) * c.rank * 4);
   L.ssum = take(n * c.rank * 4);
@@ -1584,9 +1709,12 @@ AdapterLayout layout_of(const sfb_adapter_config& c) {
   const bool odd_w = pitch_odd(c.ldw ? c.ldw : c.cols) && c.max_samples >= kCopyUses;
   const bool odd_x = pitch_odd(round_up(c.cols, 8)) && c.rows >= kCopyUses, odd_y = pitch_odd(round_up(c.rows, 8)) && c.cols >= kCopyUses;
   L.wcopy = take(odd_w ? static_cast<size_t>(c.rows) * round_up(c.cols, BK) * 2 : 0);
-  L.zcopy = take(n <= kFewMost ? 0 : std::max(odd_x ? n * round_up(c.cols, BK) * 2 : 0, odd_y ? n * round_up(c.rows, BK) * 2 : 0));
+  const bool sorts = sort_may_pay(c, c.max_samples);
+  L.zcopy = take(n <= kFewMost ? 0 : std::max(odd_x || sorts ? n * round_up(c.cols, BK) * 2 : 0, odd_y || sorts ? n * round_up(c.rows, BK) * 2 : 0));
   L.order = take(n * 4);
+  L.sorted_ids = take(sorts ? n * 4 : 0);
   L.begin = take(static_cast<size_t>(c.adapters) * 4);
+  L.position = take(n * 4);
   L.work = take((static_cast<size_t>(c.adapters) + 1) * 8);
   L.count = take(static_cast<size_t>(c.adapters) * 4);
   L.total = off;
@@ -1665,17 +1793,30 @@ cudaError_t allow_beside(int bytes) {
   return e;
 }
 
+// The samples' operand: as it is, or a copy whose rows lie better; and in the order of their adapters, where sort.on() says so.
+struct Samples {
+  const void* at;
+  int64_t pitch;
+  const void* in_order;
+  int64_t pitch_in_order;
+  Sorting sort;
+};
+
 // p = F[a] z for n samples.  *got: where, and in how many parts.  Up to 64 samples it is in `sum` in one part, with all that a product
 // with the other factors (MN: with V) takes; for more adapter_sum_kernel has to follow.
 template <bool MN>
-cudaError_t rank_products(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const int32_t* ids, float* out, float* sum, Ranked* got) {
+cudaError_t rank_products(sfb_adapters* h, int64_t n, const Samples& z, const int32_t* ids, float* out, float* sum, Ranked* got) {
   const sfb_adapter_config& c = h->cfg;
   const int64_t d = MN ? c.rows : c.cols;
   const int tn = rank_tile(n), parts = rank_parts(n, d), tiles = static_cast<int>((n + tn - 1) / tn);
   const CUtensorMap& mf = MN ? h->mapU : h->mapV;
-  CUtensorMap mz;
-  if (!operand_map(h, &mz, Z, d, n, ldz, BK, tn, CU_TENSOR_MAP_L2_PROMOTION_L2_256B)) return cudaErrorInvalidValue;
+  CUtensorMap mz, ms;
+  if (!operand_map(h, &mz, z.at, d, n, z.pitch, BK, tn, CU_TENSOR_MAP_L2_PROMOTION_L2_256B) ||
+      (z.in_order != z.at && !operand_map(h, &ms, z.in_order, d, n, z.pitch_in_order, BK, tn, CU_TENSOR_MAP_L2_PROMOTION_L2_256B)))
+    return cudaErrorInvalidValue;
+  if (z.in_order == z.at) ms = mz;
   RankParams p{};
+  p.sort = z.sort;
   p.n = static_cast<int32_t>(n); p.tn = tn; p.kseg = static_cast<int32_t>((d + BK - 1) / BK);
   p.stages = std::min(kMaxStages, (n <= kFewMost ? kFewRing : kSmallRing) / stage_bytes(tn));
   p.rank = c.rank; p.adapters = c.adapters; p.boxed = h->boxed_slices; p.ids = ids; p.out = out; p.status = h->at<uint32_t>(h->lay.status);
@@ -1688,13 +1829,13 @@ cudaError_t rank_products(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz
     if (e != cudaSuccess) return e;
     *got = Ranked{sum, 1, 0};
     // a block an SM, and no more than there can be parts of chunks
-    return launch_kernel(adapter_rank_kernel<true>, dim3(std::max(1, std::min(kModelSms, chunks * parts))), dim3(kRankThreads), smem, h->stream, 1, mf, mz, p);
+    return launch_kernel(adapter_rank_kernel<true>, dim3(std::max(1, std::min(kModelSms, chunks * parts))), dim3(kRankThreads), smem, h->stream, 1, mf, mz, ms, p);
   }
   const int groups = std::max(1, std::min(chunks, 2 * kModelSms / (parts * tiles)));
   const cudaError_t e = allow_smem<adapter_rank_kernel<false>>(kSmallRing + 1024);
   if (e != cudaSuccess) return e;
   *got = Ranked{out, parts, n * c.rank};
-  return launch_kernel(adapter_rank_kernel<false>, dim3(parts, tiles, groups), dim3(kRankThreads), smem, h->stream, 1, mf, mz, p);
+  return launch_kernel(adapter_rank_kernel<false>, dim3(parts, tiles, groups), dim3(kRankThreads), smem, h->stream, 1, mf, mz, ms, p);
 }
 
 // CTAs of a cluster of adapter_few_kernel, each with four k-blocks at least: up to four as long as nine tenths of the places, two an SM,
@@ -1707,16 +1848,23 @@ int few_parts(int64_t tiles, int64_t kseg) {
   return best;
 }
 
-// A bf16 operand [outer x inner] where the products take it: itself, or a copy in `room`, with *pitch entries from row to row.
-cudaError_t placed(sfb_adapters* h, const void** at, int64_t* pitch, int64_t outer, int64_t inner, int64_t uses, size_t room, size_t bytes) {
-  const int64_t to = round_up(inner, BK);
-  if (!pitch_odd(*pitch) || uses < kCopyUses || bytes < static_cast<size_t>(outer) * to * 2) return cudaSuccess;
-  uint4* copy = h->at<uint4>(room);
-  const cudaError_t e = launch_kernel(adapter_copy_kernel, dim3(grid1d(outer * ((inner + 7) / 8), 1024)), dim3(256), 0, h->stream, 1,
-                                      static_cast<const uint4*>(*at), *pitch / 8, copy, to / 8, outer, (inner + 7) / 8);
-  *at = copy;
-  *pitch = to;
-  return e;
+// Copies a bf16 operand [outer x inner] to workspace, with round_up(inner, BK) entries from row to row.
+cudaError_t copy_operand(sfb_adapters* h, const void* from, int64_t pitch, int64_t outer, int64_t inner, size_t room, const Sorting& sort, bool if_sorted) {
+  return launch_kernel(adapter_copy_kernel, dim3(grid1d(outer * ((inner + 7) / 8), 1024)), dim3(256), 0, h->stream, 1, static_cast<const uint4*>(from),
+                       pitch / 8, h->at<uint4>(room), round_up(inner, BK) / 8, outer, (inner + 7) / 8, sort, if_sorted);
+}
+bool fits(int64_t outer, int64_t inner, size_t bytes) { return bytes >= static_cast<size_t>(outer) * round_up(inner, BK) * 2; }
+
+// Z [n x d] where the products take it.
+cudaError_t placed(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, int64_t d, int64_t uses, const Sorting& sort, Samples* z) {
+  const size_t room = h->lay.order - h->lay.zcopy;
+  const bool copy = n > kFewMost && pitch_odd(ldz) && uses >= kCopyUses && fits(n, d, room);
+  *z = Samples{Z, ldz, Z, ldz, sort};
+  if (!copy && !sort.sorted) return cudaSuccess;
+  z->in_order = h->at<char>(h->lay.zcopy);
+  z->pitch_in_order = round_up(d, BK);
+  if (copy) { z->at = z->in_order; z->pitch = z->pitch_in_order; }
+  return copy_operand(h, Z, ldz, n, d, h->lay.zcopy, sort, !copy);
 }
 
 // What adapter_rank_kernel or adapter_sum_kernel leaves for the products.
@@ -1768,19 +1916,26 @@ PairPlan plan_pairs(int64_t tiles, int64_t kseg, int tn, int64_t most) {
 }
 
 template <bool MN>
-cudaError_t pairs(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const Term& term, void* Y, int64_t ldy) {
+cudaError_t pairs(sfb_adapters* h, int64_t n, const Samples& z, const Term& term, void* Y, int64_t ldy) {
   const sfb_adapter_config& c = h->cfg;
   const int64_t m = MN ? c.cols : c.rows, d = MN ? c.rows : c.cols;
   const int tn = tile_of(n);
   const void* W = h->W;
   int64_t ldw = c.ldw;
-  cudaError_t e = placed(h, &W, &ldw, c.rows, c.cols, n, h->lay.wcopy, h->lay.zcopy - h->lay.wcopy);
-  if (e != cudaSuccess) return e;
-  CUtensorMap ma, mz;
+  if (pitch_odd(ldw) && n >= kCopyUses && fits(c.rows, c.cols, h->lay.zcopy - h->lay.wcopy)) {
+    const cudaError_t e = copy_operand(h, W, ldw, c.rows, c.cols, h->lay.wcopy, Sorting{}, false);
+    if (e != cudaSuccess) return e;
+    W = h->at<char>(h->lay.wcopy);
+    ldw = round_up(c.cols, BK);
+  }
+  CUtensorMap ma, mz, ms;
   if (!operand_map(h, &ma, W, c.cols, c.rows, ldw, BK, MN ? BK : BM, CU_TENSOR_MAP_L2_PROMOTION_NONE) ||
-      !operand_map(h, &mz, Z, d, n, ldz, BK, tn / 2, CU_TENSOR_MAP_L2_PROMOTION_NONE))
+      !operand_map(h, &mz, z.at, d, n, z.pitch, BK, tn / 2, CU_TENSOR_MAP_L2_PROMOTION_NONE) ||
+      (z.in_order != z.at && !operand_map(h, &ms, z.in_order, d, n, z.pitch_in_order, BK, tn / 2, CU_TENSOR_MAP_L2_PROMOTION_NONE)))
     return cudaErrorInvalidValue;
+  if (z.in_order == z.at) ms = mz;
   PairParams p{};
+  p.sort = z.sort;
   p.n = static_cast<int32_t>(n); p.tn = tn; p.tilesT = static_cast<int32_t>((n + tn - 1) / tn);
   p.tilesM = static_cast<int32_t>((m + 2 * BM - 1) / (2 * BM)); p.m = static_cast<int32_t>(m);
   p.kseg = static_cast<int32_t>((d + BK - 1) / BK);
@@ -1789,26 +1944,47 @@ cudaError_t pairs(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const 
   p.term = term; p.Y = static_cast<__nv_bfloat16*>(Y); p.ldy = ldy;
   p.partial = h->at<float>(h->lay.partial); p.ready = h->at<uint32_t>(h->lay.ready); p.status = h->at<uint32_t>(h->lay.status);
   return launch_kernel_if(static_cast<int64_t>(p.tilesT) * p.tilesM <= plan.pairs, adapter_pair_kernel<MN>, dim3(2u * static_cast<unsigned>(plan.pairs)),
-                          dim3(kPairThreads), kPairSmem, h->stream, 1, ma, mz, MN ? h->unitV : h->unitU, p);
+                          dim3(kPairThreads), kPairSmem, h->stream, 1, ma, mz, ms, MN ? h->unitV : h->unitU, p);
 }
 
-// y = A z + scale F^T p.  p in parts goes to `to` first; *s: p where it is afterwards.
+// y = A z + scale F^T p.  p in parts goes to `to` first, and for more than 64 samples to the words that are wanted; *s: p where it is afterwards.
 template <bool MN>
-cudaError_t product(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const int32_t* ids, Ranked* s, float* to, void* Y, int64_t ldy) {
+cudaError_t product(sfb_adapters* h, int64_t n, const Samples& z, const int32_t* ids, Ranked* s, float* to, void* Y, int64_t ldy, const WordsParams& words) {
   const sfb_adapter_config& c = h->cfg;
   if (n <= kFewMost) {
     const Term term = term_of<MN>(h, ids, s->at);
-    return n <= 16 ? few<16, MN>(h, n, Z, ldz, term, Y, ldy) : n <= 32 ? few<32, MN>(h, n, Z, ldz, term, Y, ldy) : few<kFewMost, MN>(h, n, Z, ldz, term, Y, ldy);
+    return n <= 16 ? few<16, MN>(h, n, z.at, z.pitch, term, Y, ldy) : n <= 32 ? few<32, MN>(h, n, z.at, z.pitch, term, Y, ldy)
+                                                                             : few<kFewMost, MN>(h, n, z.at, z.pitch, term, Y, ldy);
   }
   SumParams p{};
-  p.p = *s; p.ids = ids; p.scale = h->scale; p.n = n; p.rank = c.rank; p.adapters = c.adapters; p.out = to; p.status = h->at<uint32_t>(h->lay.status);
+  p.p = *s; p.ids = ids; p.sort = z.sort; p.scale = h->scale; p.n = n; p.rank = c.rank; p.adapters = c.adapters; p.out = to; p.status = h->at<uint32_t>(h->lay.status);
   p.pb = h->at<__nv_bfloat16>(h->lay.pb);
   p.tn = tile_of(n); p.tiles = static_cast<int32_t>((n + p.tn - 1) / p.tn); p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place);
-  const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(p.tiles + grid1d(n * ((c.rank + kUnit - 1) / kUnit), 64)), dim3(256), 0, h->stream,
+  p.words = words;
+  const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(p.tiles + (words.out[0] || words.out[1] ? 1 : 0) + grid1d(n * ((c.rank + kUnit - 1) / kUnit), 64)), dim3(256), 0, h->stream,
                                       1, p);
   if (e != cudaSuccess) return e;
   *s = Ranked{to, 1, 0};
-  return pairs<MN>(h, n, Z, ldz, term_of<MN>(h, ids, to), Y, ldy);
+  return pairs<MN>(h, n, z, term_of<MN>(h, ids, to), Y, ldy);
+}
+
+// The samples by adapters.  sort (may be null): also finds out whether the products had better take them so.
+cudaError_t index_samples(sfb_adapters* h, int64_t n, const int32_t* ids, Sorting* sort) {
+  const AdapterLayout& l = h->lay;
+  const sfb_adapter_config& c = h->cfg;
+  IndexParams p{};
+  p.ids = ids; p.n = static_cast<int32_t>(n); p.adapters = c.adapters; p.rank16 = (c.rank + kSlice - 1) / kSlice * kSlice;
+  p.order = h->at<int32_t>(l.order); p.begin = h->at<int32_t>(l.begin); p.count = h->at<int32_t>(l.count); p.position = h->at<int32_t>(l.position); p.sorted_ids = h->at<int32_t>(l.sorted_ids);
+  p.tally = h->at<uint32_t>(l.tally); p.sorted = h->at<uint32_t>(l.sorted); p.status = h->at<uint32_t>(l.status);
+  if (sort) {
+    p.tiles = static_cast<int32_t>((n + kRankTile - 1) / kRankTile);
+    *sort = Sorting{p.sorted, p.order, p.sorted_ids};
+  }
+  return launch_kernel(adapter_index_kernel, dim3(c.adapters + 1 + p.tiles), dim3(n <= 2048 ? 256 : 32 * kIndexWarps), 0, h->stream, 1, p);
+}
+// ... whether there is room for that too.
+bool sorts(const sfb_adapters* h, int64_t n, int64_t d) {
+  return sort_may_pay(h->cfg, n) && h->lay.begin > h->lay.sorted_ids && fits(n, d, h->lay.order - h->lay.zcopy);
 }
 
 int fail(sfb_adapters* h, cudaError_t e) {
@@ -1896,9 +2072,12 @@ extern "C" int sfb_adapter_forward(sfb_adapters* h, int64_t n, const void* X_dev
   ACK(on.err);
   Ranked s{};
   float* sum = S_dev ? S_dev : h->at<float>(h->lay.ssum);
-  if (n > kFewMost) ACK(placed(h, &X_dev, &ldx, n, c.cols, c.rows, h->lay.zcopy, h->lay.order - h->lay.zcopy));
-  ACK(rank_products<false>(h, n, X_dev, ldx, ids_dev, h->at<float>(h->lay.s), sum, &s));
-  ACK(product<false>(h, n, X_dev, ldx, ids_dev, &s, sum, Y_dev, ldy));
+  Sorting sort{};
+  Samples z;
+  if (sorts(h, n, c.cols)) ACK(index_samples(h, n, ids_dev, &sort));
+  ACK(placed(h, n, X_dev, ldx, c.cols, c.rows, sort, &z));
+  ACK(rank_products<false>(h, n, z, ids_dev, h->at<float>(h->lay.s), sum, &s));
+  ACK(product<false>(h, n, z, ids_dev, &s, sum, Y_dev, ldy, WordsParams{}));
   return SFB_OK;
 }
 
@@ -1922,23 +2101,27 @@ extern "C" int sfb_adapter_backward(sfb_adapters* h, int64_t n, const void* dY_d
   if (!al(dY_dev, 16) || !al(X_dev, 16) || !al(dX_dev, 16) || !al(ids_dev, 4) || !al(S_dev, 4)) return SFB_ERR_ALIGN;
   uint32_t* status = h->at<uint32_t>(h->lay.status);
   int32_t *order = h->at<int32_t>(h->lay.order), *begin = h->at<int32_t>(h->lay.begin), *count = h->at<int32_t>(h->lay.count);
-  if (dU_dev || dV_dev)
-    ACK(launch_kernel(adapter_index_kernel, dim3(c.adapters), dim3(256), 0, h->stream, 1, ids_dev, static_cast<int32_t>(n), c.adapters, order,
-                      begin, count, status));
+  Sorting sort{};
+  const bool sorting = dX_dev && sorts(h, n, c.rows);
+  if (dU_dev || dV_dev || sorting) ACK(index_samples(h, n, ids_dev, sorting ? &sort : nullptr));
   Ranked s{S_dev, 1, 0}, t{};
-  if (dU_dev && !S_dev) ACK(rank_products<false>(h, n, X_dev, ldx, ids_dev, h->at<float>(h->lay.s), h->at<float>(h->lay.ssum), &s));
-  const void* Z = dY_dev;
-  int64_t ldz = lddy;
-  if (dX_dev && n > kFewMost) ACK(placed(h, &Z, &ldz, n, c.rows, c.cols, h->lay.zcopy, h->lay.order - h->lay.zcopy));
-  if (dX_dev || dV_dev) ACK(rank_products<true>(h, n, Z, ldz, ids_dev, h->at<float>(h->lay.t), h->at<float>(h->lay.tsum), &t));
-  if (dX_dev) ACK(product<true>(h, n, Z, ldz, ids_dev, &t, h->at<float>(h->lay.tsum), dX_dev, lddx));
+  if (dU_dev && !S_dev)
+    ACK(rank_products<false>(h, n, Samples{X_dev, ldx, X_dev, ldx, Sorting{}}, ids_dev, h->at<float>(h->lay.s), h->at<float>(h->lay.ssum), &s));
+  Samples z{dY_dev, lddy, dY_dev, lddy, Sorting{}};
+  if (dX_dev) ACK(placed(h, n, dY_dev, lddy, c.rows, c.cols, sort, &z));
+  if (dX_dev || dV_dev) ACK(rank_products<true>(h, n, z, ids_dev, h->at<float>(h->lay.t), h->at<float>(h->lay.tsum), &t));
+  __nv_bfloat16 *swords = h->at<__nv_bfloat16>(h->lay.swords), *twords = h->at<__nv_bfloat16>(h->lay.twords);
+  WordsParams w{};
+  w.out[0] = dU_dev ? swords : nullptr; w.out[1] = dV_dev ? twords : nullptr;
+  w.p[0] = s; w.p[1] = t;
+  w.ids = ids_dev; w.order = order; w.begin = begin; w.count = count; w.position = h->at<int32_t>(h->lay.position);
+  w.work = h->at<int64_t>(h->lay.work); w.scale = h->scale; w.rank = c.rank; w.adapters = c.adapters;
+  if (dX_dev) ACK(product<true>(h, n, z, ids_dev, &t, h->at<float>(h->lay.tsum), dX_dev, lddx, w));
   if (dU_dev || dV_dev) {
-    __nv_bfloat16 *swords = h->at<__nv_bfloat16>(h->lay.swords), *twords = h->at<__nv_bfloat16>(h->lay.twords);
-    WordsParams w{};
-    if (dU_dev) { w.p[0] = s; w.out[0] = swords; }
-    if (dV_dev) { w.p[1] = t; w.out[1] = twords; }
-    w.ids = ids_dev; w.order = order; w.begin = begin; w.count = count; w.work = h->at<int64_t>(h->lay.work); w.scale = h->scale; w.rank = c.rank; w.adapters = c.adapters;
-    ACK(launch_kernel(adapter_words_kernel, dim3(grid1d(n * ((c.rank + 15) / 16 * 2), 256), 3), dim3(256), 0, h->stream, 1, w));
+    if (!dX_dev || n <= kFewMost) {
+      w.p[1] = t;
+      ACK(launch_kernel(adapter_words_kernel, dim3(grid1d(n * ((c.rank + 15) / 16 * 2), 256), 3), dim3(256), 0, h->stream, 1, w));
+    }
     GradParams p{};
     const int tile = grad_halves(c.rank) * BM;
     if (dU_dev)

@@ -157,6 +157,13 @@ SIZES = [
     # operands that are copied first: rows an odd multiple of 16 bytes apart (X and dY; W)
     (70, 5000, 4104, 3, 16, "mixed"),
     (4100, 72, 136, 3, 24, "runs"),
+    # many adapters among the samples of a tile: taken in the order of their adapters, or not, as they come
+    (1500, 700, 6000, 100, 16, "every"),
+    (1501, 700, 6000, 100, 16, "runs"),
+    (1502, 6001, 707, 90, 24, "mixed"),
+    (333, 9000, 1000, 150, 128, "mixed"),
+    (4160, 2100, 4104, 64, 16, "mixed"),
+    (1024, 6000, 6000, 100, 20, "none"),
     # as many samples of one adapter as are taken out of the accumulators in several turns; the widest adapters
     (3000, 300, 200, 1, 20, "one"),
     (900, 136, 264, 2, 128, "mixed"),
@@ -181,10 +188,10 @@ def test_wide_pitches_and_s_not_given(size):
     assert (part["dX"] == 7).all() and (part["dU"] == 7).all() and torch.equal(part["dV"], got["dV"])
 
 
-@pytest.mark.parametrize("n", [5, 40, 300, 1100])
-def test_what_is_not_finite_stays_where_it_is(n):
+@pytest.mark.parametrize("n,rows,cols,adapters", [(5, 300, 520, 6), (40, 300, 520, 6), (300, 300, 520, 6), (1100, 300, 520, 6), (1500, 700, 6000, 100)])
+def test_what_is_not_finite_stays_where_it_is(n, rows, cols, adapters):
     """An adapter and a sample that hold infinities and NaN: every result of the others has the bits it had."""
-    c = Case(n, 300, 520, 6, 20, "mixed", seed=n)
+    c = Case(n, rows, cols, adapters, 20, "mixed", seed=n)
     before = c.run()
     c.U[2, 3, 17], c.U[2, 19, 299], c.V[2, 5, 100], c.V[2, 0, 0] = float("inf"), float("nan"), float("nan"), float("-inf")
     bad = n // 2
@@ -195,7 +202,7 @@ def test_what_is_not_finite_stays_where_it_is(n):
     for k in ("Y", "S", "dX"):
         assert torch.equal(before[k][other], after[k][other]), k
     owner = int(c.ids[bad])
-    keep = [a for a in range(6) if a not in (2, owner)]
+    keep = [a for a in range(adapters) if a not in (2, owner)]
     for k in ("dU", "dV"):
         assert torch.equal(before[k][keep], after[k][keep]), k
     assert torch.isnan(after["Y"][bad]).all()
@@ -239,9 +246,10 @@ def test_gradients_of_infinite_entries_are_infinite(rank):
     assert (got["dV"][1][:, 7] == float("-inf")).all() and torch.isfinite(got["dV"][1][:, keep]).all()
 
 
-def test_ids_out_of_range_take_no_adapter_and_are_reported():
-    c = Case(50, 100, 200, 4, 8, "mixed", seed=2)
-    c.ids[7], c.ids[20], c.ids[49] = 4, -2, 2 ** 31 - 1
+@pytest.mark.parametrize("n,rows,cols,adapters,rank", [(50, 100, 200, 4, 8), (1500, 700, 6000, 100, 16)])
+def test_ids_out_of_range_take_no_adapter_and_are_reported(n, rows, cols, adapters, rank):
+    c = Case(n, rows, cols, adapters, rank, "mixed", seed=2)
+    c.ids[7], c.ids[20], c.ids[49] = adapters, -2, 2 ** 31 - 1
     got = c.run()
     assert c.plan.sfb_adapter_get_status() == S.STATUS_ADAPTER_RANGE
     assert c.plan.sfb_adapter_get_status() == 0
