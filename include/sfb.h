@@ -342,12 +342,18 @@ int sfb_get_plan(const sfb_config* cfg, int64_t samples, int32_t* product, int32
  *    X_dev, dY_dev, Y_dev, dX_dev are bf16, sums fp32; scale_dev [adapters], S_dev [n x rank], dU_dev [adapters][rank][rows] and
  *    dV_dev [adapters][rank][cols] fp32, the last three without gaps; ids_dev int32.  Every pitch of a bf16 operand is a multiple
  *    of 8 entries (rows, cols, n and rank are any size), every such pointer 16-byte aligned; scale, S and ids 4-byte aligned.
- *    The operand copy of W that sfb_get_operand_copy gives (SFB_MLR, bf16 mode) is such a W.
+ *    The operand copy of W that sfb_get_operand_copy gives (SFB_MLR, bf16 mode) is such a W.  Pitches that are a multiple of 16
+ *    entries are the better ones: with others the products of thousands of samples copy their operands into the workspace first.
+ *  - Rounded to bf16 on the way: scale s and scale t where they enter y and dx (2^-8 of that term at most, which is what y and dx
+ *    are rounded by), not where they enter dU and dV.  Results are the same bits from call to call; they may differ in the last
+ *    bits with n and with the order of the samples.
  *  - What lies behind the last column of a row, or in rows of other samples and adapters, is neither read into a result nor
  *    written: infinities and NaN in a sample or an adapter reach the results of that sample, or of that adapter's samples, alone.
+ *    (Where an infinite factor meets an infinite s or t, the term is NaN.)
  *  - Outputs do not overlap the inputs or one another.
  *  - The handle borrows W, U, V and scale (training may change their values between calls: nothing derived from them is kept)
- *    and the workspace.  One handle per stream; calls on one handle are not re-entrant.  n = 0 .. max_samples. */
+ *    and the workspace.  One handle per stream; calls on one handle are not re-entrant, and graphs that were captured from one
+ *    handle run one after another.  n = 0 .. max_samples; the device that was current at sfb_adapter_init is the one. */
 typedef struct sfb_adapters sfb_adapters;
 #define SFB_ADAPTER_MAX_RANK 128
 typedef struct sfb_adapter_config {
@@ -385,8 +391,9 @@ int sfb_adapter_destroy(sfb_adapters* h);
  *
  *  - Tensor t has counts[t] >= 0 entries of dtypes[t] (0 fp32, 1 bf16, 2 fp16) without gaps at src[t], aligned to its entries; dst[t]
  *    (of the same type) is src[t] itself, or does not overlap any tensor.  dst null: every tensor in place.
- *  - The handle keeps these addresses (the table is copied to the workspace by sfb_clip_init, which waits for that copy),
- *    never values.  One handle per stream; calls on one handle are not re-entrant.
+ *  - The handle keeps these addresses (the table is copied to the workspace by sfb_clip_init, which waits for that copy: not while
+ *    a stream is being captured), never values.  One handle per stream; calls on one handle are not re-entrant, and graphs that were
+ *    captured from one handle run one after another.
  *  - Gradients that lie on several GPUs: sfb_clip_sum writes this handle's sum of squares to sum_dev (fp64), the caller adds those
  *    of all ranks, and sfb_clip_scale takes the total.  sfb_clip_gradients is both. */
 typedef struct sfb_clip sfb_clip;

@@ -509,7 +509,7 @@ __device__ __forceinline__ void read_units(const uint4* src, int at, int g0, int
 // of the accumulator, 128 of them a tile.  Bound by the way of W to the SMs: two CTAs an SM, up to 192 KB of loads under way on it.  A tile
 // a cluster, whose CTAs share the contraction and the k-blocks of the term; the parts are added in rank order, each CTA finishing some of
 // the samples.  The loads of A and z do not wait for the launch before (adapter_rank_kernel lets this one start once those before it are
-// done).  325,000 x 10,000 with 64 samples: 961 us, 6.9 TB/s.  (A CTA an SM that takes its even share of all tiles, with parts through
+// done).  325,000 x 10,000 with 64 samples: 955 to 1,130 us by the GPU, 6.9 to 5.8 TB/s.  (A CTA an SM that takes its even share of all tiles, with parts through
 // global memory: 1,030; 10,000 x 20,000 with 37 samples of 64 adapters 84, here 77.)
 // Warps: 0 TMA producer, 1 MMA issuer and TMEM owner, 2..5 epilogue, 6 and 7 the samples' operand of the term and the
 // loads of its factors, 8 and 9 the look at them.
@@ -710,9 +710,12 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // ---------------------------------------------------------------------------------------------------------
 // The same for more samples, on pairs of CTAs (cta_group::2): a tile of 256 rows of A x tn samples (128 or 256), a CTA 128 of the rows in
 // its TMEM; it loads its own rows and its half of the samples, 32 KB a k-block.  Two accumulators: the end of a tile runs beside the next
-// one's products.  Whole rounds of tiles are taken whole, the k-blocks of the rest are shared out (Segments in sfb_tile.cuh).
-//
-// The pair that finishes a tile has its term.
+// one's products.  Whole rounds of tiles are taken whole, the k-blocks of the rest are shared out (Segments in sfb_tile.cuh); the pair that
+// finishes a tile has its term.
+// Bound by the tensor cores where the contraction is long: 4,096 samples, 10,000 x 20,000: 1,170 us in a loop, 1.40 PFLOP/s, the rate the GPU
+// sustains at its power cap.  Where it is short, by what a k-block of the term waits for: it takes a stage only once that is free, and its
+// copies, the look at them and the other CTA's word come to 4,500 cycles, of which the stages ahead cover 3,000 (1,024 samples of 64 adapters
+// of 8 ranks, 1,000 x 20,000, 57 us: a tile of 16 + 3 k-blocks takes 16,000 cycles, 9,700 of them products).
 //
 // Warps: 0 TMA producer, 1 MMA issuer (leader CTA) and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the columns), 10..13
 // the samples' operand of the term and the loads of its factors, 14..17 the look at them, 18 and 19 hand the other CTA's on to the leader.
@@ -955,8 +958,8 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   } else if (warp >= 2 + kEpi + 2 * kPairBuild) {
     // ---------------- hand on the other CTA's operands ----------------
     // (A release to the cluster by each of the eight warps that make them took 1 us a k-block, and one warp, with no accesses of its own,
-    // that hands all of them on is not much faster: these take them in turn.  Gradients of 1,024 samples of 64 adapters, 1,000 x 20,000: 98,
-    // 89 and 76 us.)
+    // that hands all of them on is not much faster: these take them in turn.  1,024 samples, 1,000 x 20,000, eight k-blocks of the term a tile:
+    // 98, 89 and 76 us.)
     uint32_t s = 0, bph = 0, turn = warp - 2 - kEpi - 2 * kPairBuild;
     bool ok = true;
     for (int i = 0; i < segs.n && ok && rank == 1; ++i) {
@@ -1390,7 +1393,7 @@ __global__ void __launch_bounds__(32 * kIndexWarps) adapter_index_kernel(const _
 // waited for its copies and fenced them had one k-block under way), 8 MMA issuer and TMEM owner, 9..16 epilogue, four of them a half of
 // the columns.
 // Bound by the instructions around a k-block, of which an adapter with few samples has one a tile: 1,024 samples of 64 adapters, 21,000
-// columns, 8 ranks: 63 us with tiles of 128 columns, 40 with 256, 31 with two blocks an SM, which share its TMEM (up to 16 ranks: with more
+// columns, 8 ranks: 63 us with tiles of 128 columns, 40 with 256, 33 with two blocks an SM, which share its TMEM (up to 16 ranks: with more
 // a block has no second accumulator then, and 24 to 32 ranks take 1.2 times as long).
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kLoaders = 8, kGradThreads = 32 * (kLoaders + 9), kGradBuffers = 8, kGradStages = 8, kGradRing = 196608;
