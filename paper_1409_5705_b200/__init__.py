@@ -381,7 +381,9 @@ class Adapters:
         if W.dim() != 2 or U.dim() != 3 or V.dim() != 3 or tuple(U.shape[:2]) != tuple(V.shape[:2]) or \
                 U.shape[2] != W.shape[0] or V.shape[2] != W.shape[1] or tuple(scale.shape) != (U.shape[0],):
             raise ValueError("W [rows, cols], U [adapters, rank, rows], V [adapters, rank, cols], scale [adapters]")
-        self._device = W.device
+        if not W.is_cuda:
+            raise ValueError(f"CUDA tensors are wanted, not one on {W.device}")
+        self._device, self._bf16, self._f32, self._i32 = W.device, bf16, f32, torch.int32
         for t, dt in ((W, bf16), (U, bf16), (V, bf16), (scale, f32)):
             self._check(t, dt)
         for t in (U, V):
@@ -405,9 +407,9 @@ class Adapters:
             raise SfbError(rc, "sfb_adapter_init")
 
     def _check(self, t, dtype):
-        if t.dtype != dtype or t.device != self._device or not t.is_cuda:
+        if t.dtype is not dtype or t.device != self._device:
             raise ValueError(f"a {dtype} tensor on {self._device} is wanted, not {t.dtype} on {t.device}")
-        if t.shape[-1] > 1 and t.stride(-1) != 1:
+        if t.stride(-1) != 1 and t.shape[-1] > 1:
             raise ValueError("the last dimension of a tensor has no gaps")
 
     @staticmethod
@@ -418,17 +420,16 @@ class Adapters:
         return t.stride(0) if t.dim() == 3 and t.shape[0] > 1 else (t.shape[-1] + 7) // 8 * 8
 
     def _operand(self, t, n, width):
-        import torch
-        self._check(t, torch.bfloat16)
-        if t.dim() != 2 or t.shape[0] != n or t.shape[1] != width:
+        self._check(t, self._bf16)
+        if t.shape != (n, width):
             raise ValueError(f"a tensor [{n}, {width}] is wanted, not {list(t.shape)}")
-        return t.data_ptr(), self._pitch(t)
+        return t.data_ptr(), t.stride(0) if n > 1 else (width + 7) // 8 * 8
 
     def _whole(self, t, dtype, shape):
         if t is None:
             return None
         self._check(t, dtype)
-        if tuple(t.shape) != shape or not t.is_contiguous():
+        if t.shape != shape or not t.is_contiguous():
             raise ValueError(f"a contiguous tensor {list(shape)} is wanted, not {list(t.shape)}")
         return t.data_ptr()
 
@@ -439,22 +440,20 @@ class Adapters:
     def sfb_adapter_forward(self, X, ids, Y, S=None):
         """Y [n, rows] (bf16) receives W x_i + scale[a_i] U[a_i]^T V[a_i] x_i for X [n, cols] (bf16) and ids [n] (int32; -1: no
         adapter); S (fp32 [n, rank], may be None) V[a_i] x_i."""
-        import torch
         n = X.shape[0]
         x, ldx = self._operand(X, n, self.cols)
         y, ldy = self._operand(Y, n, self.rows)
-        i, s = self._whole(ids, torch.int32, (n,)), self._whole(S, torch.float32, (n, self.rank))
+        i, s = self._whole(ids, self._i32, (n,)), self._whole(S, self._f32, (n, self.rank))
         self._ck(lib().sfb_adapter_forward(self._h, n, x, ldx, i, y, ldy, s), "sfb_adapter_forward")
 
     def sfb_adapter_backward(self, dY, X, ids, S=None, dX=None, dU=None, dV=None):
         """The gradients for dY [n, rows] (bf16): dX [n, cols] (bf16), dU [adapters, rank, rows] and dV [adapters, rank, cols]
         (fp32, written whole); None: not wanted.  S: what the forward pass gave for these samples; None: computed again."""
-        import torch
-        n, a, r, f32 = X.shape[0], self.adapters, self.rank, torch.float32
+        n, a, r, f32 = X.shape[0], self.adapters, self.rank, self._f32
         x, ldx = self._operand(X, n, self.cols)
         dy, lddy = self._operand(dY, n, self.rows)
         dx, lddx = self._operand(dX, n, self.cols) if dX is not None else (None, 0)
-        i, s = self._whole(ids, torch.int32, (n,)), self._whole(S, f32, (n, r))
+        i, s = self._whole(ids, self._i32, (n,)), self._whole(S, f32, (n, r))
         du, dv = self._whole(dU, f32, (a, r, self.rows)), self._whole(dV, f32, (a, r, self.cols))
         self._ck(lib().sfb_adapter_backward(self._h, n, dy, lddy, x, ldx, i, s, dx, lddx, du, dv), "sfb_adapter_backward")
 

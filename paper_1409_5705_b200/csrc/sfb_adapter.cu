@@ -1,11 +1,12 @@
 // Low-rank adapters of many requests beside the shared W (sfb_adapter_* in sfb.h): the logits of samples, each with the adapter
 // (a set of factor pairs) that its request names, and the gradients of the samples and of the adapters' factors.
 //
-// Launches of a forward pass of up to 64 samples:  adapter_rank_kernel (s = V x), adapter_few_kernel (y = W x + scale U^T s).  Of more:
-// adapter_index_kernel and adapter_copy_kernel (where the samples had better be taken in the order of their adapters, or copied because of the
-// way their rows lie), adapter_rank_kernel, adapter_sum_kernel (what follows s), adapter_pair_kernel (y).
+// Launches of a forward pass of up to 64 samples:  adapter_dot_kernel or, for many entries, adapter_rank_kernel (s = V x), adapter_few_kernel
+// (y = W x + scale U^T s).  Of more:  adapter_index_kernel and adapter_copy_kernel (where the samples had better be taken in the order of their
+// adapters, or copied because of the way their rows lie), adapter_dot_kernel or adapter_rank_kernel and adapter_sum_kernel (s, and what follows
+// it), adapter_pair_kernel (y).
 // Of a backward pass:  adapter_index_kernel (the samples of each adapter), the products as in a forward pass (t = U dy, dx), adapter_words_kernel
-// where adapter_sum_kernel has not done its work, adapter_gradient_kernel (dU, dV).
+// where none of them has done its work, adapter_gradient_kernel (dU, dV).
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -1162,14 +1163,10 @@ struct SumParams {
   WordsParams words;           // of p (p[1], from here) and of the other side's products
 };
 
-__global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant__ SumParams p) {
+// Blocks 0 .. tiles: a tile's list; what the gradients' blocks share the work by.
+__device__ __forceinline__ void lists_and_work(const SumParams& p, int tile, const int32_t* ids) {
   __shared__ alignas(16) TileList<kMaxTile> L;
   __shared__ int64_t sums[256];
-  pdl_launch_dependents();
-  pdl_wait();
-  const int tile = blockIdx.x;
-  const bool sorted = p.sort.on();
-  const int32_t* ids = sorted ? p.sort.ids : p.ids;
   if (tile < p.tiles) {
     const int first = tile * p.tn;
     build_list(L, ids, first, static_cast<int>(p.n), p.tn, p.adapters, p.status);
@@ -1179,12 +1176,21 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
       if (t < L.count) to[1 + t] = L.list[t];
       if (first + t < p.n) p.place[first + t] = L.place[t];
     }
-    return;
+  } else {
+    sum_work(p.words, sums);
   }
+}
+
+__global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant__ SumParams p) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int tile = blockIdx.x;
+  const bool sorted = p.sort.on();
+  const int32_t* ids = sorted ? p.sort.ids : p.ids;
   const bool wanted = p.words.out[0] || p.words.out[1];
   const int more = p.tiles + (wanted ? 1 : 0);
   if (tile < more) {
-    sum_work(p.words, sums);
+    lists_and_work(p, tile, ids);
     return;
   }
   const int per = (p.rank + kUnit - 1) / kUnit, rp = (p.rank + 15) & ~15;
@@ -1249,6 +1255,96 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
       put_words(to + row, rp, u);
       if (behind) put_words(to + row + kUnit, rp, zeros);
     }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------
+// adapter_rank_kernel and adapter_sum_kernel in one for few entries in all, in fp32 FMAs: a block takes four ranks of one sample, its threads
+// pieces of 16 bytes of the contraction.  Bound by latency: ids, then the factors, then the block's sum, where the tensor cores have tiles to
+// set up, parts to add and a list ahead of their first load.  (us a forward pass, those and this one: 1 sample of 16 ranks, 10,000 x 5,000:
+// 24.5 and 22.3; 16, 2,000 x 3,000: 17 and 11; 64, 22 and 12; 37, 10,000 x 20,000: 77.6 and 72.7; 64 of 64 ranks, 2,000 x 10,000: 30.8 and 27.5,
+// 2,000 x 20,000: 40.0 and 41.6; 64 of 128 and 30 adapters, 2,000 x 20,000: 64 and 72; 100 of 16, 2,000 x 3,000: 40 and 27; 200 of 16, 5,000 x
+// 10,000: 68 and 56.  Gradients: 128 samples of 4 ranks, 64 x 256: 34 and 22; 1,000 of 16, 2,000 x 3,000: 61 and 62.)
+// ---------------------------------------------------------------------------------------------------------
+constexpr int kDotRanks = 4;
+struct DotParams {
+  SumParams s;                 // s.p: not used
+  const __nv_bfloat16 *F, *Z;
+  int64_t ldf, ldz;
+  int32_t d;
+};
+__device__ __forceinline__ void dot8(const uint4& a, const uint4& b, float& sum) {
+  const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    sum = fmaf(__uint_as_float(x[j] << 16), __uint_as_float(y[j] << 16), sum);
+    sum = fmaf(__uint_as_float(x[j] & 0xffff0000u), __uint_as_float(y[j] & 0xffff0000u), sum);
+  }
+}
+
+__global__ void __launch_bounds__(256) adapter_dot_kernel(const __grid_constant__ DotParams p) {
+  __shared__ float part[8][kDotRanks];
+  pdl_wait();
+  pdl_launch_dependents();
+  const SumParams& q = p.s;
+  const bool sorted = q.sort.on(), wanted = q.words.out[0] || q.words.out[1];
+  const int more = q.tiles + (wanted ? 1 : 0), block = static_cast<int>(blockIdx.x) - more;
+  if (block < 0) {
+    lists_and_work(q, blockIdx.x, sorted ? q.sort.ids : q.ids);
+    return;
+  }
+  const int rank = q.rank, per8 = (rank + kUnit - 1) / kUnit * kUnit, groups = per8 / kDotRanks;
+  const int i = block / groups, r0 = (block - i * groups) * kDotRanks, sample = sorted ? q.sort.order[i] : i, id = q.ids[sample];
+  const bool has = id >= 0 && id < q.adapters;
+  float sum[kDotRanks] = {};
+  if (has && r0 < rank) {
+    const __nv_bfloat16* z = p.Z + sample * p.ldz;
+    const __nv_bfloat16* f[kDotRanks];
+#pragma unroll
+    for (int r = 0; r < kDotRanks; ++r) f[r] = p.F + (static_cast<int64_t>(id) * rank + min(r0 + r, rank - 1)) * p.ldf;
+    const int whole = p.d / 8;
+#pragma unroll 2
+    for (int c = threadIdx.x; c < whole; c += 256) {
+      const uint4 a = *reinterpret_cast<const uint4*>(z + c * 8);
+      uint4 b[kDotRanks];
+#pragma unroll
+      for (int r = 0; r < kDotRanks; ++r) b[r] = *reinterpret_cast<const uint4*>(f[r] + c * 8);
+#pragma unroll
+      for (int r = 0; r < kDotRanks; ++r) dot8(a, b[r], sum[r]);
+    }
+    const int e = whole * 8 + threadIdx.x;
+    if (e < p.d)
+#pragma unroll
+      for (int r = 0; r < kDotRanks; ++r) sum[r] = fmaf(__bfloat162float(z[e]), __bfloat162float(f[r][e]), sum[r]);
+  }
+#pragma unroll
+  for (int r = 0; r < kDotRanks; ++r) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], o);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5][r] = sum[r];
+  }
+  __syncthreads();
+  const int rp = (rank + 15) & ~15, r = r0 + threadIdx.x;
+  // the last block of a sample also has the words behind the ranks
+  if (r >= (r0 + kDotRanks == per8 ? rp : r0 + kDotRanks)) return;
+  float v = 0.f;
+  if (threadIdx.x < kDotRanks)
+#pragma unroll
+    for (int w = 0; w < 8; ++w) v += part[w][threadIdx.x];
+  const int64_t at = static_cast<int64_t>(sample) * rank + r;
+  const float sc = has ? q.scale[id] : 0.f;
+  if (r < rank) q.out[at] = v;
+  if (r < per8) q.pb[static_cast<int64_t>(i) * per8 + r] = __float2bfloat16_rn(has && r < rank ? sc * v : 0.f);
+  if (!wanted || !has) return;
+  const int64_t row = static_cast<int64_t>(q.words.position[sample]) * 3 * rp + r;
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    __nv_bfloat16* to = q.words.out[side];
+    if (!to) continue;
+    float w[3];
+    three_words(r < rank ? sc * (side ? v : ranked(q.words.p[0], at)) : 0.f, w);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) to[row + k * rp] = __float2bfloat16_rn(w[k]);
   }
 }
 
@@ -1797,7 +1893,11 @@ cudaError_t allow_beside(int bytes) {
 }
 
 // The samples' operand: as it is, or a copy whose rows lie better; and in the order of their adapters, where sort.on() says so.
+constexpr int64_t kDotMost = 48 << 20;               // n x ranks x entries up to which adapter_dot_kernel is the faster one
+constexpr int64_t kDotUnits = 2048;                  // ... and samples x units of ranks
 struct Samples {
+  const void* given;
+  int64_t given_pitch;
   const void* at;
   int64_t pitch;
   const void* in_order;
@@ -1805,13 +1905,35 @@ struct Samples {
   Sorting sort;
 };
 
-// p = F[a] z for n samples.  *got: where, and in how many parts.  Up to 64 samples it is in `sum` in one part, with all that a product
-// with the other factors (MN: with V) takes; for more adapter_sum_kernel has to follow.
+SumParams sum_params(const sfb_adapters* h, int64_t n, const Sorting& sort, const int32_t* ids, float* out, const WordsParams& words) {
+  SumParams p{};
+  p.ids = ids; p.sort = sort; p.scale = h->scale; p.n = n; p.rank = h->cfg.rank; p.adapters = h->cfg.adapters; p.out = out;
+  p.status = h->at<uint32_t>(h->lay.status);
+  p.pb = h->at<__nv_bfloat16>(h->lay.pb);
+  p.tn = tile_of(n); p.tiles = static_cast<int32_t>((n + p.tn - 1) / p.tn); p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place);
+  p.words = words;
+  return p;
+}
+
+// p = F[a] z for n samples.  *got: where, and in how many parts.  *all: it is in `sum` in one part, with all that a product with the other
+// factors (MN: with V) takes, and the words that are wanted.  So it is up to 64 samples, but for the words; for more adapter_sum_kernel has to
+// follow.
 template <bool MN>
-cudaError_t rank_products(sfb_adapters* h, int64_t n, const Samples& z, const int32_t* ids, float* out, float* sum, Ranked* got) {
+cudaError_t rank_products(sfb_adapters* h, int64_t n, const Samples& z, const int32_t* ids, float* out, float* sum, const WordsParams& words, Ranked* got,
+                          bool* all) {
   const sfb_adapter_config& c = h->cfg;
   const int64_t d = MN ? c.rows : c.cols;
   const int tn = rank_tile(n), parts = rank_parts(n, d), tiles = static_cast<int>((n + tn - 1) / tn);
+  *all = n * c.rank * d <= kDotMost && n * ((c.rank + kUnit - 1) / kUnit) <= kDotUnits;
+  if (*all) {
+    *got = Ranked{sum, 1, 0};
+    DotParams p{};
+    p.s = sum_params(h, n, z.sort, ids, sum, words);
+    p.F = static_cast<const __nv_bfloat16*>(MN ? h->U : h->V); p.Z = static_cast<const __nv_bfloat16*>(z.given);
+    p.ldf = MN ? c.ldu : c.ldv; p.ldz = z.given_pitch; p.d = static_cast<int32_t>(d);
+    const int64_t blocks = n * ((c.rank + kUnit - 1) / kUnit) * (kUnit / kDotRanks) + p.s.tiles + (words.out[0] || words.out[1] ? 1 : 0);
+    return launch_kernel(adapter_dot_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, h->stream, 1, p);
+  }
   const CUtensorMap& mf = MN ? h->mapU : h->mapV;
   CUtensorMap mz, ms;
   if (!operand_map(h, &mz, z.at, d, n, z.pitch, BK, tn, CU_TENSOR_MAP_L2_PROMOTION_L2_256B) ||
@@ -1862,7 +1984,7 @@ bool fits(int64_t outer, int64_t inner, size_t bytes) { return bytes >= static_c
 cudaError_t placed(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, int64_t d, int64_t uses, const Sorting& sort, Samples* z) {
   const size_t room = h->lay.order - h->lay.zcopy;
   const bool copy = n > kFewMost && pitch_odd(ldz) && uses >= kCopyUses && fits(n, d, room);
-  *z = Samples{Z, ldz, Z, ldz, sort};
+  *z = Samples{Z, ldz, Z, ldz, Z, ldz, sort};
   if (!copy && !sort.sorted) return cudaSuccess;
   z->in_order = h->at<char>(h->lay.zcopy);
   z->pitch_in_order = round_up(d, BK);
@@ -1950,24 +2072,25 @@ cudaError_t pairs(sfb_adapters* h, int64_t n, const Samples& z, const Term& term
                           dim3(kPairThreads), kPairSmem, h->stream, 1, ma, mz, ms, MN ? h->unitV : h->unitU, p);
 }
 
-// y = A z + scale F^T p.  p in parts goes to `to` first, and for more than 64 samples to the words that are wanted; *s: p where it is afterwards.
+// y = A z + scale F^T p.  Unless all is there already, p of more than 64 samples goes from its parts to `to` first, and to the words that are
+// wanted; *s: p where it is afterwards.
 template <bool MN>
-cudaError_t product(sfb_adapters* h, int64_t n, const Samples& z, const int32_t* ids, Ranked* s, float* to, void* Y, int64_t ldy, const WordsParams& words) {
+cudaError_t product(sfb_adapters* h, int64_t n, const Samples& z, const int32_t* ids, bool all, Ranked* s, float* to, void* Y, int64_t ldy,
+                    const WordsParams& words) {
   const sfb_adapter_config& c = h->cfg;
   if (n <= kFewMost) {
     const Term term = term_of<MN>(h, ids, s->at);
     return n <= 16 ? few<16, MN>(h, n, z.at, z.pitch, term, Y, ldy) : n <= 32 ? few<32, MN>(h, n, z.at, z.pitch, term, Y, ldy)
                                                                              : few<kFewMost, MN>(h, n, z.at, z.pitch, term, Y, ldy);
   }
-  SumParams p{};
-  p.p = *s; p.ids = ids; p.sort = z.sort; p.scale = h->scale; p.n = n; p.rank = c.rank; p.adapters = c.adapters; p.out = to; p.status = h->at<uint32_t>(h->lay.status);
-  p.pb = h->at<__nv_bfloat16>(h->lay.pb);
-  p.tn = tile_of(n); p.tiles = static_cast<int32_t>((n + p.tn - 1) / p.tn); p.lists = h->at<int32_t>(h->lay.lists); p.place = h->at<int32_t>(h->lay.place);
-  p.words = words;
-  const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(p.tiles + (words.out[0] || words.out[1] ? 1 : 0) + grid1d(n * ((c.rank + kUnit - 1) / kUnit), 64)), dim3(256), 0, h->stream,
-                                      1, p);
-  if (e != cudaSuccess) return e;
-  *s = Ranked{to, 1, 0};
+  if (!all) {
+    SumParams p = sum_params(h, n, z.sort, ids, to, words);
+    p.p = *s;
+    const cudaError_t e = launch_kernel(adapter_sum_kernel, dim3(p.tiles + (words.out[0] || words.out[1] ? 1 : 0) + grid1d(n * ((c.rank + kUnit - 1) / kUnit), 64)),
+                                        dim3(256), 0, h->stream, 1, p);
+    if (e != cudaSuccess) return e;
+    *s = Ranked{to, 1, 0};
+  }
   return pairs<MN>(h, n, z, term_of<MN>(h, ids, to), Y, ldy);
 }
 
@@ -2079,8 +2202,9 @@ extern "C" int sfb_adapter_forward(sfb_adapters* h, int64_t n, const void* X_dev
   Samples z;
   if (sorts(h, n, c.cols)) ACK(index_samples(h, n, ids_dev, &sort));
   ACK(placed(h, n, X_dev, ldx, c.cols, c.rows, sort, &z));
-  ACK(rank_products<false>(h, n, z, ids_dev, h->at<float>(h->lay.s), sum, &s));
-  ACK(product<false>(h, n, z, ids_dev, &s, sum, Y_dev, ldy, WordsParams{}));
+  bool all;
+  ACK(rank_products<false>(h, n, z, ids_dev, h->at<float>(h->lay.s), sum, WordsParams{}, &s, &all));
+  ACK(product<false>(h, n, z, ids_dev, all, &s, sum, Y_dev, ldy, WordsParams{}));
   return SFB_OK;
 }
 
@@ -2108,29 +2232,30 @@ extern "C" int sfb_adapter_backward(sfb_adapters* h, int64_t n, const void* dY_d
   const bool sorting = dX_dev && sorts(h, n, c.rows);
   if (dU_dev || dV_dev || sorting) ACK(index_samples(h, n, ids_dev, sorting ? &sort : nullptr));
   Ranked s{S_dev, 1, 0}, t{};
-  if (dU_dev && !S_dev)
-    ACK(rank_products<false>(h, n, Samples{X_dev, ldx, X_dev, ldx, Sorting{}}, ids_dev, h->at<float>(h->lay.s), h->at<float>(h->lay.ssum), &s));
-  Samples z{dY_dev, lddy, dY_dev, lddy, Sorting{}};
-  if (dX_dev) ACK(placed(h, n, dY_dev, lddy, c.rows, c.cols, sort, &z));
-  if (dX_dev || dV_dev) ACK(rank_products<true>(h, n, z, ids_dev, h->at<float>(h->lay.t), h->at<float>(h->lay.tsum), &t));
-  __nv_bfloat16 *swords = h->at<__nv_bfloat16>(h->lay.swords), *twords = h->at<__nv_bfloat16>(h->lay.twords);
+  bool all = false;
+  Samples z{X_dev, ldx, X_dev, ldx, X_dev, ldx, Sorting{}};
+  if (dU_dev && !S_dev) ACK(rank_products<false>(h, n, z, ids_dev, h->at<float>(h->lay.s), h->at<float>(h->lay.ssum), WordsParams{}, &s, &all));
   WordsParams w{};
-  w.out[0] = dU_dev ? swords : nullptr; w.out[1] = dV_dev ? twords : nullptr;
-  w.p[0] = s; w.p[1] = t;
+  w.out[0] = dU_dev ? h->at<__nv_bfloat16>(h->lay.swords) : nullptr; w.out[1] = dV_dev ? h->at<__nv_bfloat16>(h->lay.twords) : nullptr;
+  w.p[0] = s;
   w.ids = ids_dev; w.order = order; w.begin = begin; w.count = count; w.position = h->at<int32_t>(h->lay.position);
   w.work = h->at<int64_t>(h->lay.work); w.scale = h->scale; w.rank = c.rank; w.adapters = c.adapters;
-  if (dX_dev) ACK(product<true>(h, n, z, ids_dev, &t, h->at<float>(h->lay.tsum), dX_dev, lddx, w));
+  all = false;
+  z = Samples{dY_dev, lddy, dY_dev, lddy, dY_dev, lddy, Sorting{}};
+  if (dX_dev) ACK(placed(h, n, dY_dev, lddy, c.rows, c.cols, sort, &z));
+  if (dX_dev || dV_dev) ACK(rank_products<true>(h, n, z, ids_dev, h->at<float>(h->lay.t), h->at<float>(h->lay.tsum), w, &t, &all));
+  if (dX_dev) ACK(product<true>(h, n, z, ids_dev, all, &t, h->at<float>(h->lay.tsum), dX_dev, lddx, w));
   if (dU_dev || dV_dev) {
-    if (!dX_dev || n <= kFewMost) {
+    if (!all && (!dX_dev || n <= kFewMost)) {
       w.p[1] = t;
       ACK(launch_kernel(adapter_words_kernel, dim3(grid1d(n * ((c.rank + 15) / 16 * 2), 256), 3), dim3(256), 0, h->stream, 1, w));
     }
     GradParams p{};
     const int tile = grad_halves(c.rank) * BM;
     if (dU_dev)
-      p.side[0] = GradSide{static_cast<const __nv_bfloat16*>(dY_dev), lddy, static_cast<int32_t>(c.rows), static_cast<int32_t>((c.rows + tile - 1) / tile), swords, dU_dev};
+      p.side[0] = GradSide{static_cast<const __nv_bfloat16*>(dY_dev), lddy, static_cast<int32_t>(c.rows), static_cast<int32_t>((c.rows + tile - 1) / tile), w.out[0], dU_dev};
     if (dV_dev)
-      p.side[1] = GradSide{static_cast<const __nv_bfloat16*>(X_dev), ldx, static_cast<int32_t>(c.cols), static_cast<int32_t>((c.cols + tile - 1) / tile), twords, dV_dev};
+      p.side[1] = GradSide{static_cast<const __nv_bfloat16*>(X_dev), ldx, static_cast<int32_t>(c.cols), static_cast<int32_t>((c.cols + tile - 1) / tile), w.out[1], dV_dev};
     p.rank = c.rank; p.adapters = c.adapters; p.order = order; p.begin = begin; p.count = count; p.work = w.work; p.status = status;
     const int64_t items = (static_cast<int64_t>(p.side[0].tiles) + p.side[1].tiles) * c.adapters;
     const int stage = grad_stage(c.rank);
