@@ -6,7 +6,7 @@
 // adapters, or copied because of the way their rows lie), adapter_dot_kernel or adapter_rank_kernel and adapter_sum_kernel (s, and what follows
 // it), adapter_pair_kernel (y).
 // Of a backward pass:  adapter_index_kernel (the samples of each adapter), the products as in a forward pass (t = U dy, dx), adapter_words_kernel
-// where none of them has done its work, adapter_gradient_kernel (dU, dV).
+// where none of them has done its work, adapter_gradient_kernel (dU, dV), adapter_join_kernel where few adapters' samples are cut into shares.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -1059,12 +1059,18 @@ struct WordsParams {
   __nv_bfloat16* out[2];       // both null: none
   const int32_t *ids, *order, *begin, *count;
   const int32_t* position;     // of a sample in `order`
-  int64_t* work;               // [adapters + 1]: what a column tile takes of the adapters before each one (see adapter_work)
+  int64_t* work;               // [adapters * shares + 1]: what a column tile takes of the shares of adapters before each one (see adapter_work)
   const float* scale;
-  int32_t rank, adapters;
+  int32_t rank, adapters, shares;
 };
 // What a tile of dF[a] costs, in k-blocks: its contraction, and its end.
 __device__ __forceinline__ int adapter_work(int count) { return (count + BK - 1) / BK + 1; }
+// Share c of `shares` of an adapter's samples, in whole k-blocks: where it begins, and how many they are.
+__device__ __forceinline__ int share_of(int count, int shares, int c, int* first) {
+  const int each = ((count + BK - 1) / BK + shares - 1) / shares * BK;
+  *first = min(c * each, count);
+  return min(each, count - *first);
+}
 // v = w0 + w1 + w2.  (What overflows in the rounding to the first word is cut off instead; of what is not finite there is no rest.)
 __device__ __forceinline__ void three_words(float v, float (&w)[3]) {
   w[0] = __bfloat162float(__float2bfloat16_rn(v));
@@ -1092,9 +1098,14 @@ __device__ __forceinline__ void put_words(__nv_bfloat16* to, int rp, const float
 }
 // work, by a block of 256 threads.
 __device__ __forceinline__ void sum_work(const WordsParams& p, int64_t (&sums)[256]) {
-  const int each = (p.adapters + 255) / 256, from = min(static_cast<int>(threadIdx.x) * each, p.adapters), to = min(from + each, p.adapters);
+  const int all_shares = p.adapters * p.shares, each = (all_shares + 255) / 256;
+  const int from = min(static_cast<int>(threadIdx.x) * each, all_shares), to = min(from + each, all_shares);
+  auto work = [&](int x) {
+    int first;
+    return adapter_work(share_of(p.count[x / p.shares], p.shares, x % p.shares, &first));
+  };
   int64_t s = 0;
-  for (int a = from; a < to; ++a) s += adapter_work(p.count[a]);
+  for (int a = from; a < to; ++a) s += work(a);
   sums[threadIdx.x] = s;
   __syncthreads();
   if (threadIdx.x < 32) {                            // a lane the eight sums from 8 * lane on
@@ -1113,8 +1124,8 @@ __device__ __forceinline__ void sum_work(const WordsParams& p, int64_t (&sums)[2
   }
   __syncthreads();
   s = sums[threadIdx.x];
-  for (int a = from; a < to; ++a) { p.work[a] = s; s += adapter_work(p.count[a]); }
-  if (to == p.adapters && from < to) p.work[p.adapters] = s;
+  for (int a = from; a < to; ++a) { p.work[a] = s; s += work(a); }
+  if (to == all_shares && from < to) p.work[all_shares] = s;
 }
 
 __global__ void __launch_bounds__(256) adapter_words_kernel(const __grid_constant__ WordsParams p) {
@@ -1498,11 +1509,12 @@ struct GradSide {
   int64_t ldz;
   int32_t width, tiles;        // columns; tiles of them (0: not wanted)
   const __nv_bfloat16* words;
-  float* out;                  // [adapters][rank][width]
+  float* out;                  // [adapters][rank][width]: of the first share
+  float* more;                 // [shares - 1][adapters][rank][width]: of the others
 };
 struct GradParams {
   GradSide side[2];
-  int32_t rank, adapters, stages;
+  int32_t rank, adapters, shares, stages;
   const int32_t *order, *begin, *count;
   const int64_t* work;
   uint32_t* status;
@@ -1519,16 +1531,16 @@ __host__ __device__ inline int grad_stage(int rank) { return grad_halves(rank) *
 struct GradWalk {
   const GradParams& p;
   GradSide sd;
-  int side, a, tile, count, begin;
-  int64_t at, end;             // where the tile's work begins; the end of the block's share
+  int side, a, tile, count, begin;      // a: share a % shares of adapter a / shares
+  int64_t at, end;             // where the tile's work begins; the end of the block's part of all work
   __device__ __forceinline__ GradWalk(const GradParams& p_) : p(p_) {
-    const int64_t each = p.work[p.adapters], first = each * p.side[0].tiles, all = first + each * p.side[1].tiles;
+    const int64_t each = p.work[p.adapters * p.shares], first = each * p.side[0].tiles, all = first + each * p.side[1].tiles;
     at = all * blockIdx.x / gridDim.x;
     end = all * (blockIdx.x + 1) / gridDim.x;
     side = at >= first;
     sd = side ? p.side[1] : p.side[0];
     const int64_t base = side ? first : 0, tiles = sd.tiles;
-    int lo = 0, len = at < end ? p.adapters : 1;     // the last adapter whose work begins at or before `at`
+    int lo = 0, len = at < end ? p.adapters * p.shares : 1;     // the last adapter whose work begins at or before `at`
     const int lane = threadIdx.x & 31;
     while (len > 1) {
       const int step = (len + 31) / 32, x = lane * step;
@@ -1544,11 +1556,22 @@ struct GradWalk {
     at = from + tile * w;
     settle();
   }
-  __device__ __forceinline__ void load() { count = p.count[a]; begin = p.begin[a]; }
+  __device__ __forceinline__ void load() {
+    const int of = a / p.shares;
+    int first;
+    count = share_of(p.count[of], p.shares, a - of * p.shares, &first);
+    begin = p.begin[of] + first;
+  }
+  // where the share's dF goes
+  __device__ __forceinline__ float* out() const {
+    const int of = a / p.shares, c = a - of * p.shares;
+    const int64_t entries = static_cast<int64_t>(p.rank) * sd.width;
+    return (c ? sd.more + static_cast<int64_t>(c - 1) * p.adapters * entries : sd.out) + of * entries;
+  }
   __device__ __forceinline__ void settle() {
     while (at < end && tile >= sd.tiles) {
       tile = 0;
-      if (++a == p.adapters) {
+      if (++a == p.adapters * p.shares) {
         a = 0;
         if (++side > 1) { at = end; return; }
         sd = p.side[1];
@@ -1684,7 +1707,7 @@ __global__ void __launch_bounds__(kGradThreads, BLOCKS) adapter_gradient_kernel(
       const int m = (it.tile * static_cast<int>(halves) + static_cast<int>(h)) * BM + q * 32 + lane, nk = (it.count + BK - 1) / BK;
       const bool in = m < sd.width;
       const int64_t width = sd.width;
-      float* const out = sd.out + static_cast<int64_t>(it.a) * p.rank * width + m;
+      float* const out = it.out() + m;
       if (nk == 0 && in) {
         float* to = out;
         for (int r = 0; r < p.rank; ++r, to += width) *to = 0.f;
@@ -1737,6 +1760,29 @@ __global__ void __launch_bounds__(kGradThreads, BLOCKS) adapter_gradient_kernel(
   if (warp == kLoaders) { tc_fence_after(); tmem_dealloc(tmem_base, kColumns); }
 }
 
+// The shares of dF added up, in their order.  (16-byte pieces where there are only whole ones.)
+__global__ void __launch_bounds__(256) adapter_join_kernel(float* out, const float* more, int64_t entries, int shares) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int64_t step = static_cast<int64_t>(gridDim.x) * 256, first = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (entries % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0) {
+    for (int64_t x = first; x < entries / 4; x += step) {
+      float4 v = reinterpret_cast<float4*>(out)[x];
+      for (int c = 0; c + 1 < shares; ++c) {
+        const float4 w = reinterpret_cast<const float4*>(more + c * entries)[x];
+        v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+      }
+      reinterpret_cast<float4*>(out)[x] = v;
+    }
+  } else {
+    for (int64_t x = first; x < entries; x += step) {
+      float v = out[x];
+      for (int c = 0; c + 1 < shares; ++c) v += more[c * entries + x];
+      out[x] = v;
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------------------
@@ -1757,6 +1803,15 @@ int64_t rank_rows(int64_t n, int64_t d) {
   return std::max(most, n);
 }
 
+// Shares that the samples of every adapter are cut into for the gradients: as many as the SMs have room for beside one another, of four
+// k-blocks at least on average, since a block takes the k-blocks of a tile one after another.
+// (us, gradients with one share and with these: 8,192 samples of one adapter of 16 ranks, 4,096 x 4,096: 427 and 253; 2,048, 1,000 x 1,000: 80 and
+// 60; 12,000 of 8 adapters of 1 rank, 40 x 100: 137 and 76.)
+int grad_shares(const sfb_adapter_config& c, int64_t n) {
+  const int64_t tile = grad_halves(c.rank) * BM, items = ((c.rows + tile - 1) / tile + (c.cols + tile - 1) / tile) * c.adapters;
+  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({8, grad_blocks(c.rank) * kModelSms / items, n / c.adapters / (4 * BK)})));
+}
+
 // Whether n samples, each with an adapter at random, had better be taken in the order of their adapters (see adapter_index_kernel), and would
 // read 32 MB less of factors, 5 us, which is what finding out takes.
 bool sort_may_pay(const sfb_adapter_config& c, int64_t n) {
@@ -1768,8 +1823,8 @@ bool sort_may_pay(const sfb_adapter_config& c, int64_t n) {
 bool pitch_odd(int64_t pitch) { return pitch % 16 != 0; }      // of bf16 entries: not a multiple of 32 bytes
 
 struct AdapterLayout {
-  size_t status, ready, arrived, tally, sorted, s, t, ssum, tsum, pb, swords, twords, order, sorted_ids, begin, count, position, work, lists, place, partial, wcopy,
-      zcopy, total;
+  size_t status, ready, arrived, tally, sorted, s, t, ssum, tsum, pb, swords, twords, order, sorted_ids, begin, count, position, work, gparts, lists,
+      place, partial, wcopy, zcopy, total;
 };
 
 int check(const sfb_adapter_config* c) {
@@ -1814,7 +1869,9 @@ AdapterLayout layout_of(const sfb_adapter_config& c) {
   L.sorted_ids = take(sorts ? n * 4 : 0);
   L.begin = take(static_cast<size_t>(c.adapters) * 4);
   L.position = take(n * 4);
-  L.work = take((static_cast<size_t>(c.adapters) + 1) * 8);
+  const size_t shares = grad_shares(c, c.max_samples);
+  L.work = take((static_cast<size_t>(c.adapters) * shares + 1) * 8);
+  L.gparts = take((shares - 1) * c.adapters * c.rank * (round_up(c.rows, 4) + round_up(c.cols, 4)) * 4);
   L.count = take(static_cast<size_t>(c.adapters) * 4);
   L.total = off;
   return L;
@@ -2240,6 +2297,7 @@ extern "C" int sfb_adapter_backward(sfb_adapters* h, int64_t n, const void* dY_d
   w.p[0] = s;
   w.ids = ids_dev; w.order = order; w.begin = begin; w.count = count; w.position = h->at<int32_t>(h->lay.position);
   w.work = h->at<int64_t>(h->lay.work); w.scale = h->scale; w.rank = c.rank; w.adapters = c.adapters;
+  w.shares = grad_shares(c, n);
   all = false;
   z = Samples{dY_dev, lddy, dY_dev, lddy, dY_dev, lddy, Sorting{}};
   if (dX_dev) ACK(placed(h, n, dY_dev, lddy, c.rows, c.cols, sort, &z));
@@ -2252,12 +2310,14 @@ extern "C" int sfb_adapter_backward(sfb_adapters* h, int64_t n, const void* dY_d
     }
     GradParams p{};
     const int tile = grad_halves(c.rank) * BM;
+    const int64_t pairs_all = static_cast<int64_t>(c.adapters) * c.rank, others = (w.shares - 1) * pairs_all;
+    float* more = h->at<float>(h->lay.gparts);
     if (dU_dev)
-      p.side[0] = GradSide{static_cast<const __nv_bfloat16*>(dY_dev), lddy, static_cast<int32_t>(c.rows), static_cast<int32_t>((c.rows + tile - 1) / tile), w.out[0], dU_dev};
+      p.side[0] = GradSide{static_cast<const __nv_bfloat16*>(dY_dev), lddy, static_cast<int32_t>(c.rows), static_cast<int32_t>((c.rows + tile - 1) / tile), w.out[0], dU_dev, more};
     if (dV_dev)
-      p.side[1] = GradSide{static_cast<const __nv_bfloat16*>(X_dev), ldx, static_cast<int32_t>(c.cols), static_cast<int32_t>((c.cols + tile - 1) / tile), w.out[1], dV_dev};
-    p.rank = c.rank; p.adapters = c.adapters; p.order = order; p.begin = begin; p.count = count; p.work = w.work; p.status = status;
-    const int64_t items = (static_cast<int64_t>(p.side[0].tiles) + p.side[1].tiles) * c.adapters;
+      p.side[1] = GradSide{static_cast<const __nv_bfloat16*>(X_dev), ldx, static_cast<int32_t>(c.cols), static_cast<int32_t>((c.cols + tile - 1) / tile), w.out[1], dV_dev, more + others * round_up(c.rows, 4)};
+    p.rank = c.rank; p.adapters = c.adapters; p.shares = w.shares; p.order = order; p.begin = begin; p.count = count; p.work = w.work; p.status = status;
+    const int64_t items = (static_cast<int64_t>(p.side[0].tiles) + p.side[1].tiles) * c.adapters * w.shares;
     const int stage = grad_stage(c.rank);
     const int blocks = grad_blocks(c.rank);
     p.stages = std::min(kGradStages, kGradRing / blocks / stage);
@@ -2270,6 +2330,10 @@ extern "C" int sfb_adapter_backward(sfb_adapters* h, int64_t n, const void* dY_d
       ACK(allow_smem<adapter_gradient_kernel<1>>(kGradRing + 1024));
       ACK(launch_kernel(adapter_gradient_kernel<1>, grid, dim3(kGradThreads), smem, h->stream, 1, p));
     }
+    for (const GradSide& sd : p.side)
+      if (sd.tiles && w.shares > 1)
+        ACK(launch_kernel(adapter_join_kernel, dim3(grid1d(pairs_all * sd.width / 4 + 1, 256)), dim3(256), 0, h->stream, 1, sd.out,
+                          static_cast<const float*>(sd.more), pairs_all * sd.width, w.shares));
   }
   return SFB_OK;
 }

@@ -164,6 +164,13 @@ SIZES = [
     (333, 9000, 1000, 150, 128, "mixed"),
     (4160, 2100, 4104, 64, 16, "mixed"),
     (1024, 6000, 6000, 100, 20, "none"),
+    # few adapters with many samples each, whose gradients are summed in shares
+    (3000, 300, 500, 1, 16, "mixed"),
+    (2600, 131, 77, 2, 7, "runs"),
+    (1700, 100, 900, 2, 100, "every"),
+    # samples of few entries, by themselves and in the order of their adapters
+    (70, 50, 60, 3, 20, "mixed"),
+    (400, 30, 3000, 300, 8, "mixed"),
     # as many samples of one adapter as are taken out of the accumulators in several turns; the widest adapters
     (3000, 300, 200, 1, 20, "one"),
     (900, 136, 264, 2, 128, "mixed"),
