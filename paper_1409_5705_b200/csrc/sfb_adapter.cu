@@ -1399,9 +1399,10 @@ __global__ void __launch_bounds__(256) adapter_copy_kernel(const uint4* in, int6
 //
 // Whether the products had better take the samples in that order: a tile of samples reads the factors of each adapter among them, and its
 // share of the term grows by as much, while samples in order have to be copied.  More blocks (tiles of them) count the adapters of each 128
-// samples as they come, and the last block of all compares what a column costs: 2 bytes a rank of each pair of a tile and an adapter that
-// there are fewer of, against 4 a sample.  (Gradients, us as the samples come and in order: 1,024 samples of 64 adapters of 8 ranks at random,
-// 1,000 x 20,000: 143 and 132; 2,000 of 100 adapters of 32 ranks, 5,000 x 5,000: 330 and 206; 4,096 of 8 adapters of 128, 4,000 x 20,000: 855
+// samples as they come, and the last block of all compares the bytes: a factor's entries times the ranks of the pairs of a tile and an
+// adapter that there are fewer of, against those of the samples, read and written.  (Gradients, us as the samples come and in order: 1,024
+// samples of 64 adapters of 8 ranks at random, 1,000 x 20,000: 143 and 132; 2,000 of 100 adapters of 32 ranks, 5,000 x 5,000: 330 and 206;
+// 4,096 of 8 adapters of 128, 4,000 x 20,000: 855
 // and 695.  Finding out that it does not pay, a forward pass of 8,192 samples one request after another, 10,000 x 5,000: 670 and 679.)
 // ---------------------------------------------------------------------------------------------------------
 struct IndexParams {
@@ -1410,6 +1411,7 @@ struct IndexParams {
   int32_t *order, *begin, *count, *position;
   int32_t* sorted_ids;
   int32_t tiles;               // 0: the samples stay as they are
+  int64_t width, d;            // entries of a factor that a tile reads, of a sample
   uint32_t *tally, *sorted;    // [3]: pairs, adapters with samples, blocks done
   uint32_t* status;
 };
@@ -1486,7 +1488,7 @@ __global__ void __launch_bounds__(32 * kIndexWarps) adapter_index_kernel(const _
     if (atomicAdd(p.tally + 2, 1u) == gridDim.x - 1) {
       __threadfence();
       const int64_t fewer = static_cast<int64_t>(__ldcg(p.tally)) - p.tiles - __ldcg(p.tally + 1);
-      *p.sorted = fewer * p.rank16 > 2ll * p.n;
+      *p.sorted = fewer * p.rank16 * p.width > 2ll * p.n * p.d;
       p.tally[0] = p.tally[1] = p.tally[2] = 0;      // for the next launch
     }
   }
@@ -1812,12 +1814,20 @@ int grad_shares(const sfb_adapter_config& c, int64_t n) {
   return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({8, grad_blocks(c.rank) * kModelSms / items, n / c.adapters / (4 * BK)})));
 }
 
+// Whether adapter_dot_kernel is the one that forms the products of n samples with factors of d entries: up to these products, and samples x units
+// of ranks.
+constexpr int64_t kDotMost = 48 << 20, kDotUnits = 2048;
+bool use_dot(const sfb_adapter_config& c, int64_t n, int64_t d) {
+  return n * c.rank * d <= kDotMost && n * ((c.rank + kUnit - 1) / kUnit) <= kDotUnits;
+}
+// Entries of a factor that a tile reads once for each adapter among its samples, in a product from d entries to m.
+int64_t sort_width(const sfb_adapter_config& c, int64_t n, int64_t m, int64_t d) { return m + (use_dot(c, n, d) ? 0 : d); }
 // Whether n samples, each with an adapter at random, had better be taken in the order of their adapters (see adapter_index_kernel), and would
 // read 32 MB less of factors, 5 us, which is what finding out takes.
-bool sort_may_pay(const sfb_adapter_config& c, int64_t n) {
+bool sort_may_pay(const sfb_adapter_config& c, int64_t n, int64_t m, int64_t d) {
   const int64_t tiles = (n + kRankTile - 1) / kRankTile, rank16 = (c.rank + kSlice - 1) / kSlice * kSlice;
-  const int64_t fewer = tiles * std::min<int64_t>(c.adapters, kRankTile) - tiles - c.adapters;
-  return n > kFewMost && fewer * rank16 > 2 * n && fewer * rank16 * (c.rows + c.cols) > 16 << 20;
+  const int64_t fewer = tiles * std::min<int64_t>(c.adapters, kRankTile) - tiles - c.adapters, less = fewer * rank16 * sort_width(c, n, m, d);
+  return n > kFewMost && less > 2 * n * d && less > 16 << 20;
 }
 
 bool pitch_odd(int64_t pitch) { return pitch % 16 != 0; }      // of bf16 entries: not a multiple of 32 bytes
@@ -1863,7 +1873,7 @@ AdapterLayout layout_of(const sfb_adapter_config& c) {
   const bool odd_w = pitch_odd(c.ldw ? c.ldw : c.cols) && c.max_samples >= kCopyUses;
   const bool odd_x = pitch_odd(round_up(c.cols, 8)) && c.rows >= kCopyUses, odd_y = pitch_odd(round_up(c.rows, 8)) && c.cols >= kCopyUses;
   L.wcopy = take(odd_w ? static_cast<size_t>(c.rows) * round_up(c.cols, BK) * 2 : 0);
-  const bool sorts = sort_may_pay(c, c.max_samples);
+  const bool sorts = sort_may_pay(c, c.max_samples, c.rows, c.cols) || sort_may_pay(c, c.max_samples, c.cols, c.rows);
   L.zcopy = take(n <= kFewMost ? 0 : std::max(odd_x || sorts ? n * round_up(c.cols, BK) * 2 : 0, odd_y || sorts ? n * round_up(c.rows, BK) * 2 : 0));
   L.order = take(n * 4);
   L.sorted_ids = take(sorts ? n * 4 : 0);
@@ -1950,8 +1960,6 @@ cudaError_t allow_beside(int bytes) {
 }
 
 // The samples' operand: as it is, or a copy whose rows lie better; and in the order of their adapters, where sort.on() says so.
-constexpr int64_t kDotMost = 48 << 20;               // n x ranks x entries up to which adapter_dot_kernel is the faster one
-constexpr int64_t kDotUnits = 2048;                  // ... and samples x units of ranks
 struct Samples {
   const void* given;
   int64_t given_pitch;
@@ -1981,7 +1989,7 @@ cudaError_t rank_products(sfb_adapters* h, int64_t n, const Samples& z, const in
   const sfb_adapter_config& c = h->cfg;
   const int64_t d = MN ? c.rows : c.cols;
   const int tn = rank_tile(n), parts = rank_parts(n, d), tiles = static_cast<int>((n + tn - 1) / tn);
-  *all = n * c.rank * d <= kDotMost && n * ((c.rank + kUnit - 1) / kUnit) <= kDotUnits;
+  *all = use_dot(c, n, d);
   if (*all) {
     *got = Ranked{sum, 1, 0};
     DotParams p{};
@@ -2151,8 +2159,8 @@ cudaError_t product(sfb_adapters* h, int64_t n, const Samples& z, const int32_t*
   return pairs<MN>(h, n, z, term_of<MN>(h, ids, to), Y, ldy);
 }
 
-// The samples by adapters.  sort (may be null): also finds out whether the products had better take them so.
-cudaError_t index_samples(sfb_adapters* h, int64_t n, const int32_t* ids, Sorting* sort) {
+// The samples by adapters.  sort (may be null): also finds out whether the products, from d entries to m, had better take them so.
+cudaError_t index_samples(sfb_adapters* h, int64_t n, const int32_t* ids, int64_t m, int64_t d, Sorting* sort) {
   const AdapterLayout& l = h->lay;
   const sfb_adapter_config& c = h->cfg;
   IndexParams p{};
@@ -2161,13 +2169,14 @@ cudaError_t index_samples(sfb_adapters* h, int64_t n, const int32_t* ids, Sortin
   p.tally = h->at<uint32_t>(l.tally); p.sorted = h->at<uint32_t>(l.sorted); p.status = h->at<uint32_t>(l.status);
   if (sort) {
     p.tiles = static_cast<int32_t>((n + kRankTile - 1) / kRankTile);
+    p.width = sort_width(c, n, m, d); p.d = d;
     *sort = Sorting{p.sorted, p.order, p.sorted_ids};
   }
   return launch_kernel(adapter_index_kernel, dim3(c.adapters + 1 + p.tiles), dim3(n <= 2048 ? 256 : 32 * kIndexWarps), 0, h->stream, 1, p);
 }
 // ... whether there is room for that too.
-bool sorts(const sfb_adapters* h, int64_t n, int64_t d) {
-  return sort_may_pay(h->cfg, n) && h->lay.begin > h->lay.sorted_ids && fits(n, d, h->lay.order - h->lay.zcopy);
+bool sorts(const sfb_adapters* h, int64_t n, int64_t m, int64_t d) {
+  return sort_may_pay(h->cfg, n, m, d) && h->lay.begin > h->lay.sorted_ids && fits(n, d, h->lay.order - h->lay.zcopy);
 }
 
 int fail(sfb_adapters* h, cudaError_t e) {
@@ -2257,7 +2266,7 @@ extern "C" int sfb_adapter_forward(sfb_adapters* h, int64_t n, const void* X_dev
   float* sum = S_dev ? S_dev : h->at<float>(h->lay.ssum);
   Sorting sort{};
   Samples z;
-  if (sorts(h, n, c.cols)) ACK(index_samples(h, n, ids_dev, &sort));
+  if (sorts(h, n, c.rows, c.cols)) ACK(index_samples(h, n, ids_dev, c.rows, c.cols, &sort));
   ACK(placed(h, n, X_dev, ldx, c.cols, c.rows, sort, &z));
   bool all;
   ACK(rank_products<false>(h, n, z, ids_dev, h->at<float>(h->lay.s), sum, WordsParams{}, &s, &all));
@@ -2286,8 +2295,8 @@ extern "C" int sfb_adapter_backward(sfb_adapters* h, int64_t n, const void* dY_d
   uint32_t* status = h->at<uint32_t>(h->lay.status);
   int32_t *order = h->at<int32_t>(h->lay.order), *begin = h->at<int32_t>(h->lay.begin), *count = h->at<int32_t>(h->lay.count);
   Sorting sort{};
-  const bool sorting = dX_dev && sorts(h, n, c.rows);
-  if (dU_dev || dV_dev || sorting) ACK(index_samples(h, n, ids_dev, sorting ? &sort : nullptr));
+  const bool sorting = dX_dev && sorts(h, n, c.cols, c.rows);
+  if (dU_dev || dV_dev || sorting) ACK(index_samples(h, n, ids_dev, c.cols, c.rows, sorting ? &sort : nullptr));
   Ranked s{S_dev, 1, 0}, t{};
   bool all = false;
   Samples z{X_dev, ldx, X_dev, ldx, X_dev, ldx, Sorting{}};
