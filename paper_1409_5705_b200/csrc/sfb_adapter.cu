@@ -783,7 +783,8 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kPairStages; ++i) {
-      mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&landed[i], 1); mbar_init(&built[i], 2 * kPairBuild); mbar_init(&joined[i], 1);
+      mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&landed[i], 1); mbar_init(&joined[i], 1);
+      mbar_init(&built[i], 2 * kPairBuild + (rank ? kHand : 0));       // (see the hand-over)
     }
     for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 2 * kEpi); mbar_init(&looked[i], kPairBuild); mbar_init(&taken[i], kEpi); }
     abort_word = 0;
@@ -961,8 +962,12 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     // (A release to the cluster by each of the eight warps that make them took 1 us a k-block, and one warp, with no accesses of its own,
     // that hands all of them on is not much faster: these take them in turn.  1,024 samples, 1,000 x 20,000, eight k-blocks of the term a tile:
     // 98, 89 and 76 us.)
+    // Both see every k-block, and its stage is built again only once both have: each arrives for the next phase of `built` when it has seen
+    // one (for the first at once).  Without that the warp whose turn it is not could still be looking for a phase when the next one
+    // is complete, whose parity is that of the phase before, and wait for good.
     uint32_t s = 0, bph = 0, turn = warp - 2 - kEpi - 2 * kPairBuild;
     bool ok = true;
+    if (rank == 1 && lane < kPairStages) mbar_arrive(&built[lane]);
     for (int i = 0; i < segs.n && ok && rank == 1; ++i) {
       const Segment sg = segs.get(i);
       int m0, tt;
@@ -976,6 +981,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
           turn = kHand;
         }
         --turn;
+        if (ok && lane == 0) mbar_arrive(&built[s]);
         if (++s == static_cast<uint32_t>(kPairStages)) s = 0;
       }
     }
