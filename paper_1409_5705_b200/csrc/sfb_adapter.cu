@@ -1797,7 +1797,7 @@ __global__ void __launch_bounds__(256) adapter_join_kernel(float* out, const flo
 // Samples of a tile of adapter_rank_kernel; parts of its contraction: as many as give every SM two blocks, of four k-blocks at least.
 int rank_tile(int64_t n) { return std::min(tile_of(n), kRankTile); }
 int rank_parts(int64_t n, int64_t d) {
-  const int64_t tiles = (n + rank_tile(n) - 1) / rank_tile(n), kseg = (d + BK - 1) / BK;
+  const int64_t tiles = std::max<int64_t>(1, (n + rank_tile(n) - 1) / rank_tile(n)), kseg = (d + BK - 1) / BK;     // (a handle's n may be 0)
   return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({kMaxParts, 2 * kModelSms / tiles, kseg / 4})));
 }
 // Most samples x parts of a call of up to n samples.

@@ -23,3 +23,16 @@ def test_the_term_in_the_same_stage_of_tile_after_tile(cols):
         c.plan.sfb_adapter_forward(c.X, c.ids, Y, Sx)
     assert c.plan.sfb_adapter_get_status() == 0
     assert torch.equal(Y, first)
+
+
+def test_a_handle_for_no_samples():
+    """max_samples = 0: calls of no samples, whose gradients are zeros; one sample is refused."""
+    c = Case(3, 40, 48, 2, 4, "one")
+    plan = S.Adapters(c.W, c.U, c.V, c.scale, max_samples=0)
+    ids = torch.empty(0, dtype=torch.int32, device="cuda")
+    dU, dV = torch.ones(2, 4, 40, device="cuda"), torch.ones(2, 4, 48, device="cuda")
+    plan.sfb_adapter_forward(c.X[:0], ids, c.dY[:0])
+    plan.sfb_adapter_backward(c.dY[:0], c.X[:0], ids, None, c.X[:0], dU, dV)
+    assert plan.sfb_adapter_get_status() == 0 and (dU == 0).all() and (dV == 0).all()
+    with pytest.raises(S.SfbError):
+        plan.sfb_adapter_forward(c.X[:1], c.ids[:1], c.dY[:1])
