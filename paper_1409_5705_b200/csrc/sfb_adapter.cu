@@ -122,7 +122,23 @@ struct Sorting {
   __device__ __forceinline__ bool on() const { return sorted && *sorted; }
 };
 
-constexpr int kUnit = 8, kUnits = BK / kUnit;       // ranks of a unit of the adapters' term (see Term), units of a k-block
+constexpr int kUnit = 8, kUnits = BK / (2 * kUnit); // ranks of a unit of the adapters' term (see Term), units of a k-block of it
+
+// v = w0 + w1, 2^-16 of v apart: two words of bf16.  (What overflows in the rounding to the first word is cut off instead; of what is not
+// finite there is no rest.)
+__device__ __forceinline__ void two_words(float v, float (&w)[2]) {
+  w[0] = __bfloat162float(__float2bfloat16_rn(v));
+  if (isinf(w[0]) && !isinf(v)) w[0] = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+  w[1] = isfinite(v) ? v - w[0] : 0.f;
+}
+// Rank r of row i of pb (see Term).
+__device__ __forceinline__ void put_pair(__nv_bfloat16* pb, int64_t i, int per, int r, float v) {
+  float w[2];
+  two_words(v, w);
+  __nv_bfloat16* to = pb + (i * per + r / kUnit) * (2 * kUnit) + r % kUnit;
+  to[0] = __float2bfloat16_rn(w[0]);
+  to[kUnit] = __float2bfloat16_rn(w[1]);
+}
 
 // ---------------------------------------------------------------------------------------------------------
 // p_i = F[a_i] z_i:  the adapters' factors as the rows of the accumulator, 16 ranks (a slice) of one adapter after another, up to 128
@@ -146,7 +162,7 @@ struct RankParams {
   // FEW
   const float* scale;
   float* p;                    // [n][rank]
-  __nv_bfloat16* pb;           // [n][rank rounded up to 8]
+  __nv_bfloat16* pb;           // see Term
   int32_t *lists, *place;
   uint32_t* arrived;           // [kFewChunks]
 };
@@ -195,14 +211,14 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
   if (FEW) {
     if (blockIdx.x == 0) {
       if (threadIdx.x == 0) p.lists[0] = L.count;
-      const int per8 = (p.rank + kUnit - 1) / kUnit * kUnit;
+      const int per_pb = (p.rank + kUnit - 1) / kUnit, per8 = per_pb * kUnit;
       for (int t = threadIdx.x; t < p.tn; t += kRankThreads) {
         if (t < L.count) p.lists[1 + t] = L.list[t];
         if (t < p.n) p.place[t] = L.place[t];
       }
       for (int x = threadIdx.x; x < p.n * per8; x += kRankThreads) {       // samples without an adapter, and what lies behind the ranks
         const int t = x / per8, r = x - t * per8;
-        if (r >= p.rank || L.place[t] < 0) p.pb[x] = __float2bfloat16_rn(0.f);
+        if (r >= p.rank || L.place[t] < 0) put_pair(p.pb, t, per_pb, r, 0.f);
         if (r < p.rank && L.place[t] < 0) p.p[t * p.rank + r] = 0.f;
       }
     }
@@ -318,13 +334,13 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
       }
       __syncthreads();
       if (last) {
-        const int per8 = (p.rank + kUnit - 1) / kUnit * kUnit;
+        const int per_pb = (p.rank + kUnit - 1) / kUnit;
         for (int x = threadIdx.x; x < p.n * p.rank; x += kRankThreads) {
           const int t = x / p.rank, r = x - t * p.rank, at = L.place[t];
           if (at < 0 || (at * per + r / kSlice) / 8 != c) continue;
           const float v = ranked(Ranked{p.out, parts, static_cast<int64_t>(p.n) * p.rank}, x);
           p.p[x] = v;
-          p.pb[t * per8 + r] = __float2bfloat16_rn(p.scale[L.list[at]] * v);
+          put_pair(p.pb, t, per_pb, r, p.scale[L.list[at]] * v);
         }
       }
       __syncthreads();
@@ -375,8 +391,9 @@ __device__ __forceinline__ void store_chunk(__nv_bfloat16* Y, int64_t ldy, int i
 
 // ---------------------------------------------------------------------------------------------------------
 // The adapters' term, scale F[a_i]^T p_i, of the three products below is more contraction behind the k-blocks of A: the factors of the
-// adapters in the tile's list, eight units of 8 ranks a k-block, against  scale p  of the samples in bf16 (one rounding, 2^-8 of the term;
-// the result is rounded by as much), with zeros where a sample has another adapter.  Zeros do not hide what is not finite: some warps look
+// adapters in the tile's list, four units of 8 ranks a k-block, against  scale p  of the samples as two words of bf16 (2^-16 of the term;
+// with one word, and eight units a k-block, the term's rounding was as large as that of the result), with zeros where a sample has another
+// adapter.  Zeros do not hide what is not finite: some warps look
 // through the factors in shared memory and replace what is not finite by zeros, and the end of the tile adds those entries alone to their
 // own samples, in fp32.
 // (In fp32 FMAs from global memory, as it was for up to 64 samples, a tile's term is a chain of loads: 64 samples of 8 ranks took 99 us a
@@ -390,7 +407,7 @@ struct Term {
   const __nv_bfloat16* F;      // [adapters][rank][ldf]
   int64_t ldf;
   const float* p;              // [n][rank]
-  const uint4* pb;             // [n][units of an adapter]: scale p in bf16, zeros behind
+  const uint4* pb;             // [n][units of an adapter][2]: scale p, first and second words of its eight ranks, zeros behind
 };
 __device__ __forceinline__ int units_of(const Term& t) { return (t.rank + kUnit - 1) / kUnit; }
 // What the tensor cores have left out of the term of sample i at row m: the factors that are not finite.
@@ -481,14 +498,14 @@ __device__ __forceinline__ uint32_t clean_units(uint8_t* st, int t, int nu) {
   }
   return bad;
 }
-// Row t of the samples' operand of a k-block of `nu` units (row: this thread has one), and, beside an odd last unit, zeros in the factors'
+// Row t of the samples' operand of a k-block of `nu` units, first words and then second ones (row: this thread has one), and, beside an odd last unit, zeros in the factors'
 // operand.  By THREADS threads, t of them.
 template <int THREADS>
-__device__ __forceinline__ void write_units(const uint4 (&words)[kUnits], uint8_t* st, int t, bool row, int nu) {
+__device__ __forceinline__ void write_units(const uint4 (&words)[2 * kUnits], uint8_t* st, int t, bool row, int nu) {
   if (row) {
     const uint32_t to = smem_u32(st) + kTileBytesA + t * 128;
 #pragma unroll
-    for (int j = 0; j < kUnits; ++j)
+    for (int j = 0; j < 2 * kUnits; ++j)
       asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((j ^ (t & 7)) << 4)), "r"(words[j].x), "r"(words[j].y),
                    "r"(words[j].z), "r"(words[j].w) : "memory");
   }
@@ -497,11 +514,13 @@ __device__ __forceinline__ void write_units(const uint4 (&words)[kUnits], uint8_
       *reinterpret_cast<uint4*>(st + (x >> 6) * (kTileBytesA / 2) + nu * (kUnit * 128) + (x & 63) * 16) = make_uint4(0, 0, 0, 0);
 }
 // The words of the units [g0, g0 + nu) of a sample whose first unit is `at` (below zero: no adapter): zeros for those that are not its own.
-__device__ __forceinline__ void read_units(const uint4* src, int at, int g0, int nu, int per, uint4 (&words)[kUnits]) {
+__device__ __forceinline__ void read_units(const uint4* src, int at, int g0, int nu, int per, uint4 (&words)[2 * kUnits]) {
 #pragma unroll
   for (int j = 0; j < kUnits; ++j) {
     const int u = g0 + j - at;
-    words[j] = at >= 0 && j < nu && u >= 0 && u < per ? src[u] : make_uint4(0, 0, 0, 0);
+    const bool own = at >= 0 && j < nu && u >= 0 && u < per;
+    words[j] = own ? src[2 * u] : make_uint4(0, 0, 0, 0);
+    words[kUnits + j] = own ? src[2 * u + 1] : make_uint4(0, 0, 0, 0);
   }
 }
 
@@ -548,7 +567,10 @@ __device__ __forceinline__ void few_mma(uint32_t st, uint32_t d_tmem, uint32_t i
 }
 __device__ __forceinline__ void few_mma_units(uint32_t st, uint32_t d_tmem, uint32_t idesc, int nu) {
   const uint64_t da = umma_desc_mn128(st), db = umma_desc_k128(st + kTileBytesA);
-  for (int j = 0; j < (nu + 1) / 2; ++j) umma_bf16(d_tmem, da + 128 * j, db + 2 * j, idesc, 1u);
+  for (int j = 0; j < (nu + 1) / 2; ++j) {           // two units each: their first words, their second ones
+    umma_bf16(d_tmem, da + 128 * j, db + 2 * j, idesc, 1u);
+    umma_bf16(d_tmem, da + 128 * j, db + kUnits + 2 * j, idesc, 1u);
+  }
 }
 
 template <int TN, bool MN>
@@ -645,9 +667,9 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     const bool writes = warp < 6 + kWrite;
     const int t = (writes ? warp - 6 : warp - 6 - kWrite) * 32 + lane;     // this thread's sample, or share of the factors
     const int units = p.term.lists[0] * per, at = writes && t < p.n ? p.term.place[t] * per : -1;
-    const uint4* src = p.term.pb + t * per;
+    const uint4* src = p.term.pb + t * per * 2;
     uint32_t s = static_cast<uint32_t>(nk) % p.stages, ph = 0, bad = 0;    // ph: the phases of free_, or of landed, a bit per stage
-    uint4 words[kUnits];
+    uint4 words[2 * kUnits];
     if (writes) read_units(src, at, mine * kUnits, min(kUnits, units - mine * kUnits), per, words);
     for (int g0 = mine * kUnits; g0 < units; g0 += p.parts * kUnits) {
       const int nu = min(kUnits, units - g0);
@@ -723,7 +745,8 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kPairBuild = 4, kHand = 2, kPairThreads = 32 * (2 + kEpi + 2 * kPairBuild + kHand), kGroup = 8;      // kGroup: tiles of samples that follow one another
 constexpr int kPairStages = 6, kPairStage = 2 * kTileBytesA;
-constexpr int kPairSmem = kPairStages * kPairStage + 128 * SFB_ADAPTER_MAX_RANK * 2 + 1024;      // (behind the stages: a row of pb per writing thread)
+constexpr int kPairHeld = 2 * kUnits;               // units of its row of pb that a writing thread has at hand, behind the stages
+constexpr int kPairSmem = kPairStages * kPairStage + 128 * kPairHeld * 32 + 1024;
 constexpr int kPartFloats = BM * kMaxTile;          // what a CTA leaves of a tile
 struct PairParams {
   Term term;
@@ -874,11 +897,14 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
           if (!mbar_wait_warp(&built[s], (bph >> s) & 1, abort_flag) || !mbar_wait_cluster(&joined[s], (bph >> s) & 1, abort_flag)) { ok = false; break; }
           bph ^= 1u << s;
           tc_fence_after();
-          const int ns = (min(kUnits, left) + 1) / 2;                  // instructions: two units each
+          const int ns = (min(kUnits, left) + 1) / 2;                  // two units each: of their first words, of their second ones
           if (elect_one()) {
             const uint32_t st = smem_u32(smem + s * kPairStage);
             const uint64_t da = umma_desc_mn128(st), db = umma_desc_k128(st + kTileBytesA);
-            for (int j = 0; j < ns; ++j) umma_bf16_pair(d_tmem, da + 128 * j, db + 2 * j, idesc_f, 1u);
+            for (int j = 0; j < ns; ++j) {
+              umma_bf16_pair(d_tmem, da + 128 * j, db + 2 * j, idesc_f, 1u);
+              umma_bf16_pair(d_tmem, da + 128 * j, db + kUnits + 2 * j, idesc_f, 1u);
+            }
             umma_commit_pair(&empty[s], 3);
           }
           if (++s == static_cast<uint32_t>(kPairStages)) s = 0;
@@ -990,7 +1016,8 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     const bool writes = warp < 2 + kEpi + kPairBuild;
     const int w = warp - 2 - kEpi - (writes ? 0 : kPairBuild), t = w * 32 + lane;    // this thread's sample of the CTA's half of the tile, or
     uint32_t s = 0, ph = 0;                          // share of the factors; ph: the phases of free_, or of landed, a bit per stage
-    const uint32_t mine = smem_u32(smem + kPairStages * kPairStage) + t * (SFB_ADAPTER_MAX_RANK * 2);
+    const uint32_t mine = smem_u32(smem + kPairStages * kPairStage) + t * (kPairHeld * 32);
+    auto held_at = [&](int u, int w) { return mine + (((u % kPairHeld) * 2 + w) ^ (t & 15)) * 16; };
     bool ok = true;
     for (int i = 0; i < segs.n && ok; ++i) {
       const Segment sg = segs.get(i);
@@ -1000,14 +1027,20 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       const int units = sg.k1 == p.kseg ? p.term.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0;
       const int smp = tt * p.tn + static_cast<int>(rank) * half + t;
       const int at = writes && t < half && smp < p.n ? p.term.place[smp] * per : -1;   // this sample's first unit
-      const uint4* src = p.term.pb + static_cast<int64_t>(smp) * per;
+      const uint4* src = p.term.pb + static_cast<int64_t>(smp) * per * 2;
       const uint32_t a = i & 1, aph = (i >> 1) & 1;
       const int32_t* list = p.term.lists + static_cast<int64_t>(tt) * kListPitch;
       Held held = hold_units(list, lane, writes ? units : 0, per);
-      // a thread's own row of pb comes to shared memory while the k-blocks of A are under way
+      // a thread's own units come to shared memory two k-blocks ahead, those of the first two while the k-blocks of A are under way
+      auto fetch = [&](int g0) {
+        for (int g = max(g0, at); at >= 0 && g < min(g0 + kUnits, at + per); ++g) {
+          cp_async_16(held_at(g, 0), src + 2 * (g - at), 16);
+          cp_async_16(held_at(g, 1), src + 2 * (g - at) + 1, 16);
+        }
+        cp_async_commit();
+      };
       if (writes) {
-        if (units > 0 && at >= 0)
-          for (int u = 0; u < per; ++u) cp_async_16(mine + u * 16, src + u, 16);
+        if (units > 0) { fetch(0); fetch(kUnits); }
       } else if (!mbar_wait_warp(&taken[a], aph ^ 1, abort_flag)) break;
       uint32_t bad = 0;
       for (int g0 = 0; g0 < units; g0 += kUnits) {
@@ -1018,14 +1051,17 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         uint32_t wrote = 1;
         if (writes) {
           load_units<kPairBuild>(st, &landed[s], tmF, held, g0, nu, p.term.boxed, m0, w);
-          if (g0 == 0) cp_async_wait_all();
-          uint4 words[kUnits];
+          cp_async_wait_group<1>();
+          uint4 words[2 * kUnits];
 #pragma unroll
           for (int j = 0; j < kUnits; ++j) {
             const int u = g0 + j - at;
-            words[j] = at >= 0 && j < nu && u >= 0 && u < per ? lds_v4(mine + u * 16) : make_uint4(0, 0, 0, 0);
+            const bool own = at >= 0 && j < nu && u >= 0 && u < per;
+            words[j] = own ? lds_v4(held_at(g0 + j, 0)) : make_uint4(0, 0, 0, 0);
+            words[kUnits + j] = own ? lds_v4(held_at(g0 + j, 1)) : make_uint4(0, 0, 0, 0);
           }
           write_units<32 * kPairBuild>(words, st, t, t < half, nu);
+          fetch(g0 + 2 * kUnits);
           if (((g0 + kUnits) & 31) == 0) held = hold_units(list, g0 + kUnits + lane, units, per);
         } else bad |= wrote = clean_units<32 * kPairBuild>(st, t, nu);
         if (wrote) fence_proxy_async_smem();
@@ -1039,6 +1075,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         mbar_arrive(&looked[a]);
       }
     }
+    cp_async_wait_group<0>();
   }
 
   // ---------------- teardown ----------------
@@ -1161,7 +1198,7 @@ __global__ void __launch_bounds__(256) adapter_words_kernel(const __grid_constan
 }
 
 // ---------------------------------------------------------------------------------------------------------
-// More than 64 samples: p from its parts, zeros for a sample without an adapter, and scale p in bf16 (pb).  In the first blocks the lists of
+// More than 64 samples: p from its parts, zeros for a sample without an adapter, and scale p as two words (pb).  In the first blocks the lists of
 // the tiles of the product.
 // ---------------------------------------------------------------------------------------------------------
 struct SumParams {
@@ -1252,13 +1289,20 @@ __global__ void __launch_bounds__(256) adapter_sum_kernel(const __grid_constant_
       for (int j = 0; j < kUnit; ++j)
         if (r0 + j < p.rank) p.out[into + j] = v[j];
     }
-    uint32_t w[kUnit / 2];
+    uint32_t w[2][kUnit / 2];
 #pragma unroll
     for (int j = 0; j < kUnit / 2; ++j) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(has ? sc * v[2 * j] : 0.f, has ? sc * v[2 * j + 1] : 0.f);
-      w[j] = *reinterpret_cast<const uint32_t*>(&b);
+      float a[2], b[2];
+      two_words(has ? sc * v[2 * j] : 0.f, a);
+      two_words(has ? sc * v[2 * j + 1] : 0.f, b);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const __nv_bfloat162 ab = __floats2bfloat162_rn(a[k], b[k]);
+        w[k][j] = *reinterpret_cast<const uint32_t*>(&ab);
+      }
     }
-    reinterpret_cast<uint4*>(p.pb)[x] = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) reinterpret_cast<uint4*>(p.pb)[2 * x + k] = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
     if (!wanted || !has) continue;
     const int64_t row = (static_cast<int64_t>(p.words.position[sample]) * 3) * rp + r0;
     const bool behind = r0 + 2 * kUnit == rp && r0 + kUnit >= p.rank;        // a piece of zeros follows
@@ -1351,7 +1395,7 @@ __global__ void __launch_bounds__(256) adapter_dot_kernel(const __grid_constant_
   const int64_t at = static_cast<int64_t>(sample) * rank + r;
   const float sc = has ? q.scale[id] : 0.f;
   if (r < rank) q.out[at] = v;
-  if (r < per8) q.pb[static_cast<int64_t>(i) * per8 + r] = __float2bfloat16_rn(has && r < rank ? sc * v : 0.f);
+  if (r < per8) put_pair(q.pb, i, per8 / kUnit, r, has && r < rank ? sc * v : 0.f);
   if (!wanted || !has) return;
   const int64_t row = static_cast<int64_t>(q.words.position[sample]) * 3 * rp + r;
 #pragma unroll
@@ -1869,7 +1913,7 @@ AdapterLayout layout_of(const sfb_adapter_config& c) {
   L.t = take(static_cast<size_t>(rank_rows(c.max_samples, c.rows)) * c.rank * 4);
   L.ssum = take(n * c.rank * 4);
   L.tsum = take(n * c.rank * 4);
-  L.pb = take(n * ((static_cast<size_t>(c.rank) + kUnit - 1) / kUnit) * kUnit * 2);
+  L.pb = take(n * ((static_cast<size_t>(c.rank) + kUnit - 1) / kUnit) * kUnit * 4);
   L.swords = take(n * 3 * rp * 2);
   L.twords = take(n * 3 * rp * 2);
   L.lists = take((n / kMaxTile + 1) * kListPitch * 4);

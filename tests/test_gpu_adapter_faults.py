@@ -36,3 +36,37 @@ def test_a_handle_for_no_samples():
     assert plan.sfb_adapter_get_status() == 0 and (dU == 0).all() and (dV == 0).all()
     with pytest.raises(S.SfbError):
         plan.sfb_adapter_forward(c.X[:1], c.ids[:1], c.dY[:1])
+
+
+def two_word_bounds(c):
+    """Y and dX with the adapters' term from scale * s in two words, 2^-16 of it, and one rounding to bf16 of the result."""
+    U24, U23, U8 = 2.0 ** -24, 2.0 ** -23, 2.0 ** -8
+    ids, has, at, sc = c.wide()
+    W, U, V, X, dY = (t.double() for t in (c.W, c.U, c.V, c.X, c.dY))
+    got = {}
+    for name, Z, A, F, G in (("Y", X, W, V, U), ("dX", dY, W.t(), U, V)):
+        d = Z.shape[1]
+        y, M = Z @ A.t(), Z.abs() @ A.abs().t()
+        word = torch.zeros_like(y)
+        for a in range(c.adapters):
+            i = torch.nonzero(ids == a).flatten()
+            p, m = sc[i] * (Z[i] @ F[a].t()), sc[i].abs() * (Z[i].abs() @ F[a].abs().t())
+            y[i] += p @ G[a]
+            # the words of scale * s and its product's rounding; what s itself is off (see test_gpu_adapters)
+            word[i] = (p.abs() * (2.0 ** -16 + U24) + (d / 16 + 16) * U23 * m) @ G[a].abs()
+            M[i] += p.abs() @ G[a].abs()
+        got[name] = y, U8 * y.abs() + word + (d / 16 + 16 + 2 * 2 * c.rank) * U23 * M
+    return got
+
+
+@pytest.mark.parametrize("size", [(1, 300, 200, 2, 16, "one"), (16, 130, 264, 5, 20, "every"), (30, 700, 120, 30, 33, "mixed"), (64, 1000, 300, 9, 128, "mixed"),
+                                  (64, 200, 6400, 9, 128, "mixed"), (100, 515, 777, 100, 8, "every"), (300, 320, 200, 3, 64, "runs"), (513, 260, 300, 5, 128, "mixed"),
+                                  (1500, 700, 6000, 100, 16, "every"), (700, 136, 3000, 40, 7, "mixed")], ids=lambda s: "-".join(map(str, s)))
+def test_the_term_is_not_held_in_one_word(size):
+    """The adapters' term is most of the result, and its parts cancel: one rounding of scale * s to bf16 would be far outside."""
+    c = Case(*size, seed=sum(size[:5]))
+    c.W.mul_(0.01)
+    got = c.run()
+    for k, (v, b) in two_word_bounds(c).items():
+        off = (got[k].double() - v).abs()
+        assert (off <= b).all(), f"{k}: {(off / b.clamp(min=1e-300)).max().item():.3g} of the bound"
