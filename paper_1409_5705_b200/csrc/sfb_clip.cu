@@ -5,8 +5,7 @@
 //   clip_sum_kernel    blocks take pieces in turn; a thread's squares go into fp64 sums, a block's sum to its place
 //   clip_scale_kernel  every block adds the blocks' sums in the same order, and takes its pieces from the list's end backwards: what
 //                      the first pass read last is still in L2
-// Squares: eight in fp32 (their sum is off by at most 8 * 2^-24 of itself, all terms being positive), then fp64; a group whose sum
-// leaves [1e-30, 1e37], where fp32 squares lose bits or overflow, is squared in fp64.
+// Squares and sums in fp64, so the norm and the factor are those of 64 bits but for their last rounding.
 // Bound by HBM: one read for the norm, one read and one write for the copies, less what L2 holds of the second read.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -77,30 +76,17 @@ __device__ __forceinline__ uint4 narrow(const float (&v)[8], const __half*) {
                     two(__floats2half2_rn(v[6], v[7])));
 }
 
+// The squares of entries of up to 32 bits are exact in fp64.  Two sums, so that a thread does not wait for each addition.
 template <int N>
-__device__ __forceinline__ bool all_zero(const float (&v)[N]) {
-  bool z = true;
+__device__ __forceinline__ void add_squares(const float (&v)[N], double (&sum)[2]) {
 #pragma unroll
-  for (int j = 0; j < N; ++j) z &= v[j] == 0.f;
-  return z;
-}
-template <int N>
-__device__ __forceinline__ void add_squares(const float (&v)[N], double& sum) {
-  float q = 0.f;
-#pragma unroll
-  for (int j = 0; j < N; ++j) q = fmaf(v[j], v[j], q);
-  if ((q >= 1e-30f && q <= 1e37f) || (q == 0.f && all_zero(v))) {
-    sum += static_cast<double>(q);
-  } else {
-#pragma unroll
-    for (int j = 0; j < N; ++j) sum += static_cast<double>(v[j]) * static_cast<double>(v[j]);
-  }
+  for (int j = 0; j < N; ++j) sum[j & 1] = fma(static_cast<double>(v[j]), static_cast<double>(v[j]), sum[j & 1]);
 }
 
 // Entries [0, n) of a piece: up to the first 16-byte boundary and behind the last one singly, the rest 16 bytes at a time, four of
 // them under way.
 template <typename T>
-__device__ __forceinline__ double sum_piece(const T* p, int n, double sum) {
+__device__ __forceinline__ void sum_piece(const T* p, int n, double (&sum)[2]) {
   constexpr int kV = 16 / sizeof(T);
   const int lead = min(n, static_cast<int>(((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / sizeof(T)));
   const int vecs = (n - lead) / kV;
@@ -118,7 +104,6 @@ __device__ __forceinline__ double sum_piece(const T* p, int n, double sum) {
       add_squares(v, sum);
     }
   }
-  return sum;
 }
 
 // dst = coef * src, or src bit for bit where coef is 1; the two may be the same addresses.  Where they lie differently to a 16-byte boundary,
@@ -175,16 +160,16 @@ __device__ __forceinline__ double block_sum(double v) {
 __global__ void __launch_bounds__(kThreads, kSumBlocks) clip_sum_kernel(const Piece* pieces, int64_t n, double* part) {
   pdl_launch_dependents();
   pdl_wait();
-  double sum = 0.0;
+  double sums[2] = {};
   Piece next = blockIdx.x < n ? pieces[blockIdx.x] : Piece{};
   for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
     const Piece c = next;
     if (i + gridDim.x < n) next = pieces[i + gridDim.x];
-    if (c.dtype == SFB_F32) sum = sum_piece(reinterpret_cast<const float*>(c.src), c.count, sum);
-    else if (c.dtype == SFB_BF16) sum = sum_piece(reinterpret_cast<const __nv_bfloat16*>(c.src), c.count, sum);
-    else sum = sum_piece(reinterpret_cast<const __half*>(c.src), c.count, sum);
+    if (c.dtype == SFB_F32) sum_piece(reinterpret_cast<const float*>(c.src), c.count, sums);
+    else if (c.dtype == SFB_BF16) sum_piece(reinterpret_cast<const __nv_bfloat16*>(c.src), c.count, sums);
+    else sum_piece(reinterpret_cast<const __half*>(c.src), c.count, sums);
   }
-  sum = block_sum(sum);
+  const double sum = block_sum(sums[0] + sums[1]);
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 

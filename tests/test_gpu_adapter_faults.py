@@ -70,3 +70,17 @@ def test_the_term_is_not_held_in_one_word(size):
     for k, (v, b) in two_word_bounds(c).items():
         off = (got[k].double() - v).abs()
         assert (off <= b).all(), f"{k}: {(off / b.clamp(min=1e-300)).max().item():.3g} of the bound"
+
+
+@pytest.mark.parametrize("value,count", [(1.174750804901123, 123_456), (1.174750804901123, 200_000), (1.174750804901123, 500_000), (1.6343168020248413, 5_000), (1.6343168020248413, 40_000)])
+def test_squares_are_not_rounded_to_32_bits(value, count):
+    """Entries whose squares all round the same way in fp32: the norm and the factor are the 64-bit ones, rounded once.  (fp64 sums are
+    off by 1e-12 at most; the norms lie further than that from where the rounding turns.)"""
+    t = torch.full((count,), value, device="cuda")
+    norm = t.double().square().sum().sqrt().item()
+    result = torch.zeros(2, device="cuda")
+    S.GradientClip([t]).sfb_clip_gradients(1.5, result)
+    want = torch.tensor([norm, 1.5 / norm], dtype=torch.float64)
+    for near in (want * (1 - 1e-11), want * (1 + 1e-11)):
+        assert torch.equal(near.float(), want.float())
+    assert torch.equal(result.cpu(), want.float())
