@@ -386,7 +386,9 @@ int sfb_adapter_destroy(sfb_adapters* h);
  * vector,
  *     norm = sqrt(sum_t sum_j g_tj^2),   coef = max_norm / norm where norm > max_norm, else 1,   out_t = coef * g_t.
  * Squares are summed in fp64, in an order that does not depend on timing.  result_dev[0] = norm, result_dev[1] = coef (fp32).
- * Where the norm is infinite or not a number, out_t = g_t unscaled and coef = 0 (a multiplier that drops the step).
+ * Where the norm is infinite or not a number, out_t = g_t unscaled and coef = 0: not what the tensors were multiplied with, but a
+ * multiplier for the caller's step that drops it.  The norm is formed in fp64: where it is finite there but beyond fp32,
+ * result_dev[0] is infinite, and the tensors are rescaled by coef as ever.
  *
  *  - Tensor t has counts[t] >= 0 entries of dtypes[t] (0 fp32, 1 bf16, 2 fp16) without gaps at src[t], aligned to its entries; dst[t]
  *    (of the same type) is src[t] itself, or does not overlap any tensor.  dst null: every tensor in place.

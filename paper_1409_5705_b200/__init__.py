@@ -526,7 +526,8 @@ class GradientClip:
         return t.data_ptr()
 
     def sfb_clip_gradients(self, max_norm, result):
-        """result (fp32, 2 entries) receives the norm and the factor that the tensors were multiplied with."""
+        """result (fp32, 2 entries) receives the norm and the factor that the tensors were multiplied with.  Where the norm is infinite or
+        NaN the tensors are not multiplied (outs are copies), and the second entry is 0, which tells the caller to drop the step."""
         import torch
         self._ck(lib().sfb_clip_gradients(self._h, max_norm, self._out(result, torch.float32, 2)), "sfb_clip_gradients")
 

@@ -84,3 +84,18 @@ def test_squares_are_not_rounded_to_32_bits(value, count):
     for near in (want * (1 - 1e-11), want * (1 + 1e-11)):
         assert torch.equal(near.float(), want.float())
     assert torch.equal(result.cpu(), want.float())
+
+
+@pytest.mark.parametrize("place", ["apart", "inside"])
+def test_a_norm_beyond_fp32_is_still_a_factor(place):
+    """norm = 6e38 in fp64: result[0] is infinite in fp32, the factor 1 / 6e38 (below fp32's normal numbers: 2^-150 off at most) and applied."""
+    src = [torch.full((3,), 3e38, device="cuda"), torch.full((1,), 3e38, dtype=torch.bfloat16, device="cuda")]
+    ts = [t.clone() for t in src]
+    outs = [torch.zeros_like(t) for t in src] if place == "apart" else None
+    result = torch.zeros(2, device="cuda")
+    S.GradientClip(src, outs).sfb_clip_gradients(1.0, result)
+    norm = sum(t.double().square().sum().item() for t in ts) ** 0.5
+    assert result[0] == float("inf") and abs(result[1].item() - 1.0 / norm) <= 2.0 ** -150
+    for t, o in zip(ts, outs or src):
+        want = t.double() / norm
+        assert ((o.double() - want).abs() <= (torch.finfo(t.dtype).eps / 2 + 2.0 ** -24) * want + t.double() * 2.0 ** -150).all()
