@@ -358,6 +358,15 @@ def sfb_adapter_workspace_bytes(cfg: sfb_adapter_config) -> int:
     return out.value
 
 
+def _workspace(nbytes, device, stream):
+    """Memory that a handle uses on ``stream``, whichever stream is current here: given up with calls still under way there, it is not
+    handed out again before they are done."""
+    import torch
+    t = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    t.record_stream(stream)
+    return t
+
+
 def _capture(stream, calls):
     import torch
     g = torch.cuda.CUDAGraph()
@@ -399,7 +408,7 @@ class Adapters:
         nbytes = sfb_adapter_workspace_bytes(self.cfg)
         self._h = ctypes.c_void_p()
         with torch.cuda.device(W.device):
-            self.workspace = torch.empty(nbytes + 1024, dtype=torch.uint8, device=W.device)
+            self.workspace = _workspace(nbytes + 1024, W.device, self.stream)
             base = (self.workspace.data_ptr() + 1023) // 1024 * 1024
             rc = lib().sfb_adapter_init(ctypes.byref(self.cfg), W.data_ptr(), U.data_ptr(), V.data_ptr(), scale.data_ptr(), base,
                                         nbytes, ctypes.byref(self._h))
@@ -510,7 +519,7 @@ class GradientClip:
             raise SfbError(rc, "sfb_clip_workspace_bytes")
         self._h = ctypes.c_void_p()
         with torch.cuda.device(dev):
-            self.workspace = torch.empty(nbytes.value, dtype=torch.uint8, device=dev)
+            self.workspace = _workspace(nbytes.value, dev, self.stream)
             rc = lib().sfb_clip_init(m, src, dst, counts, dtypes, self.workspace.data_ptr(), nbytes.value, self.stream.cuda_stream,
                                      ctypes.byref(self._h))
         if rc:

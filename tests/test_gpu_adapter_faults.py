@@ -99,3 +99,33 @@ def test_a_norm_beyond_fp32_is_still_a_factor(place):
     for t, o in zip(ts, outs or src):
         want = t.double() / norm
         assert ((o.double() - want).abs() <= (torch.finfo(t.dtype).eps / 2 + 2.0 ** -24) * want + t.double() * 2.0 ** -150).all()
+
+
+@pytest.mark.parametrize("kind", ["adapters", "clip"])
+def test_memory_of_a_dropped_handle_whose_calls_are_under_way(kind):
+    """A handle on a stream of its own is dropped before its call has run: its workspace is not handed out again until it has."""
+    s = torch.cuda.Stream()
+    c = Case(300, 400, 320, 5, 16, "runs", seed=1)
+    Y, Sx = torch.zeros(300, 400, dtype=torch.bfloat16, device="cuda"), torch.zeros(300, 16, device="cuda")
+    g, result = torch.full((100_000,), 2.0, device="cuda"), torch.zeros(2, device="cuda")
+    torch.cuda.synchronize()
+    plan = S.Adapters(c.W, c.U, c.V, c.scale, max_samples=300, stream=s) if kind == "adapters" else S.GradientClip([g], stream=s)
+    call = (lambda: plan.sfb_adapter_forward(c.X, c.ids, Y, Sx)) if kind == "adapters" else (lambda: plan.sfb_clip_gradients(1.0, result))
+    call()                                              # (kernels are loaded by their first launches, which wait)
+    torch.cuda.synchronize()
+    g.fill_(2.0)
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(1)
+        s.synchronize()
+        torch.cuda._sleep(100_000_000)                  # about 50 ms
+    call()
+    at, n = plan.workspace.data_ptr(), plan.workspace.numel()
+    del plan, call
+    again = torch.empty(n, dtype=torch.uint8, device="cuda")
+    busy = not s.query()
+    torch.cuda.synchronize()
+    assert busy and again.data_ptr() != at
+    if kind == "adapters":
+        check(c, {"Y": Y, "S": Sx}, ("Y", "S"))
+    else:
+        assert (g * 100_000 ** 0.5 - 1.0).abs().max() <= 2.0 ** -20
