@@ -376,6 +376,14 @@ int sfb_adapter_forward(sfb_adapters* h, int64_t n, const void* X_dev, int64_t l
  * null: dX_dev [n x lddx], dU_dev, dV_dev.  dU and dV are written whole, zeros for adapters without a sample. */
 int sfb_adapter_backward(sfb_adapters* h, int64_t n, const void* dY_dev, int64_t lddy, const void* X_dev, int64_t ldx,
                          const int32_t* ids_dev, const float* S_dev, void* dX_dev, int64_t lddx, float* dU_dev, float* dV_dev);
+/* Which way a call of `samples` samples takes (0 .. max_samples; backward 0: the forward pass, 1: the backward pass with all outputs).
+ * Host-only; no CUDA call.  For measurements and tests.
+ *   factors       0: s (backward: t) in fp32 FMAs, 1: on the tensor cores
+ *   factor_blocks k-blocks of 64 that a part of its contraction has, at most (1); sums leave the tensor cores every 12
+ *   in_order      1: the device decides whether the samples are taken in the order of their adapters
+ *   share_blocks  k-blocks of 64 samples that a share of dU and dV has, at most, where all samples name one adapter (0: forward) */
+int sfb_adapter_get_plan(const sfb_adapter_config* cfg, int64_t samples, int32_t backward, int32_t* factors, int32_t* factor_blocks,
+                         int32_t* in_order, int32_t* share_blocks);
 /* As sfb_get_status, sfb_last_cuda_error and sfb_destroy. */
 int sfb_adapter_get_status(sfb_adapters* h, uint32_t* status_out);
 int sfb_adapter_last_cuda_error(sfb_adapters* h);

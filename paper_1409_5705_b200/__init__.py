@@ -27,7 +27,7 @@ EXPORTS = ("sfb_workspace_bytes", "sfb_init", "sfb_compute_factors", "sfb_gather
            "sfb_sdca_step", "sfb_set_factors", "sfb_set_eta", "sfb_get_operand_copy", "sfb_compute_factors_csr",
            "sfb_step_csr", "sfb_export_factors", "sfb_forward_partials_pairs",
            "sfb_adapter_workspace_bytes", "sfb_adapter_init", "sfb_adapter_forward", "sfb_adapter_backward",
-           "sfb_adapter_get_status", "sfb_adapter_last_cuda_error", "sfb_adapter_destroy",
+           "sfb_adapter_get_plan", "sfb_adapter_get_status", "sfb_adapter_last_cuda_error", "sfb_adapter_destroy",
            "sfb_clip_workspace_bytes", "sfb_clip_init", "sfb_clip_sum", "sfb_clip_scale", "sfb_clip_gradients",
            "sfb_clip_last_cuda_error", "sfb_clip_destroy")
 NOALLOC_MAX_COLS = 16384
@@ -117,6 +117,7 @@ def lib() -> ctypes.CDLL:
         L.sfb_adapter_init.argtypes = [acfgp, vp, vp, vp, vp, vp, ctypes.c_size_t, ctypes.POINTER(vp)]
         L.sfb_adapter_forward.argtypes = [vp, i64, vp, i64, vp, vp, i64, vp]
         L.sfb_adapter_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp]
+        L.sfb_adapter_get_plan.argtypes = [acfgp, i64, i32] + [ctypes.POINTER(i32)] * 4
         L.sfb_adapter_get_status.argtypes = [vp, ctypes.POINTER(ctypes.c_uint32)]
         L.sfb_adapter_last_cuda_error.argtypes = [vp]
         L.sfb_adapter_destroy.argtypes = [vp]
@@ -356,6 +357,15 @@ def sfb_adapter_workspace_bytes(cfg: sfb_adapter_config) -> int:
     if rc:
         raise SfbError(rc, "sfb_adapter_workspace_bytes")
     return out.value
+
+
+def sfb_adapter_get_plan(cfg: sfb_adapter_config, samples: int, backward: bool = False):
+    """(factors, factor_blocks, in_order, share_blocks) of a call of ``samples`` samples; see include/sfb.h."""
+    out = [ctypes.c_int32(0) for _ in range(4)]
+    rc = lib().sfb_adapter_get_plan(ctypes.byref(cfg), samples, 1 if backward else 0, *(ctypes.byref(o) for o in out))
+    if rc:
+        raise SfbError(rc, "sfb_adapter_get_plan")
+    return tuple(o.value for o in out)
 
 
 def _workspace(nbytes, device, stream):

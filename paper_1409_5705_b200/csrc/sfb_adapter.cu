@@ -151,6 +151,11 @@ __device__ __forceinline__ void put_pair(__nv_bfloat16* pb, int64_t i, int per, 
 // registers from drain to drain.
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kRankThreads = 320, kRankTile = 128, kFewChunks = 64;
+// FEW: parts of the contraction that the grid's blocks make for each chunk.
+__host__ __device__ inline int few_rank_parts(int blocks, int chunks, int kseg) {
+  const int most = blocks / chunks < kMaxParts ? blocks / chunks : kMaxParts, parts = most < kseg / 4 ? most : kseg / 4;
+  return parts < 1 ? 1 : parts;
+}
 struct RankParams {
   int32_t n, tn, kseg, stages;
   int32_t rank, adapters;
@@ -201,7 +206,7 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
   // this block's chunks [c0, c0 + step, ..) and its part of their contraction
   int c0 = blockIdx.z, step = gridDim.z, part = blockIdx.x, parts = gridDim.x;
   if (FEW) {
-    parts = chunks ? max(1, min(min(kMaxParts, static_cast<int>(gridDim.x) / chunks), p.kseg / 4)) : 1;
+    parts = chunks ? few_rank_parts(gridDim.x, chunks, p.kseg) : 1;
     step = parts > 1 ? chunks : gridDim.x;
     c0 = parts > 1 ? blockIdx.x % chunks : blockIdx.x;
     part = parts > 1 ? blockIdx.x / chunks : 0;
@@ -1844,6 +1849,9 @@ int rank_parts(int64_t n, int64_t d) {
   const int64_t tiles = std::max<int64_t>(1, (n + rank_tile(n) - 1) / rank_tile(n)), kseg = (d + BK - 1) / BK;     // (a handle's n may be 0)
   return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({kMaxParts, 2 * kModelSms / tiles, kseg / 4})));
 }
+// Chunks of a tile, at most; blocks up to 64 samples: one an SM, and no more than there can be parts of chunks.
+int rank_chunks(const sfb_adapter_config& c, int64_t n) { return (std::min(rank_tile(n), c.adapters) * ((c.rank + kSlice - 1) / kSlice) + 7) / 8; }
+int few_rank_blocks(const sfb_adapter_config& c, int64_t n, int64_t d) { return std::max(1, std::min(kModelSms, rank_chunks(c, n) * rank_parts(n, d))); }
 // Most samples x parts of a call of up to n samples.
 int64_t rank_rows(int64_t n, int64_t d) {
   int64_t most = 0;
@@ -2060,7 +2068,7 @@ cudaError_t rank_products(sfb_adapters* h, int64_t n, const Samples& z, const in
   p.n = static_cast<int32_t>(n); p.tn = tn; p.kseg = static_cast<int32_t>((d + BK - 1) / BK);
   p.stages = std::min(kMaxStages, (n <= kFewMost ? kFewRing : kSmallRing) / stage_bytes(tn));
   p.rank = c.rank; p.adapters = c.adapters; p.boxed = h->boxed_slices; p.ids = ids; p.out = out; p.status = h->at<uint32_t>(h->lay.status);
-  const int per = (c.rank + kSlice - 1) / kSlice, chunks = (std::min(tn, c.adapters) * per + 7) / 8;
+  const int chunks = rank_chunks(c, n);
   const int smem = p.stages * stage_bytes(tn) + 1024;
   if (n <= kFewMost) {
     p.scale = h->scale; p.p = sum; p.pb = h->at<__nv_bfloat16>(h->lay.pb);
@@ -2068,8 +2076,7 @@ cudaError_t rank_products(sfb_adapters* h, int64_t n, const Samples& z, const in
     const cudaError_t e = allow_beside<adapter_rank_kernel<true>>(kFewRing + 1024);
     if (e != cudaSuccess) return e;
     *got = Ranked{sum, 1, 0};
-    // a block an SM, and no more than there can be parts of chunks
-    return launch_kernel(adapter_rank_kernel<true>, dim3(std::max(1, std::min(kModelSms, chunks * parts))), dim3(kRankThreads), smem, h->stream, 1, mf, mz, ms, p);
+    return launch_kernel(adapter_rank_kernel<true>, dim3(few_rank_blocks(c, n, d)), dim3(kRankThreads), smem, h->stream, 1, mf, mz, ms, p);
   }
   const int groups = std::max(1, std::min(chunks, 2 * kModelSms / (parts * tiles)));
   const cudaError_t e = allow_smem<adapter_rank_kernel<false>>(kSmallRing + 1024);
@@ -2225,8 +2232,8 @@ cudaError_t index_samples(sfb_adapters* h, int64_t n, const int32_t* ids, int64_
   return launch_kernel(adapter_index_kernel, dim3(c.adapters + 1 + p.tiles), dim3(n <= 2048 ? 256 : 32 * kIndexWarps), 0, h->stream, 1, p);
 }
 // ... whether there is room for that too.
-bool sorts(const sfb_adapters* h, int64_t n, int64_t m, int64_t d) {
-  return sort_may_pay(h->cfg, n, m, d) && h->lay.begin > h->lay.sorted_ids && fits(n, d, h->lay.order - h->lay.zcopy);
+bool sorts(const sfb_adapter_config& c, const AdapterLayout& lay, int64_t n, int64_t m, int64_t d) {
+  return sort_may_pay(c, n, m, d) && lay.begin > lay.sorted_ids && fits(n, d, lay.order - lay.zcopy);
 }
 
 int fail(sfb_adapters* h, cudaError_t e) {
@@ -2250,6 +2257,27 @@ extern "C" int sfb_adapter_workspace_bytes(const sfb_adapter_config* cfg, size_t
   const int rc = check(cfg);
   if (rc) return rc;
   *out_bytes = layout_of(*cfg).total;
+  return SFB_OK;
+}
+
+extern "C" int sfb_adapter_get_plan(const sfb_adapter_config* cfg, int64_t samples, int32_t backward, int32_t* factors, int32_t* factor_blocks,
+                                    int32_t* in_order, int32_t* share_blocks) {
+  const int rc = check(cfg);
+  if (rc) return rc;
+  if (samples < 0 || !factors || !factor_blocks || !in_order || !share_blocks) return SFB_ERR_ARG;
+  if (samples > cfg->max_samples) return SFB_ERR_SHAPE;
+  const sfb_adapter_config& c = *cfg;
+  const int64_t d = backward ? c.rows : c.cols, m = backward ? c.cols : c.rows;
+  const int kseg = static_cast<int>((d + BK - 1) / BK);
+  *factors = use_dot(c, samples, d) ? 0 : 1;
+  *factor_blocks = 0;
+  if (*factors) {
+    const int parts = samples <= kFewMost ? few_rank_parts(few_rank_blocks(c, samples, d), rank_chunks(c, samples), kseg) : rank_parts(samples, d);
+    *factor_blocks = (kseg + parts - 1) / parts;
+  }
+  *in_order = sorts(c, layout_of(c), samples, m, d) ? 1 : 0;
+  const int64_t blocks = (samples + BK - 1) / BK;
+  *share_blocks = backward ? static_cast<int32_t>((blocks + grad_shares(c, samples) - 1) / grad_shares(c, samples)) : 0;
   return SFB_OK;
 }
 
@@ -2316,7 +2344,7 @@ extern "C" int sfb_adapter_forward(sfb_adapters* h, int64_t n, const void* X_dev
   float* sum = S_dev ? S_dev : h->at<float>(h->lay.ssum);
   Sorting sort{};
   Samples z;
-  if (sorts(h, n, c.rows, c.cols)) ACK(index_samples(h, n, ids_dev, c.rows, c.cols, &sort));
+  if (sorts(c, h->lay, n, c.rows, c.cols)) ACK(index_samples(h, n, ids_dev, c.rows, c.cols, &sort));
   ACK(placed(h, n, X_dev, ldx, c.cols, c.rows, sort, &z));
   bool all;
   ACK(rank_products<false>(h, n, z, ids_dev, h->at<float>(h->lay.s), sum, WordsParams{}, &s, &all));
@@ -2345,7 +2373,7 @@ extern "C" int sfb_adapter_backward(sfb_adapters* h, int64_t n, const void* dY_d
   uint32_t* status = h->at<uint32_t>(h->lay.status);
   int32_t *order = h->at<int32_t>(h->lay.order), *begin = h->at<int32_t>(h->lay.begin), *count = h->at<int32_t>(h->lay.count);
   Sorting sort{};
-  const bool sorting = dX_dev && sorts(h, n, c.cols, c.rows);
+  const bool sorting = dX_dev && sorts(c, h->lay, n, c.cols, c.rows);
   if (dU_dev || dV_dev || sorting) ACK(index_samples(h, n, ids_dev, c.cols, c.rows, sorting ? &sort : nullptr));
   Ranked s{S_dev, 1, 0}, t{};
   bool all = false;
