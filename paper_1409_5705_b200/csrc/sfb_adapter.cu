@@ -206,10 +206,11 @@ adapter_rank_kernel(const __grid_constant__ CUtensorMap tmF, const __grid_consta
   // this block's chunks [c0, c0 + step, ..) and its part of their contraction
   int c0 = blockIdx.z, step = gridDim.z, part = blockIdx.x, parts = gridDim.x;
   if (FEW) {
+    // (the grid has a block for each chunk at least: up to 64 samples have 64 chunks at most)
     parts = chunks ? few_rank_parts(gridDim.x, chunks, p.kseg) : 1;
-    step = parts > 1 ? chunks : gridDim.x;
-    c0 = parts > 1 ? blockIdx.x % chunks : blockIdx.x;
-    part = parts > 1 ? blockIdx.x / chunks : 0;
+    step = max(chunks, 1);
+    c0 = blockIdx.x % step;
+    part = blockIdx.x / step;
     if (part >= parts) c0 = chunks;                  // nothing
   }
   const int kbeg = static_cast<int>(static_cast<int64_t>(part) * p.kseg / parts), kend = static_cast<int>(static_cast<int64_t>(part + 1) * p.kseg / parts);
