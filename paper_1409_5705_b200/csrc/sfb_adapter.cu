@@ -399,7 +399,10 @@ __device__ __forceinline__ void store_chunk(__nv_bfloat16* Y, int64_t ldy, int i
 // The adapters' term, scale F[a_i]^T p_i, of the three products below is more contraction behind the k-blocks of A: the factors of the
 // adapters in the tile's list, four units of 8 ranks a k-block, against  scale p  of the samples as two words of bf16 (2^-16 of the term;
 // with one word, and eight units a k-block, the term's rounding was as large as that of the result), with zeros where a sample has another
-// adapter.  Zeros do not hide what is not finite: some warps look
+// adapter.  (us with one word and with two: 37 samples of 64 adapters of 16 ranks, 10,000 x 20,000, 73.0 and 73.5; 1,024 of 64 of 8, gradients,
+// 1,000 x 20,000, 116.6 and 122.5; 64 of 64 of 64, 10,000 x 5,000, 47.2 and 52.6; where the term is nearly all of the work, 333 of 150 of 128,
+// 9,000 x 1,000, 213 and 301.  Eight units a k-block with a ring of two or four places for the second words: 303 and 230 of the last, but 2 to
+// 7 us more for the second and for 1,003 samples, whose ring of stages is as much shorter, and for 37 samples 83.)  Zeros do not hide what is not finite: some warps look
 // through the factors in shared memory and replace what is not finite by zeros, and the end of the tile adds those entries alone to their
 // own samples, in fp32.
 // (In fp32 FMAs from global memory, as it was for up to 64 samples, a tile's term is a chain of loads: 64 samples of 8 ranks took 99 us a
@@ -741,15 +744,15 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // its TMEM; it loads its own rows and its half of the samples, 32 KB a k-block.  Two accumulators: the end of a tile runs beside the next
 // one's products.  Whole rounds of tiles are taken whole, the k-blocks of the rest are shared out (Segments in sfb_tile.cuh); the pair that
 // finishes a tile has its term.
-// Bound by the tensor cores where the contraction is long: 4,096 samples, 10,000 x 20,000: 1,170 us in a loop, 1.40 PFLOP/s, the rate the GPU
-// sustains at its power cap.  Where it is short, by what a k-block of the term waits for: it takes a stage only once that is free, and its
+// Bound by the tensor cores where the contraction is long: 4,096 samples, 10,000 x 20,000: 1,266 us in a stream of gradients, 1.30 PFLOP/s at the
+// power cap.  Where it is short, by what a k-block of the term waits for: it takes a stage only once that is free, and its
 // copies, the look at them and the other CTA's word come to 4,500 cycles, of which the stages ahead cover 3,000 (1,024 samples of 64 adapters
-// of 8 ranks, 1,000 x 20,000, 57 us: a tile of 16 + 3 k-blocks takes 16,000 cycles, 9,700 of them products).
+// of 8 ranks, 1,000 x 20,000: 61 us; with a word, and 16 + 3 k-blocks a tile instead of 16 + 5, 57: a tile took 16,000 cycles, 9,700 of them products).
 //
 // Warps: 0 TMA producer, 1 MMA issuer (leader CTA) and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the columns), 10..13
-// the samples' operand of the term and the loads of its factors, 14..17 the look at them, 18 and 19 hand the other CTA's on to the leader.
+// the samples' operand of the term and the loads of its factors, 14..17 the look at them, 18, 19 and, in the other CTA, 1 hand that CTA's on to the leader.
 // ---------------------------------------------------------------------------------------------------------
-constexpr int kPairBuild = 4, kHand = 2, kPairThreads = 32 * (2 + kEpi + 2 * kPairBuild + kHand), kGroup = 8;      // kGroup: tiles of samples that follow one another
+constexpr int kPairBuild = 4, kHand = 3, kPairThreads = 32 * (2 + kEpi + 2 * kPairBuild + kHand - 1), kGroup = 8;      // kGroup: tiles of samples that follow one another
 constexpr int kPairStages = 6, kPairStage = 2 * kTileBytesA;
 constexpr int kPairHeld = 2 * kUnits;               // units of its row of pb that a writing thread has at hand, behind the stages
 constexpr int kPairSmem = kPairStages * kPairStage + 128 * kPairHeld * 32 + 1024;
@@ -810,10 +813,32 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     tt = g * kGroup + at % width;
   };
 
+  // Hands on, in the other CTA, the term's k-blocks in the stages s with s % kHand == h: a release to the cluster, 1,650 cycles of a warp that has
+  // no accesses of its own.  A stage is built again only once its k-block is multiplied, so once the warp that it belongs to has seen it: no
+  // warp looks for a phase that it could miss.
+  auto hand_on = [&](int h) {
+    uint32_t s = 0, bph = 0;
+    bool ok = true;
+    for (int i = 0; i < segs.n && ok; ++i) {
+      const Segment sg = segs.get(i);
+      int m0, tt;
+      tile_coords(sg.tile, m0, tt);
+      s = (s + sg.k1 - sg.k0) % kPairStages;
+      for (int left = sg.k1 == p.kseg ? p.term.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0; left > 0 && ok; left -= kUnits) {
+        if (static_cast<int>(s % kHand) == h) {
+          ok = mbar_wait_warp(&built[s], (bph >> s) & 1, abort_flag);
+          bph ^= 1u << s;
+          if (ok && lane == 0) mbar_arrive_cluster(mapa_u32(smem_u32(&joined[s]), 0));
+        }
+        if (++s == static_cast<uint32_t>(kPairStages)) s = 0;
+      }
+    }
+  };
+
   if (threadIdx.x == 0) {
     for (int i = 0; i < kPairStages; ++i) {
-      mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&landed[i], 1); mbar_init(&joined[i], 1);
-      mbar_init(&built[i], 2 * kPairBuild + (rank ? kHand : 0));       // (see the hand-over)
+      mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&landed[i], 1); mbar_init(&built[i], 2 * kPairBuild);
+      mbar_init(&joined[i], 1);
     }
     for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 2 * kEpi); mbar_init(&looked[i], kPairBuild); mbar_init(&taken[i], kEpi); }
     abort_word = 0;
@@ -917,6 +942,8 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         }
         if (ok && elect_one()) umma_commit_pair(&tfull[a], 3);
       }
+    } else {
+      hand_on(kHand - 1);
     }
   } else if (warp < 2 + kEpi) {
     // ---------------- epilogue ----------------
@@ -991,32 +1018,10 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     }
   } else if (warp >= 2 + kEpi + 2 * kPairBuild) {
     // ---------------- hand on the other CTA's operands ----------------
-    // (A release to the cluster by each of the eight warps that make them took 1 us a k-block, and one warp, with no accesses of its own,
-    // that hands all of them on is not much faster: these take them in turn.  1,024 samples, 1,000 x 20,000, eight k-blocks of the term a tile:
-    // 98, 89 and 76 us.)
-    // Both see every k-block, and its stage is built again only once both have: each arrives for the next phase of `built` when it has seen
-    // one (for the first at once).  Without that the warp whose turn it is not could still be looking for a phase when the next one
-    // is complete, whose parity is that of the phase before, and wait for good.
-    uint32_t s = 0, bph = 0, turn = warp - 2 - kEpi - 2 * kPairBuild;
-    bool ok = true;
-    if (rank == 1 && lane < kPairStages) mbar_arrive(&built[lane]);
-    for (int i = 0; i < segs.n && ok && rank == 1; ++i) {
-      const Segment sg = segs.get(i);
-      int m0, tt;
-      tile_coords(sg.tile, m0, tt);
-      s = (s + sg.k1 - sg.k0) % kPairStages;
-      for (int left = sg.k1 == p.kseg ? p.term.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0; left > 0 && ok; left -= kUnits) {
-        ok = mbar_wait_warp(&built[s], (bph >> s) & 1, abort_flag);
-        bph ^= 1u << s;
-        if (turn == 0) {
-          if (ok && lane == 0) mbar_arrive_cluster(mapa_u32(smem_u32(&joined[s]), 0));
-          turn = kHand;
-        }
-        --turn;
-        if (ok && lane == 0) mbar_arrive(&built[s]);
-        if (++s == static_cast<uint32_t>(kPairStages)) s = 0;
-      }
-    }
+    // (1,024 samples, 1,000 x 20,000, eight k-blocks of the term a tile: 98 us with releases by each of the eight warps that make the operands, 89
+    // with one warp that hands all on, 76 with two in turn.  333 samples of 150 adapters of 128 ranks, 9,000 x 1,000: 351 with two in turn,
+    // 311 with two by stages, 300 with three.)
+    if (rank == 1) hand_on(warp - 2 - kEpi - 2 * kPairBuild);
   } else {
     // ---------------- the samples' operand of the term, and its factors ----------------
     const bool writes = warp < 2 + kEpi + kPairBuild;
