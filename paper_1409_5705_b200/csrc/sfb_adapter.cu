@@ -401,8 +401,8 @@ __device__ __forceinline__ void store_chunk(__nv_bfloat16* Y, int64_t ldy, int i
 // with one word, and eight units a k-block, the term's rounding was as large as that of the result), with zeros where a sample has another
 // adapter.  (us with one word and with two: 37 samples of 64 adapters of 16 ranks, 10,000 x 20,000, 73.0 and 73.5; 1,024 of 64 of 8, gradients,
 // 1,000 x 20,000, 116.6 and 122.5; 64 of 64 of 64, 10,000 x 5,000, 47.2 and 52.6; where the term is nearly all of the work, 333 of 150 of 128,
-// 9,000 x 1,000, 213 and 301.  Eight units a k-block with a ring of two or four places for the second words: 303 and 230 of the last, but 2 to
-// 7 us more for the second and for 1,003 samples, whose ring of stages is as much shorter, and for 37 samples 83.)  Zeros do not hide what is not finite: some warps look
+// 9,000 x 1,000, 213 and 301.  Eight units a k-block with a ring of two places for the second words: 303 of the last and 83 of the first; with
+// four, and a stage less for W: 230 of the last, the same or a per cent more of the others.)  Zeros do not hide what is not finite: some warps look
 // through the factors in shared memory and replace what is not finite by zeros, and the end of the tile adds those entries alone to their
 // own samples, in fp32.
 // (In fp32 FMAs from global memory, as it was for up to 64 samples, a tile's term is a chain of loads: 64 samples of 8 ranks took 99 us a
@@ -1424,7 +1424,9 @@ __global__ void __launch_bounds__(256) adapter_dot_kernel(const __grid_constant_
 // [rows][pitch_in] to [rows][pitch_out], `pieces` of 16 bytes a row.  A row of a box is 128 bytes, four sectors of L2; where the rows of an
 // operand are an odd multiple of 16 bytes apart, half of them are five, and the products of many samples, which move their operands
 // through L2 at its rate, take up to 1.4 times as long (8,192 samples, 10,000 x 5,000 in a loop: pitches of 5,000 entries 997 us, 5,008 774,
-// 5,056 720).  Such operands are copied where the copy, 4 bytes an entry at HBM's rate, costs less than that: from 2,100 uses of a row on.
+// 5,056 720).  Such operands are copied where the copy, 4 bytes an entry at HBM's rate and a launch, costs less than that, which it does from
+// 3,500 uses of a row on: us without and with it, of X for 8,192 samples and 2,200 rows of 5,000 entries 205 and 216, 3,000 277 and 281, 3,500 310
+// and 310, 4,000 340 and 334; of W, 10,000 x 5,000, for 2,200 samples 247 and 261, 3,000 327 and 331, 3,500 375 and 373, 4,000 426 and 419.
 // ---------------------------------------------------------------------------------------------------------
 // Samples that are taken in the order of their adapters come here too (if_sorted: only then is there anything to do).
 constexpr int64_t kCopyUses = 4096;
@@ -1462,9 +1464,11 @@ __global__ void __launch_bounds__(256) adapter_copy_kernel(const uint4* in, int6
 // share of the term grows by as much, while samples in order have to be copied.  More blocks (tiles of them) count the adapters of each 128
 // samples as they come, and the last block of all compares the bytes: a factor's entries times the ranks of the pairs of a tile and an
 // adapter that there are fewer of, against those of the samples, read and written.  (Gradients, us as the samples come and in order: 1,024
-// samples of 64 adapters of 8 ranks at random, 1,000 x 20,000: 143 and 132; 2,000 of 100 adapters of 32 ranks, 5,000 x 5,000: 330 and 206;
-// 4,096 of 8 adapters of 128, 4,000 x 20,000: 855
-// and 695.  Finding out that it does not pay, a forward pass of 8,192 samples one request after another, 10,000 x 5,000: 670 and 679.)
+// samples of 64 adapters of 8 ranks at random, 1,000 x 20,000: 150 and 122; 2,000 of 100 adapters of 32 ranks, 5,000 x 5,000: 390 and 206;
+// 4,096 of 8 adapters of 128, 4,000 x 20,000: 1,093 and 793.  Finding out that it does not pay, a forward pass of 8,192 samples of 64 adapters of
+// 16 ranks, one request after another, 10,000 x 5,000: 776 to 785 and 787 to 799.)
+//
+// Every block reads all ids, adapters x samples reads: 6 us of a call for 64 adapters and 1,024 samples, 12 for 32 and 4,096.
 // ---------------------------------------------------------------------------------------------------------
 struct IndexParams {
   const int32_t* ids;
@@ -1988,9 +1992,9 @@ struct OnDevice {                      // the handle's device is current for the
   }
 };
 
-// A matrix [outer x inner], boxes with the 128-byte swizzle.  Operands that are streamed once are asked for 256 bytes at a time (up to 64
-// samples, 10,000 x 20,000: 69 us, 75 with boxes alone; 325,000 x 10,000: 1,522 and 1,588), those that tiles share in L2 by boxes alone (8,192
-// samples, 10,000 x 5,000, whose rows are 16 bytes off a sector: 755 us, 882 with 256 bytes; 1,024, 10,000 x 20,000: 302 and 395).
+// A matrix [outer x inner], boxes with the 128-byte swizzle.  Operands that are streamed once are asked for 256 bytes at a time (64 samples,
+// 10,000 x 20,000: 71.2 us, 73.8 with boxes alone; 325,000 x 10,000: 1,025 and 1,056), those that tiles share in L2 by boxes alone (1,024 samples,
+// 10,000 x 20,000: 390 us, 442 with 256 bytes; 8,192, 10,000 x 5,000, whose operands are copied: 790 and 795).
 bool operand_map(sfb_adapters* h, CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t pitch, int box_inner, int box_outer,
                  CUtensorMapL2promotion promotion) {
   cuuint64_t dims[2] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(outer)}, strides[1] = {static_cast<cuuint64_t>(pitch) * 2};

@@ -23,7 +23,10 @@ constexpr int kModelSms = 148;        // what the cost models, hence the layout 
 // programmatic stream serialisation, so that its blocks are scheduled and its set-up runs while the kernel before it
 // drains.  Every kernel launched this way calls pdl_wait() before it touches memory (it returns when the kernels before it
 // have completed and their writes are visible) and pdl_launch_dependents() early (the next kernel may then start its own
-// set-up once all blocks of this one are running).  The tile kernels are launched this way only when they have at most one
+// set-up once all blocks of this one are running).  One kernel reads before its wait: adapter_few_kernel, W and the samples.  The launch ahead of
+// it is always adapter_rank_kernel<true> or adapter_dot_kernel of the same call, neither of which writes those, and which call pdl_wait()
+// BEFORE pdl_launch_dependents(), so that all that was enqueued before the call is complete when adapter_few_kernel starts.  No kernel may
+// come between them that does not keep that order.  The tile kernels are launched this way only when they have at most one
 // tile per SM: started while the SMs fall free one by one, their blocks land on them in that order, neighbours apart, and the
 // operands that neighbours share are read across the dies (3-4 % of a step at 325,000 x 10,000).
 // ---------------------------------------------------------------------------------------------------------
