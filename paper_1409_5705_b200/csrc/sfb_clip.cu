@@ -24,7 +24,9 @@ using sfb::pdl_wait;
 
 constexpr int kThreads = 256;
 constexpr int64_t kPieceBytes = 16384;               // four 16-byte loads a thread
-constexpr int kSumBlocks = 4, kScaleBlocks = 4;      // an SM
+// Blocks an SM.  (The sum's squares in fp64 want more threads than its loads do: us with 4, 6 and 8 of its blocks, 500 M fp32 1,030, 1,011 and 1,022;
+// 40 M of three types 57.1, 55.5 and 55.0; 21 M bf16 25.7, 24.8 and 25.8.)
+constexpr int kSumBlocks = 6, kScaleBlocks = 4;
 
 struct Piece {
   const char* src;
