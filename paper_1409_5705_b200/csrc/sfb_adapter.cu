@@ -744,10 +744,10 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // its TMEM; it loads its own rows and its half of the samples, 32 KB a k-block.  Two accumulators: the end of a tile runs beside the next
 // one's products.  Whole rounds of tiles are taken whole, the k-blocks of the rest are shared out (Segments in sfb_tile.cuh); the pair that
 // finishes a tile has its term.
-// Bound by the tensor cores where the contraction is long: 4,096 samples, 10,000 x 20,000: 1,266 us in a stream of gradients, 1.30 PFLOP/s at the
-// power cap.  Where it is short, by what a k-block of the term waits for: it takes a stage only once that is free, and its
+// Bound by the tensor cores where the contraction is long: 4,096 samples, 10,000 x 20,000: 1,270 to 1,300 us in a stream of gradients, 1.26 to 1.29 PFLOP/s at
+// the power cap (8,192, 10,000 x 5,000: 640 to 660 us, and 586 by itself, the tensor pipe 86 % busy).  Where it is short, by what a k-block of the term waits for: it takes a stage only once that is free, and its
 // copies, the look at them and the other CTA's word come to 4,500 cycles, of which the stages ahead cover 3,000 (1,024 samples of 64 adapters
-// of 8 ranks, 1,000 x 20,000: 61 us; with a word, and 16 + 3 k-blocks a tile instead of 16 + 5, 57: a tile took 16,000 cycles, 9,700 of them products).
+// of 8 ranks, 1,000 x 20,000: 62 us; with a word, and 16 + 3 k-blocks a tile instead of 16 + 5, 57: a tile took 16,000 cycles, 9,700 of them products).
 //
 // Warps: 0 TMA producer, 1 MMA issuer (leader CTA) and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the columns), 10..13
 // the samples' operand of the term and the loads of its factors, 14..17 the look at them, 18, 19 and, in the other CTA, 1 hand that CTA's on to the leader.
