@@ -344,8 +344,8 @@ int sfb_get_plan(const sfb_config* cfg, int64_t samples, int32_t* product, int32
  *    of 8 entries (rows, cols, n and rank are any size), every such pointer 16-byte aligned; scale, S and ids 4-byte aligned.
  *    The operand copy of W that sfb_get_operand_copy gives (SFB_MLR, bf16 mode) is such a W.  Pitches that are a multiple of 16
  *    entries are the better ones: with others the products of thousands of samples copy their operands into the workspace first.
- *  - On their way into y and dx scale s and scale t are two words of bf16 (2^-16 of that term at most), into dU and dV three.  Results are the same bits from call to call; they may differ in the last
- *    bits with n and with the order of the samples.
+ *  - On their way into y and dx scale s and scale t are two words of bf16 (2^-16 of that term at most), into dU and dV three.  Results
+ *    are the same bits from call to call; they may differ in the last bits with n and with the order of the samples.
  *  - What lies behind the last column of a row, or in rows of other samples and adapters, is neither read into a result nor
  *    written: infinities and NaN in a sample or an adapter reach the results of that sample, or of that adapter's samples, alone.
  *    (Where an infinite factor meets an infinite s or t, the term is NaN.)
