@@ -122,7 +122,7 @@ struct Sorting {
   __device__ __forceinline__ bool on() const { return sorted && *sorted; }
 };
 
-constexpr int kUnit = 8, kUnits = BK / (2 * kUnit); // ranks of a unit of the adapters' term (see Term), units of a k-block of it
+constexpr int kUnit = 8;                             // ranks of a unit of the adapters' term (see Term)
 
 // v = w0 + w1, 2^-16 of v apart: two words of bf16.  (What overflows in the rounding to the first word is cut off instead; of what is not
 // finite there is no rest.)
@@ -397,12 +397,10 @@ __device__ __forceinline__ void store_chunk(__nv_bfloat16* Y, int64_t ldy, int i
 
 // ---------------------------------------------------------------------------------------------------------
 // The adapters' term, scale F[a_i]^T p_i, of the three products below is more contraction behind the k-blocks of A: the factors of the
-// adapters in the tile's list, four units of 8 ranks a k-block, against  scale p  of the samples as two words of bf16 (2^-16 of the term;
-// with one word, and eight units a k-block, the term's rounding was as large as that of the result), with zeros where a sample has another
-// adapter.  (us with one word and with two: 37 samples of 64 adapters of 16 ranks, 10,000 x 20,000, 73.0 and 73.5; 1,024 of 64 of 8, gradients,
-// 1,000 x 20,000, 116.6 and 122.5; 64 of 64 of 64, 10,000 x 5,000, 47.2 and 52.6; where the term is nearly all of the work, 333 of 150 of 128,
-// 9,000 x 1,000, 213 and 301.  Eight units a k-block with a ring of two places for the second words: 303 of the last and 83 of the first; with
-// four, and a stage less for W: 230 of the last, the same or a per cent more of the others.)  Zeros do not hide what is not finite: some warps look
+// adapters in the tile's list, in units of 8 ranks, against  scale p  of the samples as two words of bf16 (2^-16 of the term; with one word
+// its rounding was as large as that of the result), with zeros where a sample has another adapter.  (us with one word and with two: 37 samples of
+// 64 adapters of 16 ranks, 10,000 x 20,000, 75.0 and 75.4; 64 of 32 of 128, 3,000 x 3,000, 28.4 and 32.3; 8,192 of 8 of 64, 10,000 x 5,000, 785
+// and 808; 300 of 32 of 128, 5,000 x 2,000, 83 and 90; gradients of 1,024 of 64 of 8, 1,000 x 20,000, 116.5 and 120.5.)  Zeros do not hide what is not finite: some warps look
 // through the factors in shared memory and replace what is not finite by zeros, and the end of the tile adds those entries alone to their
 // own samples, in fp32.
 // (In fp32 FMAs from global memory, as it was for up to 64 samples, a tile's term is a chain of loads: 64 samples of 8 ranks took 99 us a
@@ -445,9 +443,9 @@ __device__ __forceinline__ Held hold_units(const int32_t* list, int g, int units
   }
   return h;
 }
-template <int WARPS>
+template <int WARPS, int UNITS>
 __device__ __forceinline__ void load_units(uint8_t* st, uint64_t* landed, const CUtensorMap& tmF, const Held& held, int g0, int nu, int boxed, int m0, int w) {
-  constexpr int kMost = kUnits / WARPS;              // copies of a warp, for each of the two panels
+  constexpr int kMost = UNITS / WARPS;              // copies of a warp, for each of the two panels
   int a[kMost], y[kMost];
 #pragma unroll
   for (int i = 0; i < kMost; ++i) {
@@ -470,11 +468,11 @@ __device__ __forceinline__ uint4 lds_v4(uint32_t at) {
   return v;
 }
 // Replaces what is not finite of the factors of `nu` units in a stage by zeros; whether there was anything.  By THREADS threads, t of them.
-template <int THREADS>
+template <int THREADS, int UNITS>
 __device__ __forceinline__ uint32_t clean_units(uint8_t* st, int t, int nu) {
   // bit 15 / 31: the exponent of the low / high half is all ones
   auto found = [](uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; };
-  constexpr int kBatch = 4, kPieces = 2 * kUnits * 64 / THREADS;       // of a thread, in both panels
+  constexpr int kBatch = 4, kPieces = 2 * UNITS * 64 / THREADS;       // of a thread, in both panels
   uint32_t bad = 0;
 #pragma unroll 1
   for (int b = 0; b < kPieces; b += kBatch) {        // (loads first: with a branch behind each of them a block took 1.3 us)
@@ -482,12 +480,12 @@ __device__ __forceinline__ uint32_t clean_units(uint8_t* st, int t, int nu) {
     uint4 v[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      const int i = (b + u) * THREADS + t, panel = i / (kUnits * 64), in = i % (kUnits * 64);
+      const int i = (b + u) * THREADS + t, panel = i / (UNITS * 64), in = i % (UNITS * 64);
       v[u] = lds_v4(smem_u32(st) + panel * (kTileBytesA / 2) + in * 16);
     }
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      const int in = ((b + u) * THREADS + t) % (kUnits * 64);
+      const int in = ((b + u) * THREADS + t) % (UNITS * 64);
       const uint32_t f = found(v[u].x) | found(v[u].y) | found(v[u].z) | found(v[u].w);
       hit |= in < nu * 64 ? f : 0u;
     }
@@ -495,7 +493,7 @@ __device__ __forceinline__ uint32_t clean_units(uint8_t* st, int t, int nu) {
       bad = 1;
 #pragma unroll 1
       for (int u = 0; u < kBatch; ++u) {
-        const int i = (b + u) * THREADS + t, panel = i / (kUnits * 64), in = i % (kUnits * 64);
+        const int i = (b + u) * THREADS + t, panel = i / (UNITS * 64), in = i % (UNITS * 64);
         if (in >= nu * 64) continue;
         const uint32_t at = smem_u32(st) + panel * (kTileBytesA / 2) + in * 16;
         uint4 w = lds_v4(at);
@@ -507,14 +505,17 @@ __device__ __forceinline__ uint32_t clean_units(uint8_t* st, int t, int nu) {
   }
   return bad;
 }
+// Up to 64 samples: both words are one operand, four units a k-block.  (A ring of second words, as for more samples, leaves room for one place
+// of 64 samples: 37 samples of 64 adapters of 16 ranks, 10,000 x 20,000, 75.4 us and 76.0 with it; 64 of 64 of 64, 10,000 x 5,000, 52.5 and 54.4.)
+constexpr int kFewUnits = BK / (2 * kUnit);
 // Row t of the samples' operand of a k-block of `nu` units, first words and then second ones (row: this thread has one), and, beside an odd last unit, zeros in the factors'
 // operand.  By THREADS threads, t of them.
 template <int THREADS>
-__device__ __forceinline__ void write_units(const uint4 (&words)[2 * kUnits], uint8_t* st, int t, bool row, int nu) {
+__device__ __forceinline__ void write_units(const uint4 (&words)[2 * kFewUnits], uint8_t* st, int t, bool row, int nu) {
   if (row) {
     const uint32_t to = smem_u32(st) + kTileBytesA + t * 128;
 #pragma unroll
-    for (int j = 0; j < 2 * kUnits; ++j)
+    for (int j = 0; j < 2 * kFewUnits; ++j)
       asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((j ^ (t & 7)) << 4)), "r"(words[j].x), "r"(words[j].y),
                    "r"(words[j].z), "r"(words[j].w) : "memory");
   }
@@ -523,13 +524,13 @@ __device__ __forceinline__ void write_units(const uint4 (&words)[2 * kUnits], ui
       *reinterpret_cast<uint4*>(st + (x >> 6) * (kTileBytesA / 2) + nu * (kUnit * 128) + (x & 63) * 16) = make_uint4(0, 0, 0, 0);
 }
 // The words of the units [g0, g0 + nu) of a sample whose first unit is `at` (below zero: no adapter): zeros for those that are not its own.
-__device__ __forceinline__ void read_units(const uint4* src, int at, int g0, int nu, int per, uint4 (&words)[2 * kUnits]) {
+__device__ __forceinline__ void read_units(const uint4* src, int at, int g0, int nu, int per, uint4 (&words)[2 * kFewUnits]) {
 #pragma unroll
-  for (int j = 0; j < kUnits; ++j) {
+  for (int j = 0; j < kFewUnits; ++j) {
     const int u = g0 + j - at;
     const bool own = at >= 0 && j < nu && u >= 0 && u < per;
     words[j] = own ? src[2 * u] : make_uint4(0, 0, 0, 0);
-    words[kUnits + j] = own ? src[2 * u + 1] : make_uint4(0, 0, 0, 0);
+    words[kFewUnits + j] = own ? src[2 * u + 1] : make_uint4(0, 0, 0, 0);
   }
 }
 
@@ -578,7 +579,7 @@ __device__ __forceinline__ void few_mma_units(uint32_t st, uint32_t d_tmem, uint
   const uint64_t da = umma_desc_mn128(st), db = umma_desc_k128(st + kTileBytesA);
   for (int j = 0; j < (nu + 1) / 2; ++j) {           // two units each: their first words, their second ones
     umma_bf16(d_tmem, da + 128 * j, db + 2 * j, idesc, 1u);
-    umma_bf16(d_tmem, da + 128 * j, db + kUnits + 2 * j, idesc, 1u);
+    umma_bf16(d_tmem, da + 128 * j, db + kFewUnits + 2 * j, idesc, 1u);
   }
 }
 
@@ -621,10 +622,10 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     }
     pdl_wait();
     const int units = p.term.lists[0] * per;
-    for (int g0 = mine * kUnits; g0 < units && ok; g0 += p.parts * kUnits, next()) {
+    for (int g0 = mine * kFewUnits; g0 < units && ok; g0 += p.parts * kFewUnits, next()) {
       ok = mbar_wait_warp(&empty[s], ph ^ 1, abort_flag);
       if (ok && elect_one()) {
-        mbar_expect_tx(&landed[s], min(kUnits, units - g0) * 2 * kUnit * 128);
+        mbar_expect_tx(&landed[s], min(kFewUnits, units - g0) * 2 * kUnit * 128);
         mbar_arrive(&free_[s]);
       }
     }
@@ -644,12 +645,12 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     }
     pdl_wait();
     const int units = p.term.lists[0] * per;
-    for (int g0 = mine * kUnits; g0 < units && ok; g0 += p.parts * kUnits, next()) {
+    for (int g0 = mine * kFewUnits; g0 < units && ok; g0 += p.parts * kFewUnits, next()) {
       ok = mbar_wait_warp(&built[s], (bph >> s) & 1, abort_flag);
       bph ^= 1u << s;
       tc_fence_after();
       if (ok && elect_one()) {
-        few_mma_units(smem_u32(smem + s * kStage), tmem_base, idesc_f, min(kUnits, units - g0));
+        few_mma_units(smem_u32(smem + s * kStage), tmem_base, idesc_f, min(kFewUnits, units - g0));
         umma_commit(&empty[s]);
       }
     }
@@ -678,21 +679,21 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     const int units = p.term.lists[0] * per, at = writes && t < p.n ? p.term.place[t] * per : -1;
     const uint4* src = p.term.pb + t * per * 2;
     uint32_t s = static_cast<uint32_t>(nk) % p.stages, ph = 0, bad = 0;    // ph: the phases of free_, or of landed, a bit per stage
-    uint4 words[2 * kUnits];
-    if (writes) read_units(src, at, mine * kUnits, min(kUnits, units - mine * kUnits), per, words);
-    for (int g0 = mine * kUnits; g0 < units; g0 += p.parts * kUnits) {
-      const int nu = min(kUnits, units - g0);
+    uint4 words[2 * kFewUnits];
+    if (writes) read_units(src, at, mine * kFewUnits, min(kFewUnits, units - mine * kFewUnits), per, words);
+    for (int g0 = mine * kFewUnits; g0 < units; g0 += p.parts * kFewUnits) {
+      const int nu = min(kFewUnits, units - g0);
       if (!mbar_wait_warp(writes ? &free_[s] : &landed[s], (ph >> s) & 1, abort_flag)) break;
       ph ^= 1u << s;
       uint32_t wrote = 1;
       if (writes) {
-        load_units<kWrite>(smem + s * kStage, &landed[s], tmF, hold_units(p.term.lists, (g0 & ~31) + lane, units, per), g0, nu, p.term.boxed, m0, warp - 6);
+        load_units<kWrite, kFewUnits>(smem + s * kStage, &landed[s], tmF, hold_units(p.term.lists, (g0 & ~31) + lane, units, per), g0, nu, p.term.boxed, m0, warp - 6);
         write_units<32 * kWrite>(words, smem + s * kStage, t, t < TN, nu);
-      } else bad |= wrote = clean_units<32 * kClean>(smem + s * kStage, t, nu);
+      } else bad |= wrote = clean_units<32 * kClean, kFewUnits>(smem + s * kStage, t, nu);
       if (wrote) fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&built[s]);
-      if (writes) read_units(src, at, g0 + p.parts * kUnits, min(kUnits, units - g0 - p.parts * kUnits), per, words);
+      if (writes) read_units(src, at, g0 + p.parts * kFewUnits, min(kFewUnits, units - g0 - p.parts * kFewUnits), per, words);
       if (++s == static_cast<uint32_t>(p.stages)) s = 0;
     }
     if (bad) odd = 1;
@@ -744,18 +745,37 @@ adapter_few_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // its TMEM; it loads its own rows and its half of the samples, 32 KB a k-block.  Two accumulators: the end of a tile runs beside the next
 // one's products.  Whole rounds of tiles are taken whole, the k-blocks of the rest are shared out (Segments in sfb_tile.cuh); the pair that
 // finishes a tile has its term.
-// Bound by the tensor cores where the contraction is long: 4,096 samples, 10,000 x 20,000: 1,270 to 1,300 us in a stream of gradients, 1.26 to 1.29 PFLOP/s at
-// the power cap (8,192, 10,000 x 5,000: 640 to 660 us, and 586 by itself, the tensor pipe 86 % busy).  Where it is short, by what a k-block of the term waits for: it takes a stage only once that is free, and its
-// copies, the look at them and the other CTA's word come to 4,500 cycles, of which the stages ahead cover 3,000 (1,024 samples of 64 adapters
-// of 8 ranks, 1,000 x 20,000: 62 us; with a word, and 16 + 3 k-blocks a tile instead of 16 + 5, 57: a tile took 16,000 cycles, 9,700 of them products).
+// Bound by the tensor cores where the contraction is long: 4,096 samples, 10,000 x 20,000: 1,260 to 1,340 us in a stream of gradients, 1.22 to
+// 1.30 PFLOP/s at the power cap (8,192, 10,000 x 5,000: 640 to 710 us, and 592 by itself, the tensor pipe 83 % busy).  Where it is short, by what a
+// k-block of the term waits for: it takes a stage only once that is free, and its copies, the look at them and the other CTA's word come to
+// 4,500 cycles, of which the stages ahead cover 2,500 (1,024 samples of 64 adapters of 8 ranks, 1,000 x 20,000: 61 us for 4.3 rounds of tiles of
+// 16 + 3 k-blocks; with one word 57, 16,000 cycles a tile, 9,700 of them products).
 //
 // Warps: 0 TMA producer, 1 MMA issuer (leader CTA) and TMEM owner, 2..9 epilogue (TMEM lane quarter q, half h of the columns), 10..13
 // the samples' operand of the term and the loads of its factors, 14..17 the look at them, 18, 19 and, in the other CTA, 1 hand that CTA's on to the leader.
 // ---------------------------------------------------------------------------------------------------------
 constexpr int kPairBuild = 4, kHand = 3, kPairThreads = 32 * (2 + kEpi + 2 * kPairBuild + kHand - 1), kGroup = 8;      // kGroup: tiles of samples that follow one another
-constexpr int kPairStages = 6, kPairStage = 2 * kTileBytesA;
-constexpr int kPairHeld = 2 * kUnits;               // units of its row of pb that a writing thread has at hand, behind the stages
-constexpr int kPairSmem = kPairStages * kPairStage + 128 * kPairHeld * 32 + 1024;
+constexpr int kPairUnits = BK / kUnit;              // units of a k-block of the term: their first words in its stage, the second ones in a ring
+// Operand stages, and places of the ring of second words behind them.  (With both words in one stage, four units a k-block, six stages, half of
+// the factors' places are empty, and as many fewer factors are under way: 333 samples of 150 adapters of 128 ranks, 9,000 x 1,000, 301 us, here
+// 221; 300 of 32 of 128, 5,000 x 2,000, 109 and 90; 700 of 16 of 32, 4,000 x 4,000, 56.7 and 57.1; long contractions the same.  14 single places, of
+// which k-blocks take two or three: long contractions 7 % longer.)
+constexpr int kPairStages = 5, kPairStage = 2 * kTileBytesA, kPairSecond = 4;
+constexpr int kPairSmem = kPairStages * kPairStage + kPairSecond * kTileBytesA + 1024;
+// The words of the units [g0, g0 + nu) of a sample whose first unit is `at` (below zero: no adapter), zeros for those that are not its own, to
+// row t of two operands: by copies of this thread, which make zeros without reading.  (With a number of bytes that is zero instead: 99 us of the 90
+// above, 146 of the 135 of 150 samples of 128 adapters of 32 ranks, 20,000 x 3,000.)
+__device__ __forceinline__ void copy_words(uint32_t first, uint32_t second, int t, const uint4* src, int at, int g0, int nu, int per) {
+#pragma unroll
+  for (int j = 0; j < kPairUnits; ++j) {
+    const int u = g0 + j - at;
+    const bool own = at >= 0 && j < nu && u >= 0 && u < per;
+    const uint4* from = own ? src + 2 * u : src;
+    const uint32_t to = t * 128 + ((j ^ (t & 7)) << 4);
+    cp_async_16_or_zero(first + to, from, own);
+    cp_async_16_or_zero(second + to, from + 1, own);
+  }
+}
 constexpr int kPartFloats = BM * kMaxTile;          // what a CTA leaves of a tile
 struct PairParams {
   Term term;
@@ -797,6 +817,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   __shared__ uint64_t free_[kPairStages], built[kPairStages];      // of a k-block of factors: the stage is free for the samples' operand;
                                                                    // this CTA has its operands
   __shared__ uint64_t landed[kPairStages], joined[kPairStages];    // its factors are here; the leader's: the other CTA has built its operands
+  __shared__ uint64_t second[kPairSecond];                         // a place for second words is free
   __shared__ uint64_t tfull[2], tempty[2], looked[2], taken[2];    // looked: whether factors of a tile were not finite is known; taken: read
   __shared__ uint32_t tmem_slot, abort_word, odd[2][kPairBuild];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -824,10 +845,11 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       int m0, tt;
       tile_coords(sg.tile, m0, tt);
       s = (s + sg.k1 - sg.k0) % kPairStages;
-      for (int left = sg.k1 == p.kseg ? p.term.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0; left > 0 && ok; left -= kUnits) {
+      for (int left = sg.k1 == p.kseg ? p.term.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0; left > 0 && ok; left -= kPairUnits) {
         if (static_cast<int>(s % kHand) == h) {
           ok = mbar_wait_warp(&built[s], (bph >> s) & 1, abort_flag);
           bph ^= 1u << s;
+          fence_proxy_async_smem();                  // the words are generic writes
           if (ok && lane == 0) mbar_arrive_cluster(mapa_u32(smem_u32(&joined[s]), 0));
         }
         if (++s == static_cast<uint32_t>(kPairStages)) s = 0;
@@ -837,9 +859,10 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kPairStages; ++i) {
-      mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&landed[i], 1); mbar_init(&built[i], 2 * kPairBuild);
-      mbar_init(&joined[i], 1);
+      mbar_init(&full[i], 1); mbar_init(&empty[i], 1); mbar_init(&free_[i], 1); mbar_init(&landed[i], 1); mbar_init(&joined[i], 1);
+      mbar_init(&built[i], 33 * kPairBuild);         // the threads that write words, the warps that look
     }
+    for (int i = 0; i < kPairSecond; ++i) mbar_init(&second[i], 1);
     for (int i = 0; i < 2; ++i) { mbar_init(&tfull[i], 1); mbar_init(&tempty[i], 2 * kEpi); mbar_init(&looked[i], kPairBuild); mbar_init(&taken[i], kEpi); }
     abort_word = 0;
     fence_barrier_init();
@@ -886,10 +909,10 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         }
       };
       loads(sg.k0, sg.k1);
-      const int units = count * per, more = (units + kUnits - 1) / kUnits;
+      const int units = count * per, more = (units + kPairUnits - 1) / kPairUnits;
       for (int k = 0; k < more && ok; ++k) {
         if (!mbar_wait_warp(&empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
-        const int nu = min(kUnits, units - k * kUnits);
+        const int nu = min(kPairUnits, units - k * kPairUnits);
         if (elect_one()) {
           mbar_expect_tx(&landed[s], nu * 2 * kUnit * 128);
           mbar_arrive(&free_[s]);
@@ -901,7 +924,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     // ---------------- MMA issuer ----------------
     if (rank == 0) {
       const uint32_t idesc = umma_idesc_bf16(2 * BM, p.tn) | (MN ? 1u << 15 : 0u), idesc_f = umma_idesc_bf16(2 * BM, p.tn) | 1u << 15;
-      uint32_t s = 0, fph = 0, bph = 0;              // the phases of full and of built, a bit per stage
+      uint32_t s = 0, l = 0, fph = 0, bph = 0;       // stage, place of second words; the phases of full and of built, a bit per stage
       bool ok = true;
       for (int i = 0; i < segs.n && ok; ++i) {
         const Segment sg = segs.get(i);
@@ -924,20 +947,24 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
           }
           if (++s == static_cast<uint32_t>(kPairStages)) s = 0;
         }
-        for (int left = count * per; left > 0 && ok; left -= kUnits) {
+        for (int left = count * per; left > 0 && ok; left -= kPairUnits) {
           if (!mbar_wait_warp(&built[s], (bph >> s) & 1, abort_flag) || !mbar_wait_cluster(&joined[s], (bph >> s) & 1, abort_flag)) { ok = false; break; }
           bph ^= 1u << s;
+          fence_proxy_async_smem();                  // the words are generic writes; the other CTA's are fenced where they are handed on
           tc_fence_after();
-          const int ns = (min(kUnits, left) + 1) / 2;                  // two units each: of their first words, of their second ones
+          const int ns = (min(kPairUnits, left) + 1) / 2;                  // two units each: of their first words, of their second ones
           if (elect_one()) {
             const uint32_t st = smem_u32(smem + s * kPairStage);
             const uint64_t da = umma_desc_mn128(st), db = umma_desc_k128(st + kTileBytesA);
+            const uint64_t dl = umma_desc_k128(smem_u32(smem + kPairStages * kPairStage + l * kTileBytesA));
             for (int j = 0; j < ns; ++j) {
               umma_bf16_pair(d_tmem, da + 128 * j, db + 2 * j, idesc_f, 1u);
-              umma_bf16_pair(d_tmem, da + 128 * j, db + kUnits + 2 * j, idesc_f, 1u);
+              umma_bf16_pair(d_tmem, da + 128 * j, dl + 2 * j, idesc_f, 1u);
             }
             umma_commit_pair(&empty[s], 3);
+            umma_commit_pair(&second[l], 3);
           }
+          if (++l == kPairSecond) l = 0;
           if (++s == static_cast<uint32_t>(kPairStages)) s = 0;
         }
         if (ok && elect_one()) umma_commit_pair(&tfull[a], 3);
@@ -1019,16 +1046,15 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
   } else if (warp >= 2 + kEpi + 2 * kPairBuild) {
     // ---------------- hand on the other CTA's operands ----------------
     // (1,024 samples, 1,000 x 20,000, eight k-blocks of the term a tile: 98 us with releases by each of the eight warps that make the operands, 89
-    // with one warp that hands all on, 76 with two in turn.  333 samples of 150 adapters of 128 ranks, 9,000 x 1,000: 351 with two in turn,
-    // 311 with two by stages, 300 with three.)
+    // with one warp that hands all on, 76 with two in turn.  With both words in one stage, 333 samples of 150 adapters of 128 ranks, 9,000 x 1,000:
+    // 351 with two in turn, 311 with two by stages, 300 with three.)
     if (rank == 1) hand_on(warp - 2 - kEpi - 2 * kPairBuild);
   } else {
     // ---------------- the samples' operand of the term, and its factors ----------------
     const bool writes = warp < 2 + kEpi + kPairBuild;
     const int w = warp - 2 - kEpi - (writes ? 0 : kPairBuild), t = w * 32 + lane;    // this thread's sample of the CTA's half of the tile, or
     uint32_t s = 0, ph = 0;                          // share of the factors; ph: the phases of free_, or of landed, a bit per stage
-    const uint32_t mine = smem_u32(smem + kPairStages * kPairStage) + t * (kPairHeld * 32);
-    auto held_at = [&](int u, int w) { return mine + (((u % kPairHeld) * 2 + w) ^ (t & 15)) * 16; };
+    uint32_t l = 0, lph = 0;                         // place of second words, and phase
     bool ok = true;
     for (int i = 0; i < segs.n && ok; ++i) {
       const Segment sg = segs.get(i);
@@ -1038,46 +1064,33 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
       const int units = sg.k1 == p.kseg ? p.term.lists[static_cast<int64_t>(tt) * kListPitch] * per : 0;
       const int smp = tt * p.tn + static_cast<int>(rank) * half + t;
       const int at = writes && t < half && smp < p.n ? p.term.place[smp] * per : -1;   // this sample's first unit
-      const uint4* src = p.term.pb + static_cast<int64_t>(smp) * per * 2;
+      const uint4* src = p.term.pb + (at >= 0 ? static_cast<int64_t>(smp) * per * 2 : 0);
       const uint32_t a = i & 1, aph = (i >> 1) & 1;
       const int32_t* list = p.term.lists + static_cast<int64_t>(tt) * kListPitch;
       Held held = hold_units(list, lane, writes ? units : 0, per);
-      // a thread's own units come to shared memory two k-blocks ahead, those of the first two while the k-blocks of A are under way
-      auto fetch = [&](int g0) {
-        for (int g = max(g0, at); at >= 0 && g < min(g0 + kUnits, at + per); ++g) {
-          cp_async_16(held_at(g, 0), src + 2 * (g - at), 16);
-          cp_async_16(held_at(g, 1), src + 2 * (g - at) + 1, 16);
-        }
-        cp_async_commit();
-      };
-      if (writes) {
-        if (units > 0) { fetch(0); fetch(kUnits); }
-      } else if (!mbar_wait_warp(&taken[a], aph ^ 1, abort_flag)) break;
+      if (!writes && !mbar_wait_warp(&taken[a], aph ^ 1, abort_flag)) break;
       uint32_t bad = 0;
-      for (int g0 = 0; g0 < units; g0 += kUnits) {
-        const int nu = min(kUnits, units - g0);
+      for (int g0 = 0; g0 < units; g0 += kPairUnits) {
+        const int nu = min(kPairUnits, units - g0);
         uint8_t* st = smem + s * kPairStage;
         if (!mbar_wait_warp(writes ? &free_[s] : &landed[s], (ph >> s) & 1, abort_flag)) { ok = false; break; }
         ph ^= 1u << s;
-        uint32_t wrote = 1;
         if (writes) {
-          load_units<kPairBuild>(st, &landed[s], tmF, held, g0, nu, p.term.boxed, m0, w);
-          cp_async_wait_group<1>();
-          uint4 words[2 * kUnits];
-#pragma unroll
-          for (int j = 0; j < kUnits; ++j) {
-            const int u = g0 + j - at;
-            const bool own = at >= 0 && j < nu && u >= 0 && u < per;
-            words[j] = own ? lds_v4(held_at(g0 + j, 0)) : make_uint4(0, 0, 0, 0);
-            words[kUnits + j] = own ? lds_v4(held_at(g0 + j, 1)) : make_uint4(0, 0, 0, 0);
-          }
-          write_units<32 * kPairBuild>(words, st, t, t < half, nu);
-          fetch(g0 + 2 * kUnits);
-          if (((g0 + kUnits) & 31) == 0) held = hold_units(list, g0 + kUnits + lane, units, per);
-        } else bad |= wrote = clean_units<32 * kPairBuild>(st, t, nu);
-        if (wrote) fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&built[s]);
+          load_units<kPairBuild, kPairUnits>(st, &landed[s], tmF, held, g0, nu, p.term.boxed, m0, w);
+          if (!mbar_wait_warp(&second[l], lph ^ 1, abort_flag)) { ok = false; break; }
+          if (t < half) copy_words(smem_u32(st) + kTileBytesA, smem_u32(smem + kPairStages * kPairStage + l * kTileBytesA), t, src, at, g0, nu, per);
+          if (nu & 1)                                // beside an odd last unit, zeros in the factors' operand
+            cp_async_16(smem_u32(st) + (t >> 6) * (kTileBytesA / 2) + nu * (kUnit * 128) + (t & 63) * 16, src, 0);
+          cp_async_arrive(&built[s]);                // (the copies arrive by themselves)
+          if (++l == kPairSecond) { l = 0; lph ^= 1; }
+          if (((g0 + kPairUnits) & 31) == 0) held = hold_units(list, g0 + kPairUnits + lane, units, per);
+        } else {
+          const uint32_t wrote = clean_units<32 * kPairBuild, kPairUnits>(st, t, nu);
+          bad |= wrote;
+          if (wrote) fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&built[s]);
+        }
         if (++s == static_cast<uint32_t>(kPairStages)) s = 0;
       }
       bad = __any_sync(0xffffffffu, bad);
@@ -1086,7 +1099,7 @@ adapter_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         mbar_arrive(&looked[a]);
       }
     }
-    cp_async_wait_group<0>();
+    cp_async_wait_all();
   }
 
   // ---------------- teardown ----------------
@@ -1969,8 +1982,9 @@ struct sfb_adapters {
   cudaStream_t stream;
   int device, last_cuda, max_pairs;
   CUtensorMap mapU, mapV;              // boxes of 64 entries x `boxed_slices` times 16 ranks of an adapter
-  CUtensorMap unitU, unitV;            // x `boxed` units of 8 ranks
-  int32_t boxed, boxed_slices;
+  CUtensorMap unitU, unitV;            // x `boxed` units of 8 ranks,
+  CUtensorMap fewU, fewV;              // `boxed_few` of them
+  int32_t boxed, boxed_few, boxed_slices;
   sfb::EncodeTiledFn encode;           // cuTensorMapEncodeTiled
 
   template <typename T>
@@ -2140,9 +2154,10 @@ cudaError_t few(sfb_adapters* h, int64_t n, const void* Z, int64_t ldz, const Te
   if (!operand_map(h, &ma, h->W, c.cols, c.rows, c.ldw, BK, MN ? BK : BM, CU_TENSOR_MAP_L2_PROMOTION_L2_256B) ||
       !operand_map(h, &mz, Z, d, n, ldz, BK, TN, CU_TENSOR_MAP_L2_PROMOTION_L2_256B))
     return cudaErrorInvalidValue;
-  const CUtensorMap& mf = MN ? h->unitV : h->unitU;
+  const CUtensorMap& mf = MN ? h->fewV : h->fewU;
   FewParams p{};
   p.term = term;
+  p.term.boxed = h->boxed_few;
   p.n = static_cast<int32_t>(n); p.m = static_cast<int32_t>(m);
   p.kseg = static_cast<int32_t>((d + BK - 1) / BK);
   p.Y = static_cast<__nv_bfloat16*>(Y); p.ldy = ldy; p.status = h->at<uint32_t>(h->lay.status);
@@ -2326,9 +2341,11 @@ extern "C" int sfb_adapter_init(const sfb_adapter_config* cfg, const void* W_dev
   h->max_pairs = std::min(sm_count(), kModelSms) / 2;
   h->boxed = h->boxed_slices = 1;
   while (h->boxed_slices < 8 && (c.rank + kSlice - 1) / kSlice % (2 * h->boxed_slices) == 0) h->boxed_slices *= 2;
-  while (h->boxed < kUnits && (c.rank + kUnit - 1) / kUnit % (2 * h->boxed) == 0) h->boxed *= 2;
+  while (h->boxed < kPairUnits && (c.rank + kUnit - 1) / kUnit % (2 * h->boxed) == 0) h->boxed *= 2;
+  h->boxed_few = std::min(h->boxed, kFewUnits);
   if (!factor_map(h, &h->mapU, U_dev, c.rows, c.ldu, kSlice * h->boxed_slices) || !factor_map(h, &h->mapV, V_dev, c.cols, c.ldv, kSlice * h->boxed_slices) ||
       !factor_map(h, &h->unitU, U_dev, c.rows, c.ldu, kUnit * h->boxed) || !factor_map(h, &h->unitV, V_dev, c.cols, c.ldv, kUnit * h->boxed) ||
+      !factor_map(h, &h->fewU, U_dev, c.rows, c.ldu, kUnit * h->boxed_few) || !factor_map(h, &h->fewV, V_dev, c.cols, c.ldv, kUnit * h->boxed_few) ||
       prepare_pair_kernel(adapter_pair_kernel<false>, kPairThreads, kPairSmem, &h->max_pairs) != cudaSuccess ||
       prepare_pair_kernel(adapter_pair_kernel<true>, kPairThreads, kPairSmem, &h->max_pairs) != cudaSuccess || h->max_pairs < 1 ||
       cudaMemsetAsync(h->ws + lay.status, 0, lay.s - lay.status, h->stream) != cudaSuccess) {

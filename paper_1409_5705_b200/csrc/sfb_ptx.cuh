@@ -138,14 +138,19 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* m, int
 __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
+// All 16 bytes, or, where not `wanted`, zeros.
+__device__ __forceinline__ void cp_async_16_or_zero(uint32_t dst, const void* src, bool wanted) {
+  asm volatile(
+      "{\n\t"
+      ".reg .pred P;\n\t"
+      "setp.eq.u32 P, %2, 0;\n\t"
+      "cp.async.cg.shared.global [%0], [%1], 16, P;\n\t"
+      "}\n" ::"r"(dst), "l"(src), "r"(static_cast<uint32_t>(wanted)) : "memory");
+}
 // Arrives on the barrier once all copies that this thread has issued have landed.
 __device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
-// A thread's copies in groups; waits until no more than N of its groups are under way.
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait_group() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // 2-D tiled store shared -> global (bulk group).
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* m, const void* src, int32_t x, int32_t y) {

@@ -9,10 +9,10 @@ from test_gpu_adapters import Case, check
 pytestmark = pytest.mark.gpu
 
 
-@pytest.mark.parametrize("cols", [320, 200, 700])
+@pytest.mark.parametrize("cols", [320, 200, 576])
 def test_the_term_in_the_same_stage_of_tile_after_tile(cols):
-    """One k-block of the adapters' term a tile, behind five of W (six stages: always the same one), four or eleven: the two warps that hand
-    the other CTA's operands on see every phase of that stage.  Many tiles a pair of CTAs, many calls; no wait may run out."""
+    """One k-block of the adapters' term a tile, behind five, four or nine of W, so that it is always in the same one of five or six stages: the
+    warps that hand the other CTA's operands on see every phase of it.  Many tiles a pair of CTAs, many calls; no wait may run out."""
     c = Case(6000, 3000, cols, 1, 8, "one", seed=cols)
     Y = torch.zeros(c.n, c.rows, dtype=torch.bfloat16, device="cuda")
     Sx = torch.zeros(c.n, c.rank, device="cuda")
