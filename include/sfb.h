@@ -74,7 +74,8 @@ enum sfb_error {
 #define SFB_STATUS_SAMPLE_RANGE 0x4u   /* SDCA: a sample id outside [0, sdca_n) was skipped */
 #define SFB_STATUS_ADAPTER_RANGE 0x10u /* an adapter id outside [-1, adapters): the sample took none */
 #define SFB_STATUS_INDEX_RANGE 0x8u    /* sparse samples: a column index outside [0, cols), or row pointers that do not
-                                          describe the stated number of entries; the entry or the sample was skipped */
+                                          describe the stated number of entries; the entry or the sample was skipped.
+                                          Lookup: a token id outside [-1, tokens); the sample took none */
 
 typedef struct sfb_config {
   int32_t model;          /* enum sfb_model                                                            */
@@ -389,6 +390,95 @@ int sfb_adapter_get_status(sfb_adapters* h, uint32_t* status_out);
 int sfb_adapter_last_cuda_error(sfb_adapters* h);
 int sfb_adapter_destroy(sfb_adapters* h);
 
+/* ---- Samples from token ids, and dropout ------------------------------------------------------------------------------------
+ * Samples need not come as features: those of a text are rows of a table E [tokens x dim], one a token, and the table is learnt as W is.
+ * Its gradient is a sum of sufficient factors whose u is one-hot, so it is the rows of dX summed by token:
+ *   lookup     X_i   = scale * m_i * E[ids_i]                       (* by entries)
+ *   gradient   dE[t] = alpha * scale * sum_{i: ids_i = t} m_i * dX_i
+ * with a dropout m (below) or without one (m = 1).  ids_dev int32; -1: no token (zeros in X, no part of dE).  An id outside
+ * [-1, tokens) sets SFB_STATUS_INDEX_RANGE and counts as -1.
+ *
+ *  - E is fp32, bf16 or fp16, X and dX of another of these or the same; dE fp32.  Any pitch >= dim, pointers aligned to their entries
+ *    (rows that all start on 16-byte boundaries are the faster ones).  Products are rounded once, to X's type; sums are fp32.
+ *  - dE is written whole, zeros for tokens without a sample; or, with add = 1, the sums are added to the rows of the tokens that
+ *    some sample names, and the other rows are not touched: with alpha = -eta and dE = the fp32 table itself that is its step.
+ *  - The samples are taken in the order of their tokens, those of a token in their own order: results are the same bits from call to
+ *    call.  They may differ in the last bits with n.
+ *  - The handle borrows E (its values may change between calls) and the workspace.  One handle per stream; calls on one handle are not
+ *    re-entrant, and graphs that were captured from one handle run one after another.  n = 0 .. max_ids.  X does not overlap E, nor dE dX.
+ *
+ * Dropout: m_ij = 65536 / (65536 - t) where entry (i, j) is kept, else 0 (whatever the entry is, NaN too), t = round(65536 p): the mean
+ * of m is 1 for the t that is used.  Which are kept is a function of (seed, offset, i, j) alone, by the counter-based generator Philox4x32-10
+ * (Salmon, Moraes, Dror and Shaw, 2011): key (seed low, seed high), counter (j / 8, i, offset low, offset high), of whose four words entry j takes
+ * the low (j even) or high 16 bits of word (j mod 8) / 2; it is kept where they are >= t.  No mask is stored: the backward pass
+ * makes it again.  rng_dev (two uint64 in device memory, borrowed) holds the seed and the offset's base, to which a call adds `call`:
+ * captured graphs take new masks from replay to replay where the caller moves rng_dev[1] on in between, and layers of one step
+ * their own by `call`.  (i and j count from 0 in each call: rows beyond 2^32 and columns beyond 2^30 are refused.) */
+typedef struct sfb_dropout sfb_dropout;
+enum sfb_dtype { SFB_F32 = 0, SFB_BF16 = 1, SFB_F16 = 2 };
+/* p in [0, 1]; 1: nothing is kept. */
+int sfb_dropout_init(float p, const uint64_t* rng_dev, void* stream, sfb_dropout** out);
+/* y = m * x + r (R_dev may be null: y = m * x), all of dtype, rounded once.  Y_dev may be X_dev or R_dev (with its pitch); no other overlap.
+ * The backward pass of x is the same call for dy, with no r; that of r is dy itself. */
+int sfb_dropout_apply(sfb_dropout* h, uint64_t call, int64_t n, int64_t cols, int32_t dtype, const void* X_dev, int64_t ldx,
+                      const void* R_dev, int64_t ldr, void* Y_dev, int64_t ldy);
+int sfb_dropout_last_cuda_error(sfb_dropout* h);
+int sfb_dropout_destroy(sfb_dropout* h);
+
+typedef struct sfb_embed sfb_embed;
+typedef struct sfb_embed_config {
+  int64_t tokens, dim;        /* shape of E, up to 2^30 x 2^24                                         */
+  int64_t ldt;                /* row pitch of E in entries; 0: dim                                     */
+  int32_t table_dtype;        /* enum sfb_dtype                                                        */
+  int32_t out_dtype;          /* of X and dX                                                           */
+  float   scale;
+  int64_t max_ids;            /* of a call, up to 2^26                                                 */
+  void*   stream;             /* cudaStream_t                                                          */
+} sfb_embed_config;
+/* Bytes of device workspace of a handle.  Host-only; no CUDA call. */
+int sfb_embed_workspace_bytes(const sfb_embed_config* cfg, size_t* out_bytes);
+/* workspace_dev: 1024-byte aligned.  Clears the status word (enqueued). */
+int sfb_embed_init(const sfb_embed_config* cfg, const void* table_dev, void* workspace_dev, size_t workspace_bytes, sfb_embed** out);
+/* drop may be null; of its handle the calls take p and rng_dev, not the stream. */
+int sfb_embed_forward(sfb_embed* h, int64_t n, const int32_t* ids_dev, void* X_dev, int64_t ldx, const sfb_dropout* drop, uint64_t call);
+int sfb_embed_backward(sfb_embed* h, int64_t n, const int32_t* ids_dev, const void* dX_dev, int64_t lddx, const sfb_dropout* drop,
+                       uint64_t call, float alpha, int32_t add, float* dE_dev, int64_t ldde);
+/* As sfb_get_status, sfb_last_cuda_error and sfb_destroy. */
+int sfb_embed_get_status(sfb_embed* h, uint32_t* status_out);
+int sfb_embed_last_cuda_error(sfb_embed* h);
+int sfb_embed_destroy(sfb_embed* h);
+
+/* ---- Answers: a class drawn for each row of logits -----------------------------------------------------------------------------
+ * For row i of Z [n x classes] (what sfb_adapter_forward gives, or any logits), with its largest logit m and a random number u_i from [0, 1):
+ *   weights       w_j = exp((z_j - m) / temperature_i)
+ *   top-k         of the order by falling logit and rising index the first top_k_i
+ *   top-p         of these the shortest beginning whose weights come to top_p_i of theirs
+ *   min-p         of these the ones with w_j >= min_p_i
+ *   the draw      the first class, by rising index, up to and with which the weights of what is kept come to more than u_i of theirs
+ * ids_dev[i] = the class; logp_dev[i] (may be null) = log of its share of the kept weights; kept_dev[i] (may be null) = how many were kept.
+ *
+ *  - Per row, each array may be null (filter off, temperature 1): temperature <= 0 or NaN: the largest logit, the first one of equals
+ *    (log-probability 0, one kept); +infinity: all logits above -infinity alike.  top_k <= 0: off.  top_p >= 1 or NaN: off; <= 0: the first of
+ *    the order.  min_p is taken into [0, 1] (NaN: 0).  u outside [0, 1) is taken to the next end (NaN: 0).
+ *  - A logit of -infinity, or one that is not a number, is no class: it is neither kept nor drawn.  A row of such ones has ids = -1,
+ *    logp = -infinity, kept = 0.  Where logits are +infinity, these alone have weight, 1 each.  Weights below e^-45 count as 0: such classes
+ *    are kept where the filters say so, but not drawn.
+ *  - Weights and their sums are in 64 bits, and the same from call to call; logp is rounded to fp32 at its end.
+ *  - Z of dtype, any pitch ldz >= classes, aligned to its entries (rows on 16-byte boundaries are the faster ones); the arrays are contiguous.
+ *    n = 0 .. max_samples.  Calls on one handle are not re-entrant. */
+typedef struct sfb_sampler sfb_sampler;
+typedef struct sfb_sampler_config {
+  int64_t classes;            /* up to 2^30                                                            */
+  int64_t max_samples;        /* of a call, up to 2^27                                                 */
+  int32_t dtype;              /* of Z: enum sfb_dtype                                                  */
+  void*   stream;             /* cudaStream_t                                                          */
+} sfb_sampler_config;
+int sfb_sampler_init(const sfb_sampler_config* cfg, sfb_sampler** out);
+int sfb_sample(sfb_sampler* h, int64_t n, const void* Z_dev, int64_t ldz, const float* u_dev, const float* temperature_dev,
+               const int32_t* top_k_dev, const float* top_p_dev, const float* min_p_dev, int32_t* ids_dev, float* logp_dev, int32_t* kept_dev);
+int sfb_sampler_last_cuda_error(sfb_sampler* h);
+int sfb_sampler_destroy(sfb_sampler* h);
+
 /* ---- Global norm of gradients, and clipping -----------------------------------------------------------------------------
  * The column prox bounds the norm of a column of W; this bounds the norm of a whole step: with the tensors g_1 .. g_m taken as one
  * vector,
@@ -406,7 +496,6 @@ int sfb_adapter_destroy(sfb_adapters* h);
  *  - Gradients that lie on several GPUs: sfb_clip_sum writes this handle's sum of squares to sum_dev (fp64), the caller adds those
  *    of all ranks, and sfb_clip_scale takes the total.  sfb_clip_gradients is both. */
 typedef struct sfb_clip sfb_clip;
-enum sfb_dtype { SFB_F32 = 0, SFB_BF16 = 1, SFB_F16 = 2 };
 int sfb_clip_workspace_bytes(int64_t tensors, const int64_t* counts, const int32_t* dtypes, size_t* out_bytes);
 int sfb_clip_init(int64_t tensors, const void* const* src, void* const* dst, const int64_t* counts, const int32_t* dtypes,
                   void* workspace_dev, size_t workspace_bytes, void* stream, sfb_clip** out);

@@ -29,7 +29,11 @@ EXPORTS = ("sfb_workspace_bytes", "sfb_init", "sfb_compute_factors", "sfb_gather
            "sfb_adapter_workspace_bytes", "sfb_adapter_init", "sfb_adapter_forward", "sfb_adapter_backward",
            "sfb_adapter_get_plan", "sfb_adapter_get_status", "sfb_adapter_last_cuda_error", "sfb_adapter_destroy",
            "sfb_clip_workspace_bytes", "sfb_clip_init", "sfb_clip_sum", "sfb_clip_scale", "sfb_clip_gradients",
-           "sfb_clip_last_cuda_error", "sfb_clip_destroy")
+           "sfb_clip_last_cuda_error", "sfb_clip_destroy",
+           "sfb_dropout_init", "sfb_dropout_apply", "sfb_dropout_last_cuda_error", "sfb_dropout_destroy",
+           "sfb_embed_workspace_bytes", "sfb_embed_init", "sfb_embed_forward", "sfb_embed_backward", "sfb_embed_get_status",
+           "sfb_embed_last_cuda_error", "sfb_embed_destroy",
+           "sfb_sampler_init", "sfb_sample", "sfb_sampler_last_cuda_error", "sfb_sampler_destroy")
 NOALLOC_MAX_COLS = 16384
 ADAPTER_MAX_RANK = 128
 
@@ -56,6 +60,15 @@ class sfb_adapter_config(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ldw", ctypes.c_int64), ("ldu", ctypes.c_int64),
                 ("ldv", ctypes.c_int64), ("adapters", ctypes.c_int32), ("rank", ctypes.c_int32),
                 ("max_samples", ctypes.c_int64), ("stream", ctypes.c_void_p)]
+
+
+class sfb_embed_config(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("dim", ctypes.c_int64), ("ldt", ctypes.c_int64), ("table_dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("max_ids", ctypes.c_int64), ("stream", ctypes.c_void_p)]
+
+
+class sfb_sampler_config(ctypes.Structure):
+    _fields_ = [("classes", ctypes.c_int64), ("max_samples", ctypes.c_int64), ("dtype", ctypes.c_int32), ("stream", ctypes.c_void_p)]
 
 
 class SfbError(RuntimeError):
@@ -128,6 +141,23 @@ def lib() -> ctypes.CDLL:
         L.sfb_clip_gradients.argtypes = [vp, ctypes.c_float, vp]
         L.sfb_clip_last_cuda_error.argtypes = [vp]
         L.sfb_clip_destroy.argtypes = [vp]
+        u64, f32 = ctypes.c_uint64, ctypes.c_float
+        L.sfb_dropout_init.argtypes = [f32, vp, vp, ctypes.POINTER(vp)]
+        L.sfb_dropout_apply.argtypes = [vp, u64, i64, i64, i32, vp, i64, vp, i64, vp, i64]
+        L.sfb_dropout_last_cuda_error.argtypes = [vp]
+        L.sfb_dropout_destroy.argtypes = [vp]
+        ecfgp, scfgp = ctypes.POINTER(sfb_embed_config), ctypes.POINTER(sfb_sampler_config)
+        L.sfb_embed_workspace_bytes.argtypes = [ecfgp, ctypes.POINTER(ctypes.c_size_t)]
+        L.sfb_embed_init.argtypes = [ecfgp, vp, vp, ctypes.c_size_t, ctypes.POINTER(vp)]
+        L.sfb_embed_forward.argtypes = [vp, i64, vp, vp, i64, vp, u64]
+        L.sfb_embed_backward.argtypes = [vp, i64, vp, vp, i64, vp, u64, f32, i32, vp, i64]
+        L.sfb_embed_get_status.argtypes = [vp, ctypes.POINTER(ctypes.c_uint32)]
+        L.sfb_embed_last_cuda_error.argtypes = [vp]
+        L.sfb_embed_destroy.argtypes = [vp]
+        L.sfb_sampler_init.argtypes = [scfgp, ctypes.POINTER(vp)]
+        L.sfb_sample.argtypes = [vp, i64, vp, i64] + [vp] * 8
+        L.sfb_sampler_last_cuda_error.argtypes = [vp]
+        L.sfb_sampler_destroy.argtypes = [vp]
         for name in EXPORTS:
             if name != "sfb_strerror":
                 getattr(L, name).restype = ctypes.c_int
@@ -575,6 +605,176 @@ class GradientClip:
             self.close()
         except Exception:
             pass
+
+
+class _Handle:
+    """What the handles of the operators on single tensors share: a device, a stream, the checks of tensors."""
+
+    def _begin(self, tensor, stream):
+        import torch
+        if not tensor.is_cuda:
+            raise ValueError(f"CUDA tensors are wanted, not one on {tensor.device}")
+        self._types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+        self._f32, self._i32, self._device = torch.float32, torch.int32, tensor.device
+        self.stream = stream if stream is not None else torch.cuda.current_stream(tensor.device)
+        self._h = ctypes.c_void_p()
+
+    def _ck(self, rc, what):
+        if rc:
+            raise SfbError(rc, what, getattr(lib(), self._last)(self._h))
+
+    def _matrix(self, t, dtype, n, width):
+        """Address and row pitch of a tensor [n, width] without gaps in a row."""
+        if t.dtype is not dtype or t.device != self._device:
+            raise ValueError(f"a {dtype} tensor on {self._device} is wanted, not {t.dtype} on {t.device}")
+        if t.shape != (n, width):
+            raise ValueError(f"a tensor [{n}, {width}] is wanted, not {list(t.shape)}")
+        if width > 1 and t.stride(1) != 1:
+            raise ValueError("the last dimension of a tensor has no gaps")
+        return t.data_ptr(), t.stride(0) if n > 1 else (width + 7) // 8 * 8
+
+    def _vector(self, t, dtype, n):
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.device != self._device or t.shape != (n,) or not t.is_contiguous():
+            raise ValueError(f"{n} contiguous entries of {dtype} on {self._device} are wanted, not {list(t.shape)} of {t.dtype} on {t.device}")
+        return t.data_ptr()
+
+    def capture(self, calls):
+        """As ``Context.capture``: the handle's stream is not the default one, and every kind of call has run once before."""
+        return _capture(self.stream, calls)
+
+    def close(self):
+        if getattr(self, "_h", None):
+            getattr(lib(), self._destroy)(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Dropout(_Handle):
+    """Owns one ``sfb_dropout``: entries dropped with probability ``p``, the others multiplied with 1 / (1 - p), by a counter-based
+    generator whose mask is never stored (include/sfb.h has the formulas).
+
+    ``rng``: two int64 on the device, the seed and the offset's base, which the caller moves on from step to step (``rng[1] += 1``,
+    in a captured graph too); ``call`` of a call is added to the offset, so that the layers of a step differ.  The same
+    (rng, call) is the same mask: the backward pass is ``sfb_dropout_apply(dY, dX)``.  All work is enqueued on ``stream``
+    (default: the current one at construction)."""
+    _last, _destroy = "sfb_dropout_last_cuda_error", "sfb_dropout_destroy"
+
+    def __init__(self, p, rng, stream=None):
+        import torch
+        if rng.dtype not in (torch.int64, torch.uint64) or rng.shape != (2,) or not rng.is_contiguous():
+            raise ValueError("rng: two contiguous 64-bit integers")
+        self._begin(rng, stream)
+        self.p, self.rng = float(p), rng
+        with torch.cuda.device(self._device):
+            rc = lib().sfb_dropout_init(self.p, rng.data_ptr(), self.stream.cuda_stream, ctypes.byref(self._h))
+        if rc:
+            raise SfbError(rc, "sfb_dropout_init")
+
+    def sfb_dropout_apply(self, X, Y, R=None, call=0):
+        """Y [n, cols] receives m * X, plus R where one is given; all of one type.  Y may be X or R."""
+        if X.dim() != 2 or X.dtype not in self._types:
+            raise ValueError("X [n, cols] of fp32, bf16 or fp16")
+        n, cols = X.shape
+        x, ldx = self._matrix(X, X.dtype, n, cols)
+        y, ldy = self._matrix(Y, X.dtype, n, cols)
+        r, ldr = self._matrix(R, X.dtype, n, cols) if R is not None else (None, 0)
+        self._ck(lib().sfb_dropout_apply(self._h, call, n, cols, self._types[X.dtype], x, ldx, r, ldr, y, ldy), "sfb_dropout_apply")
+
+
+class Embedding(_Handle):
+    """Owns one ``sfb_embed``: samples that are rows of a table, one a token id, and the table's gradient (include/sfb.h has the formulas).
+
+    ``table`` [tokens, dim] is a CUDA tensor of fp32, bf16 or fp16 whose rows have no gaps; it is borrowed: its values may change between
+    calls, its memory stays.  ``out_dtype``: of the samples and of their gradients (default: the table's).  All work is enqueued on
+    ``stream`` (default: the current one at construction)."""
+    _last, _destroy = "sfb_embed_last_cuda_error", "sfb_embed_destroy"
+
+    def __init__(self, table, max_ids, out_dtype=None, scale=1.0, stream=None):
+        import torch
+        self._begin(table, stream)
+        self.out_dtype = out_dtype if out_dtype is not None else table.dtype
+        if table.dim() != 2 or table.dtype not in self._types or self.out_dtype not in self._types:
+            raise ValueError("table [tokens, dim]; fp32, bf16 or fp16")
+        self.table, (self.tokens, self.dim) = table, table.shape
+        _, ldt = self._matrix(table, table.dtype, self.tokens, self.dim)
+        self.cfg = sfb_embed_config(self.tokens, self.dim, ldt, self._types[table.dtype], self._types[self.out_dtype], scale, max_ids,
+                                    self.stream.cuda_stream)
+        nbytes = sfb_embed_workspace_bytes(self.cfg)
+        with torch.cuda.device(self._device):
+            self.workspace = _workspace(nbytes + 1024, self._device, self.stream)
+            base = (self.workspace.data_ptr() + 1023) // 1024 * 1024
+            rc = lib().sfb_embed_init(ctypes.byref(self.cfg), table.data_ptr(), base, nbytes, ctypes.byref(self._h))
+        if rc:
+            raise SfbError(rc, "sfb_embed_init")
+
+    def _drop(self, drop):
+        if drop is not None and not isinstance(drop, Dropout):
+            raise ValueError("drop: a Dropout, or None")
+        return drop._h if drop is not None else None
+
+    def sfb_embed_forward(self, ids, X, drop=None, call=0):
+        """X [n, dim] receives scale * table[ids] (zeros for -1), dropped out where a ``Dropout`` is given."""
+        n = ids.shape[0]
+        i, (x, ldx) = self._vector(ids, self._i32, n), self._matrix(X, self.out_dtype, n, self.dim)
+        self._ck(lib().sfb_embed_forward(self._h, n, i, x, ldx, self._drop(drop), call), "sfb_embed_forward")
+
+    def sfb_embed_backward(self, ids, dX, dE, drop=None, call=0, alpha=1.0, add=False):
+        """dE [tokens, dim] (fp32) receives alpha times the table's gradient for dX [n, dim], whole; ``add``: it is added to dE.  With
+        alpha = -eta and the fp32 table itself for dE that is its step."""
+        n = ids.shape[0]
+        i, (dx, lddx) = self._vector(ids, self._i32, n), self._matrix(dX, self.out_dtype, n, self.dim)
+        de, ldde = self._matrix(dE, self._f32, self.tokens, self.dim)
+        self._ck(lib().sfb_embed_backward(self._h, n, i, dx, lddx, self._drop(drop), call, alpha, 1 if add else 0, de, ldde), "sfb_embed_backward")
+
+    def sfb_embed_get_status(self) -> int:
+        st = ctypes.c_uint32(0)
+        self._ck(lib().sfb_embed_get_status(self._h, ctypes.byref(st)), "sfb_embed_get_status")
+        return st.value
+
+
+class Sampler(_Handle):
+    """Owns one ``sfb_sampler``: a class drawn for each row of logits [n, classes] of ``dtype`` (include/sfb.h has the formulas).  All
+    work is enqueued on ``stream`` (default: the current one of ``device``, at construction)."""
+    _last, _destroy = "sfb_sampler_last_cuda_error", "sfb_sampler_destroy"
+
+    def __init__(self, classes, dtype, max_samples, stream=None, device=None):
+        import torch
+        if stream is None:
+            stream = torch.cuda.current_stream(device)
+        self._types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+        if dtype not in self._types:
+            raise ValueError("logits of fp32, bf16 or fp16")
+        self._f32, self._i32, self._device, self.stream, self._h = torch.float32, torch.int32, stream.device, stream, ctypes.c_void_p()
+        self.classes, self.dtype = classes, dtype
+        self.cfg = sfb_sampler_config(classes, max_samples, self._types[dtype], stream.cuda_stream)
+        with torch.cuda.device(self._device):
+            rc = lib().sfb_sampler_init(ctypes.byref(self.cfg), ctypes.byref(self._h))
+        if rc:
+            raise SfbError(rc, "sfb_sampler_init")
+
+    def sfb_sample(self, Z, u, ids, temperature=None, top_k=None, top_p=None, min_p=None, logp=None, kept=None):
+        """ids (int32 [n]) receives the classes drawn from logits Z [n, classes] with the random numbers u (fp32 [n], from [0, 1)); logp
+        (fp32) their log-probabilities under what the filters kept, kept (int32) how many classes that were.  temperature, top_p, min_p
+        (fp32) and top_k (int32) are [n] too, or None."""
+        n, f32, i32, v = Z.shape[0], self._f32, self._i32, self._vector
+        z, ldz = self._matrix(Z, self.dtype, n, self.classes)
+        self._ck(lib().sfb_sample(self._h, n, z, ldz, v(u, f32, n), v(temperature, f32, n), v(top_k, i32, n), v(top_p, f32, n), v(min_p, f32, n),
+                                  v(ids, i32, n), v(logp, f32, n), v(kept, i32, n)), "sfb_sample")
+
+
+def sfb_embed_workspace_bytes(cfg: sfb_embed_config) -> int:
+    n = ctypes.c_size_t(0)
+    rc = lib().sfb_embed_workspace_bytes(ctypes.byref(cfg), ctypes.byref(n))
+    if rc:
+        raise SfbError(rc, "sfb_embed_workspace_bytes")
+    return n.value
 
 
 def sfb_prox_columns_noalloc(W, stream=None):
