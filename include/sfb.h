@@ -413,7 +413,7 @@ int sfb_adapter_destroy(sfb_adapters* h);
  * the low (j even) or high 16 bits of word (j mod 8) / 2; it is kept where they are >= t.  No mask is stored: the backward pass
  * makes it again.  rng_dev (two uint64 in device memory, borrowed) holds the seed and the offset's base, to which a call adds `call`:
  * captured graphs take new masks from replay to replay where the caller moves rng_dev[1] on in between, and layers of one step
- * their own by `call`.  (i and j count from 0 in each call: rows beyond 2^32 and columns beyond 2^30 are refused.) */
+ * their own by `call`.  (i and j count from 0 in each call: 2^31 rows, 2^30 columns and pitches of 4 GB, or more, are refused.) */
 typedef struct sfb_dropout sfb_dropout;
 enum sfb_dtype { SFB_F32 = 0, SFB_BF16 = 1, SFB_F16 = 2 };
 /* p in [0, 1]; 1: nothing is kept. */

@@ -102,30 +102,35 @@ __device__ __forceinline__ uint4 philox(uint4 c, uint2 k) {
 }
 #endif
 
-// What a kernel takes of a dropout: entry j of a group is kept where its 16 bits are at least `threshold`.
+// What a kernel takes of a dropout: an entry is kept where its 16 bits are at least `threshold`.
 struct DropParams {
   const uint64_t* rng;                 // seed, offset; device memory
   uint64_t call;                       // added to the offset
-  uint32_t threshold;                  // round(65536 p)
+  uint32_t threshold;                  // round(65536 p), 0 .. 65536
+  uint32_t last;                       // 65536 threshold - 1, where that is not 0
   float factor;                        // 65536 / (65536 - threshold); 0 where nothing is kept
 };
 
 #ifdef __CUDACC__
+// Called by whole warps.
 struct Generator {
   uint2 key{}, offset{};
   __device__ __forceinline__ void begin(const DropParams& p) {
     const uint64_t seed = p.rng[0], at = p.rng[1] + p.call;
-    key = make_uint2(static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32));
-    offset = make_uint2(static_cast<uint32_t>(at), static_cast<uint32_t>(at >> 32));
+    key = make_uint2(same(static_cast<uint32_t>(seed)), same(static_cast<uint32_t>(seed >> 32)));
+    offset = make_uint2(same(static_cast<uint32_t>(at)), same(static_cast<uint32_t>(at >> 32)));
   }
-  // Zeroes the dropped ones of a group's entries (whatever they are: infinities and NaN too).
-  __device__ __forceinline__ void drop(float (&v)[kGroup], uint32_t row, uint32_t group, uint32_t threshold) const {
+  // A value that is the same in all lanes, known to be: what follows from it alone is computed once a warp.
+  static __device__ __forceinline__ uint32_t same(uint32_t v) { return __reduce_or_sync(0xffffffffu, v); }
+  // Zeroes the dropped ones of a group's entries (whatever they are: infinities and NaN too).  `last`: (threshold << 16) - 1, which 16 bits
+  // on top of a word exceed where they are at least the threshold, whatever lies below them.
+  __device__ __forceinline__ void drop(float (&v)[kGroup], uint32_t row, uint32_t group, uint32_t last) const {
     const uint4 w = philox(make_uint4(group, row, offset.x, offset.y), key);
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if ((u[j] & 0xffffu) < threshold) v[2 * j] = 0.f;
-      if ((u[j] >> 16) < threshold) v[2 * j + 1] = 0.f;
+      v[2 * j] = (u[j] << 16) > last ? v[2 * j] : 0.f;
+      v[2 * j + 1] = u[j] > last ? v[2 * j + 1] : 0.f;
     }
   }
 };

@@ -14,6 +14,7 @@
 #include <new>
 
 #include "sfb_elem.cuh"
+#include "sfb_ptx.cuh"
 
 namespace {
 
@@ -26,78 +27,94 @@ using sfb::pdl_launch_dependents;
 using sfb::pdl_wait;
 using sfb::Raw;
 
-// A matrix of groups, cut into blocks of kThreads * N of them: row and group of each that a thread takes, N of them kThreads apart.
+// A matrix of groups, cut into pieces of kThreads * N of them, of which a thread takes N, kThreads apart.
 constexpr int kThreads = 256;
-template <int N>
-struct Places {
-  int64_t row;
-  uint32_t group;
-  // A block's first place by a division of 64 bits where there are that many, the others by their distance from it.
-  __device__ __forceinline__ Places(const Divisor& groups, int64_t block) {
-    const uint64_t first = static_cast<uint64_t>(block) * (kThreads * N);
-    if (first < 0x7fffffffull) {
-      row = groups(static_cast<uint32_t>(first));
-    } else {
-      row = static_cast<int64_t>(first / groups.d);
-    }
-    group = static_cast<uint32_t>(first - static_cast<uint64_t>(row) * groups.d);
-  }
-  __device__ __forceinline__ void at(const Divisor& groups, int k, int64_t& r, uint32_t& g) const {
-    const uint32_t n = group + threadIdx.x + k * kThreads, q = groups(n);
-    r = row + q;
-    g = n - q * groups.d;
-  }
+struct Grid {
+  Divisor groups;                      // of a row
+  uint32_t rows, tail;                 // tail: entries of a row's last group
+  __device__ __forceinline__ int count(uint32_t group) const { return group + 1 < groups.d ? kGroup : static_cast<int>(tail); }
 };
+struct Place { uint32_t row, group; };
+// The first place of a piece (a division of 64 bits where there are that many), and others by their distance from it.
+template <int N>
+__device__ __forceinline__ Place first_place(const Grid& g, int64_t piece) {
+  const uint64_t first = static_cast<uint64_t>(piece) * (kThreads * N);
+  const uint32_t row = first < 0x7fffffffull ? g.groups(static_cast<uint32_t>(first)) : static_cast<uint32_t>(first / g.groups.d);
+  return Place{row, static_cast<uint32_t>(first - static_cast<uint64_t>(row) * g.groups.d)};
+}
+__device__ __forceinline__ Place place_at(const Grid& g, const Place& first, int k) {
+  const uint32_t n = first.group + threadIdx.x + k * kThreads, q = g.groups(n);
+  return Place{first.row + q, n - q * g.groups.d};
+}
+// A matrix of rows `pitch` bytes apart.
+template <typename T>
+__device__ __forceinline__ T* address(void* base, uint32_t pitch, const Place& at) {
+  return reinterpret_cast<T*>(static_cast<char*>(base) + static_cast<uint64_t>(at.row) * pitch) + at.group * static_cast<uint64_t>(kGroup);
+}
+template <typename T>
+__device__ __forceinline__ const T* address(const void* base, uint32_t pitch, const Place& at) {
+  return address<const T>(const_cast<void*>(base), pitch, at);
+}
 
 // ---- lookup ------------------------------------------------------------------------------------------------------------------------
 struct RowsParams {
   const void* table;
-  int64_t ldt, tokens, n, dim;
-  const int32_t* ids;
   void* out;
-  int64_t ldo;
-  Divisor groups;
+  const int32_t* ids;
+  int64_t pieces;
+  Grid grid;
+  uint32_t tokens, pitch_in, pitch_out;
   float factor;                        // scale, times the dropout's factor
   bool wide_in, wide_out;
   uint32_t* status;
   DropParams drop;
 };
 
+// Blocks take pieces in turn, the ids of the next one under way while one is copied.
 template <typename In, typename Out, bool DROP, int N>
-__global__ void __launch_bounds__(kThreads) embed_rows_kernel(const __grid_constant__ RowsParams p) {
+__global__ void __launch_bounds__(kThreads, N == 1 ? 1 : 4) embed_rows_kernel(const __grid_constant__ RowsParams p) {
   pdl_launch_dependents();
   pdl_wait();
-  const Places<N> places(p.groups, blockIdx.x);
   Generator generator;
   if constexpr (DROP) generator.begin(p.drop);
-  Raw<In> raw[N];
-  int64_t row[N];
-  uint32_t group[N];
-  bool named[N];
+  Place next[N];
+  int32_t id[N];
+  auto look = [&](int64_t piece) {
+    const Place first = first_place<N>(p.grid, piece);
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    places.at(p.groups, k, row[k], group[k]);
-    const int32_t id = row[k] < p.n ? p.ids[row[k]] : -1;
-    named[k] = id >= 0 && id < p.tokens;
-    if (!named[k] && id != -1 && group[k] == 0) atomicOr(p.status, SFB_STATUS_INDEX_RANGE);
-    const int64_t col = static_cast<int64_t>(group[k]) * kGroup;
-    if (named[k])
-      sfb::load_group(static_cast<const In*>(p.table) + id * p.ldt + col, static_cast<int>(min(static_cast<int64_t>(kGroup), p.dim - col)), p.wide_in, raw[k]);
-  }
-#pragma unroll
-  for (int k = 0; k < N; ++k) {
-    if (row[k] >= p.n) break;
-    float v[kGroup] = {};
-    if (named[k]) {
-      sfb::unpack(raw[k], v);
-      if constexpr (DROP) generator.drop(v, static_cast<uint32_t>(row[k]), group[k], p.drop.threshold);
-#pragma unroll
-      for (int j = 0; j < kGroup; ++j) v[j] *= p.factor;
+    for (int k = 0; k < N; ++k) {
+      next[k] = place_at(p.grid, first, k);
+      id[k] = next[k].row < p.grid.rows ? p.ids[next[k].row] : -1;
     }
-    const int64_t col = static_cast<int64_t>(group[k]) * kGroup;
-    Raw<Out> r;
-    sfb::pack(v, r);
-    sfb::store_group(static_cast<Out*>(p.out) + row[k] * p.ldo + col, static_cast<int>(min(static_cast<int64_t>(kGroup), p.dim - col)), p.wide_out, r);
+  };
+  look(blockIdx.x);
+  for (int64_t piece = blockIdx.x; piece < p.pieces; piece += gridDim.x) {
+    Raw<In> raw[N];
+    bool named[N];
+    Place at[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      at[k] = next[k];
+      named[k] = static_cast<uint32_t>(id[k]) < p.tokens;
+      if (!named[k] && id[k] != -1 && at[k].group == 0) atomicOr(p.status, SFB_STATUS_INDEX_RANGE);
+      if (named[k])
+        sfb::load_group(address<In>(p.table, p.pitch_in, Place{static_cast<uint32_t>(id[k]), at[k].group}), p.grid.count(at[k].group), p.wide_in, raw[k]);
+    }
+    if (N > 1 && piece + gridDim.x < p.pieces) look(piece + gridDim.x);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      if (at[k].row >= p.grid.rows) break;
+      float v[kGroup] = {};
+      if (named[k]) {
+        sfb::unpack(raw[k], v);
+        if constexpr (DROP) generator.drop(v, at[k].row, at[k].group, p.drop.last);
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) v[j] *= p.factor;
+      }
+      Raw<Out> r;
+      sfb::pack(v, r);
+      sfb::store_group(address<Out>(p.out, p.pitch_out, at[k]), p.grid.count(at[k].group), p.wide_out, r);
+    }
   }
 }
 
@@ -106,37 +123,35 @@ __global__ void __launch_bounds__(kThreads) embed_rows_kernel(const __grid_const
 struct DropoutParams {
   const void *x, *r;
   void* y;
-  int64_t ldx, ldr, ldy, n, cols;
-  Divisor groups;
+  Grid grid;
+  uint32_t pitch_x, pitch_r, pitch_y;
   bool wide;
   DropParams drop;
 };
 
 template <typename T, bool RESIDUAL, int N>
-__global__ void __launch_bounds__(kThreads) dropout_kernel(const __grid_constant__ DropoutParams p) {
+__global__ void __launch_bounds__(kThreads, N == 1 ? 1 : 4) dropout_kernel(const __grid_constant__ DropoutParams p) {
   pdl_launch_dependents();
   pdl_wait();
-  const Places<N> places(p.groups, blockIdx.x);
+  const Place first = first_place<N>(p.grid, blockIdx.x);
   Raw<T> raw[N], more[RESIDUAL ? N : 1];
-  int64_t row[N];
-  uint32_t group[N];
+  Place at[N];
 #pragma unroll
   for (int k = 0; k < N; ++k) {
-    places.at(p.groups, k, row[k], group[k]);
-    if (row[k] >= p.n) continue;
-    const int64_t col = static_cast<int64_t>(group[k]) * kGroup;
-    const int count = static_cast<int>(min(static_cast<int64_t>(kGroup), p.cols - col));
-    sfb::load_group(static_cast<const T*>(p.x) + row[k] * p.ldx + col, count, p.wide, raw[k]);
-    if constexpr (RESIDUAL) sfb::load_group(static_cast<const T*>(p.r) + row[k] * p.ldr + col, count, p.wide, more[k]);
+    at[k] = place_at(p.grid, first, k);
+    if (at[k].row >= p.grid.rows) continue;
+    const int count = p.grid.count(at[k].group);
+    sfb::load_group(address<T>(p.x, p.pitch_x, at[k]), count, p.wide, raw[k]);
+    if constexpr (RESIDUAL) sfb::load_group(address<T>(p.r, p.pitch_r, at[k]), count, p.wide, more[k]);
   }
   Generator generator;
   generator.begin(p.drop);
 #pragma unroll
   for (int k = 0; k < N; ++k) {
-    if (row[k] >= p.n) break;
+    if (at[k].row >= p.grid.rows) break;
     float v[kGroup];
     sfb::unpack(raw[k], v);
-    generator.drop(v, static_cast<uint32_t>(row[k]), group[k], p.drop.threshold);
+    if (p.drop.threshold) generator.drop(v, at[k].row, at[k].group, p.drop.last);
     if constexpr (RESIDUAL) {
       float u[kGroup];
       sfb::unpack(more[k], u);
@@ -146,10 +161,9 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const __grid_constant
 #pragma unroll
       for (int j = 0; j < kGroup; ++j) v[j] *= p.drop.factor;
     }
-    const int64_t col = static_cast<int64_t>(group[k]) * kGroup;
     Raw<T> r;
     sfb::pack(v, r);
-    sfb::store_group(static_cast<T*>(p.y) + row[k] * p.ldy + col, static_cast<int>(min(static_cast<int64_t>(kGroup), p.cols - col)), p.wide, r);
+    sfb::store_group(address<T>(p.y, p.pitch_y, at[k]), p.grid.count(at[k].group), p.wide, r);
   }
 }
 
@@ -158,14 +172,14 @@ __global__ void __launch_bounds__(kThreads) dropout_kernel(const __grid_constant
 // its share of the samples, a warp a run of them; the lanes of a warp that hold the same digit find one another by a ballot a bit.
 // More samples take three launches a digit (counts of tiles, their sums, the move), each tile as a CTA of the cluster does it.
 constexpr int kSortThreads = 1024, kSortWarps = 32, kSortPer = 8, kSortTile = kSortThreads * kSortPer;
-constexpr int kSortCtas = 8;
-constexpr int64_t kSortMost = static_cast<int64_t>(kSortTile) * kSortCtas;
+constexpr int kSortCtas = 16;          // (more than 8 are asked for: allow_clusters)
+constexpr int64_t kSortMost = static_cast<int64_t>(kSortThreads) * 4 * kSortCtas;
 constexpr int kMaxBits = 10, kMaxBins = 1 << kMaxBits;
 
 struct SortParams {
-  const int32_t* ids;                  // of the first digit; the others read keys_in, at_in
-  const uint32_t *keys_in, *at_in;
-  uint32_t *keys_out, *at_out;
+  const int32_t* ids;                  // of the first digit; the others read `in`
+  const uint2* in;                     // (key, sample)
+  uint2* out;
   int64_t n;
   uint32_t tokens;                     // a sample that names none of them takes this as its key
   int bits, shift;                     // of the digit
@@ -184,31 +198,29 @@ struct SortShared {
 
 // Digits of a tile that begins at `first`: key and the rank within the CTA among those of the same digit, of each of a thread's samples.
 template <int PER>
-__device__ __forceinline__ void rank_tile(SortShared& s, const SortParams& p, int64_t first, uint32_t (&key)[PER], uint32_t (&at)[PER],
-                                          uint16_t (&rank)[PER]) {
+__device__ __forceinline__ void rank_tile(SortShared& s, const SortParams& p, int64_t first, uint2 (&e)[PER], uint16_t (&rank)[PER]) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1 << p.bits;
-  for (int i = threadIdx.x; i < kSortWarps * kMaxBins / 2; i += kSortThreads) reinterpret_cast<uint32_t*>(s.rank)[i] = 0;
-  __syncthreads();
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     const int64_t i = first + warp * (32 * PER) + j * 32 + lane;
-    key[j] = 0;
-    at[j] = static_cast<uint32_t>(i);
+    e[j] = make_uint2(0, static_cast<uint32_t>(i));
     if (i >= p.n) continue;
     if (p.ids) {
       const int32_t id = p.ids[i];
       const bool named = id >= 0 && static_cast<uint32_t>(id) < p.tokens;
       if (!named && id != -1) atomicOr(p.status, SFB_STATUS_INDEX_RANGE);
-      key[j] = named ? static_cast<uint32_t>(id) : p.tokens;
+      e[j].x = named ? static_cast<uint32_t>(id) : p.tokens;
     } else {
-      key[j] = __ldcg(p.keys_in + i);
-      at[j] = __ldcg(p.at_in + i);
+      e[j] = __ldcg(p.in + i);
     }
   }
+  // (its own warp's counts: no other looks at them before the barrier)
+  for (int i = lane; i < bins / 2; i += 32) reinterpret_cast<uint32_t*>(s.rank[warp])[i] = 0;
+  __syncwarp();
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     const bool there = first + warp * (32 * PER) + j * 32 + lane < p.n;
-    const uint32_t digit = (key[j] >> p.shift) & (bins - 1);
+    const uint32_t digit = (e[j].x >> p.shift) & (bins - 1);
     uint32_t same = __ballot_sync(0xffffffffu, there);
     if (!same) break;
     for (int b = 0; b < p.bits; ++b) {
@@ -225,10 +237,16 @@ __device__ __forceinline__ void rank_tile(SortShared& s, const SortParams& p, in
   __syncthreads();
   if (threadIdx.x < bins) {
     uint32_t sum = 0;
-    for (int w = 0; w < kSortWarps; ++w) {
-      const uint32_t c = s.rank[w][threadIdx.x];
-      s.rank[w][threadIdx.x] = static_cast<uint16_t>(sum);
-      sum += c;
+#pragma unroll
+    for (int w0 = 0; w0 < kSortWarps; w0 += 16) {        // (loads that do not wait for stores)
+      uint32_t c[16];
+#pragma unroll
+      for (int w = 0; w < 16; ++w) c[w] = s.rank[w0 + w][threadIdx.x];
+#pragma unroll
+      for (int w = 0; w < 16; ++w) {
+        s.rank[w0 + w][threadIdx.x] = static_cast<uint16_t>(sum);
+        sum += c[w];
+      }
     }
     s.total[threadIdx.x] = sum;
   }
@@ -251,16 +269,14 @@ __device__ __forceinline__ uint32_t scan_bins(SortShared& s, uint32_t value) {
 }
 
 template <int PER>
-__device__ __forceinline__ void move_tile(const SortShared& s, const SortParams& p, int64_t first, const uint32_t (&key)[PER],
-                                          const uint32_t (&at)[PER], const uint16_t (&rank)[PER]) {
+__device__ __forceinline__ void move_tile(const SortShared& s, const SortParams& p, int64_t first, const uint2 (&e)[PER],
+                                          const uint16_t (&rank)[PER]) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
     if (first + warp * (32 * PER) + j * 32 + lane >= p.n) break;
-    const uint32_t digit = (key[j] >> p.shift) & ((1u << p.bits) - 1);
-    const uint32_t to = s.base[digit] + s.rank[warp][digit] + rank[j];
-    __stcg(p.keys_out + to, key[j]);
-    __stcg(p.at_out + to, at[j]);
+    const uint32_t digit = (e[j].x >> p.shift) & ((1u << p.bits) - 1);
+    __stcg(p.out + s.base[digit] + s.rank[warp][digit] + rank[j], e[j]);
   }
 }
 
@@ -277,7 +293,7 @@ __device__ __forceinline__ uint32_t cluster_read(const uint32_t* here, int cta) 
 
 // Where the sorted samples and what goes with them lie; two buffers that the digits take in turn, the last one writes the first.
 struct Order {
-  uint32_t *keys[2], *at[2];
+  uint2* entries[2];                   // (key, sample)
   uint32_t* touched;                   // a bit for each token that some sample names
   uint32_t* crossing;                  // [0]: how many chunks hold the beginning of a token that goes beyond them, then which
   int64_t words;                       // of touched; 0: not wanted
@@ -297,14 +313,13 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(SortParams p, con
   const int64_t first = static_cast<int64_t>(cta) * (kSortThreads * PER);
   if (cta == 0 && threadIdx.x == 0) o.crossing[0] = 0;
   for (int64_t i = static_cast<int64_t>(cta) * kSortThreads + threadIdx.x; i < o.words; i += static_cast<int64_t>(ctas) * kSortThreads) o.touched[i] = 0;
-  uint32_t key[PER], at[PER];
+  uint2 e[PER];
   uint16_t rank[PER];
   for (int d = 0; d < digits; ++d) {
     const int to = (digits - 1 - d) & 1;
-    p.keys_out = o.keys[to];
-    p.at_out = o.at[to];
+    p.out = o.entries[to];
     p.shift = d * p.bits;
-    rank_tile<PER>(s, p, first, key, at, rank);
+    rank_tile<PER>(s, p, first, e, rank);
     cluster_sync();                    // every CTA's totals are there (and, the first time, the bits are clear)
     uint32_t all = 0, before = 0;
     if (threadIdx.x < (1 << p.bits)) {
@@ -317,16 +332,15 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(SortParams p, con
     const uint32_t base = scan_bins(s, all) + before;
     if (threadIdx.x < (1 << p.bits)) s.base[threadIdx.x] = base;
     __syncthreads();
-    move_tile<PER>(s, p, first, key, at, rank);
+    move_tile<PER>(s, p, first, e, rank);
     if (d == 0 && o.words) {
 #pragma unroll
       for (int j = 0; j < PER; ++j)
-        if (first + (threadIdx.x >> 5) * (32 * PER) + j * 32 + (threadIdx.x & 31) < p.n) mark(o, key[j], p.tokens);
+        if (first + (threadIdx.x >> 5) * (32 * PER) + j * 32 + (threadIdx.x & 31) < p.n) mark(o, e[j].x, p.tokens);
     }
     cluster_sync();                    // the order is written, the totals are read
     p.ids = nullptr;
-    p.keys_in = o.keys[to];
-    p.at_in = o.at[to];
+    p.in = o.entries[to];
   }
 }
 
@@ -345,14 +359,14 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_count_kernel(const __gri
   pdl_launch_dependents();
   pdl_wait();
   const int64_t first = static_cast<int64_t>(blockIdx.x) * kSortTile;
-  uint32_t key[kSortPer], at[kSortPer];
+  uint2 e[kSortPer];
   uint16_t rank[kSortPer];
-  rank_tile<kSortPer>(s, p, first, key, at, rank);
+  rank_tile<kSortPer>(s, p, first, e, rank);
   if (threadIdx.x < (1 << p.bits)) p.counts[threadIdx.x * p.tiles + blockIdx.x] = s.total[threadIdx.x];
   if (p.ids && o.words) {
 #pragma unroll
     for (int j = 0; j < kSortPer; ++j)
-      if (first + (threadIdx.x >> 5) * (32 * kSortPer) + j * 32 + (threadIdx.x & 31) < p.n) mark(o, key[j], p.tokens);
+      if (first + (threadIdx.x >> 5) * (32 * kSortPer) + j * 32 + (threadIdx.x & 31) < p.n) mark(o, e[j].x, p.tokens);
   }
 }
 
@@ -384,26 +398,26 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_move_kernel(const __grid
   pdl_launch_dependents();
   pdl_wait();
   const int64_t first = static_cast<int64_t>(blockIdx.x) * kSortTile;
-  uint32_t key[kSortPer], at[kSortPer];
+  uint2 e[kSortPer];
   uint16_t rank[kSortPer];
-  rank_tile<kSortPer>(s, p, first, key, at, rank);
+  rank_tile<kSortPer>(s, p, first, e, rank);
   const bool bin = threadIdx.x < (1 << p.bits);
   const uint32_t base = scan_bins(s, bin ? p.totals[threadIdx.x] : 0);
   if (bin) s.base[threadIdx.x] = base + p.counts[threadIdx.x * p.tiles + blockIdx.x];
   __syncthreads();
-  move_tile<kSortPer>(s, p, first, key, at, rank);
+  move_tile<kSortPer>(s, p, first, e, rank);
 }
 
 // ---- the gradient ------------------------------------------------------------------------------------------------------------------
 struct GradientParams {
-  const uint32_t *keys, *at;           // in order
+  const uint2* order;                  // (key, sample)
   const uint32_t* touched;
   uint32_t* crossing;
   float* parts;                        // [2 chunks][groups][8]: what a chunk's first token has of an earlier one's, and its last one's
                                        // beginning
   int64_t n;
   int32_t per;                         // samples a chunk
-  uint32_t chunks, work;               // work: blocks that add; the others zero
+  uint32_t chunks, zero;               // zero: the first blocks, which zero; the others add
   uint32_t tokens;
   Divisor groups;
   const void* dx;
@@ -416,92 +430,112 @@ struct GradientParams {
   DropParams drop;
 };
 
-__device__ __forceinline__ void store_sum(const GradientParams& p, uint32_t key, uint32_t group, const float (&sum)[kGroup]) {
-  const int64_t col = static_cast<int64_t>(group) * kGroup;
-  const int count = static_cast<int>(min(static_cast<int64_t>(kGroup), p.dim - col));
-  float* to = p.table + key * p.lddt + col;
-  Raw<float> r;
-  float v[kGroup] = {};
-  if (p.add) {
-    sfb::load_group(to, count, p.wide_out, r);
-    sfb::unpack(r, v);
-  }
-#pragma unroll
-  for (int j = 0; j < kGroup; ++j) v[j] = fmaf(p.factor, sum[j], v[j]);
-  sfb::pack(v, r);
-  sfb::store_group(to, count, p.wide_out, r);
-}
-
-constexpr int kAhead = 4;              // samples under way a thread
-
-template <typename T, bool DROP>
-__global__ void __launch_bounds__(kThreads) gradient_kernel(const __grid_constant__ GradientParams p) {
-  pdl_launch_dependents();
-  pdl_wait();
-  if (blockIdx.x >= p.work) {          // rows that no sample names
-    const Places<4> places(p.groups, blockIdx.x - p.work);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      int64_t row;
-      uint32_t group;
-      places.at(p.groups, k, row, group);
-      if (row >= p.tokens || (p.touched[row >> 5] >> (row & 31) & 1)) continue;
-      const int64_t col = static_cast<int64_t>(group) * kGroup;
-      const Raw<float> zero{};
-      sfb::store_group(p.table + row * p.lddt + col, static_cast<int>(min(static_cast<int64_t>(kGroup), p.dim - col)), p.wide_out, zero);
+// Rows that start on 16-byte boundaries by copies of zeros from shared memory, a row a thread; what lies behind the last 16 bytes, and
+// other rows, by stores.
+constexpr int kZeroBytes = 4096;
+__device__ __forceinline__ void zero_rows(const GradientParams& p) {
+  __shared__ __align__(128) uint4 zeros[kZeroBytes / 16];
+  for (int i = threadIdx.x; i < kZeroBytes / 16; i += kThreads) zeros[i] = make_uint4(0, 0, 0, 0);
+  sfb::ptx::fence_proxy_async_smem();
+  __syncthreads();
+  auto untouched = [&](int64_t row) { return !(p.touched[row >> 5] >> (row & 31) & 1); };
+  if (p.wide_out) {
+    const int64_t bytes = p.dim / 4 * 16;
+    for (int64_t row = static_cast<int64_t>(threadIdx.x) * p.zero + blockIdx.x; row < p.tokens; row += static_cast<int64_t>(p.zero) * kThreads) {
+      if (!untouched(row)) continue;
+      float* to = p.table + row * p.lddt;
+      for (int64_t at = 0; at < bytes; at += kZeroBytes)
+        sfb::ptx::bulk_store(reinterpret_cast<char*>(to) + at, zeros, static_cast<uint32_t>(min(static_cast<int64_t>(kZeroBytes), bytes - at)));
+      for (int64_t col = p.dim / 4 * 4; col < p.dim; ++col) to[col] = 0.f;
     }
+    sfb::ptx::tma_commit_group();
+    sfb::ptx::tma_wait_group<0>();     // (the copies read this block's shared memory)
     return;
   }
-  const uint32_t place = blockIdx.x * kThreads + threadIdx.x, chunk = p.groups(place), group = place - chunk * p.groups.d;
+  const int lane = threadIdx.x & 31, warps = kThreads / 32;
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * warps + (threadIdx.x >> 5); row < p.tokens; row += static_cast<int64_t>(p.zero) * warps)
+    if (untouched(row))
+      for (int64_t col = lane; col < p.dim; col += 32) p.table[row * p.lddt + col] = 0.f;
+}
+
+constexpr int kAhead = 2;          // samples under way a thread
+
+template <typename T, bool DROP, bool ADD>
+__global__ void __launch_bounds__(kThreads, 4) gradient_kernel(const __grid_constant__ GradientParams p) {
+  pdl_launch_dependents();
+  pdl_wait();
+  if (blockIdx.x < p.zero) {           // rows that no sample names
+    zero_rows(p);
+    return;
+  }
+  const uint32_t place = (blockIdx.x - p.zero) * kThreads + threadIdx.x, chunk = p.chunks - 1 - p.groups(place), group = place - p.groups(place) * p.groups.d;
+  Generator generator;
+  if constexpr (DROP) generator.begin(p.drop);
   if (chunk >= p.chunks) return;
-  const int64_t first = static_cast<int64_t>(chunk) * p.per, last = min(p.n, first + p.per);
+  const uint32_t n = static_cast<uint32_t>(p.n), first = chunk * p.per, last = min(n, first + p.per);
   const int64_t col = static_cast<int64_t>(group) * kGroup;
   const int count = static_cast<int>(min(static_cast<int64_t>(kGroup), p.dim - col));
   const T* dx = static_cast<const T*>(p.dx) + col;
-  uint32_t key = p.keys[first];
-  if (key == p.tokens) return;
-  Generator generator;
-  if constexpr (DROP) generator.begin(p.drop);
-  bool lead = first > 0 && p.keys[first - 1] == key;
+  float* table = p.table + col;
+  float* parts = p.parts + (2 * static_cast<int64_t>(chunk) * p.groups.d + group) * kGroup;
+  auto entry = [&](uint32_t i) { return i < last ? p.order[i] : make_uint2(p.tokens, 0); };
+  uint2 next[kAhead];
+#pragma unroll
+  for (int q = 0; q < kAhead; ++q) next[q] = entry(first + q);
+  const uint32_t first_key = next[0].x;
+  if (first_key == p.tokens) return;
+  // what the chunk's first token has of an earlier chunk's, and whether its last one goes on
+  const uint32_t lead_key = first > 0 && p.order[first - 1].x == first_key ? first_key : p.tokens;
+  const uint32_t trail_key = last < n ? p.order[last].x : p.tokens;
   float sum[kGroup] = {};
-  auto leave = [&](bool trail) {
-    if (!lead && !trail) {
-      store_sum(p, key, group, sum);
-      return;
-    }
-    Raw<float> r;
-    sfb::pack(sum, r);
-    sfb::store_group(p.parts + ((2 * static_cast<int64_t>(chunk) + !lead) * p.groups.d + group) * kGroup, kGroup, true, r);
-    if (!lead && group == 0) p.crossing[1 + atomicAdd(p.crossing, 1u)] = chunk;
-  };
-  for (int64_t i = first; i < last; i += kAhead) {
-    uint32_t keys[kAhead], at[kAhead];
+  for (uint32_t i = first; i < last; i += kAhead) {
+    uint2 e[kAhead];
     Raw<T> raw[kAhead];
-#pragma unroll
-    for (int q = 0; q < kAhead; ++q) keys[q] = i + q < last ? p.keys[i + q] : p.tokens;
+    Raw<float> old[ADD ? kAhead : 1];
 #pragma unroll
     for (int q = 0; q < kAhead; ++q) {
-      at[q] = keys[q] < p.tokens ? p.at[i + q] : 0;
-      if (keys[q] < p.tokens) sfb::load_group(dx + at[q] * p.lddx, count, p.wide_in, raw[q]);
+      e[q] = next[q];
+      if (e[q].x < p.tokens) sfb::load_group(dx + e[q].y * p.lddx, count, p.wide_in, raw[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) next[q] = entry(i + kAhead + q);
+    bool ends[kAhead], whole[kAhead];
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) {
+      ends[q] = e[q].x != (q + 1 < kAhead ? e[q + 1].x : next[0].x) && e[q].x < p.tokens;
+      whole[q] = ends[q] && e[q].x != lead_key && (e[q].x != trail_key || i + q + 1 < last);
+      if constexpr (ADD) {             // (with the samples: nothing waits for a row by itself)
+        if (whole[q]) sfb::load_group(table + e[q].x * p.lddt, count, p.wide_out, old[q]);
+      }
     }
 #pragma unroll
     for (int q = 0; q < kAhead; ++q) {
-      if (keys[q] == p.tokens) break;  // nothing follows
-      if (keys[q] != key) {
-        leave(false);
-        key = keys[q];
-        lead = false;
-#pragma unroll
-        for (int j = 0; j < kGroup; ++j) sum[j] = 0.f;
-      }
+      if (e[q].x == p.tokens) break;   // nothing follows
       float v[kGroup];
       sfb::unpack(raw[q], v);
-      if constexpr (DROP) generator.drop(v, at[q], group, p.drop.threshold);
+      if constexpr (DROP) generator.drop(v, e[q].y, group, p.drop.last);
 #pragma unroll
       for (int j = 0; j < kGroup; ++j) sum[j] += v[j];
+      if (!ends[q]) continue;
+      Raw<float> r;
+      float* to = table + e[q].x * p.lddt;
+      if (whole[q]) {
+        float o[kGroup] = {};
+        if constexpr (ADD) sfb::unpack(old[q], o);
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) o[j] = fmaf(p.factor, sum[j], o[j]);
+        sfb::pack(o, r);
+      } else {
+        const bool begins = e[q].x != lead_key;
+        to = parts + (begins ? static_cast<int64_t>(p.groups.d) * kGroup : 0);
+        sfb::pack(sum, r);
+        if (begins && group == 0) p.crossing[1 + atomicAdd(p.crossing, 1u)] = chunk;
+      }
+      sfb::store_group(to, whole[q] ? count : kGroup, p.wide_out || !whole[q], r);
+#pragma unroll
+      for (int j = 0; j < kGroup; ++j) sum[j] = 0.f;
     }
   }
-  leave(last < p.n && p.keys[last] == key);
 }
 
 // Blocks take (token, 32 groups) in turn: eight warps add contiguous shares of the parts, the first adds the shares.
@@ -513,12 +547,12 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Gradi
   const int share = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (uint64_t item = blockIdx.x; item < static_cast<uint64_t>(count) * slabs; item += gridDim.x) {
     const uint32_t chunk = p.crossing[1 + item / slabs], group = static_cast<uint32_t>(item % slabs) * 32 + lane;
-    const uint32_t key = p.keys[(static_cast<int64_t>(chunk) + 1) * p.per - 1];
+    const uint32_t key = p.order[(static_cast<int64_t>(chunk) + 1) * p.per - 1].x;
     // the chunks behind it that begin with this token
     int64_t more = 0;
     for (int got = 256; got == 256; more += got) {
       const int64_t at = (static_cast<int64_t>(chunk) + 1 + more + threadIdx.x) * p.per;
-      got = __syncthreads_count(at < p.n && p.keys[at] == key);
+      got = __syncthreads_count(at < p.n && p.order[at].x == key);
     }
     const int64_t each = (more + 1 + 7) / 8, from = share * each, to = min(more + 1, from + each);
     float sum[kGroup] = {};
@@ -541,7 +575,17 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Gradi
       for (int w = 1; w < 8 && w * each <= more; ++w)
 #pragma unroll
         for (int j = 0; j < kGroup; ++j) sum[j] += shares[w][lane][j];
-      store_sum(p, key, group, sum);
+      const int64_t col = static_cast<int64_t>(group) * kGroup;
+      const int count = static_cast<int>(min(static_cast<int64_t>(kGroup), p.dim - col));
+      float* to = p.table + key * p.lddt + col;
+      Raw<float> r{};
+      float v[kGroup];
+      if (p.add) sfb::load_group(to, count, p.wide_out, r);
+      sfb::unpack(r, v);
+#pragma unroll
+      for (int j = 0; j < kGroup; ++j) v[j] = fmaf(p.factor, sum[j], v[j]);
+      sfb::pack(v, r);
+      sfb::store_group(to, count, p.wide_out, r);
     }
     __syncthreads();
   }
@@ -568,19 +612,27 @@ int fail(H* h, cudaError_t e) {
   return SFB_ERR_CUDA;
 }
 
+constexpr int64_t kPieces = static_cast<int64_t>(sfb::kModelSms) * 2048;
 constexpr int kPer[] = {4, 8, 16, 32, 64};
 constexpr int64_t kBlocksMost = (1ll << 31) - 1;
+
+// Of a matrix that the element-wise kernels take: up to 2^31 rows, rows less than 4 GB apart.
+bool fits(int64_t n, int64_t pitch, int32_t dtype) { return n < (1ll << 31) && pitch < static_cast<int64_t>((1ull << 32) / sfb::size_of(dtype)); }
+Grid grid_of(int64_t n, int64_t cols) {
+  const int64_t groups = groups_of(cols);
+  return Grid{Divisor(static_cast<uint32_t>(groups)), static_cast<uint32_t>(n), static_cast<uint32_t>(cols - (groups - 1) * kGroup)};
+}
 
 // Samples a chunk: the fewest (more, smaller pieces of work) that still are two full rounds of threads or, beyond that, keep what is left
 // of tokens that go beyond a chunk a small part of what is read.
 int samples_per_chunk(int64_t n, int64_t groups) {
   for (const int per : kPer)
-    if ((n + per - 1) / per * groups <= static_cast<int64_t>(sfb::kModelSms) * 2048) return per;
+    if ((n + per - 1) / per * groups <= kPieces) return per;
   return 64;
 }
 
 struct EmbedLayout {
-  size_t status, crossing, touched, keys[2], at[2], counts, totals, parts, bytes;
+  size_t status, crossing, touched, entries[2], counts, totals, parts, bytes;
   int64_t words, tiles;
 };
 
@@ -600,15 +652,12 @@ EmbedLayout layout_of(const sfb_embed_config& c) {
   int64_t chunks = 1;
   for (const int per : kPer) {
     // the rule takes `per` up to this many samples
-    const int64_t most = per == 64 ? n : std::min(n, static_cast<int64_t>(sfb::kModelSms) * 2048 / groups * per);
+    const int64_t most = per == 64 ? n : std::min(n, kPieces / groups * per);
     chunks = std::max(chunks, (most + per - 1) / per);
   }
   l.crossing = take((chunks + 1) * 4);
   l.touched = take(l.words * 4);
-  for (int k = 0; k < 2; ++k) {
-    l.keys[k] = take(n * 4);
-    l.at[k] = take(n * 4);
-  }
+  for (size_t& e : l.entries) e = take(n * 8);
   l.counts = take(l.tiles * kMaxBins * 4);
   l.totals = take(kMaxBins * 4);
   l.parts = take(static_cast<size_t>(chunks) * 2 * groups * kGroup * 4);
@@ -620,17 +669,22 @@ int check(const sfb_embed_config* c) {
   if (!c || c->tokens <= 0 || c->dim <= 0 || c->ldt < 0 || c->max_ids < 0 || !std::isfinite(c->scale)) return SFB_ERR_ARG;
   if (!sfb::is_dtype(c->table_dtype) || !sfb::is_dtype(c->out_dtype)) return SFB_ERR_ARG;
   if (c->tokens > (1ll << 30) || c->dim > (1ll << 24) || c->max_ids > (1ll << 26)) return SFB_ERR_SHAPE;
-  if (c->ldt && c->ldt < c->dim) return SFB_ERR_SHAPE;
+  if ((c->ldt && c->ldt < c->dim) || c->ldt >= (1ll << 32) / static_cast<int64_t>(sfb::size_of(c->table_dtype))) return SFB_ERR_SHAPE;
   return SFB_OK;
 }
 
 template <typename In, typename Out, bool DROP>
-cudaError_t launch_rows(const RowsParams& p, cudaStream_t s) {
-  const int64_t all = p.n * p.groups.d;
-  // (four groups a thread, their loads under way together, once that still is a block for each SM)
-  if (all >= static_cast<int64_t>(sfb::kModelSms) * kThreads * 4)
-    return sfb::launch_kernel(embed_rows_kernel<In, Out, DROP, 4>, dim3(static_cast<unsigned>((all + kThreads * 4 - 1) / (kThreads * 4))), dim3(kThreads), 0, s, 1, p);
-  return sfb::launch_kernel(embed_rows_kernel<In, Out, DROP, 1>, dim3(static_cast<unsigned>((all + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, 1, p);
+cudaError_t launch_rows(RowsParams p, cudaStream_t s) {
+  const int64_t all = static_cast<int64_t>(p.grid.rows) * p.grid.groups.d;
+  // (groups a thread, their loads under way together, once that still is a block for each SM)
+  constexpr int N = 2;
+  if (all < static_cast<int64_t>(sfb::kModelSms) * kThreads * N) {
+    p.pieces = (all + kThreads - 1) / kThreads;
+    return sfb::launch_kernel(embed_rows_kernel<In, Out, DROP, 1>, dim3(static_cast<unsigned>(p.pieces)), dim3(kThreads), 0, s, 1, p);
+  }
+  p.pieces = (all + kThreads * N - 1) / (kThreads * N);
+  const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(p.pieces, sfb::sm_count() * 4));
+  return sfb::launch_kernel(embed_rows_kernel<In, Out, DROP, N>, dim3(blocks), dim3(kThreads), 0, s, 1, p);
 }
 template <typename In, typename Out>
 cudaError_t launch_rows(const RowsParams& p, bool drop, cudaStream_t s) {
@@ -645,9 +699,10 @@ cudaError_t launch_rows(const RowsParams& p, int32_t out, bool drop, cudaStream_
 
 template <typename T, bool RESIDUAL>
 cudaError_t launch_dropout(const DropoutParams& p, cudaStream_t s) {
-  const int64_t all = p.n * p.groups.d;
-  if (all >= static_cast<int64_t>(sfb::kModelSms) * kThreads * 4)
-    return sfb::launch_kernel(dropout_kernel<T, RESIDUAL, 4>, dim3(static_cast<unsigned>((all + kThreads * 4 - 1) / (kThreads * 4))), dim3(kThreads), 0, s, 1, p);
+  constexpr int N = RESIDUAL ? 2 : 4;
+  const int64_t all = static_cast<int64_t>(p.grid.rows) * p.grid.groups.d;
+  if (all >= static_cast<int64_t>(sfb::kModelSms) * kThreads * N)
+    return sfb::launch_kernel(dropout_kernel<T, RESIDUAL, N>, dim3(static_cast<unsigned>((all + kThreads * N - 1) / (kThreads * N))), dim3(kThreads), 0, s, 1, p);
   return sfb::launch_kernel(dropout_kernel<T, RESIDUAL, 1>, dim3(static_cast<unsigned>((all + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, 1, p);
 }
 template <typename T>
@@ -657,7 +712,8 @@ cudaError_t launch_dropout(const DropoutParams& p, cudaStream_t s) {
 
 template <int PER>
 cudaError_t launch_sort(const SortParams& p, const Order& o, int digits, int ctas, cudaStream_t s) {
-  const cudaError_t e = sfb::allow_smem<sort_kernel<PER>>(sizeof(SortShared));
+  cudaError_t e = sfb::allow_smem<sort_kernel<PER>>(sizeof(SortShared));
+  if (e == cudaSuccess) e = sfb::allow_clusters<sort_kernel<PER>>();
   return e == cudaSuccess ? sfb::launch_kernel(sort_kernel<PER>, dim3(ctas), dim3(kSortThreads), sizeof(SortShared), s, ctas, p, o, digits, ctas) : e;
 }
 
@@ -673,13 +729,12 @@ cudaError_t sort_samples(const EmbedLayout& l, char* ws, const sfb_embed_config&
   p.status = reinterpret_cast<uint32_t*>(ws + l.status);
   const cudaStream_t s = static_cast<cudaStream_t>(c.stream);
   if (n <= kSortMost) {
-    const int per = n <= kSortThreads * kSortCtas ? 1 : n <= 2 * kSortThreads * kSortCtas ? 2 : n <= 4 * kSortThreads * kSortCtas ? 4 : 8;
+    const int per = n <= kSortThreads * kSortCtas ? 1 : n <= 2 * kSortThreads * kSortCtas ? 2 : 4;
     int ctas = 1;
     while (static_cast<int64_t>(ctas) * kSortThreads * per < n) ctas *= 2;
     if (per == 1) return launch_sort<1>(p, o, digits, ctas, s);
     if (per == 2) return launch_sort<2>(p, o, digits, ctas, s);
-    if (per == 4) return launch_sort<4>(p, o, digits, ctas, s);
-    return launch_sort<8>(p, o, digits, ctas, s);
+    return launch_sort<4>(p, o, digits, ctas, s);
   }
   p.tiles = (n + kSortTile - 1) / kSortTile;
   p.counts = reinterpret_cast<uint32_t*>(ws + l.counts);
@@ -689,24 +744,26 @@ cudaError_t sort_samples(const EmbedLayout& l, char* ws, const sfb_embed_config&
   if (e == cudaSuccess) e = sfb::launch_kernel(sort_clear_kernel, dim3(static_cast<unsigned>(std::max<int64_t>(1, (o.words + 255) / 256))), dim3(256), 0, s, 1, o);
   for (int d = 0; d < digits && e == cudaSuccess; ++d) {
     const int to = (digits - 1 - d) & 1;
-    p.keys_out = o.keys[to];
-    p.at_out = o.at[to];
+    p.out = o.entries[to];
     p.shift = d * p.bits;
     const dim3 tiles(static_cast<unsigned>(p.tiles));
     e = sfb::launch_kernel(sort_count_kernel, tiles, dim3(kSortThreads), sizeof(SortShared), s, 1, p, o);
     if (e == cudaSuccess) e = sfb::launch_kernel(sort_sum_kernel, dim3(((1 << p.bits) + 7) / 8), dim3(256), 0, s, 1, p);
     if (e == cudaSuccess) e = sfb::launch_kernel(sort_move_kernel, tiles, dim3(kSortThreads), sizeof(SortShared), s, 1, p);
     p.ids = nullptr;
-    p.keys_in = p.keys_out;
-    p.at_in = p.at_out;
+    p.in = p.out;
   }
   return e;
 }
 
+template <typename T, bool DROP>
+cudaError_t launch_gradient(const GradientParams& p, unsigned blocks, cudaStream_t s) {
+  return p.add ? sfb::launch_kernel(gradient_kernel<T, DROP, true>, dim3(blocks), dim3(kThreads), 0, s, 1, p)
+               : sfb::launch_kernel(gradient_kernel<T, DROP, false>, dim3(blocks), dim3(kThreads), 0, s, 1, p);
+}
 template <typename T>
 cudaError_t launch_gradient(const GradientParams& p, bool drop, unsigned blocks, cudaStream_t s) {
-  return drop ? sfb::launch_kernel(gradient_kernel<T, true>, dim3(blocks), dim3(kThreads), 0, s, 1, p)
-              : sfb::launch_kernel(gradient_kernel<T, false>, dim3(blocks), dim3(kThreads), 0, s, 1, p);
+  return drop ? launch_gradient<T, true>(p, blocks, s) : launch_gradient<T, false>(p, blocks, s);
 }
 
 }  // namespace
@@ -723,6 +780,7 @@ extern "C" int sfb_dropout_init(float p, const uint64_t* rng_dev, void* stream, 
   if (!h) return SFB_ERR_ARG;
   h->drop.rng = rng_dev;
   h->drop.threshold = static_cast<uint32_t>(std::nearbyint(static_cast<double>(p) * 65536.0));
+  h->drop.last = (h->drop.threshold << 16) - 1;        // (of 65536: all ones)
   h->drop.factor = h->drop.threshold < 65536 ? static_cast<float>(65536.0 / (65536.0 - h->drop.threshold)) : 0.f;
   h->stream = static_cast<cudaStream_t>(stream);
   h->device = dev;
@@ -736,13 +794,15 @@ extern "C" int sfb_dropout_apply(sfb_dropout* h, uint64_t call, int64_t n, int64
   if (n == 0) return SFB_OK;
   if (!X_dev || !Y_dev) return SFB_ERR_ARG;
   if (!R_dev) ldr = ldx;
-  if (n > (1ll << 32) || cols > (1ll << 30) || ldx < cols || ldy < cols || ldr < cols) return SFB_ERR_SHAPE;
+  if (cols > (1ll << 30) || ldx < cols || ldy < cols || ldr < cols) return SFB_ERR_SHAPE;
+  if (!fits(n, ldx, dtype) || !fits(n, ldy, dtype) || !fits(n, ldr, dtype)) return SFB_ERR_SHAPE;
   if (!sfb::lies_aligned(X_dev, dtype) || !sfb::lies_aligned(Y_dev, dtype) || !sfb::lies_aligned(R_dev, dtype)) return SFB_ERR_ALIGN;
   const int64_t groups = groups_of(cols);
   if (n > kBlocksMost / groups * kThreads) return SFB_ERR_SHAPE;
   const OnDevice on(h->device);
   if (on.err != cudaSuccess) return fail(h, on.err);
-  DropoutParams p{X_dev, R_dev, Y_dev, ldx, ldr, ldy, n, cols, Divisor(static_cast<uint32_t>(groups)), false, h->drop};
+  const int64_t size = static_cast<int64_t>(sfb::size_of(dtype));
+  DropoutParams p{X_dev, R_dev, Y_dev, grid_of(n, cols), static_cast<uint32_t>(ldx * size), static_cast<uint32_t>(ldr * size), static_cast<uint32_t>(ldy * size), false, h->drop};
   p.wide = sfb::lies_wide(X_dev, ldx, dtype) && sfb::lies_wide(Y_dev, ldy, dtype) && (!R_dev || sfb::lies_wide(R_dev, ldr, dtype));
   p.drop.call = call;
   const cudaError_t e = dtype == SFB_F32 ? launch_dropout<float>(p, h->stream)
@@ -800,20 +860,18 @@ extern "C" int sfb_embed_forward(sfb_embed* h, int64_t n, const int32_t* ids_dev
   if (!ids_dev || !X_dev) return SFB_ERR_ARG;
   if (ldx < c.dim) return SFB_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(ids_dev) & 3u) || !sfb::lies_aligned(X_dev, c.out_dtype)) return SFB_ERR_ALIGN;
-  if (n > kBlocksMost / groups_of(c.dim) * kThreads) return SFB_ERR_SHAPE;
+  if (n > kBlocksMost / groups_of(c.dim) * kThreads || !fits(n, ldx, c.out_dtype)) return SFB_ERR_SHAPE;
   const OnDevice on(h->device);
   if (on.err != cudaSuccess) return fail(h, on.err);
   const bool drops = drop && drop->drop.threshold > 0;
   RowsParams p{};
   p.table = h->table;
-  p.ldt = c.ldt;
-  p.tokens = c.tokens;
-  p.n = n;
-  p.dim = c.dim;
-  p.ids = ids_dev;
   p.out = X_dev;
-  p.ldo = ldx;
-  p.groups = Divisor(static_cast<uint32_t>(groups_of(c.dim)));
+  p.ids = ids_dev;
+  p.grid = grid_of(n, c.dim);
+  p.tokens = static_cast<uint32_t>(c.tokens);
+  p.pitch_in = static_cast<uint32_t>(c.ldt * static_cast<int64_t>(sfb::size_of(c.table_dtype)));
+  p.pitch_out = static_cast<uint32_t>(ldx * static_cast<int64_t>(sfb::size_of(c.out_dtype)));
   p.factor = c.scale * (drops ? drop->drop.factor : 1.f);
   p.wide_in = sfb::lies_wide(h->table, c.ldt, c.table_dtype);
   p.wide_out = sfb::lies_wide(X_dev, ldx, c.out_dtype);
@@ -842,10 +900,7 @@ extern "C" int sfb_embed_backward(sfb_embed* h, int64_t n, const int32_t* ids_de
   const EmbedLayout l = layout_of(c);
   const bool drops = drop && drop->drop.threshold > 0;
   Order o{};
-  for (int k = 0; k < 2; ++k) {
-    o.keys[k] = reinterpret_cast<uint32_t*>(h->ws + l.keys[k]);
-    o.at[k] = reinterpret_cast<uint32_t*>(h->ws + l.at[k]);
-  }
+  for (int k = 0; k < 2; ++k) o.entries[k] = reinterpret_cast<uint2*>(h->ws + l.entries[k]);
   o.touched = reinterpret_cast<uint32_t*>(h->ws + l.touched);
   o.crossing = reinterpret_cast<uint32_t*>(h->ws + l.crossing);
   o.words = add ? 0 : l.words;
@@ -854,8 +909,7 @@ extern "C" int sfb_embed_backward(sfb_embed* h, int64_t n, const int32_t* ids_de
                         : sfb::launch_kernel(sort_clear_kernel, dim3(static_cast<unsigned>(std::max<int64_t>(1, (o.words + 255) / 256))), dim3(256), 0, s, 1, o);
   if (e != cudaSuccess) return fail(h, e);
   GradientParams p{};
-  p.keys = o.keys[0];
-  p.at = o.at[0];
+  p.order = o.entries[0];
   p.touched = o.touched;
   p.crossing = o.crossing;
   p.parts = reinterpret_cast<float*>(h->ws + l.parts);
@@ -864,9 +918,9 @@ extern "C" int sfb_embed_backward(sfb_embed* h, int64_t n, const int32_t* ids_de
   p.per = samples_per_chunk(n, p.groups.d);
   p.chunks = static_cast<uint32_t>((n + p.per - 1) / p.per);
   const int64_t work = (static_cast<int64_t>(p.chunks) * p.groups.d + kThreads - 1) / kThreads;
-  const int64_t zero = add ? 0 : (c.tokens * p.groups.d + kThreads * 4 - 1) / (kThreads * 4);
+  const int64_t zero = add ? 0 : std::min<int64_t>((c.tokens + 31) / 32, sfb::sm_count());
   if (work * kThreads > kBlocksMost || work + zero > kBlocksMost) return SFB_ERR_SHAPE;
-  p.work = static_cast<uint32_t>(work);
+  p.zero = static_cast<uint32_t>(zero);
   p.tokens = static_cast<uint32_t>(c.tokens);
   p.dx = dX_dev;
   p.lddx = lddx;

@@ -103,6 +103,17 @@ cudaError_t allow_smem(int bytes) {
   if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
   return e;
 }
+// Clusters of more than eight CTAs are there for kernels that ask for them, once per device.
+template <auto Kernel>
+cudaError_t allow_clusters() {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (done.load(std::memory_order_acquire) >> (dev & 63) & 1)) return e;
+  e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) done.fetch_or(1ull << (dev & 63), std::memory_order_release);
+  return e;
+}
 #endif
 
 // ---------------------------------------------------------------------------------------------------------

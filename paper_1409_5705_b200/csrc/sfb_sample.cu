@@ -1,23 +1,21 @@
 // One class drawn for each row of logits (sfb_sample in sfb.h).
 //
-// A cluster of up to eight CTAs has a row.  The row is read once, into shared memory (what does not fit there is read again), and then
-// gone over as often as the filters want:
-//   1. the largest logit m and the first place that has it (all that a greedy answer takes)
-//   2. (top-k, top-p) how many logits lie in each 1/32 of (m - z) / T below 32: 1024 counts
-//   3. (top-k) counts of ordered keys within the part of 2 that holds the k-th largest, until a bin is a single key
-//   4. (top-p) bounds on the sums of weights by 2 say within which keys the nucleus ends; the weights of these are summed by key until a
-//      bin is a single key
-//   5. sums of the weights that are kept by warp, whose shares of the row follow one another: prefix sums say which warp the random
+// A cluster of CTAs has a row.  The row is read once, into shared memory (what does not fit there is read again), and then gone over as
+// often as the filters want:
+//   1. the largest logit m (all that a greedy answer takes, but for its place)
+//   2. (top-k, top-p) counts of the logits by their distance from m, in up to 1024 bins
+//   3. (top-k) the bin of the k-th largest; (top-p) between which bins the nucleus ends, by bounds on what weights of a bin can come to
+//   4. where what lies up to there is as many logits as there are bins, or fewer, they are gathered, sorted, and the rest follows from prefix sums over them
+//   5. else the logits of the bins in question alone, once they are that few; until then they are counted (or their weights summed) by ordered
+//      key in bins of fewer and fewer keys.  Out comes a key and how many of the logits with that key are kept, the first ones: all
+//      filters keep a beginning of the order by falling logit and rising index.
+//   6. sums of the weights that are kept by warp, whose shares of the row follow one another: prefix sums say which warp the random
 //      number falls on, and that warp goes over its share once more
-// A filter's result is a key and how many of the logits with that key are kept, the first ones: all filters keep a beginning of the
-// order by falling logit and rising index.
 //
 // Whole numbers come out: a class is right or wrong.  So the weights exp((z - m) / T) are taken in 64 bits (an error of 1e-7 in a sum over
-// 325,000 classes would move one draw in a hundred to the class beside), by a table of 64 powers of two and a polynomial of the fourth
-// degree: ten operations, 4e-14.  Sums by key are whole numbers (2^-F of the largest weight), so that their order changes nothing; the
+// 325,000 classes would move one draw in a hundred to the class beside), by a table of 256 powers of two and a polynomial of the third
+// degree: eight operations, 2e-13.  Sums by key are whole numbers (2^-F of the largest weight), so that their order changes nothing; the
 // others are added in a fixed order.
-//
-// Bound by HBM (the row, once) where little is kept, by the 64-bit unit where all classes are weighed: 0.16 cycles an SM and class.
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -29,11 +27,16 @@ namespace {
 using sfb::pdl_launch_dependents;
 using sfb::pdl_wait;
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kBins = 1024, kEach = kBins / kThreads;
-constexpr float kPerUnit = 32.f;             // bins of 2 in a factor e
+// What follows from the threads of a CTA (N): two bins, and two places of the list of logits that are gathered, for each.
+constexpr int kEach = 2;
+template <int N>
+struct Of {
+  static constexpr int kWarps = N / 32, kBins = kEach * N, kList = kEach * N;
+};
+constexpr float kWidest = 32.f;              // bins of 2 reach to e^-32 of the largest weight at most
 constexpr float kFar = 45.f;                 // weights below e^-45 of the largest count as zero: all of them together are below 1e-13
-constexpr int kMaxCtas = 8;
+constexpr int kMaxCtas = 16;                 // (more than eight: a launch that asks for them)
+constexpr int kTable = 256;
 
 struct SampleParams {
   const void* z;
@@ -47,17 +50,61 @@ struct SampleParams {
   bool wide;
 };
 
+constexpr float kNone = -INFINITY, kLargest = 3.4028234663852886e38f;
+
+// ---- types -------------------------------------------------------------------------------------------------------------------------
+// kLow: bits of an fp32 word that such a value leaves zero.  A vector's largest value (which is no NaN where one is not), and a running
+// smallest one, which is NaN from the first NaN on.
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 template <typename T> struct Type;
-template <> struct Type<float> { static constexpr int kLow = 0; };           // bits of an fp32 word that such a value leaves zero
-template <> struct Type<__nv_bfloat16> { static constexpr int kLow = 16; };
-template <> struct Type<__half> { static constexpr int kLow = 13; };
+template <> struct Type<float> {
+  static constexpr int kLow = 0;
+  using Pair = float;
+  static __device__ __forceinline__ Pair most(const uint4& w) {
+    return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
+  }
+  static __device__ __forceinline__ Pair least(const uint4& w, Pair so_far) {
+    return min_nan(min_nan(so_far, min_nan(__uint_as_float(w.x), __uint_as_float(w.y))), min_nan(__uint_as_float(w.z), __uint_as_float(w.w)));
+  }
+  static __device__ __forceinline__ Pair all(float v) { return v; }
+  static __device__ __forceinline__ Pair larger(Pair a, Pair b) { return fmaxf(a, b); }
+  static __device__ __forceinline__ float largest(Pair v) { return v; }
+  static __device__ __forceinline__ float smallest(Pair v) { return v; }
+};
+#define SFB_SAMPLE_TYPE(T, T2, LOW, BOTH, FLOAT)                                                                                    \
+  template <> struct Type<T> {                                                                                                      \
+    static constexpr int kLow = LOW;                                                                                                \
+    using Pair = T2;                                                                                                                \
+    static __device__ __forceinline__ T2 of(uint32_t w) { return *reinterpret_cast<T2*>(&w); }                                      \
+    static __device__ __forceinline__ T2 most(const uint4& w) { return __hmax2(__hmax2(of(w.x), of(w.y)), __hmax2(of(w.z), of(w.w))); } \
+    static __device__ __forceinline__ T2 least(const uint4& w, T2 so_far) {                                                         \
+      return __hmin2_nan(__hmin2_nan(so_far, __hmin2_nan(of(w.x), of(w.y))), __hmin2_nan(of(w.z), of(w.w)));                        \
+    }                                                                                                                               \
+    static __device__ __forceinline__ T2 all(float v) { return BOTH(v, v); }                                                        \
+    static __device__ __forceinline__ T2 larger(T2 a, T2 b) { return __hmax2(a, b); }                                               \
+    static __device__ __forceinline__ float largest(T2 v) { return fmaxf(FLOAT(__low2##LOW(v)), FLOAT(__high2##LOW(v))); }          \
+    static __device__ __forceinline__ float smallest(T2 v) { return min_nan(FLOAT(__low2##LOW(v)), FLOAT(__high2##LOW(v))); }       \
+  };
+#define __low216 __low2bfloat16
+#define __high216 __high2bfloat16
+#define __low213 __low2half
+#define __high213 __high2half
+SFB_SAMPLE_TYPE(__nv_bfloat16, __nv_bfloat162, 16, __floats2bfloat162_rn, __bfloat162float)
+SFB_SAMPLE_TYPE(__half, __half2, 13, __floats2half2_rn, __half2float)
+#undef __low216
+#undef __high216
+#undef __low213
+#undef __high213
+#undef SFB_SAMPLE_TYPE
 
-constexpr float kNone = -INFINITY;
-
-// Ordered like the values.
+// Whole numbers that are ordered like the values (-0 counts as 0).
 template <int LOW>
 __device__ __forceinline__ uint32_t key_of(float z) {
-  const uint32_t u = __float_as_uint(z);
+  const uint32_t u = __float_as_uint(z + 0.f);
   return (u >> 31 ? ~u : u | 0x80000000u) >> LOW;
 }
 template <int LOW>
@@ -66,28 +113,40 @@ __device__ __forceinline__ float value_of(uint32_t key) {
   return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~(u | ((1u << LOW) - 1)));
 }
 
+// ---- shared memory -------------------------------------------------------------------------------------------------------------------
+template <int N>
 struct Shared {
+  static constexpr int kBins = Of<N>::kBins, kList = Of<N>::kList, kWarps = Of<N>::kWarps;
   union {
     uint32_t count[kBins];
     unsigned long long mass[kBins];
+    unsigned long long list[kList];          // of this CTA
   };
-  double power[64];                          // 2^(j / 64)
+  union {
+    unsigned long long order[kList];         // of all of the row's CTAs (also parts of the bins' sums)
+    struct {                                 // of the row's warps, in their order: what is kept ahead of each
+      double upto[kMaxCtas * kWarps];
+      uint32_t ties_ahead[kMaxCtas * kWarps];
+    };
+  };
+  unsigned long long value[kList];           // (bits of) weights of the order (also this CTA's share of the bins, summed over the row)
+  double power[kTable];                      // 2^(j / 256)
   double scan[kWarps];                       // (also of the other types that are scanned)
-  unsigned long long best;                   // of this CTA: key of the largest, ~ its index
-  unsigned long long warp_best[kWarps];
-  double above, all;                         // of this CTA: weights above the keys looked at; all kept ones
-  uint32_t above_count;
-  double warp_above[kWarps], warp_all[kWarps];
-  uint32_t warp_count[kWarps];
-  double sum[kWarps];                        // of this CTA's warps: what is kept, but for the last key, of which there are `ties`
-  uint32_t ties[kWarps], keeps[kWarps];
-  uint32_t found[2];
+  double part[2][kWarps];
+  uint32_t part_count[kWarps];
+  float part_most[kWarps], part_least[kWarps], part_gate[kWarps];
+  uint32_t listed, found[2], first;
+  uint32_t low_before;
   double found_at;
-  // the row's warps, in their order
-  double upto[kMaxCtas * kWarps];
-  uint32_t ties_ahead[kMaxCtas * kWarps];
+  // what the row's CTAs have written here
+  float most[kMaxCtas], least[kMaxCtas];
+  double sums[2][kMaxCtas];
+  uint32_t counts[kMaxCtas];
+  float gates[kMaxCtas];
+  // the row's warps, in their order: what is kept, but for the last key, of which there are `ties`
+  double sum[kMaxCtas * kWarps];
+  uint32_t ties[kMaxCtas * kWarps], keeps[kMaxCtas * kWarps];
   double total;
-  uint32_t kept;
   int32_t winner;
 };
 
@@ -106,10 +165,12 @@ __device__ __forceinline__ unsigned long long read(const unsigned long long* her
   asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(remote(here, cta)) : "memory");
   return v;
 }
-__device__ __forceinline__ double read(const double* here, int cta) {
-  double v;
-  asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(remote(here, cta)) : "memory");
-  return v;
+__device__ __forceinline__ void write(uint32_t* here, int cta, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(remote(here, cta)), "r"(v) : "memory");
+}
+__device__ __forceinline__ void write(float* here, int cta, float v) { write(reinterpret_cast<uint32_t*>(here), cta, __float_as_uint(v)); }
+__device__ __forceinline__ void write(double* here, int cta, double v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(remote(here, cta)), "l"(__double_as_longlong(v)) : "memory");
 }
 // All of the row's threads.
 __device__ __forceinline__ void row_sync(int ctas) {
@@ -117,32 +178,41 @@ __device__ __forceinline__ void row_sync(int ctas) {
   else asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
 
-// exp((z - m) / T).
+// ---- weights -------------------------------------------------------------------------------------------------------------------------
+// exp((z - m) / T), 0 for z below `far`.  Where m is infinite: 1 for such logits (m, per are 0 here and far is infinite).
 struct Weight {
   const double* power;
-  double m, per;                             // 64 log2(e) / T
-  float top, far;                            // m, and below which weights are zero
+  double m, per;                             // 256 log2(e) / T
+  float far;
   __device__ __forceinline__ double operator()(float z) const {
-    // t = (z - m) per = k + f, |f| <= 1/2: the sum with 1.5 * 2^52 leaves k in the low bits
-    const double d = static_cast<double>(z) - m;
+    // (z - m) per = k + f, |f| <= 1/2: the sum with 1.5 * 2^52 leaves k in the low bits
+    const double d = static_cast<double>(fminf(fmaxf(z, far), kLargest)) - m;
     const double shifted = fma(d, per, 6755399441055744.0);
     const int k = __double2loint(shifted);
-    const double f = fma(d, per, -(shifted - 6755399441055744.0));
-    // 2^(f / 64): (ln 2 / 64)^j / j!
-    constexpr double c1 = 0.6931471805599453 / 64, c2 = c1 * c1 / 2, c3 = c2 * c1 / 3, c4 = c3 * c1 / 4;
-    const double s = power[k & 63], e = fma(fma(fma(fma(c4, f, c3), f, c2), f, c1), f, 1.0);
-    const double r = s * e;
-    const double w = __hiloint2double(__double2hiint(r) + ((k >> 6) << 20), __double2loint(r));
-    return z == top ? 1.0 : z < far ? 0.0 : w;
+    const double f = fma(d, per, 6755399441055744.0 - shifted);
+    // 2^(f / 256): (ln 2 / 256)^j / j!
+    constexpr double c1 = 0.6931471805599453 / kTable, c2 = c1 * c1 / 2, c3 = c2 * c1 / 3;
+    const double e = fma(fma(fma(c3, f, c2), f, c1), f, 1.0);
+    const double t = power[k & (kTable - 1)];
+    const double s = __hiloint2double(__double2hiint(t) + ((k >> 8) << 20), __double2loint(t));
+    return z >= far ? s * e : 0.0;
   }
 };
 
 template <typename V>
 __device__ __forceinline__ V shuffle_up(V v, int o) { return __shfl_up_sync(0xffffffffu, v, o); }
+__device__ __forceinline__ uint32_t warp_sum(uint32_t v) { return __reduce_add_sync(0xffffffffu, v); }
+__device__ __forceinline__ double warp_sum(double v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
 
+// (Functions of their own, not copies at each call: a CTA goes through the kernel once, and waits for its instructions.)
 // What lies in the threads before this one; the whole in `all`.
-template <typename V>
-__device__ __forceinline__ V block_scan(Shared& s, V value, V& all) {
+template <int N, typename V>
+__device__ __noinline__ V block_scan(Shared<N>& s, V value, V& all) {
+  constexpr int kWarps = Of<N>::kWarps;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   V* part = reinterpret_cast<V*>(s.scan);
   V sum = value;
@@ -163,8 +233,42 @@ __device__ __forceinline__ V block_scan(Shared& s, V value, V& all) {
   all = whole;
   return ahead + sum - value;
 }
+// The threads' sum (of small whole numbers).
+template <int N>
+__device__ __noinline__ uint32_t block_sum(Shared<N>& s, uint32_t value) {
+  constexpr int kWarps = Of<N>::kWarps;
+  const uint32_t v = warp_sum(value);
+  if ((threadIdx.x & 31) == 0) s.part_count[threadIdx.x >> 5] = v;
+  __syncthreads();
+  uint32_t all = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) all += s.part_count[w];
+  __syncthreads();
+  return all;
+}
 
-// A CTA's share of a row.
+// Ascending, n of them padded to a power of two.  (Strides of 32 and less stay within what a warp has.)
+template <int N>
+__device__ __noinline__ void sort(unsigned long long* a, int n) {
+  int p = 64;
+  while (p < n) p <<= 1;
+  for (int i = n + threadIdx.x; i < p; i += N) a[i] = ~0ull;
+  __syncthreads();
+  for (int k = 2; k <= p; k <<= 1) {
+    for (int stride = k >> 1; stride > 0; stride >>= 1) {
+      for (int t = threadIdx.x; t < p / 2; t += N) {
+        const int i = 2 * t - (t & (stride - 1)), j = i + stride;
+        const unsigned long long x = a[i], y = a[j];
+        if ((x > y) == ((i & k) == 0)) a[i] = y, a[j] = x;
+      }
+      if (stride > 32 || (stride == 1 && 2 * k > 64)) __syncthreads();
+      else __syncwarp();
+    }
+  }
+  __syncthreads();
+}
+
+// ---- a CTA's share of a row ------------------------------------------------------------------------------------------------------------
 template <typename T>
 struct Slice {
   static constexpr int kV = 16 / sizeof(T);
@@ -183,40 +287,52 @@ struct Slice {
     for (int j = 0; j < kV; ++j) e[j] = at + j < entries ? z[at + j] : sfb::from_float<T>(kNone);
     return w;
   }
-  // No numbers count as minus infinity, and -0 as 0.
+  __device__ __forceinline__ uint4 vector(int i) const { return i < resident ? held[i] : fetch(i); }
   static __device__ __forceinline__ void widen(const uint4& w, float (&v)[kV]) {
     const T* e = reinterpret_cast<const T*>(&w);
 #pragma unroll
-    for (int j = 0; j < kV; ++j) v[j] = fmaxf(sfb::to_float(e[j]), kNone) + 0.f;
+    for (int j = 0; j < kV; ++j) v[j] = sfb::to_float(e[j]);
   }
-  __device__ __forceinline__ void values(int i, float (&v)[kV]) const { widen(i < resident ? held[i] : fetch(i), v); }
 };
 
-// Calls f(z) for the logits of a warp's vectors.
+// Calls f(z, place in the share) for the logits of a warp's vectors that are at least `gate`, one after another.
 template <typename T, typename F>
-__device__ __forceinline__ void each(const Slice<T>& s, int from, int to, F&& f) {
+__device__ __forceinline__ void each_hit(const Slice<T>& s, int from, int to, float gate, F&& f) {
   for (int i = from + (threadIdx.x & 31); i < to; i += 32) {
+    const uint4 w = s.vector(i);
+    if (!(Type<T>::largest(Type<T>::most(w)) >= gate)) continue;
     float v[Slice<T>::kV];
-    s.values(i, v);
+    Slice<T>::widen(w, v);
+    uint32_t hits = 0;
 #pragma unroll
-    for (int j = 0; j < Slice<T>::kV; ++j) f(v[j]);
+    for (int j = 0; j < Slice<T>::kV; ++j) hits |= (v[j] >= gate ? 1u : 0u) << j;
+#pragma unroll 1
+    for (; hits; hits &= hits - 1) {
+      const int at = i * Slice<T>::kV + __ffs(hits) - 1;
+      f(sfb::to_float(i < s.resident ? reinterpret_cast<const T*>(s.held)[at] : s.z[at]), at);
+    }
+  }
+}
+// Calls f(values) for the vectors that hold one.
+template <typename T, typename F>
+__device__ __forceinline__ void each_vector(const Slice<T>& s, int from, int to, float gate, F&& f) {
+#pragma unroll 1
+  for (int i = from + (threadIdx.x & 31); i < to; i += 32) {
+    const uint4 w = s.vector(i);
+    if (!(Type<T>::largest(Type<T>::most(w)) >= gate)) continue;
+    float v[Slice<T>::kV];
+    Slice<T>::widen(w, v);
+    f(v);
   }
 }
 
-__device__ __forceinline__ uint32_t warp_sum(uint32_t v) { return __reduce_add_sync(0xffffffffu, v); }
-__device__ __forceinline__ double warp_sum(double v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
-// A range of keys and what lies above it.
+// ---- keys ------------------------------------------------------------------------------------------------------------------------------
 struct Range { uint32_t low, high; };
 
 // The keys that bins [first, last] can hold (and some more beside them: the bins were found in 32 bits).
-template <int LOW>
+template <int LOW, int kBins>
 __device__ __forceinline__ Range range_of(float m, double unit, int first, int last) {
-  Range r{key_of<LOW>(-3.4028234663852886e38f), key_of<LOW>(m)};
+  Range r{key_of<LOW>(-kLargest), key_of<LOW>(m)};
   if (isinf(m)) {
     if (last == 0) r.low = r.high;
     return r;
@@ -230,23 +346,82 @@ __device__ __forceinline__ Range range_of(float m, double unit, int first, int l
   r.high = max(r.high, r.low);
   return r;
 }
+template <int kBins>
 __device__ __forceinline__ int shift_of(const Range& r) {
   const uint32_t width = r.high - r.low;     // the largest distance
-  return width < kBins ? 0 : 32 - __clz(width) - 10;
+  return width < kBins ? 0 : __clz(kBins) + 1 - __clz(width);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ SampleParams p) {
+// The bins' sums over the row's CTAs, two a thread.  Every CTA has passed a row_sync since it filled its own.  Each adds a share of the bins,
+// then all read the shares: a sixteenth of what it is if all read all.
+template <int N, typename V>
+__device__ __noinline__ void sum_bins(Shared<N>& s, const V* bins, int ctas, int cta, V (&out)[kEach]) {
+  if (ctas == 1) {
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) out[j] = bins[threadIdx.x * kEach + j];
+    __syncthreads();
+    return;
+  }
+  const int share = Of<N>::kBins / ctas, groups = N / share, mine = threadIdx.x % share, group = threadIdx.x / share;      // of two CTAs each
+  V* part = reinterpret_cast<V*>(s.order);
+  V* summed = reinterpret_cast<V*>(s.value);
+  part[threadIdx.x] = read(&bins[cta * share + mine], 2 * group) + read(&bins[cta * share + mine], 2 * group + 1);
+  __syncthreads();
+  if (threadIdx.x < share) {
+    V v = 0;
+    for (int g = 0; g < groups; ++g) v += part[g * share + threadIdx.x];
+    summed[threadIdx.x] = v;
+  }
+  row_sync(ctas);
+  const int owner = threadIdx.x * kEach / share, at = threadIdx.x * kEach % share;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) out[j] = read(&summed[at + j], owner);
+}
+
+// What the CTAs have listed, in the order of falling keys and rising places: (~key, place).  Returns how many; -1: more than `most`, or
+// than one of the lists holds.  (Every CTA has passed a row_sync since it listed.)
+template <int N>
+__device__ __noinline__ int collect(Shared<N>& s, unsigned long long* to, int most, int ctas, bool wanted) {
+  const int lane = threadIdx.x & 31;
+  const uint32_t n = lane < ctas ? read(&s.listed, lane) : 0;
+  uint32_t upto = n;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t v = shuffle_up(upto, o);
+    if (lane >= o) upto += v;
+  }
+  const uint32_t all = __shfl_sync(0xffffffffu, upto, 31);
+  if (all > most || __any_sync(0xffffffffu, n > Of<N>::kList)) return -1;
+  if (!wanted) return static_cast<int>(all);
+  for (uint32_t i0 = 0; i0 < all; i0 += N) {
+    const uint32_t i = i0 + threadIdx.x;
+    uint32_t c = 0, begin = 0;               // the CTA that has it: the first whose sum goes beyond it
+    for (int q = 0; q < ctas - 1; ++q) {
+      const uint32_t end = __shfl_sync(0xffffffffu, upto, q);
+      if (i >= end) c = q + 1, begin = end;
+    }
+    if (i < all) to[i] = read(&s.list[i - begin], c);
+  }
+  sort<N>(to, static_cast<int>(all));        // (begins with a barrier)
+  return static_cast<int>(all);
+}
+
+template <typename T, int N>
+__global__ void __launch_bounds__(N, 1024 / N) sample_kernel(const __grid_constant__ SampleParams p) {
   constexpr int LOW = Type<T>::kLow, kV = Slice<T>::kV;
   extern __shared__ __align__(16) unsigned char dynamic[];
-  __shared__ Shared s;
+  constexpr int kWarps = Of<N>::kWarps, kBins = Of<N>::kBins, kList = Of<N>::kList;
+  __shared__ Shared<N> s;
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (threadIdx.x < 64) s.power[threadIdx.x] = exp2(threadIdx.x / 64.0);
+  for (int i = threadIdx.x; i < kTable; i += N) s.power[i] = exp2(i / static_cast<double>(kTable));
+  if (threadIdx.x == 0) s.listed = 0, s.first = 0xffffffffu;
+  const int ctas = p.ctas;
+  if (ctas > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
   pdl_wait();
 
-  const int64_t row = blockIdx.x / p.ctas;
-  const int cta = blockIdx.x % p.ctas;
+  const int64_t row = blockIdx.x / ctas;
+  const int cta = blockIdx.x % ctas;
   const int64_t first = static_cast<int64_t>(cta) * p.share * kV;             // entry of the row
   Slice<T> slice;
   slice.z = static_cast<const T*>(p.z) + row * p.ldz + first;
@@ -257,12 +432,16 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   slice.wide = p.wide;
   const int per_warp = (p.share + kWarps - 1) / kWarps;
   const int from = min(warp * per_warp, slice.vectors), to = min(from + per_warp, slice.vectors);
+  const float temperature = p.temperature ? p.temperature[row] : 1.f;
+  const int32_t top_k = p.top_k ? p.top_k[row] : 0;
+  const float top_p = p.top_p ? p.top_p[row] : 1.f;
+  const double min_p = p.min_p ? fmin(1.0, fmax(0.0, static_cast<double>(p.min_p[row]))) : 0.0;
 
   // 1. the row comes in
-  unsigned long long best = 0;               // (minus infinity, which is above key 0, has no place)
+  float m, least, k_gate = -kLargest;        // at least top_k logits are no smaller than k_gate
   {
-    float most = kNone;
-    int at = -1;
+    typename Type<T>::Pair high = Type<T>::all(kNone), low = Type<T>::all(INFINITY);
+    float tail = INFINITY;
     for (int i = from + lane; i < to; i += 4 * 32) {
       uint4 w[4];
 #pragma unroll
@@ -272,104 +451,343 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       for (int q = 0; q < 4; ++q) {
         if (i + 32 * q >= to) break;
         if (i + 32 * q < slice.resident) slice.held[i + 32 * q] = w[q];
-        float v[kV];
-        Slice<T>::widen(w[q], v);
-#pragma unroll
-        for (int j = 0; j < kV; ++j)
-          if (v[j] > most) {
-            most = v[j];
-            at = (i + 32 * q) * kV + j;
-          }
+        high = Type<T>::larger(high, Type<T>::most(w[q]));
+        if (static_cast<int64_t>(i + 32 * q + 1) * kV <= slice.entries) {
+          low = Type<T>::least(w[q], low);
+        } else {                             // (what lies behind the row's end is minus infinity too, but no hole)
+          float v[kV];
+          Slice<T>::widen(w[q], v);
+          for (int j = 0; (i + 32 * q) * kV + j < slice.entries; ++j) tail = min_nan(tail, v[j]);
+        }
       }
     }
-    if (at >= 0) best = static_cast<unsigned long long>(key_of<LOW>(most)) << 32 | ~static_cast<uint32_t>(first + at);
+    m = fmaxf(Type<T>::largest(high), kNone);
+    // so many of each warp's lanes have a largest logit of at least the warp's gate that the warps together have top_k
+    const int64_t rounds = (static_cast<int64_t>(top_k) + ctas * kWarps - 1) / (ctas * kWarps);
+    float gate = kNone;
+    if (top_k > 1 && rounds <= 8) {
+      uint32_t key = key_of<0>(m), best = 0;
+      for (int q = 0; q < rounds; ++q) {
+        best = __reduce_max_sync(0xffffffffu, key);
+        if (lane == __ffs(__ballot_sync(0xffffffffu, key == best)) - 1) key = 0;
+      }
+      gate = value_of<0>(best);              // (where a warp has fewer logits: minus infinity, or what is no number)
+    }
+    least = min_nan(Type<T>::smallest(low), tail);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
-    if (lane == 0) s.warp_best[warp] = best;
+    for (int o = 16; o > 0; o >>= 1) {
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      least = min_nan(least, __shfl_xor_sync(0xffffffffu, least, o));
+    }
+    if (lane == 0) s.part_most[warp] = m, s.part_least[warp] = least, s.part_gate[warp] = gate;
     __syncthreads();
-    for (int w = 0; w < kWarps; ++w) best = max(best, s.warp_best[w]);
-    if (p.ctas > 1) {
-      if (threadIdx.x == 0) s.best = best;
-      row_sync(p.ctas);
-      for (int c = 0; c < p.ctas; ++c) best = max(best, read(&s.best, c));
+    m = s.part_most[0];
+    least = s.part_least[0];
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) m = fmaxf(m, s.part_most[w]), least = min_nan(least, s.part_least[w]);
+    gate = s.part_gate[0];
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) gate = min_nan(gate, s.part_gate[w]);
+    if (ctas > 1) {
+      asm volatile("barrier.cluster.wait;" ::: "memory");          // (all of the row's CTAs are there)
+      if (threadIdx.x < ctas)
+        write(&s.most[cta], threadIdx.x, m), write(&s.least[cta], threadIdx.x, least), write(&s.gates[cta], threadIdx.x, gate);
+      row_sync(ctas);
+      for (int c = 0; c < ctas; ++c) m = fmaxf(m, s.most[c]), least = min_nan(least, s.least[c]), gate = min_nan(gate, s.gates[c]);
     }
+    m += 0.f;
+    if (gate > k_gate) k_gate = gate;
   }
-  const float temperature = p.temperature ? p.temperature[row] : 1.f;
-  const int32_t top_k = p.top_k ? p.top_k[row] : 0;
-  const float top_p = p.top_p ? p.top_p[row] : 1.f;
-  const double min_p = p.min_p ? fmin(1.0, fmax(0.0, static_cast<double>(p.min_p[row]))) : 0.0;
-  if (best == 0 || !(temperature > 0.f) || top_k == 1 || top_p <= 0.f) {      // nothing to draw from, or nothing to draw
+  const bool holes = !(least > kNone);       // some logit is minus infinity or no number
+  if (m == kNone) {                          // nothing to draw from
     if (cta == 0 && threadIdx.x == 0) {
-      p.ids[row] = best ? static_cast<int32_t>(~static_cast<uint32_t>(best)) : -1;
-      if (p.logp) p.logp[row] = best ? 0.f : kNone;
-      if (p.kept) p.kept[row] = best ? 1 : 0;
+      p.ids[row] = -1;
+      if (p.logp) p.logp[row] = kNone;
+      if (p.kept) p.kept[row] = 0;
     }
-    row_sync(p.ctas);                        // (no CTA leaves while another reads its shared memory)
+    return;                                  // (nothing of another CTA's is read any more)
+  }
+  if (!(temperature > 0.f) || top_k == 1 || top_p <= 0.f) {                   // nothing to draw: the first place of m
+    uint32_t at = 0xffffffffu;
+    each_hit(slice, from, to, m, [&](float, int i) { at = min(at, static_cast<uint32_t>(first + i)); });
+    at = __reduce_min_sync(0xffffffffu, at);
+    if (lane == 0) atomicMin(&s.first, at);
+    __syncthreads();
+    if (threadIdx.x == 0 && ctas > 1) write(&s.counts[cta], 0, s.first);
+    row_sync(ctas);
+    if (cta == 0 && threadIdx.x == 0) {
+      at = s.first;
+      for (int c = 1; c < ctas; ++c) at = min(at, s.counts[c]);
+      p.ids[row] = static_cast<int32_t>(at);
+      if (p.logp) p.logp[row] = 0.f;
+      if (p.kept) p.kept[row] = 1;
+    }
     return;
   }
-  const float m = value_of<LOW>(static_cast<uint32_t>(best >> 32));
-  const Weight weight{s.power, m, 92.33248261893196 / temperature, m,
-                      isinf(m) ? m : m - kFar * temperature};                // 64 log2(e)
-  const double unit = static_cast<double>(temperature) / kPerUnit;
+  const bool endless = isinf(m);
+  const Weight weight{s.power, endless ? 0.0 : m, endless ? 0.0 : 369.3299304757463 / temperature,             // 256 log2(e)
+                      endless ? m : fmaxf(m - kFar * temperature, -kLargest)};
+  const double u = fmax(0.0, static_cast<double>(p.u[row]));
+  const bool nucleus = top_p < 1.f;
 
-  uint32_t last_key = 0, last_ties = 0xffffffffu;        // of what is kept: all above the key, and so many that have it
-  if (top_k > 0 || top_p < 1.f) {
-    // 2. counts by distance
-    for (int b = threadIdx.x; b < kBins; b += kThreads) s.count[b] = 0;
+  // Sums of this CTA's threads, to every CTA.
+  auto spread = [&](double a, double b, uint32_t n) {
+    a = warp_sum(a);
+    b = warp_sum(b);
+    n = warp_sum(n);
+    if (lane == 0) s.part[0][warp] = a, s.part[1][warp] = b, s.part_count[warp] = n;
     __syncthreads();
-    const float scale = fminf(kPerUnit / temperature, 1e30f);
-    each(slice, from, to, [&](float z) {
-      if (z == kNone) return;
-      const float x = z == m ? 0.f : isinf(m) ? kBins : fminf(m - z, 3.4028234663852886e38f) * scale;
-      atomicAdd(&s.count[min(static_cast<int>(fminf(x, kBins - 1.f)), kBins - 1)], 1u);
-    });
-    row_sync(p.ctas);
-    uint32_t count[kEach] = {}, before[kEach], mine = 0, finite;
-    for (int c = 0; c < p.ctas; ++c)
+    if (warp == 0) {
+      a = warp_sum(lane < kWarps ? s.part[0][lane] : 0.0);
+      b = warp_sum(lane < kWarps ? s.part[1][lane] : 0.0);
+      n = warp_sum(lane < kWarps ? s.part_count[lane] : 0u);
+      if (lane < ctas) write(&s.sums[0][cta], lane, a), write(&s.sums[1][cta], lane, b), write(&s.counts[cta], lane, n);
+    }
+  };
+  auto gathered = [&](double& a, double& b, uint32_t& n) {                    // (after a row_sync, and before the next)
+    a = b = 0.0;
+    n = 0;
+    for (int c = 0; c < ctas; ++c) a += s.sums[0][c], b += s.sums[1][c], n += s.counts[c];
+  };
+
+  // 2. counts by distance
+  bool cuts = false;                         // top-k leaves something out
+  uint32_t k = 0, k_bin = 0, k_before = 0, k_upto = 0, low_bin = 0, high_bin = 0, nucleus_before = 0, nucleus_upto = 0;
+  const bool filters = top_k > 0 || nucleus;
+  const float reach = holes ? kWidest : fminf(kWidest, fmaxf((m - least) / temperature, 1.f / 1024));
+  const float scale = endless ? 0.f : fminf(kBins / reach / temperature, 1e30f);                                 // bins a unit
+  const double unit = scale > 0.f ? 1.0 / scale : INFINITY, width = scale > 0.f ? unit / temperature : 0.0;      // in logits; in exponents
+  // (the difference first: m itself is in bin 0)
+  auto bin_of = [&](float z) {
+    return endless ? (z == m ? 0u : kBins - 1) : min(__float2uint_rz((m - z) * scale), static_cast<uint32_t>(kBins - 1));
+  };
+  if (filters) {
+    for (int b = threadIdx.x; b < kBins; b += N) s.count[b] = 0;
+    __syncthreads();
+    // (all logits; those from k_gate on, where they are top_k or more and nothing is asked of the others)
+    if (k_gate > -kLargest) {
+      each_hit(slice, from, to, k_gate, [&](float z, int) { atomicAdd(&s.count[bin_of(z)], 1u); });
+    } else {
+#pragma unroll 1
+      for (int i = from + lane; i < to; i += 32) {
+        float v[kV];
+        Slice<T>::widen(slice.vector(i), v);
 #pragma unroll
-      for (int j = 0; j < kEach; ++j) count[j] += read(&s.count[threadIdx.x * kEach + j], c);
+        for (int j = 0; j < kV; ++j)
+          if (v[j] > kNone) atomicAdd(&s.count[bin_of(v[j])], 1u);
+      }
+    }
+    row_sync(ctas);
+    uint32_t count[kEach], before[kEach], mine = 0, finite;
+    sum_bins(s, s.count, ctas, cta, count);
 #pragma unroll
     for (int j = 0; j < kEach; ++j) mine += count[j];
     before[0] = block_scan(s, mine, finite);
 #pragma unroll
     for (int j = 1; j < kEach; ++j) before[j] = before[j - 1] + count[j - 1];
-    if (threadIdx.x == 0) s.found[0] = 0;
-    row_sync(p.ctas);                        // the counts are read
 
-    // 3. the k-th largest
-    const bool cuts = top_k > 0 && static_cast<uint32_t>(top_k) < finite;
-    const uint32_t k = cuts ? static_cast<uint32_t>(top_k) : finite;
-    if (cuts) {
+    // 3. the bin of the k-th largest, and bins of the nucleus's end.  With S the sum of the weights, that is the first bin up to which they
+    // come to top_p S, or behind which (1 - top_p) S or less is left.  A bin's weights lie within a factor that is known: so what bins up to,
+    // or behind, which these sums have bounds.
+    cuts = top_k > 0 && (static_cast<uint32_t>(top_k) < finite || k_gate > -kLargest);
+    k = cuts ? static_cast<uint32_t>(top_k) : finite;
 #pragma unroll
-      for (int j = 0; j < kEach; ++j)
-        if (before[j] < k && before[j] + count[j] >= k) s.found[0] = threadIdx.x * kEach + j;
+    for (int j = 0; j < kEach; ++j)
+      if (before[j] < k && before[j] + count[j] >= k) {
+        s.found[0] = threadIdx.x * kEach + j;
+        s.found[1] = before[j] + count[j];
+        s.low_before = before[j];
+      }
+    __syncthreads();
+    k_bin = s.found[0];
+    nucleus_upto = k_upto = s.found[1];
+    nucleus_before = k_before = s.low_before;
+    low_bin = high_bin = k_bin;
+    if (nucleus) {
+      const double share = top_p, rest = 1.0 - share;
+      constexpr double slack = 1e-4;         // (of bins that were found in 32 bits)
+      double low = 0.0, high = 0.0, all_low, all_high, bin_low[kEach], bin_high[kEach];
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        const int b = threadIdx.x * kEach + j;
+        const uint32_t c = before[j] < k ? min(count[j], k - before[j]) : 0;
+        bin_low[j] = b < kBins - 1 ? c * static_cast<double>(__expf(static_cast<float>(-(b + 1) * width))) : 0.0;
+        // (the last bin: what lies beyond it too, and where the temperature is that high, differences beyond fp32)
+        bin_high[j] = c * (b < kBins - 1 || temperature < 1e36f ? static_cast<double>(__expf(static_cast<float>(-b * width))) : 1.0);
+        low += bin_low[j];
+        high += bin_high[j];
+      }
+      low = block_scan(s, low, all_low);
+      high = block_scan(s, high, all_high);
+      uint32_t early = 0, open = 0;
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        low += bin_low[j];
+        high += bin_high[j];
+        early += high * (1 + slack) < share * all_low || (all_low - low) * (1 - slack) > rest * all_high;
+        open += !(low * (1 - slack) >= share * all_high || (all_high - high) * (1 + slack) <= rest * all_low);
+      }
+      const uint32_t both = block_sum(s, early << 16 | open);
+      low_bin = min(both >> 16, k_bin);
+      high_bin = min(max(both & 0xffffu, low_bin), k_bin);
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        if (threadIdx.x * kEach + j == high_bin) s.found[1] = before[j] + count[j];
+        if (threadIdx.x * kEach + j == low_bin) s.low_before = before[j];
+      }
       __syncthreads();
-      Range r = range_of<LOW>(m, unit, s.found[0], s.found[0]);
-      for (;;) {
-        const int shift = shift_of(r);
-        __syncthreads();
-        for (int b = threadIdx.x; b < kBins; b += kThreads) s.count[b] = 0;
-        if (threadIdx.x == 0) s.found[0] = 0, s.found[1] = 1;
-        __syncthreads();
-        uint32_t above = 0;
-        each(slice, from, to, [&](float z) {
-          const uint32_t key = key_of<LOW>(z);
-          if (z == kNone || key < r.low) return;
-          if (key > r.high) ++above;
-          else atomicAdd(&s.count[(r.high - key) >> shift], 1u);
-        });
-        above = warp_sum(above);
-        if (lane == 0) s.warp_count[warp] = above;
-        row_sync(p.ctas);
-        uint32_t some[kEach] = {}, a = 0, whole, sum = 0;
-        for (int c = 0; c < p.ctas; ++c) {
+      nucleus_upto = s.found[1];
+      nucleus_before = s.low_before;
+    }
+  }
+
+  // the weights of all logits, where something takes their sum
+  double all = 0.0;
+  if (!cuts && (nucleus || min_p == 0.0)) {
+#pragma unroll 2
+    for (int i = from + lane; i < to; i += 32) {
+      float v[kV];
+      Slice<T>::widen(slice.vector(i), v);
 #pragma unroll
-          for (int j = 0; j < kEach; ++j) some[j] += read(&s.count[threadIdx.x * kEach + j], c);
-          a += warp_sum(lane < kWarps ? read(&s.warp_count[lane], c) : 0u);
+      for (int j = 0; j < kV; ++j) all += weight(v[j]);
+    }
+  }
+
+  uint32_t last_key = 0, last_ties = 0xffffffffu;        // of what is kept: all above the key, and so many that have it
+  if (filters) {
+    // Adds a logit to this CTA's list.
+    auto list = [&](float z, int i) {
+      const uint32_t at = atomicAdd(&s.listed, 1u);
+      if (at < kList) s.list[at] = static_cast<unsigned long long>(~key_of<LOW>(z)) << 32 | static_cast<uint32_t>(first + i);
+    };
+    double above = 0.0, whole = 0.0;
+    uint32_t none;
+    // 4. all that can be kept, where that is little enough for a list, which takes the place of CTA 0's share of the row
+    const int room = p.resident >= 2 * kList ? 2 * kList : kList;
+    if ((cuts ? k_upto : nucleus_upto) <= room) {
+      const uint32_t top_bin = cuts ? k_bin : high_bin;
+      const float gate = fmaxf(value_of<LOW>(range_of<LOW, kBins>(m, unit, 0, top_bin).low), k_gate);
+      each_hit(slice, from, to, gate, [&](float z, int i) {
+        if (z > kNone && bin_of(z) <= top_bin) list(z, i);
+      });
+      spread(all, 0.0, 0u);
+      row_sync(ctas);
+      gathered(whole, above, none);
+      unsigned long long* order = room > kList ? reinterpret_cast<unsigned long long*>(dynamic) : s.order;
+      double* value = room > kList ? reinterpret_cast<double*>(dynamic) + room : reinterpret_cast<double*>(s.value);
+      const int n_all = collect(s, order, room, ctas, cta == 0);
+      row_sync(ctas);                        // (the lists are read)
+      if (n_all >= 0) {
+        if (cta != 0) return;
+        const int n = min(n_all, static_cast<int>(min(k, static_cast<uint32_t>(room)))), per = (n + N - 1) / N, begin = threadIdx.x * per;
+        for (int i = threadIdx.x; i < n; i += N) value[i] = weight(value_of<LOW>(~static_cast<uint32_t>(order[i] >> 32)));
+        __syncthreads();
+        // threads have neighbours of the order
+        double ahead = 0.0, sum;
+        for (int i = begin; i < min(begin + per, n); ++i) ahead += value[i];
+        ahead = block_scan(s, ahead, sum);
+        const double target = static_cast<double>(top_p) * (cuts ? sum : whole);
+        uint32_t kept = 0;                   // (the first ones: each of the conditions holds for a beginning)
+        for (int i = begin; i < min(begin + per, n); ++i) {
+          kept += (i == 0 || !nucleus || ahead < target) && value[i] >= min_p;
+          ahead += value[i];
         }
+        kept = block_sum(s, kept);
+        // by rising place, with the place in the order
+        for (int i = threadIdx.x; i < kept; i += N) order[i] = order[i] << 32 | i;
+        sort<N>(order, kept);
+        const int each = (kept + N - 1) / N, start = threadIdx.x * each, end = min(start + each, static_cast<int>(kept));
+        ahead = 0.0;
+        for (int i = start; i < end; ++i) ahead += value[static_cast<uint32_t>(order[i])];
+        ahead = block_scan(s, ahead, sum);
+        // the first one up to and with which the weights exceed u of theirs; where rounding leaves none, the last one that has a weight
+        const double mark = u < 1.0 ? u * sum : INFINITY;
+        uint32_t passed = 0, drawable = 1;
+        for (int i = start; i < end; ++i) {
+          const double w = value[static_cast<uint32_t>(order[i])];
+          ahead += w;
+          if (w > 0.0) drawable = i + 1;
+          passed += !(ahead > mark);
+        }
+        drawable = __reduce_max_sync(0xffffffffu, drawable);
+        if (lane == 0) s.ties[warp] = drawable;
+        passed = block_sum(s, passed);
+        if (threadIdx.x == 0) {
+          for (int q = 0; q < kWarps; ++q) drawable = max(drawable, s.ties[q]);
+          const uint32_t i = min(passed, drawable - 1);
+          p.ids[row] = static_cast<int32_t>(order[i] >> 32);
+          if (p.logp) p.logp[row] = static_cast<float>(log(value[static_cast<uint32_t>(order[i])] / sum));
+          if (p.kept) p.kept[row] = static_cast<int32_t>(kept);
+        }
+        return;
+      }
+      if (threadIdx.x == 0) s.listed = 0;    // (too much in one CTA's share)
+      __syncthreads();
+    }
+
+    // All lists, sorted, to every CTA.  How many they are; -1: too many for one of them.
+    auto sorted = [&]() {                    // (after a row_sync)
+      const int n = collect(s, s.order, kList, ctas, true);
+      row_sync(ctas);                        // (the lists are read)
+      if (threadIdx.x == 0) s.listed = 0;
+      return n;
+    };
+    auto list_range = [&](const Range& r) {  // of keys; no more of them than a list holds
+      each_hit(slice, from, to, fmaxf(value_of<LOW>(r.low), k_gate), [&](float z, int i) {
+        const uint32_t key = key_of<LOW>(z);
+        if (key >= r.low && key <= r.high) list(z, i);
+      });
+      row_sync(ctas);
+      return sorted();
+    };
+    // Of a sorted list the entry that is the last one kept: its key, and how many of that key are kept with it.
+    auto ends_at = [&](int at) {
+      const uint32_t key = static_cast<uint32_t>(s.order[max(at, 0)] >> 32);
+      int begin = 0, end = max(at, 0);       // the first of that key
+      while (begin < end) {
+        const int mid = (begin + end) / 2;
+        if (static_cast<uint32_t>(s.order[mid] >> 32) < key) begin = mid + 1;
+        else end = mid;
+      }
+      last_key = ~key;
+      last_ties = at - begin + 1;
+    };
+
+    // 5. the k-th largest
+    if (cuts) {
+      Range r = range_of<LOW, kBins>(m, unit, k_bin, k_bin);
+      const bool few = k_upto - k_before <= kList;
+      if (few) {
+        each_hit(slice, from, to, fmaxf(value_of<LOW>(r.low), k_gate), [&](float z, int i) {
+          if (bin_of(z) == k_bin) list(z, i);
+        });
+        row_sync(ctas);
+        ends_at(min(static_cast<int>(k - k_before), sorted()) - 1);
+      }
+      while (!few) {
+        const int shift = shift_of<kBins>(r);
+        __syncthreads();
+        for (int b = threadIdx.x; b < kBins; b += N) s.count[b] = 0;
+        __syncthreads();
+        uint32_t over = 0;
+        each_hit(slice, from, to, fmaxf(value_of<LOW>(r.low), k_gate), [&](float z, int) {
+          const uint32_t key = key_of<LOW>(z);
+          if (key > r.high) ++over;
+          else if (key >= r.low) atomicAdd(&s.count[(r.high - key) >> shift], 1u);
+        });
+        spread(0.0, 0.0, over);
+        row_sync(ctas);
+        double unused;
+        uint32_t some[kEach], inside, sum = 0;
+        gathered(unused, unused, over);
+        sum_bins(s, s.count, ctas, cta, some);
 #pragma unroll
         for (int j = 0; j < kEach; ++j) sum += some[j];
-        a += block_scan(s, sum, whole);
+        uint32_t a = over + block_scan(s, sum, inside);
+        if (shift > 0 && inside <= kList) {
+          ends_at(min(static_cast<int>(k - over), list_range(r)) - 1);
+          break;
+        }
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
           if (a < k && a + some[j] >= k) {
@@ -378,7 +796,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
           }
           a += some[j];
         }
-        row_sync(p.ctas);                    // all is read, and found
+        __syncthreads();
         const uint32_t high = r.high - (s.found[0] << shift), span = (1u << shift) - 1;
         if (shift == 0) {
           last_key = high;
@@ -389,96 +807,114 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       }
     }
 
-    // 4. the nucleus.  With S the sum of the weights, it ends in the first bin up to which they come to top_p S, or behind which
-    // (1 - top_p) S or less is left.  A bin's weights lie within a factor of e^(1/32): what bins up to, or behind, which these sums have bounds.
-    if (top_p < 1.f) {
-      double low = 0.0, high = 0.0, all_low, all_high, bin_low[kEach], bin_high[kEach];
-#pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        const int b = threadIdx.x * kEach + j;
-        const uint32_t c = before[j] < k ? min(count[j], k - before[j]) : 0;
-        bin_low[j] = b < kBins - 1 ? c * static_cast<double>(expf(-(b + 1) / kPerUnit)) : 0.0;
-        bin_high[j] = c * static_cast<double>(expf(-b / kPerUnit));
-        low += bin_low[j];
-        high += bin_high[j];
-      }
-      low = block_scan(s, low, all_low);
-      high = block_scan(s, high, all_high);
-      __syncthreads();
-      if (threadIdx.x == 0) s.found[0] = s.found[1] = kBins - 1;
-      __syncthreads();
-      const double share = top_p, rest = 1.0 - share, slack = 1e-5;
-#pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        const uint32_t b = threadIdx.x * kEach + j;
-        low += bin_low[j];
-        high += bin_high[j];
-        const bool early = high * (1 + slack) < share * all_low || (all_low - low) * (1 - slack) > rest * all_high;
-        const bool enough = low * (1 - slack) >= share * all_high || (all_high - high) * (1 + slack) <= rest * all_low;
-        if (!early) atomicMin(&s.found[0], b);
-        if (enough) atomicMin(&s.found[1], b);
-      }
-      __syncthreads();
-      Range r = range_of<LOW>(m, unit, s.found[0], max(s.found[0], s.found[1]));
+    // the nucleus
+    if (nucleus) {
+      Range r = range_of<LOW, kBins>(m, unit, low_bin, high_bin);
       r.low = max(r.low, last_key);
       r.high = max(r.high, r.low);
       const uint32_t cut_key = last_key, cut_ties = last_ties;       // of top-k; key 0: none
       const double cut_weight = cuts ? weight(value_of<LOW>(cut_key)) : 0.0;
+      const float cut_value = cuts ? value_of<LOW>(cut_key) : kNone;
       const double grain = ldexp(1.0, p.fraction), back = ldexp(1.0, -p.fraction);
       double target = 0.0;
-      for (bool begins = true;; begins = false) {
-        const int shift = shift_of(r);
-        __syncthreads();
-        for (int b = threadIdx.x; b < kBins; b += kThreads) s.mass[b] = 0;
-        if (threadIdx.x == 0) s.found[0] = kBins, s.found[1] = 0;
-        __syncthreads();
-        double above = 0.0, all = 0.0;
-        each(slice, from, to, [&](float z) {
-          const uint32_t key = key_of<LOW>(z);
-          if (z == kNone || key <= cut_key || (!begins && key < r.low)) return;
-          const double w = weight(z);
-          all += w;
-          if (key > r.high) above += w;
-          else if (key >= r.low) atomicAdd(&s.mass[(r.high - key) >> shift], static_cast<unsigned long long>(__double2ll_rn(w * grain)));
-        });
-        above = warp_sum(above);
-        all = warp_sum(all);
-        if (lane == 0) s.warp_above[warp] = above, s.warp_all[warp] = all;
-        row_sync(p.ctas);
-        unsigned long long some[kEach] = {}, sum = 0, whole;
-        above = all = 0.0;
-        for (int c = 0; c < p.ctas; ++c) {
-#pragma unroll
-          for (int j = 0; j < kEach; ++j) some[j] += read(&s.mass[threadIdx.x * kEach + j], c);
-          above += warp_sum(lane < kWarps ? read(&s.warp_above[lane], c) : 0.0);
-          if (begins) all += warp_sum(lane < kWarps ? read(&s.warp_all[lane], c) : 0.0);
-        }
-        if (begins) target = share * (all + (cuts ? cut_ties * cut_weight : 0.0));
+      bool cut_inside = cuts && high_bin == k_bin;
+      // A sorted list of n logits that follow others with the sum `above`, behind them what top-k leaves of its last key (where that is in
+      // reach): where the target is met.
+      auto meet = [&](int n) {
+        double w[kEach], a = 0.0, listed;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-          if (cuts && cut_key >= r.low && cut_key <= r.high && (r.high - cut_key) >> shift == threadIdx.x * kEach + j)
+          const int i = threadIdx.x * kEach + j;
+          w[j] = i < n ? weight(value_of<LOW>(~static_cast<uint32_t>(s.order[i] >> 32))) : 0.0;
+          a += w[j];
+        }
+        a = above + block_scan(s, a, listed);
+        uint32_t passed = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+          a += w[j];
+          passed += threadIdx.x * kEach + j < n && !(a >= target);
+        }
+        passed = block_sum(s, passed);
+        if (static_cast<int>(passed) < n || (n > 0 && !cut_inside)) {
+          ends_at(min(static_cast<int>(passed), n - 1));
+        } else if (cut_inside) {
+          const double more = ceil((target - above - listed) / cut_weight);
+          last_key = cut_key;
+          last_ties = more >= cut_ties || !(cut_weight > 0.0) ? cut_ties : more > 1.0 ? static_cast<uint32_t>(more) : 1u;
+        } else {                             // (no logit where there are some)
+          last_key = r.high;
+          last_ties = 1;
+        }
+      };
+      // sums of the weights: of all that top-k leaves, and of those above the range (by bins at first, then by keys)
+      const bool few = nucleus_upto - nucleus_before <= kList;
+      int listed = -1;
+      for (bool begins = true;; begins = false) {
+        const int shift = shift_of<kBins>(r);
+        __syncthreads();
+        if (!few)
+          for (int b = threadIdx.x; b < kBins; b += N) s.mass[b] = 0;
+        __syncthreads();
+        double over = 0.0;
+        uint32_t inside = 0;
+        each_vector(slice, from, to, begins && cuts ? cut_value : value_of<LOW>(r.low), [&](const float (&v)[kV]) {
+#pragma unroll
+          for (int j = 0; j < kV; ++j) {
+            const double w = v[j] > cut_value ? weight(v[j]) : 0.0;
+            if (begins && cuts) all += w;
+            if (few ? bin_of(v[j]) < low_bin : key_of<LOW>(v[j]) > r.high) over += w;
+          }
+        });
+        each_hit(slice, from, to, value_of<LOW>(r.low), [&](float z, int i) {
+          if (!(z > cut_value)) return;      // (equal ones are added below)
+          if (few) {
+            const uint32_t bin = bin_of(z);
+            if (bin >= low_bin && bin <= high_bin) list(z, i);
+            return;
+          }
+          const uint32_t key = key_of<LOW>(z);
+          if (key < r.low || key > r.high) return;
+          ++inside;
+          atomicAdd(&s.mass[(r.high - key) >> shift], static_cast<unsigned long long>(__double2ll_rn(weight(z) * grain)));
+        });
+        spread(over, all, inside);
+        row_sync(ctas);
+        double sum_all;
+        gathered(above, sum_all, inside);
+        if (begins) target = static_cast<double>(top_p) * (sum_all + (cuts ? cut_ties * cut_weight : 0.0));
+        if (few) {
+          listed = sorted();
+          break;
+        }
+        unsigned long long some[kEach], sum = 0, mass;
+        sum_bins(s, s.mass, ctas, cta, some);
+        cut_inside = cuts && cut_key >= r.low && cut_key <= r.high;
+        if (shift > 0 && inside <= kList) {
+          listed = list_range(Range{max(r.low, cut_key + 1), r.high});
+          break;
+        }
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+          if (cut_inside && (r.high - cut_key) >> shift == threadIdx.x * kEach + j)
             some[j] += cut_ties * static_cast<unsigned long long>(__double2ll_rn(cut_weight * grain));
           sum += some[j];
         }
-        const unsigned long long ahead = block_scan(s, sum, whole);
-        unsigned long long upto = ahead;
+        unsigned long long ahead = block_scan(s, sum, mass);
+        // in whole numbers: what the target leaves for the bins, and at least one and at most what they hold, so that one thread finds it
+        const double left = ceil((target - above) * grain);
+        const unsigned long long want = min(left > 1.0 ? static_cast<unsigned long long>(left) : 1ull, mass);
+        if (mass == 0 && threadIdx.x == 0) s.found[0] = 0, s.found_at = above;       // (no weight in the range)
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-          upto += some[j];
-          if (some[j]) atomicMax(&s.found[1], threadIdx.x * kEach + j);
-          if (some[j] && above + upto * back >= target) atomicMin(&s.found[0], threadIdx.x * kEach + j);
+          if (ahead < want && ahead + some[j] >= want) {
+            s.found[0] = threadIdx.x * kEach + j;
+            s.found_at = above + ahead * back;
+          }
+          ahead += some[j];
         }
         __syncthreads();
-        const uint32_t bin = s.found[0] < kBins ? s.found[0] : s.found[1];   // (rounding may leave the target just beyond the last one)
-        if (bin / kEach == threadIdx.x) {
-          upto = ahead;
-#pragma unroll
-          for (int j = 0; j < kEach; ++j)
-            if (threadIdx.x * kEach + j < bin) upto += some[j];
-          s.found_at = above + upto * back;
-        }
-        row_sync(p.ctas);                    // all is read, and found
-        const uint32_t top = r.high - (bin << shift), span = (1u << shift) - 1;
+        const uint32_t top = r.high - (s.found[0] << shift), span = (1u << shift) - 1;
         if (shift == 0) {
           const double w = weight(value_of<LOW>(top)), ties = ceil((target - s.found_at) / w);
           last_key = top;
@@ -488,46 +924,61 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         }
         r = Range{max(r.low, top > span ? top - span : 0u), top};
       }
+      if (listed >= 0) meet(listed);
     }
   }
 
-  // 5. the draw
-  const double last_weight = last_key ? weight(value_of<LOW>(last_key)) : 0.0;
+  // 6. the draw
+  const float last_value = last_key ? value_of<LOW>(last_key) : kNone;
+  const double last_weight = last_key ? weight(last_value) : 0.0;
   if (last_weight < min_p) last_ties = 0;
   {
-    double sum = 0.0;
+    double sum = all;
     uint32_t keeps = 0, ties = 0;
-    each(slice, from, to, [&](float z) {
-      const uint32_t key = key_of<LOW>(z);
-      if (z == kNone || key < last_key) return;
-      if (key == last_key) {
-        ++ties;
-        return;
+    if (!last_key && min_p == 0.0) {
+      if (!holes) {
+        if (lane == 0) keeps = static_cast<uint32_t>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(to) * kV, slice.entries) - static_cast<int64_t>(from) * kV));
+      } else {
+        each_hit(slice, from, to, -kLargest, [&](float, int) { ++keeps; });
       }
-      const double w = weight(z);
-      if (w < min_p) return;
-      sum += w;
-      ++keeps;
-    });
+    } else {
+      // (a bound on logits that min-p keeps, in 32 bits: the weights decide)
+      float gate = last_key ? last_value : -kLargest;
+      if (min_p > 0.0 && !endless) {
+        const float by = m + temperature * (__logf(static_cast<float>(min_p)) - 1e-3f) - 1e-6f * fabsf(m);
+        if (by > gate) gate = by;            // (not where it is no number)
+      }
+      sum = 0.0;
+      each_vector(slice, from, to, gate, [&](const float (&v)[kV]) {
+#pragma unroll
+        for (int j = 0; j < kV; ++j) {
+          const double w = weight(v[j]);
+          const bool keep = v[j] > last_value && w >= min_p;                  // (minus infinity and what is no number is not above)
+          if (keep) sum += w;
+          keeps += keep;
+          ties += v[j] == last_value;
+        }
+      });
+    }
     sum = warp_sum(sum);
     keeps = warp_sum(keeps);
-    ties = warp_sum(ties);
-    if (lane == 0) s.sum[warp] = sum, s.keeps[warp] = keeps, s.ties[warp] = ties;
+    ties = last_key ? warp_sum(ties) : 0;
+    const int at = cta * kWarps + warp;
+    if (lane < ctas) write(&s.sum[at], lane, sum), write(&s.keeps[at], lane, keeps), write(&s.ties[at], lane, ties);
   }
-  row_sync(p.ctas);
-  const double u = fmax(0.0, static_cast<double>(p.u[row]));
+  row_sync(ctas);
   if (warp == 0) {                           // the row's warps, a few of them a lane
     constexpr int kMost = kMaxCtas * kWarps / 32;
-    const int each_lane = (p.ctas * kWarps + 31) / 32;
+    const int each_lane = (ctas * kWarps + 31) / 32;
     double sum[kMost], mine = 0.0;
     uint32_t ties[kMost], mine_ties = 0, kept = 0;
 #pragma unroll
     for (int j = 0; j < kMost; ++j) {
-      const int i = lane * each_lane + j, c = i / kWarps;
-      const bool there = j < each_lane && c < p.ctas;
-      sum[j] = there ? read(&s.sum[i % kWarps], c) : 0.0;
-      ties[j] = there ? read(&s.ties[i % kWarps], c) : 0u;
-      kept += there ? read(&s.keeps[i % kWarps], c) : 0u;
+      const int i = lane * each_lane + j;
+      const bool there = j < each_lane && i < ctas * kWarps;
+      sum[j] = there ? s.sum[i] : 0.0;
+      ties[j] = there ? s.ties[i] : 0u;
+      kept += there ? s.keeps[i] : 0u;
       mine_ties += ties[j];
     }
     uint32_t ties_ahead = mine_ties;
@@ -557,12 +1008,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     upto = shuffle_up(upto, 1);              // (not upto - mine: what one lane's sums end with, the next one's begin with)
     if (lane == 0) upto = 0.0;
     kept = warp_sum(kept);
-    const double target = u * total;
+    const double target = u < 1.0 ? u * total : INFINITY;
     int found = 0x7fffffff, last = -1;
 #pragma unroll
     for (int j = 0; j < kMost; ++j) {
       const int i = lane * each_lane + j;
-      if (j < each_lane && i < p.ctas * kWarps) {
+      if (j < each_lane && i < ctas * kWarps) {
         s.upto[i] = upto;
         s.ties_ahead[i] = first_ties[j];
         upto += sum[j];
@@ -583,7 +1034,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   __syncthreads();
   const int winner = s.winner;
   if (winner == cta * kWarps + warp) {
-    const double total = s.total, target = u * total;
+    const double total = s.total, target = u < 1.0 ? u * total : INFINITY;
     double upto = s.upto[winner];
     uint32_t seen = s.ties_ahead[winner];
     int at = -1, last_at = -1;               // of the slice
@@ -593,11 +1044,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       float v[kV];
       double w[kV], sum = 0.0;
       uint32_t ties = 0;
-      if (i < to) slice.values(i, v);
+      if (i < to) Slice<T>::widen(slice.vector(i), v);
 #pragma unroll
       for (int j = 0; j < kV; ++j) {
         if (i >= to) v[j] = kNone;
-        if (v[j] != kNone && key_of<LOW>(v[j]) == last_key) ++ties;
+        if (last_key && v[j] == last_value) ++ties;
       }
       uint32_t ahead = ties;
 #pragma unroll
@@ -610,12 +1061,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       seen += here;
 #pragma unroll
       for (int j = 0; j < kV; ++j) {
-        const uint32_t key = key_of<LOW>(v[j]);
         w[j] = 0.0;
-        if (v[j] == kNone || key < last_key) continue;
-        if (key == last_key) {
+        if (last_key && v[j] == last_value) {
           if (ahead++ < last_ties) w[j] = last_weight;
-        } else {
+        } else if (v[j] > last_value) {      // (minus infinity and what is no number is not)
           w[j] = weight(v[j]);
           if (w[j] < min_p) w[j] = 0.0;
         }
@@ -653,7 +1102,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       if (p.logp) p.logp[row] = static_cast<float>(log(last_w / total));
     }
   }
-  row_sync(p.ctas);                          // (no CTA leaves while another reads its shared memory)
 }
 
 }  // namespace
@@ -672,20 +1120,29 @@ int check(const sfb_sampler_config* c) {
   return SFB_OK;
 }
 
-constexpr int kHeldMost = 200 << 10;         // of a CTA's shared memory, for the row
-constexpr int kHeldTwo = 96 << 10;           // ... where two CTAs are to share an SM
+constexpr int kHeldMost = 192 << 10;         // of a CTA's shared memory, for the row
+constexpr int kHeldFour = 40 << 10;          // ... where four CTAs of half the threads are
+constexpr int kHeldTwo = 80 << 10;           // ... where two CTAs are to share an SM
+
+template <typename T, int N>
+cudaError_t launch(const SampleParams& p, int64_t n, cudaStream_t s) {
+  cudaError_t e = sfb::allow_smem<sample_kernel<T, N>>(kHeldMost);
+  if (e == cudaSuccess && p.ctas > 8) e = sfb::allow_clusters<sample_kernel<T, N>>();
+  if (e != cudaSuccess) return e;
+  return sfb::launch_kernel(sample_kernel<T, N>, dim3(static_cast<unsigned>(n * p.ctas)), dim3(N), static_cast<size_t>(p.resident) * 16, s, p.ctas, p);
+}
 
 template <typename T>
 cudaError_t launch(SampleParams p, int64_t n, cudaStream_t s) {
   const int64_t vectors = (p.classes * static_cast<int64_t>(sizeof(T)) + 15) / 16;
   // As many CTAs a row as leave room for two of them on an SM; more where there are few rows and enough of each.
   int ctas = 1;
-  while (ctas < kMaxCtas && (vectors * 16 > static_cast<int64_t>(kHeldTwo) * ctas || (n * ctas < sfb::kModelSms && vectors * 16 > (16 << 10) * ctas))) ctas *= 2;
+  while (ctas < 8 && vectors * 16 > static_cast<int64_t>(kHeldTwo) * ctas) ctas *= 2;
+  while (ctas < kMaxCtas && n * ctas * 2 <= sfb::kModelSms && vectors * 16 > (8 << 10) * ctas) ctas *= 2;
   p.ctas = ctas;
   p.share = static_cast<int32_t>((vectors + ctas - 1) / ctas);
   p.resident = std::min(p.share, kHeldMost / 16);
-  const cudaError_t e = sfb::allow_smem<sample_kernel<T>>(kHeldMost);
-  return e == cudaSuccess ? sfb::launch_kernel(sample_kernel<T>, dim3(static_cast<unsigned>(n * ctas)), dim3(kThreads), static_cast<size_t>(p.resident) * 16, s, ctas, p) : e;
+  return p.share <= kHeldFour / 16 && n * ctas > 2 * sfb::kModelSms ? launch<T, 256>(p, n, s) : launch<T, 512>(p, n, s);
 }
 
 }  // namespace
