@@ -461,8 +461,8 @@ int sfb_embed_destroy(sfb_embed* h);
  *    (log-probability 0, one kept); +infinity: all logits above -infinity alike.  top_k <= 0: off.  top_p >= 1 or NaN: off; <= 0: the first of
  *    the order.  min_p is taken into [0, 1] (NaN: 0).  u outside [0, 1) is taken to the next end (NaN: 0).
  *  - A logit of -infinity, or one that is not a number, is no class: it is neither kept nor drawn.  A row of such ones has ids = -1,
- *    logp = -infinity, kept = 0.  Where logits are +infinity, these alone have weight, 1 each.  Weights below e^-45 count as 0: such classes
- *    are kept where the filters say so, but not drawn.
+ *    logp = -infinity, kept = 0.  Where logits are +infinity, these alone have weight, 1 each.  Weights below e^-34 may count as 0: such
+ *    classes are kept where the filters say so, but not drawn.
  *  - Weights and their sums are in 64 bits, and the same from call to call; logp is rounded to fp32 at its end.
  *  - Z of dtype, any pitch ldz >= classes, aligned to its entries (rows on 16-byte boundaries are the faster ones); the arrays are contiguous.
  *    n = 0 .. max_samples.  Calls on one handle are not re-entrant. */

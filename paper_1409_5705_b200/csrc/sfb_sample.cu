@@ -37,6 +37,7 @@ constexpr float kWidest = 32.f;              // bins of 2 reach to e^-32 of the 
 constexpr float kFar = 45.f;                 // weights below e^-45 of the largest count as zero: all of them together are below 1e-13
 constexpr int kMaxCtas = 16;                 // (more than eight: a launch that asks for them)
 constexpr int kTable = 256;
+constexpr uint32_t kSmall = 256;             // logits that are compared each with each, at most
 
 struct SampleParams {
   const void* z;
@@ -138,6 +139,7 @@ struct Shared {
   uint32_t listed, found[2], first;
   uint32_t low_before;
   double found_at;
+  unsigned long long found_sum;
   // what the row's CTAs have written here
   float most[kMaxCtas], least[kMaxCtas];
   double sums[2][kMaxCtas];
@@ -223,15 +225,16 @@ __device__ __noinline__ V block_scan(Shared<N>& s, V value, V& all) {
   }
   if (lane == 31) part[warp] = sum;
   __syncthreads();
-  V ahead = 0, whole = 0;
+  V upto = lane < kWarps ? part[lane] : 0;
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    if (w == warp) ahead = whole;
-    whole += part[w];
+  for (int o = 1; o < kWarps; o <<= 1) {
+    const V v = shuffle_up(upto, o);
+    if (lane >= o) upto += v;
   }
+  all = __shfl_sync(0xffffffffu, upto, kWarps - 1);
+  const V ahead = __shfl_sync(0xffffffffu, upto, max(warp - 1, 0));
   __syncthreads();
-  all = whole;
-  return ahead + sum - value;
+  return (warp ? ahead : 0) + (sum - value);
 }
 // The threads' sum (of small whole numbers).
 template <int N>
@@ -240,9 +243,7 @@ __device__ __noinline__ uint32_t block_sum(Shared<N>& s, uint32_t value) {
   const uint32_t v = warp_sum(value);
   if ((threadIdx.x & 31) == 0) s.part_count[threadIdx.x >> 5] = v;
   __syncthreads();
-  uint32_t all = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) all += s.part_count[w];
+  const uint32_t all = warp_sum((threadIdx.x & 31) < kWarps ? s.part_count[threadIdx.x & 31] : 0u);
   __syncthreads();
   return all;
 }
@@ -378,10 +379,10 @@ __device__ __noinline__ void sum_bins(Shared<N>& s, const V* bins, int ctas, int
   for (int j = 0; j < kEach; ++j) out[j] = read(&summed[at + j], owner);
 }
 
-// What the CTAs have listed, in the order of falling keys and rising places: (~key, place).  Returns how many; -1: more than `most`, or
-// than one of the lists holds.  (Every CTA has passed a row_sync since it listed.)
-template <int N>
-__device__ __noinline__ int collect(Shared<N>& s, unsigned long long* to, int most, int ctas, bool wanted) {
+// Calls f(i, entry) for what the CTAs have listed, CTA by CTA.  Returns how many; -1: more than `most`, or than one of the lists holds.  (Every
+// CTA has passed a row_sync since it listed.)
+template <int N, typename F>
+__device__ __forceinline__ int from_lists(Shared<N>& s, int ctas, int most, bool wanted, F&& f) {
   const int lane = threadIdx.x & 31;
   const uint32_t n = lane < ctas ? read(&s.listed, lane) : 0;
   uint32_t upto = n;
@@ -400,14 +401,29 @@ __device__ __noinline__ int collect(Shared<N>& s, unsigned long long* to, int mo
       const uint32_t end = __shfl_sync(0xffffffffu, upto, q);
       if (i >= end) c = q + 1, begin = end;
     }
-    if (i < all) to[i] = read(&s.list[i - begin], c);
+    if (i < all) f(i, read(&s.list[i - begin], c));
   }
-  sort<N>(to, static_cast<int>(all));        // (begins with a barrier)
   return static_cast<int>(all);
 }
+// All lists in the order of falling keys and rising places, to s.order: entries (~key, place).
+template <int N>
+__device__ __noinline__ int collect(Shared<N>& s, int ctas) {
+  const int all = from_lists(s, ctas, Of<N>::kList, true, [&](uint32_t i, unsigned long long e) { s.order[i] = e; });
+  if (all >= 0) sort<N>(s.order, all);       // (begins with a barrier)
+  return all;
+}
+// All lists as they are: entries (logit, place).
+template <int N>
+__device__ __noinline__ int pull(Shared<N>& s, int ctas, int most, bool wanted, float* z, uint32_t* place) {
+  return from_lists(s, ctas, most, wanted, [&](uint32_t i, unsigned long long e) {
+    z[i] = __uint_as_float(static_cast<uint32_t>(e >> 32));
+    place[i] = static_cast<uint32_t>(e);
+  });
+}
 
-template <typename T, int N>
-__global__ void __launch_bounds__(N, 1024 / N) sample_kernel(const __grid_constant__ SampleParams p) {
+// FILTERS: top-k or top-p may be asked for (without them a smaller kernel, of which more threads fit an SM).
+template <typename T, int N, bool FILTERS>
+__global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(const __grid_constant__ SampleParams p) {
   constexpr int LOW = Type<T>::kLow, kV = Slice<T>::kV;
   extern __shared__ __align__(16) unsigned char dynamic[];
   constexpr int kWarps = Of<N>::kWarps, kBins = Of<N>::kBins, kList = Of<N>::kList;
@@ -433,8 +449,8 @@ __global__ void __launch_bounds__(N, 1024 / N) sample_kernel(const __grid_consta
   const int per_warp = (p.share + kWarps - 1) / kWarps;
   const int from = min(warp * per_warp, slice.vectors), to = min(from + per_warp, slice.vectors);
   const float temperature = p.temperature ? p.temperature[row] : 1.f;
-  const int32_t top_k = p.top_k ? p.top_k[row] : 0;
-  const float top_p = p.top_p ? p.top_p[row] : 1.f;
+  const int32_t top_k = FILTERS && p.top_k ? p.top_k[row] : 0;
+  const float top_p = FILTERS && p.top_p ? p.top_p[row] : 1.f;
   const double min_p = p.min_p ? fmin(1.0, fmax(0.0, static_cast<double>(p.min_p[row]))) : 0.0;
 
   // 1. the row comes in
@@ -553,7 +569,7 @@ __global__ void __launch_bounds__(N, 1024 / N) sample_kernel(const __grid_consta
   // 2. counts by distance
   bool cuts = false;                         // top-k leaves something out
   uint32_t k = 0, k_bin = 0, k_before = 0, k_upto = 0, low_bin = 0, high_bin = 0, nucleus_before = 0, nucleus_upto = 0;
-  const bool filters = top_k > 0 || nucleus;
+  const bool filters = FILTERS && (top_k > 0 || nucleus);
   const float reach = holes ? kWidest : fminf(kWidest, fmaxf((m - least) / temperature, 1.f / 1024));
   const float scale = endless ? 0.f : fminf(kBins / reach / temperature, 1e30f);                                 // bins a unit
   const double unit = scale > 0.f ? 1.0 / scale : INFINITY, width = scale > 0.f ? unit / temperature : 0.0;      // in logits; in exponents
@@ -604,16 +620,17 @@ __global__ void __launch_bounds__(N, 1024 / N) sample_kernel(const __grid_consta
     nucleus_before = k_before = s.low_before;
     low_bin = high_bin = k_bin;
     if (nucleus) {
-      const double share = top_p, rest = 1.0 - share;
-      constexpr double slack = 1e-4;         // (of bins that were found in 32 bits)
-      double low = 0.0, high = 0.0, all_low, all_high, bin_low[kEach], bin_high[kEach];
+      // (in fp32: sums of up to 1024 bins are off by less than 1e-5 of the whole, bins that were found in 32 bits by less than that)
+      const float share = top_p, rest = 1.f - share, per_bin = static_cast<float>(width);
+      constexpr float slack = 1e-4f, lost = 2e-5f;
+      float low = 0.f, high = 0.f, all_low, all_high, bin_low[kEach], bin_high[kEach];
 #pragma unroll
       for (int j = 0; j < kEach; ++j) {
         const int b = threadIdx.x * kEach + j;
         const uint32_t c = before[j] < k ? min(count[j], k - before[j]) : 0;
-        bin_low[j] = b < kBins - 1 ? c * static_cast<double>(__expf(static_cast<float>(-(b + 1) * width))) : 0.0;
+        bin_low[j] = b < kBins - 1 ? c * __expf(-(b + 1) * per_bin) : 0.f;
         // (the last bin: what lies beyond it too, and where the temperature is that high, differences beyond fp32)
-        bin_high[j] = c * (b < kBins - 1 || temperature < 1e36f ? static_cast<double>(__expf(static_cast<float>(-b * width))) : 1.0);
+        bin_high[j] = c * (b < kBins - 1 || temperature < 1e36f ? __expf(-b * per_bin) : 1.f);
         low += bin_low[j];
         high += bin_high[j];
       }
@@ -624,8 +641,8 @@ __global__ void __launch_bounds__(N, 1024 / N) sample_kernel(const __grid_consta
       for (int j = 0; j < kEach; ++j) {
         low += bin_low[j];
         high += bin_high[j];
-        early += high * (1 + slack) < share * all_low || (all_low - low) * (1 - slack) > rest * all_high;
-        open += !(low * (1 - slack) >= share * all_high || (all_high - high) * (1 + slack) <= rest * all_low);
+        early += (high + lost * all_high) * (1 + slack) < share * all_low || (all_low - low - lost * all_low) * (1 - slack) > rest * all_high;
+        open += !((low - lost * all_low) * (1 - slack) >= share * all_high || (all_high - high + lost * all_high) * (1 + slack) <= rest * all_low);
       }
       const uint32_t both = block_sum(s, early << 16 | open);
       low_bin = min(both >> 16, k_bin);
@@ -641,83 +658,183 @@ __global__ void __launch_bounds__(N, 1024 / N) sample_kernel(const __grid_consta
     }
   }
 
-  // the weights of all logits, where something takes their sum
-  double all = 0.0;
+  // The weights of all logits, where something takes their sum, and of those in the bins before the nucleus's end; what lies in the bins of that end
+  // is listed, where it is no more than a list holds (and not all that can be kept is listed below).
+  const int room = p.resident >= 2 * kList ? 2 * kList : p.resident >= kList ? kList : 0;
+  const bool listed_all = filters && (cuts ? k_upto : nucleus_upto) <= room && (!cuts || k_upto - k_before <= kSmall) && (!nucleus || nucleus_upto - nucleus_before <= kSmall);
+  const bool few = filters && nucleus && !cuts && !listed_all && nucleus_upto - nucleus_before <= kList;
+  // Adds a logit to this CTA's list.
+  auto list = [&](float z, int i) {
+    const uint32_t at = atomicAdd(&s.listed, 1u);
+    if (at < kList) s.list[at] = static_cast<unsigned long long>(~key_of<LOW>(z)) << 32 | static_cast<uint32_t>(first + i);
+  };
+  double all = 0.0, over = 0.0;
+  uint32_t over_count = 0;
   if (!cuts && (nucleus || min_p == 0.0)) {
-#pragma unroll 2
-    for (int i = from + lane; i < to; i += 32) {
-      float v[kV];
-      Slice<T>::widen(slice.vector(i), v);
+    if (few) {
+      const float low_edge = static_cast<float>(low_bin), high_edge = high_bin < kBins - 1 ? static_cast<float>(high_bin + 1) : INFINITY;
+#pragma unroll 1
+      for (int i = from + lane; i < to; i += 32) {
+        float v[kV];
+        Slice<T>::widen(slice.vector(i), v);
+        uint32_t hits = 0;
 #pragma unroll
-      for (int j = 0; j < kV; ++j) all += weight(v[j]);
+        for (int j = 0; j < kV; ++j) {
+          const double w = weight(v[j]);
+          const float x = endless ? (v[j] == m ? 0.f : INFINITY) : (m - v[j]) * scale;         // as bin_of has it
+          all += w;
+          if (x < low_edge && v[j] > kNone) over += w, ++over_count;
+          else if ((x < high_edge || high_bin == kBins - 1) && v[j] > kNone) hits |= 1u << j;
+        }
+        for (; hits; hits &= hits - 1) {
+          const int e = i * kV + __ffs(hits) - 1;
+          list(sfb::to_float(i < slice.resident ? reinterpret_cast<const T*>(slice.held)[e] : slice.z[e]), e);
+        }
+      }
+    } else {
+#pragma unroll 2
+      for (int i = from + lane; i < to; i += 32) {
+        float v[kV];
+        Slice<T>::widen(slice.vector(i), v);
+#pragma unroll
+        for (int j = 0; j < kV; ++j) all += weight(v[j]);
+      }
     }
   }
 
   uint32_t last_key = 0, last_ties = 0xffffffffu;        // of what is kept: all above the key, and so many that have it
+  int listed = -1;                           // in s.order, of the nucleus's end
   if (filters) {
-    // Adds a logit to this CTA's list.
-    auto list = [&](float z, int i) {
-      const uint32_t at = atomicAdd(&s.listed, 1u);
-      if (at < kList) s.list[at] = static_cast<unsigned long long>(~key_of<LOW>(z)) << 32 | static_cast<uint32_t>(first + i);
-    };
     double above = 0.0, whole = 0.0;
     uint32_t none;
-    // 4. all that can be kept, where that is little enough for a list, which takes the place of CTA 0's share of the row
-    const int room = p.resident >= 2 * kList ? 2 * kList : kList;
-    if ((cuts ? k_upto : nucleus_upto) <= room) {
+    // 4. all that can be kept, where that is little enough for a list, which takes the place of CTA 0's share of the row: there the filters' ends
+    // are found among the few logits of their bins, each compared with each.  Sums are whole numbers (2^-50 of the largest weight): in any order.
+    if (listed_all) {
       const uint32_t top_bin = cuts ? k_bin : high_bin;
       const float gate = fmaxf(value_of<LOW>(range_of<LOW, kBins>(m, unit, 0, top_bin).low), k_gate);
       each_hit(slice, from, to, gate, [&](float z, int i) {
-        if (z > kNone && bin_of(z) <= top_bin) list(z, i);
+        if (z <= kNone || bin_of(z) > top_bin) return;
+        const uint32_t at = atomicAdd(&s.listed, 1u);
+        if (at < kList) s.list[at] = static_cast<unsigned long long>(__float_as_uint(z + 0.f)) << 32 | static_cast<uint32_t>(first + i);
       });
       spread(all, 0.0, 0u);
       row_sync(ctas);
       gathered(whole, above, none);
-      unsigned long long* order = room > kList ? reinterpret_cast<unsigned long long*>(dynamic) : s.order;
-      double* value = room > kList ? reinterpret_cast<double*>(dynamic) + room : reinterpret_cast<double*>(s.value);
-      const int n_all = collect(s, order, room, ctas, cta == 0);
+      float* z_of = reinterpret_cast<float*>(dynamic);                        // of the list: logits, places, weights (2^63: out)
+      uint32_t* place_of = reinterpret_cast<uint32_t*>(dynamic) + room;
+      unsigned long long* value = reinterpret_cast<unsigned long long*>(dynamic) + room;
+      const int n = pull(s, ctas, room, cta == 0, z_of, place_of);
       row_sync(ctas);                        // (the lists are read)
-      if (n_all >= 0) {
+      if (n >= 0) {
         if (cta != 0) return;
-        const int n = min(n_all, static_cast<int>(min(k, static_cast<uint32_t>(room)))), per = (n + N - 1) / N, begin = threadIdx.x * per;
-        for (int i = threadIdx.x; i < n; i += N) value[i] = weight(value_of<LOW>(~static_cast<uint32_t>(order[i] >> 32)));
+        constexpr unsigned long long kOut = 1ull << 63;
+        constexpr double kGrain = 1125899906842624.0;
+        for (int i = threadIdx.x; i < n; i += N) value[i] = __double2ull_rn(weight(z_of[i]) * kGrain);
+        if (threadIdx.x == 0) s.found[0] = 0, s.found[1] = 0;
         __syncthreads();
-        // threads have neighbours of the order
-        double ahead = 0.0, sum;
-        for (int i = begin; i < min(begin + per, n); ++i) ahead += value[i];
-        ahead = block_scan(s, ahead, sum);
-        const double target = static_cast<double>(top_p) * (cuts ? sum : whole);
-        uint32_t kept = 0;                   // (the first ones: each of the conditions holds for a beginning)
-        for (int i = begin; i < min(begin + per, n); ++i) {
-          kept += (i == 0 || !nucleus || ahead < target) && value[i] >= min_p;
-          ahead += value[i];
+        // The logits of bins [a, b] that are kept so far, to a list of their own, whose length `count` gets.
+        unsigned long long* few_of = s.order;
+        unsigned long long* few_value = s.value;
+        auto pick = [&](uint32_t a, uint32_t b, uint32_t* count) {
+          for (int i = threadIdx.x; i < n; i += N) {
+            const uint32_t bin = bin_of(z_of[i]);
+            if (value[i] == kOut || bin < a || bin > b) continue;
+            const uint32_t at = atomicAdd(count, 1u);
+            if (at < kList) few_of[at] = static_cast<unsigned long long>(~key_of<LOW>(z_of[i])) << 32 | place_of[i], few_value[at] = value[i] << 11 | i;
+          }
+          __syncthreads();
+          return min(*count, static_cast<uint32_t>(kList));
+        };
+        if (cuts) {
+          const uint32_t count = pick(k_bin, k_bin, &s.found[0]), left = k - k_before;
+          for (uint32_t i = threadIdx.x; i < count; i += N) {
+            const unsigned long long me = few_of[i];
+            uint32_t rank = 0;
+#pragma unroll 4
+            for (uint32_t j = 0; j < count; ++j) rank += few_of[j] < me;
+            if (rank >= left) value[few_value[i] & 0x7ff] = kOut;
+          }
+          __syncthreads();
+        }
+        if (nucleus) {
+          unsigned long long mine = 0, ahead = 0, sum;
+          for (int i = threadIdx.x; i < n; i += N) {
+            if (value[i] == kOut) continue;
+            mine += value[i];
+            if (bin_of(z_of[i]) < low_bin) ahead += value[i];
+          }
+          if (cuts) block_scan(s, mine, sum);
+          block_scan(s, ahead, ahead);
+          const double goal = ceil(static_cast<double>(top_p) * (cuts ? static_cast<double>(sum) : whole * kGrain));
+          const unsigned long long target = __double2ull_rn(fmin(fmax(goal, 1.0), 9.0e18));
+          const uint32_t count = pick(low_bin, high_bin, &s.found[1]);
+          for (uint32_t i = threadIdx.x; i < count; i += N) {
+            const unsigned long long me = few_of[i];
+            unsigned long long upto = ahead;
+#pragma unroll 4
+            for (uint32_t j = 0; j < count; ++j)
+              if (few_of[j] < me) upto += few_value[j] >> 11;
+            if (upto >= target) value[few_value[i] & 0x7ff] = kOut;
+          }
+          __syncthreads();
+          for (int i = threadIdx.x; i < n; i += N)
+            if (bin_of(z_of[i]) > high_bin) value[i] = kOut;
+        }
+        // The draw, in the order of the places: sums by shares of the row, then by shares of the share that the random number falls on, then
+        // each with each.
+        unsigned long long total = 0;
+        uint32_t kept = 0;
+        for (int i = threadIdx.x; i < n; i += N) {
+          if (value[i] != kOut && min_p > 0.0 && weight(z_of[i]) < min_p) value[i] = kOut;
+          if (value[i] == kOut) continue;
+          ++kept;
+          total += value[i];
         }
         kept = block_sum(s, kept);
-        // by rising place, with the place in the order
-        for (int i = threadIdx.x; i < kept; i += N) order[i] = order[i] << 32 | i;
-        sort<N>(order, kept);
-        const int each = (kept + N - 1) / N, start = threadIdx.x * each, end = min(start + each, static_cast<int>(kept));
-        ahead = 0.0;
-        for (int i = start; i < end; ++i) ahead += value[static_cast<uint32_t>(order[i])];
-        ahead = block_scan(s, ahead, sum);
-        // the first one up to and with which the weights exceed u of theirs; where rounding leaves none, the last one that has a weight
-        const double mark = u < 1.0 ? u * sum : INFINITY;
-        uint32_t passed = 0, drawable = 1;
-        for (int i = start; i < end; ++i) {
-          const double w = value[static_cast<uint32_t>(order[i])];
-          ahead += w;
-          if (w > 0.0) drawable = i + 1;
-          passed += !(ahead > mark);
+        unsigned long long mine_total = total;
+        block_scan(s, mine_total, total);
+        unsigned long long goal = u < 1.0 ? __double2ull_rz(u * static_cast<double>(total)) : total;         // the first sum beyond it; at most the last one
+        goal = min(goal, total - 1);
+        int64_t base = 0, size = p.classes;
+        unsigned long long ahead = 0;
+        for (int round = 0; round < 2; ++round) {
+          const int64_t part = (size + kBins - 1) / kBins;
+          for (int b = threadIdx.x; b < kBins; b += N) s.mass[b] = 0;
+          __syncthreads();
+          for (int i = threadIdx.x; i < n; i += N) {
+            const int64_t at = static_cast<int64_t>(place_of[i]) - base;
+            if (value[i] != kOut && at >= 0 && at < size) atomicAdd(&s.mass[static_cast<uint32_t>(at) / static_cast<uint32_t>(part)], value[i]);
+          }
+          __syncthreads();
+          unsigned long long sum = 0, whole_sum;
+#pragma unroll
+          for (int j = 0; j < kEach; ++j) sum += s.mass[threadIdx.x * kEach + j];
+          unsigned long long upto = ahead + block_scan(s, sum, whole_sum);
+#pragma unroll
+          for (int j = 0; j < kEach; ++j) {
+            const unsigned long long v = s.mass[threadIdx.x * kEach + j];
+            if (upto <= goal && upto + v > goal) s.found[0] = threadIdx.x * kEach + j, s.found_sum = upto;
+            upto += v;
+          }
+          __syncthreads();
+          base += s.found[0] * part;
+          size = min(part, p.classes - base);
+          ahead = s.found_sum;
+          __syncthreads();
+          if (part == 1) break;
         }
-        drawable = __reduce_max_sync(0xffffffffu, drawable);
-        if (lane == 0) s.ties[warp] = drawable;
-        passed = block_sum(s, passed);
-        if (threadIdx.x == 0) {
-          for (int q = 0; q < kWarps; ++q) drawable = max(drawable, s.ties[q]);
-          const uint32_t i = min(passed, drawable - 1);
-          p.ids[row] = static_cast<int32_t>(order[i] >> 32);
-          if (p.logp) p.logp[row] = static_cast<float>(log(value[static_cast<uint32_t>(order[i])] / sum));
-          if (p.kept) p.kept[row] = static_cast<int32_t>(kept);
+        for (int i = threadIdx.x; i < n; i += N) {       // (of at most a millionth of the row, and eight more)
+          const int64_t at = static_cast<int64_t>(place_of[i]) - base;
+          if (value[i] == kOut || at < 0 || at >= size) continue;
+          unsigned long long upto = ahead;
+          if (size > 1)
+            for (int j = 0; j < n; ++j)
+              if (value[j] != kOut && place_of[j] >= base && place_of[j] < place_of[i]) upto += value[j];
+          if (upto <= goal && upto + value[i] > goal) {
+            p.ids[row] = static_cast<int32_t>(place_of[i]);
+            if (p.logp) p.logp[row] = static_cast<float>(log(weight(z_of[i]) * kGrain / static_cast<double>(total)));
+            if (p.kept) p.kept[row] = static_cast<int32_t>(kept);
+          }
         }
         return;
       }
@@ -727,7 +844,7 @@ __global__ void __launch_bounds__(N, 1024 / N) sample_kernel(const __grid_consta
 
     // All lists, sorted, to every CTA.  How many they are; -1: too many for one of them.
     auto sorted = [&]() {                    // (after a row_sync)
-      const int n = collect(s, s.order, kList, ctas, true);
+      const int n = collect(s, ctas);
       row_sync(ctas);                        // (the lists are read)
       if (threadIdx.x == 0) s.listed = 0;
       return n;
@@ -756,15 +873,15 @@ __global__ void __launch_bounds__(N, 1024 / N) sample_kernel(const __grid_consta
     // 5. the k-th largest
     if (cuts) {
       Range r = range_of<LOW, kBins>(m, unit, k_bin, k_bin);
-      const bool few = k_upto - k_before <= kList;
-      if (few) {
+      const bool few_k = k_upto - k_before <= kList;
+      if (few_k) {
         each_hit(slice, from, to, fmaxf(value_of<LOW>(r.low), k_gate), [&](float z, int i) {
           if (bin_of(z) == k_bin) list(z, i);
         });
         row_sync(ctas);
         ends_at(min(static_cast<int>(k - k_before), sorted()) - 1);
       }
-      while (!few) {
+      while (!few_k) {
         const int shift = shift_of<kBins>(r);
         __syncthreads();
         for (int b = threadIdx.x; b < kBins; b += N) s.count[b] = 0;
@@ -821,14 +938,14 @@ __global__ void __launch_bounds__(N, 1024 / N) sample_kernel(const __grid_consta
       // A sorted list of n logits that follow others with the sum `above`, behind them what top-k leaves of its last key (where that is in
       // reach): where the target is met.
       auto meet = [&](int n) {
-        double w[kEach], a = 0.0, listed;
+        double w[kEach], a = 0.0, sum;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
           const int i = threadIdx.x * kEach + j;
           w[j] = i < n ? weight(value_of<LOW>(~static_cast<uint32_t>(s.order[i] >> 32))) : 0.0;
           a += w[j];
         }
-        a = above + block_scan(s, a, listed);
+        a = above + block_scan(s, a, sum);
         uint32_t passed = 0;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
@@ -839,7 +956,7 @@ __global__ void __launch_bounds__(N, 1024 / N) sample_kernel(const __grid_consta
         if (static_cast<int>(passed) < n || (n > 0 && !cut_inside)) {
           ends_at(min(static_cast<int>(passed), n - 1));
         } else if (cut_inside) {
-          const double more = ceil((target - above - listed) / cut_weight);
+          const double more = ceil((target - above - sum) / cut_weight);
           last_key = cut_key;
           last_ties = more >= cut_ties || !(cut_weight > 0.0) ? cut_ties : more > 1.0 ? static_cast<uint32_t>(more) : 1u;
         } else {                             // (no logit where there are some)
@@ -848,12 +965,19 @@ __global__ void __launch_bounds__(N, 1024 / N) sample_kernel(const __grid_consta
         }
       };
       // sums of the weights: of all that top-k leaves, and of those above the range (by bins at first, then by keys)
-      const bool few = nucleus_upto - nucleus_before <= kList;
-      int listed = -1;
+      const bool few_left = nucleus_upto - nucleus_before <= kList;
+      if (few) {                  // (the sums are there already, and the list)
+        spread(over, all, 0u);
+        row_sync(ctas);
+        double sum_all;
+        gathered(above, sum_all, none);
+        target = static_cast<double>(top_p) * sum_all;
+        listed = sorted();
+      } else
       for (bool begins = true;; begins = false) {
         const int shift = shift_of<kBins>(r);
         __syncthreads();
-        if (!few)
+        if (!few_left)
           for (int b = threadIdx.x; b < kBins; b += N) s.mass[b] = 0;
         __syncthreads();
         double over = 0.0;
@@ -863,12 +987,12 @@ __global__ void __launch_bounds__(N, 1024 / N) sample_kernel(const __grid_consta
           for (int j = 0; j < kV; ++j) {
             const double w = v[j] > cut_value ? weight(v[j]) : 0.0;
             if (begins && cuts) all += w;
-            if (few ? bin_of(v[j]) < low_bin : key_of<LOW>(v[j]) > r.high) over += w;
+            if (few_left ? bin_of(v[j]) < low_bin : key_of<LOW>(v[j]) > r.high) over += w;
           }
         });
         each_hit(slice, from, to, value_of<LOW>(r.low), [&](float z, int i) {
           if (!(z > cut_value)) return;      // (equal ones are added below)
-          if (few) {
+          if (few_left) {
             const uint32_t bin = bin_of(z);
             if (bin >= low_bin && bin <= high_bin) list(z, i);
             return;
@@ -883,7 +1007,7 @@ __global__ void __launch_bounds__(N, 1024 / N) sample_kernel(const __grid_consta
         double sum_all;
         gathered(above, sum_all, inside);
         if (begins) target = static_cast<double>(top_p) * (sum_all + (cuts ? cut_ties * cut_weight : 0.0));
-        if (few) {
+        if (few_left) {
           listed = sorted();
           break;
         }
@@ -935,7 +1059,17 @@ __global__ void __launch_bounds__(N, 1024 / N) sample_kernel(const __grid_consta
   {
     double sum = all;
     uint32_t keeps = 0, ties = 0;
-    if (!last_key && min_p == 0.0) {
+    if (few && min_p == 0.0) {               // what lies in the bins before, and what is kept of the list
+      sum = over;
+      keeps = over_count;
+      const int64_t begin = first + static_cast<int64_t>(from) * kV, end = first + static_cast<int64_t>(to) * kV;
+      for (int i = lane; i < listed; i += 32) {
+        const uint32_t place = static_cast<uint32_t>(s.order[i]), key = ~static_cast<uint32_t>(s.order[i] >> 32);
+        if (place < begin || place >= end) continue;
+        if (key == last_key) ++ties;
+        else if (key > last_key) sum += weight(value_of<LOW>(key)), ++keeps;
+      }
+    } else if (!last_key && min_p == 0.0) {
       if (!holes) {
         if (lane == 0) keeps = static_cast<uint32_t>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(to) * kV, slice.entries) - static_cast<int64_t>(from) * kV));
       } else {
@@ -1124,12 +1258,12 @@ constexpr int kHeldMost = 192 << 10;         // of a CTA's shared memory, for th
 constexpr int kHeldFour = 40 << 10;          // ... where four CTAs of half the threads are
 constexpr int kHeldTwo = 80 << 10;           // ... where two CTAs are to share an SM
 
-template <typename T, int N>
+template <typename T, int N, bool FILTERS>
 cudaError_t launch(const SampleParams& p, int64_t n, cudaStream_t s) {
-  cudaError_t e = sfb::allow_smem<sample_kernel<T, N>>(kHeldMost);
-  if (e == cudaSuccess && p.ctas > 8) e = sfb::allow_clusters<sample_kernel<T, N>>();
+  cudaError_t e = sfb::allow_smem<sample_kernel<T, N, FILTERS>>(kHeldMost);
+  if (e == cudaSuccess && p.ctas > 8) e = sfb::allow_clusters<sample_kernel<T, N, FILTERS>>();
   if (e != cudaSuccess) return e;
-  return sfb::launch_kernel(sample_kernel<T, N>, dim3(static_cast<unsigned>(n * p.ctas)), dim3(N), static_cast<size_t>(p.resident) * 16, s, p.ctas, p);
+  return sfb::launch_kernel(sample_kernel<T, N, FILTERS>, dim3(static_cast<unsigned>(n * p.ctas)), dim3(N), static_cast<size_t>(p.resident) * 16, s, p.ctas, p);
 }
 
 template <typename T>
@@ -1142,7 +1276,9 @@ cudaError_t launch(SampleParams p, int64_t n, cudaStream_t s) {
   p.ctas = ctas;
   p.share = static_cast<int32_t>((vectors + ctas - 1) / ctas);
   p.resident = std::min(p.share, kHeldMost / 16);
-  return p.share <= kHeldFour / 16 && n * ctas > 2 * sfb::kModelSms ? launch<T, 256>(p, n, s) : launch<T, 512>(p, n, s);
+  const bool small = p.share <= kHeldFour / 16 && n * ctas > 2 * sfb::kModelSms;
+  if (p.top_k || p.top_p) return small ? launch<T, 256, true>(p, n, s) : launch<T, 512, true>(p, n, s);
+  return small ? launch<T, 256, false>(p, n, s) : launch<T, 512, false>(p, n, s);
 }
 
 }  // namespace
