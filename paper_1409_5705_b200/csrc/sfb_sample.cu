@@ -5,7 +5,7 @@
 //   1. the largest logit m (all that a greedy answer takes, but for its place)
 //   2. (top-k, top-p) counts of the logits by their distance from m, in up to 1024 bins
 //   3. (top-k) the bin of the k-th largest; (top-p) between which bins the nucleus ends, by bounds on what weights of a bin can come to
-//   4. where what lies up to there is as many logits as there are bins, or fewer, they are gathered, sorted, and the rest follows from prefix sums over them
+//   4. where what lies up to there is as many logits as there are bins, or fewer, they are gathered, and the rest follows from them
 //   5. else the logits of the bins in question alone, once they are that few; until then they are counted (or their weights summed) by ordered
 //      key in bins of fewer and fewer keys.  Out comes a key and how many of the logits with that key are kept, the first ones: all
 //      filters keep a beginning of the order by falling logit and rising index.
@@ -33,11 +33,13 @@ template <int N>
 struct Of {
   static constexpr int kWarps = N / 32, kBins = kEach * N, kList = kEach * N;
 };
+constexpr unsigned long long kOut = 1ull << 63;          // the weight of what a filter has left out of a list
+constexpr double kGrain = 1125899906842624.0;            // weights of a list are whole numbers, 2^-50 of the largest
 constexpr float kWidest = 32.f;              // bins of 2 reach to e^-32 of the largest weight at most
 constexpr float kFar = 45.f;                 // weights below e^-45 of the largest count as zero: all of them together are below 1e-13
 constexpr int kMaxCtas = 16;                 // (more than eight: a launch that asks for them)
 constexpr int kTable = 256;
-constexpr uint32_t kSmall = 256;             // logits that are compared each with each, at most
+constexpr uint32_t kSmall = 64;              // logits that are compared each with each, at most
 
 struct SampleParams {
   const void* z;
@@ -115,9 +117,9 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 }
 
 // ---- shared memory -------------------------------------------------------------------------------------------------------------------
-template <int N>
+template <int N, bool FILTERS>
 struct Shared {
-  static constexpr int kBins = Of<N>::kBins, kList = Of<N>::kList, kWarps = Of<N>::kWarps;
+  static constexpr int kWarps = Of<N>::kWarps, kBins = FILTERS ? Of<N>::kBins : 2, kList = FILTERS ? Of<N>::kList : 2;
   union {
     uint32_t count[kBins];
     unsigned long long mass[kBins];
@@ -139,7 +141,7 @@ struct Shared {
   uint32_t listed, found[2], first;
   uint32_t low_before;
   double found_at;
-  unsigned long long found_sum;
+  unsigned long long found_sum, found_value;
   // what the row's CTAs have written here
   float most[kMaxCtas], least[kMaxCtas];
   double sums[2][kMaxCtas];
@@ -212,8 +214,8 @@ __device__ __forceinline__ double warp_sum(double v) {
 
 // (Functions of their own, not copies at each call: a CTA goes through the kernel once, and waits for its instructions.)
 // What lies in the threads before this one; the whole in `all`.
-template <int N, typename V>
-__device__ __noinline__ V block_scan(Shared<N>& s, V value, V& all) {
+template <int N, bool FILTERS, typename V>
+__device__ __noinline__ V block_scan(Shared<N, FILTERS>& s, V value, V& all) {
   constexpr int kWarps = Of<N>::kWarps;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   V* part = reinterpret_cast<V*>(s.scan);
@@ -237,8 +239,8 @@ __device__ __noinline__ V block_scan(Shared<N>& s, V value, V& all) {
   return (warp ? ahead : 0) + (sum - value);
 }
 // The threads' sum (of small whole numbers).
-template <int N>
-__device__ __noinline__ uint32_t block_sum(Shared<N>& s, uint32_t value) {
+template <int N, bool FILTERS>
+__device__ __noinline__ uint32_t block_sum(Shared<N, FILTERS>& s, uint32_t value) {
   constexpr int kWarps = Of<N>::kWarps;
   const uint32_t v = warp_sum(value);
   if ((threadIdx.x & 31) == 0) s.part_count[threadIdx.x >> 5] = v;
@@ -246,27 +248,6 @@ __device__ __noinline__ uint32_t block_sum(Shared<N>& s, uint32_t value) {
   const uint32_t all = warp_sum((threadIdx.x & 31) < kWarps ? s.part_count[threadIdx.x & 31] : 0u);
   __syncthreads();
   return all;
-}
-
-// Ascending, n of them padded to a power of two.  (Strides of 32 and less stay within what a warp has.)
-template <int N>
-__device__ __noinline__ void sort(unsigned long long* a, int n) {
-  int p = 64;
-  while (p < n) p <<= 1;
-  for (int i = n + threadIdx.x; i < p; i += N) a[i] = ~0ull;
-  __syncthreads();
-  for (int k = 2; k <= p; k <<= 1) {
-    for (int stride = k >> 1; stride > 0; stride >>= 1) {
-      for (int t = threadIdx.x; t < p / 2; t += N) {
-        const int i = 2 * t - (t & (stride - 1)), j = i + stride;
-        const unsigned long long x = a[i], y = a[j];
-        if ((x > y) == ((i & k) == 0)) a[i] = y, a[j] = x;
-      }
-      if (stride > 32 || (stride == 1 && 2 * k > 64)) __syncthreads();
-      else __syncwarp();
-    }
-  }
-  __syncthreads();
 }
 
 // ---- a CTA's share of a row ------------------------------------------------------------------------------------------------------------
@@ -355,8 +336,8 @@ __device__ __forceinline__ int shift_of(const Range& r) {
 
 // The bins' sums over the row's CTAs, two a thread.  Every CTA has passed a row_sync since it filled its own.  Each adds a share of the bins,
 // then all read the shares: a sixteenth of what it is if all read all.
-template <int N, typename V>
-__device__ __noinline__ void sum_bins(Shared<N>& s, const V* bins, int ctas, int cta, V (&out)[kEach]) {
+template <int N, bool FILTERS, typename V>
+__device__ __noinline__ void sum_bins(Shared<N, FILTERS>& s, const V* bins, int ctas, int cta, V (&out)[kEach]) {
   if (ctas == 1) {
 #pragma unroll
     for (int j = 0; j < kEach; ++j) out[j] = bins[threadIdx.x * kEach + j];
@@ -379,10 +360,10 @@ __device__ __noinline__ void sum_bins(Shared<N>& s, const V* bins, int ctas, int
   for (int j = 0; j < kEach; ++j) out[j] = read(&summed[at + j], owner);
 }
 
-// Calls f(i, entry) for what the CTAs have listed, CTA by CTA.  Returns how many; -1: more than `most`, or than one of the lists holds.  (Every
+// What the CTAs have listed, CTA by CTA: entries (~key, place).  Returns how many; -1: more than `most`, or than one of the lists holds.  (Every
 // CTA has passed a row_sync since it listed.)
-template <int N, typename F>
-__device__ __forceinline__ int from_lists(Shared<N>& s, int ctas, int most, bool wanted, F&& f) {
+template <int N, bool FILTERS>
+__device__ __noinline__ int collect(Shared<N, FILTERS>& s, int ctas, int most, bool wanted, unsigned long long* to) {
   const int lane = threadIdx.x & 31;
   const uint32_t n = lane < ctas ? read(&s.listed, lane) : 0;
   uint32_t upto = n;
@@ -392,7 +373,7 @@ __device__ __forceinline__ int from_lists(Shared<N>& s, int ctas, int most, bool
     if (lane >= o) upto += v;
   }
   const uint32_t all = __shfl_sync(0xffffffffu, upto, 31);
-  if (all > most || __any_sync(0xffffffffu, n > Of<N>::kList)) return -1;
+  if (all > most || __any_sync(0xffffffffu, n > Shared<N, FILTERS>::kList)) return -1;
   if (!wanted) return static_cast<int>(all);
   for (uint32_t i0 = 0; i0 < all; i0 += N) {
     const uint32_t i = i0 + threadIdx.x;
@@ -401,24 +382,77 @@ __device__ __forceinline__ int from_lists(Shared<N>& s, int ctas, int most, bool
       const uint32_t end = __shfl_sync(0xffffffffu, upto, q);
       if (i >= end) c = q + 1, begin = end;
     }
-    if (i < all) f(i, read(&s.list[i - begin], c));
+    if (i < all) to[i] = read(&s.list[i - begin], c);
   }
   return static_cast<int>(all);
 }
-// All lists in the order of falling keys and rising places, to s.order: entries (~key, place).
-template <int N>
-__device__ __noinline__ int collect(Shared<N>& s, int ctas) {
-  const int all = from_lists(s, ctas, Of<N>::kList, true, [&](uint32_t i, unsigned long long e) { s.order[i] = e; });
-  if (all >= 0) sort<N>(s.order, all);       // (begins with a barrier)
-  return all;
+
+__device__ __forceinline__ uint32_t key_in(unsigned long long entry) { return ~static_cast<uint32_t>(entry >> 32); }
+
+// The beginning of the order by falling key whose values (value null: 1 each) first come to `target`, among a list's entries with keys of r: its last
+// key, and how many entries of that key belong to it.  All of them where they do not come to that; `whole` is what they come to.
+// BY_PLACE: among the entries of the key `only`, and ~place takes the place of the key.
+template <bool BY_PLACE, int N, bool FILTERS>
+__device__ __noinline__ uint2 find_end(Shared<N, FILTERS>& s, const unsigned long long* list, const unsigned long long* value, int n, Range r,
+                                       unsigned long long target, unsigned long long& whole, uint32_t only = 0) {
+  constexpr int kBins = Shared<N, FILTERS>::kBins;
+  unsigned long long before = 0;
+  for (bool begins = true;; begins = false) {
+    const int shift = shift_of<kBins>(r);
+    __syncthreads();
+    for (int b = threadIdx.x; b < kBins; b += N) s.mass[b] = 0;
+    if (threadIdx.x == 0) s.found[0] = 0, s.found_sum = before, s.found_value = 1;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += N) {
+      const uint32_t key = BY_PLACE ? ~static_cast<uint32_t>(list[i]) : key_in(list[i]);
+      const unsigned long long v = value ? value[i] : 1;
+      if (key >= r.low && key <= r.high && v != kOut && (!BY_PLACE || key_in(list[i]) == only)) atomicAdd(&s.mass[(r.high - key) >> shift], v);
+    }
+    __syncthreads();
+    unsigned long long mass[kEach], sum = 0, all;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) mass[j] = s.mass[threadIdx.x * kEach + j], sum += mass[j];
+    unsigned long long upto = before + block_scan(s, sum, all);
+    if (begins) whole = all;
+    const unsigned long long want = min(target, before + all);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      if (upto < want && upto + mass[j] >= want) s.found[0] = threadIdx.x * kEach + j, s.found_sum = upto;
+      upto += mass[j];
+    }
+    __syncthreads();
+    const uint32_t high = r.high - (s.found[0] << shift), span = (1u << shift) - 1;
+    before = s.found_sum;
+    if (shift == 0) {
+      if (value) {
+        for (int i = threadIdx.x; i < n; i += N)
+          if (key_in(list[i]) == high && value[i] != kOut) s.found_value = value[i];
+        __syncthreads();
+      }
+      const unsigned long long each = max(s.found_value, 1ull), left = max(want, before + 1) - before;
+      return make_uint2(high, static_cast<uint32_t>(min((left + each - 1) / each, 0xffffffffull)));
+    }
+    r = Range{max(r.low, high > span ? high - span : 0u), high};
+  }
 }
-// All lists as they are: entries (logit, place).
-template <int N>
-__device__ __noinline__ int pull(Shared<N>& s, int ctas, int most, bool wanted, float* z, uint32_t* place) {
-  return from_lists(s, ctas, most, wanted, [&](uint32_t i, unsigned long long e) {
-    z[i] = __uint_as_float(static_cast<uint32_t>(e >> 32));
-    place[i] = static_cast<uint32_t>(e);
-  });
+
+// Leaves out of a list what lies behind the first `ties` entries of a key, in the order by falling key and rising place.
+template <int N, bool FILTERS>
+__device__ __noinline__ void leave_out(Shared<N, FILTERS>& s, const unsigned long long* list, unsigned long long* value, int n, uint2 end) {
+  uint32_t equal = 0;
+  for (int i = threadIdx.x; i < n; i += N) {
+    const uint32_t key = key_in(list[i]);
+    if (key < end.x) value[i] = kOut;
+    equal += key == end.x && value[i] != kOut;
+  }
+  equal = block_sum(s, equal);
+  if (equal <= end.y) return;
+  // (what earlier filters left out of the key are its last places: the first ones are the others' first ones)
+  unsigned long long unused;
+  const uint2 last = find_end<true>(s, list, nullptr, n, Range{0, 0xffffffffu}, end.y, unused, end.x);
+  for (int i = threadIdx.x; i < n; i += N)
+    if (key_in(list[i]) == end.x && ~static_cast<uint32_t>(list[i]) < last.x) value[i] = kOut;
+  __syncthreads();
 }
 
 // FILTERS: top-k or top-p may be asked for (without them a smaller kernel, of which more threads fit an SM).
@@ -427,7 +461,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
   constexpr int LOW = Type<T>::kLow, kV = Slice<T>::kV;
   extern __shared__ __align__(16) unsigned char dynamic[];
   constexpr int kWarps = Of<N>::kWarps, kBins = Of<N>::kBins, kList = Of<N>::kList;
-  __shared__ Shared<N> s;
+  __shared__ Shared<N, FILTERS> s;
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int i = threadIdx.x; i < kTable; i += N) s.power[i] = exp2(i / static_cast<double>(kTable));
@@ -661,7 +695,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
   // The weights of all logits, where something takes their sum, and of those in the bins before the nucleus's end; what lies in the bins of that end
   // is listed, where it is no more than a list holds (and not all that can be kept is listed below).
   const int room = p.resident >= 2 * kList ? 2 * kList : p.resident >= kList ? kList : 0;
-  const bool listed_all = filters && (cuts ? k_upto : nucleus_upto) <= room && (!cuts || k_upto - k_before <= kSmall) && (!nucleus || nucleus_upto - nucleus_before <= kSmall);
+  const bool listed_all = filters && (cuts ? k_upto : nucleus_upto) <= room;
   const bool few = filters && nucleus && !cuts && !listed_all && nucleus_upto - nucleus_before <= kList;
   // Adds a logit to this CTA's list.
   auto list = [&](float z, int i) {
@@ -703,136 +737,99 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
   }
 
   uint32_t last_key = 0, last_ties = 0xffffffffu;        // of what is kept: all above the key, and so many that have it
-  int listed = -1;                           // in s.order, of the nucleus's end
+  int listed = -1;                           // in s.order, s.value: of the nucleus's end
   if (filters) {
     double above = 0.0, whole = 0.0;
     uint32_t none;
-    // 4. all that can be kept, where that is little enough for a list, which takes the place of CTA 0's share of the row: there the filters' ends
-    // are found among the few logits of their bins, each compared with each.  Sums are whole numbers (2^-50 of the largest weight): in any order.
+    // 4. all that can be kept, where that is little enough for a list, which takes the place of CTA 0's share of the row
     if (listed_all) {
       const uint32_t top_bin = cuts ? k_bin : high_bin;
-      const float gate = fmaxf(value_of<LOW>(range_of<LOW, kBins>(m, unit, 0, top_bin).low), k_gate);
-      each_hit(slice, from, to, gate, [&](float z, int i) {
-        if (z <= kNone || bin_of(z) > top_bin) return;
-        const uint32_t at = atomicAdd(&s.listed, 1u);
-        if (at < kList) s.list[at] = static_cast<unsigned long long>(__float_as_uint(z + 0.f)) << 32 | static_cast<uint32_t>(first + i);
+      Range r = range_of<LOW, kBins>(m, unit, 0, top_bin);
+      each_hit(slice, from, to, fmaxf(value_of<LOW>(r.low), k_gate), [&](float z, int i) {
+        if (z > kNone && bin_of(z) <= top_bin) list(z, i);
       });
       spread(all, 0.0, 0u);
       row_sync(ctas);
       gathered(whole, above, none);
-      float* z_of = reinterpret_cast<float*>(dynamic);                        // of the list: logits, places, weights (2^63: out)
-      uint32_t* place_of = reinterpret_cast<uint32_t*>(dynamic) + room;
-      unsigned long long* value = reinterpret_cast<unsigned long long*>(dynamic) + room;
-      const int n = pull(s, ctas, room, cta == 0, z_of, place_of);
+      unsigned long long* entry = reinterpret_cast<unsigned long long*>(dynamic);
+      unsigned long long* value = entry + room;
+      const int n = collect(s, ctas, room, cta == 0, entry);
       row_sync(ctas);                        // (the lists are read)
       if (n >= 0) {
         if (cta != 0) return;
-        constexpr unsigned long long kOut = 1ull << 63;
-        constexpr double kGrain = 1125899906842624.0;
-        for (int i = threadIdx.x; i < n; i += N) value[i] = __double2ull_rn(weight(z_of[i]) * kGrain);
-        if (threadIdx.x == 0) s.found[0] = 0, s.found[1] = 0;
+        for (int i = threadIdx.x; i < n; i += N) value[i] = __double2ull_rn(weight(value_of<LOW>(key_in(entry[i]))) * kGrain);
         __syncthreads();
-        // The logits of bins [a, b] that are kept so far, to a list of their own, whose length `count` gets.
-        unsigned long long* few_of = s.order;
-        unsigned long long* few_value = s.value;
-        auto pick = [&](uint32_t a, uint32_t b, uint32_t* count) {
-          for (int i = threadIdx.x; i < n; i += N) {
-            const uint32_t bin = bin_of(z_of[i]);
-            if (value[i] == kOut || bin < a || bin > b) continue;
-            const uint32_t at = atomicAdd(count, 1u);
-            if (at < kList) few_of[at] = static_cast<unsigned long long>(~key_of<LOW>(z_of[i])) << 32 | place_of[i], few_value[at] = value[i] << 11 | i;
-          }
-          __syncthreads();
-          return min(*count, static_cast<uint32_t>(kList));
-        };
-        if (cuts) {
-          const uint32_t count = pick(k_bin, k_bin, &s.found[0]), left = k - k_before;
-          for (uint32_t i = threadIdx.x; i < count; i += N) {
-            const unsigned long long me = few_of[i];
-            uint32_t rank = 0;
-#pragma unroll 4
-            for (uint32_t j = 0; j < count; ++j) rank += few_of[j] < me;
-            if (rank >= left) value[few_value[i] & 0x7ff] = kOut;
-          }
-          __syncthreads();
-        }
+        unsigned long long unused, total = 0;
+        if (cuts) leave_out(s, entry, value, n, find_end<false>(s, entry, nullptr, n, r, k, unused));
         if (nucleus) {
-          unsigned long long mine = 0, ahead = 0, sum;
-          for (int i = threadIdx.x; i < n; i += N) {
-            if (value[i] == kOut) continue;
-            mine += value[i];
-            if (bin_of(z_of[i]) < low_bin) ahead += value[i];
+          double goal = whole * kGrain;
+          if (cuts) {
+            for (int i = threadIdx.x; i < n; i += N) total += value[i] != kOut ? value[i] : 0;
+            block_scan(s, total, total);
+            goal = static_cast<double>(total);
           }
-          if (cuts) block_scan(s, mine, sum);
-          block_scan(s, ahead, ahead);
-          const double goal = ceil(static_cast<double>(top_p) * (cuts ? static_cast<double>(sum) : whole * kGrain));
-          const unsigned long long target = __double2ull_rn(fmin(fmax(goal, 1.0), 9.0e18));
-          const uint32_t count = pick(low_bin, high_bin, &s.found[1]);
-          for (uint32_t i = threadIdx.x; i < count; i += N) {
-            const unsigned long long me = few_of[i];
-            unsigned long long upto = ahead;
-#pragma unroll 4
-            for (uint32_t j = 0; j < count; ++j)
-              if (few_of[j] < me) upto += few_value[j] >> 11;
-            if (upto >= target) value[few_value[i] & 0x7ff] = kOut;
-          }
-          __syncthreads();
-          for (int i = threadIdx.x; i < n; i += N)
-            if (bin_of(z_of[i]) > high_bin) value[i] = kOut;
+          goal = fmin(fmax(ceil(static_cast<double>(top_p) * goal), 1.0), 9.0e18);
+          leave_out(s, entry, value, n, find_end<false>(s, entry, value, n, r, __double2ull_rn(goal), unused));
         }
-        // The draw, in the order of the places: sums by shares of the row, then by shares of the share that the random number falls on, then
-        // each with each.
-        unsigned long long total = 0;
+        // The draw, in the order of the places: sums by shares of the row, by shares of the share that the random number falls on, until what is
+        // left is little enough to compare each with each.
         uint32_t kept = 0;
+        total = 0;
         for (int i = threadIdx.x; i < n; i += N) {
-          if (value[i] != kOut && min_p > 0.0 && weight(z_of[i]) < min_p) value[i] = kOut;
+          if (min_p > 0.0 && value[i] != kOut && weight(value_of<LOW>(key_in(entry[i]))) < min_p) value[i] = kOut;
           if (value[i] == kOut) continue;
           ++kept;
           total += value[i];
         }
         kept = block_sum(s, kept);
-        unsigned long long mine_total = total;
-        block_scan(s, mine_total, total);
-        unsigned long long goal = u < 1.0 ? __double2ull_rz(u * static_cast<double>(total)) : total;         // the first sum beyond it; at most the last one
-        goal = min(goal, total - 1);
+        block_scan(s, total, total);
+        // the first sum beyond u of the whole; at most the last one
+        const unsigned long long goal = min(u < 1.0 ? __double2ull_rz(u * static_cast<double>(total)) : total, total - 1);
         int64_t base = 0, size = p.classes;
         unsigned long long ahead = 0;
-        for (int round = 0; round < 2; ++round) {
-          const int64_t part = (size + kBins - 1) / kBins;
+        for (;;) {
+          const uint32_t part = static_cast<uint32_t>((size + kBins - 1) / kBins);
           for (int b = threadIdx.x; b < kBins; b += N) s.mass[b] = 0;
+          if (threadIdx.x == 0) s.listed = 0;
           __syncthreads();
           for (int i = threadIdx.x; i < n; i += N) {
-            const int64_t at = static_cast<int64_t>(place_of[i]) - base;
-            if (value[i] != kOut && at >= 0 && at < size) atomicAdd(&s.mass[static_cast<uint32_t>(at) / static_cast<uint32_t>(part)], value[i]);
+            const int64_t at = static_cast<uint32_t>(entry[i]) - base;
+            if (value[i] != kOut && at >= 0 && at < size) atomicAdd(&s.mass[static_cast<uint32_t>(at) / part], value[i]);
           }
           __syncthreads();
-          unsigned long long sum = 0, whole_sum;
+          unsigned long long mass[kEach], sum = 0, none;
 #pragma unroll
-          for (int j = 0; j < kEach; ++j) sum += s.mass[threadIdx.x * kEach + j];
-          unsigned long long upto = ahead + block_scan(s, sum, whole_sum);
+          for (int j = 0; j < kEach; ++j) mass[j] = s.mass[threadIdx.x * kEach + j], sum += mass[j];
+          unsigned long long upto = ahead + block_scan(s, sum, none);
 #pragma unroll
           for (int j = 0; j < kEach; ++j) {
-            const unsigned long long v = s.mass[threadIdx.x * kEach + j];
-            if (upto <= goal && upto + v > goal) s.found[0] = threadIdx.x * kEach + j, s.found_sum = upto;
-            upto += v;
+            if (upto <= goal && upto + mass[j] > goal) s.found[0] = threadIdx.x * kEach + j, s.found_sum = upto;
+            upto += mass[j];
           }
           __syncthreads();
-          base += s.found[0] * part;
-          size = min(part, p.classes - base);
+          base += static_cast<int64_t>(s.found[0]) * part;
+          size = min(static_cast<int64_t>(part), size - static_cast<int64_t>(s.found[0]) * part);
           ahead = s.found_sum;
+          for (int i = threadIdx.x; i < n; i += N) {
+            const int64_t at = static_cast<uint32_t>(entry[i]) - base;
+            if (value[i] == kOut || at < 0 || at >= size) continue;
+            const uint32_t to_at = atomicAdd(&s.listed, 1u);
+            if (to_at < kSmall) s.order[to_at] = entry[i] << 32 | i;
+          }
           __syncthreads();
-          if (part == 1) break;
+          if (part == 1 || s.listed <= kSmall) break;
+          __syncthreads();
         }
-        for (int i = threadIdx.x; i < n; i += N) {       // (of at most a millionth of the row, and eight more)
-          const int64_t at = static_cast<int64_t>(place_of[i]) - base;
-          if (value[i] == kOut || at < 0 || at >= size) continue;
+        const uint32_t left = min(s.listed, kSmall);     // (one place has one entry)
+        if (threadIdx.x < left) {
+          const unsigned long long me = s.order[threadIdx.x];
+          const int i = static_cast<int>(static_cast<uint32_t>(me));
           unsigned long long upto = ahead;
-          if (size > 1)
-            for (int j = 0; j < n; ++j)
-              if (value[j] != kOut && place_of[j] >= base && place_of[j] < place_of[i]) upto += value[j];
+          for (uint32_t j = 0; j < left; ++j)
+            if (s.order[j] < me) upto += value[static_cast<uint32_t>(s.order[j])];
           if (upto <= goal && upto + value[i] > goal) {
-            p.ids[row] = static_cast<int32_t>(place_of[i]);
-            if (p.logp) p.logp[row] = static_cast<float>(log(weight(z_of[i]) * kGrain / static_cast<double>(total)));
+            p.ids[row] = static_cast<int32_t>(me >> 32);
+            if (p.logp) p.logp[row] = static_cast<float>(log(weight(value_of<LOW>(key_in(entry[i]))) * kGrain / static_cast<double>(total)));
             if (p.kept) p.kept[row] = static_cast<int32_t>(kept);
           }
         }
@@ -842,9 +839,9 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       __syncthreads();
     }
 
-    // All lists, sorted, to every CTA.  How many they are; -1: too many for one of them.
-    auto sorted = [&]() {                    // (after a row_sync)
-      const int n = collect(s, ctas);
+    // All lists to every CTA.
+    auto gather = [&]() {                    // (after a row_sync)
+      const int n = collect(s, ctas, kList, true, s.order);
       row_sync(ctas);                        // (the lists are read)
       if (threadIdx.x == 0) s.listed = 0;
       return n;
@@ -855,21 +852,8 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         if (key >= r.low && key <= r.high) list(z, i);
       });
       row_sync(ctas);
-      return sorted();
+      return gather();
     };
-    // Of a sorted list the entry that is the last one kept: its key, and how many of that key are kept with it.
-    auto ends_at = [&](int at) {
-      const uint32_t key = static_cast<uint32_t>(s.order[max(at, 0)] >> 32);
-      int begin = 0, end = max(at, 0);       // the first of that key
-      while (begin < end) {
-        const int mid = (begin + end) / 2;
-        if (static_cast<uint32_t>(s.order[mid] >> 32) < key) begin = mid + 1;
-        else end = mid;
-      }
-      last_key = ~key;
-      last_ties = at - begin + 1;
-    };
-
     // 5. the k-th largest
     if (cuts) {
       Range r = range_of<LOW, kBins>(m, unit, k_bin, k_bin);
@@ -879,7 +863,11 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
           if (bin_of(z) == k_bin) list(z, i);
         });
         row_sync(ctas);
-        ends_at(min(static_cast<int>(k - k_before), sorted()) - 1);
+        const int n = gather();
+        unsigned long long unused;
+        const uint2 end = find_end<false>(s, s.order, nullptr, n, r, k - k_before, unused);
+        last_key = end.x;
+        last_ties = end.y;
       }
       while (!few_k) {
         const int shift = shift_of<kBins>(r);
@@ -902,7 +890,11 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         for (int j = 0; j < kEach; ++j) sum += some[j];
         uint32_t a = over + block_scan(s, sum, inside);
         if (shift > 0 && inside <= kList) {
-          ends_at(min(static_cast<int>(k - over), list_range(r)) - 1);
+          const int n = list_range(r);
+          unsigned long long unused;
+          const uint2 end = find_end<false>(s, s.order, nullptr, n, r, k - over, unused);
+          last_key = end.x;
+          last_ties = end.y;
           break;
         }
 #pragma unroll
@@ -935,33 +927,19 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       const double grain = ldexp(1.0, p.fraction), back = ldexp(1.0, -p.fraction);
       double target = 0.0;
       bool cut_inside = cuts && high_bin == k_bin;
-      // A sorted list of n logits that follow others with the sum `above`, behind them what top-k leaves of its last key (where that is in
-      // reach): where the target is met.
+      // A list of n logits that follow others with the sum `above`, behind them what top-k leaves of its last key (where that is in reach):
+      // where the target is met.
       auto meet = [&](int n) {
-        double w[kEach], a = 0.0, sum;
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          const int i = threadIdx.x * kEach + j;
-          w[j] = i < n ? weight(value_of<LOW>(~static_cast<uint32_t>(s.order[i] >> 32))) : 0.0;
-          a += w[j];
-        }
-        a = above + block_scan(s, a, sum);
-        uint32_t passed = 0;
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          a += w[j];
-          passed += threadIdx.x * kEach + j < n && !(a >= target);
-        }
-        passed = block_sum(s, passed);
-        if (static_cast<int>(passed) < n || (n > 0 && !cut_inside)) {
-          ends_at(min(static_cast<int>(passed), n - 1));
-        } else if (cut_inside) {
-          const double more = ceil((target - above - sum) / cut_weight);
+        for (int i = threadIdx.x; i < n; i += N) s.value[i] = __double2ull_rn(weight(value_of<LOW>(key_in(s.order[i]))) * kGrain);
+        const double goal = fmax(ceil((target - above) * kGrain), 1.0);
+        unsigned long long sum;
+        const uint2 end = find_end<false>(s, s.order, s.value, n, r, __double2ull_rn(fmin(goal, 9.0e18)), sum);
+        last_key = end.x;
+        last_ties = end.y;
+        if (cut_inside && goal > static_cast<double>(sum)) {
+          const double more = ceil((goal - static_cast<double>(sum)) / (cut_weight * kGrain));
           last_key = cut_key;
           last_ties = more >= cut_ties || !(cut_weight > 0.0) ? cut_ties : more > 1.0 ? static_cast<uint32_t>(more) : 1u;
-        } else {                             // (no logit where there are some)
-          last_key = r.high;
-          last_ties = 1;
         }
       };
       // sums of the weights: of all that top-k leaves, and of those above the range (by bins at first, then by keys)
@@ -972,7 +950,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         double sum_all;
         gathered(above, sum_all, none);
         target = static_cast<double>(top_p) * sum_all;
-        listed = sorted();
+        listed = gather();
       } else
       for (bool begins = true;; begins = false) {
         const int shift = shift_of<kBins>(r);
@@ -1008,7 +986,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         gathered(above, sum_all, inside);
         if (begins) target = static_cast<double>(top_p) * (sum_all + (cuts ? cut_ties * cut_weight : 0.0));
         if (few_left) {
-          listed = sorted();
+          listed = gather();
           break;
         }
         unsigned long long some[kEach], sum = 0, mass;
@@ -1063,12 +1041,14 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       sum = over;
       keeps = over_count;
       const int64_t begin = first + static_cast<int64_t>(from) * kV, end = first + static_cast<int64_t>(to) * kV;
+      unsigned long long more = 0;           // (in whole numbers: their order says nothing)
       for (int i = lane; i < listed; i += 32) {
-        const uint32_t place = static_cast<uint32_t>(s.order[i]), key = ~static_cast<uint32_t>(s.order[i] >> 32);
+        const uint32_t place = static_cast<uint32_t>(s.order[i]), key = key_in(s.order[i]);
         if (place < begin || place >= end) continue;
         if (key == last_key) ++ties;
-        else if (key > last_key) sum += weight(value_of<LOW>(key)), ++keeps;
+        else if (key > last_key) more += s.value[i], ++keeps;
       }
+      sum += static_cast<double>(more) / kGrain;
     } else if (!last_key && min_p == 0.0) {
       if (!holes) {
         if (lane == 0) keeps = static_cast<uint32_t>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(to) * kV, slice.entries) - static_cast<int64_t>(from) * kV));
