@@ -33,7 +33,6 @@ template <int N>
 struct Of {
   static constexpr int kWarps = N / 32, kBins = kEach * N, kList = kEach * N;
 };
-constexpr unsigned long long kOut = 1ull << 63;          // the weight of what a filter has left out of a list
 constexpr double kGrain = 1125899906842624.0;            // weights of a list are whole numbers, 2^-50 of the largest
 constexpr float kWidest = 32.f;              // bins of 2 reach to e^-32 of the largest weight at most
 constexpr float kFar = 45.f;                 // weights below e^-45 of the largest count as zero: all of them together are below 1e-13
@@ -141,7 +140,7 @@ struct Shared {
   uint32_t listed, found[2], first;
   uint32_t low_before;
   double found_at;
-  unsigned long long found_sum, found_value;
+  unsigned long long found_sum;
   // what the row's CTAs have written here
   float most[kMaxCtas], least[kMaxCtas];
   double sums[2][kMaxCtas];
@@ -389,70 +388,65 @@ __device__ __noinline__ int collect(Shared<N, FILTERS>& s, int ctas, int most, b
 
 __device__ __forceinline__ uint32_t key_in(unsigned long long entry) { return ~static_cast<uint32_t>(entry >> 32); }
 
-// The beginning of the order by falling key whose values (value null: 1 each) first come to `target`, among a list's entries with keys of r: its last
-// key, and how many entries of that key belong to it.  All of them where they do not come to that; `whole` is what they come to.
-// BY_PLACE: among the entries of the key `only`, and ~place takes the place of the key.
-template <bool BY_PLACE, int N, bool FILTERS>
-__device__ __noinline__ uint2 find_end(Shared<N, FILTERS>& s, const unsigned long long* list, const unsigned long long* value, int n, Range r,
-                                       unsigned long long target, unsigned long long& whole, uint32_t only = 0) {
-  constexpr int kBins = Shared<N, FILTERS>::kBins;
-  unsigned long long before = 0;
-  for (bool begins = true;; begins = false) {
-    const int shift = shift_of<kBins>(r);
-    __syncthreads();
-    for (int b = threadIdx.x; b < kBins; b += N) s.mass[b] = 0;
-    if (threadIdx.x == 0) s.found[0] = 0, s.found_sum = before, s.found_value = 1;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += N) {
-      const uint32_t key = BY_PLACE ? ~static_cast<uint32_t>(list[i]) : key_in(list[i]);
-      const unsigned long long v = value ? value[i] : 1;
-      if (key >= r.low && key <= r.high && v != kOut && (!BY_PLACE || key_in(list[i]) == only)) atomicAdd(&s.mass[(r.high - key) >> shift], v);
-    }
-    __syncthreads();
-    unsigned long long mass[kEach], sum = 0, all;
+// Ascending (bitonic; padded to a power of two).  Entry q N + t is in a thread's register q: strides below 32 are shuffles, N and more lie within
+// a thread, those between go through memory, by turns to the list's place and another one.
+template <int N, int Q>
+__device__ __forceinline__ void sort_of(unsigned long long* list, unsigned long long* other, int n, int p) {
+  const int t = threadIdx.x;
+  unsigned long long e[Q];
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) mass[j] = s.mass[threadIdx.x * kEach + j], sum += mass[j];
-    unsigned long long upto = before + block_scan(s, sum, all);
-    if (begins) whole = all;
-    const unsigned long long want = min(target, before + all);
+  for (int q = 0; q < Q; ++q) e[q] = q * N + t < n ? list[q * N + t] : ~0ull;
+  unsigned long long *to = other, *spare = list;
+#pragma unroll 1
+  for (int k = 2; k <= p; k <<= 1) {
+#pragma unroll 1
+    for (int stride = k >> 1; stride > 0; stride >>= 1) {
+      if (stride >= N) {
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      if (upto < want && upto + mass[j] >= want) s.found[0] = threadIdx.x * kEach + j, s.found_sum = upto;
-      upto += mass[j];
-    }
-    __syncthreads();
-    const uint32_t high = r.high - (s.found[0] << shift), span = (1u << shift) - 1;
-    before = s.found_sum;
-    if (shift == 0) {
-      if (value) {
-        for (int i = threadIdx.x; i < n; i += N)
-          if (key_in(list[i]) == high && value[i] != kOut) s.found_value = value[i];
+        for (int q = 0; q < Q; ++q) {
+          const int other_q = q ^ (stride / N);
+#pragma unroll
+          for (int o = 0; o < Q; ++o)
+            if (o == other_q && o > q && ((e[q] > e[o]) == (((q * N + t) & k) == 0))) {
+              const unsigned long long x = e[q];
+              e[q] = e[o];
+              e[o] = x;
+            }
+        }
+        continue;
+      }
+      if (stride >= 32) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) to[q * N + t] = e[q];
         __syncthreads();
       }
-      const unsigned long long each = max(s.found_value, 1ull), left = max(want, before + 1) - before;
-      return make_uint2(high, static_cast<uint32_t>(min((left + each - 1) / each, 0xffffffffull)));
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const unsigned long long x = stride >= 32 ? to[q * N + (t ^ stride)] : __shfl_xor_sync(0xffffffffu, e[q], stride);
+        const bool low = (t & stride) == 0, up = ((q * N + t) & k) == 0;      // the lower of the two; ascending here
+        if ((x < e[q]) == (low == up)) e[q] = x;
+      }
+      if (stride >= 32) {
+        unsigned long long* x = to;
+        to = spare;
+        spare = x;
+      }
     }
-    r = Range{max(r.low, high > span ? high - span : 0u), high};
   }
-}
-
-// Leaves out of a list what lies behind the first `ties` entries of a key, in the order by falling key and rising place.
-template <int N, bool FILTERS>
-__device__ __noinline__ void leave_out(Shared<N, FILTERS>& s, const unsigned long long* list, unsigned long long* value, int n, uint2 end) {
-  uint32_t equal = 0;
-  for (int i = threadIdx.x; i < n; i += N) {
-    const uint32_t key = key_in(list[i]);
-    if (key < end.x) value[i] = kOut;
-    equal += key == end.x && value[i] != kOut;
-  }
-  equal = block_sum(s, equal);
-  if (equal <= end.y) return;
-  // (what earlier filters left out of the key are its last places: the first ones are the others' first ones)
-  unsigned long long unused;
-  const uint2 last = find_end<true>(s, list, nullptr, n, Range{0, 0xffffffffu}, end.y, unused, end.x);
-  for (int i = threadIdx.x; i < n; i += N)
-    if (key_in(list[i]) == end.x && ~static_cast<uint32_t>(list[i]) < last.x) value[i] = kOut;
   __syncthreads();
+#pragma unroll
+  for (int q = 0; q < Q; ++q)
+    if (q * N + t < n) list[q * N + t] = e[q];
+  __syncthreads();
+}
+template <int N>
+__device__ __noinline__ void sort(unsigned long long* list, unsigned long long* other, int n) {
+  int p = 64;
+  while (p < n) p <<= 1;
+  __syncthreads();
+  if (p <= N) sort_of<N, 1>(list, other, n, p);
+  else if (p <= 2 * N) sort_of<N, 2>(list, other, n, p);
+  else sort_of<N, 4>(list, other, n, p);
 }
 
 // FILTERS: top-k or top-p may be asked for (without them a smaller kernel, of which more threads fit an SM).
@@ -744,8 +738,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
     // 4. all that can be kept, where that is little enough for a list, which takes the place of CTA 0's share of the row
     if (listed_all) {
       const uint32_t top_bin = cuts ? k_bin : high_bin;
-      Range r = range_of<LOW, kBins>(m, unit, 0, top_bin);
-      each_hit(slice, from, to, fmaxf(value_of<LOW>(r.low), k_gate), [&](float z, int i) {
+      each_hit(slice, from, to, fmaxf(value_of<LOW>(range_of<LOW, kBins>(m, unit, 0, top_bin).low), k_gate), [&](float z, int i) {
         if (z > kNone && bin_of(z) <= top_bin) list(z, i);
       });
       spread(all, 0.0, 0u);
@@ -757,31 +750,27 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       row_sync(ctas);                        // (the lists are read)
       if (n >= 0) {
         if (cta != 0) return;
+        sort<N>(entry, value, n);
         for (int i = threadIdx.x; i < n; i += N) value[i] = __double2ull_rn(weight(value_of<LOW>(key_in(entry[i]))) * kGrain);
         __syncthreads();
-        unsigned long long unused, total = 0;
-        if (cuts) leave_out(s, entry, value, n, find_end<false>(s, entry, nullptr, n, r, k, unused));
-        if (nucleus) {
-          double goal = whole * kGrain;
-          if (cuts) {
-            for (int i = threadIdx.x; i < n; i += N) total += value[i] != kOut ? value[i] : 0;
-            block_scan(s, total, total);
-            goal = static_cast<double>(total);
-          }
-          goal = fmin(fmax(ceil(static_cast<double>(top_p) * goal), 1.0), 9.0e18);
-          leave_out(s, entry, value, n, find_end<false>(s, entry, value, n, r, __double2ull_rn(goal), unused));
-        }
-        // The draw, in the order of the places: sums by shares of the row, by shares of the share that the random number falls on, until what is
-        // left is little enough to compare each with each.
-        uint32_t kept = 0;
-        total = 0;
-        for (int i = threadIdx.x; i < n; i += N) {
-          if (min_p > 0.0 && value[i] != kOut && weight(value_of<LOW>(key_in(entry[i]))) < min_p) value[i] = kOut;
-          if (value[i] == kOut) continue;
-          ++kept;
-          total += value[i];
+        unsigned long long total = 0;
+        const int count = cuts ? min(n, static_cast<int>(k)) : n, per = (count + N - 1) / N, begin = min(static_cast<int>(threadIdx.x) * per, count),
+                  end = min(begin + per, count);
+        for (int i = begin; i < end; ++i) total += value[i];
+        unsigned long long ahead_of = total;
+        ahead_of = block_scan(s, ahead_of, total);
+        const double top = ceil(static_cast<double>(top_p) * (cuts ? static_cast<double>(total) : whole * kGrain));
+        const unsigned long long target = nucleus ? __double2ull_rn(fmin(fmax(top, 1.0), 9.0e18)) : ~0ull;
+        uint32_t kept = 0;                   // the first ones: each of the conditions holds for a beginning
+        for (int i = begin; i < end; ++i) {
+          kept += ahead_of < target && (min_p == 0.0 || weight(value_of<LOW>(key_in(entry[i]))) >= min_p);
+          ahead_of += value[i];
         }
         kept = block_sum(s, kept);
+        // The draw, in the order of the places: sums by shares of the row, by shares of the share that the random number falls on, until what is
+        // left is little enough to compare each with each.
+        total = 0;
+        for (int i = threadIdx.x; i < kept; i += N) total += value[i];
         block_scan(s, total, total);
         // the first sum beyond u of the whole; at most the last one
         const unsigned long long goal = min(u < 1.0 ? __double2ull_rz(u * static_cast<double>(total)) : total, total - 1);
@@ -792,9 +781,9 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
           for (int b = threadIdx.x; b < kBins; b += N) s.mass[b] = 0;
           if (threadIdx.x == 0) s.listed = 0;
           __syncthreads();
-          for (int i = threadIdx.x; i < n; i += N) {
+          for (int i = threadIdx.x; i < kept; i += N) {
             const int64_t at = static_cast<uint32_t>(entry[i]) - base;
-            if (value[i] != kOut && at >= 0 && at < size) atomicAdd(&s.mass[static_cast<uint32_t>(at) / part], value[i]);
+            if (at >= 0 && at < size) atomicAdd(&s.mass[static_cast<uint32_t>(at) / part], value[i]);
           }
           __syncthreads();
           unsigned long long mass[kEach], sum = 0, none;
@@ -810,9 +799,9 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
           base += static_cast<int64_t>(s.found[0]) * part;
           size = min(static_cast<int64_t>(part), size - static_cast<int64_t>(s.found[0]) * part);
           ahead = s.found_sum;
-          for (int i = threadIdx.x; i < n; i += N) {
+          for (int i = threadIdx.x; i < kept; i += N) {
             const int64_t at = static_cast<uint32_t>(entry[i]) - base;
-            if (value[i] == kOut || at < 0 || at >= size) continue;
+            if (at < 0 || at >= size) continue;
             const uint32_t to_at = atomicAdd(&s.listed, 1u);
             if (to_at < kSmall) s.order[to_at] = entry[i] << 32 | i;
           }
@@ -839,11 +828,12 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       __syncthreads();
     }
 
-    // All lists to every CTA.
+    // All lists, sorted, to every CTA.
     auto gather = [&]() {                    // (after a row_sync)
       const int n = collect(s, ctas, kList, true, s.order);
       row_sync(ctas);                        // (the lists are read)
       if (threadIdx.x == 0) s.listed = 0;
+      sort<N>(s.order, s.value, n);
       return n;
     };
     auto list_range = [&](const Range& r) {  // of keys; no more of them than a list holds
@@ -854,6 +844,19 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       row_sync(ctas);
       return gather();
     };
+    // Of a sorted list the entry that is the last one kept: its key, and how many of that key are kept with it.
+    auto ends_at = [&](int at) {
+      const uint32_t key = key_in(s.order[max(at, 0)]);
+      int begin = 0, end = max(at, 0);       // the first of that key
+      while (begin < end) {
+        const int mid = (begin + end) / 2;
+        if (key_in(s.order[mid]) > key) begin = mid + 1;
+        else end = mid;
+      }
+      last_key = key;
+      last_ties = at - begin + 1;
+    };
+
     // 5. the k-th largest
     if (cuts) {
       Range r = range_of<LOW, kBins>(m, unit, k_bin, k_bin);
@@ -863,11 +866,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
           if (bin_of(z) == k_bin) list(z, i);
         });
         row_sync(ctas);
-        const int n = gather();
-        unsigned long long unused;
-        const uint2 end = find_end<false>(s, s.order, nullptr, n, r, k - k_before, unused);
-        last_key = end.x;
-        last_ties = end.y;
+        ends_at(min(static_cast<int>(k - k_before), gather()) - 1);
       }
       while (!few_k) {
         const int shift = shift_of<kBins>(r);
@@ -890,11 +889,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         for (int j = 0; j < kEach; ++j) sum += some[j];
         uint32_t a = over + block_scan(s, sum, inside);
         if (shift > 0 && inside <= kList) {
-          const int n = list_range(r);
-          unsigned long long unused;
-          const uint2 end = find_end<false>(s, s.order, nullptr, n, r, k - over, unused);
-          last_key = end.x;
-          last_ties = end.y;
+          ends_at(min(static_cast<int>(k - over), list_range(r)) - 1);
           break;
         }
 #pragma unroll
@@ -927,15 +922,27 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       const double grain = ldexp(1.0, p.fraction), back = ldexp(1.0, -p.fraction);
       double target = 0.0;
       bool cut_inside = cuts && high_bin == k_bin;
-      // A list of n logits that follow others with the sum `above`, behind them what top-k leaves of its last key (where that is in reach):
+      // A sorted list of n logits that follow others with the sum `above`, behind them what top-k leaves of its last key (where that is in reach):
       // where the target is met.
       auto meet = [&](int n) {
-        for (int i = threadIdx.x; i < n; i += N) s.value[i] = __double2ull_rn(weight(value_of<LOW>(key_in(s.order[i]))) * kGrain);
         const double goal = fmax(ceil((target - above) * kGrain), 1.0);
-        unsigned long long sum;
-        const uint2 end = find_end<false>(s, s.order, s.value, n, r, __double2ull_rn(fmin(goal, 9.0e18)), sum);
-        last_key = end.x;
-        last_ties = end.y;
+        unsigned long long w[kEach], a = 0, sum;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+          const int i = threadIdx.x * kEach + j;
+          w[j] = i < n ? __double2ull_rn(weight(value_of<LOW>(key_in(s.order[i]))) * kGrain) : 0;
+          s.value[i] = w[j];
+          a += w[j];
+        }
+        a = block_scan(s, a, sum);
+        uint32_t passed = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+          a += w[j];
+          passed += static_cast<int>(threadIdx.x * kEach + j) < n && static_cast<double>(a) < goal;
+        }
+        passed = block_sum(s, passed);
+        ends_at(min(static_cast<int>(passed), n - 1));
         if (cut_inside && goal > static_cast<double>(sum)) {
           const double more = ceil((goal - static_cast<double>(sum)) / (cut_weight * kGrain));
           last_key = cut_key;
