@@ -33,12 +33,13 @@ template <int N>
 struct Of {
   static constexpr int kWarps = N / 32, kBins = kEach * N, kList = kEach * N;
 };
+constexpr unsigned long long kOut = 1ull << 63;          // the weight of what a filter has left out of a list
 constexpr double kGrain = 1125899906842624.0;            // weights of a list are whole numbers, 2^-50 of the largest
 constexpr float kWidest = 32.f;              // bins of 2 reach to e^-32 of the largest weight at most
 constexpr float kFar = 45.f;                 // weights below e^-45 of the largest count as zero: all of them together are below 1e-13
 constexpr int kMaxCtas = 16;                 // (more than eight: a launch that asks for them)
 constexpr int kTable = 256;
-constexpr uint32_t kSmall = 64;              // logits that are compared each with each, at most
+constexpr uint32_t kSmall = 128;             // logits that are compared each with each, at most
 
 struct SampleParams {
   const void* z;
@@ -138,7 +139,8 @@ struct Shared {
   uint32_t part_count[kWarps];
   float part_most[kWarps], part_least[kWarps], part_gate[kWarps];
   uint32_t listed, found[2], first;
-  uint32_t low_before;
+  uint32_t low_before, likely_before, likely_upto;
+  float last_bin;
   double found_at;
   unsigned long long found_sum;
   // what the row's CTAs have written here
@@ -596,7 +598,8 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
 
   // 2. counts by distance
   bool cuts = false;                         // top-k leaves something out
-  uint32_t k = 0, k_bin = 0, k_before = 0, k_upto = 0, low_bin = 0, high_bin = 0, nucleus_before = 0, nucleus_upto = 0;
+  uint32_t k = 0, k_bin = 0, k_before = 0, k_upto = 0, low_bin = 0, high_bin = 0, nucleus_before = 0, nucleus_upto = 0, likely_low = 0, likely_high = 0,
+           likely = 0;
   const bool filters = FILTERS && (top_k > 0 || nucleus);
   const float reach = holes ? kWidest : fminf(kWidest, fmaxf((m - least) / temperature, 1.f / 1024));
   const float scale = endless ? 0.f : fminf(kBins / reach / temperature, 1e30f);                                 // bins a unit
@@ -631,8 +634,9 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
     for (int j = 1; j < kEach; ++j) before[j] = before[j - 1] + count[j - 1];
 
     // 3. the bin of the k-th largest, and bins of the nucleus's end.  With S the sum of the weights, that is the first bin up to which they
-    // come to top_p S, or behind which (1 - top_p) S or less is left.  A bin's weights lie within a factor that is known: so what bins up to,
-    // or behind, which these sums have bounds.
+    // come to top_p S, or behind which (1 - top_p) S or less is left.  A bin's weights lie within a factor of the one at its middle: so what bins
+    // up to, or behind, which these sums have bounds (low_bin .. high_bin), and are about what the middles come to (likely_low .. likely_high, which
+    // the weights themselves have to bear out).
     cuts = top_k > 0 && (static_cast<uint32_t>(top_k) < finite || k_gate > -kLargest);
     k = cuts ? static_cast<uint32_t>(top_k) : finite;
 #pragma unroll
@@ -648,41 +652,54 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
     nucleus_before = k_before = s.low_before;
     low_bin = high_bin = k_bin;
     if (nucleus) {
-      // (in fp32: sums of up to 1024 bins are off by less than 1e-5 of the whole, bins that were found in 32 bits by less than that)
-      const float share = top_p, rest = 1.f - share, per_bin = static_cast<float>(width);
-      constexpr float slack = 1e-4f, lost = 2e-5f;
-      float low = 0.f, high = 0.f, all_low, all_high, bin_low[kEach], bin_high[kEach];
+      // (in fp32: sums of up to 1024 bins are off by less than 1e-5 of the whole, bins that were found in 32 bits by less than that; the last
+      // bin has what lies beyond it too, and where the temperature is that high, differences beyond fp32)
+      const float share = top_p, rest = 1.f - share, per_bin = static_cast<float>(width), spread_by = __expf(0.5f * per_bin) * 1.0001f, near = 1e-4f + 0.12f * per_bin;
+      constexpr float lost = 2e-5f;
+      float mid = 0.f, all_mid, bin_mid[kEach];
 #pragma unroll
       for (int j = 0; j < kEach; ++j) {
         const int b = threadIdx.x * kEach + j;
         const uint32_t c = before[j] < k ? min(count[j], k - before[j]) : 0;
-        bin_low[j] = b < kBins - 1 ? c * __expf(-(b + 1) * per_bin) : 0.f;
-        // (the last bin: what lies beyond it too, and where the temperature is that high, differences beyond fp32)
-        bin_high[j] = c * (b < kBins - 1 || temperature < 1e36f ? __expf(-b * per_bin) : 1.f);
-        low += bin_low[j];
-        high += bin_high[j];
+        bin_mid[j] = b < kBins - 1 ? c * __expf(-(b + 0.5f) * per_bin) : 0.f;
+        if (b == kBins - 1) s.last_bin = c * (temperature < 1e36f ? __expf(-b * per_bin) : 1.f);
+        mid += bin_mid[j];
       }
-      low = block_scan(s, low, all_low);
-      high = block_scan(s, high, all_high);
+      mid = block_scan(s, mid, all_mid);
+      const float last = s.last_bin, some = lost * all_mid;
+      const float all_low = (all_mid - some) / spread_by, all_high = (all_mid + some) * spread_by + last;
       uint32_t early = 0, open = 0;
 #pragma unroll
       for (int j = 0; j < kEach; ++j) {
-        low += bin_low[j];
-        high += bin_high[j];
-        early += (high + lost * all_high) * (1 + slack) < share * all_low || (all_low - low - lost * all_low) * (1 - slack) > rest * all_high;
-        open += !((low - lost * all_low) * (1 - slack) >= share * all_high || (all_high - high + lost * all_high) * (1 + slack) <= rest * all_low);
+        const bool end = threadIdx.x * kEach + j == kBins - 1;
+        mid += bin_mid[j];
+        const float left = end ? 0.f : fmaxf(all_mid - mid, 0.f);
+        const float high = end ? all_high : (mid + some) * spread_by, low = (mid - some) / spread_by;
+        const float left_low = end ? 0.f : (left - some) / spread_by, left_high = end ? 0.f : (left + some) * spread_by + last;
+        early += high < share * all_low || left_low > rest * all_high;
+        open += !(low >= share * all_high || left_high <= rest * all_low);
+        // the same by the middles alone, and a little to either side
+        early += (mid * (1 + near) < share * all_mid || left * (1 - near) > rest * all_mid ? 1u : 0u) << 16;
+        open += (mid * (1 - near) >= share * all_mid || left * (1 + near) <= rest * all_mid ? 0u : 1u) << 16;
       }
-      const uint32_t both = block_sum(s, early << 16 | open);
-      low_bin = min(both >> 16, k_bin);
-      high_bin = min(max(both & 0xffffu, low_bin), k_bin);
+      early = block_sum(s, early);
+      open = block_sum(s, open);
+      low_bin = min(early & 0xffffu, k_bin);
+      high_bin = min(max(open & 0xffffu, low_bin), k_bin);
+      likely_low = min(max(early >> 16, low_bin), high_bin);
+      likely_high = min(max(open >> 16, likely_low), high_bin);
 #pragma unroll
       for (int j = 0; j < kEach; ++j) {
-        if (threadIdx.x * kEach + j == high_bin) s.found[1] = before[j] + count[j];
-        if (threadIdx.x * kEach + j == low_bin) s.low_before = before[j];
+        const uint32_t b = threadIdx.x * kEach + j;
+        if (b == high_bin) s.found[1] = before[j] + count[j];
+        if (b == low_bin) s.low_before = before[j];
+        if (b == likely_low) s.likely_before = before[j];
+        if (b == likely_high) s.likely_upto = before[j] + count[j];
       }
       __syncthreads();
       nucleus_upto = s.found[1];
       nucleus_before = s.low_before;
+      likely = s.likely_upto - s.likely_before;
     }
   }
 
@@ -690,7 +707,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
   // is listed, where it is no more than a list holds (and not all that can be kept is listed below).
   const int room = p.resident >= 2 * kList ? 2 * kList : p.resident >= kList ? kList : 0;
   const bool listed_all = filters && (cuts ? k_upto : nucleus_upto) <= room;
-  const bool few = filters && nucleus && !cuts && !listed_all && nucleus_upto - nucleus_before <= kList;
+  const bool few = filters && nucleus && !cuts && !listed_all && likely <= kList;
   // Adds a logit to this CTA's list.
   auto list = [&](float z, int i) {
     const uint32_t at = atomicAdd(&s.listed, 1u);
@@ -700,7 +717,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
   uint32_t over_count = 0;
   if (!cuts && (nucleus || min_p == 0.0)) {
     if (few) {
-      const float low_edge = static_cast<float>(low_bin), high_edge = high_bin < kBins - 1 ? static_cast<float>(high_bin + 1) : INFINITY;
+      const float low_edge = static_cast<float>(likely_low), high_edge = static_cast<float>(likely_high + 1);
 #pragma unroll 1
       for (int i = from + lane; i < to; i += 32) {
         float v[kV];
@@ -712,7 +729,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
           const float x = endless ? (v[j] == m ? 0.f : INFINITY) : (m - v[j]) * scale;         // as bin_of has it
           all += w;
           if (x < low_edge && v[j] > kNone) over += w, ++over_count;
-          else if ((x < high_edge || high_bin == kBins - 1) && v[j] > kNone) hits |= 1u << j;
+          else if ((x < high_edge || likely_high == kBins - 1) && v[j] > kNone) hits |= 1u << j;
         }
         for (; hits; hits &= hits - 1) {
           const int e = i * kV + __ffs(hits) - 1;
@@ -750,27 +767,97 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       row_sync(ctas);                        // (the lists are read)
       if (n >= 0) {
         if (cta != 0) return;
-        sort<N>(entry, value, n);
+        // In the order by falling key and rising place: where the filters end, by the logits of the bins they end in, each compared with each,
+        // and what is left out; or, where these are many, all sorted.
+        if (threadIdx.x == 0) s.found[0] = 0, s.found[1] = 0;
         for (int i = threadIdx.x; i < n; i += N) value[i] = __double2ull_rn(weight(value_of<LOW>(key_in(entry[i]))) * kGrain);
         __syncthreads();
-        unsigned long long total = 0;
-        const int count = cuts ? min(n, static_cast<int>(k)) : n, per = (count + N - 1) / N, begin = min(static_cast<int>(threadIdx.x) * per, count),
-                  end = min(begin + per, count);
-        for (int i = begin; i < end; ++i) total += value[i];
-        unsigned long long ahead_of = total;
-        ahead_of = block_scan(s, ahead_of, total);
-        const double top = ceil(static_cast<double>(top_p) * (cuts ? static_cast<double>(total) : whole * kGrain));
-        const unsigned long long target = nucleus ? __double2ull_rn(fmin(fmax(top, 1.0), 9.0e18)) : ~0ull;
-        uint32_t kept = 0;                   // the first ones: each of the conditions holds for a beginning
-        for (int i = begin; i < end; ++i) {
-          kept += ahead_of < target && (min_p == 0.0 || weight(value_of<LOW>(key_in(entry[i]))) >= min_p);
-          ahead_of += value[i];
+        unsigned long long total = 0, ahead_of = 0;
+        uint32_t kept = 0;
+        auto pick = [&](uint32_t a, uint32_t b, uint32_t* count) {           // to s.order, and their numbers to s.value
+          for (int i = threadIdx.x; i < n; i += N) {
+            const uint32_t bin = bin_of(value_of<LOW>(key_in(entry[i])));
+            if (value[i] == kOut || bin < a || bin > b) continue;
+            const uint32_t at = atomicAdd(count, 1u);
+            if (at < kSmall) s.order[at] = entry[i], s.value[at] = i;
+          }
+          __syncthreads();
+          return *count;
+        };
+        bool sorts = cuts && k_upto - k_before > kSmall;
+        if (cuts && !sorts) {
+          const uint32_t count = pick(k_bin, k_bin, &s.found[0]);
+          if (threadIdx.x < count) {
+            const unsigned long long me = s.order[threadIdx.x];
+            uint32_t rank = 0;
+#pragma unroll 4
+            for (uint32_t j = 0; j < count; ++j) rank += s.order[j] < me;
+            if (rank >= k - k_before) value[s.value[threadIdx.x]] = kOut;
+          }
+          __syncthreads();
         }
-        kept = block_sum(s, kept);
+        if (nucleus && !sorts) {
+          unsigned long long mine = 0, inside = 0;
+          for (int i = threadIdx.x; i < n; i += N) {
+            if (value[i] == kOut) continue;
+            const uint32_t bin = bin_of(value_of<LOW>(key_in(entry[i])));
+            mine += value[i];
+            if (bin < likely_low) ahead_of += value[i];
+            else if (bin <= likely_high) inside += value[i];
+          }
+          if (cuts) block_scan(s, mine, total);
+          block_scan(s, ahead_of, ahead_of);
+          block_scan(s, inside, inside);
+          const double goal = fmax(ceil(static_cast<double>(top_p) * (cuts ? static_cast<double>(total) : whole * kGrain)), 1.0);
+          const unsigned long long target = __double2ull_rn(fmin(goal, 9.0e18));
+          const uint32_t count = pick(likely_low, likely_high, &s.found[1]);
+          sorts = count > kSmall || !(ahead_of < target && target <= ahead_of + inside);
+          if (!sorts) {
+            bool out = false;
+            if (threadIdx.x < count) {
+              const unsigned long long me = s.order[threadIdx.x];
+              unsigned long long upto = ahead_of;
+#pragma unroll 4
+              for (uint32_t j = 0; j < count; ++j)
+                if (s.order[j] < me) upto += value[s.value[j]];
+              out = upto >= target;
+            }
+            __syncthreads();
+            if (out) value[s.value[threadIdx.x]] = kOut;
+            for (int i = threadIdx.x; i < n; i += N)
+              if (bin_of(value_of<LOW>(key_in(entry[i]))) > likely_high) value[i] = kOut;
+            __syncthreads();
+          }
+        }
+        if (sorts) {
+          sort<N>(entry, value, n);
+          for (int i = threadIdx.x; i < n; i += N) value[i] = __double2ull_rn(weight(value_of<LOW>(key_in(entry[i]))) * kGrain);
+          __syncthreads();
+          const int count = cuts ? min(n, static_cast<int>(k)) : n, per = (count + N - 1) / N, begin = min(static_cast<int>(threadIdx.x) * per, count),
+                    end = min(begin + per, count);
+          ahead_of = 0;
+          for (int i = begin; i < end; ++i) ahead_of += value[i];
+          ahead_of = block_scan(s, ahead_of, total);
+          const double goal = ceil(static_cast<double>(top_p) * (cuts ? static_cast<double>(total) : whole * kGrain));
+          const unsigned long long target = nucleus ? __double2ull_rn(fmin(fmax(goal, 1.0), 9.0e18)) : ~0ull;
+          for (int i = begin; i < end; ++i) {
+            const unsigned long long v = value[i];
+            if (ahead_of >= target) value[i] = kOut;
+            ahead_of += v;
+          }
+          for (int i = count + threadIdx.x; i < n; i += N) value[i] = kOut;
+          __syncthreads();
+        }
         // The draw, in the order of the places: sums by shares of the row, by shares of the share that the random number falls on, until what is
         // left is little enough to compare each with each.
         total = 0;
-        for (int i = threadIdx.x; i < kept; i += N) total += value[i];
+        for (int i = threadIdx.x; i < n; i += N) {
+          if (min_p > 0.0 && value[i] != kOut && weight(value_of<LOW>(key_in(entry[i]))) < min_p) value[i] = kOut;
+          if (value[i] == kOut) continue;
+          ++kept;
+          total += value[i];
+        }
+        kept = block_sum(s, kept);
         block_scan(s, total, total);
         // the first sum beyond u of the whole; at most the last one
         const unsigned long long goal = min(u < 1.0 ? __double2ull_rz(u * static_cast<double>(total)) : total, total - 1);
@@ -781,9 +868,9 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
           for (int b = threadIdx.x; b < kBins; b += N) s.mass[b] = 0;
           if (threadIdx.x == 0) s.listed = 0;
           __syncthreads();
-          for (int i = threadIdx.x; i < kept; i += N) {
+          for (int i = threadIdx.x; i < n; i += N) {
             const int64_t at = static_cast<uint32_t>(entry[i]) - base;
-            if (at >= 0 && at < size) atomicAdd(&s.mass[static_cast<uint32_t>(at) / part], value[i]);
+            if (value[i] != kOut && at >= 0 && at < size) atomicAdd(&s.mass[static_cast<uint32_t>(at) / part], value[i]);
           }
           __syncthreads();
           unsigned long long mass[kEach], sum = 0, none;
@@ -799,9 +886,9 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
           base += static_cast<int64_t>(s.found[0]) * part;
           size = min(static_cast<int64_t>(part), size - static_cast<int64_t>(s.found[0]) * part);
           ahead = s.found_sum;
-          for (int i = threadIdx.x; i < kept; i += N) {
+          for (int i = threadIdx.x; i < n; i += N) {
             const int64_t at = static_cast<uint32_t>(entry[i]) - base;
-            if (at < 0 || at >= size) continue;
+            if (value[i] == kOut || at < 0 || at >= size) continue;
             const uint32_t to_at = atomicAdd(&s.listed, 1u);
             if (to_at < kSmall) s.order[to_at] = entry[i] << 32 | i;
           }
@@ -942,23 +1029,27 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
           passed += static_cast<int>(threadIdx.x * kEach + j) < n && static_cast<double>(a) < goal;
         }
         passed = block_sum(s, passed);
+        if (few && listed >= 0 && !(above < target && goal <= static_cast<double>(sum))) return false;
         ends_at(min(static_cast<int>(passed), n - 1));
         if (cut_inside && goal > static_cast<double>(sum)) {
           const double more = ceil((goal - static_cast<double>(sum)) / (cut_weight * kGrain));
           last_key = cut_key;
           last_ties = more >= cut_ties || !(cut_weight > 0.0) ? cut_ties : more > 1.0 ? static_cast<uint32_t>(more) : 1u;
         }
+        return true;
       };
       // sums of the weights: of all that top-k leaves, and of those above the range (by bins at first, then by keys)
       const bool few_left = nucleus_upto - nucleus_before <= kList;
-      if (few) {                  // (the sums are there already, and the list)
+      if (few) {                             // (the sums are there already, and the list)
         spread(over, all, 0u);
         row_sync(ctas);
         double sum_all;
         gathered(above, sum_all, none);
         target = static_cast<double>(top_p) * sum_all;
         listed = gather();
-      } else
+        if (!meet(listed)) listed = -1;      // (the end lies outside the likely bins)
+      }
+      if (listed < 0)
       for (bool begins = true;; begins = false) {
         const int shift = shift_of<kBins>(r);
         __syncthreads();
@@ -993,14 +1084,14 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         gathered(above, sum_all, inside);
         if (begins) target = static_cast<double>(top_p) * (sum_all + (cuts ? cut_ties * cut_weight : 0.0));
         if (few_left) {
-          listed = gather();
+          meet(gather());
           break;
         }
         unsigned long long some[kEach], sum = 0, mass;
         sum_bins(s, s.mass, ctas, cta, some);
         cut_inside = cuts && cut_key >= r.low && cut_key <= r.high;
         if (shift > 0 && inside <= kList) {
-          listed = list_range(Range{max(r.low, cut_key + 1), r.high});
+          meet(list_range(Range{max(r.low, cut_key + 1), r.high}));
           break;
         }
 #pragma unroll
@@ -1033,7 +1124,6 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         }
         r = Range{max(r.low, top > span ? top - span : 0u), top};
       }
-      if (listed >= 0) meet(listed);
     }
   }
 
@@ -1044,7 +1134,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
   {
     double sum = all;
     uint32_t keeps = 0, ties = 0;
-    if (few && min_p == 0.0) {               // what lies in the bins before, and what is kept of the list
+    if (listed >= 0 && min_p == 0.0) {       // what lies in the bins before, and what is kept of the list
       sum = over;
       keeps = over_count;
       const int64_t begin = first + static_cast<int64_t>(from) * kV, end = first + static_cast<int64_t>(to) * kV;
