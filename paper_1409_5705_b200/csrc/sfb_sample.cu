@@ -39,7 +39,7 @@ constexpr float kWidest = 32.f;              // bins of 2 reach to e^-32 of the 
 constexpr float kFar = 45.f;                 // weights below e^-45 of the largest count as zero: all of them together are below 1e-13
 constexpr int kMaxCtas = 16;                 // (more than eight: a launch that asks for them)
 constexpr int kTable = 256;
-constexpr uint32_t kSmall = 128;             // logits that are compared each with each, at most
+constexpr uint32_t kSmall = 64;              // logits that are compared each with each, at most
 
 struct SampleParams {
   const void* z;
@@ -49,7 +49,7 @@ struct SampleParams {
   int32_t *ids, *kept;
   float* logp;
   int32_t ctas, share, resident;             // of a row; vectors of 16 bytes that a CTA has at most, and that its shared memory holds
-  int32_t fraction;                          // F
+  int32_t fraction, place_bits;              // F; of a class's number
   bool wide;
 };
 
@@ -142,7 +142,8 @@ struct Shared {
   uint32_t low_before, likely_before, likely_upto;
   float last_bin;
   double found_at;
-  unsigned long long found_sum;
+  unsigned long long found_sum, found_entry, small_entry[kSmall], small_value[kSmall];
+  uint32_t small;
   // what the row's CTAs have written here
   float most[kMaxCtas], least[kMaxCtas];
   double sums[2][kMaxCtas];
@@ -278,17 +279,21 @@ struct Slice {
   }
 };
 
-// Calls f(z, place in the share) for the logits of a warp's vectors that are at least `gate`, one after another.
+// Calls f(z, place in the share) for the logits of a warp's vectors from `gate` to `top`, one after another.
 template <typename T, typename F>
-__device__ __forceinline__ void each_hit(const Slice<T>& s, int from, int to, float gate, F&& f) {
-  for (int i = from + (threadIdx.x & 31); i < to; i += 32) {
-    const uint4 w = s.vector(i);
+__device__ __forceinline__ void each_hit(const Slice<T>& s, int from, int to, float gate, float top, F&& f) {
+  const int first = from + (threadIdx.x & 31);
+  uint4 next = first < to ? s.vector(first) : make_uint4(0, 0, 0, 0);
+#pragma unroll 1
+  for (int i = first; i < to; i += 32) {
+    const uint4 w = next;
+    if (i + 32 < to) next = s.vector(i + 32);
     if (!(Type<T>::largest(Type<T>::most(w)) >= gate)) continue;
     float v[Slice<T>::kV];
     Slice<T>::widen(w, v);
     uint32_t hits = 0;
 #pragma unroll
-    for (int j = 0; j < Slice<T>::kV; ++j) hits |= (v[j] >= gate ? 1u : 0u) << j;
+    for (int j = 0; j < Slice<T>::kV; ++j) hits |= (v[j] >= gate && v[j] <= top ? 1u : 0u) << j;
 #pragma unroll 1
     for (; hits; hits &= hits - 1) {
       const int at = i * Slice<T>::kV + __ffs(hits) - 1;
@@ -361,7 +366,15 @@ __device__ __noinline__ void sum_bins(Shared<N, FILTERS>& s, const V* bins, int 
   for (int j = 0; j < kEach; ++j) out[j] = read(&summed[at + j], owner);
 }
 
-// What the CTAs have listed, CTA by CTA: entries (~key, place).  Returns how many; -1: more than `most`, or than one of the lists holds.  (Every
+// Adds to a whole number of 64 bits in shared memory by its halves: the hardware adds 32 bits at a time, and takes many threads at one address in
+// its stride, where a 64-bit addition is a loop that each of them wins once.
+__device__ __forceinline__ void add(unsigned long long* to, unsigned long long v) {
+  uint32_t* half = reinterpret_cast<uint32_t*>(to);
+  const uint32_t low = static_cast<uint32_t>(v), old = atomicAdd(half, low), high = static_cast<uint32_t>(v >> 32) + (old + low < old ? 1 : 0);
+  if (high) atomicAdd(half + 1, high);
+}
+
+// What the CTAs have listed, CTA by CTA: entries.  Returns how many; -1: more than `most`, or than one of the lists holds.  (Every
 // CTA has passed a row_sync since it listed.)
 template <int N, bool FILTERS>
 __device__ __noinline__ int collect(Shared<N, FILTERS>& s, int ctas, int most, bool wanted, unsigned long long* to) {
@@ -388,67 +401,75 @@ __device__ __noinline__ int collect(Shared<N, FILTERS>& s, int ctas, int most, b
   return static_cast<int>(all);
 }
 
-__device__ __forceinline__ uint32_t key_in(unsigned long long entry) { return ~static_cast<uint32_t>(entry >> 32); }
+// Entries of lists: falling keys and rising places in one number, places in its low `bits` bits.
+__device__ __forceinline__ uint32_t key_in(unsigned long long entry, int bits) { return ~static_cast<uint32_t>(entry >> bits); }
+__device__ __forceinline__ uint32_t place_in(unsigned long long entry, int bits) { return static_cast<uint32_t>(entry) & ((1u << bits) - 1); }
 
-// Ascending (bitonic; padded to a power of two).  Entry q N + t is in a thread's register q: strides below 32 are shuffles, N and more lie within
-// a thread, those between go through memory, by turns to the list's place and another one.
-template <int N, int Q>
-__device__ __forceinline__ void sort_of(unsigned long long* list, unsigned long long* other, int n, int p) {
-  const int t = threadIdx.x;
-  unsigned long long e[Q];
-#pragma unroll
-  for (int q = 0; q < Q; ++q) e[q] = q * N + t < n ? list[q * N + t] : ~0ull;
-  unsigned long long *to = other, *spare = list;
-#pragma unroll 1
-  for (int k = 2; k <= p; k <<= 1) {
-#pragma unroll 1
-    for (int stride = k >> 1; stride > 0; stride >>= 1) {
-      if (stride >= N) {
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-          const int other_q = q ^ (stride / N);
-#pragma unroll
-          for (int o = 0; o < Q; ++o)
-            if (o == other_q && o > q && ((e[q] > e[o]) == (((q * N + t) & k) == 0))) {
-              const unsigned long long x = e[q];
-              e[q] = e[o];
-              e[o] = x;
-            }
-        }
-        continue;
-      }
-      if (stride >= 32) {
-#pragma unroll
-        for (int q = 0; q < Q; ++q) to[q * N + t] = e[q];
-        __syncthreads();
-      }
-#pragma unroll
-      for (int q = 0; q < Q; ++q) {
-        const unsigned long long x = stride >= 32 ? to[q * N + (t ^ stride)] : __shfl_xor_sync(0xffffffffu, e[q], stride);
-        const bool low = (t & stride) == 0, up = ((q * N + t) & k) == 0;      // the lower of the two; ascending here
-        if ((x < e[q]) == (low == up)) e[q] = x;
-      }
-      if (stride >= 32) {
-        unsigned long long* x = to;
-        to = spare;
-        spare = x;
-      }
+// Entries in ascending order are logits in the order by falling logit and rising place.  The last entry of the beginning of that order whose
+// values (value null: 1 each; kOut: none) first come to `target` (1 or more), or the last of all: looked for among [low, high] first, among all where
+// it is not there.  By sums of bins of the range, then of the bin that it is in, until that has few entries, which are compared each with each.
+template <int N, bool FILTERS>
+__device__ __noinline__ unsigned long long find_end(Shared<N, FILTERS>& s, const unsigned long long* list, const unsigned long long* value, int n,
+                                                    unsigned long long low, unsigned long long high, unsigned long long target) {
+  constexpr int kBins = Shared<N, FILTERS>::kBins;
+  auto worth = [&](int i) { return value ? (value[i] == kOut ? 0 : value[i]) : 1ull; };
+  unsigned long long before = 0, all;
+  for (int i = threadIdx.x; i < n; i += N) before += list[i] < low ? worth(i) : 0;
+  block_scan(s, before, before);
+  for (bool begins = true;; begins = false) {
+    const unsigned long long width = high - low;
+    const int shift = width < kBins ? 0 : __clz(kBins) + 33 - __clzll(static_cast<long long>(width));
+    for (int b = threadIdx.x; b < kBins; b += N) s.mass[b] = 0;
+    if (threadIdx.x == 0) s.small = 0, s.found[0] = 0, s.found_sum = before;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += N) {
+      const unsigned long long v = worth(i);
+      if (v && list[i] >= low && list[i] <= high) add(&s.mass[(list[i] - low) >> shift], v);
     }
-  }
-  __syncthreads();
+    __syncthreads();
+    unsigned long long mass[kEach], sum = 0;
 #pragma unroll
-  for (int q = 0; q < Q; ++q)
-    if (q * N + t < n) list[q * N + t] = e[q];
-  __syncthreads();
-}
-template <int N>
-__device__ __noinline__ void sort(unsigned long long* list, unsigned long long* other, int n) {
-  int p = 64;
-  while (p < n) p <<= 1;
-  __syncthreads();
-  if (p <= N) sort_of<N, 1>(list, other, n, p);
-  else if (p <= 2 * N) sort_of<N, 2>(list, other, n, p);
-  else sort_of<N, 4>(list, other, n, p);
+    for (int j = 0; j < kEach; ++j) mass[j] = s.mass[threadIdx.x * kEach + j], sum += mass[j];
+    unsigned long long upto = before + block_scan(s, sum, all);
+    if (begins && (target <= before || target > before + all) && (low > 0 || ~high > 0)) {
+      low = before = 0;
+      high = ~0ull;
+      begins = true;
+      continue;
+    }
+    const unsigned long long want = min(target, before + all);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      if (upto < want && upto + mass[j] >= want) s.found[0] = threadIdx.x * kEach + j, s.found_sum = upto;
+      upto += mass[j];
+    }
+    __syncthreads();
+    low += static_cast<unsigned long long>(s.found[0]) << shift;
+    high = min(high, low + ((1ull << shift) - 1));
+    before = s.found_sum;
+    for (int i = threadIdx.x; i < n; i += N) {
+      if (list[i] < low || list[i] > high || !worth(i)) continue;
+      const uint32_t at = atomicAdd(&s.small, 1u);
+      if (at < kSmall) s.small_entry[at] = list[i], s.small_value[at] = worth(i);
+    }
+    __syncthreads();
+    const uint32_t count = s.small;
+    if (count <= kSmall) {
+      if (threadIdx.x < count) {
+        const unsigned long long me = s.small_entry[threadIdx.x], mine = s.small_value[threadIdx.x];
+        unsigned long long ahead = before;
+#pragma unroll 4
+        for (uint32_t j = 0; j < count; ++j)
+          if (s.small_entry[j] < me) ahead += s.small_value[j];
+        if (ahead < want && ahead + mine >= want) s.found_entry = me;
+      }
+      __syncthreads();
+      const unsigned long long end = s.found_entry;
+      __syncthreads();
+      return end;
+    }
+    __syncthreads();
+  }
 }
 
 // FILTERS: top-k or top-p may be asked for (without them a smaller kernel, of which more threads fit an SM).
@@ -462,7 +483,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int i = threadIdx.x; i < kTable; i += N) s.power[i] = exp2(i / static_cast<double>(kTable));
   if (threadIdx.x == 0) s.listed = 0, s.first = 0xffffffffu;
-  const int ctas = p.ctas;
+  const int ctas = p.ctas, bits = p.place_bits;
   if (ctas > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
   pdl_wait();
 
@@ -555,7 +576,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
   }
   if (!(temperature > 0.f) || top_k == 1 || top_p <= 0.f) {                   // nothing to draw: the first place of m
     uint32_t at = 0xffffffffu;
-    each_hit(slice, from, to, m, [&](float, int i) { at = min(at, static_cast<uint32_t>(first + i)); });
+    each_hit(slice, from, to, m, INFINITY, [&](float, int i) { at = min(at, static_cast<uint32_t>(first + i)); });
     at = __reduce_min_sync(0xffffffffu, at);
     if (lane == 0) atomicMin(&s.first, at);
     __syncthreads();
@@ -613,12 +634,14 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
     __syncthreads();
     // (all logits; those from k_gate on, where they are top_k or more and nothing is asked of the others)
     if (k_gate > -kLargest) {
-      each_hit(slice, from, to, k_gate, [&](float z, int) { atomicAdd(&s.count[bin_of(z)], 1u); });
+      each_hit(slice, from, to, k_gate, INFINITY, [&](float z, int) { atomicAdd(&s.count[bin_of(z)], 1u); });
     } else {
+      uint4 next = from + lane < to ? slice.vector(from + lane) : make_uint4(0, 0, 0, 0);
 #pragma unroll 1
       for (int i = from + lane; i < to; i += 32) {
         float v[kV];
-        Slice<T>::widen(slice.vector(i), v);
+        Slice<T>::widen(next, v);
+        if (i + 32 < to) next = slice.vector(i + 32);
 #pragma unroll
         for (int j = 0; j < kV; ++j)
           if (v[j] > kNone) atomicAdd(&s.count[bin_of(v[j])], 1u);
@@ -711,17 +734,19 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
   // Adds a logit to this CTA's list.
   auto list = [&](float z, int i) {
     const uint32_t at = atomicAdd(&s.listed, 1u);
-    if (at < kList) s.list[at] = static_cast<unsigned long long>(~key_of<LOW>(z)) << 32 | static_cast<uint32_t>(first + i);
+    if (at < kList) s.list[at] = static_cast<unsigned long long>(~key_of<LOW>(z)) << bits | static_cast<uint32_t>(first + i);
   };
   double all = 0.0, over = 0.0;
   uint32_t over_count = 0;
   if (!cuts && (nucleus || min_p == 0.0)) {
     if (few) {
       const float low_edge = static_cast<float>(likely_low), high_edge = static_cast<float>(likely_high + 1);
+      uint4 next = from + lane < to ? slice.vector(from + lane) : make_uint4(0, 0, 0, 0);
 #pragma unroll 1
       for (int i = from + lane; i < to; i += 32) {
         float v[kV];
-        Slice<T>::widen(slice.vector(i), v);
+        Slice<T>::widen(next, v);
+        if (i + 32 < to) next = slice.vector(i + 32);
         uint32_t hits = 0;
 #pragma unroll
         for (int j = 0; j < kV; ++j) {
@@ -750,12 +775,15 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
   uint32_t last_key = 0, last_ties = 0xffffffffu;        // of what is kept: all above the key, and so many that have it
   int listed = -1;                           // in s.order, s.value: of the nucleus's end
   if (filters) {
+    // Of a range of keys the first and the last entry.
+    auto first_of = [&](const Range& r) { return static_cast<unsigned long long>(~r.high) << bits; };
+    auto last_of = [&](const Range& r) { return (static_cast<unsigned long long>(~r.low) << bits) + ((1ull << bits) - 1); };
     double above = 0.0, whole = 0.0;
     uint32_t none;
     // 4. all that can be kept, where that is little enough for a list, which takes the place of CTA 0's share of the row
     if (listed_all) {
       const uint32_t top_bin = cuts ? k_bin : high_bin;
-      each_hit(slice, from, to, fmaxf(value_of<LOW>(range_of<LOW, kBins>(m, unit, 0, top_bin).low), k_gate), [&](float z, int i) {
+      each_hit(slice, from, to, fmaxf(value_of<LOW>(range_of<LOW, kBins>(m, unit, 0, top_bin).low), k_gate), INFINITY, [&](float z, int i) {
         if (z > kNone && bin_of(z) <= top_bin) list(z, i);
       });
       spread(all, 0.0, 0u);
@@ -767,92 +795,35 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       row_sync(ctas);                        // (the lists are read)
       if (n >= 0) {
         if (cta != 0) return;
-        // In the order by falling key and rising place: where the filters end, by the logits of the bins they end in, each compared with each,
-        // and what is left out; or, where these are many, all sorted.
-        if (threadIdx.x == 0) s.found[0] = 0, s.found[1] = 0;
-        for (int i = threadIdx.x; i < n; i += N) value[i] = __double2ull_rn(weight(value_of<LOW>(key_in(entry[i]))) * kGrain);
+        for (int i = threadIdx.x; i < n; i += N) value[i] = __double2ull_rn(weight(value_of<LOW>(key_in(entry[i], bits))) * kGrain);
         __syncthreads();
-        unsigned long long total = 0, ahead_of = 0;
+        unsigned long long total = 0;
         uint32_t kept = 0;
-        auto pick = [&](uint32_t a, uint32_t b, uint32_t* count) {           // to s.order, and their numbers to s.value
-          for (int i = threadIdx.x; i < n; i += N) {
-            const uint32_t bin = bin_of(value_of<LOW>(key_in(entry[i])));
-            if (value[i] == kOut || bin < a || bin > b) continue;
-            const uint32_t at = atomicAdd(count, 1u);
-            if (at < kSmall) s.order[at] = entry[i], s.value[at] = i;
-          }
+        auto leave_out = [&](unsigned long long end) {
+          for (int i = threadIdx.x; i < n; i += N)
+            if (entry[i] > end) value[i] = kOut;
           __syncthreads();
-          return *count;
         };
-        bool sorts = cuts && k_upto - k_before > kSmall;
-        if (cuts && !sorts) {
-          const uint32_t count = pick(k_bin, k_bin, &s.found[0]);
-          if (threadIdx.x < count) {
-            const unsigned long long me = s.order[threadIdx.x];
-            uint32_t rank = 0;
-#pragma unroll 4
-            for (uint32_t j = 0; j < count; ++j) rank += s.order[j] < me;
-            if (rank >= k - k_before) value[s.value[threadIdx.x]] = kOut;
-          }
-          __syncthreads();
+        if (cuts) {
+          const Range r = range_of<LOW, kBins>(m, unit, k_bin, k_bin);
+          leave_out(find_end(s, entry, nullptr, n, first_of(r), last_of(r), k));
         }
-        if (nucleus && !sorts) {
-          unsigned long long mine = 0, inside = 0;
-          for (int i = threadIdx.x; i < n; i += N) {
-            if (value[i] == kOut) continue;
-            const uint32_t bin = bin_of(value_of<LOW>(key_in(entry[i])));
-            mine += value[i];
-            if (bin < likely_low) ahead_of += value[i];
-            else if (bin <= likely_high) inside += value[i];
+        if (nucleus) {
+          double goal = whole * kGrain;
+          if (cuts) {
+            for (int i = threadIdx.x; i < n; i += N) total += value[i] != kOut ? value[i] : 0;
+            block_scan(s, total, total);
+            goal = static_cast<double>(total);
           }
-          if (cuts) block_scan(s, mine, total);
-          block_scan(s, ahead_of, ahead_of);
-          block_scan(s, inside, inside);
-          const double goal = fmax(ceil(static_cast<double>(top_p) * (cuts ? static_cast<double>(total) : whole * kGrain)), 1.0);
-          const unsigned long long target = __double2ull_rn(fmin(goal, 9.0e18));
-          const uint32_t count = pick(likely_low, likely_high, &s.found[1]);
-          sorts = count > kSmall || !(ahead_of < target && target <= ahead_of + inside);
-          if (!sorts) {
-            bool out = false;
-            if (threadIdx.x < count) {
-              const unsigned long long me = s.order[threadIdx.x];
-              unsigned long long upto = ahead_of;
-#pragma unroll 4
-              for (uint32_t j = 0; j < count; ++j)
-                if (s.order[j] < me) upto += value[s.value[j]];
-              out = upto >= target;
-            }
-            __syncthreads();
-            if (out) value[s.value[threadIdx.x]] = kOut;
-            for (int i = threadIdx.x; i < n; i += N)
-              if (bin_of(value_of<LOW>(key_in(entry[i]))) > likely_high) value[i] = kOut;
-            __syncthreads();
-          }
-        }
-        if (sorts) {
-          sort<N>(entry, value, n);
-          for (int i = threadIdx.x; i < n; i += N) value[i] = __double2ull_rn(weight(value_of<LOW>(key_in(entry[i]))) * kGrain);
-          __syncthreads();
-          const int count = cuts ? min(n, static_cast<int>(k)) : n, per = (count + N - 1) / N, begin = min(static_cast<int>(threadIdx.x) * per, count),
-                    end = min(begin + per, count);
-          ahead_of = 0;
-          for (int i = begin; i < end; ++i) ahead_of += value[i];
-          ahead_of = block_scan(s, ahead_of, total);
-          const double goal = ceil(static_cast<double>(top_p) * (cuts ? static_cast<double>(total) : whole * kGrain));
-          const unsigned long long target = nucleus ? __double2ull_rn(fmin(fmax(goal, 1.0), 9.0e18)) : ~0ull;
-          for (int i = begin; i < end; ++i) {
-            const unsigned long long v = value[i];
-            if (ahead_of >= target) value[i] = kOut;
-            ahead_of += v;
-          }
-          for (int i = count + threadIdx.x; i < n; i += N) value[i] = kOut;
-          __syncthreads();
+          goal = fmin(fmax(ceil(static_cast<double>(top_p) * goal), 1.0), 9.0e18);
+          const Range r = range_of<LOW, kBins>(m, unit, likely_low, likely_high);
+          leave_out(find_end(s, entry, value, n, first_of(r), last_of(r), __double2ull_rn(goal)));
         }
         // The draw, in the order of the places: sums by shares of the row, by shares of the share that the random number falls on, until what is
         // left is little enough to compare each with each.
         total = 0;
         for (int i = threadIdx.x; i < n; i += N) {
-          if (min_p > 0.0 && value[i] != kOut && weight(value_of<LOW>(key_in(entry[i]))) < min_p) value[i] = kOut;
+          if (min_p > 0.0 && value[i] != kOut && weight(value_of<LOW>(key_in(entry[i], bits))) < min_p) value[i] = kOut;
           if (value[i] == kOut) continue;
           ++kept;
           total += value[i];
@@ -869,8 +840,8 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
           if (threadIdx.x == 0) s.listed = 0;
           __syncthreads();
           for (int i = threadIdx.x; i < n; i += N) {
-            const int64_t at = static_cast<uint32_t>(entry[i]) - base;
-            if (value[i] != kOut && at >= 0 && at < size) atomicAdd(&s.mass[static_cast<uint32_t>(at) / part], value[i]);
+            const int64_t at = static_cast<int64_t>(place_in(entry[i], bits)) - base;
+            if (value[i] != kOut && at >= 0 && at < size) add(&s.mass[static_cast<uint32_t>(at) / part], value[i]);
           }
           __syncthreads();
           unsigned long long mass[kEach], sum = 0, none;
@@ -887,10 +858,10 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
           size = min(static_cast<int64_t>(part), size - static_cast<int64_t>(s.found[0]) * part);
           ahead = s.found_sum;
           for (int i = threadIdx.x; i < n; i += N) {
-            const int64_t at = static_cast<uint32_t>(entry[i]) - base;
+            const int64_t at = static_cast<int64_t>(place_in(entry[i], bits)) - base;
             if (value[i] == kOut || at < 0 || at >= size) continue;
             const uint32_t to_at = atomicAdd(&s.listed, 1u);
-            if (to_at < kSmall) s.order[to_at] = entry[i] << 32 | i;
+            if (to_at < kSmall) s.small_entry[to_at] = static_cast<unsigned long long>(place_in(entry[i], bits)) << 32 | i;
           }
           __syncthreads();
           if (part == 1 || s.listed <= kSmall) break;
@@ -898,14 +869,14 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         }
         const uint32_t left = min(s.listed, kSmall);     // (one place has one entry)
         if (threadIdx.x < left) {
-          const unsigned long long me = s.order[threadIdx.x];
+          const unsigned long long me = s.small_entry[threadIdx.x];
           const int i = static_cast<int>(static_cast<uint32_t>(me));
           unsigned long long upto = ahead;
           for (uint32_t j = 0; j < left; ++j)
-            if (s.order[j] < me) upto += value[static_cast<uint32_t>(s.order[j])];
+            if (s.small_entry[j] < me) upto += value[static_cast<uint32_t>(s.small_entry[j])];
           if (upto <= goal && upto + value[i] > goal) {
             p.ids[row] = static_cast<int32_t>(me >> 32);
-            if (p.logp) p.logp[row] = static_cast<float>(log(weight(value_of<LOW>(key_in(entry[i]))) * kGrain / static_cast<double>(total)));
+            if (p.logp) p.logp[row] = static_cast<float>(log(weight(value_of<LOW>(key_in(entry[i], bits))) * kGrain / static_cast<double>(total)));
             if (p.kept) p.kept[row] = static_cast<int32_t>(kept);
           }
         }
@@ -915,33 +886,27 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       __syncthreads();
     }
 
-    // All lists, sorted, to every CTA.
+    // All lists to every CTA.
     auto gather = [&]() {                    // (after a row_sync)
       const int n = collect(s, ctas, kList, true, s.order);
       row_sync(ctas);                        // (the lists are read)
       if (threadIdx.x == 0) s.listed = 0;
-      sort<N>(s.order, s.value, n);
       return n;
     };
     auto list_range = [&](const Range& r) {  // of keys; no more of them than a list holds
-      each_hit(slice, from, to, fmaxf(value_of<LOW>(r.low), k_gate), [&](float z, int i) {
+      each_hit(slice, from, to, fmaxf(value_of<LOW>(r.low), k_gate), value_of<LOW>(r.high), [&](float z, int i) {
         const uint32_t key = key_of<LOW>(z);
         if (key >= r.low && key <= r.high) list(z, i);
       });
       row_sync(ctas);
       return gather();
     };
-    // Of a sorted list the entry that is the last one kept: its key, and how many of that key are kept with it.
-    auto ends_at = [&](int at) {
-      const uint32_t key = key_in(s.order[max(at, 0)]);
-      int begin = 0, end = max(at, 0);       // the first of that key
-      while (begin < end) {
-        const int mid = (begin + end) / 2;
-        if (key_in(s.order[mid]) > key) begin = mid + 1;
-        else end = mid;
-      }
-      last_key = key;
-      last_ties = at - begin + 1;
+    // The last entry of a list that is kept: its key, and how many of that key are kept with it.
+    auto ends_at = [&](int n, unsigned long long end) {
+      uint32_t ties = 0;
+      for (int i = threadIdx.x; i < n; i += N) ties += key_in(s.order[i], bits) == key_in(end, bits) && s.order[i] <= end;
+      last_ties = block_sum(s, ties);
+      last_key = key_in(end, bits);
     };
 
     // 5. the k-th largest
@@ -949,11 +914,12 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       Range r = range_of<LOW, kBins>(m, unit, k_bin, k_bin);
       const bool few_k = k_upto - k_before <= kList;
       if (few_k) {
-        each_hit(slice, from, to, fmaxf(value_of<LOW>(r.low), k_gate), [&](float z, int i) {
+        each_hit(slice, from, to, fmaxf(value_of<LOW>(r.low), k_gate), value_of<LOW>(r.high), [&](float z, int i) {
           if (bin_of(z) == k_bin) list(z, i);
         });
         row_sync(ctas);
-        ends_at(min(static_cast<int>(k - k_before), gather()) - 1);
+        const int n = gather();
+        ends_at(n, find_end(s, s.order, nullptr, n, first_of(r), last_of(r), k - k_before));
       }
       while (!few_k) {
         const int shift = shift_of<kBins>(r);
@@ -961,7 +927,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         for (int b = threadIdx.x; b < kBins; b += N) s.count[b] = 0;
         __syncthreads();
         uint32_t over = 0;
-        each_hit(slice, from, to, fmaxf(value_of<LOW>(r.low), k_gate), [&](float z, int) {
+        each_hit(slice, from, to, fmaxf(value_of<LOW>(r.low), k_gate), INFINITY, [&](float z, int) {
           const uint32_t key = key_of<LOW>(z);
           if (key > r.high) ++over;
           else if (key >= r.low) atomicAdd(&s.count[(r.high - key) >> shift], 1u);
@@ -976,7 +942,8 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         for (int j = 0; j < kEach; ++j) sum += some[j];
         uint32_t a = over + block_scan(s, sum, inside);
         if (shift > 0 && inside <= kList) {
-          ends_at(min(static_cast<int>(k - over), list_range(r)) - 1);
+          const int n = list_range(r);
+          ends_at(n, find_end(s, s.order, nullptr, n, first_of(r), last_of(r), k - over));
           break;
         }
 #pragma unroll
@@ -1000,7 +967,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
 
     // the nucleus
     if (nucleus) {
-      Range r = range_of<LOW, kBins>(m, unit, low_bin, high_bin);
+      Range r = few ? range_of<LOW, kBins>(m, unit, likely_low, likely_high) : range_of<LOW, kBins>(m, unit, low_bin, high_bin);
       r.low = max(r.low, last_key);
       r.high = max(r.high, r.low);
       const uint32_t cut_key = last_key, cut_ties = last_ties;       // of top-k; key 0: none
@@ -1009,32 +976,27 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       const double grain = ldexp(1.0, p.fraction), back = ldexp(1.0, -p.fraction);
       double target = 0.0;
       bool cut_inside = cuts && high_bin == k_bin;
-      // A sorted list of n logits that follow others with the sum `above`, behind them what top-k leaves of its last key (where that is in reach):
-      // where the target is met.
-      auto meet = [&](int n) {
+      // A list of n logits that follow others with the sum `above`, behind them what top-k leaves of its last key (where that is in reach):
+      // where the target is met.  False: not within a list that had to hold it.
+      auto meet = [&](int n, bool sure) {
         const double goal = fmax(ceil((target - above) * kGrain), 1.0);
-        unsigned long long w[kEach], a = 0, sum;
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          const int i = threadIdx.x * kEach + j;
-          w[j] = i < n ? __double2ull_rn(weight(value_of<LOW>(key_in(s.order[i]))) * kGrain) : 0;
-          s.value[i] = w[j];
-          a += w[j];
+        unsigned long long sum = 0;
+        for (int i = threadIdx.x; i < n; i += N) {
+          s.value[i] = __double2ull_rn(weight(value_of<LOW>(key_in(s.order[i], bits))) * kGrain);
+          sum += s.value[i];
         }
-        a = block_scan(s, a, sum);
-        uint32_t passed = 0;
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          a += w[j];
-          passed += static_cast<int>(threadIdx.x * kEach + j) < n && static_cast<double>(a) < goal;
-        }
-        passed = block_sum(s, passed);
-        if (few && listed >= 0 && !(above < target && goal <= static_cast<double>(sum))) return false;
-        ends_at(min(static_cast<int>(passed), n - 1));
-        if (cut_inside && goal > static_cast<double>(sum)) {
+        block_scan(s, sum, sum);
+        if (!sure && !(above < target && goal <= static_cast<double>(sum))) return false;
+        if (sum > 0 && !(cut_inside && goal > static_cast<double>(sum))) {
+          ends_at(n, find_end(s, s.order, s.value, n, first_of(r), last_of(r), __double2ull_rn(fmin(goal, 9.0e18))));
+        } else if (cut_inside) {
           const double more = ceil((goal - static_cast<double>(sum)) / (cut_weight * kGrain));
           last_key = cut_key;
           last_ties = more >= cut_ties || !(cut_weight > 0.0) ? cut_ties : more > 1.0 ? static_cast<uint32_t>(more) : 1u;
+        } else {                             // (weights that are too small for the sums: all is kept)
+          last_key = cuts ? cut_key : 0;
+          last_ties = cuts ? cut_ties : 0xffffffffu;
+          listed = -1;
         }
         return true;
       };
@@ -1047,7 +1009,10 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         gathered(above, sum_all, none);
         target = static_cast<double>(top_p) * sum_all;
         listed = gather();
-        if (!meet(listed)) listed = -1;      // (the end lies outside the likely bins)
+        if (!meet(listed, false)) {          // (the end lies outside the likely bins)
+          listed = -1;
+          r = range_of<LOW, kBins>(m, unit, low_bin, high_bin);
+        }
       }
       if (listed < 0)
       for (bool begins = true;; begins = false) {
@@ -1066,7 +1031,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
             if (few_left ? bin_of(v[j]) < low_bin : key_of<LOW>(v[j]) > r.high) over += w;
           }
         });
-        each_hit(slice, from, to, value_of<LOW>(r.low), [&](float z, int i) {
+        each_hit(slice, from, to, value_of<LOW>(r.low), value_of<LOW>(r.high), [&](float z, int i) {
           if (!(z > cut_value)) return;      // (equal ones are added below)
           if (few_left) {
             const uint32_t bin = bin_of(z);
@@ -1076,7 +1041,8 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
           const uint32_t key = key_of<LOW>(z);
           if (key < r.low || key > r.high) return;
           ++inside;
-          atomicAdd(&s.mass[(r.high - key) >> shift], static_cast<unsigned long long>(__double2ll_rn(weight(z) * grain)));
+          if (shift == 0) atomicAdd(&s.count[r.high - key], 1u);             // (a bin is one key: its weight comes in below)
+          else add(&s.mass[(r.high - key) >> shift], static_cast<unsigned long long>(__double2ll_rn(weight(z) * grain)));
         });
         spread(over, all, inside);
         row_sync(ctas);
@@ -1084,14 +1050,22 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         gathered(above, sum_all, inside);
         if (begins) target = static_cast<double>(top_p) * (sum_all + (cuts ? cut_ties * cut_weight : 0.0));
         if (few_left) {
-          meet(gather());
+          meet(gather(), true);
           break;
         }
         unsigned long long some[kEach], sum = 0, mass;
-        sum_bins(s, s.mass, ctas, cta, some);
+        if (shift == 0) {
+          uint32_t count[kEach];
+          sum_bins(s, s.count, ctas, cta, count);
+#pragma unroll
+          for (int j = 0; j < kEach; ++j)
+            some[j] = count[j] ? count[j] * static_cast<unsigned long long>(__double2ll_rn(weight(value_of<LOW>(r.high - threadIdx.x * kEach - j)) * grain)) : 0;
+        } else {
+          sum_bins(s, s.mass, ctas, cta, some);
+        }
         cut_inside = cuts && cut_key >= r.low && cut_key <= r.high;
         if (shift > 0 && inside <= kList) {
-          meet(list_range(Range{max(r.low, cut_key + 1), r.high}));
+          meet(list_range(Range{max(r.low, cut_key + 1), r.high}), true);
           break;
         }
 #pragma unroll
@@ -1140,7 +1114,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       const int64_t begin = first + static_cast<int64_t>(from) * kV, end = first + static_cast<int64_t>(to) * kV;
       unsigned long long more = 0;           // (in whole numbers: their order says nothing)
       for (int i = lane; i < listed; i += 32) {
-        const uint32_t place = static_cast<uint32_t>(s.order[i]), key = key_in(s.order[i]);
+        const uint32_t place = place_in(s.order[i], bits), key = key_in(s.order[i], bits);
         if (place < begin || place >= end) continue;
         if (key == last_key) ++ties;
         else if (key > last_key) more += s.value[i], ++keeps;
@@ -1150,7 +1124,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       if (!holes) {
         if (lane == 0) keeps = static_cast<uint32_t>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(to) * kV, slice.entries) - static_cast<int64_t>(from) * kV));
       } else {
-        each_hit(slice, from, to, -kLargest, [&](float, int) { ++keeps; });
+        each_hit(slice, from, to, -kLargest, INFINITY, [&](float, int) { ++keeps; });
       }
     } else {
       // (a bound on logits that min-p keeps, in 32 bits: the weights decide)
@@ -1332,8 +1306,12 @@ int check(const sfb_sampler_config* c) {
 }
 
 constexpr int kHeldMost = 192 << 10;         // of a CTA's shared memory, for the row
-constexpr int kHeldFour = 40 << 10;          // ... where four CTAs of half the threads are
-constexpr int kHeldTwo = 80 << 10;           // ... where two CTAs are to share an SM
+constexpr int kHeldFour = 40 << 10;          // ... where four CTAs of half the threads are on an SM
+constexpr int kHeldTwo = 79 << 10;           // ... where two CTAs are (the rest of the row is read from L2 again)
+constexpr int kShareMost = 256 << 10;        // bytes of a row that a CTA has, at most: what is under way at a time then stays in L2
+
+// CTAs that are there at a time, two on an SM, in clusters of so many (what the driver says for 148 SMs: a cluster lies within a part of the chip).
+int slots(int ctas) { return ctas <= 2 ? 296 : ctas == 4 ? 284 : ctas == 8 ? 264 : 224; }
 
 template <typename T, int N, bool FILTERS>
 cudaError_t launch(const SampleParams& p, int64_t n, cudaStream_t s) {
@@ -1346,16 +1324,19 @@ cudaError_t launch(const SampleParams& p, int64_t n, cudaStream_t s) {
 template <typename T>
 cudaError_t launch(SampleParams p, int64_t n, cudaStream_t s) {
   const int64_t vectors = (p.classes * static_cast<int64_t>(sizeof(T)) + 15) / 16;
-  // As many CTAs a row as leave room for two of them on an SM; more where there are few rows and enough of each.
+  // More CTAs a row where all rows still are under way at once, and a CTA has enough of its row.
   int ctas = 1;
-  while (ctas < 8 && vectors * 16 > static_cast<int64_t>(kHeldTwo) * ctas) ctas *= 2;
-  while (ctas < kMaxCtas && n * ctas * 2 <= sfb::kModelSms && vectors * 16 > (8 << 10) * ctas) ctas *= 2;
+  while (ctas < 8 && vectors * 16 > static_cast<int64_t>(kShareMost) * ctas) ctas *= 2;
+  while (ctas < kMaxCtas && n * ctas * 2 <= slots(ctas * 2) && vectors * 16 > (16 << 10) * ctas) ctas *= 2;
   p.ctas = ctas;
   p.share = static_cast<int32_t>((vectors + ctas - 1) / ctas);
-  p.resident = std::min(p.share, kHeldMost / 16);
+  p.resident = std::min(p.share, (n * ctas <= 112 ? kHeldMost : kHeldTwo) / 16);
+#ifndef SMALLN
+#define SMALLN 256
+#endif
   const bool small = p.share <= kHeldFour / 16 && n * ctas > 2 * sfb::kModelSms;
-  if (p.top_k || p.top_p) return small ? launch<T, 256, true>(p, n, s) : launch<T, 512, true>(p, n, s);
-  return small ? launch<T, 256, false>(p, n, s) : launch<T, 512, false>(p, n, s);
+  if (p.top_k || p.top_p) return small ? launch<T, SMALLN, true>(p, n, s) : launch<T, 512, true>(p, n, s);
+  return small ? launch<T, SMALLN, false>(p, n, s) : launch<T, 512, false>(p, n, s);
 }
 
 }  // namespace
@@ -1408,6 +1389,7 @@ extern "C" int sfb_sample(sfb_sampler* h, int64_t n, const void* Z_dev, int64_t 
   p.kept = kept_dev;
   int bits = 0;
   while ((1ll << bits) < c.classes) ++bits;
+  p.place_bits = bits;
   p.fraction = 62 - bits;                    // the weights are 1 at most: their sum is below 2^63
   p.wide = sfb::lies_wide(Z_dev, ldz, c.dtype);
   const cudaStream_t s = static_cast<cudaStream_t>(c.stream);
