@@ -1,11 +1,13 @@
 // Samples from token ids, the gradient of that with respect to the table, and dropout (sfb_embed_*, sfb_dropout_* in sfb.h).
 //
 //   lookup, dropout   embed_rows_kernel, dropout_kernel: a thread takes groups of eight entries of the output rows
-//   gradient          dE[t] = alpha s sum_{i: id_i = t} m_i dX_i, in three launches:
-//     sort_kernel     the samples in the order of their tokens (stable: a token's samples stay in their order)
+//   gradient          dE[t] = alpha s sum_{i: id_i = t} m_i dX_i:
+//     mark_kernel     a bit for each token that some sample names (where dE is written whole)
+//     sort_kernel     the samples in the order of their tokens (stable: a token's samples stay in their order); meanwhile other SMs zero the
+//                     rows that no sample names
 //     gradient_kernel chunks of that order, whichever tokens they hold: a thread adds the samples of a chunk for a group of columns and
 //                     writes the sum where the token changes.  Work is even however often a token comes up.  A token that goes beyond
-//                     a chunk leaves a part in each.  Other blocks zero the rows that no sample names.
+//                     a chunk leaves a part in each.
 //     join_kernel     adds the parts of such tokens in their order
 // Sums are in fp32, in an order that depends on the ids alone: the same bits from call to call.
 // All are bound by HBM: the rows read once, the table's rows written once.
@@ -172,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, N == 1 ? 1 : 4) dropout_kernel(const
 // its share of the samples, a warp a run of them; the lanes of a warp that hold the same digit find one another by a ballot a bit.
 // More samples take three launches a digit (counts of tiles, their sums, the move), each tile as a CTA of the cluster does it.
 constexpr int kSortThreads = 1024, kSortWarps = 32, kSortPer = 8, kSortTile = kSortThreads * kSortPer;
-constexpr int kSortCtas = 16;          // (more than 8 are asked for: allow_clusters)
+constexpr int kSortCtas = 16;          // (more than 8: a launch that asks for them)
 constexpr int64_t kSortMost = static_cast<int64_t>(kSortThreads) * 4 * kSortCtas;
 constexpr int kMaxBits = 10, kMaxBins = 1 << kMaxBits;
 
@@ -192,8 +194,10 @@ struct SortParams {
 struct SortShared {
   uint16_t rank[kSortWarps][kMaxBins]; // of a warp: how many of a digit so far, then how many in the warps before it
   uint32_t total[kMaxBins];            // of the CTA
-  uint32_t base[kMaxBins];
+  uint32_t base[kMaxBins];             // where the CTA's of a digit begin
   uint32_t scan[kSortWarps];
+  uint32_t part[kSortThreads];         // of a share of the bins, the CTAs' totals
+  uint32_t shares[kSortCtas];          // what the CTAs' shares of the bins hold
 };
 
 // Digits of a tile that begins at `first`: key and the rank within the CTA among those of the same digit, of each of a thread's samples.
@@ -283,12 +287,18 @@ __device__ __forceinline__ void move_tile(const SortShared& s, const SortParams&
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
+__device__ __forceinline__ uint32_t in_cluster(const uint32_t* here, int cta) {
+  uint32_t there;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(here))), "r"(cta));
+  return there;
+}
 __device__ __forceinline__ uint32_t cluster_read(const uint32_t* here, int cta) {
-  uint32_t v, there;
-  const uint32_t a = static_cast<uint32_t>(__cvta_generic_to_shared(here));
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(a), "r"(cta));
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(there) : "memory");
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(in_cluster(here, cta)) : "memory");
   return v;
+}
+__device__ __forceinline__ void cluster_write(uint32_t* here, int cta, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_cluster(here, cta)), "r"(v) : "memory");
 }
 
 // Where the sorted samples and what goes with them lie; two buffers that the digits take in turn, the last one writes the first.
@@ -303,16 +313,96 @@ __device__ __forceinline__ void mark(const Order& o, uint32_t key, uint32_t toke
   if (key < tokens) atomicOr(o.touched + (key >> 5), 1u << (key & 31));
 }
 
+// Where the CTAs' samples of each digit begin, to their `base`.  A CTA takes a share of the bins: the totals of all CTAs there, added up over CTAs
+// and bins; what lies in the shares before it comes to every CTA as one number.
+__device__ __forceinline__ void place_digits(SortShared& s, int bits, int ctas, int cta) {
+  const int bins = 1 << bits, t = threadIdx.x;
+  cluster_sync();                      // every CTA's totals are there
+  if (ctas == 1) {
+    const uint32_t base = scan_bins(s, t < bins ? s.total[t] : 0);
+    if (t < bins) s.base[t] = base;
+    __syncthreads();
+    return;
+  }
+  const int share = bins < ctas ? 1 : bins / ctas, first = cta * share, at = t % share, from = t / share;        // bins * ctas threads at most: one each
+  const bool mine = from < ctas && first < bins;
+  s.part[t] = mine ? cluster_read(&s.total[first + at], from) : 0;
+  __syncthreads();
+  uint32_t before = 0, all = 0;        // of this bin: in the CTAs before `from`, in all
+  if (mine) {
+    for (int c = 0; c < ctas; ++c) {
+      const uint32_t v = s.part[c * share + at];
+      all += v;
+      if (c < from) before += v;
+    }
+  }
+  __syncthreads();
+  // the share's bins in turn: the threads of the first CTA hold their totals
+  const uint32_t ahead = scan_bins(s, t < share && mine ? all : 0);
+  if (t < share) s.part[t] = ahead;
+  __syncthreads();
+  if (mine) cluster_write(&s.base[first + at], from, s.part[at] + before);
+  uint32_t whole = 0;
+  if (t < kSortWarps) whole = __reduce_add_sync(0xffffffffu, s.scan[t]);
+  if (t < ctas) cluster_write(&s.shares[cta], t, first < bins ? whole : 0);
+  cluster_sync();
+  if (t < bins) {
+    uint32_t v = s.base[t];
+    for (int c = 0; c < t / share; ++c) v += s.shares[c];
+    s.base[t] = v;
+  }
+  __syncthreads();
+}
+
+// Rows of dE that no sample names.
+struct ZeroParams {
+  const uint32_t* touched;
+  float* table;
+  int64_t ldt, tokens, dim;
+  bool wide;
+};
+// Rows that start on 16-byte boundaries by copies of zeros from shared memory, a row a thread; what lies behind the last 16 bytes, and
+// other rows, by stores.  `zeros`: kZeroBytes of shared memory.
+constexpr int kZeroBytes = 4096;
+template <int THREADS>
+__device__ __forceinline__ void zero_rows(const ZeroParams& p, uint4* zeros, int64_t block, int64_t blocks) {
+  for (int i = threadIdx.x; i < kZeroBytes / 16; i += THREADS) zeros[i] = make_uint4(0, 0, 0, 0);
+  sfb::ptx::fence_proxy_async_smem();
+  __syncthreads();
+  auto untouched = [&](int64_t row) { return !(p.touched[row >> 5] >> (row & 31) & 1); };
+  if (p.wide) {
+    const int64_t bytes = p.dim / 4 * 16;
+    for (int64_t row = static_cast<int64_t>(threadIdx.x) * blocks + block; row < p.tokens; row += blocks * THREADS) {
+      if (!untouched(row)) continue;
+      float* to = p.table + row * p.ldt;
+      for (int64_t at = 0; at < bytes; at += kZeroBytes)
+        sfb::ptx::bulk_store(reinterpret_cast<char*>(to) + at, zeros, static_cast<uint32_t>(min(static_cast<int64_t>(kZeroBytes), bytes - at)));
+      for (int64_t col = p.dim / 4 * 4; col < p.dim; ++col) to[col] = 0.f;
+    }
+    sfb::ptx::tma_commit_group();
+    sfb::ptx::tma_wait_group<0>();     // (the copies read this block's shared memory)
+    return;
+  }
+  const int lane = threadIdx.x & 31, warps = THREADS / 32;
+  for (int64_t row = block * warps + (threadIdx.x >> 5); row < p.tokens; row += blocks * warps)
+    if (untouched(row))
+      for (int64_t col = lane; col < p.dim; col += 32) p.table[row * p.ldt + col] = 0.f;
+}
+
+// The first cluster sorts, the others zero.
 template <int PER>
-__global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(SortParams p, const __grid_constant__ Order o, int digits, int ctas) {
-  extern __shared__ __align__(16) unsigned char shared[];
+__global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(SortParams p, const __grid_constant__ Order o, const __grid_constant__ ZeroParams zero, int digits, int ctas) {
+  extern __shared__ __align__(128) unsigned char shared[];
   SortShared& s = *reinterpret_cast<SortShared*>(shared);
   pdl_launch_dependents();
   pdl_wait();
   const int cta = blockIdx.x;
+  if (cta >= ctas) {
+    zero_rows<kSortThreads>(zero, reinterpret_cast<uint4*>(shared), cta - ctas, gridDim.x - ctas);
+    return;
+  }
   const int64_t first = static_cast<int64_t>(cta) * (kSortThreads * PER);
   if (cta == 0 && threadIdx.x == 0) o.crossing[0] = 0;
-  for (int64_t i = static_cast<int64_t>(cta) * kSortThreads + threadIdx.x; i < o.words; i += static_cast<int64_t>(ctas) * kSortThreads) o.touched[i] = 0;
   uint2 e[PER];
   uint16_t rank[PER];
   for (int d = 0; d < digits; ++d) {
@@ -320,28 +410,32 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(SortParams p, con
     p.out = o.entries[to];
     p.shift = d * p.bits;
     rank_tile<PER>(s, p, first, e, rank);
-    cluster_sync();                    // every CTA's totals are there (and, the first time, the bits are clear)
-    uint32_t all = 0, before = 0;
-    if (threadIdx.x < (1 << p.bits)) {
-      for (int c = 0; c < ctas; ++c) {
-        const uint32_t v = c == cta ? s.total[threadIdx.x] : cluster_read(&s.total[threadIdx.x], c);
-        all += v;
-        if (c < cta) before += v;
-      }
-    }
-    const uint32_t base = scan_bins(s, all) + before;
-    if (threadIdx.x < (1 << p.bits)) s.base[threadIdx.x] = base;
-    __syncthreads();
+    place_digits(s, p.bits, ctas, cta);
     move_tile<PER>(s, p, first, e, rank);
-    if (d == 0 && o.words) {
-#pragma unroll
-      for (int j = 0; j < PER; ++j)
-        if (first + (threadIdx.x >> 5) * (32 * PER) + j * 32 + (threadIdx.x & 31) < p.n) mark(o, e[j].x, p.tokens);
-    }
-    cluster_sync();                    // the order is written, the totals are read
+    cluster_sync();                    // the order is written, the places are read
     p.ids = nullptr;
     p.in = o.entries[to];
   }
+}
+
+// A bit for each token that some sample names: one cluster, which clears them all first.
+__global__ void __launch_bounds__(1024) mark_kernel(const int32_t* ids, int64_t n, uint32_t tokens, uint32_t* touched, int64_t words) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * 1024 + threadIdx.x, step = static_cast<int64_t>(gridDim.x) * 1024;
+  for (int64_t i = at; i < words; i += step) touched[i] = 0;
+  cluster_sync();
+  for (int64_t i = at; i < n; i += step) {
+    const uint32_t id = static_cast<uint32_t>(ids[i]);
+    if (id < tokens) atomicOr(touched + (id >> 5), 1u << (id & 31));
+  }
+}
+
+__global__ void __launch_bounds__(256) zero_kernel(const __grid_constant__ ZeroParams p) {
+  __shared__ __align__(128) uint4 zeros[kZeroBytes / 16];
+  pdl_launch_dependents();
+  pdl_wait();
+  zero_rows<256>(p, zeros, blockIdx.x, gridDim.x);
 }
 
 // The same for more samples, a launch each.
@@ -354,7 +448,7 @@ __global__ void __launch_bounds__(256) sort_clear_kernel(const __grid_constant__
 }
 
 __global__ void __launch_bounds__(kSortThreads, 1) sort_count_kernel(const __grid_constant__ SortParams p, const __grid_constant__ Order o) {
-  extern __shared__ __align__(16) unsigned char shared[];
+  extern __shared__ __align__(128) unsigned char shared[];
   SortShared& s = *reinterpret_cast<SortShared*>(shared);
   pdl_launch_dependents();
   pdl_wait();
@@ -393,7 +487,7 @@ __global__ void __launch_bounds__(256) sort_sum_kernel(const __grid_constant__ S
 }
 
 __global__ void __launch_bounds__(kSortThreads, 1) sort_move_kernel(const __grid_constant__ SortParams p) {
-  extern __shared__ __align__(16) unsigned char shared[];
+  extern __shared__ __align__(128) unsigned char shared[];
   SortShared& s = *reinterpret_cast<SortShared*>(shared);
   pdl_launch_dependents();
   pdl_wait();
@@ -411,13 +505,12 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_move_kernel(const __grid
 // ---- the gradient ------------------------------------------------------------------------------------------------------------------
 struct GradientParams {
   const uint2* order;                  // (key, sample)
-  const uint32_t* touched;
   uint32_t* crossing;
   float* parts;                        // [2 chunks][groups][8]: what a chunk's first token has of an earlier one's, and its last one's
                                        // beginning
   int64_t n;
   int32_t per;                         // samples a chunk
-  uint32_t chunks, zero;               // zero: the first blocks, which zero; the others add
+  uint32_t chunks;
   uint32_t tokens;
   Divisor groups;
   const void* dx;
@@ -430,45 +523,13 @@ struct GradientParams {
   DropParams drop;
 };
 
-// Rows that start on 16-byte boundaries by copies of zeros from shared memory, a row a thread; what lies behind the last 16 bytes, and
-// other rows, by stores.
-constexpr int kZeroBytes = 4096;
-__device__ __forceinline__ void zero_rows(const GradientParams& p) {
-  __shared__ __align__(128) uint4 zeros[kZeroBytes / 16];
-  for (int i = threadIdx.x; i < kZeroBytes / 16; i += kThreads) zeros[i] = make_uint4(0, 0, 0, 0);
-  sfb::ptx::fence_proxy_async_smem();
-  __syncthreads();
-  auto untouched = [&](int64_t row) { return !(p.touched[row >> 5] >> (row & 31) & 1); };
-  if (p.wide_out) {
-    const int64_t bytes = p.dim / 4 * 16;
-    for (int64_t row = static_cast<int64_t>(threadIdx.x) * p.zero + blockIdx.x; row < p.tokens; row += static_cast<int64_t>(p.zero) * kThreads) {
-      if (!untouched(row)) continue;
-      float* to = p.table + row * p.lddt;
-      for (int64_t at = 0; at < bytes; at += kZeroBytes)
-        sfb::ptx::bulk_store(reinterpret_cast<char*>(to) + at, zeros, static_cast<uint32_t>(min(static_cast<int64_t>(kZeroBytes), bytes - at)));
-      for (int64_t col = p.dim / 4 * 4; col < p.dim; ++col) to[col] = 0.f;
-    }
-    sfb::ptx::tma_commit_group();
-    sfb::ptx::tma_wait_group<0>();     // (the copies read this block's shared memory)
-    return;
-  }
-  const int lane = threadIdx.x & 31, warps = kThreads / 32;
-  for (int64_t row = static_cast<int64_t>(blockIdx.x) * warps + (threadIdx.x >> 5); row < p.tokens; row += static_cast<int64_t>(p.zero) * warps)
-    if (untouched(row))
-      for (int64_t col = lane; col < p.dim; col += 32) p.table[row * p.lddt + col] = 0.f;
-}
-
 constexpr int kAhead = 2;          // samples under way a thread
 
 template <typename T, bool DROP, bool ADD>
 __global__ void __launch_bounds__(kThreads, 4) gradient_kernel(const __grid_constant__ GradientParams p) {
   pdl_launch_dependents();
   pdl_wait();
-  if (blockIdx.x < p.zero) {           // rows that no sample names
-    zero_rows(p);
-    return;
-  }
-  const uint32_t place = (blockIdx.x - p.zero) * kThreads + threadIdx.x, chunk = p.chunks - 1 - p.groups(place), group = place - p.groups(place) * p.groups.d;
+  const uint32_t place = blockIdx.x * kThreads + threadIdx.x, chunk = p.chunks - 1 - p.groups(place), group = place - p.groups(place) * p.groups.d;
   Generator generator;
   if constexpr (DROP) generator.begin(p.drop);
   if (chunk >= p.chunks) return;
@@ -552,12 +613,13 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Gradi
     int64_t more = 0;
     for (int got = 256; got == 256; more += got) {
       const int64_t at = (static_cast<int64_t>(chunk) + 1 + more + threadIdx.x) * p.per;
-      got = __syncthreads_count(at < p.n && p.order[at].x == key);
+      const uint32_t there = at < p.n ? p.order[at].x : p.tokens;
+      got = __syncthreads_count(there == key);
     }
     const int64_t each = (more + 1 + 7) / 8, from = share * each, to = min(more + 1, from + each);
     float sum[kGroup] = {};
     if (group < p.groups.d) {
-#pragma unroll 4
+#pragma unroll 8
       for (int64_t k = from; k < to; ++k) {
         const int64_t slot = k == 0 ? 2 * static_cast<int64_t>(chunk) + 1 : 2 * (chunk + k);
         Raw<float> r;
@@ -711,13 +773,13 @@ cudaError_t launch_dropout(const DropoutParams& p, cudaStream_t s) {
 }
 
 template <int PER>
-cudaError_t launch_sort(const SortParams& p, const Order& o, int digits, int ctas, cudaStream_t s) {
+cudaError_t launch_sort(const SortParams& p, const Order& o, const ZeroParams& zero, int digits, int ctas, int zeros, cudaStream_t s) {
   cudaError_t e = sfb::allow_smem<sort_kernel<PER>>(sizeof(SortShared));
   if (e == cudaSuccess) e = sfb::allow_clusters<sort_kernel<PER>>();
-  return e == cudaSuccess ? sfb::launch_kernel(sort_kernel<PER>, dim3(ctas), dim3(kSortThreads), sizeof(SortShared), s, ctas, p, o, digits, ctas) : e;
+  return e == cudaSuccess ? sfb::launch_kernel(sort_kernel<PER>, dim3(ctas + zeros), dim3(kSortThreads), sizeof(SortShared), s, ctas, p, o, zero, digits, ctas) : e;
 }
 
-cudaError_t sort_samples(const EmbedLayout& l, char* ws, const sfb_embed_config& c, int64_t n, const int32_t* ids, const Order& o) {
+cudaError_t sort_samples(const EmbedLayout& l, char* ws, const sfb_embed_config& c, int64_t n, const int32_t* ids, const Order& o, const ZeroParams& zero) {
   int bits = 1;
   while ((1ll << bits) <= c.tokens) ++bits;            // of the keys 0 .. tokens
   const int digits = (bits + kMaxBits - 1) / kMaxBits;
@@ -732,9 +794,16 @@ cudaError_t sort_samples(const EmbedLayout& l, char* ws, const sfb_embed_config&
     const int per = n <= kSortThreads * kSortCtas ? 1 : n <= 2 * kSortThreads * kSortCtas ? 2 : 4;
     int ctas = 1;
     while (static_cast<int64_t>(ctas) * kSortThreads * per < n) ctas *= 2;
-    if (per == 1) return launch_sort<1>(p, o, digits, ctas, s);
-    if (per == 2) return launch_sort<2>(p, o, digits, ctas, s);
-    return launch_sort<4>(p, o, digits, ctas, s);
+    int zeros = 0;                     // CTAs that zero, in clusters like the one that sorts: as many as the chip has room for beside it
+    if (o.words > 0) {
+      const cudaError_t e = sfb::launch_kernel(mark_kernel, dim3(8), dim3(1024), 0, s, 8, ids, n, p.tokens, o.touched, o.words);
+      if (e != cudaSuccess) return e;
+      zeros = static_cast<int>(std::min<int64_t>(112 - ctas, (c.tokens + 31) / 32));
+      zeros = std::max(1, zeros / ctas) * ctas;
+    }
+    if (per == 1) return launch_sort<1>(p, o, zero, digits, ctas, zeros, s);
+    if (per == 2) return launch_sort<2>(p, o, zero, digits, ctas, zeros, s);
+    return launch_sort<4>(p, o, zero, digits, ctas, zeros, s);
   }
   p.tiles = (n + kSortTile - 1) / kSortTile;
   p.counts = reinterpret_cast<uint32_t*>(ws + l.counts);
@@ -753,6 +822,8 @@ cudaError_t sort_samples(const EmbedLayout& l, char* ws, const sfb_embed_config&
     p.ids = nullptr;
     p.in = p.out;
   }
+  if (e == cudaSuccess && o.words > 0)
+    e = sfb::launch_kernel(zero_kernel, dim3(static_cast<unsigned>(std::min<int64_t>((c.tokens + 31) / 32, sfb::sm_count()))), dim3(256), 0, s, 1, zero);
   return e;
 }
 
@@ -895,6 +966,8 @@ extern "C" int sfb_embed_backward(sfb_embed* h, int64_t n, const int32_t* ids_de
   if (n > 0 && lddx < c.dim) return SFB_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(ids_dev) & 3u) || !sfb::lies_aligned(dX_dev, c.out_dtype) || !sfb::lies_aligned(dE_dev, SFB_F32)) return SFB_ERR_ALIGN;
   if (n == 0 && add) return SFB_OK;
+  // (groups of chunks are numbered in 31 bits: a million tokens' samples of 16 million columns)
+  if ((n + 63) / 64 * groups_of(c.dim) > kBlocksMost - kThreads) return SFB_ERR_SHAPE;
   const OnDevice on(h->device);
   if (on.err != cudaSuccess) return fail(h, on.err);
   const EmbedLayout l = layout_of(c);
@@ -905,22 +978,18 @@ extern "C" int sfb_embed_backward(sfb_embed* h, int64_t n, const int32_t* ids_de
   o.crossing = reinterpret_cast<uint32_t*>(h->ws + l.crossing);
   o.words = add ? 0 : l.words;
   const cudaStream_t s = static_cast<cudaStream_t>(c.stream);
-  cudaError_t e = n > 0 ? sort_samples(l, h->ws, c, n, ids_dev, o)
-                        : sfb::launch_kernel(sort_clear_kernel, dim3(static_cast<unsigned>(std::max<int64_t>(1, (o.words + 255) / 256))), dim3(256), 0, s, 1, o);
+  const ZeroParams zero{o.touched, dE_dev, ldde, c.tokens, c.dim, sfb::lies_wide(dE_dev, ldde, SFB_F32)};
+  cudaError_t e = sort_samples(l, h->ws, c, n, ids_dev, o, zero);
   if (e != cudaSuccess) return fail(h, e);
+  if (n == 0) return SFB_OK;
   GradientParams p{};
   p.order = o.entries[0];
-  p.touched = o.touched;
   p.crossing = o.crossing;
   p.parts = reinterpret_cast<float*>(h->ws + l.parts);
   p.n = n;
   p.groups = Divisor(static_cast<uint32_t>(groups_of(c.dim)));
   p.per = samples_per_chunk(n, p.groups.d);
   p.chunks = static_cast<uint32_t>((n + p.per - 1) / p.per);
-  const int64_t work = (static_cast<int64_t>(p.chunks) * p.groups.d + kThreads - 1) / kThreads;
-  const int64_t zero = add ? 0 : std::min<int64_t>((c.tokens + 31) / 32, sfb::sm_count());
-  if (work * kThreads > kBlocksMost || work + zero > kBlocksMost) return SFB_ERR_SHAPE;
-  p.zero = static_cast<uint32_t>(zero);
   p.tokens = static_cast<uint32_t>(c.tokens);
   p.dx = dX_dev;
   p.lddx = lddx;
@@ -935,7 +1004,7 @@ extern "C" int sfb_embed_backward(sfb_embed* h, int64_t n, const int32_t* ids_de
     p.drop = drop->drop;
     p.drop.call = call;
   }
-  const unsigned blocks = static_cast<unsigned>(work + zero);
+  const unsigned blocks = static_cast<unsigned>((static_cast<int64_t>(p.chunks) * p.groups.d + kThreads - 1) / kThreads);
   e = c.out_dtype == SFB_F32 ? launch_gradient<float>(p, drops, blocks, s)
       : c.out_dtype == SFB_BF16 ? launch_gradient<__nv_bfloat16>(p, drops, blocks, s) : launch_gradient<__half>(p, drops, blocks, s);
   // (a single chunk has nothing that goes beyond it)

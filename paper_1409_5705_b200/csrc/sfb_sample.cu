@@ -1026,24 +1026,28 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         each_vector(slice, from, to, begins && cuts ? cut_value : value_of<LOW>(r.low), [&](const float (&v)[kV]) {
 #pragma unroll
           for (int j = 0; j < kV; ++j) {
-            const double w = v[j] > cut_value ? weight(v[j]) : 0.0;
+            const bool there = v[j] > cut_value;                             // (equal ones are added below)
+            const double w = there ? weight(v[j]) : 0.0;
             if (begins && cuts) all += w;
-            if (few_left ? bin_of(v[j]) < low_bin : key_of<LOW>(v[j]) > r.high) over += w;
+            if (few_left) {
+              if (bin_of(v[j]) < low_bin) over += w;
+              continue;
+            }
+            const uint32_t key = key_of<LOW>(v[j]);
+            if (key > r.high) {
+              over += w;
+            } else if (there && key >= r.low) {
+              ++inside;
+              if (shift == 0) atomicAdd(&s.count[r.high - key], 1u);         // (a bin is one key: its weight comes in below)
+              else add(&s.mass[(r.high - key) >> shift], static_cast<unsigned long long>(__double2ll_rn(w * grain)));
+            }
           }
         });
-        each_hit(slice, from, to, value_of<LOW>(r.low), value_of<LOW>(r.high), [&](float z, int i) {
-          if (!(z > cut_value)) return;      // (equal ones are added below)
-          if (few_left) {
+        if (few_left)
+          each_hit(slice, from, to, value_of<LOW>(r.low), value_of<LOW>(r.high), [&](float z, int i) {
             const uint32_t bin = bin_of(z);
-            if (bin >= low_bin && bin <= high_bin) list(z, i);
-            return;
-          }
-          const uint32_t key = key_of<LOW>(z);
-          if (key < r.low || key > r.high) return;
-          ++inside;
-          if (shift == 0) atomicAdd(&s.count[r.high - key], 1u);             // (a bin is one key: its weight comes in below)
-          else add(&s.mass[(r.high - key) >> shift], static_cast<unsigned long long>(__double2ll_rn(weight(z) * grain)));
-        });
+            if (z > cut_value && bin >= low_bin && bin <= high_bin) list(z, i);
+          });
         spread(over, all, inside);
         row_sync(ctas);
         double sum_all;
@@ -1308,7 +1312,7 @@ int check(const sfb_sampler_config* c) {
 constexpr int kHeldMost = 192 << 10;         // of a CTA's shared memory, for the row
 constexpr int kHeldFour = 40 << 10;          // ... where four CTAs of half the threads are on an SM
 constexpr int kHeldTwo = 79 << 10;           // ... where two CTAs are (the rest of the row is read from L2 again)
-constexpr int kShareMost = 256 << 10;        // bytes of a row that a CTA has, at most: what is under way at a time then stays in L2
+constexpr int kShareMost = 128 << 10;        // bytes of a row that a CTA has, at most: what is under way at a time then stays in L2
 
 // CTAs that are there at a time, two on an SM, in clusters of so many (what the driver says for 148 SMs: a cluster lies within a part of the chip).
 int slots(int ctas) { return ctas <= 2 ? 296 : ctas == 4 ? 284 : ctas == 8 ? 264 : 224; }
