@@ -185,25 +185,48 @@ __device__ __forceinline__ void row_sync(int ctas) {
 }
 
 // ---- weights -------------------------------------------------------------------------------------------------------------------------
+// 2^(j / kTable), by the exponential series.
+struct Powers { double of[kTable]; };
+constexpr Powers powers() {
+  Powers p{};
+  for (int j = 0; j < kTable; ++j) {
+    long double x = 0.693147180559945309417232121458L * j / kTable, term = 1.0L, sum = 1.0L;
+    for (int i = 1; i < 24; ++i) sum += term *= x / i;
+    p.of[j] = static_cast<double>(sum);
+  }
+  return p;
+}
+__device__ const Powers kPowers = powers();
+
 // exp((z - m) / T), 0 for z below `far`.  Where m is infinite: 1 for such logits (m, per are 0 here and far is infinite).
 struct Weight {
   const double* power;
   double m, per;                             // 256 log2(e) / T
   float far;
-  __device__ __forceinline__ double operator()(float z) const {
+  // For finite z from `far` to m: two factors of it.
+  __device__ __forceinline__ void factors(float z, double& s, double& e) const {
     // (z - m) per = k + f, |f| <= 1/2: the sum with 1.5 * 2^52 leaves k in the low bits
-    const double d = static_cast<double>(fminf(fmaxf(z, far), kLargest)) - m;
+    const double d = static_cast<double>(z) - m;
     const double shifted = fma(d, per, 6755399441055744.0);
     const int k = __double2loint(shifted);
     const double f = fma(d, per, 6755399441055744.0 - shifted);
     // 2^(f / 256): (ln 2 / 256)^j / j!
     constexpr double c1 = 0.6931471805599453 / kTable, c2 = c1 * c1 / 2, c3 = c2 * c1 / 3;
-    const double e = fma(fma(fma(c3, f, c2), f, c1), f, 1.0);
+    e = fma(fma(fma(c3, f, c2), f, c1), f, 1.0);
     const double t = power[k & (kTable - 1)];
-    const double s = __hiloint2double(__double2hiint(t) + ((k >> 8) << 20), __double2loint(t));
+    s = __hiloint2double(__double2hiint(t) + ((k >> 8) << 20), __double2loint(t));
+  }
+  __device__ __forceinline__ double operator()(float z) const {
+    double s, e;
+    factors(fminf(fmaxf(z, far), kLargest), s, e);
     return z >= far ? s * e : 0.0;
   }
 };
+
+__device__ __forceinline__ Weight weight_of(const double* power, float m, float temperature, double per) {
+  return isinf(m) ? Weight{power, 0.0, 0.0, m} : Weight{power, m, per, fmaxf(m - kFar * temperature, -kLargest)};
+}
+__device__ __forceinline__ double per_of(float temperature) { return 369.3299304757463 / temperature; }        // 256 log2(e)
 
 template <typename V>
 __device__ __forceinline__ V shuffle_up(V v, int o) { return __shfl_up_sync(0xffffffffu, v, o); }
@@ -278,6 +301,16 @@ struct Slice {
     for (int j = 0; j < kV; ++j) v[j] = sfb::to_float(e[j]);
   }
 };
+
+// A vector of one value.
+template <typename T>
+__device__ __forceinline__ uint4 filled(float v) {
+  uint4 w;
+  T* e = reinterpret_cast<T*>(&w);
+#pragma unroll
+  for (int j = 0; j < Slice<T>::kV; ++j) e[j] = sfb::from_float<T>(v);
+  return w;
+}
 
 // Calls f(z, place in the share) for the logits of a warp's vectors from `gate` to `top`, one after another.
 template <typename T, typename F>
@@ -481,7 +514,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
   __shared__ Shared<N, FILTERS> s;
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int i = threadIdx.x; i < kTable; i += N) s.power[i] = exp2(i / static_cast<double>(kTable));
+  for (int i = threadIdx.x; i < kTable; i += N) s.power[i] = kPowers.of[i];
   if (threadIdx.x == 0) s.listed = 0, s.first = 0xffffffffu;
   const int ctas = p.ctas, bits = p.place_bits;
   if (ctas > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
@@ -592,8 +625,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
     return;
   }
   const bool endless = isinf(m);
-  const Weight weight{s.power, endless ? 0.0 : m, endless ? 0.0 : 369.3299304757463 / temperature,             // 256 log2(e)
-                      endless ? m : fmaxf(m - kFar * temperature, -kLargest)};
+  const Weight weight = weight_of(s.power, m, temperature, per_of(temperature));
   const double u = fmax(0.0, static_cast<double>(p.u[row]));
   const bool nucleus = top_p < 1.f;
 
@@ -1293,6 +1325,243 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
   }
 }
 
+// Many rows without top-k and top-p: a CTA a row, whose warps go over their shares of it once, from global memory, with sums relative to the
+// largest logit that each has seen (when a larger one comes up, what it has is rescaled).  Sums and largest logits of the warps say which one the
+// random number falls on, and that warp goes over its share again.  Rows with min-p, which needs the largest logit first, are gone over twice.
+template <typename T, int N>
+__global__ void __launch_bounds__(N, 1024 / N) sample_plain_kernel(const __grid_constant__ SampleParams p) {
+  constexpr int kV = Slice<T>::kV, kWarps = N / 32, kAhead = 4;
+  __shared__ double power[kTable], sum_of[kWarps], upto_of[kWarps], total_of;
+  __shared__ float most_of[kWarps];
+  __shared__ uint32_t keeps_of[kWarps];
+  __shared__ int winner_of;
+  pdl_launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int i = threadIdx.x; i < kTable; i += N) power[i] = kPowers.of[i];
+  pdl_wait();
+  const int64_t row = blockIdx.x;
+  Slice<T> slice;
+  slice.z = static_cast<const T*>(p.z) + row * p.ldz;
+  slice.held = nullptr;
+  slice.entries = p.classes;
+  slice.vectors = p.share;
+  slice.resident = 0;
+  slice.wide = p.wide;
+  const int per_warp = (p.share + kWarps - 1) / kWarps, from = min(warp * per_warp, p.share), to = min(from + per_warp, p.share);
+  const float temperature = p.temperature ? p.temperature[row] : 1.f;
+  const double min_p = p.min_p ? fmin(1.0, fmax(0.0, static_cast<double>(p.min_p[row]))) : 0.0;
+  const bool draws = temperature > 0.f;
+  __syncthreads();                           // the table is there
+
+  float most = kNone;                        // of the warp
+  double sum[2] = {0.0, 0.0};
+  bool holes = false;
+  const double per = draws ? per_of(temperature) : 0.0;
+  Weight weight{power, 0.0, 0.0, 0.f};
+  for (int i0 = from; i0 < to; i0 += kAhead * 32) {
+    uint4 w[kAhead];
+    uint32_t ragged = 0;
+    typename Type<T>::Pair high = Type<T>::all(kNone), low = Type<T>::all(INFINITY);
+    if (slice.wide && i0 + kAhead * 32 <= to && static_cast<int64_t>(i0 + kAhead * 32) * kV <= slice.entries) {
+      const uint4* z = reinterpret_cast<const uint4*>(slice.z) + i0 + lane;
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) w[q] = __ldg(z + q * 32);
+    } else {
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        const int i = i0 + q * 32 + lane;
+        w[q] = i < to ? slice.fetch(i) : filled<T>(kNone);
+        if (i < to && static_cast<int64_t>(i + 1) * kV <= slice.entries) continue;
+        // (what lies behind the row's end, or the warp's, is no hole)
+        if (i < to) {
+          float v[kV];
+          Slice<T>::widen(w[q], v);
+          for (int j = 0; static_cast<int64_t>(i) * kV + j < slice.entries; ++j) holes |= !(v[j] > kNone);
+        }
+        ragged |= 1u << q;
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) {
+      high = Type<T>::larger(high, Type<T>::most(w[q]));
+      if (!(ragged >> q & 1)) low = Type<T>::least(w[q], low);
+    }
+    holes |= !(Type<T>::smallest(low) > kNone);
+    const float here = fmaxf(Type<T>::largest(high), kNone) + 0.f;
+    if (__any_sync(0xffffffffu, here > most)) {
+      float larger = here;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) larger = fmaxf(larger, __shfl_xor_sync(0xffffffffu, larger, o));
+      if (draws) {
+        weight = weight_of(power, larger, temperature, per);
+        const double by = most > kNone ? weight(most) : 0.0;
+        sum[0] *= by;
+        sum[1] *= by;
+      }
+      most = larger;
+    }
+    if (!draws || min_p > 0.0 || most == kNone) continue;
+    if (isinf(most)) {
+      for (int q = 0; q < kAhead; ++q) {
+        float v[kV];
+        Slice<T>::widen(w[q], v);
+        for (int j = 0; j < kV; ++j) sum[0] += v[j] == most ? 1.0 : 0.0;
+      }
+      continue;
+    }
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) {
+      float v[kV];
+      Slice<T>::widen(w[q], v);
+#pragma unroll
+      for (int j = 0; j < kV; ++j) {
+        double s, e;
+        weight.factors(fmaxf(v[j], weight.far), s, e);
+        if (v[j] >= weight.far) sum[j & 1] = fma(s, e, sum[j & 1]);
+      }
+    }
+  }
+  const bool some_holes = __any_sync(0xffffffffu, holes);
+  if (lane == 0) most_of[warp] = most;
+  __syncthreads();
+  float m = most_of[0];
+#pragma unroll
+  for (int w = 1; w < kWarps; ++w) m = fmaxf(m, most_of[w]);
+  if (m == kNone || !draws) {                // nothing to draw from, or nothing to draw: the first place of m
+    int at = 0x7fffffff;
+    if (m != kNone && most == m) each_hit(slice, from, to, m, INFINITY, [&](float, int i) { at = min(at, i); });
+    at = __reduce_min_sync(0xffffffffu, at);
+    if (lane == 0) keeps_of[warp] = at;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int w = 1; w < kWarps; ++w) at = min(at, static_cast<int>(keeps_of[w]));
+      p.ids[row] = m == kNone ? -1 : at;
+      if (p.logp) p.logp[row] = m == kNone ? kNone : 0.f;
+      if (p.kept) p.kept[row] = m == kNone ? 0 : 1;
+    }
+    return;
+  }
+  // what the warp has, relative to the row's largest logit
+  const Weight row_weight = weight_of(power, m, temperature, per);
+  double mine, scale = 1.0;
+  uint32_t keeps = 0;
+  if (min_p > 0.0) {
+    weight = row_weight;
+    mine = 0.0;
+    each_vector(slice, from, to, -kLargest, [&](const float (&v)[kV]) {
+#pragma unroll
+      for (int j = 0; j < kV; ++j) {
+        const double w = weight(v[j]);
+        const bool keep = v[j] > kNone && w >= min_p;
+        if (keep) mine += w;
+        keeps += keep;
+      }
+    });
+    mine = warp_sum(mine);
+  } else {
+    scale = most > kNone ? row_weight(most) : 0.0;
+    mine = warp_sum(sum[0] + sum[1]) * scale;
+    if (some_holes) each_hit(slice, from, to, -kLargest, INFINITY, [&](float, int) { ++keeps; });
+    else if (lane == 0) keeps = static_cast<uint32_t>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(to) * kV, p.classes) - static_cast<int64_t>(from) * kV));
+  }
+  keeps = warp_sum(keeps);
+  if (lane == 0) sum_of[warp] = mine, keeps_of[warp] = keeps;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const double u = fmax(0.0, static_cast<double>(p.u[row]));
+    double total = 0.0;
+    uint32_t kept = 0;
+    for (int w = 0; w < kWarps; ++w) upto_of[w] = total, total += sum_of[w], kept += keeps_of[w];
+    const double target = u < 1.0 ? u * total : INFINITY;
+    int found = -1, last = 0;
+    for (int w = 0; w < kWarps; ++w) {
+      if (!(sum_of[w] > 0.0)) continue;
+      last = w;
+      if (found < 0 && upto_of[w] + sum_of[w] > target) found = w;
+    }
+    winner_of = found >= 0 ? found : last;
+    total_of = total;
+    if (p.kept) p.kept[row] = static_cast<int32_t>(kept);
+  }
+  __syncthreads();
+  // over that share again, relative to its own largest logit as before: each warp a part of it, then the one that the random number falls on
+  const int winner = winner_of, share_from = min(winner * per_warp, p.share), share_to = min(share_from + per_warp, p.share);
+  const double u = fmax(0.0, static_cast<double>(p.u[row])), total = total_of, target = u < 1.0 ? u * total : INFINITY;
+  if (!(min_p > 0.0)) {
+    weight = weight_of(power, most_of[winner], temperature, per);
+    scale = row_weight(most_of[winner]);
+  }
+  const int per_part = ((share_to - share_from + kWarps - 1) / kWarps + 31) / 32 * 32, part_from = min(share_from + warp * per_part, share_to),
+            part_to = min(part_from + per_part, share_to);
+  double part = 0.0;
+  for (int i = part_from + lane; i < part_to; i += 32) {
+    float v[kV];
+    Slice<T>::widen(slice.fetch(i), v);
+#pragma unroll
+    for (int j = 0; j < kV; ++j) {
+      const double w = v[j] > kNone ? weight(v[j]) : 0.0;
+      if (w >= min_p) part += w;
+    }
+  }
+  part = warp_sum(part) * scale;
+  __syncthreads();                           // (upto_of is read below alone)
+  if (lane == 0) sum_of[warp] = part;
+  __syncthreads();
+  double upto = upto_of[winner], last_upto = upto;
+  int chosen = -1, last_part = 0;
+  for (int w = 0; w < kWarps; ++w) {
+    if (sum_of[w] > 0.0) last_part = w, last_upto = upto;
+    if (chosen < 0 && sum_of[w] > 0.0 && upto + sum_of[w] > target) {
+      chosen = w;
+      break;
+    }
+    upto += sum_of[w];
+  }
+  if (chosen < 0) chosen = last_part, upto = last_upto;
+  if (warp != chosen) return;
+  int at = -1, last_at = -1;
+  double w_at = 0.0, last_w = 0.0;
+  for (int i0 = part_from; i0 < part_to; i0 += 32) {
+    const int i = i0 + lane;
+    float v[kV];
+    double w[kV], here = 0.0;
+    if (i < part_to) Slice<T>::widen(slice.fetch(i), v);
+#pragma unroll
+    for (int j = 0; j < kV; ++j) {
+      w[j] = i < part_to && v[j] > kNone ? weight(v[j]) : 0.0;
+      w[j] = w[j] < min_p ? 0.0 : w[j] * scale;
+      here += w[j];
+      if (w[j] > 0.0) last_at = i * kV + j, last_w = w[j];
+    }
+    double incl = here;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const double t = shuffle_up(incl, o);
+      if (lane >= o) incl += t;
+    }
+    const uint32_t over = __ballot_sync(0xffffffffu, here > 0.0 && upto + incl > target);
+    if (over) {
+      if (lane == __ffs(over) - 1) {
+        double a = upto + (incl - here);
+#pragma unroll
+        for (int j = 0; j < kV; ++j) {
+          if (w[j] > 0.0 && (at < 0 || a <= target)) at = i * kV + j, w_at = w[j];
+          a += w[j];
+        }
+      }
+      last_at = at;
+      last_w = w_at;
+      break;
+    }
+    upto += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  const int best_at = __reduce_max_sync(0xffffffffu, last_at);
+  if (best_at >= 0 && last_at == best_at) {
+    p.ids[row] = best_at;
+    if (p.logp) p.logp[row] = static_cast<float>(log(last_w / total));
+  }
+}
+
 }  // namespace
 
 struct sfb_sampler {
@@ -1335,12 +1604,16 @@ cudaError_t launch(SampleParams p, int64_t n, cudaStream_t s) {
   p.ctas = ctas;
   p.share = static_cast<int32_t>((vectors + ctas - 1) / ctas);
   p.resident = std::min(p.share, (n * ctas <= 112 ? kHeldMost : kHeldTwo) / 16);
-#ifndef SMALLN
-#define SMALLN 256
-#endif
   const bool small = p.share <= kHeldFour / 16 && n * ctas > 2 * sfb::kModelSms;
-  if (p.top_k || p.top_p) return small ? launch<T, SMALLN, true>(p, n, s) : launch<T, 512, true>(p, n, s);
-  return small ? launch<T, SMALLN, false>(p, n, s) : launch<T, 512, false>(p, n, s);
+  if (p.top_k || p.top_p) return small ? launch<T, 256, true>(p, n, s) : launch<T, 512, true>(p, n, s);
+  // (with a row for each CTA nothing but the random number's share is read twice)
+  if (ctas == 1) {
+#ifndef PLAINN
+#define PLAINN 256
+#endif
+    return sfb::launch_kernel(sample_plain_kernel<T, PLAINN>, dim3(static_cast<unsigned>(n)), dim3(PLAINN), 0, s, 1, p);
+  }
+  return launch<T, 512, false>(p, n, s);
 }
 
 }  // namespace
