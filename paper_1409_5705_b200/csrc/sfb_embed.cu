@@ -131,42 +131,37 @@ struct DropoutParams {
   DropParams drop;
 };
 
-template <typename T, bool RESIDUAL, int N>
-__global__ void __launch_bounds__(kThreads, N == 1 ? 1 : 4) dropout_kernel(const __grid_constant__ DropoutParams p) {
+// (One group a thread and 2,048 threads an SM: what takes the time where entries are of 16 bits is the generator, and more threads hide more of it
+// than more loads a thread do.  us at 8,192 x 5,000 bf16 with a residual: 47; with two and four groups a thread 53 and 63.)
+template <typename T, bool RESIDUAL>
+__global__ void __launch_bounds__(kThreads, 2048 / kThreads) dropout_kernel(const __grid_constant__ DropoutParams p) {
   pdl_launch_dependents();
   pdl_wait();
-  const Place first = first_place<N>(p.grid, blockIdx.x);
-  Raw<T> raw[N], more[RESIDUAL ? N : 1];
-  Place at[N];
-#pragma unroll
-  for (int k = 0; k < N; ++k) {
-    at[k] = place_at(p.grid, first, k);
-    if (at[k].row >= p.grid.rows) continue;
-    const int count = p.grid.count(at[k].group);
-    sfb::load_group(address<T>(p.x, p.pitch_x, at[k]), count, p.wide, raw[k]);
-    if constexpr (RESIDUAL) sfb::load_group(address<T>(p.r, p.pitch_r, at[k]), count, p.wide, more[k]);
+  const Place at = place_at(p.grid, first_place<1>(p.grid, blockIdx.x), 0);
+  const bool there = at.row < p.grid.rows;
+  const int count = p.grid.count(at.group);
+  Raw<T> raw, more;
+  if (there) {
+    sfb::load_group(address<T>(p.x, p.pitch_x, at), count, p.wide, raw);
+    if constexpr (RESIDUAL) sfb::load_group(address<T>(p.r, p.pitch_r, at), count, p.wide, more);
   }
   Generator generator;
   generator.begin(p.drop);
+  if (!there) return;
+  float v[kGroup];
+  sfb::unpack(raw, v);
+  if (p.drop.threshold) generator.drop(v, at.row, at.group, p.drop.last);
+  if constexpr (RESIDUAL) {
+    float u[kGroup];
+    sfb::unpack(more, u);
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    if (at[k].row >= p.grid.rows) break;
-    float v[kGroup];
-    sfb::unpack(raw[k], v);
-    if (p.drop.threshold) generator.drop(v, at[k].row, at[k].group, p.drop.last);
-    if constexpr (RESIDUAL) {
-      float u[kGroup];
-      sfb::unpack(more[k], u);
+    for (int j = 0; j < kGroup; ++j) v[j] = fmaf(v[j], p.drop.factor, u[j]);
+  } else {
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j) v[j] = fmaf(v[j], p.drop.factor, u[j]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < kGroup; ++j) v[j] *= p.drop.factor;
-    }
-    Raw<T> r;
-    sfb::pack(v, r);
-    sfb::store_group(address<T>(p.y, p.pitch_y, at[k]), p.grid.count(at[k].group), p.wide, r);
+    for (int j = 0; j < kGroup; ++j) v[j] *= p.drop.factor;
   }
+  sfb::pack(v, raw);
+  sfb::store_group(address<T>(p.y, p.pitch_y, at), count, p.wide, raw);
 }
 
 // ---- the samples in the order of their tokens ----------------------------------------------------------------------------------------
@@ -310,7 +305,8 @@ struct Order {
 };
 
 __device__ __forceinline__ void mark(const Order& o, uint32_t key, uint32_t tokens) {
-  if (key < tokens) atomicOr(o.touched + (key >> 5), 1u << (key & 31));
+  const uint32_t bit = 1u << (key & 31);
+  if (key < tokens && !(__ldcg(o.touched + (key >> 5)) & bit)) atomicOr(o.touched + (key >> 5), bit);
 }
 
 // Where the CTAs' samples of each digit begin, to their `base`.  A CTA takes a share of the bins: the totals of all CTAs there, added up over CTAs
@@ -427,7 +423,9 @@ __global__ void __launch_bounds__(1024) mark_kernel(const int32_t* ids, int64_t 
   cluster_sync();
   for (int64_t i = at; i < n; i += step) {
     const uint32_t id = static_cast<uint32_t>(ids[i]);
-    if (id < tokens) atomicOr(touched + (id >> 5), 1u << (id & 31));
+    const uint32_t bit = 1u << (id & 31);
+    // (looked at first: frequent tokens would queue)
+    if (id < tokens && !(__ldcg(touched + (id >> 5)) & bit)) atomicOr(touched + (id >> 5), bit);
   }
 }
 
@@ -761,11 +759,8 @@ cudaError_t launch_rows(const RowsParams& p, int32_t out, bool drop, cudaStream_
 
 template <typename T, bool RESIDUAL>
 cudaError_t launch_dropout(const DropoutParams& p, cudaStream_t s) {
-  constexpr int N = RESIDUAL ? 2 : 4;
   const int64_t all = static_cast<int64_t>(p.grid.rows) * p.grid.groups.d;
-  if (all >= static_cast<int64_t>(sfb::kModelSms) * kThreads * N)
-    return sfb::launch_kernel(dropout_kernel<T, RESIDUAL, N>, dim3(static_cast<unsigned>((all + kThreads * N - 1) / (kThreads * N))), dim3(kThreads), 0, s, 1, p);
-  return sfb::launch_kernel(dropout_kernel<T, RESIDUAL, 1>, dim3(static_cast<unsigned>((all + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, 1, p);
+  return sfb::launch_kernel(dropout_kernel<T, RESIDUAL>, dim3(static_cast<unsigned>((all + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, 1, p);
 }
 template <typename T>
 cudaError_t launch_dropout(const DropoutParams& p, cudaStream_t s) {

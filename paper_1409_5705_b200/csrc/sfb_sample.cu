@@ -1329,8 +1329,8 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
 // largest logit that each has seen (when a larger one comes up, what it has is rescaled).  Sums and largest logits of the warps say which one the
 // random number falls on, and that warp goes over its share again.  Rows with min-p, which needs the largest logit first, are gone over twice.
 template <typename T, int N>
-__global__ void __launch_bounds__(N, 1024 / N) sample_plain_kernel(const __grid_constant__ SampleParams p) {
-  constexpr int kV = Slice<T>::kV, kWarps = N / 32, kAhead = 4;
+__global__ void __launch_bounds__(N, 1280 / N) sample_plain_kernel(const __grid_constant__ SampleParams p) {
+  constexpr int kV = Slice<T>::kV, kWarps = N / 32, kAhead = 2;
   __shared__ double power[kTable], sum_of[kWarps], upto_of[kWarps], total_of;
   __shared__ float most_of[kWarps];
   __shared__ uint32_t keeps_of[kWarps];
@@ -1607,12 +1607,7 @@ cudaError_t launch(SampleParams p, int64_t n, cudaStream_t s) {
   const bool small = p.share <= kHeldFour / 16 && n * ctas > 2 * sfb::kModelSms;
   if (p.top_k || p.top_p) return small ? launch<T, 256, true>(p, n, s) : launch<T, 512, true>(p, n, s);
   // (with a row for each CTA nothing but the random number's share is read twice)
-  if (ctas == 1) {
-#ifndef PLAINN
-#define PLAINN 256
-#endif
-    return sfb::launch_kernel(sample_plain_kernel<T, PLAINN>, dim3(static_cast<unsigned>(n)), dim3(PLAINN), 0, s, 1, p);
-  }
+  if (ctas == 1) return sfb::launch_kernel(sample_plain_kernel<T, 256>, dim3(static_cast<unsigned>(n)), dim3(256), 0, s, 1, p);
   return launch<T, 512, false>(p, n, s);
 }
 
