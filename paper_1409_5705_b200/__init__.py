@@ -629,9 +629,10 @@ class _Handle:
             raise ValueError(f"a {dtype} tensor on {self._device} is wanted, not {t.dtype} on {t.device}")
         if t.shape != (n, width):
             raise ValueError(f"a tensor [{n}, {width}] is wanted, not {list(t.shape)}")
-        if width > 1 and t.stride(1) != 1:
+        pitch, step = t.stride()
+        if step != 1 and width > 1:
             raise ValueError("the last dimension of a tensor has no gaps")
-        return t.data_ptr(), t.stride(0) if n > 1 else (width + 7) // 8 * 8
+        return t.data_ptr(), pitch if n > 1 else (width + 7) // 8 * 8
 
     def _vector(self, t, dtype, n):
         if t is None:
