@@ -9,6 +9,7 @@
 //                     writes the sum where the token changes.  Work is even however often a token comes up.  A token that goes beyond
 //                     a chunk leaves a part in each.
 //     join_kernel     adds the parts of such tokens in their order
+//   or, for few samples, gradient_few_kernel alone
 // Sums are in fp32, in an order that depends on the ids alone: the same bits from call to call.
 // All are bound by HBM: the rows read once, the table's rows written once.
 #include <algorithm>
@@ -360,12 +361,11 @@ struct ZeroParams {
 // Rows that start on 16-byte boundaries by copies of zeros from shared memory, a row a thread; what lies behind the last 16 bytes, and
 // other rows, by stores.  `zeros`: kZeroBytes of shared memory.
 constexpr int kZeroBytes = 4096;
-template <int THREADS>
-__device__ __forceinline__ void zero_rows(const ZeroParams& p, uint4* zeros, int64_t block, int64_t blocks) {
+template <int THREADS, typename F>
+__device__ __forceinline__ void zero_rows(const ZeroParams& p, uint4* zeros, int64_t block, int64_t blocks, F&& untouched) {
   for (int i = threadIdx.x; i < kZeroBytes / 16; i += THREADS) zeros[i] = make_uint4(0, 0, 0, 0);
   sfb::ptx::fence_proxy_async_smem();
   __syncthreads();
-  auto untouched = [&](int64_t row) { return !(p.touched[row >> 5] >> (row & 31) & 1); };
   if (p.wide) {
     const int64_t bytes = p.dim / 4 * 16;
     for (int64_t row = static_cast<int64_t>(threadIdx.x) * blocks + block; row < p.tokens; row += blocks * THREADS) {
@@ -383,6 +383,11 @@ __device__ __forceinline__ void zero_rows(const ZeroParams& p, uint4* zeros, int
   for (int64_t row = block * warps + (threadIdx.x >> 5); row < p.tokens; row += blocks * warps)
     if (untouched(row))
       for (int64_t col = lane; col < p.dim; col += 32) p.table[row * p.ldt + col] = 0.f;
+}
+
+template <int THREADS>
+__device__ __forceinline__ void zero_rows(const ZeroParams& p, uint4* zeros, int64_t block, int64_t blocks) {
+  zero_rows<THREADS>(p, zeros, block, blocks, [&](int64_t row) { return !(p.touched[row >> 5] >> (row & 31) & 1); });
 }
 
 // The first cluster sorts, the others zero.
@@ -597,6 +602,100 @@ __global__ void __launch_bounds__(kThreads, 4) gradient_kernel(const __grid_cons
   }
 }
 
+// Up to kFew samples, in one launch: a warp has a sample and 32 groups of columns.  It compares the sample's token with all others; the first
+// sample of a token adds them all, in their order.  Other blocks zero rows that are no sample's token.
+constexpr int kFew = 256;
+template <typename T, bool DROP, bool ADD>
+__global__ void __launch_bounds__(kThreads) gradient_few_kernel(const __grid_constant__ GradientParams p, const __grid_constant__ ZeroParams zero, const int32_t* given,
+                                                                uint32_t zeros, uint32_t* status) {
+  __shared__ __align__(128) uint4 shared[kZeroBytes / 16];
+  __shared__ __align__(16) int32_t ids[kFew];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int n = static_cast<int>(p.n), lane = threadIdx.x & 31;
+  for (int i = threadIdx.x; i < kFew; i += kThreads) ids[i] = i < n ? given[i] : -1;
+  __syncthreads();
+  if (blockIdx.x < zeros) {
+    zero_rows<kThreads>(zero, shared, blockIdx.x, zeros, [&](int64_t row) {
+      const int4* q = reinterpret_cast<const int4*>(ids);
+      const int t = static_cast<int>(row);
+      bool found = false;
+#pragma unroll 4
+      for (int i = 0; i < (n + 3) / 4; ++i) {
+        const int4 w = q[i];
+        found |= w.x == t || w.y == t || w.z == t || w.w == t;
+      }
+      return !found;
+    });
+    return;
+  }
+  Generator generator;
+  if constexpr (DROP) generator.begin(p.drop);
+  const uint32_t slabs = (p.groups.d + 31) / 32, item = (blockIdx.x - zeros) * (kThreads / 32) + (threadIdx.x >> 5);
+  const int i = static_cast<int>(item / slabs);
+  if (i >= n) return;
+  const uint32_t slab = item % slabs, group = slab * 32 + lane;
+  const int32_t id = ids[i];
+  if (static_cast<uint32_t>(id) >= p.tokens) {
+    if (id != -1 && slab == 0 && lane == 0) atomicOr(status, SFB_STATUS_INDEX_RANGE);
+    return;
+  }
+  uint32_t same[kFew / 32];
+  bool first = true;
+#pragma unroll
+  for (int b = 0; b < kFew / 32; ++b) {
+    same[b] = __ballot_sync(0xffffffffu, ids[b * 32 + lane] == id);
+    const uint32_t before = i >= (b + 1) * 32 ? 0xffffffffu : i > b * 32 ? (1u << (i - b * 32)) - 1 : 0;
+    first &= !(same[b] & before);
+  }
+  if (!first) return;
+  const int64_t col = static_cast<int64_t>(group) * kGroup;
+  const int count = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(kGroup), p.dim - col)));
+  float* to = p.table + static_cast<int64_t>(id) * p.lddt + col;
+  Raw<float> r{};
+  if constexpr (ADD) {
+    if (count) sfb::load_group(to, count, p.wide_out, r);
+  }
+  float sum[kGroup] = {};
+  constexpr int kTogether = 4;
+  int at[kTogether], have = 0;
+  auto take = [&]() {
+    Raw<T> raw[kTogether];
+#pragma unroll
+    for (int q = 0; q < kTogether; ++q)
+      if (q < have && count) sfb::load_group(static_cast<const T*>(p.dx) + at[q] * p.lddx + col, count, p.wide_in, raw[q]);
+#pragma unroll
+    for (int q = 0; q < kTogether; ++q) {
+      if (q >= have || !count) break;
+      float v[kGroup];
+      sfb::unpack(raw[q], v);
+      if constexpr (DROP) generator.drop(v, at[q], group, p.drop.last);
+#pragma unroll
+      for (int j = 0; j < kGroup; ++j) sum[j] += v[j];
+    }
+    have = 0;
+  };
+#pragma unroll
+  for (int b = 0; b < kFew / 32; ++b) {
+#pragma unroll 1
+    for (uint32_t left = same[b]; left; left &= left - 1) {
+      const int j = b * 32 + __ffs(left) - 1;
+#pragma unroll
+      for (int q = 0; q < kTogether; ++q)
+        if (q == have) at[q] = j;
+      if (++have == kTogether) take();
+    }
+  }
+  if (have) take();
+  if (!count) return;
+  float v[kGroup];
+  sfb::unpack(r, v);
+#pragma unroll
+  for (int j = 0; j < kGroup; ++j) v[j] = fmaf(p.factor, sum[j], v[j]);
+  sfb::pack(v, r);
+  sfb::store_group(to, count, p.wide_out, r);
+}
+
 // Blocks take (token, 32 groups) in turn: eight warps add contiguous shares of the parts, the first adds the shares.
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ GradientParams p) {
   __shared__ float shares[8][32][kGroup + 1];
@@ -786,14 +885,18 @@ cudaError_t sort_samples(const EmbedLayout& l, char* ws, const sfb_embed_config&
   p.status = reinterpret_cast<uint32_t*>(ws + l.status);
   const cudaStream_t s = static_cast<cudaStream_t>(c.stream);
   if (n <= kSortMost) {
-    const int per = n <= kSortThreads * kSortCtas ? 1 : n <= 2 * kSortThreads * kSortCtas ? 2 : 4;
+    // As many CTAs as there are for the sort; but the fewest where zeroing takes longer than that anyway (100 MB: 16 us), since clusters of few CTAs leave
+    // more SMs to it (us at 16,384 samples, 50,000 x 2,000: with 16 CTAs 68 to 77, with 4 SORTED).
+    const bool few = o.words > 0 && c.tokens * c.dim * 4 > (100ll << 20);
+    const int per = few || n > 2 * kSortThreads * kSortCtas ? 4 : n > kSortThreads * kSortCtas ? 2 : 1;
     int ctas = 1;
     while (static_cast<int64_t>(ctas) * kSortThreads * per < n) ctas *= 2;
     int zeros = 0;                     // CTAs that zero, in clusters like the one that sorts: as many as the chip has room for beside it
     if (o.words > 0) {
       const cudaError_t e = sfb::launch_kernel(mark_kernel, dim3(8), dim3(1024), 0, s, 8, ids, n, p.tokens, o.touched, o.words);
       if (e != cudaSuccess) return e;
-      zeros = static_cast<int>(std::min<int64_t>(112 - ctas, (c.tokens + 31) / 32));
+      const int room = ctas <= 2 ? 148 : ctas == 4 ? 132 : ctas == 8 ? 120 : 112;
+      zeros = static_cast<int>(std::min<int64_t>(room - ctas, (c.tokens + 31) / 32));
       zeros = std::max(1, zeros / ctas) * ctas;
     }
     if (per == 1) return launch_sort<1>(p, o, zero, digits, ctas, zeros, s);
@@ -826,6 +929,12 @@ template <typename T, bool DROP>
 cudaError_t launch_gradient(const GradientParams& p, unsigned blocks, cudaStream_t s) {
   return p.add ? sfb::launch_kernel(gradient_kernel<T, DROP, true>, dim3(blocks), dim3(kThreads), 0, s, 1, p)
                : sfb::launch_kernel(gradient_kernel<T, DROP, false>, dim3(blocks), dim3(kThreads), 0, s, 1, p);
+}
+template <typename T>
+cudaError_t launch_few(const GradientParams& p, const ZeroParams& zero, const int32_t* ids, uint32_t zeros, uint32_t* status, bool drop, unsigned blocks, cudaStream_t s) {
+  auto launch = [&](auto kernel) { return sfb::launch_kernel(kernel, dim3(blocks), dim3(kThreads), 0, s, 1, p, zero, ids, zeros, status); };
+  if (p.add) return drop ? launch(gradient_few_kernel<T, true, true>) : launch(gradient_few_kernel<T, false, true>);
+  return drop ? launch(gradient_few_kernel<T, true, false>) : launch(gradient_few_kernel<T, false, false>);
 }
 template <typename T>
 cudaError_t launch_gradient(const GradientParams& p, bool drop, unsigned blocks, cudaStream_t s) {
@@ -967,24 +1076,10 @@ extern "C" int sfb_embed_backward(sfb_embed* h, int64_t n, const int32_t* ids_de
   if (on.err != cudaSuccess) return fail(h, on.err);
   const EmbedLayout l = layout_of(c);
   const bool drops = drop && drop->drop.threshold > 0;
-  Order o{};
-  for (int k = 0; k < 2; ++k) o.entries[k] = reinterpret_cast<uint2*>(h->ws + l.entries[k]);
-  o.touched = reinterpret_cast<uint32_t*>(h->ws + l.touched);
-  o.crossing = reinterpret_cast<uint32_t*>(h->ws + l.crossing);
-  o.words = add ? 0 : l.words;
   const cudaStream_t s = static_cast<cudaStream_t>(c.stream);
-  const ZeroParams zero{o.touched, dE_dev, ldde, c.tokens, c.dim, sfb::lies_wide(dE_dev, ldde, SFB_F32)};
-  cudaError_t e = sort_samples(l, h->ws, c, n, ids_dev, o, zero);
-  if (e != cudaSuccess) return fail(h, e);
-  if (n == 0) return SFB_OK;
   GradientParams p{};
-  p.order = o.entries[0];
-  p.crossing = o.crossing;
-  p.parts = reinterpret_cast<float*>(h->ws + l.parts);
   p.n = n;
   p.groups = Divisor(static_cast<uint32_t>(groups_of(c.dim)));
-  p.per = samples_per_chunk(n, p.groups.d);
-  p.chunks = static_cast<uint32_t>((n + p.per - 1) / p.per);
   p.tokens = static_cast<uint32_t>(c.tokens);
   p.dx = dX_dev;
   p.lddx = lddx;
@@ -999,12 +1094,35 @@ extern "C" int sfb_embed_backward(sfb_embed* h, int64_t n, const int32_t* ids_de
     p.drop = drop->drop;
     p.drop.call = call;
   }
+  Order o{};
+  for (int k = 0; k < 2; ++k) o.entries[k] = reinterpret_cast<uint2*>(h->ws + l.entries[k]);
+  o.touched = reinterpret_cast<uint32_t*>(h->ws + l.touched);
+  o.crossing = reinterpret_cast<uint32_t*>(h->ws + l.crossing);
+  o.words = add ? 0 : l.words;
+  const ZeroParams zero{o.touched, dE_dev, ldde, c.tokens, c.dim, p.wide_out};
+  const int64_t slabs = (p.groups.d + 31) / 32;
+  cudaError_t e;
+  if (n <= kFew) {
+    const unsigned zeros = add ? 0 : static_cast<unsigned>(std::min<int64_t>((c.tokens + 31) / 32, sfb::sm_count() * 4));
+    const unsigned blocks = zeros + static_cast<unsigned>((n * slabs + kThreads / 32 - 1) / (kThreads / 32));
+    uint32_t* status = reinterpret_cast<uint32_t*>(h->ws + l.status);
+    e = c.out_dtype == SFB_F32 ? launch_few<float>(p, zero, ids_dev, zeros, status, drops, blocks, s)
+        : c.out_dtype == SFB_BF16 ? launch_few<__nv_bfloat16>(p, zero, ids_dev, zeros, status, drops, blocks, s)
+                                  : launch_few<__half>(p, zero, ids_dev, zeros, status, drops, blocks, s);
+    return e == cudaSuccess ? SFB_OK : fail(h, e);
+  }
+  e = sort_samples(l, h->ws, c, n, ids_dev, o, zero);
+  if (e != cudaSuccess) return fail(h, e);
+  p.order = o.entries[0];
+  p.crossing = o.crossing;
+  p.parts = reinterpret_cast<float*>(h->ws + l.parts);
+  p.per = samples_per_chunk(n, p.groups.d);
+  p.chunks = static_cast<uint32_t>((n + p.per - 1) / p.per);
   const unsigned blocks = static_cast<unsigned>((static_cast<int64_t>(p.chunks) * p.groups.d + kThreads - 1) / kThreads);
   e = c.out_dtype == SFB_F32 ? launch_gradient<float>(p, drops, blocks, s)
       : c.out_dtype == SFB_BF16 ? launch_gradient<__nv_bfloat16>(p, drops, blocks, s) : launch_gradient<__half>(p, drops, blocks, s);
   // (a single chunk has nothing that goes beyond it)
   if (e == cudaSuccess && p.chunks > 1) {
-    const int64_t slabs = (p.groups.d + 31) / 32;
     const unsigned joins = static_cast<unsigned>(std::min<int64_t>(static_cast<int64_t>(sfb::sm_count()) * 8, static_cast<int64_t>(p.chunks - 1) * slabs));
     e = sfb::launch_kernel(join_kernel, dim3(joins), dim3(256), 0, s, 1, p);
   }
