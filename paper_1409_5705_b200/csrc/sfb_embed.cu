@@ -2,9 +2,8 @@
 //
 //   lookup, dropout   embed_rows_kernel, dropout_kernel: a thread takes groups of eight entries of the output rows
 //   gradient          dE[t] = alpha s sum_{i: id_i = t} m_i dX_i:
-//     mark_kernel     a bit for each token that some sample names (where dE is written whole)
-//     sort_kernel     the samples in the order of their tokens (stable: a token's samples stay in their order); meanwhile other SMs zero the
-//                     rows that no sample names
+//     sort_kernel     the samples in the order of their tokens (stable: a token's samples stay in their order); meanwhile other SMs zero dE
+//                     (where it is written whole)
 //     gradient_kernel chunks of that order, whichever tokens they hold: a thread adds the samples of a chunk for a group of columns and
 //                     writes the sum where the token changes.  Work is even however often a token comes up.  A token that goes beyond
 //                     a chunk leaves a part in each.
@@ -300,15 +299,8 @@ __device__ __forceinline__ void cluster_write(uint32_t* here, int cta, uint32_t 
 // Where the sorted samples and what goes with them lie; two buffers that the digits take in turn, the last one writes the first.
 struct Order {
   uint2* entries[2];                   // (key, sample)
-  uint32_t* touched;                   // a bit for each token that some sample names
   uint32_t* crossing;                  // [0]: how many chunks hold the beginning of a token that goes beyond them, then which
-  int64_t words;                       // of touched; 0: not wanted
 };
-
-__device__ __forceinline__ void mark(const Order& o, uint32_t key, uint32_t tokens) {
-  const uint32_t bit = 1u << (key & 31);
-  if (key < tokens && !(__ldcg(o.touched + (key >> 5)) & bit)) atomicOr(o.touched + (key >> 5), bit);
-}
 
 // Where the CTAs' samples of each digit begin, to their `base`.  A CTA takes a share of the bins: the totals of all CTAs there, added up over CTAs
 // and bins; what lies in the shares before it comes to every CTA as one number.
@@ -351,9 +343,9 @@ __device__ __forceinline__ void place_digits(SortShared& s, int bits, int ctas, 
   __syncthreads();
 }
 
-// Rows of dE that no sample names.
+// dE, all of it: what the rows that samples name cost twice is less than a list of the others (16,384 samples, 50,000 x 2,000: 7 us for 43 MB, 8 for bits
+// of the tokens; with 100 tokens the bits took 26, of threads that queue for few words).
 struct ZeroParams {
-  const uint32_t* touched;
   float* table;
   int64_t ldt, tokens, dim;
   bool wide;
@@ -362,14 +354,14 @@ struct ZeroParams {
 // other rows, by stores.  `zeros`: kZeroBytes of shared memory.
 constexpr int kZeroBytes = 4096;
 template <int THREADS, typename F>
-__device__ __forceinline__ void zero_rows(const ZeroParams& p, uint4* zeros, int64_t block, int64_t blocks, F&& untouched) {
+__device__ __forceinline__ void zero_rows(const ZeroParams& p, uint4* zeros, int64_t block, int64_t blocks, F&& wanted) {
   for (int i = threadIdx.x; i < kZeroBytes / 16; i += THREADS) zeros[i] = make_uint4(0, 0, 0, 0);
   sfb::ptx::fence_proxy_async_smem();
   __syncthreads();
   if (p.wide) {
     const int64_t bytes = p.dim / 4 * 16;
     for (int64_t row = static_cast<int64_t>(threadIdx.x) * blocks + block; row < p.tokens; row += blocks * THREADS) {
-      if (!untouched(row)) continue;
+      if (!wanted(row)) continue;
       float* to = p.table + row * p.ldt;
       for (int64_t at = 0; at < bytes; at += kZeroBytes)
         sfb::ptx::bulk_store(reinterpret_cast<char*>(to) + at, zeros, static_cast<uint32_t>(min(static_cast<int64_t>(kZeroBytes), bytes - at)));
@@ -381,13 +373,13 @@ __device__ __forceinline__ void zero_rows(const ZeroParams& p, uint4* zeros, int
   }
   const int lane = threadIdx.x & 31, warps = THREADS / 32;
   for (int64_t row = block * warps + (threadIdx.x >> 5); row < p.tokens; row += blocks * warps)
-    if (untouched(row))
+    if (wanted(row))
       for (int64_t col = lane; col < p.dim; col += 32) p.table[row * p.ldt + col] = 0.f;
 }
 
 template <int THREADS>
 __device__ __forceinline__ void zero_rows(const ZeroParams& p, uint4* zeros, int64_t block, int64_t blocks) {
-  zero_rows<THREADS>(p, zeros, block, blocks, [&](int64_t row) { return !(p.touched[row >> 5] >> (row & 31) & 1); });
+  zero_rows<THREADS>(p, zeros, block, blocks, [](int64_t) { return true; });
 }
 
 // The first cluster sorts, the others zero.
@@ -419,21 +411,6 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(SortParams p, con
   }
 }
 
-// A bit for each token that some sample names: one cluster, which clears them all first.
-__global__ void __launch_bounds__(1024) mark_kernel(const int32_t* ids, int64_t n, uint32_t tokens, uint32_t* touched, int64_t words) {
-  pdl_launch_dependents();
-  pdl_wait();
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * 1024 + threadIdx.x, step = static_cast<int64_t>(gridDim.x) * 1024;
-  for (int64_t i = at; i < words; i += step) touched[i] = 0;
-  cluster_sync();
-  for (int64_t i = at; i < n; i += step) {
-    const uint32_t id = static_cast<uint32_t>(ids[i]);
-    const uint32_t bit = 1u << (id & 31);
-    // (looked at first: frequent tokens would queue)
-    if (id < tokens && !(__ldcg(touched + (id >> 5)) & bit)) atomicOr(touched + (id >> 5), bit);
-  }
-}
-
 __global__ void __launch_bounds__(256) zero_kernel(const __grid_constant__ ZeroParams p) {
   __shared__ __align__(128) uint4 zeros[kZeroBytes / 16];
   pdl_launch_dependents();
@@ -442,29 +419,17 @@ __global__ void __launch_bounds__(256) zero_kernel(const __grid_constant__ ZeroP
 }
 
 // The same for more samples, a launch each.
-__global__ void __launch_bounds__(256) sort_clear_kernel(const __grid_constant__ Order o) {
-  pdl_launch_dependents();
-  pdl_wait();
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i == 0) o.crossing[0] = 0;
-  if (i < o.words) o.touched[i] = 0;
-}
-
-__global__ void __launch_bounds__(kSortThreads, 1) sort_count_kernel(const __grid_constant__ SortParams p, const __grid_constant__ Order o) {
+__global__ void __launch_bounds__(kSortThreads, 1) sort_count_kernel(const __grid_constant__ SortParams p, uint32_t* crossing) {
   extern __shared__ __align__(128) unsigned char shared[];
   SortShared& s = *reinterpret_cast<SortShared*>(shared);
   pdl_launch_dependents();
   pdl_wait();
+  if (blockIdx.x == 0 && threadIdx.x == 0) crossing[0] = 0;
   const int64_t first = static_cast<int64_t>(blockIdx.x) * kSortTile;
   uint2 e[kSortPer];
   uint16_t rank[kSortPer];
   rank_tile<kSortPer>(s, p, first, e, rank);
   if (threadIdx.x < (1 << p.bits)) p.counts[threadIdx.x * p.tiles + blockIdx.x] = s.total[threadIdx.x];
-  if (p.ids && o.words) {
-#pragma unroll
-    for (int j = 0; j < kSortPer; ++j)
-      if (first + (threadIdx.x >> 5) * (32 * kSortPer) + j * 32 + (threadIdx.x & 31) < p.n) mark(o, e[j].x, p.tokens);
-  }
 }
 
 // A warp a bin: how many of it lie in the tiles before each, and in all.
@@ -696,57 +661,92 @@ __global__ void __launch_bounds__(kThreads) gradient_few_kernel(const __grid_con
   sfb::store_group(to, count, p.wide_out, r);
 }
 
-// Blocks take (token, 32 groups) in turn: eight warps add contiguous shares of the parts, the first adds the shares.
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ GradientParams p) {
+// Warps take (token, 32 groups) in turn and add the token's parts in their order.  Where there are more than kSerial, the block does so afterwards:
+// eight warps add contiguous shares of the parts, the first adds the shares.
+constexpr int kSerial = 16;
+__device__ __forceinline__ void add_parts(const GradientParams& p, uint32_t chunk, uint32_t group, int64_t from, int64_t to, float (&sum)[kGroup]) {
+  for (int64_t k0 = from; k0 < to; k0 += 4) {
+    Raw<float> r[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t k = k0 + q, slot = k == 0 ? 2 * static_cast<int64_t>(chunk) + 1 : 2 * (chunk + k);
+      if (k < to) sfb::load_group(p.parts + (slot * p.groups.d + group) * kGroup, kGroup, true, r[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (k0 + q >= to) break;
+      float v[kGroup];
+      sfb::unpack(r[q], v);
+#pragma unroll
+      for (int j = 0; j < kGroup; ++j) sum[j] += v[j];
+    }
+  }
+}
+__device__ __forceinline__ void store_joined(const GradientParams& p, uint32_t key, uint32_t group, const float (&sum)[kGroup]) {
+  const int64_t col = static_cast<int64_t>(group) * kGroup;
+  const int count = static_cast<int>(min(static_cast<int64_t>(kGroup), p.dim - col));
+  float* to = p.table + key * p.lddt + col;
+  Raw<float> r{};
+  float v[kGroup];
+  if (p.add) sfb::load_group(to, count, p.wide_out, r);
+  sfb::unpack(r, v);
+#pragma unroll
+  for (int j = 0; j < kGroup; ++j) v[j] = fmaf(p.factor, sum[j], v[j]);
+  sfb::pack(v, r);
+  sfb::store_group(to, count, p.wide_out, r);
+}
+
+__global__ void __launch_bounds__(256, 4) join_kernel(const __grid_constant__ GradientParams p) {
   __shared__ float shares[8][32][kGroup + 1];
+  __shared__ struct { uint32_t chunk, slab, key; int64_t parts; } later[8];
+  __shared__ uint32_t left;
   pdl_launch_dependents();
   pdl_wait();
   const uint32_t count = p.crossing[0], slabs = (p.groups.d + 31) / 32;
-  const int share = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (uint64_t item = blockIdx.x; item < static_cast<uint64_t>(count) * slabs; item += gridDim.x) {
-    const uint32_t chunk = p.crossing[1 + item / slabs], group = static_cast<uint32_t>(item % slabs) * 32 + lane;
-    const uint32_t key = p.order[(static_cast<int64_t>(chunk) + 1) * p.per - 1].x;
-    // the chunks behind it that begin with this token
-    int64_t more = 0;
-    for (int got = 256; got == 256; more += got) {
-      const int64_t at = (static_cast<int64_t>(chunk) + 1 + more + threadIdx.x) * p.per;
-      const uint32_t there = at < p.n ? p.order[at].x : p.tokens;
-      got = __syncthreads_count(there == key);
-    }
-    const int64_t each = (more + 1 + 7) / 8, from = share * each, to = min(more + 1, from + each);
-    float sum[kGroup] = {};
-    if (group < p.groups.d) {
-#pragma unroll 8
-      for (int64_t k = from; k < to; ++k) {
-        const int64_t slot = k == 0 ? 2 * static_cast<int64_t>(chunk) + 1 : 2 * (chunk + k);
-        Raw<float> r;
-        float v[kGroup];
-        sfb::load_group(p.parts + (slot * p.groups.d + group) * kGroup, kGroup, true, r);
-        sfb::unpack(r, v);
-#pragma unroll
-        for (int j = 0; j < kGroup; ++j) sum[j] += v[j];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint64_t items = static_cast<uint64_t>(count) * slabs;
+  // (a block's warps far apart in the list, where tokens of many parts may follow one another)
+  for (uint64_t first = blockIdx.x; first < items; first += static_cast<uint64_t>(gridDim.x) * 8) {
+    if (threadIdx.x == 0) left = 0;
+    __syncthreads();
+    const uint64_t item = first + static_cast<uint64_t>(warp) * gridDim.x;
+    if (item < items) {
+      const uint32_t chunk = p.crossing[1 + item / slabs], slab = static_cast<uint32_t>(item % slabs), group = slab * 32 + lane;
+      const uint32_t key = p.order[(static_cast<int64_t>(chunk) + 1) * p.per - 1].x;
+      int64_t parts = 1;               // the chunk's own, and one of each chunk behind it that begins with this token
+      for (int got = 32; got == 32; parts += got) {
+        const int64_t at = (chunk + parts + lane) * p.per;
+        const uint32_t there = at < p.n ? p.order[at].x : p.tokens;
+        got = __popc(__ballot_sync(0xffffffffu, there == key));
+      }
+      if (parts > kSerial) {
+        if (lane == 0) {
+          const uint32_t at = atomicAdd(&left, 1u);
+          later[at].chunk = chunk, later[at].slab = slab, later[at].key = key, later[at].parts = parts;
+        }
+      } else if (group < p.groups.d) {
+        float sum[kGroup] = {};
+        add_parts(p, chunk, group, 0, parts, sum);
+        store_joined(p, key, group, sum);
       }
     }
-#pragma unroll
-    for (int j = 0; j < kGroup; ++j) shares[share][lane][j] = sum[j];
     __syncthreads();
-    if (share == 0 && group < p.groups.d) {
-      for (int w = 1; w < 8 && w * each <= more; ++w)
+    for (uint32_t q = 0; q < left; ++q) {
+      const uint32_t group = later[q].slab * 32 + lane;
+      const int64_t parts = later[q].parts, each = (parts + 7) / 8, from = warp * each, to = min(parts, from + each);
+      float sum[kGroup] = {};
+      if (group < p.groups.d) add_parts(p, later[q].chunk, group, from, to, sum);
 #pragma unroll
-        for (int j = 0; j < kGroup; ++j) sum[j] += shares[w][lane][j];
-      const int64_t col = static_cast<int64_t>(group) * kGroup;
-      const int count = static_cast<int>(min(static_cast<int64_t>(kGroup), p.dim - col));
-      float* to = p.table + key * p.lddt + col;
-      Raw<float> r{};
-      float v[kGroup];
-      if (p.add) sfb::load_group(to, count, p.wide_out, r);
-      sfb::unpack(r, v);
+      for (int j = 0; j < kGroup; ++j) shares[warp][lane][j] = sum[j];
+      __syncthreads();
+      if (warp == 0 && group < p.groups.d) {
+        for (int w = 1; w < 8; ++w)
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j) v[j] = fmaf(p.factor, sum[j], v[j]);
-      sfb::pack(v, r);
-      sfb::store_group(to, count, p.wide_out, r);
+          for (int j = 0; j < kGroup; ++j) sum[j] += shares[w][lane][j];
+        store_joined(p, later[q].key, group, sum);
+      }
+      __syncthreads();
     }
-    __syncthreads();
   }
 }
 
@@ -791,8 +791,8 @@ int samples_per_chunk(int64_t n, int64_t groups) {
 }
 
 struct EmbedLayout {
-  size_t status, crossing, touched, entries[2], counts, totals, parts, bytes;
-  int64_t words, tiles;
+  size_t status, crossing, entries[2], counts, totals, parts, bytes;
+  int64_t tiles;
 };
 
 EmbedLayout layout_of(const sfb_embed_config& c) {
@@ -804,7 +804,6 @@ EmbedLayout layout_of(const sfb_embed_config& c) {
     return at;
   };
   const int64_t n = c.max_ids, groups = groups_of(c.dim);
-  l.words = (c.tokens + 31) / 32;
   l.tiles = (n + kSortTile - 1) / kSortTile;
   l.status = take(16);
   // chunks: the most that any number of samples up to n is cut into, and their parts
@@ -815,7 +814,6 @@ EmbedLayout layout_of(const sfb_embed_config& c) {
     chunks = std::max(chunks, (most + per - 1) / per);
   }
   l.crossing = take((chunks + 1) * 4);
-  l.touched = take(l.words * 4);
   for (size_t& e : l.entries) e = take(n * 8);
   l.counts = take(l.tiles * kMaxBins * 4);
   l.totals = take(kMaxBins * 4);
@@ -873,7 +871,7 @@ cudaError_t launch_sort(const SortParams& p, const Order& o, const ZeroParams& z
   return e == cudaSuccess ? sfb::launch_kernel(sort_kernel<PER>, dim3(ctas + zeros), dim3(kSortThreads), sizeof(SortShared), s, ctas, p, o, zero, digits, ctas) : e;
 }
 
-cudaError_t sort_samples(const EmbedLayout& l, char* ws, const sfb_embed_config& c, int64_t n, const int32_t* ids, const Order& o, const ZeroParams& zero) {
+cudaError_t sort_samples(const EmbedLayout& l, char* ws, const sfb_embed_config& c, int64_t n, const int32_t* ids, const Order& o, const ZeroParams* zero) {
   int bits = 1;
   while ((1ll << bits) <= c.tokens) ++bits;            // of the keys 0 .. tokens
   const int digits = (bits + kMaxBits - 1) / kMaxBits;
@@ -884,44 +882,42 @@ cudaError_t sort_samples(const EmbedLayout& l, char* ws, const sfb_embed_config&
   p.bits = (bits + digits - 1) / digits;
   p.status = reinterpret_cast<uint32_t*>(ws + l.status);
   const cudaStream_t s = static_cast<cudaStream_t>(c.stream);
+  cudaError_t e = cudaSuccess;
   if (n <= kSortMost) {
     // As many CTAs as there are for the sort; but the fewest where zeroing takes longer than that anyway (100 MB: 16 us), since clusters of few CTAs leave
     // more SMs to it (us at 16,384 samples, 50,000 x 2,000: with 16 CTAs 68 to 77, with 4 SORTED).
-    const bool few = o.words > 0 && c.tokens * c.dim * 4 > (100ll << 20);
+    const bool few = zero && c.tokens * c.dim * 4 > (100ll << 20);
     const int per = few || n > 2 * kSortThreads * kSortCtas ? 4 : n > kSortThreads * kSortCtas ? 2 : 1;
     int ctas = 1;
     while (static_cast<int64_t>(ctas) * kSortThreads * per < n) ctas *= 2;
     int zeros = 0;                     // CTAs that zero, in clusters like the one that sorts: as many as the chip has room for beside it
-    if (o.words > 0) {
-      const cudaError_t e = sfb::launch_kernel(mark_kernel, dim3(8), dim3(1024), 0, s, 8, ids, n, p.tokens, o.touched, o.words);
-      if (e != cudaSuccess) return e;
+    if (zero) {
       const int room = ctas <= 2 ? 148 : ctas == 4 ? 132 : ctas == 8 ? 120 : 112;
       zeros = static_cast<int>(std::min<int64_t>(room - ctas, (c.tokens + 31) / 32));
       zeros = std::max(1, zeros / ctas) * ctas;
     }
-    if (per == 1) return launch_sort<1>(p, o, zero, digits, ctas, zeros, s);
-    if (per == 2) return launch_sort<2>(p, o, zero, digits, ctas, zeros, s);
-    return launch_sort<4>(p, o, zero, digits, ctas, zeros, s);
+    if (per == 1) return launch_sort<1>(p, o, zero ? *zero : ZeroParams{}, digits, ctas, zeros, s);
+    if (per == 2) return launch_sort<2>(p, o, zero ? *zero : ZeroParams{}, digits, ctas, zeros, s);
+    return launch_sort<4>(p, o, zero ? *zero : ZeroParams{}, digits, ctas, zeros, s);
   }
   p.tiles = (n + kSortTile - 1) / kSortTile;
   p.counts = reinterpret_cast<uint32_t*>(ws + l.counts);
   p.totals = reinterpret_cast<uint32_t*>(ws + l.totals);
-  cudaError_t e = sfb::allow_smem<sort_count_kernel>(sizeof(SortShared));
+  e = sfb::allow_smem<sort_count_kernel>(sizeof(SortShared));
   if (e == cudaSuccess) e = sfb::allow_smem<sort_move_kernel>(sizeof(SortShared));
-  if (e == cudaSuccess) e = sfb::launch_kernel(sort_clear_kernel, dim3(static_cast<unsigned>(std::max<int64_t>(1, (o.words + 255) / 256))), dim3(256), 0, s, 1, o);
   for (int d = 0; d < digits && e == cudaSuccess; ++d) {
     const int to = (digits - 1 - d) & 1;
     p.out = o.entries[to];
     p.shift = d * p.bits;
     const dim3 tiles(static_cast<unsigned>(p.tiles));
-    e = sfb::launch_kernel(sort_count_kernel, tiles, dim3(kSortThreads), sizeof(SortShared), s, 1, p, o);
+    e = sfb::launch_kernel(sort_count_kernel, tiles, dim3(kSortThreads), sizeof(SortShared), s, 1, p, o.crossing);
     if (e == cudaSuccess) e = sfb::launch_kernel(sort_sum_kernel, dim3(((1 << p.bits) + 7) / 8), dim3(256), 0, s, 1, p);
     if (e == cudaSuccess) e = sfb::launch_kernel(sort_move_kernel, tiles, dim3(kSortThreads), sizeof(SortShared), s, 1, p);
     p.ids = nullptr;
     p.in = p.out;
   }
-  if (e == cudaSuccess && o.words > 0)
-    e = sfb::launch_kernel(zero_kernel, dim3(static_cast<unsigned>(std::min<int64_t>((c.tokens + 31) / 32, sfb::sm_count()))), dim3(256), 0, s, 1, zero);
+  if (e == cudaSuccess && zero)
+    e = sfb::launch_kernel(zero_kernel, dim3(static_cast<unsigned>(std::min<int64_t>((c.tokens + 31) / 32, sfb::sm_count() * 4))), dim3(256), 0, s, 1, *zero);
   return e;
 }
 
@@ -1096,10 +1092,8 @@ extern "C" int sfb_embed_backward(sfb_embed* h, int64_t n, const int32_t* ids_de
   }
   Order o{};
   for (int k = 0; k < 2; ++k) o.entries[k] = reinterpret_cast<uint2*>(h->ws + l.entries[k]);
-  o.touched = reinterpret_cast<uint32_t*>(h->ws + l.touched);
   o.crossing = reinterpret_cast<uint32_t*>(h->ws + l.crossing);
-  o.words = add ? 0 : l.words;
-  const ZeroParams zero{o.touched, dE_dev, ldde, c.tokens, c.dim, p.wide_out};
+  const ZeroParams zero{dE_dev, ldde, c.tokens, c.dim, p.wide_out};
   const int64_t slabs = (p.groups.d + 31) / 32;
   cudaError_t e;
   if (n <= kFew) {
@@ -1111,7 +1105,7 @@ extern "C" int sfb_embed_backward(sfb_embed* h, int64_t n, const int32_t* ids_de
                                   : launch_few<__half>(p, zero, ids_dev, zeros, status, drops, blocks, s);
     return e == cudaSuccess ? SFB_OK : fail(h, e);
   }
-  e = sort_samples(l, h->ws, c, n, ids_dev, o, zero);
+  e = sort_samples(l, h->ws, c, n, ids_dev, o, add ? nullptr : &zero);
   if (e != cudaSuccess) return fail(h, e);
   p.order = o.entries[0];
   p.crossing = o.crossing;
@@ -1123,7 +1117,7 @@ extern "C" int sfb_embed_backward(sfb_embed* h, int64_t n, const int32_t* ids_de
       : c.out_dtype == SFB_BF16 ? launch_gradient<__nv_bfloat16>(p, drops, blocks, s) : launch_gradient<__half>(p, drops, blocks, s);
   // (a single chunk has nothing that goes beyond it)
   if (e == cudaSuccess && p.chunks > 1) {
-    const unsigned joins = static_cast<unsigned>(std::min<int64_t>(static_cast<int64_t>(sfb::sm_count()) * 8, static_cast<int64_t>(p.chunks - 1) * slabs));
+    const unsigned joins = static_cast<unsigned>(std::min<int64_t>(static_cast<int64_t>(sfb::sm_count()) * 4, (static_cast<int64_t>(p.chunks - 1) * slabs + 7) / 8));
     e = sfb::launch_kernel(join_kernel, dim3(joins), dim3(256), 0, s, 1, p);
   }
   return e == cudaSuccess ? SFB_OK : fail(h, e);
