@@ -137,7 +137,7 @@ struct Shared {
   double scan[kWarps];                       // (also of the other types that are scanned)
   double part[2][kWarps];
   uint32_t part_count[kWarps];
-  float part_most[kWarps], part_least[kWarps], part_gate[kWarps];
+  float part_most[kWarps], part_least[kWarps];
   uint32_t listed, found[2], first;
   uint32_t low_before, likely_before, likely_upto;
   float last_bin;
@@ -148,9 +148,8 @@ struct Shared {
   float most[kMaxCtas], least[kMaxCtas];
   double sums[2][kMaxCtas];
   uint32_t counts[kMaxCtas];
-  float gates[kMaxCtas];
   // the row's warps, in their order: what is kept, but for the last key, of which there are `ties`
-  double sum[kMaxCtas * kWarps];
+  alignas(16) double sum[kMaxCtas * kWarps];
   uint32_t ties[kMaxCtas * kWarps], keeps[kMaxCtas * kWarps];
   double total;
   int32_t winner;
@@ -440,15 +439,17 @@ __device__ __forceinline__ uint32_t place_in(unsigned long long entry, int bits)
 
 // Entries in ascending order are logits in the order by falling logit and rising place.  The last entry of the beginning of that order whose
 // values (value null: 1 each; kOut: none) first come to `target` (1 or more), or the last of all: looked for among [low, high] first, among all where
-// it is not there.  By sums of bins of the range, then of the bin that it is in, until that has few entries, which are compared each with each.
+// it is not there (from_first: no entry lies before the range).  By sums of bins of the range, then of the bin that it is in, until that has few entries, which are compared each with each.
 template <int N, bool FILTERS>
 __device__ __noinline__ unsigned long long find_end(Shared<N, FILTERS>& s, const unsigned long long* list, const unsigned long long* value, int n,
-                                                    unsigned long long low, unsigned long long high, unsigned long long target) {
+                                                    unsigned long long low, unsigned long long high, unsigned long long target, bool from_first) {
   constexpr int kBins = Shared<N, FILTERS>::kBins;
   auto worth = [&](int i) { return value ? (value[i] == kOut ? 0 : value[i]) : 1ull; };
   unsigned long long before = 0, all;
-  for (int i = threadIdx.x; i < n; i += N) before += list[i] < low ? worth(i) : 0;
-  block_scan(s, before, before);
+  if (!from_first) {
+    for (int i = threadIdx.x; i < n; i += N) before += list[i] < low ? worth(i) : 0;
+    block_scan(s, before, before);
+  }
   for (bool begins = true;; begins = false) {
     const unsigned long long width = high - low;
     const int shift = width < kBins ? 0 : __clz(kBins) + 33 - __clzll(static_cast<long long>(width));
@@ -562,16 +563,20 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       }
     }
     m = fmaxf(Type<T>::largest(high), kNone);
-    // so many of each warp's lanes have a largest logit of at least the warp's gate that the warps together have top_k
-    const int64_t rounds = (static_cast<int64_t>(top_k) + ctas * kWarps - 1) / (ctas * kWarps);
+    // A bound below the k-th largest: of the warps' `rounds`-th largest lanes the one that so many warps come up to that they have top_k logits
+    // together.  About half of the warps, where that takes more than a lane of each: the least of all would be a poor bound.
+    constexpr int kMostRounds = 16;
+    const int warps = ctas * kWarps, rounds = top_k <= warps ? 1 : static_cast<int>(min((2ll * top_k + warps - 1) / warps, static_cast<long long>(kMostRounds + 1)));
+    const bool gated = top_k > 1 && rounds <= kMostRounds;
     float gate = kNone;
-    if (top_k > 1 && rounds <= 8) {
+    if (gated) {
       uint32_t key = key_of<0>(m), best = 0;
+#pragma unroll 1
       for (int q = 0; q < rounds; ++q) {
         best = __reduce_max_sync(0xffffffffu, key);
         if (lane == __ffs(__ballot_sync(0xffffffffu, key == best)) - 1) key = 0;
       }
-      gate = value_of<0>(best);              // (where a warp has fewer logits: minus infinity, or what is no number)
+      gate = fmaxf(value_of<0>(best), kNone);            // (where a warp has fewer logits: minus infinity)
     }
     least = min_nan(Type<T>::smallest(low), tail);
 #pragma unroll
@@ -579,24 +584,42 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
       least = min_nan(least, __shfl_xor_sync(0xffffffffu, least, o));
     }
-    if (lane == 0) s.part_most[warp] = m, s.part_least[warp] = least, s.part_gate[warp] = gate;
+    if (lane == 0) s.part_most[warp] = m, s.part_least[warp] = least;
     __syncthreads();
     m = s.part_most[0];
     least = s.part_least[0];
 #pragma unroll
     for (int w = 1; w < kWarps; ++w) m = fmaxf(m, s.part_most[w]), least = min_nan(least, s.part_least[w]);
-    gate = s.part_gate[0];
-#pragma unroll
-    for (int w = 1; w < kWarps; ++w) gate = min_nan(gate, s.part_gate[w]);
+    float* gates = reinterpret_cast<float*>(s.sum);      // of the row's warps (whose sums come in the end)
     if (ctas > 1) {
       asm volatile("barrier.cluster.wait;" ::: "memory");          // (all of the row's CTAs are there)
-      if (threadIdx.x < ctas)
-        write(&s.most[cta], threadIdx.x, m), write(&s.least[cta], threadIdx.x, least), write(&s.gates[cta], threadIdx.x, gate);
+      if (threadIdx.x < ctas) write(&s.most[cta], threadIdx.x, m), write(&s.least[cta], threadIdx.x, least);
+      if (gated && lane < ctas) write(&gates[cta * kWarps + warp], lane, gate);
       row_sync(ctas);
-      for (int c = 0; c < ctas; ++c) m = fmaxf(m, s.most[c]), least = min_nan(least, s.least[c]), gate = min_nan(gate, s.gates[c]);
+      for (int c = 0; c < ctas; ++c) m = fmaxf(m, s.most[c]), least = min_nan(least, s.least[c]);
+    } else if (gated) {
+      if (lane == 0) gates[warp] = gate;
+      __syncthreads();
     }
     m += 0.f;
-    if (gate > k_gate) k_gate = gate;
+    if (gated) {
+      const int wanted = (top_k + rounds - 1) / rounds;            // warps
+      if (threadIdx.x < warps) {
+        const float mine = gates[threadIdx.x];
+        int larger = 0;
+#pragma unroll 4
+        for (int w = 0; w < warps; w += 4) {
+          const float4 g = *reinterpret_cast<const float4*>(&s.sum[w / 2]);
+          const float of[4] = {g.x, g.y, g.z, g.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) larger += of[j] > mine || (of[j] == mine && w + j < static_cast<int>(threadIdx.x));
+        }
+        if (larger == wanted - 1) s.part_most[0] = mine;
+      }
+      __syncthreads();
+      k_gate = fmaxf(k_gate, s.part_most[0]);
+      __syncthreads();
+    }
   }
   const bool holes = !(least > kNone);       // some logit is minus infinity or no number
   if (m == kNone) {                          // nothing to draw from
@@ -649,6 +672,25 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
     for (int c = 0; c < ctas; ++c) a += s.sums[0][c], b += s.sums[1][c], n += s.counts[c];
   };
 
+  // Adds a logit to this CTA's list.
+  auto list = [&](float z, int i) {
+    const uint32_t at = atomicAdd(&s.listed, 1u);
+    if (at < kList) s.list[at] = static_cast<unsigned long long>(~key_of<LOW>(z)) << bits | static_cast<uint32_t>(first + i);
+  };
+  // Room for all lists in the place of CTA 0's share of the row; how many there are (-1: no list of all that can be kept), and among which keys
+  // top-k and the nucleus end.
+  const int room = 2 * kList;
+  unsigned long long *entry = reinterpret_cast<unsigned long long*>(dynamic), *value = entry + room;        // (p.resident is twice kList at least)
+  int in_list = -1;
+  Range k_keys{}, p_keys{};
+  auto collect_all = [&]() {                 // (after a row_sync)
+    in_list = collect(s, ctas, room, cta == 0, entry);
+    row_sync(ctas);                          // (the lists are read)
+    if (in_list >= 0) return;
+    if (threadIdx.x == 0) s.listed = 0;      // (too many, or too many in one CTA's share)
+    __syncthreads();
+  };
+
   // 2. counts by distance
   bool cuts = false;                         // top-k leaves something out
   uint32_t k = 0, k_bin = 0, k_before = 0, k_upto = 0, low_bin = 0, high_bin = 0, nucleus_before = 0, nucleus_upto = 0, likely_low = 0, likely_high = 0,
@@ -661,7 +703,18 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
   auto bin_of = [&](float z) {
     return endless ? (z == m ? 0u : kBins - 1) : min(__float2uint_rz((m - z) * scale), static_cast<uint32_t>(kBins - 1));
   };
-  if (filters) {
+  bool unbinned = false;                     // the list was made without bins
+  if (FILTERS && k_gate > -kLargest && static_cast<int64_t>(top_k) * 6 <= room) {      // (those from k_gate on are a few times top_k)
+    each_hit(slice, from, to, k_gate, INFINITY, list);
+    row_sync(ctas);
+    collect_all();
+    if (in_list >= 0) {
+      cuts = unbinned = true;
+      k = static_cast<uint32_t>(top_k);
+      k_keys = p_keys = Range{key_of<LOW>(k_gate), key_of<LOW>(m)};
+    }
+  }
+  if (filters && in_list < 0) {
     for (int b = threadIdx.x; b < kBins; b += N) s.count[b] = 0;
     __syncthreads();
     // (all logits; those from k_gate on, where they are top_k or more and nothing is asked of the others)
@@ -760,14 +813,8 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
 
   // The weights of all logits, where something takes their sum, and of those in the bins before the nucleus's end; what lies in the bins of that end
   // is listed, where it is no more than a list holds (and not all that can be kept is listed below).
-  const int room = p.resident >= 2 * kList ? 2 * kList : p.resident >= kList ? kList : 0;
-  const bool listed_all = filters && (cuts ? k_upto : nucleus_upto) <= room;
+  const bool listed_all = filters && in_list < 0 && (cuts ? k_upto : nucleus_upto) <= room;
   const bool few = filters && nucleus && !cuts && !listed_all && likely <= kList;
-  // Adds a logit to this CTA's list.
-  auto list = [&](float z, int i) {
-    const uint32_t at = atomicAdd(&s.listed, 1u);
-    if (at < kList) s.list[at] = static_cast<unsigned long long>(~key_of<LOW>(z)) << bits | static_cast<uint32_t>(first + i);
-  };
   double all = 0.0, over = 0.0;
   uint32_t over_count = 0;
   if (!cuts && (nucleus || min_p == 0.0)) {
@@ -821,10 +868,12 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       spread(all, 0.0, 0u);
       row_sync(ctas);
       gathered(whole, above, none);
-      unsigned long long* entry = reinterpret_cast<unsigned long long*>(dynamic);
-      unsigned long long* value = entry + room;
-      const int n = collect(s, ctas, room, cta == 0, entry);
-      row_sync(ctas);                        // (the lists are read)
+      k_keys = range_of<LOW, kBins>(m, unit, k_bin, k_bin);
+      p_keys = range_of<LOW, kBins>(m, unit, likely_low, likely_high);
+      collect_all();
+    }
+    {
+      const int n = in_list;
       if (n >= 0) {
         if (cta != 0) return;
         for (int i = threadIdx.x; i < n; i += N) value[i] = __double2ull_rn(weight(value_of<LOW>(key_in(entry[i], bits))) * kGrain);
@@ -836,10 +885,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
             if (entry[i] > end) value[i] = kOut;
           __syncthreads();
         };
-        if (cuts) {
-          const Range r = range_of<LOW, kBins>(m, unit, k_bin, k_bin);
-          leave_out(find_end(s, entry, nullptr, n, first_of(r), last_of(r), k));
-        }
+        if (cuts) leave_out(find_end(s, entry, nullptr, n, first_of(k_keys), last_of(k_keys), k, unbinned));
         if (nucleus) {
           double goal = whole * kGrain;
           if (cuts) {
@@ -848,8 +894,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
             goal = static_cast<double>(total);
           }
           goal = fmin(fmax(ceil(static_cast<double>(top_p) * goal), 1.0), 9.0e18);
-          const Range r = range_of<LOW, kBins>(m, unit, likely_low, likely_high);
-          leave_out(find_end(s, entry, value, n, first_of(r), last_of(r), __double2ull_rn(goal)));
+          leave_out(find_end(s, entry, value, n, first_of(p_keys), last_of(p_keys), __double2ull_rn(goal), unbinned));
         }
         // The draw, in the order of the places: sums by shares of the row, by shares of the share that the random number falls on, until what is
         // left is little enough to compare each with each.
@@ -866,7 +911,15 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         const unsigned long long goal = min(u < 1.0 ? __double2ull_rz(u * static_cast<double>(total)) : total, total - 1);
         int64_t base = 0, size = p.classes;
         unsigned long long ahead = 0;
-        for (;;) {
+        if (threadIdx.x == 0) s.listed = 0;
+        __syncthreads();
+        bool few_kept = kept <= kSmall;
+        if (few_kept) {
+          for (int i = threadIdx.x; i < n; i += N)
+            if (value[i] != kOut) s.small_entry[atomicAdd(&s.listed, 1u)] = static_cast<unsigned long long>(place_in(entry[i], bits)) << 32 | i;
+          __syncthreads();
+        }
+        while (!few_kept) {
           const uint32_t part = static_cast<uint32_t>((size + kBins - 1) / kBins);
           for (int b = threadIdx.x; b < kBins; b += N) s.mass[b] = 0;
           if (threadIdx.x == 0) s.listed = 0;
@@ -914,8 +967,6 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         }
         return;
       }
-      if (threadIdx.x == 0) s.listed = 0;    // (too much in one CTA's share)
-      __syncthreads();
     }
 
     // All lists to every CTA.
@@ -951,7 +1002,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         });
         row_sync(ctas);
         const int n = gather();
-        ends_at(n, find_end(s, s.order, nullptr, n, first_of(r), last_of(r), k - k_before));
+        ends_at(n, find_end(s, s.order, nullptr, n, first_of(r), last_of(r), k - k_before, true));
       }
       while (!few_k) {
         const int shift = shift_of<kBins>(r);
@@ -975,7 +1026,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         uint32_t a = over + block_scan(s, sum, inside);
         if (shift > 0 && inside <= kList) {
           const int n = list_range(r);
-          ends_at(n, find_end(s, s.order, nullptr, n, first_of(r), last_of(r), k - over));
+          ends_at(n, find_end(s, s.order, nullptr, n, first_of(r), last_of(r), k - over, true));
           break;
         }
 #pragma unroll
@@ -1020,7 +1071,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         block_scan(s, sum, sum);
         if (!sure && !(above < target && goal <= static_cast<double>(sum))) return false;
         if (sum > 0 && !(cut_inside && goal > static_cast<double>(sum))) {
-          ends_at(n, find_end(s, s.order, s.value, n, first_of(r), last_of(r), __double2ull_rn(fmin(goal, 9.0e18))));
+          ends_at(n, find_end(s, s.order, s.value, n, first_of(r), last_of(r), __double2ull_rn(fmin(goal, 9.0e18)), true));
         } else if (cut_inside) {
           const double more = ceil((goal - static_cast<double>(sum)) / (cut_weight * kGrain));
           last_key = cut_key;
@@ -1587,7 +1638,9 @@ constexpr int kShareMost = 128 << 10;        // bytes of a row that a CTA has, a
 int slots(int ctas) { return ctas <= 2 ? 296 : ctas == 4 ? 284 : ctas == 8 ? 264 : 224; }
 
 template <typename T, int N, bool FILTERS>
-cudaError_t launch(const SampleParams& p, int64_t n, cudaStream_t s) {
+cudaError_t launch(SampleParams p, int64_t n, cudaStream_t s) {
+  // (the lists have room in the place of the row: at least for twice what one CTA lists)
+  if (FILTERS) p.resident = std::max(p.resident, 2 * Of<N>::kList);
   cudaError_t e = sfb::allow_smem<sample_kernel<T, N, FILTERS>>(kHeldMost);
   if (e == cudaSuccess && p.ctas > 8) e = sfb::allow_clusters<sample_kernel<T, N, FILTERS>>();
   if (e != cudaSuccess) return e;
