@@ -696,7 +696,8 @@ __device__ __forceinline__ void store_joined(const GradientParams& p, uint32_t k
   sfb::store_group(to, count, p.wide_out, r);
 }
 
-__global__ void __launch_bounds__(256, 4) join_kernel(const __grid_constant__ GradientParams p) {
+// (Two blocks an SM: with the registers of four, spills took half of the time.  us at 16,384 samples, 50,000 x 2,000: 6; with three and four 8, 11.)
+__global__ void __launch_bounds__(256, 2) join_kernel(const __grid_constant__ GradientParams p) {
   __shared__ float shares[8][32][kGroup + 1];
   __shared__ struct { uint32_t chunk, slab, key; int64_t parts; } later[8];
   __shared__ uint32_t left;
@@ -771,8 +772,8 @@ int fail(H* h, cudaError_t e) {
   return SFB_ERR_CUDA;
 }
 
-constexpr int64_t kPieces = static_cast<int64_t>(sfb::kModelSms) * 2048;
-constexpr int kPer[] = {4, 8, 16, 32, 64};
+constexpr int64_t kPieces = static_cast<int64_t>(sfb::kModelSms) * 1024;
+constexpr int kPerLeast = 4, kPerMost = 64;
 constexpr int64_t kBlocksMost = (1ll << 31) - 1;
 
 // Of a matrix that the element-wise kernels take: up to 2^31 rows, rows less than 4 GB apart.
@@ -782,12 +783,11 @@ Grid grid_of(int64_t n, int64_t cols) {
   return Grid{Divisor(static_cast<uint32_t>(groups)), static_cast<uint32_t>(n), static_cast<uint32_t>(cols - (groups - 1) * kGroup)};
 }
 
-// Samples a chunk: the fewest (more, smaller pieces of work) that still are two full rounds of threads or, beyond that, keep what is left
-// of tokens that go beyond a chunk a small part of what is read.
+// Samples a chunk: one full round of threads, which end together (us at 16,384 samples, 50,000 x 2,000, and at 65,000 added to 325,000 x 1,000, with a join
+// of more registers spilled: 110 and 103; with two rounds 114 and 102, four 121 and 109); but no fewer than 4, and no more than 64, where parts are a small share of what is read.
 int samples_per_chunk(int64_t n, int64_t groups) {
-  for (const int per : kPer)
-    if ((n + per - 1) / per * groups <= kPieces) return per;
-  return 64;
+  const int64_t chunks = std::max<int64_t>(1, kPieces / groups);
+  return static_cast<int>(std::max<int64_t>(kPerLeast, std::min<int64_t>(kPerMost, (n + chunks - 1) / chunks)));
 }
 
 struct EmbedLayout {
@@ -807,12 +807,7 @@ EmbedLayout layout_of(const sfb_embed_config& c) {
   l.tiles = (n + kSortTile - 1) / kSortTile;
   l.status = take(16);
   // chunks: the most that any number of samples up to n is cut into, and their parts
-  int64_t chunks = 1;
-  for (const int per : kPer) {
-    // the rule takes `per` up to this many samples
-    const int64_t most = per == 64 ? n : std::min(n, kPieces / groups * per);
-    chunks = std::max(chunks, (most + per - 1) / per);
-  }
+  const int64_t chunks = std::max({static_cast<int64_t>(1), (n + kPerMost - 1) / kPerMost, std::min((n + kPerLeast - 1) / kPerLeast, kPieces / groups)});
   l.crossing = take((chunks + 1) * 4);
   for (size_t& e : l.entries) e = take(n * 8);
   l.counts = take(l.tiles * kMaxBins * 4);
@@ -885,7 +880,7 @@ cudaError_t sort_samples(const EmbedLayout& l, char* ws, const sfb_embed_config&
   cudaError_t e = cudaSuccess;
   if (n <= kSortMost) {
     // As many CTAs as there are for the sort; but the fewest where zeroing takes longer than that anyway (100 MB: 16 us), since clusters of few CTAs leave
-    // more SMs to it (us at 16,384 samples, 50,000 x 2,000: with 16 CTAs 68 to 77, with 4 SORTED).
+    // more SMs to it (us at 16,384 samples, 50,000 x 2,000: with 16 CTAs 75, with 4 71).
     const bool few = zero && c.tokens * c.dim * 4 > (100ll << 20);
     const int per = few || n > 2 * kSortThreads * kSortCtas ? 4 : n > kSortThreads * kSortCtas ? 2 : 1;
     int ctas = 1;
@@ -1117,7 +1112,7 @@ extern "C" int sfb_embed_backward(sfb_embed* h, int64_t n, const int32_t* ids_de
       : c.out_dtype == SFB_BF16 ? launch_gradient<__nv_bfloat16>(p, drops, blocks, s) : launch_gradient<__half>(p, drops, blocks, s);
   // (a single chunk has nothing that goes beyond it)
   if (e == cudaSuccess && p.chunks > 1) {
-    const unsigned joins = static_cast<unsigned>(std::min<int64_t>(static_cast<int64_t>(sfb::sm_count()) * 4, (static_cast<int64_t>(p.chunks - 1) * slabs + 7) / 8));
+    const unsigned joins = static_cast<unsigned>(std::min<int64_t>(static_cast<int64_t>(sfb::sm_count()) * 2, (static_cast<int64_t>(p.chunks - 1) * slabs + 7) / 8));
     e = sfb::launch_kernel(join_kernel, dim3(joins), dim3(256), 0, s, 1, p);
   }
   return e == cudaSuccess ? SFB_OK : fail(h, e);
