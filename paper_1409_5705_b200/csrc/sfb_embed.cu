@@ -10,7 +10,7 @@
 //     join_kernel     adds the parts of such tokens in their order
 //   or, for few samples, gradient_few_kernel alone
 // Sums are in fp32, in an order that depends on the ids alone: the same bits from call to call.
-// All are bound by HBM: the rows read once, the table's rows written once.
+// All are to be bound by HBM: the rows read once, the table's rows written once.  What each has reached of that stands beside it.
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -73,6 +73,9 @@ struct RowsParams {
 };
 
 // Blocks take pieces in turn, the ids of the next one under way while one is copied.
+// 16,384 samples of 2,000 from 325,000 tokens, fp32 to bf16, with dropout: 32 us for 120 MB (19 at the rate of a plain copy); a row that comes up again is
+// read from L2, and it is the loads of 196 MB through it, 32 KB under way an SM, and the generator's instructions (half of all issue slots) that take
+// the time.  One launch's latency for few samples (2.5 us at 7 of 5,000).
 template <typename In, typename Out, bool DROP, int N>
 __global__ void __launch_bounds__(kThreads, N == 1 ? 1 : 4) embed_rows_kernel(const __grid_constant__ RowsParams p) {
   pdl_launch_dependents();
@@ -382,7 +385,8 @@ __device__ __forceinline__ void zero_rows(const ZeroParams& p, uint4* zeros, int
   zero_rows<THREADS>(p, zeros, block, blocks, [](int64_t) { return true; });
 }
 
-// The first cluster sorts, the others zero.
+// The first cluster sorts, the others zero.  (65,000 samples, two digits: 25 us, of barriers, ballots and remote reads; nothing of it is HBM's.  Having the
+// other CTAs ask L2 for the samples' rows meanwhile made the gradient 2 us faster and the sort 3 us slower.)
 template <int PER>
 __global__ void __launch_bounds__(kSortThreads, 1) sort_kernel(SortParams p, const __grid_constant__ Order o, const __grid_constant__ ZeroParams zero, int digits, int ctas) {
   extern __shared__ __align__(128) unsigned char shared[];
@@ -491,6 +495,9 @@ struct GradientParams {
   DropParams drop;
 };
 
+// us, caches cold: 16,384 samples bf16 of 2,000 with dropout to 50,000 tokens 30 (66 MB of samples), 65,000 of 1,000 added to 325,000 tokens 65 (130 MB, and
+// 167 MB of rows read and written): 16 warps of 64 registers an SM with two samples' loads each are what is under way; more samples ahead took
+// as many warps away as they brought loads.
 constexpr int kAhead = 2;          // samples under way a thread
 
 template <typename T, bool DROP, bool ADD>
