@@ -1387,6 +1387,15 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
   }
 }
 
+// 16 bytes that the launch ahead may have written while this one began: no load of constant data (__ldg), which may be older than pdl_wait, or come
+// before it.  (volatile: in its place among the other asm; us at 2,048 rows of 10,000 fp32, caches cold: 53; with plain loads, which the compiler keeps
+// in order with more, 55.)
+__device__ __forceinline__ uint4 load_coherent(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+
 // Many rows without top-k and top-p: a CTA a row, whose warps go over their shares of it once, from global memory, with sums relative to the
 // largest logit that each has seen (when a larger one comes up, what it has is rescaled).  Sums and largest logits of the warps say which one the
 // random number falls on, and that warp goes over its share again.  Rows with min-p, which needs the largest logit first, are gone over twice.
@@ -1427,7 +1436,7 @@ __global__ void __launch_bounds__(N, 1280 / N) sample_plain_kernel(const __grid_
     if (slice.wide && i0 + kAhead * 32 <= to && static_cast<int64_t>(i0 + kAhead * 32) * kV <= slice.entries) {
       const uint4* z = reinterpret_cast<const uint4*>(slice.z) + i0 + lane;
 #pragma unroll
-      for (int q = 0; q < kAhead; ++q) w[q] = __ldg(z + q * 32);
+      for (int q = 0; q < kAhead; ++q) w[q] = load_coherent(z + q * 32);
     } else {
 #pragma unroll
       for (int q = 0; q < kAhead; ++q) {

@@ -1,0 +1,15 @@
+"""What once went wrong around lookup, dropout and sampling, as far as it shows without a GPU."""
+import os
+import re
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_1409_5705_b200", "csrc")
+
+
+@pytest.mark.parametrize("name", ["sfb_elem.cuh", "sfb_embed.cu", "sfb_sample.cu"])
+def test_kernels_that_start_early_read_coherently(name):
+    """A kernel that is there before the one ahead of it has ended may not load through the path for data that nobody writes while it runs: what that
+    holds may be older than its wait, and the compiler may move such a load above it."""
+    code = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, name)).read())
+    assert not re.search(r"__ldg\s*\(|ld\.global(\.\w+)*\.nc", code)
