@@ -1067,7 +1067,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       const uint32_t cut_key = last_key, cut_ties = last_ties;       // of top-k; key 0: none
       const double cut_weight = cuts ? weight(value_of<LOW>(cut_key)) : 0.0;
       const float cut_value = cuts ? value_of<LOW>(cut_key) : kNone;
-      const double grain = ldexp(1.0, p.fraction), back = ldexp(1.0, -p.fraction);
+      const double grain = ldexp(1.0, p.fraction);
       double target = 0.0;
       bool cut_inside = cuts && high_bin == k_bin;
       // A list of n logits that follow others with the sum `above`, behind them what top-k leaves of its last key (where that is in reach):
@@ -1108,14 +1108,20 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
           r = range_of<LOW, kBins>(m, unit, low_bin, high_bin);
         }
       }
+      // Sums by key are of weights as whole numbers: units of 2^-F of the largest weight that the range can have, or finer ones where all weights come to
+      // none (`lift`).  Each is off by half a unit, and equal ones all by the same, so a bin near whose edge the target falls may be the wrong one.
+      // The sums of its own weights in 64 bits say so when it is gone over, and the search goes on beside it, within `bound`, which is sure.
+      Range bound = r;
+      double lift = 1.0;
       if (listed < 0)
       for (bool begins = true;; begins = false) {
         const int shift = shift_of<kBins>(r);
+        const double top_weight = weight(value_of<LOW>(r.high)), unit_of = (top_weight > 0.0 ? grain / top_weight : grain) * lift;
         __syncthreads();
         if (!few_left)
           for (int b = threadIdx.x; b < kBins; b += N) s.mass[b] = 0;
         __syncthreads();
-        double over = 0.0;
+        double over = 0.0, within = 0.0;
         uint32_t inside = 0;
         each_vector(slice, from, to, begins && cuts ? cut_value : value_of<LOW>(r.low), [&](const float (&v)[kV]) {
 #pragma unroll
@@ -1132,8 +1138,9 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
               over += w;
             } else if (there && key >= r.low) {
               ++inside;
+              within += w;
               if (shift == 0) atomicAdd(&s.count[r.high - key], 1u);         // (a bin is one key: its weight comes in below)
-              else add(&s.mass[(r.high - key) >> shift], static_cast<unsigned long long>(__double2ll_rn(w * grain)));
+              else add(&s.mass[(r.high - key) >> shift], static_cast<unsigned long long>(__double2ll_rn(w * unit_of)));
             }
           }
         });
@@ -1142,46 +1149,73 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
             const uint32_t bin = bin_of(z);
             if (z > cut_value && bin >= low_bin && bin <= high_bin) list(z, i);
           });
-        spread(over, all, inside);
+        spread(over, begins ? all : within, inside);
         row_sync(ctas);
-        double sum_all;
-        gathered(above, sum_all, inside);
-        if (begins) target = static_cast<double>(top_p) * (sum_all + (cuts ? cut_ties * cut_weight : 0.0));
+        double sum;                          // of all that top-k leaves but for its last key; then of the range
+        gathered(above, sum, inside);
+        if (begins) target = static_cast<double>(top_p) * (sum + (cuts ? cut_ties * cut_weight : 0.0));
         if (few_left) {
           meet(gather(), true);
           break;
         }
-        unsigned long long some[kEach], sum = 0, mass;
-        if (shift == 0) {
-          uint32_t count[kEach];
-          sum_bins(s, s.count, ctas, cta, count);
-#pragma unroll
-          for (int j = 0; j < kEach; ++j)
-            some[j] = count[j] ? count[j] * static_cast<unsigned long long>(__double2ll_rn(weight(value_of<LOW>(r.high - threadIdx.x * kEach - j)) * grain)) : 0;
-        } else {
-          sum_bins(s, s.mass, ctas, cta, some);
-        }
         cut_inside = cuts && cut_key >= r.low && cut_key <= r.high;
+        if (!begins) {
+          if (cut_inside) sum += cut_ties * cut_weight;
+          const bool before = above >= target && r.high < bound.high, behind = above + sum < target && r.low > bound.low;
+          if (before || behind) {
+            if (before) bound.low = r.high + 1;
+            else bound.high = r.low - 1;
+            r = bound;
+            lift = 1.0;
+            row_sync(ctas);                  // (the sums are read)
+            continue;
+          }
+          bound = r;
+        }
         if (shift > 0 && inside <= kList) {
           meet(list_range(Range{max(r.low, cut_key + 1), r.high}), true);
           break;
         }
+        unsigned long long some[kEach], mine = 0, mass;
+        double units = unit_of;
+        if (shift == 0) {                    // counts of keys: their weights by 64-bit products, in units of 2^-61 of all of them
+          uint32_t count[kEach];
+          sum_bins(s, s.count, ctas, cta, count);
+          double here[kEach], of_mine = 0.0, of_all;
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          if (cut_inside && (r.high - cut_key) >> shift == threadIdx.x * kEach + j)
-            some[j] += cut_ties * static_cast<unsigned long long>(__double2ll_rn(cut_weight * grain));
-          sum += some[j];
+          for (int j = 0; j < kEach; ++j) {
+            const uint32_t at = threadIdx.x * kEach + j;
+            here[j] = count[j] ? count[j] * weight(value_of<LOW>(r.high - at)) : 0.0;
+            if (cut_inside && r.high - cut_key == at) here[j] += cut_ties * cut_weight;
+            of_mine += here[j];
+          }
+          block_scan(s, of_mine, of_all);
+          units = of_all > 0.0 ? 2305843009213693952.0 / of_all : 1.0;
+#pragma unroll
+          for (int j = 0; j < kEach; ++j) some[j] = __double2ull_rn(here[j] * units);
+        } else {
+          sum_bins(s, s.mass, ctas, cta, some);
+#pragma unroll
+          for (int j = 0; j < kEach; ++j)
+            if (cut_inside && (r.high - cut_key) >> shift == threadIdx.x * kEach + j) some[j] += cut_ties * __double2ull_rn(cut_weight * unit_of);
         }
-        unsigned long long ahead = block_scan(s, sum, mass);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) mine += some[j];
+        unsigned long long ahead = block_scan(s, mine, mass);
+        if (mass == 0 && shift > 0 && lift < 1e100) {    // (half a unit each at most: in units of 2^-F of that they come to 2^61 at most)
+          lift *= grain;
+          continue;
+        }
         // in whole numbers: what the target leaves for the bins, and at least one and at most what they hold, so that one thread finds it
-        const double left = ceil((target - above) * grain);
-        const unsigned long long want = min(left > 1.0 ? static_cast<unsigned long long>(left) : 1ull, mass);
+        const double left = ceil((target - above) * units);
+        const unsigned long long want = min(left > 1.0 ? __double2ull_rn(left) : 1ull, mass);
         if (mass == 0 && threadIdx.x == 0) s.found[0] = 0, s.found_at = above;       // (no weight in the range)
+        lift = 1.0;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
           if (ahead < want && ahead + some[j] >= want) {
             s.found[0] = threadIdx.x * kEach + j;
-            s.found_at = above + ahead * back;
+            s.found_at = above + ahead / units;
           }
           ahead += some[j];
         }
