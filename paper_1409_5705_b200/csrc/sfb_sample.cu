@@ -47,7 +47,7 @@ struct Of {
 constexpr unsigned long long kOut = 1ull << 63;          // the weight of what a filter has left out of a list
 constexpr double kGrain = 1125899906842624.0;            // weights of a list are whole numbers, 2^-50 of the largest
 constexpr float kWidest = 32.f;              // bins of 2 reach to e^-32 of the largest weight at most
-constexpr float kFar = 45.f;                 // weights below e^-45 of the largest count as zero: all of them together are below 1e-13
+constexpr float kFar = 104.f;                // weights below e^-104 of the largest count as zero: below what min-p can be, 2^-149, and 2^30 of them below 1e-36
 constexpr int kMaxCtas = 16;                 // (more than eight: a launch that asks for them)
 constexpr int kTable = 256;
 constexpr uint32_t kSmall = 64;              // logits that are compared each with each, at most

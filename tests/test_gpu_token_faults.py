@@ -104,3 +104,15 @@ def test_nuclei_that_end_beside_the_bin_that_rounded_sums_point_to(dtype, edge, 
     w = [math.exp(e / temperature) for e in edge]
     total = 1 + first * w[0] + (classes - first - 1) * w[1]
     agree(z.to(dtype), top_p=float(np.float32((1 + first * w[0] * (1 + past)) / total)), temperature=temperature)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, torch.float16])
+@pytest.mark.parametrize("classes", [1000, 200_001])
+@pytest.mark.parametrize("settings", [dict(), dict(top_k=20), dict(top_k=900), dict(top_p=0.5), dict(temperature=0.5), dict(temperature=2.0, top_p=0.9)], ids=str)
+def test_min_p_far_below_the_largest_weight(dtype, classes, settings):
+    """Classes are kept where their weights are min-p or more, however small both are: down to fp32's least number."""
+    z = torch.full((classes,), -50.0)
+    z[::3], z[1::7], z[5] = -60.0, -103.0, 0.0
+    for min_p in (2.0 ** -149, 1e-44, 1e-38, 1e-25, 1e-21):
+        for u in (0.25, 1.0 - 2.0 ** -24):
+            agree(z.to(dtype), u, min_p=min_p, **settings)
