@@ -716,8 +716,8 @@ class Embedding(_Handle):
             raise SfbError(rc, "sfb_embed_init")
 
     def _drop(self, drop):
-        if drop is not None and not isinstance(drop, Dropout):
-            raise ValueError("drop: a Dropout, or None")
+        if drop is not None and not (isinstance(drop, Dropout) and drop._h):
+            raise ValueError("drop: a Dropout that is not closed, or None")
         return drop._h if drop is not None else None
 
     def sfb_embed_forward(self, ids, X, drop=None, call=0):

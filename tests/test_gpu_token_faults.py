@@ -116,3 +116,14 @@ def test_min_p_far_below_the_largest_weight(dtype, classes, settings):
     for min_p in (2.0 ** -149, 1e-44, 1e-38, 1e-25, 1e-21):
         for u in (0.25, 1.0 - 2.0 ** -24):
             agree(z.to(dtype), u, min_p=min_p, **settings)
+
+
+def test_a_closed_dropout_before_a_lookup_and_before_a_gradient():
+    E, ids = torch.randn(10, 16, device="cuda"), torch.arange(4, dtype=torch.int32, device="cuda")
+    X, dE = torch.full((4, 16), 7.0, device="cuda"), torch.full((10, 16), 7.0, device="cuda")
+    plan, drop = S.Embedding(E, 4), S.Dropout(0.5, torch.zeros(2, dtype=torch.int64, device="cuda"))
+    drop.close()
+    for call in (lambda: plan.sfb_embed_forward(ids, X, drop), lambda: plan.sfb_embed_backward(ids, X, dE, drop)):
+        with pytest.raises(ValueError):
+            call()
+    assert (X == 7).all() and (dE == 7).all()

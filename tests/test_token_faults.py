@@ -1,8 +1,11 @@
 """What once went wrong around lookup, dropout and sampling, as far as it shows without a GPU."""
+import ctypes
 import os
 import re
 
 import pytest
+
+import paper_1409_5705_b200 as S
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_1409_5705_b200", "csrc")
 
@@ -13,3 +16,20 @@ def test_kernels_that_start_early_read_coherently(name):
     holds may be older than its wait, and the compiler may move such a load above it."""
     code = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, name)).read())
     assert not re.search(r"__ldg\s*\(|ld\.global(\.\w+)*\.nc", code)
+
+
+def closed_dropout():
+    """As ``Dropout.close`` leaves one; the library never sees it."""
+    drop = S.Dropout.__new__(S.Dropout)
+    drop._h = ctypes.c_void_p()
+    drop.close()
+    return drop
+
+
+def test_a_closed_dropout_is_not_none():
+    """A handle that is gone may not be taken for no dropout at all."""
+    plan = S.Embedding.__new__(S.Embedding)
+    assert plan._drop(None) is None
+    for bad in (closed_dropout(), 0.1, S.Embedding):
+        with pytest.raises(ValueError):
+            plan._drop(bad)
