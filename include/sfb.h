@@ -432,7 +432,8 @@ typedef struct sfb_embed_config {
   int32_t table_dtype;        /* enum sfb_dtype                                                        */
   int32_t out_dtype;          /* of X and dX                                                           */
   float   scale;
-  int64_t max_ids;            /* of a call, up to 2^26                                                 */
+  int64_t max_ids;            /* of a call, up to 2^26, and ceil(max_ids / 64) * ceil(dim / 8) up to
+                                 2^31 - 257 (65,472 ids of 2^24 columns, 2^26 of 16,376)               */
   void*   stream;             /* cudaStream_t                                                          */
 } sfb_embed_config;
 /* Bytes of device workspace of a handle.  Host-only; no CUDA call. */

@@ -828,6 +828,8 @@ int check(const sfb_embed_config* c) {
   if (!c || c->tokens <= 0 || c->dim <= 0 || c->ldt < 0 || c->max_ids < 0 || !std::isfinite(c->scale)) return SFB_ERR_ARG;
   if (!sfb::is_dtype(c->table_dtype) || !sfb::is_dtype(c->out_dtype)) return SFB_ERR_ARG;
   if (c->tokens > (1ll << 30) || c->dim > (1ll << 24) || c->max_ids > (1ll << 26)) return SFB_ERR_SHAPE;
+  // (a launch's blocks: groups of columns of chunks of 64 samples are numbered in 31 bits)
+  if ((c->max_ids + kPerMost - 1) / kPerMost * groups_of(c->dim) > kBlocksMost - kThreads) return SFB_ERR_SHAPE;
   if ((c->ldt && c->ldt < c->dim) || c->ldt >= (1ll << 32) / static_cast<int64_t>(sfb::size_of(c->table_dtype))) return SFB_ERR_SHAPE;
   return SFB_OK;
 }
@@ -1033,7 +1035,7 @@ extern "C" int sfb_embed_forward(sfb_embed* h, int64_t n, const int32_t* ids_dev
   if (!ids_dev || !X_dev) return SFB_ERR_ARG;
   if (ldx < c.dim) return SFB_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(ids_dev) & 3u) || !sfb::lies_aligned(X_dev, c.out_dtype)) return SFB_ERR_ALIGN;
-  if (n > kBlocksMost / groups_of(c.dim) * kThreads || !fits(n, ldx, c.out_dtype)) return SFB_ERR_SHAPE;
+  if (!fits(n, ldx, c.out_dtype)) return SFB_ERR_SHAPE;
   const OnDevice on(h->device);
   if (on.err != cudaSuccess) return fail(h, on.err);
   const bool drops = drop && drop->drop.threshold > 0;
@@ -1068,8 +1070,6 @@ extern "C" int sfb_embed_backward(sfb_embed* h, int64_t n, const int32_t* ids_de
   if (n > 0 && lddx < c.dim) return SFB_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(ids_dev) & 3u) || !sfb::lies_aligned(dX_dev, c.out_dtype) || !sfb::lies_aligned(dE_dev, SFB_F32)) return SFB_ERR_ALIGN;
   if (n == 0 && add) return SFB_OK;
-  // (groups of chunks are numbered in 31 bits: a million tokens' samples of 16 million columns)
-  if ((n + 63) / 64 * groups_of(c.dim) > kBlocksMost - kThreads) return SFB_ERR_SHAPE;
   const OnDevice on(h->device);
   if (on.err != cudaSuccess) return fail(h, on.err);
   const EmbedLayout l = layout_of(c);

@@ -33,3 +33,12 @@ def test_a_closed_dropout_is_not_none():
     for bad in (closed_dropout(), 0.1, S.Embedding):
         with pytest.raises(ValueError):
             plan._drop(bad)
+
+
+@pytest.mark.parametrize("max_ids,dim,code", [(65_472, 1 << 24, 0), (65_473, 1 << 24, -3), (1 << 26, 16_376, 0), (1 << 26, 16_377, -3), (0, 1 << 24, 0), (1 << 26, 1, 0)])
+def test_what_a_lookup_of_that_size_would_refuse_is_refused_before(max_ids, dim, code):
+    """ceil(max_ids / 64) * ceil(dim / 8) up to 2^31 - 257, as include/sfb.h has it: a handle that there is takes every call of up to max_ids."""
+    cfg, n = S.sfb_embed_config(100, dim, 0, 0, 1, 1.0, max_ids, None), ctypes.c_size_t(0)
+    assert S.lib().sfb_embed_workspace_bytes(ctypes.byref(cfg), ctypes.byref(n)) == code
+    h = ctypes.c_void_p(1)
+    assert code == 0 or (S.lib().sfb_embed_init(ctypes.byref(cfg), 1024, 1024, 1 << 62, ctypes.byref(h)) == code and not h.value)
