@@ -20,7 +20,7 @@
 // Whole numbers come out: a class is right or wrong.  So the weights exp((z - m) / T) are taken in 64 bits (an error of 1e-7 in a sum over
 // 325,000 classes would move one draw in a hundred to the class beside), by a table of 256 powers of two and a polynomial of the third
 // degree (table-driven exponentials: P. T. P. Tang, ACM Trans. Math. Softw. 15, 1989): eight operations of 64 bits, 2e-13.  Sums by key are whole
-// numbers (2^-F of the largest weight), so that their order changes nothing; the others are added in a fixed order.
+// numbers, so that their order changes nothing; the others are added in a fixed order.
 //
 // What bounds it (us, caches cold): a single row is a chain of passes of a few thousand logits a CTA, barriers of the cluster (0.3 each) and code
 // that is met for the first time (325,000 bf16 classes, top-k and top-p: 20, of which the row's bytes would take 0.1).  Many rows with filters: the
@@ -232,6 +232,10 @@ struct Weight {
     return z >= far ? s * e : 0.0;
   }
 };
+
+// 2^n, and the n of the power of two that a positive number is not below, for what is far from the type's ends.
+__device__ __forceinline__ double power_of_two(int n) { return __hiloint2double((1023 + n) << 20, 0); }
+__device__ __forceinline__ int log2_of(double v) { return (__double2hiint(v) >> 20) - 1023; }
 
 __device__ __forceinline__ Weight weight_of(const double* power, float m, float temperature, double per) {
   return isinf(m) ? Weight{power, 0.0, 0.0, m} : Weight{power, m, per, fmaxf(m - kFar * temperature, -kLargest)};
@@ -1067,7 +1071,6 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
       const uint32_t cut_key = last_key, cut_ties = last_ties;       // of top-k; key 0: none
       const double cut_weight = cuts ? weight(value_of<LOW>(cut_key)) : 0.0;
       const float cut_value = cuts ? value_of<LOW>(cut_key) : kNone;
-      const double grain = ldexp(1.0, p.fraction);
       double target = 0.0;
       bool cut_inside = cuts && high_bin == k_bin;
       // A list of n logits that follow others with the sum `above`, behind them what top-k leaves of its last key (where that is in reach):
@@ -1108,15 +1111,18 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
           r = range_of<LOW, kBins>(m, unit, low_bin, high_bin);
         }
       }
-      // Sums by key are of weights as whole numbers: units of 2^-F of the largest weight that the range can have, or finer ones where all weights come to
-      // none (`lift`).  Each is off by half a unit, and equal ones all by the same, so a bin near whose edge the target falls may be the wrong one.
+      // Sums by key are of weights as whole numbers: in units of about 2^-F of the largest weight that the range can have, or finer ones where all weights
+      // come to none.  Each is off by half a unit, and equal ones all by the same, so a bin near whose edge the target falls may be the wrong one.
       // The sums of its own weights in 64 bits say so when it is gone over, and the search goes on beside it, within `bound`, which is sure.
       Range bound = r;
-      double lift = 1.0;
+      int finer = 0;
       if (listed < 0)
       for (bool begins = true;; begins = false) {
         const int shift = shift_of<kBins>(r);
-        const double top_weight = weight(value_of<LOW>(r.high)), unit_of = (top_weight > 0.0 ? grain / top_weight : grain) * lift;
+        // (the largest weight is below 2^(most + 1))
+        const int most = endless ? 0 : max(-160, __double2int_rd((value_of<LOW>(r.high) - weight.m) * weight.per * (1.0 / kTable)));
+        int unit_bits = p.fraction - 1 - most + finer;
+        const double units = power_of_two(unit_bits);
         __syncthreads();
         if (!few_left)
           for (int b = threadIdx.x; b < kBins; b += N) s.mass[b] = 0;
@@ -1138,9 +1144,9 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
               over += w;
             } else if (there && key >= r.low) {
               ++inside;
-              within += w;
+              if (!begins) within += w;
               if (shift == 0) atomicAdd(&s.count[r.high - key], 1u);         // (a bin is one key: its weight comes in below)
-              else add(&s.mass[(r.high - key) >> shift], static_cast<unsigned long long>(__double2ll_rn(w * unit_of)));
+              else add(&s.mass[(r.high - key) >> shift], static_cast<unsigned long long>(__double2ll_rn(w * units)));
             }
           }
         });
@@ -1153,7 +1159,10 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
         row_sync(ctas);
         double sum;                          // of all that top-k leaves but for its last key; then of the range
         gathered(above, sum, inside);
-        if (begins) target = static_cast<double>(top_p) * (sum + (cuts ? cut_ties * cut_weight : 0.0));
+        if (begins) {
+          if (cuts) sum += cut_ties * cut_weight;
+          target = static_cast<double>(top_p) * sum;
+        }
         if (few_left) {
           meet(gather(), true);
           break;
@@ -1166,7 +1175,7 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
             if (before) bound.low = r.high + 1;
             else bound.high = r.low - 1;
             r = bound;
-            lift = 1.0;
+            finer = 0;
             row_sync(ctas);                  // (the sums are read)
             continue;
           }
@@ -1177,45 +1186,40 @@ __global__ void __launch_bounds__(N, (FILTERS ? 1024 : 1536) / N) sample_kernel(
           break;
         }
         unsigned long long some[kEach], mine = 0, mass;
-        double units = unit_of;
-        if (shift == 0) {                    // counts of keys: their weights by 64-bit products, in units of 2^-61 of all of them
+        if (shift == 0) {                    // counts of keys: their weights by 64-bit products, in units of 2^-62 of what holds them all
           uint32_t count[kEach];
           sum_bins(s, s.count, ctas, cta, count);
-          double here[kEach], of_mine = 0.0, of_all;
+          unit_bits = 60 - log2_of(begins ? fmax(sum - above, 1e-12 * sum) : fmax(sum, 1e-60));
 #pragma unroll
           for (int j = 0; j < kEach; ++j) {
             const uint32_t at = threadIdx.x * kEach + j;
-            here[j] = count[j] ? count[j] * weight(value_of<LOW>(r.high - at)) : 0.0;
-            if (cut_inside && r.high - cut_key == at) here[j] += cut_ties * cut_weight;
-            of_mine += here[j];
+            double here = count[j] ? count[j] * weight(value_of<LOW>(r.high - at)) : 0.0;
+            if (cut_inside && r.high - cut_key == at) here += cut_ties * cut_weight;
+            some[j] = __double2ull_rn(here * power_of_two(unit_bits));
           }
-          block_scan(s, of_mine, of_all);
-          units = of_all > 0.0 ? 2305843009213693952.0 / of_all : 1.0;
-#pragma unroll
-          for (int j = 0; j < kEach; ++j) some[j] = __double2ull_rn(here[j] * units);
         } else {
           sum_bins(s, s.mass, ctas, cta, some);
 #pragma unroll
           for (int j = 0; j < kEach; ++j)
-            if (cut_inside && (r.high - cut_key) >> shift == threadIdx.x * kEach + j) some[j] += cut_ties * __double2ull_rn(cut_weight * unit_of);
+            if (cut_inside && (r.high - cut_key) >> shift == threadIdx.x * kEach + j) some[j] += cut_ties * __double2ull_rn(cut_weight * units);
         }
 #pragma unroll
         for (int j = 0; j < kEach; ++j) mine += some[j];
         unsigned long long ahead = block_scan(s, mine, mass);
-        if (mass == 0 && shift > 0 && lift < 1e100) {    // (half a unit each at most: in units of 2^-F of that they come to 2^61 at most)
-          lift *= grain;
+        if (mass == 0 && shift > 0 && finer < 400) {     // (half a unit each at most: in units of 2^-F of that they come to 2^61 at most)
+          finer += p.fraction;
           continue;
         }
         // in whole numbers: what the target leaves for the bins, and at least one and at most what they hold, so that one thread finds it
-        const double left = ceil((target - above) * units);
+        const double left = ceil((target - above) * power_of_two(unit_bits));
         const unsigned long long want = min(left > 1.0 ? __double2ull_rn(left) : 1ull, mass);
         if (mass == 0 && threadIdx.x == 0) s.found[0] = 0, s.found_at = above;       // (no weight in the range)
-        lift = 1.0;
+        finer = 0;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
           if (ahead < want && ahead + some[j] >= want) {
             s.found[0] = threadIdx.x * kEach + j;
-            s.found_at = above + ahead / units;
+            s.found_at = above + ahead * power_of_two(-unit_bits);
           }
           ahead += some[j];
         }
