@@ -464,7 +464,10 @@ int sfb_embed_destroy(sfb_embed* h);
  *  - A logit of -infinity, or one that is not a number, is no class: it is neither kept nor drawn.  A row of such ones has ids = -1,
  *    logp = -infinity, kept = 0.  Where logits are +infinity, these alone have weight, 1 each.  Weights below e^-34 may count as 0: such
  *    classes are kept where the filters say so, but not drawn.
- *  - Weights and their sums are in 64 bits, and the same from call to call; logp is rounded to fp32 at its end.
+ *  - Weights and their sums are in 64 bits, and the same from call to call; logp is rounded to fp32 at its end.  Filters' ends and draws are those of
+ *    exact sums, but where top_p or u falls within 1e-11 of an edge (4e-11 beyond 2^28 classes), or min_p within 1e-12 of itself of a weight.
+ *  - Few rows are drawn from by clusters of up to 16 CTAs, as sfb_embed_backward sorts up to 65,536 samples: a device that cannot place those (a part
+ *    of a chip) answers SFB_ERR_CUDA.
  *  - Z of dtype, any pitch ldz >= classes, aligned to its entries (rows on 16-byte boundaries are the faster ones); the arrays are contiguous.
  *    n = 0 .. max_samples.  Calls on one handle are not re-entrant. */
 typedef struct sfb_sampler sfb_sampler;

@@ -658,8 +658,8 @@ class _Handle:
 
 
 class Dropout(_Handle):
-    """Owns one ``sfb_dropout``: entries dropped with probability ``p``, the others multiplied with 1 / (1 - p), by a counter-based
-    generator whose mask is never stored (include/sfb.h has the formulas).
+    """Owns one ``sfb_dropout``: entries dropped with probability t / 65536, t = round(65536 p), the others multiplied with
+    65536 / (65536 - t), by a counter-based generator whose mask is never stored (include/sfb.h has the formulas).
 
     ``rng``: two int64 on the device, the seed and the offset's base, which the caller moves on from step to step (``rng[1] += 1``,
     in a captured graph too); ``call`` of a call is added to the offset, so that the layers of a step differ.  The same

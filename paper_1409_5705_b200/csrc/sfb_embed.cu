@@ -74,8 +74,10 @@ struct RowsParams {
 
 // Blocks take pieces in turn, the ids of the next one under way while one is copied.
 // 16,384 samples of 2,000 from 325,000 tokens, fp32 to bf16, with dropout: 32 us for 120 MB (19 at the rate of a plain copy); a row that comes up again is
-// read from L2, and it is the loads of 196 MB through it, 32 KB under way an SM, and the generator's instructions (half of all issue slots) that take
-// the time.  One launch's latency for few samples (2.5 us at 7 of 5,000).
+// read from L2, and it is the loads of 196 MB through it, 64 KB under way an SM at most (four blocks with
+// two groups of 32 bytes a thread), and the generator's instructions (half of all issue slots) that take
+// the time; without dropout 28 where that is 37 (calls one by one, caches cold).  Rows that are not on 16-byte boundaries go entry by entry: 95 at 2,001
+// columns without gaps.  One launch's latency for few samples (2.5 us at 7 of 5,000).
 template <typename In, typename Out, bool DROP, int N>
 __global__ void __launch_bounds__(kThreads, N == 1 ? 1 : 4) embed_rows_kernel(const __grid_constant__ RowsParams p) {
   pdl_launch_dependents();
@@ -496,8 +498,8 @@ struct GradientParams {
 };
 
 // us, caches cold: 16,384 samples bf16 of 2,000 with dropout to 50,000 tokens 30 (66 MB of samples), 65,000 of 1,000 added to 325,000 tokens 65 (130 MB, and
-// 167 MB of rows read and written): 16 warps of 64 registers an SM with two samples' loads each are what is under way; more samples ahead took
-// as many warps away as they brought loads.
+// 167 MB of rows read and written): what is under way are two samples' loads of each of 32 warps an SM, as many as their 64 registers leave room for (22 to
+// 26 of them at work on average); more samples ahead took as many warps away as they brought loads.
 constexpr int kAhead = 2;          // samples under way a thread
 
 template <typename T, bool DROP, bool ADD>
@@ -894,7 +896,8 @@ cudaError_t sort_samples(const EmbedLayout& l, char* ws, const sfb_embed_config&
     const int per = few || n > 2 * kSortThreads * kSortCtas ? 4 : n > kSortThreads * kSortCtas ? 2 : 1;
     int ctas = 1;
     while (static_cast<int64_t>(ctas) * kSortThreads * per < n) ctas *= 2;
-    int zeros = 0;                     // CTAs that zero, in clusters like the one that sorts: as many as the chip has room for beside it
+    // CTAs that zero, in clusters like the one that sorts: as many as a chip of 148 SMs has room for beside it
+    int zeros = 0;
     if (zero) {
       const int room = ctas <= 2 ? 148 : ctas == 4 ? 132 : ctas == 8 ? 120 : 112;
       zeros = static_cast<int>(std::min<int64_t>(room - ctas, (c.tokens + 31) / 32));

@@ -24,7 +24,7 @@
 //
 // What bounds it (us, caches cold): a single row is a chain of passes of a few thousand logits a CTA, barriers of the cluster (0.3 each) and code
 // that is met for the first time (325,000 bf16 classes, top-k and top-p: 20, of which the row's bytes would take 0.1).  Many rows with filters: the
-// instructions of a look at each logit, some 10 to 20 for each that may count, 18 for its weight (64 rows of 325,000, mixed settings: 105 to 116; bytes 7;
+// instructions of a look at each logit, some 10 to 20 for each that may count, 18 for its weight (64 rows of 325,000, mixed settings: 98 to 116; bytes 7;
 // 37 rows of 99,999 fp32 at temperatures that keep most classes: 60).  Without filters: 64-bit arithmetic, 8 operations at 0.22 cycles a weight
 // and SM (2,048 rows of 10,000 fp32: 47 to 51; 24 of them the weights, bytes 13).
 #include <algorithm>
