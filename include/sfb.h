@@ -400,6 +400,7 @@ int sfb_adapter_destroy(sfb_adapters* h);
  *
  *  - E is fp32, bf16 or fp16, X and dX of another of these or the same; dE fp32.  Any pitch >= dim, pointers aligned to their entries
  *    (rows that all start on 16-byte boundaries are the faster ones).  Products are rounded once, to X's type; sums are fp32.
+ *    scale, alpha and the dropout's 65536 / (65536 - t) are multiplied to one fp32 factor first: where that is no finite number the call is SFB_ERR_ARG.
  *  - dE is written whole, zeros for tokens without a sample; or, with add = 1, the sums are added to the rows of the tokens that
  *    some sample names, and the other rows are not touched: with alpha = -eta and dE = the fp32 table itself that is its step.
  *  - The samples are taken in the order of their tokens, those of a token in their own order: results are the same bits from call to

@@ -1039,9 +1039,11 @@ extern "C" int sfb_embed_forward(sfb_embed* h, int64_t n, const int32_t* ids_dev
   if (ldx < c.dim) return SFB_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(ids_dev) & 3u) || !sfb::lies_aligned(X_dev, c.out_dtype)) return SFB_ERR_ALIGN;
   if (!fits(n, ldx, c.out_dtype)) return SFB_ERR_SHAPE;
+  const bool drops = drop && drop->drop.threshold > 0;
+  const float factor = c.scale * (drops ? drop->drop.factor : 1.f);
+  if (!std::isfinite(factor)) return SFB_ERR_ARG;
   const OnDevice on(h->device);
   if (on.err != cudaSuccess) return fail(h, on.err);
-  const bool drops = drop && drop->drop.threshold > 0;
   RowsParams p{};
   p.table = h->table;
   p.out = X_dev;
@@ -1050,7 +1052,7 @@ extern "C" int sfb_embed_forward(sfb_embed* h, int64_t n, const int32_t* ids_dev
   p.tokens = static_cast<uint32_t>(c.tokens);
   p.pitch_in = static_cast<uint32_t>(c.ldt * static_cast<int64_t>(sfb::size_of(c.table_dtype)));
   p.pitch_out = static_cast<uint32_t>(ldx * static_cast<int64_t>(sfb::size_of(c.out_dtype)));
-  p.factor = c.scale * (drops ? drop->drop.factor : 1.f);
+  p.factor = factor;
   p.wide_in = sfb::lies_wide(h->table, c.ldt, c.table_dtype);
   p.wide_out = sfb::lies_wide(X_dev, ldx, c.out_dtype);
   p.status = reinterpret_cast<uint32_t*>(h->ws);
@@ -1072,11 +1074,13 @@ extern "C" int sfb_embed_backward(sfb_embed* h, int64_t n, const int32_t* ids_de
   if (n > 0 && (!ids_dev || !dX_dev)) return SFB_ERR_ARG;
   if (n > 0 && lddx < c.dim) return SFB_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(ids_dev) & 3u) || !sfb::lies_aligned(dX_dev, c.out_dtype) || !sfb::lies_aligned(dE_dev, SFB_F32)) return SFB_ERR_ALIGN;
+  const bool drops = drop && drop->drop.threshold > 0;
+  const float factor = c.scale * alpha * (drops ? drop->drop.factor : 1.f);
+  if (!std::isfinite(factor)) return SFB_ERR_ARG;
   if (n == 0 && add) return SFB_OK;
   const OnDevice on(h->device);
   if (on.err != cudaSuccess) return fail(h, on.err);
   const EmbedLayout l = layout_of(c);
-  const bool drops = drop && drop->drop.threshold > 0;
   const cudaStream_t s = static_cast<cudaStream_t>(c.stream);
   GradientParams p{};
   p.n = n;
@@ -1089,7 +1093,7 @@ extern "C" int sfb_embed_backward(sfb_embed* h, int64_t n, const int32_t* ids_de
   p.wide_out = sfb::lies_wide(dE_dev, ldde, SFB_F32);
   p.table = dE_dev;
   p.lddt = ldde;
-  p.factor = c.scale * alpha * (drops ? drop->drop.factor : 1.f);
+  p.factor = factor;
   p.add = add != 0;
   if (drops) {
     p.drop = drop->drop;

@@ -127,3 +127,17 @@ def test_a_closed_dropout_before_a_lookup_and_before_a_gradient():
         with pytest.raises(ValueError):
             call()
     assert (X == 7).all() and (dE == 7).all()
+
+
+def test_factors_that_are_no_number():
+    """scale and alpha are finite, their product is not: zeros of dX would become NaN."""
+    E, ids = torch.ones(10, 16, device="cuda"), torch.arange(4, dtype=torch.int32, device="cuda")
+    X, dE, rng = torch.zeros(4, 16, device="cuda"), torch.full((10, 16), 7.0, device="cuda"), torch.zeros(2, dtype=torch.int64, device="cuda")
+    plan = S.Embedding(E, 4, scale=1e35)
+    for call in (lambda: plan.sfb_embed_backward(ids, X, dE, alpha=1e5), lambda: plan.sfb_embed_backward(ids, X, dE, alpha=-1e5, add=True),
+                 lambda: plan.sfb_embed_forward(ids, X, S.Dropout(0.9999, rng))):
+        with pytest.raises(S.SfbError):
+            call()
+    assert (X == 0).all() and (dE == 7).all()
+    plan.sfb_embed_backward(ids, X, dE, S.Dropout(1.0, rng), alpha=1.0)
+    assert (dE == 0).all()
